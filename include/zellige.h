@@ -17,7 +17,8 @@
  *     offsets in their descriptor and must lie at or after cu_seqlens[n_whole].
  *   - Tensors are [tokens, n_heads, head_dim], contiguous, bf16, base 16-byte aligned.
  *     LSE is [n_heads, total_q] fp32: natural log of the sum of exp(scale * q.k).
- *   - Attention is bidirectional: no mask, bias or dropout.  head_dim is 64 or 128.
+ *   - Attention is bidirectional, without mask, bias or dropout, except in the scored entry points
+ *     (zl_scored_attn_*).  head_dim is 64 or 128.
  *   - All tensor arguments are DEVICE pointers unless marked host.  The caller owns every
  *     tensor, the workspace and the stream; the library allocates only the small tables
  *     inside a zl_tasks handle.
@@ -62,6 +63,12 @@ typedef enum {
 typedef struct {
     int32_t q_off, q_len, kv_off, kv_len, seq_id;
 } zl_shard_desc;
+
+/* Where a shard's chunks lie in their sequence (zl_set_positions): positions of the first query and the first
+ * key row, and the number of leading keys of the sequence that every query sees. */
+typedef struct {
+    int32_t q_pos, kv_pos, prefix;
+} zl_shard_pos;
 
 typedef struct zl_tasks zl_tasks; /* opaque, immutable after zl_build_tasks */
 
@@ -152,6 +159,27 @@ zl_status zl_build_tasks_heads(const zl_whole_desc* whole, int32_t n_whole,
                                const zl_shard_desc* shards, const zl_head_range* shard_heads, int32_t n_shards,
                                int32_t total_q, int32_t total_kv, int32_t n_heads, int32_t head_dim,
                                uint32_t flags, void* stream, zl_tasks** out);
+
+/* zl_build_tasks_prefix -- a batch of sequences that share one long prefix of keys (many continuations of one
+ * context: rollouts, candidates, prompts behind one system text), with the prefix part computed for the queries of all
+ * sequences together instead of once per sequence.
+ *
+ *   cu_q, cu_kv  host, n_seqs+1 entries each, starting at 0, non-decreasing; may be NULL if n_seqs = 0.  Sequence i
+ *                owns query rows [cu_q[i], cu_q[i+1]) and, beside the prefix, key rows
+ *                [prefix_len + cu_kv[i], prefix_len + cu_kv[i+1]); its queries see the prefix rows [0, prefix_len)
+ *                and its own keys.  Any of these lengths may be zero: a row without any key gets O = 0, LSE = -inf.
+ * The handle is used like one of shards: zl_coalesced_attn_fwd, then zl_lse_merge (every row is a partial result
+ * until the merge; o_partial / lse_partial as zl_tasks_info says), then any zl_coalesced_attn_bwd form.  dK and dV of the prefix are
+ * summed over all sequences; own key rows of a sequence without queries are covered by no task and left untouched.
+ * The prefix is cut into chunks along the keys so that few query rows (one token per sequence) still occupy the GPU.
+ * Shard numbers (zl_tasks_get_partial_slot, zl_set_*_phases, zl_set_positions) are sequence numbers and mean the
+ * part over the sequence's own keys; the chunks of the prefix run in launch phase 0.
+ * Scores: caps and, after zl_set_positions, the prefix mask work (the mask applies among a sequence's own rows, the
+ * shared prefix is seen whole); scores that depend on the distance are refused (ZL_ERR_UNSUPPORTED), because the
+ * distance of a prefix key differs from sequence to sequence. */
+zl_status zl_build_tasks_prefix(const int32_t* cu_q, const int32_t* cu_kv, int32_t n_seqs, int32_t prefix_len,
+                                int32_t total_q, int32_t total_kv, int32_t n_heads, int32_t head_dim,
+                                void* stream, zl_tasks** out);
 
 zl_status zl_tasks_get_info(const zl_tasks* tasks, zl_tasks_info* info);
 
@@ -319,6 +347,73 @@ zl_status zl_phase_info(const zl_tasks* tasks, int32_t* n_fwd_phases, int32_t* n
 zl_status zl_coalesced_attn_bwd_noalloc(const zl_tasks* tasks, const void* q, const void* k, const void* v,
                                         const void* o, const float* lse, const void* d_o, float scale,
                                         void* dq, void* dk, void* dv, void* stream);
+
+/* Scored attention -- attention whose scores are more than scale * q.k.
+ *
+ * For query i and key j of one task and head h, at positions pos(i), pos(j) of their sequence:
+ *     s_ij = C(scale * q_i.k_j) - slopes[h] * |pos(j) - pos(i)|
+ *            + bucket_bias[bucket_of[clamp(pos(j) - pos(i), -max_distance, max_distance) + max_distance]][h]
+ *     C(x) = cap * tanh(x / cap) if cap > 0, else x
+ *     pair visible if !masked, or pos(j) < prefix, or pos(j) <= pos(i)
+ * (pairs of different sequences are never formed: the packed batch is its own document mask), then
+ *     O = softmax(s) V,   LSE = log sum exp s   over the visible pairs; a row that sees no key gets O = 0, LSE = -inf.
+ *
+ *   cap           0 = no cap; otherwise finite and > 0.
+ *   slopes        device, [n_heads] fp32, finite, or NULL: a linear bias by distance.
+ *   bucket_bias   device, [n_buckets, n_heads] fp32, or NULL: a learned bias by buckets of the signed distance.  An
+ *                 entry of -1e30 or less (-inf, the lowest finite value of a type) removes its pairs like a mask; other entries are finite.
+ *   bucket_of     device, [2 * max_distance + 1] int32: the bucket of every distance from -max_distance to
+ *                 max_distance; farther pairs use the bucket of the clamped distance.  A number outside
+ *                 [0, n_buckets) means no bias.
+ *   n_buckets     1 .. ZL_MAX_BUCKETS (ZL_ERR_UNSUPPORTED above) with buckets, else 0.
+ *   max_distance  0 .. 2^24.
+ *   masked        0 or 1.  1 needs zl_set_positions.
+ * Slopes and biases are read when the kernels run, so a captured graph sees their current values. */
+#define ZL_MAX_BUCKETS 64
+typedef struct {
+    float cap;
+    const float* slopes;
+    const float* bucket_bias;
+    const int32_t* bucket_of;
+    int32_t n_buckets;
+    int32_t max_distance;
+    int32_t masked;
+} zl_score;
+
+/* zl_set_positions -- where the tasks of a handle lie in their sequences, and how many leading keys every query sees.
+ *   whole_prefix  host, one entry per whole sequence (NULL = 0 for all): its rows have positions 0, 1, ...; keys at
+ *                 positions before the entry are visible to all of its queries, 0 is plain causal order.
+ *   shard_pos     host, one entry per shard (may be NULL without shards): positions of the shard's first query and key row,
+ *                 and the prefix of its sequence.  All >= 0, q_pos + q_len and kv_pos + kv_len at most 2^31 - 513.
+ * Scores by distance need this call on handles with shards, masks on all handles.  The work lists for masked calls are
+ * ordered by what the mask leaves of each item.  Synchronises `stream`; must not run while a launch of the
+ * handle is in flight; the other entry points are unaffected. */
+zl_status zl_set_positions(zl_tasks* tasks, const int32_t* whole_prefix, const zl_shard_pos* shard_pos, void* stream);
+
+/* zl_scored_attn_fwd / _fwd_packed -- zl_coalesced_attn_fwd / _fwd_packed with scores as above; shard results are partial
+ * and are joined by zl_lse_merge.  `score` is read during the call.  A query chunk whose keys all come later
+ * gets an empty partial (O = 0, LSE = -inf). */
+zl_status zl_scored_attn_fwd(const zl_tasks* tasks, const zl_score* score, const void* q, const void* k, const void* v,
+                             float scale, void* o, float* lse, float* o_partial, float* lse_partial, void* stream);
+zl_status zl_scored_attn_fwd_packed(const zl_tasks* tasks, const zl_score* score, const void* qkv, float scale,
+                                    void* o, float* lse, float* o_partial, float* lse_partial, void* stream);
+
+/* zl_scored_attn_bwd / _bwd_packed -- zl_coalesced_attn_bwd / _bwd_packed with scores as above.  With P = exp(s - LSE) and
+ * G = P o (dO V^T - D):
+ *     dV = P^T dO,  dS = G C'(scale * q.k),  dQ = scale * dS K,  dK = scale * dS^T Q,  C'(x) = 1 - tanh(x / cap)^2 or 1,
+ *     d_bucket_bias[b][h] = sum of G over the visible pairs of head h in bucket b (over all tasks of the handle).
+ *   d_bucket_bias  device, [n_buckets, n_heads] fp32, overwritten; NULL = not wanted (must be NULL without buckets).
+ *                  Its sums run in a fixed order: bit-identical from run to run.  (Slopes get no gradient.)
+ *   workspace      at least zl_scored_workspace_bytes, 256-byte aligned. */
+zl_status zl_scored_attn_bwd(const zl_tasks* tasks, const zl_score* score, const void* q, const void* k, const void* v,
+                             const void* o, const float* lse, const void* d_o, float scale,
+                             void* dq, void* dk, void* dv, float* d_bucket_bias,
+                             void* workspace, size_t workspace_bytes, void* stream);
+zl_status zl_scored_attn_bwd_packed(const zl_tasks* tasks, const zl_score* score, const void* qkv, const void* o,
+                                    const float* lse, const void* d_o, float scale, void* dqkv, float* d_bucket_bias,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+/* Workspace of zl_scored_attn_bwd for this handle and score (its cap and its buckets count, not its pointers' contents). */
+zl_status zl_scored_workspace_bytes(const zl_tasks* tasks, const zl_score* score, size_t* bytes);
 
 /* Synchronises the handle's device and reads the device status word written by the
  * kernels: code is ZL_OK or ZL_ERR_TIMEOUT, `where` identifies the wait that expired

@@ -12,6 +12,8 @@ _BINDING_NAMES = ("ZlError", "TaskHandle", "ShardDesc", "WholeDesc", "HeadRange"
                   "build_tasks_heads", "coalesced_attn_fwd", "lse_merge", "coalesced_attn_bwd",
                   "coalesced_attn_bwd_noalloc", "coalesced_attn_fwd_packed", "coalesced_attn_bwd_packed",
                   "coalesced_attn_fwd_phase", "coalesced_attn_bwd_phase", "MAX_PHASES",
+                  "build_tasks_prefix", "Score", "scored_attn_fwd", "scored_attn_fwd_packed", "scored_attn_bwd",
+                  "scored_attn_bwd_packed", "relative_position_buckets", "MAX_BUCKETS",
                   "NOALLOC_SCRATCH_BYTES", "BUILD_FUSE_LOCAL_CHUNKS", "launch_count", "library_path", "STATUS_NAMES")
 
 

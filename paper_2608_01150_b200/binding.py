@@ -41,6 +41,16 @@ class HeadRange(ctypes.Structure):
     _fields_ = [("head_begin", ctypes.c_int32), ("head_count", ctypes.c_int32)]
 
 
+class ShardPos(ctypes.Structure):
+    _fields_ = [("q_pos", ctypes.c_int32), ("kv_pos", ctypes.c_int32), ("prefix", ctypes.c_int32)]
+
+
+class ScoreDesc(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("bucket_bias", ctypes.c_void_p),
+                ("bucket_of", ctypes.c_void_p), ("n_buckets", ctypes.c_int32), ("max_distance", ctypes.c_int32),
+                ("masked", ctypes.c_int32)]
+
+
 class TasksInfo(ctypes.Structure):
     _fields_ = [("n_tasks", ctypes.c_int32), ("n_merge_groups", ctypes.c_int32),
                 ("n_kv_groups", ctypes.c_int32), ("n_fwd_items", ctypes.c_int32),
@@ -66,6 +76,8 @@ def _load():
     lib.zl_build_tasks_ex.argtypes = [vp, i32, vp, i32, i32, i32, i32, i32, ctypes.c_uint32, vp, ctypes.POINTER(vp)]
     lib.zl_build_tasks_heads.restype = ctypes.c_int
     lib.zl_build_tasks_heads.argtypes = [vp, i32, vp, vp, i32, i32, i32, i32, i32, ctypes.c_uint32, vp, ctypes.POINTER(vp)]
+    lib.zl_build_tasks_prefix.restype = ctypes.c_int
+    lib.zl_build_tasks_prefix.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32, vp, ctypes.POINTER(vp)]
     lib.zl_tasks_get_info.restype = ctypes.c_int
     lib.zl_tasks_get_info.argtypes = [vp, ctypes.POINTER(TasksInfo)]
     lib.zl_tasks_get_partial_slot.restype = ctypes.c_int
@@ -100,6 +112,20 @@ def _load():
     lib.zl_set_sm_margin.argtypes = [vp, i32]
     lib.zl_coalesced_attn_bwd_noalloc.restype = ctypes.c_int
     lib.zl_coalesced_attn_bwd_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp]
+    sd = ctypes.POINTER(ScoreDesc)
+    lib.zl_set_positions.restype = ctypes.c_int
+    lib.zl_set_positions.argtypes = [vp, vp, vp, vp]
+    lib.zl_scored_attn_fwd.restype = ctypes.c_int
+    lib.zl_scored_attn_fwd.argtypes = [vp, sd, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
+    lib.zl_scored_attn_fwd_packed.restype = ctypes.c_int
+    lib.zl_scored_attn_fwd_packed.argtypes = [vp, sd, vp, ctypes.c_float, vp, vp, vp, vp, vp]
+    lib.zl_scored_attn_bwd.restype = ctypes.c_int
+    lib.zl_scored_attn_bwd.argtypes = [vp, sd, vp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp,
+                                       ctypes.c_size_t, vp]
+    lib.zl_scored_attn_bwd_packed.restype = ctypes.c_int
+    lib.zl_scored_attn_bwd_packed.argtypes = [vp, sd, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.zl_scored_workspace_bytes.restype = ctypes.c_int
+    lib.zl_scored_workspace_bytes.argtypes = [vp, sd, ctypes.POINTER(ctypes.c_size_t)]
     lib.zl_last_device_status.restype = ctypes.c_int
     lib.zl_last_device_status.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32)]
     lib.zl_set_kernel_timing.restype = ctypes.c_int
@@ -151,10 +177,11 @@ def _ptr(t) -> Optional[int]:
 class TaskHandle:
     """Owns a ``zl_tasks*``.  Built once per placement, reused for every layer and step."""
 
-    def __init__(self, ptr: int, n_heads: int, head_dim: int, total_q: int, total_kv: int, n_shards: int):
+    def __init__(self, ptr: int, n_heads: int, head_dim: int, total_q: int, total_kv: int, n_shards: int,
+                 n_whole: int = 0):
         self._ptr = ctypes.c_void_p(ptr)
         self.n_heads, self.head_dim, self.total_q, self.total_kv = n_heads, head_dim, total_q, total_kv
-        self.n_shards = n_shards
+        self.n_shards, self.n_whole = n_shards, n_whole
         info = TasksInfo()
         _check(_lib.zl_tasks_get_info(self._ptr, ctypes.byref(info)), "zl_tasks_get_info")
         self.info = info
@@ -220,6 +247,24 @@ class TaskHandle:
         b, bp = self._phase_array(shard_phase)
         _check(_lib.zl_set_bwd_phases(self._ptr, ap, bp, n_phases, _stream_ptr(stream)), "zl_set_bwd_phases")
 
+    def set_positions(self, whole_prefix=None, shard_pos=None, stream=None):
+        """zl_set_positions: visible prefix per whole sequence (None = 0), (q_pos, kv_pos, prefix) per shard."""
+        if whole_prefix is not None and len(whole_prefix) != self.n_whole:
+            raise ZlError(1, f"set_positions: {self.n_whole} whole sequences, {len(whole_prefix)} prefixes")
+        if shard_pos is not None and len(shard_pos) != self.n_shards:
+            raise ZlError(1, f"set_positions: {self.n_shards} shards, {len(shard_pos)} positions")
+        a, ap = self._phase_array(whole_prefix)
+        b = (ShardPos * max(1, self.n_shards))(*[ShardPos(*[int(v) for v in s]) for s in shard_pos or ()])
+        bp = ctypes.cast(b, ctypes.c_void_p) if shard_pos is not None else None
+        _check(_lib.zl_set_positions(self._ptr, ap, bp, _stream_ptr(stream)), "zl_set_positions")
+
+    def scored_workspace_bytes(self, score: "Score") -> int:
+        """zl_scored_workspace_bytes: workspace of scored_attn_bwd with this score."""
+        n = ctypes.c_size_t()
+        _check(_lib.zl_scored_workspace_bytes(self._ptr, ctypes.byref(score.desc), ctypes.byref(n)),
+               "zl_scored_workspace_bytes")
+        return int(n.value)
+
     def phase_info(self):
         """zl_phase_info: (forward items per phase, backward items per phase)."""
         nf, nb = ctypes.c_int32(0), ctypes.c_int32(0)
@@ -272,7 +317,7 @@ def build_tasks(cu_seqlens: Sequence[int], shards: Sequence[Sequence[int]], tota
         st = _lib.zl_build_tasks(cu_p, n_whole, sh_p, len(shards), total_q, total_kv, n_heads, head_dim,
                                  _stream_ptr(stream), ctypes.byref(out))
     _check(st, "zl_build_tasks")
-    return TaskHandle(out.value, n_heads, head_dim, total_q, total_kv, len(shards))
+    return TaskHandle(out.value, n_heads, head_dim, total_q, total_kv, len(shards), n_whole)
 
 
 def build_tasks_heads(whole: Sequence[Sequence[int]], shards: Sequence[Sequence[int]],
@@ -294,7 +339,23 @@ def build_tasks_heads(whole: Sequence[Sequence[int]], shards: Sequence[Sequence[
                                    len(shards), total_q, total_kv, n_heads, head_dim, ctypes.c_uint32(flags),
                                    _stream_ptr(stream), ctypes.byref(out))
     _check(st, "zl_build_tasks_heads")
-    return TaskHandle(out.value, n_heads, head_dim, total_q, total_kv, len(shards))
+    return TaskHandle(out.value, n_heads, head_dim, total_q, total_kv, len(shards), len(whole))
+
+
+def build_tasks_prefix(cu_q: Sequence[int], cu_kv: Sequence[int], prefix_len: int, total_q: int, total_kv: int,
+                       n_heads: int, head_dim: int, stream=None) -> TaskHandle:
+    """zl_build_tasks_prefix: sequence i owns query rows [cu_q[i], cu_q[i+1]) and, behind the shared prefix rows
+    [0, prefix_len), key rows prefix_len + [cu_kv[i], cu_kv[i+1])."""
+    n = max(0, len(cu_q) - 1)
+    if max(0, len(cu_kv) - 1) != n:
+        raise ZlError(1, f"build_tasks_prefix: {n} query ranges, {max(0, len(cu_kv) - 1)} key ranges")
+    a = (ctypes.c_int32 * max(1, len(cu_q)))(*[int(c) for c in cu_q])
+    b = (ctypes.c_int32 * max(1, len(cu_kv)))(*[int(c) for c in cu_kv])
+    out = ctypes.c_void_p()
+    _check(_lib.zl_build_tasks_prefix(ctypes.cast(a, ctypes.c_void_p), ctypes.cast(b, ctypes.c_void_p), n, prefix_len,
+                                      total_q, total_kv, n_heads, head_dim, _stream_ptr(stream), ctypes.byref(out)),
+           "zl_build_tasks_prefix")
+    return TaskHandle(out.value, n_heads, head_dim, total_q, total_kv, n)
 
 
 def coalesced_attn_fwd(tasks: TaskHandle, q, k, v, scale: float, o, lse, o_partial=None, lse_partial=None,
@@ -358,6 +419,126 @@ def coalesced_attn_bwd_packed(tasks: TaskHandle, qkv, o, lse, d_o, scale: float,
                                              ctypes.c_float(scale), _ptr(dqkv), _ptr(workspace),
                                              ctypes.c_size_t(workspace_bytes), _stream_ptr(stream)),
            "zl_coalesced_attn_bwd_packed")
+
+
+MAX_BUCKETS = 64  # ZL_MAX_BUCKETS
+
+
+class Score:
+    """zl_score: scores beyond ``scale * q.k``.
+
+    cap          0 = none, else scores become ``cap * tanh(scale * q.k / cap)``
+    slopes       fp32 [n_heads]: ``- slope * |distance|``
+    bucket_bias  fp32 [n_buckets, n_heads]: learned bias, with
+    bucket_of    int32 [2 * max_distance + 1]: the bucket of every distance key - query from -max_distance on
+                 (see :func:`relative_position_buckets`)
+    masked       prefix mask of ``TaskHandle.set_positions``
+
+    Holds references to its tensors; their values are read when a kernel runs.
+    """
+
+    def __init__(self, cap: float = 0.0, slopes=None, bucket_bias=None, bucket_of=None, masked: bool = False):
+        import torch
+        for name, t, dtype, dims in (("slopes", slopes, torch.float32, 1), ("bucket_bias", bucket_bias, torch.float32, 2),
+                                     ("bucket_of", bucket_of, torch.int32, 1)):
+            if t is not None and (t.dtype != dtype or t.dim() != dims or not t.is_contiguous()):
+                raise ZlError(1, f"Score: {name} must be a contiguous {dtype} tensor of {dims} dimension(s)")
+        if (bucket_bias is None) != (bucket_of is None):
+            raise ZlError(1, "Score: bucket_bias and bucket_of come together")
+        if bucket_of is not None and bucket_of.numel() % 2 == 0:
+            raise ZlError(1, "Score: bucket_of has an entry for every distance from -max_distance to max_distance")
+        self.cap, self.slopes, self.bucket_bias, self.bucket_of, self.masked = cap, slopes, bucket_bias, bucket_of, masked
+        self.desc = ScoreDesc(cap, _ptr(slopes), _ptr(bucket_bias), _ptr(bucket_of),
+                              0 if bucket_bias is None else bucket_bias.shape[0],
+                              0 if bucket_of is None else bucket_of.numel() // 2, 1 if masked else 0)
+
+    def check_heads(self, tasks: TaskHandle):
+        for name, t in (("slopes", self.slopes), ("bucket_bias", self.bucket_bias)):
+            if t is not None and t.shape[-1] != tasks.n_heads:
+                raise ZlError(1, f"Score: {name} has {t.shape[-1]} heads, the handle {tasks.n_heads}")
+
+
+def relative_position_buckets(n_buckets: int, max_distance: int, bidirectional: bool = True) -> List[int]:
+    """Bucket of every distance key - query from -max_distance to max_distance, for ``Score(bucket_of=...)``.
+
+    Half of a side's buckets hold one distance each, the rest grow by a constant factor until max_distance, from which on
+    the last bucket holds everything: with m buckets of a side, e = m // 2 exact ones and a = |distance| >= e,
+    bucket = e + floor((m - e) * ln(a / e) / ln(max_distance / e)), at most m - 1.  Bidirectional: keys after the
+    query use the second half of the buckets; otherwise they share bucket 0 with distance 0 (a mask hides them).
+    The borders are compared as whole numbers, so a distance that lies on one is never rounded to the wrong side."""
+    side = n_buckets // 2 if bidirectional else n_buckets
+    exact = side // 2
+    if exact < 1 or max_distance <= exact:
+        raise ZlError(1, "relative_position_buckets: needs max_distance beyond the exact buckets, at least "
+                         f"{4 if bidirectional else 2} buckets")
+
+    def of(a: int) -> int:
+        if a < exact:
+            return a
+        steps = side - exact
+        k = 0  # largest k with exact * (max_distance / exact)^(k / steps) <= a
+        while k < steps - 1 and max_distance ** (k + 1) * exact ** (steps - k - 1) <= a ** steps:
+            k += 1
+        return exact + k
+
+    out = []
+    for d in range(-max_distance, max_distance + 1):
+        if bidirectional:
+            out.append(of(abs(d)) + (side if d > 0 else 0))
+        else:
+            out.append(of(max(0, -d)))
+    return out
+
+
+def scored_attn_fwd(tasks: TaskHandle, score: Score, q, k, v, scale: float, o, lse, o_partial=None, lse_partial=None,
+                    stream=None):
+    """zl_scored_attn_fwd: coalesced_attn_fwd with capped, biased or masked scores."""
+    score.check_heads(tasks)
+    _check(_lib.zl_scored_attn_fwd(tasks.ptr, ctypes.byref(score.desc), _ptr(q), _ptr(k), _ptr(v), ctypes.c_float(scale),
+                                   _ptr(o), _ptr(lse), _ptr(o_partial), _ptr(lse_partial), _stream_ptr(stream)),
+           "zl_scored_attn_fwd")
+
+
+def scored_attn_fwd_packed(tasks: TaskHandle, score: Score, qkv, scale: float, o, lse, o_partial=None, lse_partial=None,
+                           stream=None):
+    """zl_scored_attn_fwd_packed: qkv is [T, 3, H, d] bf16."""
+    score.check_heads(tasks)
+    _check(_lib.zl_scored_attn_fwd_packed(tasks.ptr, ctypes.byref(score.desc), _ptr(qkv), ctypes.c_float(scale), _ptr(o),
+                                          _ptr(lse), _ptr(o_partial), _ptr(lse_partial), _stream_ptr(stream)),
+           "zl_scored_attn_fwd_packed")
+
+
+def _check_table(score: Score, d_bucket_bias):
+    t = score.bucket_bias
+    if d_bucket_bias is not None and t is not None and not isinstance(d_bucket_bias, int):
+        if d_bucket_bias.shape != t.shape or d_bucket_bias.dtype != t.dtype or not d_bucket_bias.is_contiguous():
+            raise ZlError(1, "d_bucket_bias must be contiguous and of bucket_bias' shape and type")
+
+
+def scored_attn_bwd(tasks: TaskHandle, score: Score, q, k, v, o, lse, d_o, scale: float, dq, dk, dv, d_bucket_bias,
+                    workspace, workspace_bytes: Optional[int] = None, stream=None):
+    """zl_scored_attn_bwd.  d_bucket_bias: fp32 [n_buckets, n_heads] or None."""
+    score.check_heads(tasks)
+    _check_table(score, d_bucket_bias)
+    if workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
+    _check(_lib.zl_scored_attn_bwd(tasks.ptr, ctypes.byref(score.desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
+                                   _ptr(d_o), ctypes.c_float(scale), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_bucket_bias),
+                                   _ptr(workspace), ctypes.c_size_t(workspace_bytes), _stream_ptr(stream)),
+           "zl_scored_attn_bwd")
+
+
+def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, scale: float, dqkv, d_bucket_bias,
+                           workspace, workspace_bytes: Optional[int] = None, stream=None):
+    """zl_scored_attn_bwd_packed: reads qkv [T, 3, H, d], writes dqkv [T, 3, H, d]."""
+    score.check_heads(tasks)
+    _check_table(score, d_bucket_bias)
+    if workspace_bytes is None:
+        workspace_bytes = workspace.numel() * workspace.element_size()
+    _check(_lib.zl_scored_attn_bwd_packed(tasks.ptr, ctypes.byref(score.desc), _ptr(qkv), _ptr(o), _ptr(lse), _ptr(d_o),
+                                          ctypes.c_float(scale), _ptr(dqkv), _ptr(d_bucket_bias), _ptr(workspace),
+                                          ctypes.c_size_t(workspace_bytes), _stream_ptr(stream)),
+           "zl_scored_attn_bwd_packed")
 
 
 NOALLOC_SCRATCH_BYTES = 64 * 1024 * 1024

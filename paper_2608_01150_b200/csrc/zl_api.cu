@@ -33,6 +33,10 @@ struct zl_tasks {
     KvGroup* d_kv_groups = nullptr;
     int32_t* d_kv_group_tasks = nullptr;
     int32_t* d_status = nullptr;
+    uint8_t* d_positions = nullptr;  // zl_set_positions: one allocation for the three tables below
+    TaskPos* d_task_pos = nullptr;
+    WorkItem* d_fwd_items_masked = nullptr;
+    WorkItem* d_bwd_items_masked = nullptr;
     // optional per-kernel event timing (measurement only)
     mutable bool timing = false;
     mutable std::vector<cudaEvent_t> ev_start[ZL_K_COUNT], ev_stop[ZL_K_COUNT];
@@ -150,6 +154,81 @@ size_t place(size_t& off, size_t count) {
     return at;
 }
 
+zl_status upload_items(const zl_tasks* t, WorkItem* dst, const std::vector<WorkItem>& items, cudaStream_t cs) {
+    if (t->device < 0 || items.empty()) return ZL_OK;
+    if (cudaMemcpyAsync(dst, items.data(), items.size() * sizeof(WorkItem), cudaMemcpyHostToDevice, cs) != cudaSuccess ||
+        cudaStreamSynchronize(cs) != cudaSuccess)
+        return ZL_ERR_CUDA;
+    return ZL_OK;
+}
+
+// Puts the schedule's tables on the current device (none present: a host-only handle) and hands the handle out.
+zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
+    int n_dev = 0;
+    if (cudaGetDeviceCount(&n_dev) != cudaSuccess || n_dev == 0) {
+        cudaGetLastError();  // host-only handle: inspection works, launches return ZL_ERR_CUDA
+        *out = h;
+        return ZL_OK;
+    }
+    int dev = 0;
+    cudaDeviceProp prop;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaGetDeviceProperties(&prop, dev) != cudaSuccess) {
+        delete h; return ZL_ERR_CUDA;
+    }
+    if (prop.major != 10) { delete h; return ZL_ERR_UNSUPPORTED; }
+    h->device = dev;
+    h->n_sms = prop.multiProcessorCount;
+
+    const Schedule& s = h->sched;
+    size_t off = 0;
+    const size_t o_tasks = place<Task>(off, s.tasks.size());
+    const size_t o_fwd = place<WorkItem>(off, s.fwd_items.size());
+    const size_t o_bwd = place<WorkItem>(off, s.bwd_items.size());
+    const size_t o_bwd2 = place<WorkItem>(off, s.bwd_pair_items.size());
+    const size_t o_mg = place<MergeGroup>(off, s.merge_groups.size());
+    const size_t o_mp = place<int32_t>(off, s.merge_parts.size());
+    const size_t o_mr = place<int32_t>(off, s.merge_row_prefix.size());
+    const size_t o_qg = place<QGroup>(off, s.q_groups.size());
+    const size_t o_kg = place<KvGroup>(off, s.kv_groups.size());
+    const size_t o_kt = place<int32_t>(off, s.kv_group_tasks.size());
+    const size_t o_st = place<int32_t>(off, 2);
+    const size_t total = align_up(off, 256);
+
+    std::vector<uint8_t> host(total, 0);
+    auto put = [&](size_t at, const void* src, size_t bytes) { if (bytes) std::memcpy(host.data() + at, src, bytes); };
+    put(o_tasks, s.tasks.data(), s.tasks.size() * sizeof(Task));
+    put(o_fwd, s.fwd_items.data(), s.fwd_items.size() * sizeof(WorkItem));
+    put(o_bwd, s.bwd_items.data(), s.bwd_items.size() * sizeof(WorkItem));
+    put(o_bwd2, s.bwd_pair_items.data(), s.bwd_pair_items.size() * sizeof(WorkItem));
+    put(o_mg, s.merge_groups.data(), s.merge_groups.size() * sizeof(MergeGroup));
+    put(o_mp, s.merge_parts.data(), s.merge_parts.size() * sizeof(int32_t));
+    put(o_mr, s.merge_row_prefix.data(), s.merge_row_prefix.size() * sizeof(int32_t));
+    put(o_qg, s.q_groups.data(), s.q_groups.size() * sizeof(QGroup));
+    put(o_kg, s.kv_groups.data(), s.kv_groups.size() * sizeof(KvGroup));
+    put(o_kt, s.kv_group_tasks.data(), s.kv_group_tasks.size() * sizeof(int32_t));
+
+    if (cudaMalloc(&h->d_tables, total) != cudaSuccess) { delete h; return ZL_ERR_CUDA; }
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    // pageable source: the copy is staged before the call returns, so `host` may go away
+    if (cudaMemcpyAsync(h->d_tables, host.data(), total, cudaMemcpyHostToDevice, cs) != cudaSuccess ||
+        cudaStreamSynchronize(cs) != cudaSuccess) {
+        cudaFree(h->d_tables); delete h; return ZL_ERR_CUDA;
+    }
+    h->d_tasks = reinterpret_cast<Task*>(h->d_tables + o_tasks);
+    h->d_fwd_items = reinterpret_cast<WorkItem*>(h->d_tables + o_fwd);
+    h->d_bwd_items = reinterpret_cast<WorkItem*>(h->d_tables + o_bwd);
+    h->d_bwd_pair_items = reinterpret_cast<WorkItem*>(h->d_tables + o_bwd2);
+    h->d_merge_groups = reinterpret_cast<MergeGroup*>(h->d_tables + o_mg);
+    h->d_merge_parts = reinterpret_cast<int32_t*>(h->d_tables + o_mp);
+    h->d_merge_prefix = reinterpret_cast<int32_t*>(h->d_tables + o_mr);
+    h->d_q_groups = reinterpret_cast<QGroup*>(h->d_tables + o_qg);
+    h->d_kv_groups = reinterpret_cast<KvGroup*>(h->d_tables + o_kg);
+    h->d_kv_group_tasks = reinterpret_cast<int32_t*>(h->d_tables + o_kt);
+    h->d_status = reinterpret_cast<int32_t*>(h->d_tables + o_st);
+    *out = h;
+    return ZL_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -216,72 +295,26 @@ zl_status zl_build_tasks_heads(const zl_whole_desc* whole, int32_t n_whole, cons
     }
     zl_tasks* h = new (std::nothrow) zl_tasks();
     if (!h) return ZL_ERR_INVALID_ARG;
-    zl_status st = build_schedule(in, n_shards, total_q, total_kv, n_heads, head_dim, flags, &h->sched);
+    const zl_status st = build_schedule(in, n_shards, total_q, total_kv, n_heads, head_dim, flags, &h->sched);
     if (st != ZL_OK) { delete h; return st; }
+    return upload_handle(h, stream, out);
+}
 
-    int n_dev = 0;
-    if (cudaGetDeviceCount(&n_dev) != cudaSuccess || n_dev == 0) {
-        cudaGetLastError();  // host-only handle: inspection works, launches return ZL_ERR_CUDA
-        *out = h;
-        return ZL_OK;
+zl_status zl_build_tasks_prefix(const int32_t* cu_q, const int32_t* cu_kv, int32_t n_seqs, int32_t prefix_len,
+                                int32_t total_q, int32_t total_kv, int32_t n_heads, int32_t head_dim, void* stream,
+                                zl_tasks** out) {
+    if (!out) return ZL_ERR_INVALID_ARG;
+    *out = nullptr;
+    zl_tasks* h = new (std::nothrow) zl_tasks();
+    if (!h) return ZL_ERR_INVALID_ARG;
+    try {
+        const zl_status st = build_prefix_schedule(cu_q, cu_kv, n_seqs, prefix_len, total_q, total_kv, n_heads, head_dim, &h->sched);
+        if (st != ZL_OK) { delete h; return st; }
+        return upload_handle(h, stream, out);
+    } catch (const std::bad_alloc&) {
+        delete h;
+        return ZL_ERR_INVALID_ARG;
     }
-    int dev = 0;
-    cudaDeviceProp prop;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaGetDeviceProperties(&prop, dev) != cudaSuccess) {
-        delete h; return ZL_ERR_CUDA;
-    }
-    if (prop.major != 10) { delete h; return ZL_ERR_UNSUPPORTED; }
-    h->device = dev;
-    h->n_sms = prop.multiProcessorCount;
-
-    const Schedule& s = h->sched;
-    size_t off = 0;
-    const size_t o_tasks = place<Task>(off, s.tasks.size());
-    const size_t o_fwd = place<WorkItem>(off, s.fwd_items.size());
-    const size_t o_bwd = place<WorkItem>(off, s.bwd_items.size());
-    const size_t o_bwd2 = place<WorkItem>(off, s.bwd_pair_items.size());
-    const size_t o_mg = place<MergeGroup>(off, s.merge_groups.size());
-    const size_t o_mp = place<int32_t>(off, s.merge_parts.size());
-    const size_t o_mr = place<int32_t>(off, s.merge_row_prefix.size());
-    const size_t o_qg = place<QGroup>(off, s.q_groups.size());
-    const size_t o_kg = place<KvGroup>(off, s.kv_groups.size());
-    const size_t o_kt = place<int32_t>(off, s.kv_group_tasks.size());
-    const size_t o_st = place<int32_t>(off, 2);
-    const size_t total = align_up(off, 256);
-
-    std::vector<uint8_t> host(total, 0);
-    auto put = [&](size_t at, const void* src, size_t bytes) { if (bytes) std::memcpy(host.data() + at, src, bytes); };
-    put(o_tasks, s.tasks.data(), s.tasks.size() * sizeof(Task));
-    put(o_fwd, s.fwd_items.data(), s.fwd_items.size() * sizeof(WorkItem));
-    put(o_bwd, s.bwd_items.data(), s.bwd_items.size() * sizeof(WorkItem));
-    put(o_bwd2, s.bwd_pair_items.data(), s.bwd_pair_items.size() * sizeof(WorkItem));
-    put(o_mg, s.merge_groups.data(), s.merge_groups.size() * sizeof(MergeGroup));
-    put(o_mp, s.merge_parts.data(), s.merge_parts.size() * sizeof(int32_t));
-    put(o_mr, s.merge_row_prefix.data(), s.merge_row_prefix.size() * sizeof(int32_t));
-    put(o_qg, s.q_groups.data(), s.q_groups.size() * sizeof(QGroup));
-    put(o_kg, s.kv_groups.data(), s.kv_groups.size() * sizeof(KvGroup));
-    put(o_kt, s.kv_group_tasks.data(), s.kv_group_tasks.size() * sizeof(int32_t));
-
-    if (cudaMalloc(&h->d_tables, total) != cudaSuccess) { delete h; return ZL_ERR_CUDA; }
-    cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    // pageable source: the copy is staged before the call returns, so `host` may go away
-    if (cudaMemcpyAsync(h->d_tables, host.data(), total, cudaMemcpyHostToDevice, cs) != cudaSuccess ||
-        cudaStreamSynchronize(cs) != cudaSuccess) {
-        cudaFree(h->d_tables); delete h; return ZL_ERR_CUDA;
-    }
-    h->d_tasks = reinterpret_cast<Task*>(h->d_tables + o_tasks);
-    h->d_fwd_items = reinterpret_cast<WorkItem*>(h->d_tables + o_fwd);
-    h->d_bwd_items = reinterpret_cast<WorkItem*>(h->d_tables + o_bwd);
-    h->d_bwd_pair_items = reinterpret_cast<WorkItem*>(h->d_tables + o_bwd2);
-    h->d_merge_groups = reinterpret_cast<MergeGroup*>(h->d_tables + o_mg);
-    h->d_merge_parts = reinterpret_cast<int32_t*>(h->d_tables + o_mp);
-    h->d_merge_prefix = reinterpret_cast<int32_t*>(h->d_tables + o_mr);
-    h->d_q_groups = reinterpret_cast<QGroup*>(h->d_tables + o_qg);
-    h->d_kv_groups = reinterpret_cast<KvGroup*>(h->d_tables + o_kg);
-    h->d_kv_group_tasks = reinterpret_cast<int32_t*>(h->d_tables + o_kt);
-    h->d_status = reinterpret_cast<int32_t*>(h->d_tables + o_st);
-    *out = h;
-    return ZL_OK;
 }
 
 zl_status zl_tasks_get_info(const zl_tasks* t, zl_tasks_info* info) {
@@ -334,16 +367,71 @@ void zl_free_tasks(zl_tasks* t) {
         for (cudaEvent_t e : t->ev_stop[k]) cudaEventDestroy(e);
     }
     if (t->d_tables) cudaFree(t->d_tables);
+    if (t->d_positions) cudaFree(t->d_positions);
     delete t;
 }
 
 }  // extern "C"
 
 namespace {
+// A checked score: which kernel variant it needs and what that variant reads.  `any` is false when nothing is left of
+// it beyond scale * q.k, and the plain kernels run.
+struct CheckedScore {
+    ScoreParams params{};
+    bool any = false, capped = false, biased = false;
+};
+
+zl_status check_score(const zl_tasks* t, const zl_score* score, CheckedScore* out) {
+    if (!score) return ZL_ERR_INVALID_ARG;
+    const Schedule& s = t->sched;
+    auto aligned4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; };
+    if (!(score->cap >= 0.f) || !std::isfinite(score->cap)) return ZL_ERR_INVALID_ARG;
+    if (score->masked != 0 && score->masked != 1) return ZL_ERR_INVALID_ARG;
+    if (score->max_distance < 0 || score->max_distance > (1 << 24)) return ZL_ERR_INVALID_ARG;
+    if (score->bucket_bias) {
+        if (!score->bucket_of || score->n_buckets < 1) return ZL_ERR_INVALID_ARG;
+        if (score->n_buckets > ZL_MAX_BUCKETS) return ZL_ERR_UNSUPPORTED;
+    } else if (score->bucket_of || score->n_buckets != 0) {
+        return ZL_ERR_INVALID_ARG;
+    }
+    if (!aligned4(score->slopes) || !aligned4(score->bucket_bias) || !aligned4(score->bucket_of)) return ZL_ERR_INVALID_ARG;
+    out->capped = score->cap > 0.f;
+    out->biased = score->slopes || score->bucket_bias;
+    out->any = out->capped || out->biased || score->masked;
+    if (out->biased && s.shared_prefix) return ZL_ERR_UNSUPPORTED;  // a prefix key's distance differs by sequence
+    if (out->biased && !s.shard_to_task.empty() && s.task_pos.empty()) return ZL_ERR_INVALID_ARG;
+    if (score->masked && s.task_pos.empty() && !s.tasks.empty()) return ZL_ERR_INVALID_ARG;
+    ScoreParams& p = out->params;
+    p.pos = s.task_pos.empty() ? nullptr : t->d_task_pos;
+    p.slopes = score->slopes;
+    p.bucket_bias = score->bucket_bias;
+    p.bucket_of = score->bucket_of;
+    p.n_buckets = score->n_buckets;
+    p.reach = score->bucket_bias ? score->max_distance : 0;
+    p.n_heads = s.n_heads;
+    p.masked = score->masked;
+    p.cap_log2 = score->cap * 1.4426950408889634f;
+    p.n_kv_tiles = s.n_kv_tiles;
+    return ZL_OK;
+}
+
+// Byte offsets behind the plain backward's workspace: LSE tiles of capped scores, then the key tiles' shares of the
+// bucket gradient.
+struct ScoredWorkspace {
+    size_t lse, part, bytes;
+    ScoredWorkspace(const Schedule& s, const CheckedScore& c) {
+        lse = s.bwd_workspace_bytes;
+        part = lse + (c.capped ? align_up((size_t)s.q_pad_total * s.n_heads * sizeof(float), 256) : 0);
+        bytes = part + (c.params.bucket_bias ? (size_t)s.n_kv_tiles * s.n_heads * kMaxBuckets * sizeof(float) : 0);
+    }
+};
+
 // Forward over q, k, v given as token-major views with `in_stride` elements between rows.
 // `phase` < 0: the whole work list; otherwise the items of that launch phase only.
+// `score`: NULL for the plain kernel.
 zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* k, const void* v, int64_t in_stride,
-                   float scale, void* o, float* lse, float* o_partial, float* lse_partial, void* stream) {
+                   float scale, void* o, float* lse, float* o_partial, float* lse_partial, void* stream,
+                   const CheckedScore* score = nullptr) {
     const Schedule& s = t->sched;
     const int32_t n_phases = (int32_t)s.fwd_phase_begin.size() - 1;
     if (phase >= n_phases) return ZL_ERR_INVALID_ARG;
@@ -384,7 +472,15 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     p.lse_partial = lse_partial;
     p.status = t->d_status;
     const int grid = std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
-    {
+    if (score) {
+        ScoreParams sp = score->params;
+        sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
+        if (sp.masked) p.items = t->d_fwd_items_masked;
+        LaunchTimer lt(t, ZL_K_FWD, static_cast<cudaStream_t>(stream));
+        if (launch_scored_fwd(s.head_dim, score->capped, score->biased ? kScoreBias : kScorePlain, tq, tk, tv, to, top, p, sp,
+                              grid, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+            return ZL_ERR_CUDA;
+    } else {
         LaunchTimer lt(t, ZL_K_FWD, static_cast<cudaStream_t>(stream));
         if (launch_fwd(s.head_dim, tq, tk, tv, to, top, p, grid, static_cast<cudaStream_t>(stream)) != cudaSuccess)
             return ZL_ERR_CUDA;
@@ -463,9 +559,16 @@ namespace {
 // preprocess kernel, every phase runs the main kernel over its own kv groups, the last one also converts dQ.
 zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* k, const void* v, int64_t in_stride,
                    const void* o, const float* lse, const void* d_o, float scale, void* dq, void* dk, void* dv,
-                   int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream) {
+                   int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream,
+                   const CheckedScore* score = nullptr, float* d_bucket_bias = nullptr) {
     const Schedule& s = t->sched;
-    if (s.tasks.empty()) return ZL_OK;
+    if (s.tasks.empty()) {
+        if (!d_bucket_bias) return ZL_OK;
+        if (t->device < 0) return ZL_ERR_CUDA;
+        if (!on_handle_device(t)) return ZL_ERR_INVALID_ARG;
+        const size_t bytes = (size_t)score->params.n_buckets * s.n_heads * sizeof(float);
+        return cudaMemsetAsync(d_bucket_bias, 0, bytes, static_cast<cudaStream_t>(stream)) == cudaSuccess ? ZL_OK : ZL_ERR_CUDA;
+    }
     const int32_t n_phases = (int32_t)s.bwd_phase_begin.size() - 1;
     if (phase >= n_phases) return ZL_ERR_INVALID_ARG;
     const bool first = phase <= 0, last = phase < 0 || phase == n_phases - 1;
@@ -476,12 +579,12 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         !aligned16(dk) || !aligned16(dv) || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0)
         return ZL_ERR_INVALID_ARG;
     if (!(scale > 0.f) || !std::isfinite(scale)) return ZL_ERR_INVALID_ARG;
-    if (workspace_bytes < s.bwd_workspace_bytes) return ZL_ERR_WORKSPACE;
+    if (workspace_bytes < (score ? ScoredWorkspace(s, *score).bytes : s.bwd_workspace_bytes)) return ZL_ERR_WORKSPACE;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
 
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     CUtensorMap tq, tk, tv, tdo, tdq, tdk, tdv;
-    if (!make_tmap_f32_acc(&tdq, ws + s.ws_dq_acc_off, s.q_pad_total, s.n_heads, s.head_dim)) return ZL_ERR_CUDA;
+    if (!make_tmap_f32_acc(&tdq, ws + s.ws_dq_acc_off, s.dq_acc_rows, s.n_heads, s.head_dim)) return ZL_ERR_CUDA;
     const int64_t hd = (int64_t)s.n_heads * s.head_dim;
     if (!make_tmap(&tq, q, s.total_q, s.n_heads, s.head_dim, kTileQ, in_stride) ||
         !make_tmap(&tk, k, s.total_kv, s.n_heads, s.head_dim, kTileKV, in_stride) ||
@@ -504,6 +607,7 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     p.n_heads = s.n_heads;
     p.total_q = s.total_q;
     p.q_pad_total = (int32_t)s.q_pad_total;
+    p.dq_rows = (int32_t)s.dq_rows;
     p.scale = scale;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.o = static_cast<const __nv_bfloat16*>(o);
@@ -516,18 +620,27 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     p.dq_acc = reinterpret_cast<float*>(ws + s.ws_dq_acc_off);
     p.aug = ws + s.ws_aug_off;
     p.status = t->d_status;
+    ScoreParams sp{};
+    if (score) {
+        const ScoredWorkspace at(s, *score);
+        sp = score->params;
+        sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
+        if (score->capped) p.lse_tiles = reinterpret_cast<float*>(ws + at.lse);
+        if (d_bucket_bias) sp.bucket_part = reinterpret_cast<float*>(ws + at.part);
+        if (sp.masked) p.items = t->d_bwd_items_masked;
+    }
 
     if (first) {
-        if (cudaMemsetAsync(p.dq_acc, 0, (size_t)s.q_pad_total * s.n_heads * s.head_dim * sizeof(float), cs) != cudaSuccess)
+        if (cudaMemsetAsync(p.dq_acc, 0, (size_t)s.dq_acc_rows * s.n_heads * s.head_dim * sizeof(float), cs) != cudaSuccess)
             return ZL_ERR_CUDA;
         LaunchTimer lt(t, ZL_K_BWD_PRE, cs);
         if (launch_bwd_pre(s.head_dim, p, t->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
         g_launches.fetch_add(1);
     }
-    const bool pair = s.head_dim == 128 && (t->bwd_kernel == 2 || (t->bwd_kernel == 0 && kDefaultBwdPair));
+    const bool pair = !score && s.head_dim == 128 && (t->bwd_kernel == 2 || (t->bwd_kernel == 0 && kDefaultBwdPair));
     if (p.n_items > 0 && pair) {
         CUtensorMap tq64, tdo64, taug, tdq16, tdk32, tdv32;
-        if (!make_tmap_f32_acc(&tdq16, ws + s.ws_dq_acc_off, s.q_pad_total, s.n_heads, s.head_dim, 32, 16) ||
+        if (!make_tmap_f32_acc(&tdq16, ws + s.ws_dq_acc_off, s.dq_acc_rows, s.n_heads, s.head_dim, 32, 16) ||
             !make_tmap(&tdk32, dk, s.total_kv, s.n_heads, s.head_dim, 32, grad_stride) ||
             !make_tmap(&tdv32, dv, s.total_kv, s.n_heads, s.head_dim, 32, grad_stride) ||
             !make_tmap(&tq64, q, s.total_q, s.n_heads, s.head_dim, 64, in_stride) ||
@@ -546,13 +659,24 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     } else if (p.n_items > 0) {
         const int grid = std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
         LaunchTimer lt(t, ZL_K_BWD_MAIN, cs);
-        if (launch_bwd_main(s.head_dim, tq, tk, tv, tdo, tdq, tdk, tdv, p, grid, cs) != cudaSuccess) return ZL_ERR_CUDA;
+        if (score) {
+            const ScoreKind kind = !score->biased ? kScorePlain : (d_bucket_bias ? kScoreBiasGrad : kScoreBias);
+            // heads that a key tile's tasks leave out have no share
+            if (d_bucket_bias && cudaMemsetAsync(sp.bucket_part, 0, (size_t)s.n_kv_tiles * s.n_heads * kMaxBuckets * sizeof(float), cs) != cudaSuccess)
+                return ZL_ERR_CUDA;
+            if (launch_scored_bwd(s.head_dim, score->capped, kind, tq, tk, tv, tdo, tdq, tdk, tdv, p, sp, grid, cs) != cudaSuccess)
+                return ZL_ERR_CUDA;
+        } else if (launch_bwd_main(s.head_dim, tq, tk, tv, tdo, tdq, tdk, tdv, p, grid, cs) != cudaSuccess) return ZL_ERR_CUDA;
         g_launches.fetch_add(1);
     }
     if (last) {
         LaunchTimer lt(t, ZL_K_BWD_POST, cs);
         if (launch_bwd_post(s.head_dim, p, t->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
         g_launches.fetch_add(1);
+        if (d_bucket_bias) {
+            if (launch_bucket_reduce(sp, d_bucket_bias, cs) != cudaSuccess) return ZL_ERR_CUDA;
+            g_launches.fetch_add(1);
+        }
     }
     return ZL_OK;
 }
@@ -588,6 +712,106 @@ zl_status zl_coalesced_attn_bwd_packed(const zl_tasks* t, const void* qkv, const
     __nv_bfloat16* out = static_cast<__nv_bfloat16*>(dqkv);
     return bwd_impl(t, -1, in, in + hd, in + 2 * hd, 3 * hd, o, lse, d_o, scale, out, out + hd, out + 2 * hd, 3 * hd,
                     workspace, workspace_bytes, stream);
+}
+
+zl_status zl_scored_attn_fwd(const zl_tasks* t, const zl_score* score, const void* q, const void* k, const void* v,
+                             float scale, void* o, float* lse, float* o_partial, float* lse_partial, void* stream) {
+    if (!t) return ZL_ERR_INVALID_ARG;
+    CheckedScore c;
+    const zl_status st = check_score(t, score, &c);
+    if (st != ZL_OK) return st;
+    return fwd_impl(t, -1, q, k, v, (int64_t)t->sched.n_heads * t->sched.head_dim, scale, o, lse, o_partial, lse_partial,
+                    stream, c.any ? &c : nullptr);
+}
+
+zl_status zl_scored_attn_fwd_packed(const zl_tasks* t, const zl_score* score, const void* qkv, float scale, void* o,
+                                    float* lse, float* o_partial, float* lse_partial, void* stream) {
+    if (!t) return ZL_ERR_INVALID_ARG;
+    CheckedScore c;
+    const zl_status st = check_score(t, score, &c);
+    if (st != ZL_OK) return st;
+    const Schedule& s = t->sched;
+    if (s.total_q != s.total_kv) return ZL_ERR_INVALID_ARG;
+    if (!qkv) return s.fwd_items.empty() ? ZL_OK : ZL_ERR_INVALID_ARG;
+    const int64_t hd = (int64_t)s.n_heads * s.head_dim;
+    const __nv_bfloat16* base = static_cast<const __nv_bfloat16*>(qkv);
+    return fwd_impl(t, -1, base, base + hd, base + 2 * hd, 3 * hd, scale, o, lse, o_partial, lse_partial, stream,
+                    c.any ? &c : nullptr);
+}
+
+zl_status zl_scored_attn_bwd(const zl_tasks* t, const zl_score* score, const void* q, const void* k, const void* v,
+                             const void* o, const float* lse, const void* d_o, float scale, void* dq, void* dk, void* dv,
+                             float* d_bucket_bias, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!t) return ZL_ERR_INVALID_ARG;
+    CheckedScore c;
+    const zl_status st = check_score(t, score, &c);
+    if (st != ZL_OK) return st;
+    if (d_bucket_bias && (!score->bucket_bias || (reinterpret_cast<uintptr_t>(d_bucket_bias) & 3) != 0)) return ZL_ERR_INVALID_ARG;
+    const int64_t hd = (int64_t)t->sched.n_heads * t->sched.head_dim;
+    return bwd_impl(t, -1, q, k, v, hd, o, lse, d_o, scale, dq, dk, dv, hd, workspace, workspace_bytes, stream,
+                    c.any ? &c : nullptr, d_bucket_bias);
+}
+
+zl_status zl_scored_attn_bwd_packed(const zl_tasks* t, const zl_score* score, const void* qkv, const void* o,
+                                    const float* lse, const void* d_o, float scale, void* dqkv, float* d_bucket_bias,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+    if (!t) return ZL_ERR_INVALID_ARG;
+    CheckedScore c;
+    const zl_status st = check_score(t, score, &c);
+    if (st != ZL_OK) return st;
+    if (d_bucket_bias && (!score->bucket_bias || (reinterpret_cast<uintptr_t>(d_bucket_bias) & 3) != 0)) return ZL_ERR_INVALID_ARG;
+    const Schedule& s = t->sched;
+    if (s.total_q != s.total_kv) return ZL_ERR_INVALID_ARG;
+    if ((!qkv || !dqkv) && !s.tasks.empty()) return ZL_ERR_INVALID_ARG;
+    const int64_t hd = (int64_t)s.n_heads * s.head_dim;
+    const __nv_bfloat16* in = static_cast<const __nv_bfloat16*>(qkv);
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(dqkv);
+    return bwd_impl(t, -1, in, in + hd, in + 2 * hd, 3 * hd, o, lse, d_o, scale, out, out + hd, out + 2 * hd, 3 * hd,
+                    workspace, workspace_bytes, stream, c.any ? &c : nullptr, d_bucket_bias);
+}
+
+zl_status zl_scored_workspace_bytes(const zl_tasks* t, const zl_score* score, size_t* bytes) {
+    if (!t || !bytes) return ZL_ERR_INVALID_ARG;
+    CheckedScore c;
+    const zl_status st = check_score(t, score, &c);
+    if (st != ZL_OK) return st;
+    *bytes = ScoredWorkspace(t->sched, c).bytes;
+    return ZL_OK;
+}
+
+zl_status zl_set_positions(zl_tasks* t, const int32_t* whole_prefix, const zl_shard_pos* shard_pos, void* stream) {
+    if (!t) return ZL_ERR_INVALID_ARG;
+    if (t->device >= 0 && !on_handle_device(t)) return ZL_ERR_INVALID_ARG;
+    Schedule& s = t->sched;
+    try {
+        const zl_status st = set_positions(&s, whole_prefix, shard_pos);
+        if (st != ZL_OK) return st;
+        if (t->device < 0 || s.tasks.empty()) return ZL_OK;
+        // no entry is left that the device does not have: a failure below takes the positions back
+        size_t off = 0;
+        const size_t o_pos = place<TaskPos>(off, s.task_pos.size());
+        const size_t o_fwd = place<WorkItem>(off, s.fwd_items_masked.size());
+        const size_t o_bwd = place<WorkItem>(off, s.bwd_items_masked.size());
+        if (!t->d_positions && cudaMalloc(&t->d_positions, align_up(off, 256)) != cudaSuccess) {
+            t->d_positions = nullptr;
+            s.task_pos.clear();
+            return ZL_ERR_CUDA;
+        }
+        t->d_task_pos = reinterpret_cast<TaskPos*>(t->d_positions + o_pos);
+        t->d_fwd_items_masked = reinterpret_cast<WorkItem*>(t->d_positions + o_fwd);
+        t->d_bwd_items_masked = reinterpret_cast<WorkItem*>(t->d_positions + o_bwd);
+        cudaStream_t cs = static_cast<cudaStream_t>(stream);
+        if (cudaMemcpyAsync(t->d_task_pos, s.task_pos.data(), s.task_pos.size() * sizeof(TaskPos), cudaMemcpyHostToDevice, cs) != cudaSuccess ||
+            upload_items(t, t->d_fwd_items_masked, s.fwd_items_masked, cs) != ZL_OK ||
+            upload_items(t, t->d_bwd_items_masked, s.bwd_items_masked, cs) != ZL_OK || cudaStreamSynchronize(cs) != cudaSuccess) {
+            s.task_pos.clear();
+            return ZL_ERR_CUDA;
+        }
+        return ZL_OK;
+    } catch (const std::bad_alloc&) {
+        s.task_pos.clear();
+        return ZL_ERR_INVALID_ARG;
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -657,14 +881,6 @@ zl_status task_phases(const Schedule& s, const int32_t* whole_phase, const int32
         if (ph < 0 || ph >= n_phases) return ZL_ERR_INVALID_ARG;
         if (s.shard_to_task[i] >= 0) (*out)[s.shard_to_task[i]] = std::max((*out)[s.shard_to_task[i]], ph);
     }
-    return ZL_OK;
-}
-
-zl_status upload_items(const zl_tasks* t, WorkItem* dst, const std::vector<WorkItem>& items, cudaStream_t cs) {
-    if (t->device < 0 || items.empty()) return ZL_OK;
-    if (cudaMemcpyAsync(dst, items.data(), items.size() * sizeof(WorkItem), cudaMemcpyHostToDevice, cs) != cudaSuccess ||
-        cudaStreamSynchronize(cs) != cudaSuccess)
-        return ZL_ERR_CUDA;
     return ZL_OK;
 }
 }  // namespace

@@ -142,6 +142,10 @@ __global__ void __launch_bounds__(kPreThreads) zl_bwd_pre_kernel(const BwdParams
                 const int tile = slot_row[k] / kTileQ, tr = slot_row[k] % kTileQ;
                 uint8_t* base = p.aug + ((int64_t)head[k] * (p.q_pad_total / kTileQ) + tile) * 4096;
                 *reinterpret_cast<uint4*>(base + quarter * 2048 + (tr / 8) * 128 + (tr % 8) * 16) = val;
+                // capped scores add the LSE after the cap, not inside the product: plain fp32, in powers of two
+                if (p.lse_tiles && quarter == 0)
+                    p.lse_tiles[(int64_t)head[k] * p.q_pad_total + slot_row[k]] =
+                        live[k] && lse[k] > -INFINITY && lse[k] < INFINITY ? lse[k] * 1.4426950408889634f : 1e30f;
             }
         }
     }
@@ -155,7 +159,7 @@ __global__ void __launch_bounds__(kPreThreads) zl_bwd_post_kernel(const BwdParam
     constexpr int V = D / 32;
     constexpr int kBatch = 4;
     const int lane = threadIdx.x & 31;
-    for (int64_t slot_row = (int64_t)blockIdx.x * (kPreThreads / 32) + (threadIdx.x >> 5); slot_row < p.q_pad_total;
+    for (int64_t slot_row = (int64_t)blockIdx.x * (kPreThreads / 32) + (threadIdx.x >> 5); slot_row < p.dq_rows;
          slot_row += (int64_t)gridDim.x * (kPreThreads / 32)) {
         const QGroup g = p.q_groups[find_q_group(p.q_groups, p.n_q_groups, (int)slot_row)];
         const int r = (int)slot_row - g.slot;
@@ -673,7 +677,7 @@ zl_bwd_main_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             fence_proxy_async_smem();
                             __syncwarp();
                             if (leader) {
-                                tma_reduce_add_3d(&tm_dq, buf, c * 32, wi.head, t.q_slot + qt * kTileQ + quarter * 32);
+                                tma_reduce_add_3d(&tm_dq, buf, c * 32, wi.head, t.dq_slot + qt * kTileQ + quarter * 32);
                                 bulk_commit_group();
                             }
                         }
@@ -737,7 +741,7 @@ cudaError_t launch_bwd_main(int head_dim, const CUtensorMap& tq, const CUtensorM
 }
 
 cudaError_t launch_bwd_post(int head_dim, const BwdParams& p, int n_sms, cudaStream_t stream) {
-    if (p.q_pad_total == 0) return cudaSuccess;
+    if (p.dq_rows == 0) return cudaSuccess;
     const int grid = n_sms * 8;
     if (head_dim == 128) zl_bwd_post_kernel<128><<<grid, kPreThreads, 0, stream>>>(p);
     else zl_bwd_post_kernel<64><<<grid, kPreThreads, 0, stream>>>(p);

@@ -702,7 +702,7 @@ zl_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         fence_proxy_async_smem();
                         __syncwarp();
                         if (leader) {
-                            tma_reduce_add_3d(&tm_dq, buf, col_base + c * 16, wi.head, t.q_slot + qt * kTileQ + row_in_tile);
+                            tma_reduce_add_3d(&tm_dq, buf, col_base + c * 16, wi.head, t.dq_slot + qt * kTileQ + row_in_tile);
                             bulk_commit_group();
                         }
                     }

@@ -58,10 +58,36 @@ struct BwdParams {
     __nv_bfloat16* dk;
     __nv_bfloat16* dv;
     int64_t grad_row_stride;  // elements between token rows of dq, dk, dv (H*d, or 3*H*d when packed)
-    float* dq_acc;  // [q_pad_total, H, d]
+    int32_t dq_rows;  // rows of dq_acc that are converted
+    float* dq_acc;  // [dq_acc_rows, H, d]
     uint8_t* aug;   // [H, q_pad_total / 128] tiles of 4 KB: bf16 splits of -lse/scale and -rowsum(dO o O)
     int32_t* status;
+    float* lse_tiles;  // [H, q_pad_total] LSE * log2(e), 1e30 for rows without a key; NULL unless scores are capped
 };
+
+// Scores beyond scale * q.k (zl_score), as the kernels read them.
+struct ScoreParams {
+    const TaskPos* pos;          // per task; NULL: every task starts at position 0 of its sequence
+    const float* slopes;         // [H] or NULL
+    const float* bucket_bias;    // [n_buckets, H] or NULL
+    const int32_t* bucket_of;    // [2 * reach + 1] bucket of key position - query position, clamped to [-reach, reach]
+    int32_t n_buckets, reach;    // reach 0 without buckets
+    int32_t n_heads;
+    int32_t masked;
+    float cap_log2;              // cap * log2(e)
+    float scale_over_cap;        // scale / cap
+    float* bucket_part;          // backward, [H, n_kv_tiles, kMaxBuckets]: each key tile's share of the table's gradient
+    int32_t n_kv_tiles;
+};
+enum ScoreKind { kScorePlain = 0, kScoreBias = 1, kScoreBiasGrad = 2 };  // what is added to the (capped) product
+
+cudaError_t launch_scored_fwd(int head_dim, bool capped, ScoreKind kind, const CUtensorMap& tq, const CUtensorMap& tk,
+                              const CUtensorMap& tv, const CUtensorMap& to, const CUtensorMap& top, const FwdParams& p,
+                              const ScoreParams& sp, int grid, cudaStream_t stream);
+cudaError_t launch_scored_bwd(int head_dim, bool capped, ScoreKind kind, const CUtensorMap& tq, const CUtensorMap& tk,
+                              const CUtensorMap& tv, const CUtensorMap& tdo, const CUtensorMap& tdq, const CUtensorMap& tdk,
+                              const CUtensorMap& tdv, const BwdParams& p, const ScoreParams& sp, int grid, cudaStream_t stream);
+cudaError_t launch_bucket_reduce(const ScoreParams& sp, float* d_bucket_bias, cudaStream_t stream);
 
 cudaError_t launch_bwd_pre(int head_dim, const BwdParams& p, int n_sms, cudaStream_t stream);
 cudaError_t launch_bwd_main(int head_dim, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,

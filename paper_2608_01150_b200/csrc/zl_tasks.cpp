@@ -61,7 +61,77 @@ bool ranges_consistent(const std::vector<Range>& rng, const std::vector<HeadRang
     return true;
 }
 
+// A shared prefix is cut so that it gives about this many forward items (two per SM of a B200), but into chunks of no
+// fewer than kPrefixChunkMin keys: a chunk's partial row costs as much traffic as two key rows.
+constexpr int64_t kPrefixItems = 2 * 148;
+constexpr int64_t kPrefixChunkMin = 512;
+
+// Positions leave room for the padded rows of a last tile in 32-bit arithmetic.
+constexpr int64_t kMaxPos = INT32_MAX - 4 * 128;
+
 using GroupKey = std::tuple<int64_t, int64_t, int32_t, int32_t>;  // range offset, length, head range
+
+// Work lists, launch phases and workspace layout from the tasks, query groups and kv groups.
+void finish_schedule(Schedule* s) {
+    for (KvGroup& g : s->kv_groups) {
+        g.tile_begin = s->n_kv_tiles;
+        s->n_kv_tiles += (g.kv_len + kTileKV - 1) / kTileKV;
+    }
+
+    // forward work list: (task, head of the task's range, query block), longest-first
+    for (size_t ti = 0; ti < s->tasks.size(); ++ti) {
+        const Task& t = s->tasks[ti];
+        for (int32_t h = s->task_head_begin[ti]; h < s->task_head_begin[ti] + s->task_head_count[ti]; ++h)
+            for (int32_t r = 0; r < t.q_len; r += kFwdBlockQ)
+                s->fwd_items.push_back({(int32_t)ti, h, r, std::min(kFwdBlockQ, t.q_len - r)});
+    }
+    std::stable_sort(s->fwd_items.begin(), s->fwd_items.end(), [&](const WorkItem& a, const WorkItem& b) {
+        const int32_t ka = s->tasks[a.unit].kv_len, kb = s->tasks[b.unit].kv_len;
+        if (ka != kb) return ka > kb;
+        if (a.rows != b.rows) return a.rows > b.rows;
+        return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
+    });
+
+    // backward work list: (kv group, head of the group's range, key tile); cost = total query rows served
+    std::vector<int64_t> group_cost(s->kv_groups.size(), 0);
+    for (size_t g = 0; g < s->kv_groups.size(); ++g)
+        for (int32_t j = 0; j < s->kv_groups[g].n_tasks; ++j)
+            group_cost[g] += s->tasks[s->kv_group_tasks[s->kv_groups[g].task_begin + j]].q_len;
+    for (size_t g = 0; g < s->kv_groups.size(); ++g) {
+        const int32_t t0 = s->kv_group_tasks[s->kv_groups[g].task_begin];
+        for (int32_t h = s->task_head_begin[t0]; h < s->task_head_begin[t0] + s->task_head_count[t0]; ++h)
+            for (int32_t r = 0; r < s->kv_groups[g].kv_len; r += kTileKV)
+                s->bwd_items.push_back({(int32_t)g, h, r, std::min(kTileKV, s->kv_groups[g].kv_len - r)});
+    }
+    auto bwd_order = [&](const WorkItem& a, const WorkItem& b) {
+        if (group_cost[a.unit] != group_cost[b.unit]) return group_cost[a.unit] > group_cost[b.unit];
+        if (a.rows != b.rows) return a.rows > b.rows;
+        return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
+    };
+    std::stable_sort(s->bwd_items.begin(), s->bwd_items.end(), bwd_order);
+    // the same list in units of two key tiles, for the CTA-pair form of the main kernel
+    for (size_t g = 0; g < s->kv_groups.size(); ++g) {
+        const int32_t t0 = s->kv_group_tasks[s->kv_groups[g].task_begin];
+        for (int32_t h = s->task_head_begin[t0]; h < s->task_head_begin[t0] + s->task_head_count[t0]; ++h)
+            for (int32_t r = 0; r < s->kv_groups[g].kv_len; r += 2 * kTileKV)
+                s->bwd_pair_items.push_back({(int32_t)g, h, r, std::min(2 * kTileKV, s->kv_groups[g].kv_len - r)});
+    }
+    std::stable_sort(s->bwd_pair_items.begin(), s->bwd_pair_items.end(), bwd_order);
+
+    // one launch phase until the caller says otherwise
+    s->fwd_task_phase.assign(s->tasks.size(), 0);
+    s->bwd_group_phase.assign(s->kv_groups.size(), 0);
+    s->fwd_phase_begin = {0, (int32_t)s->fwd_items.size()};
+    s->bwd_phase_begin = {0, (int32_t)s->bwd_items.size()};
+    s->bwd_pair_phase_begin = {0, (int32_t)s->bwd_pair_items.size()};
+
+    // backward workspace over the padded query slots: fp32 dQ accumulator [dq_acc_rows, H, d], then one
+    // 4 KB "augmentation" tile per (head, 128-row query tile) holding -LSE/scale and -D split
+    // into bf16 pieces (see the backward preprocess kernel)
+    s->ws_dq_acc_off = 0;
+    s->ws_aug_off = align_up((size_t)s->dq_acc_rows * s->n_heads * s->head_dim * sizeof(float), 256);
+    s->bwd_workspace_bytes = s->ws_aug_off + align_up((size_t)(s->q_pad_total / kTileQ) * s->n_heads * 4096, 256);
+}
 
 }  // namespace
 
@@ -148,6 +218,10 @@ zl_status build_schedule(const std::vector<InputTask>& in, int32_t n_shards, int
     s->shard_to_task.assign(n_shards, -1);
     s->shard_slot_off.assign(n_shards, 0);
     s->shard_slot_rows.assign(n_shards, 0);
+    s->shard_kv_off.assign(n_shards, 0);
+    s->shard_kv_len.assign(n_shards, 0);
+    for (const InputTask& t : in)
+        if (t.shard_idx >= 0) { s->shard_kv_off[t.shard_idx] = t.kv_off; s->shard_kv_len[t.shard_idx] = t.kv_len; }
     std::map<GroupKey, int32_t> merge_index;          // (query range, head range) -> merge group
     std::vector<std::vector<int32_t>> merge_members;  // task indices per group
     std::vector<int32_t> merge_seq;
@@ -162,7 +236,7 @@ zl_status build_schedule(const std::vector<InputTask>& in, int32_t n_shards, int
         const InputTask& d = in[i];
         Task t{};
         t.q_off = d.q_off; t.q_len = d.q_len; t.kv_off = d.kv_off; t.kv_len = d.kv_len;
-        t.partial_slot = -1; t.q_slot = 0; t.kv_group = -1; t.q_group = -1;
+        t.partial_slot = -1; t.q_slot = 0; t.kv_group = -1; t.dq_slot = 0;
         if (d.shard_idx < 0) {  // whole sequence: final after the forward launch
             push_task(t, d);
             continue;
@@ -236,8 +310,7 @@ zl_status build_schedule(const std::vector<InputTask>& in, int32_t n_shards, int
                 s->q_pad_total += pad;
                 if (s->q_pad_total > INT32_MAX) return ZL_ERR_INVALID_ARG;
             }
-            t.q_group = qi->second;
-            t.q_slot = s->q_groups[qi->second].slot;
+            t.q_slot = t.dq_slot = s->q_groups[qi->second].slot;
             if (t.kv_len == 0) continue;
             const GroupKey kk(t.kv_off, t.kv_len, hb, he);
             auto ki = kg.find(kk);
@@ -250,7 +323,7 @@ zl_status build_schedule(const std::vector<InputTask>& in, int32_t n_shards, int
         }
         for (size_t g = 0; g < kmembers.size(); ++g) {
             const Task& t0 = s->tasks[kmembers[g][0]];
-            KvGroup kgp{t0.kv_off, t0.kv_len, (int32_t)s->kv_group_tasks.size(), (int32_t)kmembers[g].size(), 0, {0, 0, 0}};
+            KvGroup kgp{t0.kv_off, t0.kv_len, (int32_t)s->kv_group_tasks.size(), (int32_t)kmembers[g].size(), 0, 0, {0, 0}};
             for (int32_t ti : kmembers[g]) {
                 s->kv_group_tasks.push_back(ti);
                 kgp.n_q_tiles += (s->tasks[ti].q_len + kTileQ - 1) / kTileQ;
@@ -259,59 +332,167 @@ zl_status build_schedule(const std::vector<InputTask>& in, int32_t n_shards, int
         }
     }
 
-    // forward work list: (task, head of the task's range, query block), longest-first
-    for (size_t ti = 0; ti < s->tasks.size(); ++ti) {
-        const Task& t = s->tasks[ti];
-        for (int32_t h = s->task_head_begin[ti]; h < s->task_head_begin[ti] + s->task_head_count[ti]; ++h)
-            for (int32_t r = 0; r < t.q_len; r += kFwdBlockQ)
-                s->fwd_items.push_back({(int32_t)ti, h, r, std::min(kFwdBlockQ, t.q_len - r)});
-    }
-    std::stable_sort(s->fwd_items.begin(), s->fwd_items.end(), [&](const WorkItem& a, const WorkItem& b) {
-        const int32_t ka = s->tasks[a.unit].kv_len, kb = s->tasks[b.unit].kv_len;
-        if (ka != kb) return ka > kb;
-        if (a.rows != b.rows) return a.rows > b.rows;
-        return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
-    });
+    s->dq_rows = s->dq_acc_rows = s->q_pad_total;
+    finish_schedule(s);
+    return ZL_OK;
+}
 
-    // backward work list: (kv group, head of the group's range, key tile); cost = total query rows served
-    std::vector<int64_t> group_cost(s->kv_groups.size(), 0);
-    for (size_t g = 0; g < s->kv_groups.size(); ++g)
-        for (int32_t j = 0; j < s->kv_groups[g].n_tasks; ++j)
-            group_cost[g] += s->tasks[s->kv_group_tasks[s->kv_groups[g].task_begin + j]].q_len;
-    for (size_t g = 0; g < s->kv_groups.size(); ++g) {
-        const int32_t t0 = s->kv_group_tasks[s->kv_groups[g].task_begin];
-        for (int32_t h = s->task_head_begin[t0]; h < s->task_head_begin[t0] + s->task_head_count[t0]; ++h)
-            for (int32_t r = 0; r < s->kv_groups[g].kv_len; r += kTileKV)
-                s->bwd_items.push_back({(int32_t)g, h, r, std::min(kTileKV, s->kv_groups[g].kv_len - r)});
+zl_status build_prefix_schedule(const int32_t* cu_q, const int32_t* cu_kv, int32_t n_seqs, int32_t prefix_len,
+                                int32_t total_q, int32_t total_kv, int32_t n_heads, int32_t head_dim, Schedule* s) {
+    if (!s || n_seqs < 0 || prefix_len < 0 || total_q < 0 || total_kv < 0 || n_heads <= 0) return ZL_ERR_INVALID_ARG;
+    if (n_seqs > 0 && (!cu_q || !cu_kv)) return ZL_ERR_INVALID_ARG;
+    if (head_dim != 64 && head_dim != 128) return ZL_ERR_UNSUPPORTED;
+    if (n_seqs > 0 && (cu_q[0] != 0 || cu_kv[0] != 0)) return ZL_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < n_seqs; ++i)
+        if (cu_q[i + 1] < cu_q[i] || cu_kv[i + 1] < cu_kv[i]) return ZL_ERR_INVALID_ARG;
+    const int32_t batch = n_seqs > 0 ? cu_q[n_seqs] : 0;
+    if (batch > total_q || (int64_t)prefix_len + (n_seqs > 0 ? cu_kv[n_seqs] : 0) > total_kv) return ZL_ERR_INVALID_ARG;
+
+    *s = Schedule();
+    s->n_heads = n_heads; s->head_dim = head_dim; s->total_q = total_q; s->total_kv = total_kv;
+    s->shared_prefix = true;
+    s->shard_to_task.assign(n_seqs, -1);
+    s->shard_slot_off.assign(n_seqs, 0);
+    s->shard_slot_rows.assign(n_seqs, 0);
+    s->shard_kv_off.assign(n_seqs, 0);
+    s->shard_kv_len.assign(n_seqs, 0);
+    for (int32_t i = 0; i < n_seqs; ++i) {
+        s->shard_kv_off[i] = prefix_len + cu_kv[i];
+        s->shard_kv_len[i] = cu_kv[i + 1] - cu_kv[i];
     }
-    auto bwd_order = [&](const WorkItem& a, const WorkItem& b) {
-        if (group_cost[a.unit] != group_cost[b.unit]) return group_cost[a.unit] > group_cost[b.unit];
-        if (a.rows != b.rows) return a.rows > b.rows;
-        return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
+    s->merge_row_prefix.push_back(0);
+    if (batch == 0) { finish_schedule(s); return ZL_OK; }
+
+    auto push_task = [&](int32_t q_off, int32_t q_len, int32_t kv_off, int32_t kv_len) -> zl_status {
+        Task t{};
+        t.q_off = q_off; t.q_len = q_len; t.kv_off = kv_off; t.kv_len = kv_len;
+        t.kv_group = -1;
+        t.dq_slot = q_off;  // the accumulator holds the batch's rows once, whichever task adds to them
+        t.partial_slot = (int32_t)s->partial_rows;
+        s->partial_rows += align_up((size_t)q_len, kTileQ);
+        if (s->partial_rows > INT32_MAX) return ZL_ERR_INVALID_ARG;
+        if (kv_len > 0) {
+            t.kv_group = (int32_t)s->kv_groups.size();
+            s->kv_groups.push_back(KvGroup{kv_off, kv_len, (int32_t)s->kv_group_tasks.size(), 1, (q_len + kTileQ - 1) / kTileQ, 0, {0, 0}});
+            s->kv_group_tasks.push_back((int32_t)s->tasks.size());
+        }
+        s->tasks.push_back(t);
+        s->task_head_begin.push_back(0);
+        s->task_head_count.push_back(n_heads);
+        return ZL_OK;
     };
-    std::stable_sort(s->bwd_items.begin(), s->bwd_items.end(), bwd_order);
-    // the same list in units of two key tiles, for the CTA-pair form of the main kernel
-    for (size_t g = 0; g < s->kv_groups.size(); ++g) {
-        const int32_t t0 = s->kv_group_tasks[s->kv_groups[g].task_begin];
-        for (int32_t h = s->task_head_begin[t0]; h < s->task_head_begin[t0] + s->task_head_count[t0]; ++h)
-            for (int32_t r = 0; r < s->kv_groups[g].kv_len; r += 2 * kTileKV)
-                s->bwd_pair_items.push_back({(int32_t)g, h, r, std::min(2 * kTileKV, s->kv_groups[g].kv_len - r)});
+    auto push_q_group = [&](int32_t q_off, int32_t q_len) -> zl_status {
+        QGroup g{};
+        g.q_off = q_off; g.q_len = q_len; g.slot = (int32_t)s->q_pad_total; g.pad = (int32_t)align_up((size_t)q_len, kTileQ);
+        g.head_begin = 0; g.head_count = n_heads;
+        s->q_groups.push_back(g);
+        s->q_pad_total += g.pad;
+        return s->q_pad_total > INT32_MAX ? ZL_ERR_INVALID_ARG : ZL_OK;
+    };
+    // The whole batch is one query range over the prefix, cut into chunks along the keys so that its (head, row
+    // block, chunk) items fill the SMs; chunks are whole pairs of key tiles.
+    zl_status st = push_q_group(0, batch);
+    if (st != ZL_OK) return st;
+    const int64_t blocks = (int64_t)n_heads * ((batch + kFwdBlockQ - 1) / kFwdBlockQ);
+    const int64_t want = std::max<int64_t>(1, kPrefixItems / blocks);
+    const int64_t most = std::max<int64_t>(1, prefix_len / kPrefixChunkMin);
+    const int64_t chunk = (int64_t)align_up((size_t)((prefix_len + std::min(want, most) - 1) / std::min(want, most)), 2 * kTileKV);
+    int32_t n_chunks = 0;
+    for (int64_t k = 0; k < prefix_len; k += chunk, ++n_chunks) {
+        st = push_task(0, batch, (int32_t)k, (int32_t)std::min<int64_t>(chunk, prefix_len - k));
+        if (st != ZL_OK) return st;
     }
-    std::stable_sort(s->bwd_pair_items.begin(), s->bwd_pair_items.end(), bwd_order);
+    for (int32_t i = 0; i < n_seqs; ++i) {
+        const int32_t ql = cu_q[i + 1] - cu_q[i], kl = cu_kv[i + 1] - cu_kv[i];
+        if (ql == 0) continue;
+        MergeGroup mg{};
+        mg.q_off = cu_q[i]; mg.q_len = ql;
+        mg.part_begin = (int32_t)s->merge_parts.size();
+        mg.head_begin = 0; mg.head_count = n_heads;
+        for (int32_t c = 0; c < n_chunks; ++c) s->merge_parts.push_back(s->tasks[c].partial_slot + cu_q[i]);
+        if (kl > 0 || n_chunks == 0) {  // a row without any key still gets its empty partial
+            const int32_t ti = (int32_t)s->tasks.size();
+            st = push_task(cu_q[i], ql, prefix_len + cu_kv[i], kl);
+            if (st != ZL_OK) return st;
+            s->shard_to_task[i] = ti;
+            s->shard_slot_off[i] = s->tasks[ti].partial_slot;
+            s->shard_slot_rows[i] = (int32_t)align_up((size_t)ql, kTileQ);
+            s->merge_parts.push_back(s->tasks[ti].partial_slot);
+            s->tasks[ti].q_slot = (int32_t)s->q_pad_total;
+            st = push_q_group(cu_q[i], ql);
+            if (st != ZL_OK) return st;
+        }
+        mg.n_parts = (int32_t)s->merge_parts.size() - mg.part_begin;
+        s->merge_groups.push_back(mg);
+        s->merge_row_prefix.push_back(s->merge_row_prefix.back() + ql);
+    }
+    // Only the batch's own rows (the first query group) are accumulated and converted.  A ragged tile of a nested range
+    // adds zeros to the rows that follow it, up to one tile past the batch.
+    s->dq_rows = s->q_groups[0].pad;
+    s->dq_acc_rows = s->dq_rows + kTileQ;
+    finish_schedule(s);
+    return ZL_OK;
+}
 
-    // one launch phase until the caller says otherwise
-    s->fwd_task_phase.assign(s->tasks.size(), 0);
-    s->bwd_group_phase.assign(s->kv_groups.size(), 0);
-    s->fwd_phase_begin = {0, (int32_t)s->fwd_items.size()};
-    s->bwd_phase_begin = {0, (int32_t)s->bwd_items.size()};
-    s->bwd_pair_phase_begin = {0, (int32_t)s->bwd_pair_items.size()};
+zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard_pos* shard_pos) {
+    const size_t n_shards = s->shard_to_task.size();
+    if (n_shards > 0 && !shard_pos) return ZL_ERR_INVALID_ARG;
+    // chunks of a shared prefix come before every sequence's own keys: seen by all
+    std::vector<TaskPos> pos(s->tasks.size(), TaskPos{0, 0, s->shared_prefix ? INT32_MAX : 0, 0});
+    for (size_t i = 0; i < s->whole_to_task.size(); ++i) {
+        const int32_t prefix = whole_prefix ? whole_prefix[i] : 0;
+        if (prefix < 0) return ZL_ERR_INVALID_ARG;
+        if (s->whole_to_task[i] >= 0) pos[s->whole_to_task[i]].prefix = prefix;
+    }
+    std::vector<char> placed(s->tasks.size(), 0);
+    for (size_t i = 0; i < n_shards; ++i) {
+        const zl_shard_pos& sp = shard_pos[i];
+        if (sp.q_pos < 0 || sp.kv_pos < 0 || sp.prefix < 0) return ZL_ERR_INVALID_ARG;
+        const int32_t ti = s->shard_to_task[i];
+        if (ti < 0 || s->shard_kv_len[i] == 0) continue;
+        const Task& t = s->tasks[ti];
+        const int64_t kv_pos = (int64_t)sp.kv_pos - (s->shard_kv_off[i] - t.kv_off);  // a fused task starts where its first chunk does
+        if (kv_pos < 0 || (int64_t)sp.q_pos + t.q_len > kMaxPos || kv_pos + t.kv_len > kMaxPos) return ZL_ERR_INVALID_ARG;
+        const TaskPos tp{sp.q_pos, (int32_t)kv_pos, sp.prefix, 0};
+        if (placed[ti] && (pos[ti].q_pos != tp.q_pos || pos[ti].kv_pos != tp.kv_pos || pos[ti].prefix != tp.prefix))
+            return ZL_ERR_INVALID_ARG;  // the chunks of a fused task are one stretch of one sequence
+        pos[ti] = tp;
+        placed[ti] = 1;
+    }
+    s->task_pos = std::move(pos);
 
-    // backward workspace over the padded query slots: fp32 dQ accumulator [q_pad, H, d], then one
-    // 4 KB "augmentation" tile per (head, 128-row query tile) holding -LSE/scale and -D split
-    // into bf16 pieces (see the backward preprocess kernel)
-    s->ws_dq_acc_off = 0;
-    s->ws_aug_off = align_up((size_t)s->q_pad_total * n_heads * head_dim * sizeof(float), 256);
-    s->bwd_workspace_bytes = s->ws_aug_off + align_up((size_t)(s->q_pad_total / kTileQ) * n_heads * 4096, 256);
+    // the same items, ordered by what the mask leaves of them
+    auto by_work = [](std::vector<WorkItem>* items, const std::vector<int64_t>& work) {
+        std::vector<int32_t> order(items->size());
+        for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
+        std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return work[a] > work[b]; });
+        std::vector<WorkItem> sorted(items->size());
+        for (size_t i = 0; i < order.size(); ++i) sorted[i] = (*items)[order[i]];
+        items->swap(sorted);
+    };
+    s->fwd_items_masked = s->fwd_items;
+    std::vector<int64_t> work;
+    for (const WorkItem& w : s->fwd_items_masked) {
+        const Task& t = s->tasks[w.unit];
+        int64_t tiles = 0;
+        for (int32_t r = 0; r < w.rows; r += kTileQ)
+            tiles += (visible_keys(s->task_pos[w.unit], t.kv_len, w.row0 + std::min(w.rows, r + kTileQ) - 1) + kTileKV - 1) / kTileKV;
+        work.push_back(tiles);
+    }
+    by_work(&s->fwd_items_masked, work);
+    s->bwd_items_masked = s->bwd_items;
+    work.clear();
+    for (const WorkItem& w : s->bwd_items_masked) {
+        const KvGroup& g = s->kv_groups[w.unit];
+        int64_t tiles = 0;
+        for (int32_t j = 0; j < g.n_tasks; ++j) {
+            const int32_t ti = s->kv_group_tasks[g.task_begin + j];
+            const int32_t n = (s->tasks[ti].q_len + kTileQ - 1) / kTileQ;
+            tiles += n - std::min(n, first_query(s->task_pos[ti], w.row0) / kTileQ);
+        }
+        work.push_back(tiles);
+    }
+    by_work(&s->bwd_items_masked, work);
     return ZL_OK;
 }
 
