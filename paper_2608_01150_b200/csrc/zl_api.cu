@@ -446,18 +446,7 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         return ZL_ERR_INVALID_ARG;
     if (!(scale > 0.f) || !std::isfinite(scale)) return ZL_ERR_INVALID_ARG;
 
-    CUtensorMap tq, tk, tv, to, top;
     const int64_t hd = (int64_t)s.n_heads * s.head_dim;
-    if (!make_tmap(&tq, q, s.total_q, s.n_heads, s.head_dim, kTileQ, in_stride) ||
-        !make_tmap(&tk, k, s.total_kv, s.n_heads, s.head_dim, kTileKV, in_stride) ||
-        !make_tmap(&tv, v, s.total_kv, s.n_heads, s.head_dim, kTileKV, in_stride) ||
-        !make_tmap(&to, o, s.total_q, s.n_heads, s.head_dim, kTileQ, hd))
-        return ZL_ERR_CUDA;
-    // partial results leave through the same kind of store; without shards the map is never used
-    if (s.partial_rows > 0 ? !make_tmap_f32_acc(&top, o_partial, s.partial_rows, s.n_heads, s.head_dim, kTileQ)
-                           : !make_tmap(&top, o, s.total_q, s.n_heads, s.head_dim, kTileQ, hd))
-        return ZL_ERR_CUDA;
-
     FwdParams p{};
     p.tasks = t->d_tasks;
     p.items = t->d_fwd_items + item_begin;
@@ -472,17 +461,42 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     p.lse_partial = lse_partial;
     p.status = t->d_status;
     const int grid = std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
+    ScoreParams sp{};
     if (score) {
-        ScoreParams sp = score->params;
+        sp = score->params;
         sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
         if (sp.masked) p.items = t->d_fwd_items_masked;
-        LaunchTimer lt(t, ZL_K_FWD, static_cast<cudaStream_t>(stream));
-        if (launch_scored_fwd(s.head_dim, score->capped, score->biased ? kScoreBias : kScorePlain, tq, tk, tv, to, top, p, sp,
-                              grid, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+    }
+    const ScoreKind kind = score && score->biased ? kScoreBias : kScorePlain;
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    CUtensorMap tq, tk, tv, to, top;
+    if (!make_tmap(&tk, k, s.total_kv, s.n_heads, s.head_dim, kTileKV, in_stride) ||
+        !make_tmap(&tv, v, s.total_kv, s.n_heads, s.head_dim, kTileKV, in_stride))
+        return ZL_ERR_CUDA;
+    // Items of at most one query tile are bound by their keys' bytes and have a kernel of their own; plain calls on handles
+    // without a shared prefix keep the kernel (and the bits) they always had.
+    if ((score || s.shared_prefix) && s.max_item_rows <= kTileQ) {
+        const int box = (int)align_up((size_t)s.max_item_rows, 16);
+        if (!make_tmap(&tq, q, s.total_q, s.n_heads, s.head_dim, box, in_stride)) return ZL_ERR_CUDA;
+        LaunchTimer lt(t, ZL_K_FWD, cs);
+        if (launch_few_rows(s.head_dim, score && score->capped, kind, tq, tk, tv, box, p, sp, grid, cs) != cudaSuccess) return ZL_ERR_CUDA;
+        g_launches.fetch_add(1);
+        return ZL_OK;
+    }
+    if (!make_tmap(&tq, q, s.total_q, s.n_heads, s.head_dim, kTileQ, in_stride) ||
+        !make_tmap(&to, o, s.total_q, s.n_heads, s.head_dim, kTileQ, hd))
+        return ZL_ERR_CUDA;
+    // partial results leave through the same kind of store; without shards the map is never used
+    if (s.partial_rows > 0 ? !make_tmap_f32_acc(&top, o_partial, s.partial_rows, s.n_heads, s.head_dim, kTileQ)
+                           : !make_tmap(&top, o, s.total_q, s.n_heads, s.head_dim, kTileQ, hd))
+        return ZL_ERR_CUDA;
+    if (score) {
+        LaunchTimer lt(t, ZL_K_FWD, cs);
+        if (launch_scored_fwd(s.head_dim, score->capped, kind, tq, tk, tv, to, top, p, sp, grid, cs) != cudaSuccess)
             return ZL_ERR_CUDA;
     } else {
-        LaunchTimer lt(t, ZL_K_FWD, static_cast<cudaStream_t>(stream));
-        if (launch_fwd(s.head_dim, tq, tk, tv, to, top, p, grid, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+        LaunchTimer lt(t, ZL_K_FWD, cs);
+        if (launch_fwd(s.head_dim, tq, tk, tv, to, top, p, grid, cs) != cudaSuccess)
             return ZL_ERR_CUDA;
     }
     g_launches.fetch_add(1);
@@ -543,7 +557,8 @@ zl_status zl_lse_merge(const zl_tasks* t, const float* o_partial, const float* l
     for (const MergeGroup& mg : s.merge_groups) max_parts = std::max(max_parts, (int)mg.n_parts);
     {
         LaunchTimer lt(t, ZL_K_MERGE, static_cast<cudaStream_t>(stream));
-        if (launch_merge(s.head_dim, p, max_parts, t->n_sms, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+        if ((s.shared_prefix ? launch_merge_rows(s.head_dim, p, s.merge_row_prefix.back(), static_cast<cudaStream_t>(stream))
+                             : launch_merge(s.head_dim, p, max_parts, t->n_sms, static_cast<cudaStream_t>(stream))) != cudaSuccess)
             return ZL_ERR_CUDA;
     }
     g_launches.fetch_add(1);

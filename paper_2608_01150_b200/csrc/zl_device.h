@@ -84,6 +84,10 @@ enum ScoreKind { kScorePlain = 0, kScoreBias = 1, kScoreBiasGrad = 2 };  // what
 cudaError_t launch_scored_fwd(int head_dim, bool capped, ScoreKind kind, const CUtensorMap& tq, const CUtensorMap& tk,
                               const CUtensorMap& tv, const CUtensorMap& to, const CUtensorMap& top, const FwdParams& p,
                               const ScoreParams& sp, int grid, cudaStream_t stream);
+// Items of at most 128 query rows, plain or scored; `q_box_rows`: rows of the tq box, a multiple of 16 that covers every item.
+cudaError_t launch_few_rows(int head_dim, bool capped, ScoreKind kind, const CUtensorMap& tq, const CUtensorMap& tk,
+                            const CUtensorMap& tv, int q_box_rows, const FwdParams& p, const ScoreParams& sp, int grid,
+                            cudaStream_t stream);
 cudaError_t launch_scored_bwd(int head_dim, bool capped, ScoreKind kind, const CUtensorMap& tq, const CUtensorMap& tk,
                               const CUtensorMap& tv, const CUtensorMap& tdo, const CUtensorMap& tdq, const CUtensorMap& tdk,
                               const CUtensorMap& tdv, const BwdParams& p, const ScoreParams& sp, int grid, cudaStream_t stream);
@@ -107,6 +111,8 @@ cudaError_t launch_fwd(int head_dim, const CUtensorMap& tq, const CUtensorMap& t
                        cudaStream_t stream);
 // `max_parts`: the largest number of parts of any merge group (selects a register-resident variant).
 cudaError_t launch_merge(int head_dim, const MergeParams& p, int max_parts, int n_sms, cudaStream_t stream);
+// The same merge for a batch over a shared prefix: few rows, many parts each.
+cudaError_t launch_merge_rows(int head_dim, const MergeParams& p, int64_t n_rows, cudaStream_t stream);
 cudaError_t launch_wait_selftest(int32_t* status, uint64_t limit_ns, cudaStream_t stream);
 
 }  // namespace zl

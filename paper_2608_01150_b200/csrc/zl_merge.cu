@@ -152,7 +152,83 @@ __global__ void __launch_bounds__(kMergeThreads, NP == 8 ? 3 : (NP == 4 ? 4 : 8)
     }
 }
 
+// The merge of a batch over a shared prefix: few rows (one token per sequence) with a part per chunk of the prefix and one
+// of their own.  One warp per (row, head): lane t fetches the LSE of part t, and the partial outputs are read eight parts
+// at a time, so a warp waits for memory about as often as it has eighths of parts, not three times per part.
+template <int D>
+__global__ void __launch_bounds__(128) zl_merge_rows_kernel(const MergeParams p, const int64_t n_rows) {
+    constexpr int V = D / 32;
+    constexpr int kBatch = 8;
+    const int lane = threadIdx.x & 31;
+    const int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    if (u >= n_rows * p.n_heads) return;
+    const int64_t r = u / p.n_heads;
+    const int h = (int)(u - r * p.n_heads);
+    int lo = 0, hi = p.n_groups;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.row_prefix[mid] <= r) lo = mid; else hi = mid;
+    }
+    const MergeGroup g = p.groups[lo];
+    const int row = (int)(r - p.row_prefix[lo]);
+    const int32_t* part = p.parts + g.part_begin;
+    const float* lse_h = p.lse_partial + (int64_t)h * p.partial_rows + row;
+    float M = -INFINITY;
+    for (int t = lane; t < g.n_parts; t += 32) M = fmaxf(M, __ldg(lse_h + __ldg(part + t)));
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    const int64_t part_stride = (int64_t)p.n_heads * D;
+    const float* src0 = p.o_partial + ((int64_t)row * p.n_heads + h) * D + lane * V;
+    float z = 0.f, acc[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+    for (int t0 = 0; t0 < g.n_parts; t0 += 32) {
+        const int mine = t0 + lane < g.n_parts ? __ldg(part + t0 + lane) : 0;
+        const float w = t0 + lane < g.n_parts && M > -INFINITY ? __expf(__ldg(lse_h + mine) - M) : 0.f;
+        z += w;
+        const int n = min(32, g.n_parts - t0);
+        for (int b = 0; b < n; b += kBatch) {
+            alignas(16) float x[kBatch][V];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int slot = __shfl_sync(0xffffffffu, mine, min(b + k, 31));
+                const float* src = src0 + slot * part_stride;
+                if (b + k < n) {
+                    if constexpr (V == 4) *reinterpret_cast<float4*>(x[k]) = __ldcs(reinterpret_cast<const float4*>(src));
+                    else *reinterpret_cast<float2*>(x[k]) = __ldcs(reinterpret_cast<const float2*>(src));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const float wk = __shfl_sync(0xffffffffu, w, min(b + k, 31));
+                if (b + k < n) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[i] = fmaf(wk, x[k][i], acc[i]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) z += __shfl_xor_sync(0xffffffffu, z, off);
+    const float inv_z = z > 0.f ? 1.f / z : 0.f;
+    const int64_t qrow = (int64_t)g.q_off + row;
+    __nv_bfloat16* dst = p.o + (qrow * p.n_heads + h) * D + lane * V;
+#pragma unroll
+    for (int i = 0; i < V; i += 2)
+        reinterpret_cast<__nv_bfloat162*>(dst)[i / 2] = __floats2bfloat162_rn(acc[i] * inv_z, acc[i + 1] * inv_z);
+    if (lane == 0) p.lse[(int64_t)h * p.total_q + qrow] = M > -INFINITY ? M + logf(z) : -INFINITY;
+}
+
 }  // namespace
+
+cudaError_t launch_merge_rows(int head_dim, const MergeParams& p, int64_t n_rows, cudaStream_t stream) {
+    if (p.n_groups == 0) return cudaSuccess;
+    const int64_t grid = (n_rows * p.n_heads + 3) / 4;
+    if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
+    if (head_dim == 128) zl_merge_rows_kernel<128><<<(unsigned)grid, 128, 0, stream>>>(p, n_rows);
+    else zl_merge_rows_kernel<64><<<(unsigned)grid, 128, 0, stream>>>(p, n_rows);
+    return cudaGetLastError();
+}
 
 cudaError_t launch_merge(int head_dim, const MergeParams& p, int max_parts, int n_sms, cudaStream_t stream) {
     if (p.n_groups == 0) return cudaSuccess;

@@ -57,16 +57,6 @@ __device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_
 }
 
 
-// Key tiles that the query tile of an item starting at row `row0` with `rows` rows walks over.
-__device__ __forceinline__ int key_tiles(const ScoreParams& sp, const Task& t, int task, int row0, int rows) {
-    if (rows <= 0) return 0;
-    const int keys = sp.masked ? visible_keys(task_pos(sp, task), t.kv_len, row0 + rows - 1) : t.kv_len;
-    return (keys + kTileKV - 1) / kTileKV;
-}
-
-// Distances of a 32 x 128 patch: 32 + 128 - 1, rounded up to a multiple of 32.
-constexpr int kWindow = 160;
-
 // Wait used by a single elected thread.
 #define ZL_WAIT(bar, parity, site)                                        \
     do {                                                                  \
@@ -325,74 +315,8 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     }
                 }
                 tmem_wait_ld();
-                if constexpr (kCap) {
-                    float big = 0.f;
-#pragma unroll
-                    for (int c = 0; c < kTileKV; c += 2) big = max3_abs(big, sv[c], sv[c + 1]);
-                    const float2 k1 = splat(sp.scale_over_cap), cl = splat(sp.cap_log2);
-                    if (__all_sync(0xffffffffu, big * sp.scale_over_cap <= kTanhRange)) {
-#pragma unroll
-                        for (int c = 0; c < kTileKV; c += 2) {
-                            const float2 v = mul2(tanh_near(mul2(make_float2(sv[c], sv[c + 1]), k1)), cl);
-                            sv[c] = v.x;
-                            sv[c + 1] = v.y;
-                        }
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < kTileKV; ++c) sv[c] = tanh_any(sv[c] * sp.scale_over_cap) * sp.cap_log2;
-                    }
-                }
-                if constexpr (kBias) {
-                    const float mul = kCap ? 1.f : p.scale_log2;
-                    if (side == kNear) {
-                        const float* w = window + 31 - lane;
-#pragma unroll
-                        for (int c = 0; c < kTileKV; c += 2) {
-                            const float2 v = fma2(make_float2(sv[c], sv[c + 1]), splat(mul), make_float2(w[c], w[c + 1]));
-                            sv[c] = v.x;
-                            sv[c + 1] = v.y;
-                        }
-                    } else {
-                        const float step = side == kFarPos ? -hb.slope : hb.slope;
-                        const float base = (side == kFarPos ? hb.far_pos : hb.far_neg) + step * (float)(dist_lo + 31 - lane);
-                        if (step == 0.f) {  // warp-uniform
-#pragma unroll
-                            for (int c = 0; c < kTileKV; c += 2) {
-                                const float2 v = fma2(make_float2(sv[c], sv[c + 1]), splat(mul), splat(base));
-                                sv[c] = v.x;
-                                sv[c + 1] = v.y;
-                            }
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < kTileKV; c += 2) {
-                                const float2 b = make_float2(fmaf(step, (float)c, base), fmaf(step, (float)(c + 1), base));
-                                const float2 v = fma2(make_float2(sv[c], sv[c + 1]), splat(mul), b);
-                                sv[c] = v.x;
-                                sv[c + 1] = v.y;
-                            }
-                        }
-                    }
-                }
-                const int valid = keys - j * kTileKV;  // columns of this tile that the row sees
-                if (__any_sync(0xffffffffu, valid < kTileKV)) {
-#pragma unroll
-                    for (int c = 0; c < kTileKV; ++c)
-                        if (c >= valid) sv[c] = -INFINITY;  // select, never multiply
-                }
-                // four independent chains: a single running maximum is a 64-deep dependent chain
-                float mx0 = max3(sv[0], sv[1], sv[2]), mx1 = max3(sv[3], sv[4], sv[5]);
-                float mx2 = max3(sv[6], sv[7], sv[8]), mx3 = max3(sv[9], sv[10], sv[11]);
-#pragma unroll
-                for (int c = 12; c + 7 < kTileKV; c += 8) {
-                    mx0 = max3(mx0, sv[c], sv[c + 1]);
-                    mx1 = max3(mx1, sv[c + 2], sv[c + 3]);
-                    mx2 = max3(mx2, sv[c + 4], sv[c + 5]);
-                    mx3 = max3(mx3, sv[c + 6], sv[c + 7]);
-                }
-                // columns 124..127 remain (12 + 8 * 14 = 124)
-                mx0 = max3(mx0, sv[kTileKV - 4], sv[kTileKV - 3]);
-                mx1 = max3(mx1, sv[kTileKV - 2], sv[kTileKV - 1]);
-                const float mx = fmaxf(max3(mx0, mx1, mx2), mx3);
+                finish_scores<kCap, kBias>(sv, sp, hb, side, window, dist_lo, p.scale_log2, keys - j * kTileKV, lane);
+                const float mx = row_max(sv);
                 // lazy reference update: only when the tile maximum is far above the reference; a row that has seen no
                 // key yet has reference -inf, and so long as it sees none (mx = -inf, the difference is NaN) keeps it
                 const bool raise = (mx - m_ref) * sl2 > kRescaleThresholdLog2;

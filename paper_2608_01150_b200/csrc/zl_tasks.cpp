@@ -61,10 +61,21 @@ bool ranges_consistent(const std::vector<Range>& rng, const std::vector<HeadRang
     return true;
 }
 
-// A shared prefix is cut so that it gives about this many forward items (two per SM of a B200), but into chunks of no
-// fewer than kPrefixChunkMin keys: a chunk's partial row costs as much traffic as two key rows.
-constexpr int64_t kPrefixItems = 2 * 148;
-constexpr int64_t kPrefixChunkMin = 512;
+// Keys of a shared prefix per chunk, a whole number of key tiles.  `blocks` (head, row block) items per chunk run on the SMs
+// of a B200 in rounds; an item costs its key tiles and about two more to begin and to end (Q, the first S, the join, the
+// partial output).  Of the numbers of chunks with the least total, the smallest; a chunk has 512 keys at least, because a
+// partial row costs as much traffic as two key rows.
+int64_t prefix_chunk(int64_t blocks, int64_t prefix_len) {
+    constexpr int64_t kSms = 148, kItemTiles = 2, kMinKeys = 512, kMaxChunks = 256;
+    const int64_t most = std::min<int64_t>(kMaxChunks, std::max<int64_t>(1, prefix_len / kMinKeys));
+    int64_t best = 0, best_cost = INT64_MAX;
+    for (int64_t n = 1; n <= most; ++n) {
+        const int64_t chunk = (int64_t)align_up((size_t)((prefix_len + n - 1) / n), kTileKV);
+        const int64_t cost = ((blocks * n + kSms - 1) / kSms) * (chunk / kTileKV + kItemTiles);
+        if (cost < best_cost) { best_cost = cost; best = chunk; }
+    }
+    return std::max<int64_t>(best, kTileKV);
+}
 
 // Positions leave room for the padded rows of a last tile in 32-bit arithmetic.
 constexpr int64_t kMaxPos = INT32_MAX - 4 * 128;
@@ -91,6 +102,8 @@ void finish_schedule(Schedule* s) {
         if (a.rows != b.rows) return a.rows > b.rows;
         return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
     });
+
+    for (const WorkItem& w : s->fwd_items) s->max_item_rows = std::max(s->max_item_rows, w.rows);
 
     // backward work list: (kv group, head of the group's range, key tile); cost = total query rows served
     std::vector<int64_t> group_cost(s->kv_groups.size(), 0);
@@ -390,13 +403,10 @@ zl_status build_prefix_schedule(const int32_t* cu_q, const int32_t* cu_kv, int32
         return s->q_pad_total > INT32_MAX ? ZL_ERR_INVALID_ARG : ZL_OK;
     };
     // The whole batch is one query range over the prefix, cut into chunks along the keys so that its (head, row
-    // block, chunk) items fill the SMs; chunks are whole pairs of key tiles.
+    // block, chunk) items fill the SMs.
     zl_status st = push_q_group(0, batch);
     if (st != ZL_OK) return st;
-    const int64_t blocks = (int64_t)n_heads * ((batch + kFwdBlockQ - 1) / kFwdBlockQ);
-    const int64_t want = std::max<int64_t>(1, kPrefixItems / blocks);
-    const int64_t most = std::max<int64_t>(1, prefix_len / kPrefixChunkMin);
-    const int64_t chunk = (int64_t)align_up((size_t)((prefix_len + std::min(want, most) - 1) / std::min(want, most)), 2 * kTileKV);
+    const int64_t chunk = prefix_chunk((int64_t)n_heads * ((batch + kFwdBlockQ - 1) / kFwdBlockQ), prefix_len);
     int32_t n_chunks = 0;
     for (int64_t k = 0; k < prefix_len; k += chunk, ++n_chunks) {
         st = push_task(0, batch, (int32_t)k, (int32_t)std::min<int64_t>(chunk, prefix_len - k));

@@ -174,7 +174,7 @@ def test_prefix_schedule_covers_every_pair_once(qlens, klens, P, H):
 def test_prefix_chunks_fill_the_gpu_for_few_rows():
     h = _prefix_handle([1] * 64, [1] * 64, 32760, 12)
     n_prefix = sum(1 for t, _, _, _ in h.fwd_items()) - 64 * 12
-    assert 148 <= n_prefix <= 2 * 148 + 12
+    assert 0.9 * 148 <= n_prefix <= 2 * 148   # one or two rounds of the 148 SMs, or nearly
 
 
 @pytest.mark.parametrize("cu_q,cu_kv,P,tq,tk,H,d", [
