@@ -14,6 +14,8 @@
 //   * warps without a valid row only take part in the barriers.
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "zl_score.cuh"
 
 namespace zl {
@@ -38,7 +40,7 @@ struct FewSmem {
     alignas(1024) uint8_t q[2][kRows * D * 2];  // followed by K: an MMA reads 128 rows from here on
     alignas(1024) uint8_t k[kStagesK][kTileBytes];
     alignas(1024) uint8_t v[kStagesV][kTileBytes];
-    float window[8][kWindow];  // per softmax warp: the biases of a near patch
+    alignas(16) float window[8][kWindowFloats];  // per softmax warp: the biases of a near patch
     float2 stat[2][kTileQ];    // per warpgroup and row: reference maximum (powers of two) and sum
     alignas(8) uint64_t q_full[2], q_empty[2];
     uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
@@ -211,8 +213,6 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int row = quarter * 32 + lane;       // query row within the tile
         const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
         const uint32_t col_s = kColS + x * 128, col_o = kColO + x * 128;
-        constexpr bool kLog2 = kCap || kBias;
-        const float sl2 = kLog2 ? 1.f : p.scale_log2;
         float* const window = sm.window[warp - 4];
         uint32_t s_cnt = 0, o_cnt[2] = {0, 0};
         for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
@@ -254,20 +254,15 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     for (int i = 0; i < 32; ++i) sv[c * 32 + i] = __uint_as_float(r[i]);
                 }
                 if constexpr (kBias) {
-                    if (side == kNear) {
-                        __syncwarp();  // the previous patch has been read
-#pragma unroll
-                        for (int i = 0; i < kWindow / 32; ++i) window[i * 32 + lane] = near_bias[i];
-                        __syncwarp();
-                    }
+                    if (side == kNear) fill_window(window, near_bias, lane);
                 }
                 tmem_wait_ld();
-                finish_scores<kCap, kBias>(sv, sp, hb, side, window, dist_lo, p.scale_log2, keys - j * kTileKV, lane);
-                const float mx = row_max(sv);
-                const bool raise = row_ok && (mx - m_ref) * sl2 > kRescaleThresholdLog2;
+                const RowScore rs = finish_scores<kCap, kBias>(sv, sp, hb, side, window, dist_lo, p.scale_log2, keys - j * kTileKV, lane);
+                const float mx = rs.max;
+                const bool raise = row_ok && mx - m_ref > kRescaleThresholdLog2;
                 if (__any_sync(0xffffffffu, raise && j > x)) {
                     // rescale O (the previous P V product is complete: S(j) was issued after it)
-                    const float alpha = raise ? ex2((m_ref - mx) * sl2) : 1.f;
+                    const float alpha = raise ? ex2(m_ref - mx) : 1.f;
 #pragma unroll
                     for (int c = 0; c < D / 32; ++c) {
                         uint32_t r[32];
@@ -283,16 +278,16 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     if (j == x) l = 0.f;
                     m_ref = mx;
                 }
-                const float nmb = m_ref > -INFINITY ? -m_ref * sl2 : 0.f;
+                const float add = rs.base - (m_ref > -INFINITY ? m_ref : 0.f);
                 float2 sum2 = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {  // P goes to the MMA warp in two halves of 64 key columns
+                // P goes to the MMA warp in two halves of 64 key columns
+                auto half_of_p = [&](int h, auto linear) {
                     uint32_t pk[kTileKV / 4];
 #pragma unroll
                     for (int c = 0; c < kTileKV / 2; c += 2) {
                         const int cc = h * (kTileKV / 2) + c;
-                        const float2 e = kLog2 ? add2(make_float2(sv[cc], sv[cc + 1]), splat(nmb))
-                                               : fma2(make_float2(sv[cc], sv[cc + 1]), splat(sl2), splat(nmb));
+                        const float2 b = decltype(linear)::value ? make_float2(fmaf(rs.step, (float)cc, add), fmaf(rs.step, (float)(cc + 1), add)) : splat(add);
+                        const float2 e = fma2(make_float2(sv[cc], sv[cc + 1]), splat(rs.mul), b);
                         const float p0 = ex2(e.x), p1 = ex2(e.y);
                         sum2 = add2(sum2, make_float2(p0, p1));
                         pk[c / 2] = pack_bf16(p0, p1);
@@ -301,6 +296,13 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(&sm.p_half[x][h]);
+                };
+                if (kBias && rs.step != 0.f) {  // warp-uniform
+                    half_of_p(0, std::true_type());
+                    half_of_p(1, std::true_type());
+                } else {
+                    half_of_p(0, std::false_type());
+                    half_of_p(1, std::false_type());
                 }
                 l += sum2.x + sum2.y;
             }
@@ -313,7 +315,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         ++o_cnt[y];
                     }
                 tc_fence_after();
-                sm.stat[x][row] = make_float2(m_ref * sl2, l);
+                sm.stat[x][row] = make_float2(m_ref, l);
                 named_bar_sync(2, 256);
                 const float2 a = sm.stat[0][row], b = sm.stat[1][row];
                 const float m = fmaxf(a.x, b.x);

@@ -81,24 +81,57 @@ __device__ __forceinline__ int key_tiles(const ScoreParams& sp, const Task& t, i
     return (keys + kTileKV - 1) / kTileKV;
 }
 
-// Distances of a 32 x 128 patch: 32 + 128 - 1, rounded up to a multiple of 32.
+// Distances of a 32 x 128 patch: 32 + 128 - 1, rounded up to a multiple of 32.  A warp's window holds their biases four
+// times, copy s shifted by s: a thread's 128 consecutive biases start at 31 - lane, and in copy (31 - lane) % 4 that start
+// is 16-byte aligned, so the row is 32 four-word loads instead of 128 single ones.  Copies lie 8 banks apart, which keeps
+// the eight lanes of a load phase on different banks.
 constexpr int kWindow = 160;
+constexpr int kWindowStride = 168;
+constexpr int kWindowFloats = 4 * kWindowStride;
 
-// Turns a row of raw products into scores: the cap, the bias, -inf from column `valid` on.  With a cap or a bias the
-// result is in powers of two, else it stays the raw product (the exponential's multiply-add scales it).  `window` holds
-// the biases of a near patch, `dist_lo` is the distance of the patch's last row to its first column.
+__device__ __forceinline__ void fill_window(float* window, const float (&bias)[kWindow / 32], int lane) {
+    __syncwarp();  // the previous patch has been read
+#pragma unroll
+    for (int i = 0; i < kWindow / 32; ++i) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            if (i * 32 + lane >= s) window[s * kWindowStride + i * 32 + lane - s] = bias[i];
+    }
+    __syncwarp();
+}
+
+// How the exponent of a tile's row follows from its values: score(c) = v[c] * mul + base + step * c, in powers of two.
+struct RowScore {
+    float mul, base, step;
+    float max;  // of the row's scores, or an upper bound
+};
+// An upper bound serves as the softmax's reference so long as it is not far above: 2^-kSlack of the reference still leaves
+// 2^60 to the smallest fp32 number, so nothing that counts is lost, and sums and LSE are exact relative to any reference.
+constexpr float kSlack = 64.f;
+
+__device__ __forceinline__ float row_max(const float (&sv)[kTileKV]);
+
+// Turns a row of raw products into values with `mul`, `base` and `step`: the cap and near biases change the values, a far
+// bias (linear in the column) only base and step; columns from `valid` on become -inf.  `window` holds the biases of a near
+// patch, `dist_lo` is the distance of the patch's last row to its first column.
 template <bool kCap, bool kBias>
-__device__ __forceinline__ void finish_scores(float (&sv)[kTileKV], const ScoreParams& sp, const HeadBias& hb, PatchSide side,
-                                              const float* window, int dist_lo, float scale_log2, int valid, int lane) {
+__device__ __forceinline__ RowScore finish_scores(float (&sv)[kTileKV], const ScoreParams& sp, const HeadBias& hb, PatchSide side,
+                                                  const float* window, int dist_lo, float scale_log2, int valid, int lane) {
+    RowScore rs{scale_log2, 0.f, 0.f, 0.f};
     if constexpr (kCap) {
+        rs.mul = 1.f;
         float big = 0.f;
 #pragma unroll
         for (int c = 0; c < kTileKV; c += 2) big = max3_abs(big, sv[c], sv[c + 1]);
-        const float2 k1 = splat(sp.scale_over_cap), cl = splat(sp.cap_log2);
         if (__all_sync(0xffffffffu, big * sp.scale_over_cap <= kTanhRange)) {
+            const float2 k1 = splat(sp.scale_over_cap);
+            const float2 c0 = splat(kTanhC0 * sp.cap_log2), c1 = splat(kTanhC1 * sp.cap_log2), c2 = splat(kTanhC2 * sp.cap_log2),
+                         c3 = splat(kTanhC3 * sp.cap_log2), c4 = splat(kTanhC4 * sp.cap_log2);
 #pragma unroll
             for (int c = 0; c < kTileKV; c += 2) {
-                const float2 v = mul2(tanh_near(mul2(make_float2(sv[c], sv[c + 1]), k1)), cl);
+                const float2 y = mul2(make_float2(sv[c], sv[c + 1]), k1);
+                const float2 z = mul2(y, y);
+                const float2 v = mul2(y, fma2(z, fma2(z, fma2(z, fma2(z, c4, c3), c2), c1), c0));
                 sv[c] = v.x;
                 sv[c + 1] = v.y;
             }
@@ -108,33 +141,27 @@ __device__ __forceinline__ void finish_scores(float (&sv)[kTileKV], const ScoreP
         }
     }
     if constexpr (kBias) {
-        const float mul = kCap ? 1.f : scale_log2;
         if (side == kNear) {
-            const float* w = window + 31 - lane;
+            const int start = 31 - lane;
+            const float4* w = reinterpret_cast<const float4*>(window + (start & 3) * kWindowStride + (start & ~3));
 #pragma unroll
-            for (int c = 0; c < kTileKV; c += 2) {
-                const float2 v = fma2(make_float2(sv[c], sv[c + 1]), splat(mul), make_float2(w[c], w[c + 1]));
-                sv[c] = v.x;
-                sv[c + 1] = v.y;
+            for (int c = 0; c < kTileKV; c += 4) {
+                const float4 b = w[c / 4];
+                const float2 v0 = fma2(make_float2(sv[c], sv[c + 1]), splat(rs.mul), make_float2(b.x, b.y));
+                const float2 v1 = fma2(make_float2(sv[c + 2], sv[c + 3]), splat(rs.mul), make_float2(b.z, b.w));
+                sv[c] = v0.x;
+                sv[c + 1] = v0.y;
+                sv[c + 2] = v1.x;
+                sv[c + 3] = v1.y;
             }
+            rs.mul = 1.f;
         } else {
-            const float step = side == kFarPos ? -hb.slope : hb.slope;
-            const float base = (side == kFarPos ? hb.far_pos : hb.far_neg) + step * (float)(dist_lo + 31 - lane);
-            if (step == 0.f) {  // warp-uniform
+            rs.step = side == kFarPos ? -hb.slope : hb.slope;
+            rs.base = (side == kFarPos ? hb.far_pos : hb.far_neg) + rs.step * (float)(dist_lo + 31 - lane);
+            if (fabsf(rs.step) * (kTileKV - 1) > kSlack) {  // warp-uniform: steep slopes get their exact maximum
 #pragma unroll
-                for (int c = 0; c < kTileKV; c += 2) {
-                    const float2 v = fma2(make_float2(sv[c], sv[c + 1]), splat(mul), splat(base));
-                    sv[c] = v.x;
-                    sv[c + 1] = v.y;
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < kTileKV; c += 2) {
-                    const float2 b = make_float2(fmaf(step, (float)c, base), fmaf(step, (float)(c + 1), base));
-                    const float2 v = fma2(make_float2(sv[c], sv[c + 1]), splat(mul), b);
-                    sv[c] = v.x;
-                    sv[c + 1] = v.y;
-                }
+                for (int c = 0; c < kTileKV; ++c) sv[c] = fmaf(sv[c], rs.mul, fmaf(rs.step, (float)c, rs.base));
+                rs = RowScore{1.f, 0.f, 0.f, 0.f};
             }
         }
     }
@@ -143,6 +170,8 @@ __device__ __forceinline__ void finish_scores(float (&sv)[kTileKV], const ScoreP
         for (int c = 0; c < kTileKV; ++c)
             if (c >= valid) sv[c] = -INFINITY;  // select, never multiply
     }
+    rs.max = fmaf(row_max(sv), rs.mul, rs.base + fmaxf(0.f, rs.step * (kTileKV - 1)));
+    return rs;
 }
 
 __device__ __forceinline__ float row_max(const float (&sv)[kTileKV]) {

@@ -17,6 +17,8 @@
 //     else two special-function operations: see zl_score.cuh.
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "zl_score.cuh"
 
 namespace zl {
@@ -261,10 +263,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         uint32_t s_cnt = 0, o_cnt = 0;
         const bool store_leader = quarter == 0 && lane == 0;  // one thread per warpgroup issues its TMA stores
         bool store_pending = false;                            // this warpgroup's box may still be read by a store
-        // scores in powers of two once a cap or a bias has been applied, else raw products times sl2
-        constexpr bool kLog2 = kCap || kBias;
-        const float sl2 = kLog2 ? 1.f : p.scale_log2;
-        float* const window = reinterpret_cast<float*>(sm.o_stage[x]) + quarter * kWindow;
+        float* const window = reinterpret_cast<float*>(sm.o_stage[x]) + quarter * kWindowFloats;
         for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
             const WorkItem wi = p.items[it];
             const int tile_rows = min(kTileQ, wi.rows - x * kTileQ);  // rows of this warpgroup's tile
@@ -283,7 +282,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     store_pending = false;
                 }
             }
-            float m_ref = -INFINITY, l = 0.f;  // reference maximum (score units) and row sum
+            float m_ref = -INFINITY, l = 0.f;  // reference maximum (powers of two) and row sum
             for (int j = 0; j < n_kv; ++j) {
                 PatchSide side = kNear;
                 float near_bias[kWindow / 32];
@@ -307,22 +306,17 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     for (int i = 0; i < 32; ++i) sv[c * 32 + i] = __uint_as_float(r[i]);
                 }
                 if constexpr (kBias) {
-                    if (side == kNear) {
-                        __syncwarp();  // the previous patch has been read
-#pragma unroll
-                        for (int i = 0; i < kWindow / 32; ++i) window[i * 32 + lane] = near_bias[i];
-                        __syncwarp();
-                    }
+                    if (side == kNear) fill_window(window, near_bias, lane);
                 }
                 tmem_wait_ld();
-                finish_scores<kCap, kBias>(sv, sp, hb, side, window, dist_lo, p.scale_log2, keys - j * kTileKV, lane);
-                const float mx = row_max(sv);
+                const RowScore rs = finish_scores<kCap, kBias>(sv, sp, hb, side, window, dist_lo, p.scale_log2, keys - j * kTileKV, lane);
+                const float mx = rs.max;
                 // lazy reference update: only when the tile maximum is far above the reference; a row that has seen no
                 // key yet has reference -inf, and so long as it sees none (mx = -inf, the difference is NaN) keeps it
-                const bool raise = (mx - m_ref) * sl2 > kRescaleThresholdLog2;
+                const bool raise = mx - m_ref > kRescaleThresholdLog2;
                 if (__any_sync(0xffffffffu, raise && j > 0)) {
                     // rescale O (the previous P V product is complete: S(j) was issued after it)
-                    const float alpha = raise ? ex2((m_ref - mx) * sl2) : 1.f;
+                    const float alpha = raise ? ex2(m_ref - mx) : 1.f;
 #pragma unroll
                     for (int c = 0; c < D / 32; ++c) {
                         uint32_t r[32];
@@ -338,16 +332,16 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     if (j == 0) l = 0.f;
                     m_ref = mx;
                 }
-                const float nmb = m_ref > -INFINITY ? -m_ref * sl2 : 0.f;
+                const float add = rs.base - (m_ref > -INFINITY ? m_ref : 0.f);
                 float2 sum2 = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {  // P goes to the MMA warp in two halves of 64 key columns
+                // P goes to the MMA warp in two halves of 64 key columns
+                auto half_of_p = [&](int h, auto linear) {
                     uint32_t pk[kTileKV / 4];
 #pragma unroll
                     for (int c = 0; c < kTileKV / 2; c += 2) {
                         const int cc = h * (kTileKV / 2) + c;
-                        const float2 e = kLog2 ? add2(make_float2(sv[cc], sv[cc + 1]), splat(nmb))
-                                               : fma2(make_float2(sv[cc], sv[cc + 1]), splat(sl2), splat(nmb));
+                        const float2 b = decltype(linear)::value ? make_float2(fmaf(rs.step, (float)cc, add), fmaf(rs.step, (float)(cc + 1), add)) : splat(add);
+                        const float2 e = fma2(make_float2(sv[cc], sv[cc + 1]), splat(rs.mul), b);
                         const float p0 = ex2(e.x), p1 = ex2(e.y);
                         sum2 = add2(sum2, make_float2(p0, p1));
                         pk[c / 2] = pack_bf16(p0, p1);
@@ -356,13 +350,20 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(&sm.p_half[x][h]);
+                };
+                if (kBias && rs.step != 0.f) {  // warp-uniform
+                    half_of_p(0, std::true_type());
+                    half_of_p(1, std::true_type());
+                } else {
+                    half_of_p(0, std::false_type());
+                    half_of_p(1, std::false_type());
                 }
                 l += sum2.x + sum2.y;
             }
             // ---- epilogue
             const bool row_ok = row < tile_rows;
             const float inv_l = (l > 0.f) ? 1.f / l : 0.f;
-            const float lse = (l > 0.f) ? (m_ref * sl2 + log2f(l)) * 0.6931471805599453f : -INFINITY;
+            const float lse = (l > 0.f) ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
             if (n_kv > 0) {
                 ZL_WAIT_WARP(&sm.o_full[x], o_cnt & 1, 23);
                 ++o_cnt;
