@@ -386,7 +386,7 @@ typedef struct {
  *   shard_pos     host, one entry per shard (may be NULL without shards): positions of the shard's first query and key row,
  *                 and the prefix of its sequence.  All >= 0, q_pos + q_len and kv_pos + kv_len at most 2^31 - 513.
  * Scores by distance need this call on handles with shards, masks on all handles.  The work lists for masked calls are
- * ordered by what the mask leaves of each item.  Synchronises `stream`; must not run while a launch of the
+ * dealt out by what the mask leaves of each item.  Synchronises `stream`; must not run while a launch of the
  * handle is in flight; the other entry points are unaffected. */
 zl_status zl_set_positions(zl_tasks* tasks, const int32_t* whole_prefix, const zl_shard_pos* shard_pos, void* stream);
 

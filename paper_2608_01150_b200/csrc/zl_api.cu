@@ -34,6 +34,7 @@ struct zl_tasks {
     int32_t* d_kv_group_tasks = nullptr;
     int32_t* d_status = nullptr;
     uint8_t* d_positions = nullptr;  // zl_set_positions: one allocation for the three tables below
+    size_t positions_bytes = 0;
     TaskPos* d_task_pos = nullptr;
     WorkItem* d_fwd_items_masked = nullptr;
     WorkItem* d_bwd_items_masked = nullptr;
@@ -465,7 +466,10 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     if (score) {
         sp = score->params;
         sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
-        if (sp.masked) p.items = t->d_fwd_items_masked;
+        if (sp.masked && t->sm_margin == 0) {  // dealt out to as many CTAs as there are SMs; another grid takes the plain list
+            p.items = t->d_fwd_items_masked;
+            p.n_items = (int32_t)s.fwd_items_masked.size();
+        }
     }
     const ScoreKind kind = score && score->biased ? kScoreBias : kScorePlain;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
@@ -642,7 +646,10 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
         if (score->capped) p.lse_tiles = reinterpret_cast<float*>(ws + at.lse);
         if (d_bucket_bias) sp.bucket_part = reinterpret_cast<float*>(ws + at.part);
-        if (sp.masked) p.items = t->d_bwd_items_masked;
+        if (sp.masked && t->sm_margin == 0) {
+            p.items = t->d_bwd_items_masked;
+            p.n_items = (int32_t)s.bwd_items_masked.size();
+        }
     }
 
     if (first) {
@@ -799,7 +806,7 @@ zl_status zl_set_positions(zl_tasks* t, const int32_t* whole_prefix, const zl_sh
     if (t->device >= 0 && !on_handle_device(t)) return ZL_ERR_INVALID_ARG;
     Schedule& s = t->sched;
     try {
-        const zl_status st = set_positions(&s, whole_prefix, shard_pos);
+        const zl_status st = set_positions(&s, whole_prefix, shard_pos, t->device >= 0 ? t->n_sms : 148);
         if (st != ZL_OK) return st;
         if (t->device < 0 || s.tasks.empty()) return ZL_OK;
         // no entry is left that the device does not have: a failure below takes the positions back
@@ -807,10 +814,16 @@ zl_status zl_set_positions(zl_tasks* t, const int32_t* whole_prefix, const zl_sh
         const size_t o_pos = place<TaskPos>(off, s.task_pos.size());
         const size_t o_fwd = place<WorkItem>(off, s.fwd_items_masked.size());
         const size_t o_bwd = place<WorkItem>(off, s.bwd_items_masked.size());
-        if (!t->d_positions && cudaMalloc(&t->d_positions, align_up(off, 256)) != cudaSuccess) {
+        if (off > t->positions_bytes) {  // the lists' lengths depend on the positions
+            if (t->d_positions) cudaFree(t->d_positions);
             t->d_positions = nullptr;
-            s.task_pos.clear();
-            return ZL_ERR_CUDA;
+            t->positions_bytes = 0;
+            if (cudaMalloc(&t->d_positions, align_up(off, 256)) != cudaSuccess) {
+                t->d_positions = nullptr;
+                s.task_pos.clear();
+                return ZL_ERR_CUDA;
+            }
+            t->positions_bytes = off;
         }
         t->d_task_pos = reinterpret_cast<TaskPos*>(t->d_positions + o_pos);
         t->d_fwd_items_masked = reinterpret_cast<WorkItem*>(t->d_positions + o_fwd);

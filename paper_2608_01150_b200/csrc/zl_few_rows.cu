@@ -14,8 +14,6 @@
 //   * warps without a valid row only take part in the barriers.
 #include <cuda_runtime.h>
 
-#include <type_traits>
-
 #include "zl_score.cuh"
 
 namespace zl {
@@ -27,7 +25,6 @@ namespace {
 
 constexpr int kThreads = 384;
 constexpr uint64_t kWaitLimitNs = 4000000000ull;
-constexpr float kRescaleThresholdLog2 = 8.0f;  // as in the two-tile kernels: the reference maximum is raised lazily
 
 template <int D, int kRows>
 struct FewSmem {
@@ -40,11 +37,13 @@ struct FewSmem {
     alignas(1024) uint8_t q[2][kRows * D * 2];  // followed by K: an MMA reads 128 rows from here on
     alignas(1024) uint8_t k[kStagesK][kTileBytes];
     alignas(1024) uint8_t v[kStagesV][kTileBytes];
-    alignas(16) float window[8][kWindowFloats];  // per softmax warp: the biases of a near patch
+    float window[2][kWindow];  // per warpgroup: the biases of a near key tile
     float2 stat[2][kTileQ];    // per warpgroup and row: reference maximum (powers of two) and sum
     alignas(8) uint64_t q_full[2], q_empty[2];
     uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
+    uint64_t bias_full[2], bias_empty[2];
     uint64_t s_full[2], p_half[2][2], o_full[2];
+    uint64_t stat_full, join_done;  // between the warpgroups at the end of an item
     uint32_t tmem_base;
     volatile int32_t abort_flag;
 };
@@ -97,9 +96,13 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             mbar_init(&sm.p_half[x][0], 128);
             mbar_init(&sm.p_half[x][1], 128);
             mbar_init(&sm.o_full[x], 1);
+            mbar_init(&sm.bias_full[x], 1);
+            mbar_init(&sm.bias_empty[x], 128);
         }
         for (int s = 0; s < kStagesK; ++s) { mbar_init(&sm.k_full[s], 1); mbar_init(&sm.k_empty[s], 1); }
         for (int s = 0; s < kStagesV; ++s) { mbar_init(&sm.v_full[s], 1); mbar_init(&sm.v_empty[s], 1); }
+        mbar_init(&sm.stat_full, 256);
+        mbar_init(&sm.join_done, 256);
         sm.abort_flag = 0;
         fence_mbar_init();
         prefetch_tmap(&tm_q);
@@ -122,6 +125,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             uint32_t item_cnt = 0, kv_cnt = 0;
             for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
                 const WorkItem wi = p.items[it];
+                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const int n_kv = key_tiles(sp, t, wi.unit, wi.row0, wi.rows);
                 if (n_kv == 0) continue;
@@ -161,6 +165,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             uint32_t item_cnt = 0, kv_cnt = 0, p_cnt[2] = {0, 0};
             for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
                 const WorkItem wi = p.items[it];
+                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const int n_kv = key_tiles(sp, t, wi.unit, wi.row0, wi.rows);
                 if (n_kv == 0) continue;
@@ -204,6 +209,27 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 }
                 kv_cnt += n_kv;
             }
+        } else if (kBias && warp >= 2) {  // (the other lanes of warp 0 have nothing to do)
+            // -------------------------------------------------------------- biases of near tiles, one warp per warpgroup
+            const int x = warp - 2;
+            WindowFeed feed{&sm.bias_full[x], &sm.bias_empty[x], sm.window[x]};
+            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+                const WorkItem wi = p.items[it];
+                if (wi.rows == 0) break;  // end of this CTA's list
+                const Task t = p.tasks[wi.unit];
+                const TaskPos tp = task_pos(sp, wi.unit);
+                const int n_kv = key_tiles(sp, t, wi.unit, wi.row0, wi.rows);
+                HeadBias hb;
+                hb.load(sp, wi.head);
+                for (int j = x; j < n_kv; j += 2) {
+                    const int lo = tp.kv_pos + j * kTileKV - (tp.q_pos + wi.row0 + kTileQ - 1);
+                    if (patch_side(sp, lo, lo + kTileQ + kTileKV - 2) != kNear) continue;
+                    if (!feed.put(sp, hb, wi.head, lo, lane, kWaitLimitNs, &sm.abort_flag)) {
+                        report(p.status, &sm.abort_flag, 5000 + 31);
+                        goto teardown;
+                    }
+                }
+            }
         }
     } else {
         // ------------------------------------------------------------------ softmax, join and output
@@ -213,10 +239,11 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int row = quarter * 32 + lane;       // query row within the tile
         const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
         const uint32_t col_s = kColS + x * 128, col_o = kColO + x * 128;
-        float* const window = sm.window[warp - 4];
-        uint32_t s_cnt = 0, o_cnt[2] = {0, 0};
+        uint32_t bias_cnt = 0;
+        uint32_t s_cnt = 0, o_cnt[2] = {0, 0}, join_cnt = 0;
         for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
             const WorkItem wi = p.items[it];
+            if (wi.rows == 0) break;  // end of this CTA's list
             const Task t = p.tasks[wi.unit];
             const TaskPos tp = task_pos(sp, wi.unit);
             const int n_kv = key_tiles(sp, t, wi.unit, wi.row0, wi.rows);
@@ -227,19 +254,16 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if constexpr (kBias) hb.load(sp, wi.head);
             float m_ref = -INFINITY, l = 0.f;
             for (int j = x; j < n_kv; j += 2) {
-                PatchSide side = kNear;
-                float near_bias[kWindow / 32];
-                const int dist_lo = tp.kv_pos + j * kTileKV - (tp.q_pos + wi.row0 + quarter * 32 + 31);  // last row, first column
-                if constexpr (kBias) {
-                    side = patch_side(sp, dist_lo, dist_lo + 31 + kTileKV - 1);
-                    if (side == kNear && busy) {
-#pragma unroll
-                        for (int i = 0; i < kWindow / 32; ++i) near_bias[i] = hb.at(sp, wi.head, dist_lo + i * 32 + lane);
-                    }
-                }
+                const int dist_lo = tp.kv_pos + j * kTileKV - (tp.q_pos + wi.row0 + kTileQ - 1);  // last row, first column
+                const PatchSide side = kBias ? patch_side(sp, dist_lo, dist_lo + kTileQ + kTileKV - 2) : kNear;
                 ZL_WAIT_WARP(&sm.s_full[x], s_cnt & 1, 21);
                 ++s_cnt;
                 if (!busy) {  // P of rows that do not exist is whatever S was
+                    if (kBias && side == kNear) {
+                        ZL_WAIT_WARP(&sm.bias_full[x], bias_cnt & 1, 25);
+                        ++bias_cnt;
+                        mbar_arrive(&sm.bias_empty[x]);
+                    }
                     mbar_arrive(&sm.p_half[x][0]);
                     mbar_arrive(&sm.p_half[x][1]);
                     continue;
@@ -253,58 +277,14 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sv[c * 32 + i] = __uint_as_float(r[i]);
                 }
-                if constexpr (kBias) {
-                    if (side == kNear) fill_window(window, near_bias, lane);
+                if (kBias && side == kNear) {
+                    ZL_WAIT_WARP(&sm.bias_full[x], bias_cnt & 1, 26);
+                    ++bias_cnt;
                 }
                 tmem_wait_ld();
-                const RowScore rs = finish_scores<kCap, kBias>(sv, sp, hb, side, window, dist_lo, p.scale_log2, keys - j * kTileKV, lane);
-                const float mx = rs.max;
-                const bool raise = row_ok && mx - m_ref > kRescaleThresholdLog2;
-                if (__any_sync(0xffffffffu, raise && j > x)) {
-                    // rescale O (the previous P V product is complete: S(j) was issued after it)
-                    const float alpha = raise ? ex2(m_ref - mx) : 1.f;
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t r[32];
-                        tmem_ld_x32(lane_addr + col_o + c * 32, r);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-                        tmem_st_x32(lane_addr + col_o + c * 32, r);
-                    }
-                    l *= alpha;
-                }
-                if (raise) {
-                    if (j == x) l = 0.f;
-                    m_ref = mx;
-                }
-                const float add = rs.base - (m_ref > -INFINITY ? m_ref : 0.f);
-                float2 sum2 = make_float2(0.f, 0.f);
-                // P goes to the MMA warp in two halves of 64 key columns
-                auto half_of_p = [&](int h, auto linear) {
-                    uint32_t pk[kTileKV / 4];
-#pragma unroll
-                    for (int c = 0; c < kTileKV / 2; c += 2) {
-                        const int cc = h * (kTileKV / 2) + c;
-                        const float2 b = decltype(linear)::value ? make_float2(fmaf(rs.step, (float)cc, add), fmaf(rs.step, (float)(cc + 1), add)) : splat(add);
-                        const float2 e = fma2(make_float2(sv[cc], sv[cc + 1]), splat(rs.mul), b);
-                        const float p0 = ex2(e.x), p1 = ex2(e.y);
-                        sum2 = add2(sum2, make_float2(p0, p1));
-                        pk[c / 2] = pack_bf16(p0, p1);
-                    }
-                    tmem_st_x32(lane_addr + col_s + h * 32, pk);
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(&sm.p_half[x][h]);
-                };
-                if (kBias && rs.step != 0.f) {  // warp-uniform
-                    half_of_p(0, std::true_type());
-                    half_of_p(1, std::true_type());
-                } else {
-                    half_of_p(0, std::false_type());
-                    half_of_p(1, std::false_type());
-                }
-                l += sum2.x + sum2.y;
+                softmax_tile<D, kCap, kBias>(sv, sp, hb, p.scale_log2, j == x, side, sm.window[x] + kTileQ - 1 - row, &sm.bias_empty[x],
+                                             dist_lo + kTileQ - 1 - row, keys - j * kTileKV, row_ok, lane_addr + col_s, lane_addr + col_o,
+                                             sm.p_half[x], m_ref, l);
             }
             // ---- join: O = (w_0 O_0 + w_1 O_1) / (w_0 l_0 + w_1 l_1), w_x = 2^(m_x - max); warpgroup x writes half of the columns
             float w[2] = {0.f, 0.f}, lse = -INFINITY;
@@ -316,7 +296,8 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     }
                 tc_fence_after();
                 sm.stat[x][row] = make_float2(m_ref, l);
-                named_bar_sync(2, 256);
+                mbar_arrive(&sm.stat_full);
+                ZL_WAIT_WARP(&sm.stat_full, join_cnt & 1, 27);
                 const float2 a = sm.stat[0][row], b = sm.stat[1][row];
                 const float m = fmaxf(a.x, b.x);
                 if (m > -INFINITY) {
@@ -369,7 +350,11 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 }
             }
             tc_fence_before();
-            if (n_kv > 0) named_bar_sync(3, 256);  // both accumulators and the statistics have been read
+            if (n_kv > 0) {  // both accumulators and the statistics have been read
+                mbar_arrive(&sm.join_done);
+                ZL_WAIT_WARP(&sm.join_done, join_cnt & 1, 28);
+                ++join_cnt;
+            }
         }
     }
 

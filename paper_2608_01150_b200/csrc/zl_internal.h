@@ -109,7 +109,8 @@ struct Schedule {
     int32_t n_kv_tiles = 0;                 // 128-row key tiles of all kv groups
     int32_t max_item_rows = 0;              // most query rows of a forward item
     bool shared_prefix = false;             // built by build_prefix_schedule: query ranges nest
-    // Positions (zl_set_positions): one entry per task, and the work lists in the order that suits the mask.
+    // Positions (zl_set_positions): one entry per task, and the work lists dealt out to the CTAs by what the mask leaves of
+    // each item (an item without rows ends a CTA's list).
     std::vector<TaskPos> task_pos;
     std::vector<WorkItem> fwd_items_masked, bwd_items_masked;
     std::vector<KvGroup> kv_groups;
@@ -138,8 +139,8 @@ zl_status build_schedule(const std::vector<InputTask>& in, int32_t n_shards, int
 zl_status build_prefix_schedule(const int32_t* cu_q, const int32_t* cu_kv, int32_t n_seqs, int32_t prefix_len,
                                 int32_t total_q, int32_t total_kv, int32_t n_heads, int32_t head_dim, Schedule* s);
 
-// Checks the positions and fills task_pos and the masked work lists of `s` (zl_set_positions).
-zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard_pos* shard_pos);
+// Checks the positions and fills task_pos and the masked work lists of `s` (zl_set_positions), dealt out to `n_sms` CTAs.
+zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard_pos* shard_pos, int32_t n_sms);
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

@@ -1,6 +1,8 @@
 // Scores beyond scale * q.k, as the scored forward and backward kernels form them (both work in powers of two).
 #pragma once
 
+#include <type_traits>
+
 #include "zl_device.h"
 #include "zl_ptx.cuh"
 
@@ -81,98 +83,31 @@ __device__ __forceinline__ int key_tiles(const ScoreParams& sp, const Task& t, i
     return (keys + kTileKV - 1) / kTileKV;
 }
 
-// Distances of a 32 x 128 patch: 32 + 128 - 1, rounded up to a multiple of 32.  A warp's window holds their biases four
-// times, copy s shifted by s: a thread's 128 consecutive biases start at 31 - lane, and in copy (31 - lane) % 4 that start
-// is 16-byte aligned, so the row is 32 four-word loads instead of 128 single ones.  Copies lie 8 banks apart, which keeps
-// the eight lanes of a load phase on different banks.
-constexpr int kWindow = 160;
-constexpr int kWindowStride = 168;
-constexpr int kWindowFloats = 4 * kWindowStride;
+// Distances of a 128 x 128 tile: 255, and one more so that eight per lane cover them.
+constexpr int kWindow = 256;
 
-__device__ __forceinline__ void fill_window(float* window, const float (&bias)[kWindow / 32], int lane) {
-    __syncwarp();  // the previous patch has been read
+// Warps 2 and 3 of the forward kernels fetch the biases of near tiles, one distance each, ahead of the softmax warps: two
+// dependent loads from L2 (bucket, then bias) would otherwise stand in front of every near tile.
+struct WindowFeed {
+    uint64_t *full, *empty;  // arrivals: the feeding warp; the 128 threads of the warpgroup that reads
+    float* window;           // kWindow floats
+    uint32_t count = 0;
+    // Puts the biases of distances lo .. lo + 254 into the window; false: the bounded wait expired.
+    __device__ __forceinline__ bool put(const ScoreParams& sp, const HeadBias& hb, int head, int lo, int lane, uint64_t limit_ns,
+                                        const volatile int32_t* abort_flag) {
+        float v[kWindow / 32];
 #pragma unroll
-    for (int i = 0; i < kWindow / 32; ++i) {
+        for (int i = 0; i < kWindow / 32; ++i) v[i] = hb.at(sp, head, lo + i * 32 + lane);
+        const bool ok = mbar_wait(empty, (count & 1) ^ 1, limit_ns, abort_flag);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        ++count;
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-            if (i * 32 + lane >= s) window[s * kWindowStride + i * 32 + lane - s] = bias[i];
+        for (int i = 0; i < kWindow / 32; ++i) window[i * 32 + lane] = v[i];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full);
+        return true;
     }
-    __syncwarp();
-}
-
-// How the exponent of a tile's row follows from its values: score(c) = v[c] * mul + base + step * c, in powers of two.
-struct RowScore {
-    float mul, base, step;
-    float max;  // of the row's scores, or an upper bound
 };
-// An upper bound serves as the softmax's reference so long as it is not far above: 2^-kSlack of the reference still leaves
-// 2^60 to the smallest fp32 number, so nothing that counts is lost, and sums and LSE are exact relative to any reference.
-constexpr float kSlack = 64.f;
-
-__device__ __forceinline__ float row_max(const float (&sv)[kTileKV]);
-
-// Turns a row of raw products into values with `mul`, `base` and `step`: the cap and near biases change the values, a far
-// bias (linear in the column) only base and step; columns from `valid` on become -inf.  `window` holds the biases of a near
-// patch, `dist_lo` is the distance of the patch's last row to its first column.
-template <bool kCap, bool kBias>
-__device__ __forceinline__ RowScore finish_scores(float (&sv)[kTileKV], const ScoreParams& sp, const HeadBias& hb, PatchSide side,
-                                                  const float* window, int dist_lo, float scale_log2, int valid, int lane) {
-    RowScore rs{scale_log2, 0.f, 0.f, 0.f};
-    if constexpr (kCap) {
-        rs.mul = 1.f;
-        float big = 0.f;
-#pragma unroll
-        for (int c = 0; c < kTileKV; c += 2) big = max3_abs(big, sv[c], sv[c + 1]);
-        if (__all_sync(0xffffffffu, big * sp.scale_over_cap <= kTanhRange)) {
-            const float2 k1 = splat(sp.scale_over_cap);
-            const float2 c0 = splat(kTanhC0 * sp.cap_log2), c1 = splat(kTanhC1 * sp.cap_log2), c2 = splat(kTanhC2 * sp.cap_log2),
-                         c3 = splat(kTanhC3 * sp.cap_log2), c4 = splat(kTanhC4 * sp.cap_log2);
-#pragma unroll
-            for (int c = 0; c < kTileKV; c += 2) {
-                const float2 y = mul2(make_float2(sv[c], sv[c + 1]), k1);
-                const float2 z = mul2(y, y);
-                const float2 v = mul2(y, fma2(z, fma2(z, fma2(z, fma2(z, c4, c3), c2), c1), c0));
-                sv[c] = v.x;
-                sv[c + 1] = v.y;
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < kTileKV; ++c) sv[c] = tanh_any(sv[c] * sp.scale_over_cap) * sp.cap_log2;
-        }
-    }
-    if constexpr (kBias) {
-        if (side == kNear) {
-            const int start = 31 - lane;
-            const float4* w = reinterpret_cast<const float4*>(window + (start & 3) * kWindowStride + (start & ~3));
-#pragma unroll
-            for (int c = 0; c < kTileKV; c += 4) {
-                const float4 b = w[c / 4];
-                const float2 v0 = fma2(make_float2(sv[c], sv[c + 1]), splat(rs.mul), make_float2(b.x, b.y));
-                const float2 v1 = fma2(make_float2(sv[c + 2], sv[c + 3]), splat(rs.mul), make_float2(b.z, b.w));
-                sv[c] = v0.x;
-                sv[c + 1] = v0.y;
-                sv[c + 2] = v1.x;
-                sv[c + 3] = v1.y;
-            }
-            rs.mul = 1.f;
-        } else {
-            rs.step = side == kFarPos ? -hb.slope : hb.slope;
-            rs.base = (side == kFarPos ? hb.far_pos : hb.far_neg) + rs.step * (float)(dist_lo + 31 - lane);
-            if (fabsf(rs.step) * (kTileKV - 1) > kSlack) {  // warp-uniform: steep slopes get their exact maximum
-#pragma unroll
-                for (int c = 0; c < kTileKV; ++c) sv[c] = fmaf(sv[c], rs.mul, fmaf(rs.step, (float)c, rs.base));
-                rs = RowScore{1.f, 0.f, 0.f, 0.f};
-            }
-        }
-    }
-    if (__any_sync(0xffffffffu, valid < kTileKV)) {
-#pragma unroll
-        for (int c = 0; c < kTileKV; ++c)
-            if (c >= valid) sv[c] = -INFINITY;  // select, never multiply
-    }
-    rs.max = fmaf(row_max(sv), rs.mul, rs.base + fmaxf(0.f, rs.step * (kTileKV - 1)));
-    return rs;
-}
 
 __device__ __forceinline__ float row_max(const float (&sv)[kTileKV]) {
     // four independent chains: a single running maximum is a 64-deep dependent chain
@@ -189,6 +124,168 @@ __device__ __forceinline__ float row_max(const float (&sv)[kTileKV]) {
     mx0 = max3(mx0, sv[kTileKV - 4], sv[kTileKV - 3]);
     mx1 = max3(mx1, sv[kTileKV - 2], sv[kTileKV - 1]);
     return fmaxf(max3(mx0, mx1, mx2), mx3);
+}
+
+// An upper bound of a row's scores serves as the softmax's reference as well as the maximum, so long as it is not far above:
+// 2^-kSlack of the reference still leaves 2^60 to the smallest fp32 number, so nothing that counts is lost, and sums and
+// LSE are exact relative to any reference.
+constexpr float kSlack = 64.f;
+// The reference of a row is only raised when a tile's maximum exceeds it by more than this many powers of two; until then
+// exponentials stay below 2^8 and nothing is rescaled.
+constexpr float kRescaleThresholdLog2 = 8.0f;
+
+// One tile of the online softmax: a row of raw products `sv` becomes P (bf16, over S in TMEM, handed over in two halves of 64
+// columns by `p_half`); the row's reference m_ref (powers of two) and sum l move on, O in TMEM is rescaled when the
+// reference is raised.  Columns from `valid` on are invisible.  A near tile adds bias[c] (and releases the window), a far
+// one a bias that is linear in the column, from distance `dist0` of column 0: that one stays in the exponential's
+// multiply-add and costs nothing where it is constant.
+template <int D, bool kCap, bool kBias>
+__device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScoreParams& sp, const HeadBias& hb, float scale_log2,
+                                             bool first, PatchSide side, const float* bias, uint64_t* bias_empty, int dist0,
+                                             int valid, bool row_ok, uint32_t s_addr, uint32_t o_addr, uint64_t (&p_half)[2],
+                                             float& m_ref, float& l) {
+    float mul = scale_log2, base = 0.f, step = 0.f;  // score(c) = sv[c] * mul + base + step * c, in powers of two
+    float2 sum2 = make_float2(0.f, 0.f);
+    auto hand_over = [&](int h, const uint32_t (&pk)[kTileKV / 4]) {
+        tmem_st_x32(s_addr + h * 32, pk);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&p_half[h]);
+    };
+    if constexpr (kCap) {
+        mul = 1.f;
+        float big = 0.f;
+#pragma unroll
+        for (int c = 0; c < kTileKV; c += 2) big = max3_abs(big, sv[c], sv[c + 1]);
+        const bool near_zero = !row_ok || big * sp.scale_over_cap <= kTanhRange;  // rows that do not exist hold anything
+        const float2 k1 = splat(sp.scale_over_cap);
+        const float2 c0 = splat(kTanhC0 * sp.cap_log2), c1 = splat(kTanhC1 * sp.cap_log2), c2 = splat(kTanhC2 * sp.cap_log2),
+                     c3 = splat(kTanhC3 * sp.cap_log2), c4 = splat(kTanhC4 * sp.cap_log2);
+        if constexpr (!kBias) {
+            // |C(x)| <= |x|, so the largest magnitude bounds the row's scores: where that does not ask for a higher
+            // reference, cap and exponential run in one pass, the multiply-adds of one score under the exponential of another
+            const bool easy = !row_ok || (near_zero && valid >= kTileKV && big * scale_log2 - m_ref <= kRescaleThresholdLog2);
+            if (__all_sync(0xffffffffu, easy)) {
+                const float2 nm = splat(-m_ref);
+                constexpr int kGroup = 8;  // pairs whose chains run side by side
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t pk[kTileKV / 4];
+#pragma unroll
+                    for (int g = 0; g < kTileKV / 4; g += kGroup) {
+                        float2 y[kGroup], r[kGroup];
+#pragma unroll
+                        for (int i = 0; i < kGroup; ++i) {
+                            const int c = h * (kTileKV / 2) + 2 * (g + i);
+                            y[i] = mul2(make_float2(sv[c], sv[c + 1]), k1);
+                        }
+#pragma unroll
+                        for (int i = 0; i < kGroup; ++i) r[i] = fma2(mul2(y[i], y[i]), c4, c3);
+#pragma unroll
+                        for (int i = 0; i < kGroup; ++i) r[i] = fma2(mul2(y[i], y[i]), r[i], c2);
+#pragma unroll
+                        for (int i = 0; i < kGroup; ++i) r[i] = fma2(mul2(y[i], y[i]), r[i], c1);
+#pragma unroll
+                        for (int i = 0; i < kGroup; ++i) r[i] = fma2(mul2(y[i], y[i]), r[i], c0);
+#pragma unroll
+                        for (int i = 0; i < kGroup; ++i) r[i] = fma2(y[i], r[i], nm);
+#pragma unroll
+                        for (int i = 0; i < kGroup; ++i) {
+                            const float p0 = ex2(r[i].x), p1 = ex2(r[i].y);
+                            sum2 = add2(sum2, make_float2(p0, p1));
+                            pk[g + i] = pack_bf16(p0, p1);
+                        }
+                    }
+                    hand_over(h, pk);
+                }
+                l += sum2.x + sum2.y;
+                return;
+            }
+        }
+        if (__all_sync(0xffffffffu, near_zero)) {
+#pragma unroll
+            for (int c = 0; c < kTileKV; c += 2) {
+                const float2 y = mul2(make_float2(sv[c], sv[c + 1]), k1);
+                const float2 z = mul2(y, y);
+                const float2 v = mul2(y, fma2(z, fma2(z, fma2(z, fma2(z, c4, c3), c2), c1), c0));
+                sv[c] = v.x;
+                sv[c + 1] = v.y;
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < kTileKV; ++c) sv[c] = tanh_any(sv[c] * sp.scale_over_cap) * sp.cap_log2;
+        }
+    }
+    if constexpr (kBias) {
+        if (side == kNear) {
+#pragma unroll
+            for (int c = 0; c < kTileKV; c += 2) {
+                const float2 v = fma2(make_float2(sv[c], sv[c + 1]), splat(mul), make_float2(bias[c], bias[c + 1]));
+                sv[c] = v.x;
+                sv[c + 1] = v.y;
+            }
+            mbar_arrive(bias_empty);
+            mul = 1.f;
+        } else {
+            step = side == kFarPos ? -hb.slope : hb.slope;
+            base = (side == kFarPos ? hb.far_pos : hb.far_neg) + step * (float)dist0;
+            if (fabsf(step) * (kTileKV - 1) > kSlack) {  // warp-uniform: steep slopes get their exact maximum
+#pragma unroll
+                for (int c = 0; c < kTileKV; ++c) sv[c] = fmaf(sv[c], mul, fmaf(step, (float)c, base));
+                mul = 1.f;
+                base = step = 0.f;
+            }
+        }
+    }
+    if (__any_sync(0xffffffffu, valid < kTileKV)) {
+#pragma unroll
+        for (int c = 0; c < kTileKV; ++c)
+            if (c >= valid) sv[c] = -INFINITY;  // select, never multiply
+    }
+    const float mx = fmaf(row_max(sv), mul, base + fmaxf(0.f, step * (kTileKV - 1)));
+    // lazy reference update: only when the tile maximum is far above the reference; a row that has seen no key yet has
+    // reference -inf, and so long as it sees none (mx = -inf, the difference is NaN) keeps it
+    const bool raise = row_ok && mx - m_ref > kRescaleThresholdLog2;
+    if (__any_sync(0xffffffffu, raise && !first)) {
+        // rescale O (the previous P V product is complete: this S was issued after it)
+        const float alpha = raise ? ex2(m_ref - mx) : 1.f;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            uint32_t r[32];
+            tmem_ld_x32(o_addr + c * 32, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+            tmem_st_x32(o_addr + c * 32, r);
+        }
+        l *= alpha;
+    }
+    if (raise) {
+        if (first) l = 0.f;
+        m_ref = mx;
+    }
+    const float add = base - (m_ref > -INFINITY ? m_ref : 0.f);
+    auto half_of_p = [&](int h, auto linear) {
+        uint32_t pk[kTileKV / 4];
+#pragma unroll
+        for (int c = 0; c < kTileKV / 2; c += 2) {
+            const int cc = h * (kTileKV / 2) + c;
+            const float2 b = decltype(linear)::value ? make_float2(fmaf(step, (float)cc, add), fmaf(step, (float)(cc + 1), add)) : splat(add);
+            const float2 e = fma2(make_float2(sv[cc], sv[cc + 1]), splat(mul), b);
+            const float p0 = ex2(e.x), p1 = ex2(e.y);
+            sum2 = add2(sum2, make_float2(p0, p1));
+            pk[c / 2] = pack_bf16(p0, p1);
+        }
+        hand_over(h, pk);
+    };
+    if (kBias && step != 0.f) {  // warp-uniform
+        half_of_p(0, std::true_type());
+        half_of_p(1, std::true_type());
+    } else {
+        half_of_p(0, std::false_type());
+        half_of_p(1, std::false_type());
+    }
+    l += sum2.x + sum2.y;
 }
 
 }  // namespace score

@@ -57,6 +57,7 @@ struct ScoredBwdSmem {
     float window[8][kWindow];                           // per P/dS warp: biases, then sums over diagonals
     alignas(8) uint64_t kv_full, kv_empty;
     uint64_t q_full[2], q_empty[2], do_full, do_empty;
+    uint64_t sums_full, sums_empty;
     uint64_t s_full, dp_full, p_full, ds_full, ds_free, dq_full, dq_empty, acc_full;
     uint32_t tmem_base;
     volatile int32_t abort_flag;
@@ -161,6 +162,8 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         mbar_init(&sm.dq_full, 1);
         mbar_init(&sm.dq_empty, 128);
         mbar_init(&sm.acc_full, 1);
+        mbar_init(&sm.sums_full, 256);
+        mbar_init(&sm.sums_empty, 256);
         sm.abort_flag = 0;
         fence_mbar_init();
         prefetch_tmap(&tm_q);
@@ -195,6 +198,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             uint32_t item_cnt = 0, it_cnt = 0;
             for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
                 const WorkItem wi = p.items[it];
+                if (wi.rows == 0) break;  // end of this CTA's list
                 const KvGroup g = p.kv_groups[wi.unit];
                 if (count_q_tiles(p, sp, g, wi.row0) == 0) continue;  // no query sees these keys
                 ZL_WAIT(&sm.kv_empty, (item_cnt & 1) ^ 1, 1);
@@ -282,6 +286,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             uint32_t item_cnt = 0, it_cnt = 0;
             for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
                 const WorkItem wi = p.items[it];
+                if (wi.rows == 0) break;  // end of this CTA's list
                 const KvGroup g = p.kv_groups[wi.unit];
                 const int n_it = count_q_tiles(p, sp, g, wi.row0);
                 if (n_it == 0) continue;
@@ -351,12 +356,13 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         const int col0 = wg * 64;
         const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
         const uint32_t ds_row_addr = smem_u32(sm.ds) + row * 128;
-        uint32_t item_cnt = 0, it_cnt = 0;
+        uint32_t item_cnt = 0, it_cnt = 0, sums_cnt = 0;
         const bool store_leader = (warp & 3) == 0 && lane == 0;  // one thread per warpgroup issues its TMA stores
         bool store_pending = false;
         float* const window = sm.window[warp - 4];
         for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
             const WorkItem wi = p.items[it];
+            if (wi.rows == 0) break;  // end of this CTA's list
             const KvGroup g = p.kv_groups[wi.unit];
             const bool row_ok = row < wi.rows;
             HeadBias hb;
@@ -579,7 +585,8 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 __syncwarp();
                 window[lane] = bucket_sum[0];
                 window[lane + 32] = bucket_sum[1];
-                named_bar_sync(4, 256);
+                mbar_arrive(&sm.sums_full);
+                ZL_WAIT_WARP(&sm.sums_full, sums_cnt & 1, 27);
                 const int b = threadIdx.x - 128;  // 0 .. 255
                 if (b < kMaxBuckets) {
                     float v = 0.f;
@@ -587,7 +594,9 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     for (int w = 0; w < 8; ++w) v += sm.window[w][b];
                     sp.bucket_part[((int64_t)wi.head * sp.n_kv_tiles + g.tile_begin + wi.row0 / kTileKV) * kMaxBuckets + b] = v;
                 }
-                named_bar_sync(4, 256);  // the windows are free again
+                mbar_arrive(&sm.sums_empty);
+                ZL_WAIT_WARP(&sm.sums_empty, sums_cnt & 1, 28);  // the windows are free again
+                ++sums_cnt;
             }
             // ---- epilogue: warpgroup 0 stores dV, warpgroup 1 stores dK (scaled)
             const bool seen = it_cnt != it_first;  // else no query sees these keys: the gradients are zero
@@ -671,6 +680,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         uint32_t it_cnt = 0, chunk_cnt = 0;
         for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
             const WorkItem wi = p.items[it];
+            if (wi.rows == 0) break;  // end of this CTA's list
             const KvGroup g = p.kv_groups[wi.unit];
             for (int ti = 0; ti < g.n_tasks; ++ti) {
                 const int task = p.kv_group_tasks[g.task_begin + ti];

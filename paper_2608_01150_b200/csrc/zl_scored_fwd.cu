@@ -9,15 +9,14 @@
 //   * The prefix mask leaves every row a leading stretch of keys, visible_keys() of them, and later rows never fewer.  So a
 //     query tile walks the key tiles up to its last row's limit (tile A may stop before tile B), and one compare per
 //     score against the row's limit masks the tiles at the border and the ragged end alike; full tiles compare nothing.
-//   * The bias by distance needs no [Lq, Lk] matrix.  Where a warp's 32 x 128 patch lies on one side of the diagonal and
-//     beyond the buckets' reach it is linear in the column.  Near the diagonal the patch has only 159 different
-//     distances: they are fetched (table and bucket map are small and stay in L2) while S is still being computed, put into
-//     a window in shared memory, and a thread reads its row as 128 conflict-free words.
-//   * The cap costs a tanh per score.  For a patch with |x / cap| <= 0.6 it is a polynomial of five packed multiply-adds,
-//     else two special-function operations: see zl_score.cuh.
+//   * The bias by distance needs no [Lq, Lk] matrix.  Where a 128 x 128 tile lies on one side of the diagonal and beyond the
+//     buckets' reach it is linear in the column: a constant of the row, or one multiply-add more per score with slopes.
+//     Near the diagonal a tile has only 255 different distances: the two warps without another role fetch them ahead
+//     (table and bucket map are small and stay in L2) into a window in shared memory, of which a thread reads its row as
+//     128 conflict-free words.
+//   * The cap costs a tanh per score.  For a tile with |x / cap| <= 0.6 it is a polynomial of five packed multiply-adds,
+//     run under the exponentials where the row needs no new reference; else two special-function operations (zl_score.cuh).
 #include <cuda_runtime.h>
-
-#include <type_traits>
 
 #include "zl_score.cuh"
 
@@ -30,9 +29,6 @@ namespace {
 
 constexpr int kFwdThreads = 384;
 constexpr uint64_t kWaitLimitNs = 4000000000ull;
-// The reference maximum of a row is only raised when the tile maximum exceeds it by more than
-// this many powers of two; until then exponentials stay below 2^8 and nothing is rescaled.
-constexpr float kRescaleThresholdLog2 = 8.0f;
 
 template <int D>
 struct ScoredFwdSmem {
@@ -43,11 +39,11 @@ struct ScoredFwdSmem {
     alignas(1024) uint8_t q[2][kTileBytes];
     alignas(1024) uint8_t k[kStages][kTileBytes];
     alignas(1024) uint8_t v[kStages][kTileBytes];
-    // per softmax warpgroup: 128 rows x 128 bytes of O on their way out; between two items' outputs, the four warps'
-    // windows of biases
-    alignas(1024) uint8_t o_stage[2][kBoxBytes];
+    alignas(1024) uint8_t o_stage[2][kBoxBytes];  // per softmax warpgroup: 128 rows x 128 bytes of O on their way out
+    float window[2][kWindow];                      // per query tile: the biases of a near key tile
     alignas(8) uint64_t q_full[2], q_empty;
     uint64_t kv_full[kStages], kv_empty[kStages];  // K and V of a stage travel together
+    uint64_t bias_full[2], bias_empty[2];
     uint64_t s_full[2], p_half[2][2], o_full[2];  // p_half[tile][half of the key columns]
     uint32_t tmem_base;
     volatile int32_t abort_flag;
@@ -113,6 +109,8 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             mbar_init(&sm.p_half[x][0], 128);
             mbar_init(&sm.p_half[x][1], 128);
             mbar_init(&sm.o_full[x], 1);
+            mbar_init(&sm.bias_full[x], 1);
+            mbar_init(&sm.bias_empty[x], 128);
         }
         sm.abort_flag = 0;
         fence_mbar_init();
@@ -138,6 +136,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             uint32_t q_cnt = 0, qb_cnt = 0, kv_cnt = 0;
             for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
                 const WorkItem wi = p.items[it];
+                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const bool has_b = wi.rows > kTileQ;
                 const int n_a = key_tiles(sp, t, wi.unit, wi.row0, min(wi.rows, kTileQ));
@@ -203,6 +202,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             uint32_t q_cnt = 0, qb_cnt = 0, kv_cnt = 0, pa_cnt = 0, pb_cnt = 0;
             for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
                 const WorkItem wi = p.items[it];
+                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const bool has_b = wi.rows > kTileQ;
                 const int n_a = key_tiles(sp, t, wi.unit, wi.row0, min(wi.rows, kTileQ));
@@ -251,6 +251,28 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     if (j + 2 == n_kv) if (mma_lane) mma_commit(&sm.q_empty);  // last S of the item issued
                 }
             }
+        } else if (kBias && warp >= 2) {  // (the other lanes of warp 0 have nothing to do)
+            // -------------------------------------------------------------- biases of near tiles: warp 2 tile A, warp 3 tile B
+            const int x = warp - 2;
+            WindowFeed feed{&sm.bias_full[x], &sm.bias_empty[x], sm.window[x]};
+            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+                const WorkItem wi = p.items[it];
+                if (wi.rows == 0) break;  // end of this CTA's list
+                const Task t = p.tasks[wi.unit];
+                const TaskPos tp = task_pos(sp, wi.unit);
+                const int row0 = wi.row0 + x * kTileQ;
+                const int n_kv = key_tiles(sp, t, wi.unit, row0, min(kTileQ, wi.rows - x * kTileQ));
+                HeadBias hb;
+                hb.load(sp, wi.head);
+                for (int j = 0; j < n_kv; ++j) {
+                    const int lo = tp.kv_pos + j * kTileKV - (tp.q_pos + row0 + kTileQ - 1);
+                    if (patch_side(sp, lo, lo + kTileQ + kTileKV - 2) != kNear) continue;
+                    if (!feed.put(sp, hb, wi.head, lo, lane, kWaitLimitNs, &sm.abort_flag)) {
+                        report(p.status, &sm.abort_flag, 3000 + 31);
+                        goto teardown;
+                    }
+                }
+            }
         }
     } else {
         // ------------------------------------------------------------------ softmax + epilogue
@@ -263,9 +285,10 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         uint32_t s_cnt = 0, o_cnt = 0;
         const bool store_leader = quarter == 0 && lane == 0;  // one thread per warpgroup issues its TMA stores
         bool store_pending = false;                            // this warpgroup's box may still be read by a store
-        float* const window = reinterpret_cast<float*>(sm.o_stage[x]) + quarter * kWindowFloats;
+        uint32_t bias_cnt = 0;
         for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
             const WorkItem wi = p.items[it];
+            if (wi.rows == 0) break;  // end of this CTA's list
             const int tile_rows = min(kTileQ, wi.rows - x * kTileQ);  // rows of this warpgroup's tile
             if (tile_rows <= 0) continue;
             const Task t = p.tasks[wi.unit];
@@ -274,26 +297,11 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const int n_kv = key_tiles(sp, t, wi.unit, row0, tile_rows);
             const int keys = sp.masked ? visible_keys(tp, t.kv_len, row0 + row) : t.kv_len;  // this row's
             HeadBias hb;
-            if constexpr (kBias) {
-                hb.load(sp, wi.head);
-                if (store_pending) {  // the box becomes the windows
-                    if (store_leader) bulk_wait_group_read<0>();
-                    named_bar_sync(2 + x, 128);
-                    store_pending = false;
-                }
-            }
+            if constexpr (kBias) hb.load(sp, wi.head);
             float m_ref = -INFINITY, l = 0.f;  // reference maximum (powers of two) and row sum
             for (int j = 0; j < n_kv; ++j) {
-                PatchSide side = kNear;
-                float near_bias[kWindow / 32];
-                const int dist_lo = tp.kv_pos + j * kTileKV - (tp.q_pos + row0 + quarter * 32 + 31);  // last row, first column
-                if constexpr (kBias) {
-                    side = patch_side(sp, dist_lo, dist_lo + 31 + kTileKV - 1);
-                    if (side == kNear) {
-#pragma unroll
-                        for (int i = 0; i < kWindow / 32; ++i) near_bias[i] = hb.at(sp, wi.head, dist_lo + i * 32 + lane);
-                    }
-                }
+                const int dist_lo = tp.kv_pos + j * kTileKV - (tp.q_pos + row0 + kTileQ - 1);  // last row, first column
+                const PatchSide side = kBias ? patch_side(sp, dist_lo, dist_lo + kTileQ + kTileKV - 2) : kNear;
                 ZL_WAIT_WARP(&sm.s_full[x], s_cnt & 1, 21);
                 ++s_cnt;
                 tc_fence_after();
@@ -305,60 +313,14 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sv[c * 32 + i] = __uint_as_float(r[i]);
                 }
-                if constexpr (kBias) {
-                    if (side == kNear) fill_window(window, near_bias, lane);
+                if (kBias && side == kNear) {
+                    ZL_WAIT_WARP(&sm.bias_full[x], bias_cnt & 1, 22);
+                    ++bias_cnt;
                 }
                 tmem_wait_ld();
-                const RowScore rs = finish_scores<kCap, kBias>(sv, sp, hb, side, window, dist_lo, p.scale_log2, keys - j * kTileKV, lane);
-                const float mx = rs.max;
-                // lazy reference update: only when the tile maximum is far above the reference; a row that has seen no
-                // key yet has reference -inf, and so long as it sees none (mx = -inf, the difference is NaN) keeps it
-                const bool raise = mx - m_ref > kRescaleThresholdLog2;
-                if (__any_sync(0xffffffffu, raise && j > 0)) {
-                    // rescale O (the previous P V product is complete: S(j) was issued after it)
-                    const float alpha = raise ? ex2(m_ref - mx) : 1.f;
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t r[32];
-                        tmem_ld_x32(lane_addr + col_o + c * 32, r);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-                        tmem_st_x32(lane_addr + col_o + c * 32, r);
-                    }
-                    l *= alpha;
-                }
-                if (raise) {
-                    if (j == 0) l = 0.f;
-                    m_ref = mx;
-                }
-                const float add = rs.base - (m_ref > -INFINITY ? m_ref : 0.f);
-                float2 sum2 = make_float2(0.f, 0.f);
-                // P goes to the MMA warp in two halves of 64 key columns
-                auto half_of_p = [&](int h, auto linear) {
-                    uint32_t pk[kTileKV / 4];
-#pragma unroll
-                    for (int c = 0; c < kTileKV / 2; c += 2) {
-                        const int cc = h * (kTileKV / 2) + c;
-                        const float2 b = decltype(linear)::value ? make_float2(fmaf(rs.step, (float)cc, add), fmaf(rs.step, (float)(cc + 1), add)) : splat(add);
-                        const float2 e = fma2(make_float2(sv[cc], sv[cc + 1]), splat(rs.mul), b);
-                        const float p0 = ex2(e.x), p1 = ex2(e.y);
-                        sum2 = add2(sum2, make_float2(p0, p1));
-                        pk[c / 2] = pack_bf16(p0, p1);
-                    }
-                    tmem_st_x32(lane_addr + col_s + h * 32, pk);
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(&sm.p_half[x][h]);
-                };
-                if (kBias && rs.step != 0.f) {  // warp-uniform
-                    half_of_p(0, std::true_type());
-                    half_of_p(1, std::true_type());
-                } else {
-                    half_of_p(0, std::false_type());
-                    half_of_p(1, std::false_type());
-                }
-                l += sum2.x + sum2.y;
+                softmax_tile<D, kCap, kBias>(sv, sp, hb, p.scale_log2, j == 0, side, sm.window[x] + kTileQ - 1 - row, &sm.bias_empty[x],
+                                             dist_lo + kTileQ - 1 - row, keys - j * kTileKV, true, lane_addr + col_s, lane_addr + col_o,
+                                             sm.p_half[x], m_ref, l);
             }
             // ---- epilogue
             const bool row_ok = row < tile_rows;
@@ -371,7 +333,6 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             }
             const int64_t grow0 = (int64_t)(t.partial_slot >= 0 ? t.partial_slot : t.q_off) + row0;
             const int64_t grow = grow0 + row;
-            if constexpr (kBias) named_bar_sync(2 + x, 128);  // every warp has read its window: the box takes O
             if (tile_rows == kTileQ && n_kv > 0) {
                 // full tile: stage 128 bytes per row at a time in this warpgroup's box and write each box
                 // with one TMA store -- coalesced, and the warpgroup is free for the next item while the

@@ -9,7 +9,9 @@
 // matters is the one that keeps a long sequence from finishing last, so items are sorted
 // longest-first.
 #include <algorithm>
+#include <functional>
 #include <map>
+#include <queue>
 #include <tuple>
 #include <utility>
 
@@ -444,7 +446,7 @@ zl_status build_prefix_schedule(const int32_t* cu_q, const int32_t* cu_kv, int32
     return ZL_OK;
 }
 
-zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard_pos* shard_pos) {
+zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard_pos* shard_pos, int32_t n_sms) {
     const size_t n_shards = s->shard_to_task.size();
     if (n_shards > 0 && !shard_pos) return ZL_ERR_INVALID_ARG;
     // chunks of a shared prefix come before every sequence's own keys: seen by all
@@ -471,14 +473,32 @@ zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard
     }
     s->task_pos = std::move(pos);
 
-    // the same items, ordered by what the mask leaves of them
-    auto by_work = [](std::vector<WorkItem>* items, const std::vector<int64_t>& work) {
+    // The same items, dealt out by what the mask leaves of them.  A CTA of the persistent kernels walks items i, i + grid,
+    // i + 2 grid, ...; under a mask their work differs from a tile to the whole row, and round robin would give the first
+    // CTA the longest item of every round.  So the items, longest first, go to the CTA with the least work so far
+    // (an item costs its tiles and about one more to begin and end); an item without rows ends a list before the longest one.
+    auto by_work = [n_sms](std::vector<WorkItem>* items, const std::vector<int64_t>& work) {
         std::vector<int32_t> order(items->size());
         for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
         std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return work[a] > work[b]; });
-        std::vector<WorkItem> sorted(items->size());
-        for (size_t i = 0; i < order.size(); ++i) sorted[i] = (*items)[order[i]];
-        items->swap(sorted);
+        const int32_t ctas = (int32_t)std::min<size_t>(n_sms, items->size());
+        using Load = std::pair<int64_t, int32_t>;
+        std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+        for (int32_t c = 0; c < ctas; ++c) least.push({0, c});
+        std::vector<std::vector<int32_t>> lists(ctas);
+        size_t longest = 0;
+        for (int32_t i : order) {
+            const Load l = least.top();
+            least.pop();
+            lists[l.second].push_back(i);
+            longest = std::max(longest, lists[l.second].size());
+            least.push({l.first + work[i] + 1, l.second});
+        }
+        std::vector<WorkItem> dealt;
+        for (size_t r = 0; r < longest; ++r)
+            for (int32_t c = 0; c < ctas; ++c)
+                dealt.push_back(r < lists[c].size() ? (*items)[lists[c][r]] : WorkItem{0, 0, 0, 0});
+        items->swap(dealt);
     };
     s->fwd_items_masked = s->fwd_items;
     std::vector<int64_t> work;
