@@ -24,7 +24,6 @@ using namespace score;
 namespace {
 
 constexpr int kThreads = 384;
-constexpr uint64_t kWaitLimitNs = 4000000000ull;
 
 template <int D, int kRows>
 struct FewSmem {
@@ -48,21 +47,25 @@ struct FewSmem {
     volatile int32_t abort_flag;
 };
 
-__device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_flag, int where) {
-    *abort_flag = 1;
-    if (atomicCAS(status, 0, (int)ZL_ERR_TIMEOUT) == 0) status[1] = where;
-}
-
 #define ZL_WAIT(bar, parity, site)                                        \
     do {                                                                  \
-        if (!mbar_wait((bar), (parity), kWaitLimitNs, &sm.abort_flag)) { \
+        if (!wait((bar), (parity), &sm.abort_flag)) { \
             report(p.status, &sm.abort_flag, 5000 + (site));              \
             goto teardown;                                                \
         }                                                                 \
     } while (0)
 #define ZL_WAIT_WARP(bar, parity, site)                                              \
     do {                                                                             \
-        const bool ok_ = mbar_wait((bar), (parity), kWaitLimitNs, &sm.abort_flag); \
+        const bool ok_ = wait((bar), (parity), &sm.abort_flag); \
+        if (!__all_sync(0xffffffffu, ok_)) {                                         \
+            report(p.status, &sm.abort_flag, 5000 + (site));                         \
+            goto teardown;                                                           \
+        }                                                                            \
+    } while (0)
+// The same from the warps that hold tiles in registers.
+#define ZL_WAIT_REGS(bar, parity, site)                                              \
+    do {                                                                             \
+        const bool ok_ = wait_inline((bar), (parity), &sm.abort_flag); \
         if (!__all_sync(0xffffffffu, ok_)) {                                         \
             report(p.status, &sm.abort_flag, 5000 + (site));                         \
             goto teardown;                                                           \
@@ -162,7 +165,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             const uint64_t dk0 = make_desc_sw128(smem_u32(sm.k[0]), 16, 1024);
             const uint64_t dv0 = make_desc_sw128(smem_u32(sm.v[0]), Smem::kBoxBytes, 1024);  // V is the MN-major B operand
             constexpr uint32_t kTileStep = Smem::kTileBytes >> 4, kQStep = (uint32_t)sizeof(sm.q[0]) >> 4;
-            uint32_t item_cnt = 0, kv_cnt = 0, p_cnt[2] = {0, 0};
+            uint32_t item_cnt = 0, kv_cnt = 0, pa_cnt = 0, pb_cnt = 0;
             for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
                 const WorkItem wi = p.items[it];
                 if (wi.rows == 0) break;  // end of this CTA's list
@@ -179,16 +182,18 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         const uint32_t c = kv_cnt + j - 2, vs = c % kStagesV;
                         ZL_WAIT_WARP(&sm.v_full[vs], (c / kStagesV) & 1, 12);
                         const uint64_t dv = dv0 + vs * kTileStep;
-#pragma unroll
+#pragma unroll 1
                         for (int half = 0; half < 2; ++half) {
-                            ZL_WAIT_WARP(&sm.p_half[x][half], p_cnt[x] & 1, 13 + half);
+                            ZL_WAIT_WARP(&sm.p_half[x][half], (x == 0 ? pa_cnt : pb_cnt) & 1, 13);
                             tc_fence_after();
 #pragma unroll
-                            for (int ks = half * (kTileKV / 32); ks < (half + 1) * (kTileKV / 32); ++ks)
-                                if (mma_lane) mma_ts(tmem + kColO + x * 128, tmem + kColS + x * 128 + ks * 8, dv + ks * (2048 >> 4),
-                                                     idesc_o, j > 3 || ks > 0);
+                            for (int ks = 0; ks < kTileKV / 32; ++ks) {
+                                const int at = half * (kTileKV / 32) + ks;
+                                if (mma_lane) mma_ts(tmem + kColO + x * 128, tmem + kColS + x * 128 + at * 8, dv + at * (2048 >> 4),
+                                                     idesc_o, j > 3 || half > 0 || ks > 0);
+                            }
                         }
-                        ++p_cnt[x];
+                        if (x == 0) ++pa_cnt; else ++pb_cnt;
                         if (mma_lane) mma_commit(&sm.v_empty[vs]);
                         if (j >= n_kv) if (mma_lane) mma_commit(&sm.o_full[x]);  // the warpgroup's last tile
                     }
@@ -224,7 +229,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 for (int j = x; j < n_kv; j += 2) {
                     const int lo = tp.kv_pos + j * kTileKV - (tp.q_pos + wi.row0 + kTileQ - 1);
                     if (patch_side(sp, lo, lo + kTileQ + kTileKV - 2) != kNear) continue;
-                    if (!feed.put(sp, hb, wi.head, lo, lane, kWaitLimitNs, &sm.abort_flag)) {
+                    if (!feed.put(sp, hb, wi.head, lo, lane, &sm.abort_flag)) {
                         report(p.status, &sm.abort_flag, 5000 + 31);
                         goto teardown;
                     }
@@ -256,17 +261,22 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             for (int j = x; j < n_kv; j += 2) {
                 const int dist_lo = tp.kv_pos + j * kTileKV - (tp.q_pos + wi.row0 + kTileQ - 1);  // last row, first column
                 const PatchSide side = kBias ? patch_side(sp, dist_lo, dist_lo + kTileQ + kTileKV - 2) : kNear;
-                ZL_WAIT_WARP(&sm.s_full[x], s_cnt & 1, 21);
+                const bool ragged = __any_sync(0xffffffffu, keys - j * kTileKV < kTileKV);
+                ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
                 ++s_cnt;
                 if (!busy) {  // P of rows that do not exist is whatever S was
                     if (kBias && side == kNear) {
-                        ZL_WAIT_WARP(&sm.bias_full[x], bias_cnt & 1, 25);
+                        ZL_WAIT_REGS(&sm.bias_full[x], bias_cnt & 1, 25);
                         ++bias_cnt;
                         mbar_arrive(&sm.bias_empty[x]);
                     }
                     mbar_arrive(&sm.p_half[x][0]);
                     mbar_arrive(&sm.p_half[x][1]);
                     continue;
+                }
+                if (kBias && side == kNear) {
+                    ZL_WAIT_REGS(&sm.bias_full[x], bias_cnt & 1, 26);
+                    ++bias_cnt;
                 }
                 tc_fence_after();
                 float sv[kTileKV];
@@ -277,13 +287,9 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sv[c * 32 + i] = __uint_as_float(r[i]);
                 }
-                if (kBias && side == kNear) {
-                    ZL_WAIT_WARP(&sm.bias_full[x], bias_cnt & 1, 26);
-                    ++bias_cnt;
-                }
                 tmem_wait_ld();
                 softmax_tile<D, kCap, kBias>(sv, sp, hb, p.scale_log2, j == x, side, sm.window[x] + kTileQ - 1 - row, &sm.bias_empty[x],
-                                             dist_lo + kTileQ - 1 - row, keys - j * kTileKV, row_ok, lane_addr + col_s, lane_addr + col_o,
+                                             dist_lo + kTileQ - 1 - row, keys - j * kTileKV, ragged, row_ok, lane_addr + col_s, lane_addr + col_o,
                                              sm.p_half[x], m_ref, l);
             }
             // ---- join: O = (w_0 O_0 + w_1 O_1) / (w_0 l_0 + w_1 l_1), w_x = 2^(m_x - max); warpgroup x writes half of the columns
@@ -291,13 +297,13 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (n_kv > 0) {
                 for (int y = 0; y < 2; ++y)
                     if (n_kv > y) {
-                        ZL_WAIT_WARP(&sm.o_full[y], o_cnt[y] & 1, 22 + y);
+                        ZL_WAIT_REGS(&sm.o_full[y], o_cnt[y] & 1, 22 + y);
                         ++o_cnt[y];
                     }
                 tc_fence_after();
                 sm.stat[x][row] = make_float2(m_ref, l);
                 mbar_arrive(&sm.stat_full);
-                ZL_WAIT_WARP(&sm.stat_full, join_cnt & 1, 27);
+                ZL_WAIT_REGS(&sm.stat_full, join_cnt & 1, 27);
                 const float2 a = sm.stat[0][row], b = sm.stat[1][row];
                 const float m = fmaxf(a.x, b.x);
                 if (m > -INFINITY) {
@@ -311,7 +317,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (busy) {
                 const int64_t grow = (int64_t)(t.partial_slot >= 0 ? t.partial_slot : t.q_off) + wi.row0 + row;
                 const int c0 = x * (D / 2);
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D / 64; ++c) {
                     float o[32];
 #pragma unroll
@@ -352,7 +358,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             tc_fence_before();
             if (n_kv > 0) {  // both accumulators and the statistics have been read
                 mbar_arrive(&sm.join_done);
-                ZL_WAIT_WARP(&sm.join_done, join_cnt & 1, 28);
+                ZL_WAIT_REGS(&sm.join_done, join_cnt & 1, 28);
                 ++join_cnt;
             }
         }

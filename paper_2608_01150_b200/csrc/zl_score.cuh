@@ -16,6 +16,24 @@ constexpr float kLog2e = 1.4426950408889634f;
 // type cannot turn rows into sums of rounding errors.
 constexpr float kRemoved = -1e30f;
 
+// ------------------------------------------------------------------------------------------------ waits
+// The timed loop of a bounded wait is out of line where registers allow a call (the producer and the MMA issuer): the kernels
+// have dozens of wait sites and their loops should stay in the instruction cache.
+constexpr uint64_t kWaitLimitNs = 4000000000ull;
+static __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, const volatile int32_t* abort_flag) {
+    return mbar_wait_slow(bar, parity, kWaitLimitNs, abort_flag);
+}
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, const volatile int32_t* abort_flag) {
+    return mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort_flag);
+}
+__device__ __forceinline__ bool wait_inline(uint64_t* bar, uint32_t parity, const volatile int32_t* abort_flag) {
+    return mbar_wait(bar, parity, kWaitLimitNs, abort_flag);
+}
+__device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_flag, int where) {
+    *abort_flag = 1;
+    if (atomicCAS(status, 0, (int)ZL_ERR_TIMEOUT) == 0) status[1] = where;
+}
+
 // ------------------------------------------------------------------------------------------------ cap
 // tanh(y) / y as a polynomial in y^2 for |y| <= kTanhRange: fitted by iterated reweighted least squares on 4,000
 // Chebyshev nodes, largest relative error 7e-8.  Five multiply-adds in packed fp32 instead of two special-function
@@ -93,12 +111,12 @@ struct WindowFeed {
     float* window;           // kWindow floats
     uint32_t count = 0;
     // Puts the biases of distances lo .. lo + 254 into the window; false: the bounded wait expired.
-    __device__ __forceinline__ bool put(const ScoreParams& sp, const HeadBias& hb, int head, int lo, int lane, uint64_t limit_ns,
+    __device__ __forceinline__ bool put(const ScoreParams& sp, const HeadBias& hb, int head, int lo, int lane,
                                         const volatile int32_t* abort_flag) {
         float v[kWindow / 32];
 #pragma unroll
         for (int i = 0; i < kWindow / 32; ++i) v[i] = hb.at(sp, head, lo + i * 32 + lane);
-        const bool ok = mbar_wait(empty, (count & 1) ^ 1, limit_ns, abort_flag);
+        const bool ok = wait(empty, (count & 1) ^ 1, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) return false;
         ++count;
 #pragma unroll
@@ -109,21 +127,26 @@ struct WindowFeed {
     }
 };
 
-__device__ __forceinline__ float row_max(const float (&sv)[kTileKV]) {
-    // four independent chains: a single running maximum is a 64-deep dependent chain
-    float mx0 = max3(sv[0], sv[1], sv[2]), mx1 = max3(sv[3], sv[4], sv[5]);
-    float mx2 = max3(sv[6], sv[7], sv[8]), mx3 = max3(sv[9], sv[10], sv[11]);
+// Largest of sv[c] * mul + base + step * c, or no more than a bound on it: with a slope, sixteen columns share the larger of
+// their two edges' positions (sixteen independent chains of max either way).
+constexpr int kMaxGroup = 16;
+template <bool kBias>
+__device__ __forceinline__ float row_bound(const float (&sv)[kTileKV], float mul, float base, float step) {
+    float g[kTileKV / kMaxGroup];
 #pragma unroll
-    for (int c = 12; c + 7 < kTileKV; c += 8) {
-        mx0 = max3(mx0, sv[c], sv[c + 1]);
-        mx1 = max3(mx1, sv[c + 2], sv[c + 3]);
-        mx2 = max3(mx2, sv[c + 4], sv[c + 5]);
-        mx3 = max3(mx3, sv[c + 6], sv[c + 7]);
+    for (int i = 0; i < kTileKV / kMaxGroup; ++i) {
+        const int c = i * kMaxGroup;
+        g[i] = max3(sv[c], sv[c + 1], sv[c + 2]);
+#pragma unroll
+        for (int k = 3; k + 1 < kMaxGroup; k += 2) g[i] = max3(g[i], sv[c + k], sv[c + k + 1]);
     }
-    // columns 124..127 remain (12 + 8 * 14 = 124)
-    mx0 = max3(mx0, sv[kTileKV - 4], sv[kTileKV - 3]);
-    mx1 = max3(mx1, sv[kTileKV - 2], sv[kTileKV - 1]);
-    return fmaxf(max3(mx0, mx1, mx2), mx3);
+#pragma unroll
+    for (int i = 0; i < kTileKV / kMaxGroup; ++i) {
+        g[i] = fmaxf(g[i], sv[i * kMaxGroup + kMaxGroup - 1]);
+        if constexpr (kBias) g[i] = fmaf(g[i], mul, fmaf(step, (float)(i * kMaxGroup), base));
+    }
+    const float m = fmaxf(max3(max3(g[0], g[1], g[2]), g[3], g[4]), max3(g[5], g[6], g[7]));
+    return kBias ? m + fmaxf(0.f, step * (kMaxGroup - 1)) : m * mul;
 }
 
 // An upper bound of a row's scores serves as the softmax's reference as well as the maximum, so long as it is not far above:
@@ -136,13 +159,13 @@ constexpr float kRescaleThresholdLog2 = 8.0f;
 
 // One tile of the online softmax: a row of raw products `sv` becomes P (bf16, over S in TMEM, handed over in two halves of 64
 // columns by `p_half`); the row's reference m_ref (powers of two) and sum l move on, O in TMEM is rescaled when the
-// reference is raised.  Columns from `valid` on are invisible.  A near tile adds bias[c] (and releases the window), a far
+// reference is raised.  Columns from `valid` on are invisible (`ragged`: for some row of the warp).  A near tile adds bias[c] (and releases the window), a far
 // one a bias that is linear in the column, from distance `dist0` of column 0: that one stays in the exponential's
 // multiply-add and costs nothing where it is constant.
 template <int D, bool kCap, bool kBias>
 __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScoreParams& sp, const HeadBias& hb, float scale_log2,
                                              bool first, PatchSide side, const float* bias, uint64_t* bias_empty, int dist0,
-                                             int valid, bool row_ok, uint32_t s_addr, uint32_t o_addr, uint64_t (&p_half)[2],
+                                             int valid, bool ragged, bool row_ok, uint32_t s_addr, uint32_t o_addr, uint64_t (&p_half)[2],
                                              float& m_ref, float& l) {
     float mul = scale_log2, base = 0.f, step = 0.f;  // score(c) = sv[c] * mul + base + step * c, in powers of two
     float2 sum2 = make_float2(0.f, 0.f);
@@ -164,7 +187,7 @@ __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScorePa
         if constexpr (!kBias) {
             // |C(x)| <= |x|, so the largest magnitude bounds the row's scores: where that does not ask for a higher
             // reference, cap and exponential run in one pass, the multiply-adds of one score under the exponential of another
-            const bool easy = !row_ok || (near_zero && valid >= kTileKV && big * scale_log2 - m_ref <= kRescaleThresholdLog2);
+            const bool easy = !row_ok || (near_zero && !ragged && big * scale_log2 - m_ref <= kRescaleThresholdLog2);
             if (__all_sync(0xffffffffu, easy)) {
                 const float2 nm = splat(-m_ref);
                 constexpr int kGroup = 8;  // pairs whose chains run side by side
@@ -229,7 +252,7 @@ __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScorePa
         } else {
             step = side == kFarPos ? -hb.slope : hb.slope;
             base = (side == kFarPos ? hb.far_pos : hb.far_neg) + step * (float)dist0;
-            if (fabsf(step) * (kTileKV - 1) > kSlack) {  // warp-uniform: steep slopes get their exact maximum
+            if (fabsf(step) * (kMaxGroup - 1) > kSlack) {  // warp-uniform: steep slopes get their exact maximum
 #pragma unroll
                 for (int c = 0; c < kTileKV; ++c) sv[c] = fmaf(sv[c], mul, fmaf(step, (float)c, base));
                 mul = 1.f;
@@ -237,19 +260,19 @@ __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScorePa
             }
         }
     }
-    if (__any_sync(0xffffffffu, valid < kTileKV)) {
+    if (ragged) {
 #pragma unroll
         for (int c = 0; c < kTileKV; ++c)
             if (c >= valid) sv[c] = -INFINITY;  // select, never multiply
     }
-    const float mx = fmaf(row_max(sv), mul, base + fmaxf(0.f, step * (kTileKV - 1)));
+    const float mx = row_bound<kBias>(sv, mul, base, step);
     // lazy reference update: only when the tile maximum is far above the reference; a row that has seen no key yet has
     // reference -inf, and so long as it sees none (mx = -inf, the difference is NaN) keeps it
     const bool raise = row_ok && mx - m_ref > kRescaleThresholdLog2;
     if (__any_sync(0xffffffffu, raise && !first)) {
         // rescale O (the previous P V product is complete: this S was issued after it)
         const float alpha = raise ? ex2(m_ref - mx) : 1.f;
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
             uint32_t r[32];
             tmem_ld_x32(o_addr + c * 32, r);

@@ -30,7 +30,6 @@ using namespace score;
 
 namespace {
 
-constexpr uint64_t kWaitLimitNs = 4000000000ull;
 
 // Warp roles (16 warps): warp 0 TMA producer, warp 1 MMA issuer, warps 2-3 idle,
 // warps 4-7 and 8-11 two P/dS warpgroups (query columns 0-63 and 64-127 of every tile, one key
@@ -63,21 +62,25 @@ struct ScoredBwdSmem {
     volatile int32_t abort_flag;
 };
 
-__device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_flag, int where) {
-    *abort_flag = 1;
-    if (atomicCAS(status, 0, (int)ZL_ERR_TIMEOUT) == 0) status[1] = where;
-}
-
 #define ZL_WAIT(bar, parity, site)                                        \
     do {                                                                  \
-        if (!mbar_wait((bar), (parity), kWaitLimitNs, &sm.abort_flag)) { \
+        if (!wait((bar), (parity), &sm.abort_flag)) { \
             report(p.status, &sm.abort_flag, 4000 + (site));              \
             goto teardown;                                                \
         }                                                                 \
     } while (0)
 #define ZL_WAIT_WARP(bar, parity, site)                                              \
     do {                                                                             \
-        const bool ok_ = mbar_wait((bar), (parity), kWaitLimitNs, &sm.abort_flag); \
+        const bool ok_ = wait((bar), (parity), &sm.abort_flag); \
+        if (!__all_sync(0xffffffffu, ok_)) {                                         \
+            report(p.status, &sm.abort_flag, 4000 + (site));                         \
+            goto teardown;                                                           \
+        }                                                                            \
+    } while (0)
+// The same from the warps that hold tiles in registers.
+#define ZL_WAIT_REGS(bar, parity, site)                                              \
+    do {                                                                             \
+        const bool ok_ = wait_inline((bar), (parity), &sm.abort_flag); \
         if (!__all_sync(0xffffffffu, ok_)) {                                         \
             report(p.status, &sm.abort_flag, 4000 + (site));                         \
             goto teardown;                                                           \
@@ -392,8 +395,8 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             for (int i = 0; i < kWindow / 32; ++i) near_bias[i] = hb.at(sp, wi.head, dist_lo + i * 32 + lane);
                         }
                     }
-                    ZL_WAIT_WARP(&sm.s_full, it_cnt & 1, 22);
-                    if constexpr (kCap) ZL_WAIT_WARP(&sm.q_full[stage], (it_cnt >> 1) & 1, 26);  // the LSE came with Q: already complete
+                    ZL_WAIT_REGS(&sm.s_full, it_cnt & 1, 22);
+                    if constexpr (kCap) ZL_WAIT_REGS(&sm.q_full[stage], (it_cnt >> 1) & 1, 26);  // the LSE came with Q: already complete
                     tc_fence_after();
                     float pr[64];        // P of this thread's key row, fp32
                     uint32_t slope[32];  // C' of the capped scores, pairs of fp16 (off by at most 2^-11 of the value)
@@ -479,8 +482,8 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     tc_fence_before();
                     mbar_arrive(&sm.p_full);
 
-                    ZL_WAIT_WARP(&sm.dp_full, it_cnt & 1, 23);
-                    if (it_cnt > 0) ZL_WAIT_WARP(&sm.ds_free, (it_cnt - 1) & 1, 24);  // dS buffer consumed by dK/dQ
+                    ZL_WAIT_REGS(&sm.dp_full, it_cnt & 1, 23);
+                    if (it_cnt > 0) ZL_WAIT_REGS(&sm.ds_free, (it_cnt - 1) & 1, 24);  // dS buffer consumed by dK/dQ
                     if (store_pending) {
                         // this warpgroup's box of the dS tile staged the previous item's dK / dV tile
                         if (store_leader) bulk_wait_group_read<0>();
@@ -586,7 +589,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 window[lane] = bucket_sum[0];
                 window[lane + 32] = bucket_sum[1];
                 mbar_arrive(&sm.sums_full);
-                ZL_WAIT_WARP(&sm.sums_full, sums_cnt & 1, 27);
+                ZL_WAIT_REGS(&sm.sums_full, sums_cnt & 1, 27);
                 const int b = threadIdx.x - 128;  // 0 .. 255
                 if (b < kMaxBuckets) {
                     float v = 0.f;
@@ -595,13 +598,13 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     sp.bucket_part[((int64_t)wi.head * sp.n_kv_tiles + g.tile_begin + wi.row0 / kTileKV) * kMaxBuckets + b] = v;
                 }
                 mbar_arrive(&sm.sums_empty);
-                ZL_WAIT_WARP(&sm.sums_empty, sums_cnt & 1, 28);  // the windows are free again
+                ZL_WAIT_REGS(&sm.sums_empty, sums_cnt & 1, 28);  // the windows are free again
                 ++sums_cnt;
             }
             // ---- epilogue: warpgroup 0 stores dV, warpgroup 1 stores dK (scaled)
             const bool seen = it_cnt != it_first;  // else no query sees these keys: the gradients are zero
             if (seen) {
-                ZL_WAIT_WARP(&sm.acc_full, item_cnt & 1, 25);
+                ZL_WAIT_REGS(&sm.acc_full, item_cnt & 1, 25);
                 ++item_cnt;
                 tc_fence_after();
             }
@@ -612,13 +615,13 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 // tile and write them with one TMA store each -- coalesced, and the warpgroup moves on to
                 // the next item while the copy engine drains the box
                 const uint32_t box_addr = smem_u32(sm.ds) + wg * Smem::kBoxBytes + row * 128;
-#pragma unroll
+#pragma unroll 1
                 for (int b = 0; b < kBoxes; ++b) {
                     if (b > 0) {
                         if (store_leader) bulk_wait_group_read<0>();
                         named_bar_sync(2 + wg, 128);
                     }
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < 2; ++c) {
                         uint32_t r[32];
                         tmem_ld_x32(lane_addr + col_acc + b * 64 + c * 32, r);
@@ -645,7 +648,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             } else {
                 const int64_t grow = (int64_t)g.kv_off + wi.row0 + row;
                 __nv_bfloat16* dst = (wg == 0 ? p.dv : p.dk) + grow * p.grad_row_stride + wi.head * D;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t r[32];
                     if (seen) {
@@ -687,7 +690,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 const Task t = p.tasks[task];
                 const int n_q = (t.q_len + kTileQ - 1) / kTileQ;
                 for (int qt = first_tile(sp, t, task, wi.row0); qt < n_q; ++qt, ++it_cnt) {
-                    ZL_WAIT_WARP(&sm.dq_full, it_cnt & 1, 31);
+                    ZL_WAIT_REGS(&sm.dq_full, it_cnt & 1, 31);
                     tc_fence_after();
                     {
                         // read the whole tile (frees the TMEM columns for the next dP^T), then stage

@@ -28,7 +28,6 @@ using namespace score;
 namespace {
 
 constexpr int kFwdThreads = 384;
-constexpr uint64_t kWaitLimitNs = 4000000000ull;
 
 template <int D>
 struct ScoredFwdSmem {
@@ -49,16 +48,10 @@ struct ScoredFwdSmem {
     volatile int32_t abort_flag;
 };
 
-__device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_flag, int where) {
-    *abort_flag = 1;
-    if (atomicCAS(status, 0, (int)ZL_ERR_TIMEOUT) == 0) status[1] = where;
-}
-
-
 // Wait used by a single elected thread.
 #define ZL_WAIT(bar, parity, site)                                        \
     do {                                                                  \
-        if (!mbar_wait((bar), (parity), kWaitLimitNs, &sm.abort_flag)) { \
+        if (!wait((bar), (parity), &sm.abort_flag)) { \
             report(p.status, &sm.abort_flag, 3000 + (site));              \
             goto teardown;                                                \
         }                                                                 \
@@ -67,7 +60,16 @@ __device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_
 // reconverges before the .sync.aligned TMEM instructions that follow.
 #define ZL_WAIT_WARP(bar, parity, site)                                              \
     do {                                                                             \
-        const bool ok_ = mbar_wait((bar), (parity), kWaitLimitNs, &sm.abort_flag); \
+        const bool ok_ = wait((bar), (parity), &sm.abort_flag); \
+        if (!__all_sync(0xffffffffu, ok_)) {                                         \
+            report(p.status, &sm.abort_flag, 3000 + (site));                         \
+            goto teardown;                                                           \
+        }                                                                            \
+    } while (0)
+// The same from the warps that hold tiles in registers.
+#define ZL_WAIT_REGS(bar, parity, site)                                              \
+    do {                                                                             \
+        const bool ok_ = wait_inline((bar), (parity), &sm.abort_flag); \
         if (!__all_sync(0xffffffffu, ok_)) {                                         \
             report(p.status, &sm.abort_flag, 3000 + (site));                         \
             goto teardown;                                                           \
@@ -193,13 +195,13 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             // (one half of the key columns: P arrives in two halves so that the first four K steps
             // run while the softmax warps still work on the second half)
             auto issue_pv = [&](int x, uint32_t stage, bool acc, int half) {
-                const uint64_t dv = dv0 + stage * kTileStep;
+                const uint64_t dv = dv0 + stage * kTileStep + half * (kTileKV / 32) * (2048 >> 4);
+                const uint32_t tp = tmem + kColS + x * 128 + half * (kTileKV / 32) * 8;
 #pragma unroll
-                for (int ks = half * (kTileKV / 32); ks < (half + 1) * (kTileKV / 32); ++ks)
-                    if (mma_lane) mma_ts(tmem + kColO + x * 128, tmem + kColS + x * 128 + ks * 8, dv + ks * (2048 >> 4), idesc_o,
-                           acc || ks > 0);
+                for (int ks = 0; ks < kTileKV / 32; ++ks)
+                    if (mma_lane) mma_ts(tmem + kColO + x * 128, tp + ks * 8, dv + ks * (2048 >> 4), idesc_o, acc || ks > 0);
             };
-            uint32_t q_cnt = 0, qb_cnt = 0, kv_cnt = 0, pa_cnt = 0, pb_cnt = 0;
+            uint32_t q_cnt = 0, qb_cnt = 0, kv_cnt = 0, p_cnt[2] = {0, 0};
             for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
                 const WorkItem wi = p.items[it];
                 if (wi.rows == 0) break;  // end of this CTA's list
@@ -211,45 +213,42 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 if (n_kv == 0) continue;
                 ZL_WAIT_WARP(&sm.q_full[0], q_cnt & 1, 11);
                 ++q_cnt;
-                ZL_WAIT_WARP(&sm.kv_full[kv_cnt % kStages], (kv_cnt / kStages) & 1, 12);
-                tc_fence_after();
-                if (n_a > 0) issue_s(0, kv_cnt % kStages);
-                if (has_b) {
-                    ZL_WAIT_WARP(&sm.q_full[1], qb_cnt & 1, 13);
-                    ++qb_cnt;
-                    if (n_b > 0) issue_s(1, kv_cnt % kStages);
-                }
-                if (n_kv == 1) if (mma_lane) mma_commit(&sm.q_empty);
-                for (int j = 0; j < n_kv; ++j, ++kv_cnt) {
-                    const uint32_t s = kv_cnt % kStages, nk = kv_cnt + 1, sn = nk % kStages;
-                    if (j < n_a) {
-                        // tile A: P_A(j) is in TMEM (S_A(j) fully read, O_A rescaled if needed); K(j), V(j)
-                        // were waited for when S(j) was issued
-                        ZL_WAIT_WARP(&sm.p_half[0][0], pa_cnt & 1, 14);
-                        tc_fence_after();
-                        issue_pv(0, s, j > 0, 0);
-                        ZL_WAIT_WARP(&sm.p_half[0][1], pa_cnt & 1, 15);
-                        ++pa_cnt;
-                        tc_fence_after();
-                        issue_pv(0, s, true, 1);
-                        if (j + 1 == n_a) if (mma_lane) mma_commit(&sm.o_full[0]);
+                // step j: P_A V(j), S_A(j + 1), P_B V(j), S_B(j + 1); one copy of each MMA group
+#pragma unroll 1
+                for (int j = -1; j < n_kv; ++j) {
+                    const uint32_t s = (kv_cnt + j) % kStages, nk = kv_cnt + j + 1, sn = nk % kStages;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int n_x = x == 0 ? n_a : n_b;
+                        if (j >= 0 && j < n_x) {
+                            // P_x(j) is in TMEM (S_x(j) fully read, O_x rescaled if needed); K(j), V(j) were waited for
+                            // when S(j) was issued
+#pragma unroll
+                            for (int half = 0; half < 2; ++half) {
+                                ZL_WAIT_WARP(&sm.p_half[x][half], p_cnt[x] & 1, 14);
+                                tc_fence_after();
+                                issue_pv(x, s, j > 0 || half > 0, half);
+                            }
+                            ++p_cnt[x];
+                            if (j + 1 == n_x) if (mma_lane) mma_commit(&sm.o_full[x]);
+                        }
+                        if (x == 0) {
+                            if (j + 1 < n_kv) ZL_WAIT_WARP(&sm.kv_full[sn], (nk / kStages) & 1, 16);
+                        } else {
+                            if (j >= 0) if (mma_lane) mma_commit(&sm.kv_empty[s]);  // S(j) and P(j) V of both tiles are the stage's last readers
+                            if (j < 0 && has_b) {
+                                ZL_WAIT_WARP(&sm.q_full[1], qb_cnt & 1, 13);
+                                ++qb_cnt;
+                            }
+                        }
+                        if (j + 1 < n_x) {
+                            tc_fence_after();
+                            issue_s(x, sn);  // overwrites P_x(j): ordered after P_x V on the tensor pipe
+                        }
                     }
-                    if (j + 1 < n_kv) ZL_WAIT_WARP(&sm.kv_full[sn], (nk / kStages) & 1, 16);
-                    if (j + 1 < n_a) issue_s(0, sn);  // overwrites P_A(j): ordered after P_A V on the tensor pipe
-                    if (j < n_b) {
-                        ZL_WAIT_WARP(&sm.p_half[1][0], pb_cnt & 1, 17);
-                        tc_fence_after();
-                        issue_pv(1, s, j > 0, 0);
-                        ZL_WAIT_WARP(&sm.p_half[1][1], pb_cnt & 1, 18);
-                        ++pb_cnt;
-                        tc_fence_after();
-                        issue_pv(1, s, true, 1);
-                        if (j + 1 == n_b) if (mma_lane) mma_commit(&sm.o_full[1]);
-                    }
-                    if (mma_lane) mma_commit(&sm.kv_empty[s]);  // S_A(j), S_B(j), P_A V(j), P_B V(j) are the stage's last readers
-                    if (j + 1 < n_b) issue_s(1, sn);
                     if (j + 2 == n_kv) if (mma_lane) mma_commit(&sm.q_empty);  // last S of the item issued
                 }
+                kv_cnt += n_kv;
             }
         } else if (kBias && warp >= 2) {  // (the other lanes of warp 0 have nothing to do)
             // -------------------------------------------------------------- biases of near tiles: warp 2 tile A, warp 3 tile B
@@ -267,7 +266,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 for (int j = 0; j < n_kv; ++j) {
                     const int lo = tp.kv_pos + j * kTileKV - (tp.q_pos + row0 + kTileQ - 1);
                     if (patch_side(sp, lo, lo + kTileQ + kTileKV - 2) != kNear) continue;
-                    if (!feed.put(sp, hb, wi.head, lo, lane, kWaitLimitNs, &sm.abort_flag)) {
+                    if (!feed.put(sp, hb, wi.head, lo, lane, &sm.abort_flag)) {
                         report(p.status, &sm.abort_flag, 3000 + 31);
                         goto teardown;
                     }
@@ -302,8 +301,13 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             for (int j = 0; j < n_kv; ++j) {
                 const int dist_lo = tp.kv_pos + j * kTileKV - (tp.q_pos + row0 + kTileQ - 1);  // last row, first column
                 const PatchSide side = kBias ? patch_side(sp, dist_lo, dist_lo + kTileQ + kTileKV - 2) : kNear;
-                ZL_WAIT_WARP(&sm.s_full[x], s_cnt & 1, 21);
+                const bool ragged = __any_sync(0xffffffffu, keys - j * kTileKV < kTileKV);
+                ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
                 ++s_cnt;
+                if (kBias && side == kNear) {
+                    ZL_WAIT_REGS(&sm.bias_full[x], bias_cnt & 1, 22);
+                    ++bias_cnt;
+                }
                 tc_fence_after();
                 float sv[kTileKV];
 #pragma unroll
@@ -313,13 +317,9 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sv[c * 32 + i] = __uint_as_float(r[i]);
                 }
-                if (kBias && side == kNear) {
-                    ZL_WAIT_WARP(&sm.bias_full[x], bias_cnt & 1, 22);
-                    ++bias_cnt;
-                }
                 tmem_wait_ld();
                 softmax_tile<D, kCap, kBias>(sv, sp, hb, p.scale_log2, j == 0, side, sm.window[x] + kTileQ - 1 - row, &sm.bias_empty[x],
-                                             dist_lo + kTileQ - 1 - row, keys - j * kTileKV, true, lane_addr + col_s, lane_addr + col_o,
+                                             dist_lo + kTileQ - 1 - row, keys - j * kTileKV, ragged, true, lane_addr + col_s, lane_addr + col_o,
                                              sm.p_half[x], m_ref, l);
             }
             // ---- epilogue
@@ -327,7 +327,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const float inv_l = (l > 0.f) ? 1.f / l : 0.f;
             const float lse = (l > 0.f) ? (m_ref + log2f(l)) * 0.6931471805599453f : -INFINITY;
             if (n_kv > 0) {
-                ZL_WAIT_WARP(&sm.o_full[x], o_cnt & 1, 23);
+                ZL_WAIT_REGS(&sm.o_full[x], o_cnt & 1, 23);
                 ++o_cnt;
                 tc_fence_after();
             }
@@ -339,7 +339,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 // copy engine drains the box
                 const uint32_t box_row = smem_u32(sm.o_stage[x]) + row * 128;
                 if (t.partial_slot >= 0) {
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {  // 32 fp32 columns per box
                         if (c > 0 || store_pending) {
                             if (store_leader) bulk_wait_group_read<0>();
@@ -364,13 +364,13 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     }
                     p.lse_partial[(int64_t)wi.head * p.partial_rows + grow] = lse;
                 } else {
-#pragma unroll
+#pragma unroll 1
                     for (int b = 0; b < D / 64; ++b) {  // 64 bf16 columns per box
                         if (b > 0 || store_pending) {
                             if (store_leader) bulk_wait_group_read<0>();
                             named_bar_sync(2 + x, 128);
                         }
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < 2; ++c) {
                             uint32_t r[32];
                             tmem_ld_x32(lane_addr + col_o + b * 64 + c * 32, r);
@@ -397,7 +397,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 store_pending = true;
             } else if (t.partial_slot >= 0) {
                 float* dst = p.o_partial + (grow * p.n_heads + wi.head) * D;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t r[32];
                     if (n_kv > 0) {
@@ -419,7 +419,7 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 if (row_ok) p.lse_partial[(int64_t)wi.head * p.partial_rows + grow] = lse;
             } else {
                 __nv_bfloat16* dst = p.o + (grow * p.n_heads + wi.head) * D;
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t r[32];
                     if (n_kv > 0) {
