@@ -645,7 +645,14 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         sp = score->params;
         sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
         if (score->capped) p.lse_tiles = reinterpret_cast<float*>(ws + at.lse);
-        if (d_bucket_bias) sp.bucket_part = reinterpret_cast<float*>(ws + at.part);
+        if (d_bucket_bias) {
+            sp.bucket_part = reinterpret_cast<float*>(ws + at.part);
+            p.d_bucket_bias = d_bucket_bias;
+            p.bucket_part = sp.bucket_part;
+            p.n_buckets = sp.n_buckets;
+            p.n_kv_tiles = s.n_kv_tiles;
+        }
+        p.zero_dq = !s.shared_prefix;
         if (sp.masked && t->sm_margin == 0) {
             p.items = t->d_bwd_items_masked;
             p.n_items = (int32_t)s.bwd_items_masked.size();
@@ -653,7 +660,7 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     }
 
     if (first) {
-        if (cudaMemsetAsync(p.dq_acc, 0, (size_t)s.dq_acc_rows * s.n_heads * s.head_dim * sizeof(float), cs) != cudaSuccess)
+        if (!p.zero_dq && cudaMemsetAsync(p.dq_acc, 0, (size_t)s.dq_acc_rows * s.n_heads * s.head_dim * sizeof(float), cs) != cudaSuccess)
             return ZL_ERR_CUDA;
         LaunchTimer lt(t, ZL_K_BWD_PRE, cs);
         if (launch_bwd_pre(s.head_dim, p, t->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
@@ -684,7 +691,7 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         if (score) {
             const ScoreKind kind = !score->biased ? kScorePlain : (d_bucket_bias ? kScoreBiasGrad : kScoreBias);
             // heads that a key tile's tasks leave out have no share
-            if (d_bucket_bias && cudaMemsetAsync(sp.bucket_part, 0, (size_t)s.n_kv_tiles * s.n_heads * kMaxBuckets * sizeof(float), cs) != cudaSuccess)
+            if (d_bucket_bias && !s.all_heads && cudaMemsetAsync(sp.bucket_part, 0, (size_t)s.n_kv_tiles * s.n_heads * kMaxBuckets * sizeof(float), cs) != cudaSuccess)
                 return ZL_ERR_CUDA;
             if (launch_scored_bwd(s.head_dim, score->capped, kind, tq, tk, tv, tdo, tdq, tdk, tdv, p, sp, grid, cs) != cudaSuccess)
                 return ZL_ERR_CUDA;
@@ -695,10 +702,6 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         LaunchTimer lt(t, ZL_K_BWD_POST, cs);
         if (launch_bwd_post(s.head_dim, p, t->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
         g_launches.fetch_add(1);
-        if (d_bucket_bias) {
-            if (launch_bucket_reduce(sp, d_bucket_bias, cs) != cudaSuccess) return ZL_ERR_CUDA;
-            g_launches.fetch_add(1);
-        }
     }
     return ZL_OK;
 }

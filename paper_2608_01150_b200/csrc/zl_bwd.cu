@@ -130,6 +130,11 @@ __global__ void __launch_bounds__(kPreThreads) zl_bwd_pre_kernel(const BwdParams
                 const float l = lse[k];
                 if (l > -INFINITY && l < INFINITY) xl = -l * inv_scale;
             }
+            if (p.zero_dq) {
+                float4* acc = reinterpret_cast<float4*>(p.dq_acc + ((int64_t)slot_row[k] * p.n_heads + head[k]) * D) + quarter;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) acc[4 * i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
             // lane quarter 0 writes elements 0..7 of its row (-LSE/scale pieces), quarter 1 elements 8..15 (-D pieces)
             if (quarter < 2) {
                 __nv_bfloat16 hp[3];
@@ -152,15 +157,36 @@ __global__ void __launch_bounds__(kPreThreads) zl_bwd_pre_kernel(const BwdParams
 }
 
 // ======================================================================= post
+// Gradient of a bucket table for one head: four groups of 64 threads, a thread per bucket, walk the key tiles' shares; sums
+// in 64 bits, joined in a fixed order.
+__device__ __forceinline__ void sum_bucket_parts(const BwdParams& p, int head) {
+    static_assert(kPreThreads == 4 * kMaxBuckets, "a thread per bucket and group");
+    __shared__ double part[4][kMaxBuckets];
+    const int b = threadIdx.x % kMaxBuckets, grp = threadIdx.x / kMaxBuckets;
+    const float* src = p.bucket_part + (int64_t)head * p.n_kv_tiles * kMaxBuckets + b;
+    double v = 0.0;
+#pragma unroll 8
+    for (int t = grp; t < p.n_kv_tiles; t += 4) v += (double)__ldg(src + (int64_t)t * kMaxBuckets);
+    part[grp][b] = v;
+    __syncthreads();
+    if (grp == 0 && b < p.n_buckets)
+        p.d_bucket_bias[(int64_t)b * p.n_heads + head] = (float)(((part[0][b] + part[1][b]) + part[2][b]) + part[3][b]);
+}
+
 template <int D>
-__global__ void __launch_bounds__(kPreThreads) zl_bwd_post_kernel(const BwdParams p) {
+__global__ void __launch_bounds__(kPreThreads) zl_bwd_post_kernel(const BwdParams p, const int n_blocks) {
+    // Blocks from n_blocks on sum the bucket table's gradient, one head each.
+    if ((int)blockIdx.x >= n_blocks) {
+        sum_bucket_parts(p, (int)blockIdx.x - n_blocks);
+        return;
+    }
     // One warp per padded query row: every head of the row in batches of four, all four 16-byte loads
     // of a batch issued before the first conversion (2 KB in flight per warp at d=128).
     constexpr int V = D / 32;
     constexpr int kBatch = 4;
     const int lane = threadIdx.x & 31;
     for (int64_t slot_row = (int64_t)blockIdx.x * (kPreThreads / 32) + (threadIdx.x >> 5); slot_row < p.dq_rows;
-         slot_row += (int64_t)gridDim.x * (kPreThreads / 32)) {
+         slot_row += (int64_t)n_blocks * (kPreThreads / 32)) {
         const QGroup g = p.q_groups[find_q_group(p.q_groups, p.n_q_groups, (int)slot_row)];
         const int r = (int)slot_row - g.slot;
         if (r >= g.q_len) continue;
@@ -742,9 +768,9 @@ cudaError_t launch_bwd_main(int head_dim, const CUtensorMap& tq, const CUtensorM
 
 cudaError_t launch_bwd_post(int head_dim, const BwdParams& p, int n_sms, cudaStream_t stream) {
     if (p.dq_rows == 0) return cudaSuccess;
-    const int grid = n_sms * 8;
-    if (head_dim == 128) zl_bwd_post_kernel<128><<<grid, kPreThreads, 0, stream>>>(p);
-    else zl_bwd_post_kernel<64><<<grid, kPreThreads, 0, stream>>>(p);
+    const int n_blocks = n_sms * 8, grid = n_blocks + (p.d_bucket_bias ? p.n_heads : 0);
+    if (head_dim == 128) zl_bwd_post_kernel<128><<<grid, kPreThreads, 0, stream>>>(p, n_blocks);
+    else zl_bwd_post_kernel<64><<<grid, kPreThreads, 0, stream>>>(p, n_blocks);
     return cudaGetLastError();
 }
 

@@ -63,6 +63,10 @@ struct BwdParams {
     uint8_t* aug;   // [H, q_pad_total / 128] tiles of 4 KB: bf16 splits of -lse/scale and -rowsum(dO o O)
     int32_t* status;
     float* lse_tiles;  // [H, q_pad_total] LSE * log2(e), 1e30 for rows without a key; NULL unless scores are capped
+    bool zero_dq;      // the preprocess kernel clears dq_acc (its rows are the padded query rows)
+    float* d_bucket_bias;      // [n_buckets, H] gradient of the bucket table, summed beside the dQ conversion; NULL: not wanted
+    const float* bucket_part;  // [H, n_kv_tiles, kMaxBuckets] key tiles' shares of it
+    int32_t n_buckets, n_kv_tiles;
 };
 
 // Scores beyond scale * q.k (zl_score), as the kernels read them.
@@ -91,7 +95,6 @@ cudaError_t launch_few_rows(int head_dim, bool capped, ScoreKind kind, const CUt
 cudaError_t launch_scored_bwd(int head_dim, bool capped, ScoreKind kind, const CUtensorMap& tq, const CUtensorMap& tk,
                               const CUtensorMap& tv, const CUtensorMap& tdo, const CUtensorMap& tdq, const CUtensorMap& tdk,
                               const CUtensorMap& tdv, const BwdParams& p, const ScoreParams& sp, int grid, cudaStream_t stream);
-cudaError_t launch_bucket_reduce(const ScoreParams& sp, float* d_bucket_bias, cudaStream_t stream);
 
 cudaError_t launch_bwd_pre(int head_dim, const BwdParams& p, int n_sms, cudaStream_t stream);
 cudaError_t launch_bwd_main(int head_dim, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,

@@ -108,6 +108,7 @@ struct Schedule {
     int64_t dq_acc_rows = 0;                // rows of the dQ accumulator in the workspace
     int32_t n_kv_tiles = 0;                 // 128-row key tiles of all kv groups
     int32_t max_item_rows = 0;              // most query rows of a forward item
+    bool all_heads = true;                  // every task covers all heads
     bool shared_prefix = false;             // built by build_prefix_schedule: query ranges nest
     // Positions (zl_set_positions): one entry per task, and the work lists dealt out to the CTAs by what the mask leaves of
     // each item (an item without rows ends a CTA's list).

@@ -60,11 +60,16 @@ __device__ __forceinline__ float tanh_any(float y) {
 }
 
 // ------------------------------------------------------------------------------------------------ bias by distance
+// The bucket of a signed distance, -1 for none.
+__device__ __forceinline__ int bucket_at(const ScoreParams& sp, int dist) {
+    const int b = __ldg(sp.bucket_of + (min(max(dist, -sp.reach), sp.reach) + sp.reach));
+    return (uint32_t)b < (uint32_t)sp.n_buckets ? b : -1;
+}
 // The bucket part for a signed distance, in powers of two.
 __device__ __forceinline__ float bucket_bias_at(const ScoreParams& sp, int head, int dist) {
     if (!sp.bucket_bias) return 0.f;
-    const int b = __ldg(sp.bucket_of + (min(max(dist, -sp.reach), sp.reach) + sp.reach));
-    if ((uint32_t)b >= (uint32_t)sp.n_buckets) return 0.f;
+    const int b = bucket_at(sp, dist);
+    if (b < 0) return 0.f;
     const float v = __ldg(sp.bucket_bias + (int64_t)b * sp.n_heads + head);
     return v <= kRemoved ? -INFINITY : v * kLog2e;
 }

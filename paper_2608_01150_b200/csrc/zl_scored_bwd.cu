@@ -1,4 +1,4 @@
-// Backward main kernel of scored attention (sm_100a), and the sum of the bucket bias's gradient.
+// Backward main kernel of scored attention (sm_100a).
 //
 //     P = exp(s - LSE),  G = P o (dO V^T - D),  dS = G C'(scale q.k)
 //     dV = P^T dO,  dK = scale dS^T Q,  dQ = scale dS K,  dtable[b][h] = sum of G over the pairs in bucket b
@@ -14,9 +14,10 @@
 //     gradient is a sum of large cancelling terms and is fp32 from end to end.
 //   * The table's gradient needs the sums of G over diagonals.  A warp's patch of 32 keys x 64 queries either lies in the
 //     constant part of the bias (one running sum per thread and side) or near the diagonal: there a register per lane
-//     carries one diagonal's sum, moves one lane per column and is complete when it leaves lane 31; the 95 sums are
+//     carries one diagonal's sum, moves one lane per column and is complete when it leaves lane 31, all of it while the
+//     tensor core works on dS; the 95 sums are
 //     reduced by bucket (runs of equal buckets by shuffles) into registers that hold two buckets per lane.  At
-//     the end of an item the eight warps' 64 sums are added in order and stored; zl_bucket_reduce_kernel adds the key tiles in
+//     the end of an item the eight warps' 64 sums are added in order and stored; the dQ conversion's launch adds the key tiles in
 //     order.  No atomics: the same bits every time.
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -36,9 +37,20 @@ namespace {
 // row per thread), warps 12-15 dQ warpgroup (one query row per thread).
 constexpr int kBwdThreads = 512;
 
-constexpr int kWindow = 96;  // distances of a patch of 32 keys x 64 queries: 32 + 64 - 1, rounded up
+constexpr int kPatch = 96;  // distances of a patch of 32 keys x 64 queries: 32 + 64 - 1, rounded up
 
+// Sums over the diagonals of a patch run in kChains stretches of columns side by side: a step of one stretch (a shuffle and an
+// add, some 30 clocks one after the other) waits only for the step before it.  More stretches take more shared memory
+// for their sums, which head_dim 128 does not have.
 template <int D>
+struct DiagSums {
+    static constexpr int kChains = D == 64 ? 4 : 2;
+    static constexpr int kCols = 64 / kChains;        // columns of a stretch
+    static constexpr int kStride = 32 + kCols;        // its 31 + kCols diagonals, and one
+    static constexpr int kFloats = kChains * kStride > kPatch ? kChains * kStride : kPatch;
+};
+
+template <int D, bool kCap>
 struct ScoredBwdSmem {
     static constexpr int kTileBytes = 128 * D * 2;
     static constexpr int kBoxBytes = 128 * 128;
@@ -51,9 +63,9 @@ struct ScoredBwdSmem {
     alignas(1024) uint8_t ds[2 * kBoxBytes];            // dS^T tile: 128 key rows x 128 query columns, bf16
     alignas(1024) uint8_t dq_stage[kDqChunkBytes];      // one fp32 dQ chunk staged for the TMA reduce
     alignas(1024) uint8_t aug[2][4096];                 // per Q stage: bf16 pieces of -LSE/scale and -D
-    alignas(1024) uint8_t ones[3][2048];                // [zeros][ones in elements 0..2][zeros]
-    alignas(16) float lse[2][kTileQ];                   // per Q stage, capped scores: LSE * log2(e)
-    float window[8][kWindow];                           // per P/dS warp: biases, then sums over diagonals
+    alignas(1024) uint8_t ones[kCap ? 2 : 3][2048];     // [zeros][ones in elements 0..2] and, for the step of S^T, [zeros]
+    alignas(16) float lse[kCap ? 2 : 1][kCap ? kTileQ : 4];  // per Q stage, capped scores: LSE * log2(e)
+    float window[8][DiagSums<D>::kFloats];              // per P/dS warp: biases, then sums over diagonals
     alignas(8) uint64_t kv_full, kv_empty;
     uint64_t q_full[2], q_empty[2], do_full, do_empty;
     uint64_t sums_full, sums_empty;
@@ -103,26 +115,38 @@ __device__ __forceinline__ int count_q_tiles(const BwdParams& p, const ScorePara
     return n;
 }
 
-// Adds the sums `v` of 32 consecutive distances (one per lane, bucket `b`, -1 for none) to a table of kMaxBuckets sums in
-// shared memory that only this warp uses.  Runs of equal buckets are summed by shuffles; where a bucket has several
-// runs among the 32 distances their sums are added one after the other, in lane order.
-__device__ __forceinline__ void add_by_bucket(float* sums, float v, int b, int lane) {
-    const int before = __shfl_up_sync(0xffffffffu, b, 1);
-    const uint32_t heads = __ballot_sync(0xffffffffu, lane == 0 || b != before);
-    const uint32_t later = heads & (0xfffffffeu << lane);   // run starts after this lane
-    const int run_end = later ? __ffs(later) - 1 : 32;
+// Adds the sums v[i] of distances 32 i + lane (bucket b[i], -1 for none) to a table of kMaxBuckets sums in shared memory that
+// only this warp uses.  Among 32 consecutive distances runs of equal buckets are summed by shuffles; where a bucket has
+// several runs their sums are added one after the other, in lane order.
+__device__ __forceinline__ void add_by_bucket(float* sums, float (&v)[kPatch / 32], const int (&b)[kPatch / 32], int lane) {
+    bool head[kPatch / 32];
+    int run_end[kPatch / 32];
+#pragma unroll
+    for (int i = 0; i < kPatch / 32; ++i) {
+        const int before = __shfl_up_sync(0xffffffffu, b[i], 1);
+        const uint32_t heads = __ballot_sync(0xffffffffu, lane == 0 || b[i] != before);
+        const uint32_t later = heads & (0xfffffffeu << lane);  // run starts after this lane
+        run_end[i] = later ? __ffs(later) - 1 : 32;
+        head[i] = ((heads >> lane) & 1u) && b[i] >= 0;
+    }
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const float o = __shfl_down_sync(0xffffffffu, v, off);
-        if (lane + off < run_end) v += o;
+        float o[kPatch / 32];
+#pragma unroll
+        for (int i = 0; i < kPatch / 32; ++i) o[i] = __shfl_down_sync(0xffffffffu, v[i], off);
+#pragma unroll
+        for (int i = 0; i < kPatch / 32; ++i)
+            if (lane + off < run_end[i]) v[i] += o[i];
     }
-    const bool head = ((heads >> lane) & 1u) && b >= 0;
-    const uint32_t same = __match_any_sync(0xffffffffu, head ? b : -1 - lane);
-    const int rank = __popc(same & ((1u << lane) - 1u));
-    const int rounds = __reduce_max_sync(0xffffffffu, head ? rank : 0);
-    for (int r = 0; r <= rounds; ++r) {
-        if (head && rank == r) sums[b] += v;
-        __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kPatch / 32; ++i) {
+        const uint32_t same = __match_any_sync(0xffffffffu, head[i] ? b[i] : -1 - lane);
+        const int rank = __popc(same & ((1u << lane) - 1u));
+        const int rounds = __reduce_max_sync(0xffffffffu, head[i] ? rank : 0);
+        for (int r = 0; r <= rounds; ++r) {
+            if (head[i] && rank == r) sums[b[i]] += v[i];
+            __syncwarp();
+        }
     }
 }
 
@@ -133,7 +157,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                    const __grid_constant__ CUtensorMap tm_dq, const __grid_constant__ CUtensorMap tm_dk,
                    const __grid_constant__ CUtensorMap tm_dv, const BwdParams p, const ScoreParams sp) {
     constexpr bool kBias = kKind != kScorePlain, kGrad = kKind == kScoreBiasGrad;
-    using Smem = ScoredBwdSmem<D>;
+    using Smem = ScoredBwdSmem<D, kCap>;
     constexpr int kBoxes = Smem::kBoxes;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
@@ -178,7 +202,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         prefetch_tmap(&tm_dv);
     }
     // constant A operand of the augmentation steps: 128 rows x 8 bf16 per block
-    for (int i = threadIdx.x; i < 3 * 2048 / 4; i += kBwdThreads) {
+    for (int i = threadIdx.x; i < (int)sizeof(sm.ones) / 4; i += kBwdThreads) {
         const int blk = i / 512, w = i % 4;  // w: 32-bit word inside the row's 16 bytes
         uint32_t val = 0;
         if (blk == 1) val = (w == 0) ? 0x3F803F80u : (w == 1 ? 0x00003F80u : 0u);
@@ -387,12 +411,17 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     const bool tile_full = __all_sync(0xffffffffu, col_lo <= 0 && col_hi >= 64);
                     const int dist_lo = tp.kv_pos + wi.row0 + quarter * 32 - (tp.q_pos + qt * kTileQ + col0 + 63);  // first row, last column
                     PatchSide side = kNear;
-                    float near_bias[kWindow / 32];
+                    float near_bias[kPatch / 32];
+                    int near_bucket[kPatch / 32];
                     if constexpr (kBias) {
                         side = patch_side(sp, dist_lo, dist_lo + 31 + 63);
                         if (side == kNear) {
 #pragma unroll
-                            for (int i = 0; i < kWindow / 32; ++i) near_bias[i] = hb.at(sp, wi.head, dist_lo + i * 32 + lane);
+                            for (int i = 0; i < kPatch / 32; ++i) {
+                                const int d = dist_lo + i * 32 + lane;
+                                near_bias[i] = hb.at(sp, wi.head, d);
+                                if constexpr (kGrad) near_bucket[i] = i * 32 + lane < 95 ? bucket_at(sp, d) : -1;
+                            }
                         }
                     }
                     ZL_WAIT_REGS(&sm.s_full, it_cnt & 1, 22);
@@ -408,7 +437,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             if (side == kNear) {
                                 __syncwarp();  // what the window held has been read
 #pragma unroll
-                                for (int i = 0; i < kWindow / 32; ++i) window[i * 32 + lane] = near_bias[i];
+                                for (int i = 0; i < kPatch / 32; ++i) window[i * 32 + lane] = near_bias[i];
                                 __syncwarp();
                             }
                         }
@@ -491,8 +520,6 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         store_pending = false;
                     }
                     tc_fence_after();
-                    float diag = 0.f;   // sum of one diagonal of a near patch, see below
-                    float far = 0.f;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         uint32_t dr[32];
@@ -502,39 +529,14 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         for (int i = 0; i < 32; ++i) {
                             float d = __uint_as_float(dr[i]);
                             if (!tile_full) d = (c * 32 + i < col_lo || c * 32 + i >= col_hi) ? 0.f : d;  // P is zero there; keep 0 * inf out
-                            dr[i] = __float_as_uint(pr[c * 32 + i] * d);  // G
-                        }
-                        if constexpr (kGrad) {
-                            if (side == kNear) {
-                                // lane l, column k: distance index l - k + 63.  `diag` holds the sum of the lane's current
-                                // diagonal; from one column to the next the diagonals move up by one lane, and the one that
-                                // leaves lane 31 is complete.
-                                if (c == 0) __syncwarp();  // the biases have been read: the window takes the sums
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) {
-                                    if (c * 32 + i > 0) {
-                                        const float up = __shfl_sync(0xffffffffu, diag, (lane + 31) & 31);
-                                        if (lane == 0) window[31 + 63 - (c * 32 + i - 1)] = up;
-                                        diag = lane == 0 ? 0.f : up;
-                                    }
-                                    diag += __uint_as_float(dr[i]);
-                                }
-                            } else {
-                                float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-                                for (int i = 0; i < 32; i += 2) {
-                                    s0 += __uint_as_float(dr[i]);
-                                    s1 += __uint_as_float(dr[i + 1]);
-                                }
-                                far += s0 + s1;
-                            }
+                            pr[c * 32 + i] *= d;  // G
                         }
 #pragma unroll
                         for (int k4 = 0; k4 < 4; ++k4) {
                             uint32_t dd[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                float2 ds = make_float2(__uint_as_float(dr[k4 * 8 + 2 * e]), __uint_as_float(dr[k4 * 8 + 2 * e + 1]));
+                                float2 ds = make_float2(pr[c * 32 + k4 * 8 + 2 * e], pr[c * 32 + k4 * 8 + 2 * e + 1]);
                                 if constexpr (kCap)
                                     ds = mul2(ds, __half22float2(*reinterpret_cast<const __half2*>(&slope[c * 16 + k4 * 4 + e])));
                                 dd[e] = pack_bf16(ds.x, ds.y);  // the one rounding between P, dP and the products with Q and K
@@ -547,29 +549,53 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     tc_fence_before();
                     fence_proxy_async_smem();
                     mbar_arrive(&sm.ds_full);
-                    if constexpr (kGrad) {
+                    if constexpr (kGrad) {  // while the tensor core works on dS
                         if (side == kNear) {
-                            window[lane] = diag;  // the 32 diagonals that end in the last column
-                            __syncwarp();
-                            float v[kWindow / 32];
-                            int b[kWindow / 32];
+                            // Lane l, column t of a stretch: diagonal l - t + kCols - 1.  `diag` holds the sum of the lane's
+                            // current diagonal; from one column to the next the diagonals move up by one lane, and the one
+                            // that leaves lane 31 is complete.
+                            using Sums = DiagSums<D>;
+                            float diag[Sums::kChains];
+                            __syncwarp();  // the biases have been read: the window takes the sums
 #pragma unroll
-                            for (int i = 0; i < kWindow / 32; ++i) {
-                                const int at = i * 32 + lane;
-                                v[i] = at < 95 ? window[at] : 0.f;
-                                b[i] = at < 95 ? __ldg(sp.bucket_of + (min(max(dist_lo + at, -sp.reach), sp.reach) + sp.reach)) : -1;
-                                if ((uint32_t)b[i] >= (uint32_t)sp.n_buckets) b[i] = -1;
+                            for (int t = 0; t < Sums::kCols; ++t) {
+#pragma unroll
+                                for (int s = 0; s < Sums::kChains; ++s) {
+                                    if (t == 0) {
+                                        diag[s] = pr[s * Sums::kCols];
+                                    } else {
+                                        const float up = __shfl_sync(0xffffffffu, diag[s], (lane + 31) & 31);
+                                        if (lane == 0) window[s * Sums::kStride + 31 + Sums::kCols - t] = up;
+                                        diag[s] = (lane == 0 ? 0.f : up) + pr[s * Sums::kCols + t];
+                                    }
+                                }
+                            }
+#pragma unroll
+                            for (int s = 0; s < Sums::kChains; ++s) window[s * Sums::kStride + lane] = diag[s];
+                            __syncwarp();
+                            // stretch s holds the distance indexes from 64 - (s + 1) * kCols on
+                            float v[kPatch / 32];
+#pragma unroll
+                            for (int i = 0; i < kPatch / 32; ++i) {
+                                v[i] = 0.f;
+#pragma unroll
+                                for (int s = 0; s < Sums::kChains; ++s) {
+                                    const int at = i * 32 + lane - (64 - (s + 1) * Sums::kCols);
+                                    if (at >= 0 && at < Sums::kStride - 1) v[i] += window[s * Sums::kStride + at];
+                                }
                             }
                             __syncwarp();
                             window[lane] = 0.f;
                             window[lane + 32] = 0.f;
                             __syncwarp();
-#pragma unroll
-                            for (int i = 0; i < kWindow / 32; ++i) add_by_bucket(window, v[i], b[i], lane);
+                            add_by_bucket(window, v, near_bucket, lane);
                             bucket_sum[0] += window[lane];
                             bucket_sum[1] += window[lane + 32];
                         } else {
-                            far_sum[side == kFarPos] += far;
+                            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int c = 0; c < 64; ++c) s[c & 3] += pr[c];
+                            far_sum[side == kFarPos] += (s[0] + s[1]) + (s[2] + s[3]);
                         }
                     }
                 }
@@ -747,21 +773,6 @@ teardown:
     }
 }
 
-// One block per head: four groups of 64 threads, a thread per bucket, walk the key tiles; sums in 64 bits, joined in a
-// fixed order.
-__global__ void __launch_bounds__(4 * kMaxBuckets) zl_bucket_reduce_kernel(const ScoreParams sp, float* d_bucket_bias) {
-    __shared__ double part[4][kMaxBuckets];
-    const int b = threadIdx.x % kMaxBuckets, grp = threadIdx.x / kMaxBuckets, head = blockIdx.x;
-    const float* src = sp.bucket_part + (int64_t)head * sp.n_kv_tiles * kMaxBuckets + b;
-    double v = 0.0;
-#pragma unroll 8
-    for (int t = grp; t < sp.n_kv_tiles; t += 4) v += (double)__ldg(src + (int64_t)t * kMaxBuckets);
-    part[grp][b] = v;
-    __syncthreads();
-    if (grp == 0 && b < sp.n_buckets)
-        d_bucket_bias[(int64_t)b * sp.n_heads + head] = (float)(((part[0][b] + part[1][b]) + part[2][b]) + part[3][b]);
-}
-
 // The opt-in to large dynamic shared memory is a per-device attribute of the kernel.
 constexpr int kMaxDevices = 64;
 
@@ -769,7 +780,7 @@ template <int D, bool kCap, ScoreKind kKind>
 cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tdo,
                      const CUtensorMap& tdq, const CUtensorMap& tdk, const CUtensorMap& tdv, const BwdParams& p,
                      const ScoreParams& sp, int grid, cudaStream_t stream) {
-    constexpr int smem = sizeof(ScoredBwdSmem<D>);
+    constexpr int smem = sizeof(ScoredBwdSmem<D, kCap>);
     static_assert(smem <= 232448, "shared memory of a CTA");
     static bool configured[kMaxDevices] = {};
     int dev = 0;
@@ -807,11 +818,6 @@ cudaError_t launch_scored_bwd(int head_dim, bool capped, ScoreKind kind, const C
                       : launch_k<128, false>(kind, tq, tk, tv, tdo, tdq, tdk, tdv, p, sp, grid, stream);
     return capped ? launch_k<64, true>(kind, tq, tk, tv, tdo, tdq, tdk, tdv, p, sp, grid, stream)
                   : launch_k<64, false>(kind, tq, tk, tv, tdo, tdq, tdk, tdv, p, sp, grid, stream);
-}
-
-cudaError_t launch_bucket_reduce(const ScoreParams& sp, float* d_bucket_bias, cudaStream_t stream) {
-    zl_bucket_reduce_kernel<<<sp.n_heads, 4 * kMaxBuckets, 0, stream>>>(sp, d_bucket_bias);
-    return cudaGetLastError();
 }
 
 }  // namespace zl

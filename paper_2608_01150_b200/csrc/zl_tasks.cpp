@@ -105,6 +105,7 @@ void finish_schedule(Schedule* s) {
         return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
     });
 
+    for (int32_t c : s->task_head_count) s->all_heads = s->all_heads && c == s->n_heads;
     for (const WorkItem& w : s->fwd_items) s->max_item_rows = std::max(s->max_item_rows, w.rows);
 
     // backward work list: (kv group, head of the group's range, key tile); cost = total query rows served
