@@ -158,8 +158,11 @@ def _check(status: int, what: str):
 
 
 def _stream_ptr(stream=None) -> int:
-    import torch
     if stream is None:
+        import torch
+        if torch.cuda.is_initialized():
+            # the current stream's handle without building a Stream object, which costs more than some of the launches
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         if not torch.cuda.is_available():
             return 0
         stream = torch.cuda.current_stream()
