@@ -666,7 +666,9 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         if (launch_bwd_pre(s.head_dim, p, t->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
         g_launches.fetch_add(1);
     }
-    const bool pair = !score && s.head_dim == 128 && (t->bwd_kernel == 2 || (t->bwd_kernel == 0 && kDefaultBwdPair));
+    // Handles over a shared prefix take the scored kernel, which rounds dS once, unless zl_set_bwd_kernel chose another.
+    const bool scored = score || (s.shared_prefix && t->bwd_kernel == 0);
+    const bool pair = !scored && s.head_dim == 128 && (t->bwd_kernel == 2 || (t->bwd_kernel == 0 && kDefaultBwdPair));
     if (p.n_items > 0 && pair) {
         CUtensorMap tq64, tdo64, taug, tdq16, tdk32, tdv32;
         if (!make_tmap_f32_acc(&tdq16, ws + s.ws_dq_acc_off, s.dq_acc_rows, s.n_heads, s.head_dim, 32, 16) ||
@@ -688,12 +690,12 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     } else if (p.n_items > 0) {
         const int grid = std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
         LaunchTimer lt(t, ZL_K_BWD_MAIN, cs);
-        if (score) {
-            const ScoreKind kind = !score->biased ? kScorePlain : (d_bucket_bias ? kScoreBiasGrad : kScoreBias);
+        if (scored) {
+            const ScoreKind kind = !score || !score->biased ? kScorePlain : (d_bucket_bias ? kScoreBiasGrad : kScoreBias);
             // heads that a key tile's tasks leave out have no share
             if (d_bucket_bias && !s.all_heads && cudaMemsetAsync(sp.bucket_part, 0, (size_t)s.n_kv_tiles * s.n_heads * kMaxBuckets * sizeof(float), cs) != cudaSuccess)
                 return ZL_ERR_CUDA;
-            if (launch_scored_bwd(s.head_dim, score->capped, kind, tq, tk, tv, tdo, tdq, tdk, tdv, p, sp, grid, cs) != cudaSuccess)
+            if (launch_scored_bwd(s.head_dim, score && score->capped, kind, tq, tk, tv, tdo, tdq, tdk, tdv, p, sp, grid, cs) != cudaSuccess)
                 return ZL_ERR_CUDA;
         } else if (launch_bwd_main(s.head_dim, tq, tk, tv, tdo, tdq, tdk, tdv, p, grid, cs) != cudaSuccess) return ZL_ERR_CUDA;
         g_launches.fetch_add(1);

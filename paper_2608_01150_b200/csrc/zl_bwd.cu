@@ -70,6 +70,8 @@ __global__ void __launch_bounds__(kPreThreads) zl_bwd_pre_kernel(const BwdParams
     const int64_t n_units = (int64_t)(p.q_pad_total / 8) * p.n_heads;
     const int64_t stride = (int64_t)gridDim.x * (kPreThreads / 32);
     const float inv_scale = 1.f / p.scale;
+    grid_release();
+    grid_wait();
     for (int64_t u0 = (int64_t)blockIdx.x * (kPreThreads / 32) + (threadIdx.x >> 5); u0 < n_units; u0 += kUnits * stride) {
         uint4 a[kUnits][kVec], b[kUnits][kVec];
         float lse[kUnits];
@@ -175,6 +177,8 @@ __device__ __forceinline__ void sum_bucket_parts(const BwdParams& p, int head) {
 
 template <int D>
 __global__ void __launch_bounds__(kPreThreads) zl_bwd_post_kernel(const BwdParams p, const int n_blocks) {
+    grid_release();
+    grid_wait();
     // Blocks from n_blocks on sum the bucket table's gradient, one head each.
     if ((int)blockIdx.x >= n_blocks) {
         sum_bucket_parts(p, (int)blockIdx.x - n_blocks);
@@ -753,9 +757,7 @@ cudaError_t launch_main_t(const CUtensorMap& tq, const CUtensorMap& tk, const CU
 cudaError_t launch_bwd_pre(int head_dim, const BwdParams& p, int n_sms, cudaStream_t stream) {
     if (p.q_pad_total == 0) return cudaSuccess;
     const int grid = n_sms * 2;  // what is resident at once (two units per warp in flight need 92 registers): no block waves
-    if (head_dim == 128) zl_bwd_pre_kernel<128><<<grid, kPreThreads, 0, stream>>>(p);
-    else zl_bwd_pre_kernel<64><<<grid, kPreThreads, 0, stream>>>(p);
-    return cudaGetLastError();
+    return launch_dependent(head_dim == 128 ? zl_bwd_pre_kernel<128> : zl_bwd_pre_kernel<64>, grid, kPreThreads, 0, stream, true, p);
 }
 
 cudaError_t launch_bwd_main(int head_dim, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
@@ -769,9 +771,7 @@ cudaError_t launch_bwd_main(int head_dim, const CUtensorMap& tq, const CUtensorM
 cudaError_t launch_bwd_post(int head_dim, const BwdParams& p, int n_sms, cudaStream_t stream) {
     if (p.dq_rows == 0) return cudaSuccess;
     const int n_blocks = n_sms * 8, grid = n_blocks + (p.d_bucket_bias ? p.n_heads : 0);
-    if (head_dim == 128) zl_bwd_post_kernel<128><<<grid, kPreThreads, 0, stream>>>(p, n_blocks);
-    else zl_bwd_post_kernel<64><<<grid, kPreThreads, 0, stream>>>(p, n_blocks);
-    return cudaGetLastError();
+    return launch_dependent(head_dim == 128 ? zl_bwd_post_kernel<128> : zl_bwd_post_kernel<64>, grid, kPreThreads, 0, stream, true, p, n_blocks);
 }
 
 }  // namespace zl

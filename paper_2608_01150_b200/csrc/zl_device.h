@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <utility>
+
 #include "zl_internal.h"
 
 namespace zl {
@@ -84,6 +86,23 @@ struct ScoreParams {
     int32_t n_kv_tiles;
 };
 enum ScoreKind { kScorePlain = 0, kScoreBias = 1, kScoreBiasGrad = 2 };  // what is added to the (capped) product
+
+// Launches a kernel that calls ptx::grid_wait() before it touches memory that earlier work writes: it may start, and set
+// itself up, while the grid before it in the stream drains (`early` false: an ordinary launch).
+template <class... P, class... A>
+cudaError_t launch_dependent(void (*kernel)(P...), int grid, int threads, int smem, cudaStream_t stream, bool early, A&&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
 
 cudaError_t launch_scored_fwd(int head_dim, bool capped, ScoreKind kind, const CUtensorMap& tq, const CUtensorMap& tk,
                               const CUtensorMap& tv, const CUtensorMap& to, const CUtensorMap& top, const FwdParams& p,

@@ -120,6 +120,8 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem_base;
+    grid_release();
+    grid_wait();
 
     if (warp < 4) {
         reg_dec<72>();
@@ -389,8 +391,7 @@ cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtenso
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < kMaxDevices) configured[dev] = true;
     }
-    zl_few_rows_kernel<D, kRows, kCap, kBias><<<grid, kThreads, smem, stream>>>(tq, tk, tv, q_box_rows, p, sp);
-    return cudaGetLastError();
+    return launch_dependent(zl_few_rows_kernel<D, kRows, kCap, kBias>, grid, kThreads, smem, stream, true, tq, tk, tv, q_box_rows, p, sp);
 }
 
 template <int D, int kRows>

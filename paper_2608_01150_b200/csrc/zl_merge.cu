@@ -102,6 +102,8 @@ __device__ __forceinline__ float merge_one(const MergeParams& p, const MergeGrou
 template <int D, int NP>
 __global__ void __launch_bounds__(kMergeThreads, NP == 8 ? 3 : (NP == 4 ? 4 : 8)) zl_merge_kernel(const MergeParams p) {
     constexpr int V = D / 32;  // floats per lane: 4 (d=128) or 2 (d=64)
+    ptx::grid_release();
+    ptx::grid_wait();
     const int lane = threadIdx.x & 31;
     const int warps_per_block = kMergeThreads / 32;
     const int64_t n_rows = p.row_prefix[p.n_groups];
@@ -159,6 +161,8 @@ template <int D>
 __global__ void __launch_bounds__(128) zl_merge_rows_kernel(const MergeParams p, const int64_t n_rows) {
     constexpr int V = D / 32;
     constexpr int kBatch = 8;
+    ptx::grid_release();
+    ptx::grid_wait();
     const int lane = threadIdx.x & 31;
     const int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (u >= n_rows * p.n_heads) return;
@@ -225,25 +229,16 @@ cudaError_t launch_merge_rows(int head_dim, const MergeParams& p, int64_t n_rows
     if (p.n_groups == 0) return cudaSuccess;
     const int64_t grid = (n_rows * p.n_heads + 3) / 4;
     if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
-    if (head_dim == 128) zl_merge_rows_kernel<128><<<(unsigned)grid, 128, 0, stream>>>(p, n_rows);
-    else zl_merge_rows_kernel<64><<<(unsigned)grid, 128, 0, stream>>>(p, n_rows);
-    return cudaGetLastError();
+    return launch_dependent(head_dim == 128 ? zl_merge_rows_kernel<128> : zl_merge_rows_kernel<64>, (int)grid, 128, 0, stream, true, p, n_rows);
 }
 
 cudaError_t launch_merge(int head_dim, const MergeParams& p, int max_parts, int n_sms, cudaStream_t stream) {
     if (p.n_groups == 0) return cudaSuccess;
     const int grid = n_sms * 8;
     const int np = max_parts <= 4 ? 4 : (max_parts <= 8 ? 8 : 0);
-    if (head_dim == 128) {
-        if (np == 4) zl_merge_kernel<128, 4><<<grid, kMergeThreads, 0, stream>>>(p);
-        else if (np == 8) zl_merge_kernel<128, 8><<<grid, kMergeThreads, 0, stream>>>(p);
-        else zl_merge_kernel<128, 0><<<grid, kMergeThreads, 0, stream>>>(p);
-    } else {
-        if (np == 4) zl_merge_kernel<64, 4><<<grid, kMergeThreads, 0, stream>>>(p);
-        else if (np == 8) zl_merge_kernel<64, 8><<<grid, kMergeThreads, 0, stream>>>(p);
-        else zl_merge_kernel<64, 0><<<grid, kMergeThreads, 0, stream>>>(p);
-    }
-    return cudaGetLastError();
+    void (*kernel)(MergeParams) = head_dim == 128 ? (np == 4 ? zl_merge_kernel<128, 4> : np == 8 ? zl_merge_kernel<128, 8> : zl_merge_kernel<128, 0>)
+                                                  : (np == 4 ? zl_merge_kernel<64, 4> : np == 8 ? zl_merge_kernel<64, 8> : zl_merge_kernel<64, 0>);
+    return launch_dependent(kernel, grid, kMergeThreads, 0, stream, true, p);
 }
 
 // Self-test of the bounded wait: a barrier that never completes must time out, be reported through

@@ -83,6 +83,12 @@ __device__ __forceinline__ bool elect_one() {
     return pred != 0;
 }
 
+// Programmatic dependent launch: a grid launched with launch_dependent() may start while the grid before it in the stream
+// drains; it must not touch memory that others write before grid_wait(), which returns when that grid has completed and its
+// writes are visible (at once, if the launch had no such attribute).  grid_release() lets the next grid start.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ----------------------------------------------------------------------------- fences
 __device__ __forceinline__ void fence_proxy_async_smem() {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

@@ -217,6 +217,7 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem_base;
+    grid_wait();
 
     if (warp < 4) {
         reg_dec<72>();
@@ -791,8 +792,11 @@ cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtenso
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < kMaxDevices) configured[dev] = true;
     }
-    zl_scored_bwd_kernel<D, kCap, kKind><<<grid, kBwdThreads, smem, stream>>>(tq, tk, tv, tdo, tdq, tdk, tdv, p, sp);
-    return cudaGetLastError();
+    // An early start hides the launch where a CTA has an item or two (128-row keys of three short sequences: 17.6 -> 16.8 us for
+    // the whole backward); behind a full-size preprocess pass it gains nothing and costs up to 4 % (capped scores under a
+    // prefix mask, 7 k tokens, 12 heads, d 128: 225 -> 235 us), as does releasing the next launch early from here.
+    return launch_dependent(zl_scored_bwd_kernel<D, kCap, kKind>, grid, kBwdThreads, smem, stream, p.n_items <= 2 * grid,
+                            tq, tk, tv, tdo, tdq, tdk, tdv, p, sp);
 }
 
 template <int D, bool kCap>

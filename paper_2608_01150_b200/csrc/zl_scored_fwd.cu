@@ -130,6 +130,8 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem_base;
+    grid_release();
+    grid_wait();
 
     if (warp < 4) {
         reg_dec<72>();
@@ -476,8 +478,7 @@ cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtenso
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < kMaxDevices) configured[dev] = true;
     }
-    zl_scored_fwd_kernel<D, kCap, kBias><<<grid, kFwdThreads, smem, stream>>>(tq, tk, tv, to, top, p, sp);
-    return cudaGetLastError();
+    return launch_dependent(zl_scored_fwd_kernel<D, kCap, kBias>, grid, kFwdThreads, smem, stream, true, tq, tk, tv, to, top, p, sp);
 }
 
 template <int D>
