@@ -565,9 +565,9 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                                     if (t == 0) {
                                         diag[s] = pr[s * Sums::kCols];
                                     } else {
-                                        const float up = __shfl_sync(0xffffffffu, diag[s], (lane + 31) & 31);
-                                        if (lane == 0) window[s * Sums::kStride + 31 + Sums::kCols - t] = up;
-                                        diag[s] = (lane == 0 ? 0.f : up) + pr[s * Sums::kCols + t];
+                                        if (lane == 31) window[s * Sums::kStride + 31 + Sums::kCols - t] = diag[s];
+                                        const float up = __shfl_up_sync(0xffffffffu, diag[s], 1);
+                                        diag[s] = pr[s * Sums::kCols + t] + (lane == 0 ? 0.f : up);
                                     }
                                 }
                             }
@@ -593,10 +593,13 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             bucket_sum[0] += window[lane];
                             bucket_sum[1] += window[lane + 32];
                         } else {
-                            float s[4] = {0.f, 0.f, 0.f, 0.f};
+                            float2 s[4];
 #pragma unroll
-                            for (int c = 0; c < 64; ++c) s[c & 3] += pr[c];
-                            far_sum[side == kFarPos] += (s[0] + s[1]) + (s[2] + s[3]);
+                            for (int c = 0; c < 4; ++c) s[c] = make_float2(pr[2 * c], pr[2 * c + 1]);
+#pragma unroll
+                            for (int c = 4; c < 32; ++c) s[c & 3] = add2(s[c & 3], make_float2(pr[2 * c], pr[2 * c + 1]));
+                            s[0] = add2(add2(s[0], s[1]), add2(s[2], s[3]));
+                            far_sum[side == kFarPos] += s[0].x + s[0].y;
                         }
                     }
                 }
