@@ -22,6 +22,7 @@ struct zl_tasks {
     uint8_t* d_tables = nullptr;  // one allocation holding every device table
     Task* d_tasks = nullptr;
     WorkItem* d_fwd_items = nullptr;
+    WorkItem* d_fwd_items_few = nullptr;
     WorkItem* d_bwd_items = nullptr;
     WorkItem* d_bwd_pair_items = nullptr;
     int bwd_kernel = 0;           // 0: library default, 1: one CTA per key tile, 2: CTA pairs (head_dim 128)
@@ -184,6 +185,7 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     size_t off = 0;
     const size_t o_tasks = place<Task>(off, s.tasks.size());
     const size_t o_fwd = place<WorkItem>(off, s.fwd_items.size());
+    const size_t o_few = place<WorkItem>(off, s.fwd_items_few.size());
     const size_t o_bwd = place<WorkItem>(off, s.bwd_items.size());
     const size_t o_bwd2 = place<WorkItem>(off, s.bwd_pair_items.size());
     const size_t o_mg = place<MergeGroup>(off, s.merge_groups.size());
@@ -199,6 +201,7 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     auto put = [&](size_t at, const void* src, size_t bytes) { if (bytes) std::memcpy(host.data() + at, src, bytes); };
     put(o_tasks, s.tasks.data(), s.tasks.size() * sizeof(Task));
     put(o_fwd, s.fwd_items.data(), s.fwd_items.size() * sizeof(WorkItem));
+    put(o_few, s.fwd_items_few.data(), s.fwd_items_few.size() * sizeof(WorkItem));
     put(o_bwd, s.bwd_items.data(), s.bwd_items.size() * sizeof(WorkItem));
     put(o_bwd2, s.bwd_pair_items.data(), s.bwd_pair_items.size() * sizeof(WorkItem));
     put(o_mg, s.merge_groups.data(), s.merge_groups.size() * sizeof(MergeGroup));
@@ -217,6 +220,7 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     }
     h->d_tasks = reinterpret_cast<Task*>(h->d_tables + o_tasks);
     h->d_fwd_items = reinterpret_cast<WorkItem*>(h->d_tables + o_fwd);
+    h->d_fwd_items_few = reinterpret_cast<WorkItem*>(h->d_tables + o_few);
     h->d_bwd_items = reinterpret_cast<WorkItem*>(h->d_tables + o_bwd);
     h->d_bwd_pair_items = reinterpret_cast<WorkItem*>(h->d_tables + o_bwd2);
     h->d_merge_groups = reinterpret_cast<MergeGroup*>(h->d_tables + o_mg);
@@ -461,26 +465,33 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     p.o_partial = o_partial;
     p.lse_partial = lse_partial;
     p.status = t->d_status;
-    const int grid = std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
     ScoreParams sp{};
     if (score) {
         sp = score->params;
         sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
-        if (sp.masked && t->sm_margin == 0) {  // dealt out to as many CTAs as there are SMs; another grid takes the plain list
-            p.items = t->d_fwd_items_masked;
-            p.n_items = (int32_t)s.fwd_items_masked.size();
-        }
     }
+    // Items of at most one query tile are bound by their keys' bytes and have a kernel of their own, which also takes the
+    // blocks of longer query ranges where these are too few for the SMs; plain calls on handles without a shared
+    // prefix keep the kernel (and the bits) they always had, and launch phases their lists.
+    bool few = (score || s.shared_prefix) && s.max_item_rows <= kTileQ;
+    if (sp.masked && t->sm_margin == 0) {  // dealt out to as many CTAs as there are SMs; another grid takes the plain lists
+        p.items = t->d_fwd_items_masked;
+        p.n_items = (int32_t)s.fwd_items_masked.size();
+        few = s.fwd_masked_few;
+    } else if ((score || s.shared_prefix) && phase < 0 && !s.fwd_items_few.empty()) {
+        p.items = t->d_fwd_items_few;
+        p.n_items = (int32_t)s.fwd_items_few.size();
+        few = true;
+    }
+    const int grid = std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
     const ScoreKind kind = score && score->biased ? kScoreBias : kScorePlain;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     CUtensorMap tq, tk, tv, to, top;
     if (!make_tmap(&tk, k, s.total_kv, s.n_heads, s.head_dim, kTileKV, in_stride) ||
         !make_tmap(&tv, v, s.total_kv, s.n_heads, s.head_dim, kTileKV, in_stride))
         return ZL_ERR_CUDA;
-    // Items of at most one query tile are bound by their keys' bytes and have a kernel of their own; plain calls on handles
-    // without a shared prefix keep the kernel (and the bits) they always had.
-    if ((score || s.shared_prefix) && s.max_item_rows <= kTileQ) {
-        const int box = (int)align_up((size_t)s.max_item_rows, 16);
+    if (few) {
+        const int box = std::min<int>(kTileQ, (int)align_up((size_t)s.max_item_rows, 16));
         if (!make_tmap(&tq, q, s.total_q, s.n_heads, s.head_dim, box, in_stride)) return ZL_ERR_CUDA;
         LaunchTimer lt(t, ZL_K_FWD, cs);
         if (launch_few_rows(s.head_dim, score && score->capped, kind, tq, tk, tv, box, p, sp, grid, cs) != cudaSuccess) return ZL_ERR_CUDA;

@@ -114,6 +114,10 @@ struct Schedule {
     // each item (an item without rows ends a CTA's list).
     std::vector<TaskPos> task_pos;
     std::vector<WorkItem> fwd_items_masked, bwd_items_masked;
+    // Blocks of one query tile for the few-rows kernel, where they finish sooner than blocks of two (empty: they do not);
+    // fwd_masked_few says the same of fwd_items_masked.
+    std::vector<WorkItem> fwd_items_few;
+    bool fwd_masked_few = false;
     std::vector<KvGroup> kv_groups;
     std::vector<int32_t> kv_group_tasks;
     std::vector<WorkItem> fwd_items;

@@ -63,12 +63,14 @@ bool ranges_consistent(const std::vector<Range>& rng, const std::vector<HeadRang
     return true;
 }
 
+constexpr int32_t kSms = 148;  // of a B200
+
 // Keys of a shared prefix per chunk, a whole number of key tiles.  `blocks` (head, row block) items per chunk run on the SMs
 // of a B200 in rounds; an item costs its key tiles and about two more to begin and to end (Q, the first S, the join, the
 // partial output).  Of the numbers of chunks with the least total, the smallest; a chunk has 512 keys at least, because a
 // partial row costs as much traffic as two key rows.
 int64_t prefix_chunk(int64_t blocks, int64_t prefix_len) {
-    constexpr int64_t kSms = 148, kItemTiles = 2, kMinKeys = 512, kMaxChunks = 256;
+    constexpr int64_t kItemTiles = 2, kMinKeys = 512, kMaxChunks = 256;
     const int64_t most = std::min<int64_t>(kMaxChunks, std::max<int64_t>(1, prefix_len / kMinKeys));
     int64_t best = 0, best_cost = INT64_MAX;
     for (int64_t n = 1; n <= most; ++n) {
@@ -84,6 +86,72 @@ constexpr int64_t kMaxPos = INT32_MAX - 4 * 128;
 
 using GroupKey = std::tuple<int64_t, int64_t, int32_t, int32_t>;  // range offset, length, head range
 
+// Query tiles of a forward item cost about this many key-tile steps to begin and to end (descriptors, Q, the first S, the output).
+constexpr int64_t kItemSteps = 2;
+
+// Blocks of `block` query rows of every (task, head), in the order of the tasks.
+std::vector<WorkItem> forward_blocks(const Schedule& s, int32_t block) {
+    std::vector<WorkItem> items;
+    for (size_t ti = 0; ti < s.tasks.size(); ++ti) {
+        const Task& t = s.tasks[ti];
+        for (int32_t h = s.task_head_begin[ti]; h < s.task_head_begin[ti] + s.task_head_count[ti]; ++h)
+            for (int32_t r = 0; r < t.q_len; r += block)
+                items.push_back({(int32_t)ti, h, r, std::min(block, t.q_len - r)});
+    }
+    return items;
+}
+
+// Steps an item takes: blocks of two query tiles take a key tile per step, the few-rows kernel takes two key tiles for
+// its one query tile.  `masked`: only the visible keys.
+int64_t item_steps(const Schedule& s, const WorkItem& w, bool few, bool masked) {
+    const Task& t = s.tasks[w.unit];
+    const int32_t keys = masked ? visible_keys(s.task_pos[w.unit], t.kv_len, w.row0 + w.rows - 1) : t.kv_len;
+    const int64_t tiles = (keys + kTileKV - 1) / kTileKV;
+    return (few ? (tiles + 1) / 2 : tiles) + kItemSteps;
+}
+
+// Whether blocks of one query tile (`few` steps) beat blocks of two: a step of theirs loads twice the keys.
+bool few_rows_pay(int64_t few, int64_t two) { return few * 10 < two * 9; }
+
+// Most steps of a CTA that takes items i, i + ctas, ...
+int64_t makespan(const std::vector<int64_t>& steps, size_t ctas) {
+    std::vector<int64_t> load(std::max<size_t>(1, std::min(ctas, steps.size())), 0);
+    for (size_t i = 0; i < steps.size(); ++i) load[i % load.size()] += steps[i];
+    return *std::max_element(load.begin(), load.end());
+}
+
+// Deals items out to CTAs.  A CTA of the persistent kernels walks items i, i + grid, i + 2 grid, ...; under a mask their work
+// differs from a tile to the whole row, and round robin would give the first CTA the longest item of every round.  So the
+// items, longest first, go to the CTA with the least work so far, and an item without rows ends a list before the
+// longest one.  Returns the most steps of a CTA.
+int64_t deal(std::vector<WorkItem>* items, const std::vector<int64_t>& steps, int32_t n_sms) {
+    std::vector<int32_t> order(items->size());
+    for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
+    std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return steps[a] > steps[b]; });
+    const int32_t ctas = (int32_t)std::min<size_t>(n_sms, items->size());
+    using Load = std::pair<int64_t, int32_t>;
+    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+    for (int32_t c = 0; c < ctas; ++c) least.push({0, c});
+    std::vector<std::vector<int32_t>> lists(ctas);
+    size_t longest = 0;
+    int64_t most = 0;
+    for (int32_t i : order) {
+        const Load l = least.top();
+        least.pop();
+        lists[l.second].push_back(i);
+        longest = std::max(longest, lists[l.second].size());
+        most = std::max(most, l.first + steps[i]);
+        least.push({l.first + steps[i], l.second});
+    }
+    std::vector<WorkItem> dealt;
+    dealt.reserve(longest * ctas);
+    for (size_t r = 0; r < longest; ++r)
+        for (int32_t c = 0; c < ctas; ++c)
+            dealt.push_back(r < lists[c].size() ? (*items)[lists[c][r]] : WorkItem{0, 0, 0, 0});
+    items->swap(dealt);
+    return most;
+}
+
 // Work lists, launch phases and workspace layout from the tasks, query groups and kv groups.
 void finish_schedule(Schedule* s) {
     for (KvGroup& g : s->kv_groups) {
@@ -92,21 +160,26 @@ void finish_schedule(Schedule* s) {
     }
 
     // forward work list: (task, head of the task's range, query block), longest-first
-    for (size_t ti = 0; ti < s->tasks.size(); ++ti) {
-        const Task& t = s->tasks[ti];
-        for (int32_t h = s->task_head_begin[ti]; h < s->task_head_begin[ti] + s->task_head_count[ti]; ++h)
-            for (int32_t r = 0; r < t.q_len; r += kFwdBlockQ)
-                s->fwd_items.push_back({(int32_t)ti, h, r, std::min(kFwdBlockQ, t.q_len - r)});
-    }
-    std::stable_sort(s->fwd_items.begin(), s->fwd_items.end(), [&](const WorkItem& a, const WorkItem& b) {
+    auto longest_first = [&](const WorkItem& a, const WorkItem& b) {
         const int32_t ka = s->tasks[a.unit].kv_len, kb = s->tasks[b.unit].kv_len;
         if (ka != kb) return ka > kb;
         if (a.rows != b.rows) return a.rows > b.rows;
         return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
-    });
-
+    };
+    s->fwd_items = forward_blocks(*s, kFwdBlockQ);
+    std::stable_sort(s->fwd_items.begin(), s->fwd_items.end(), longest_first);
     for (int32_t c : s->task_head_count) s->all_heads = s->all_heads && c == s->n_heads;
     for (const WorkItem& w : s->fwd_items) s->max_item_rows = std::max(s->max_item_rows, w.rows);
+    if (s->max_item_rows > kTileQ) {
+        s->fwd_items_few = forward_blocks(*s, kTileQ);
+        std::stable_sort(s->fwd_items_few.begin(), s->fwd_items_few.end(), longest_first);
+        auto span = [&](const std::vector<WorkItem>& items, bool few) {
+            std::vector<int64_t> steps;
+            for (const WorkItem& w : items) steps.push_back(item_steps(*s, w, few, false));
+            return makespan(steps, kSms);
+        };
+        if (!few_rows_pay(span(s->fwd_items_few, true), span(s->fwd_items, false))) s->fwd_items_few.clear();
+    }
 
     // backward work list: (kv group, head of the group's range, key tile); cost = total query rows served
     std::vector<int64_t> group_cost(s->kv_groups.size(), 0);
@@ -474,48 +547,27 @@ zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard
     }
     s->task_pos = std::move(pos);
 
-    // The same items, dealt out by what the mask leaves of them.  A CTA of the persistent kernels walks items i, i + grid,
-    // i + 2 grid, ...; under a mask their work differs from a tile to the whole row, and round robin would give the first
-    // CTA the longest item of every round.  So the items, longest first, go to the CTA with the least work so far
-    // (an item costs its tiles and about one more to begin and end); an item without rows ends a list before the longest one.
-    auto by_work = [n_sms](std::vector<WorkItem>* items, const std::vector<int64_t>& work) {
-        std::vector<int32_t> order(items->size());
-        for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
-        std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return work[a] > work[b]; });
-        const int32_t ctas = (int32_t)std::min<size_t>(n_sms, items->size());
-        using Load = std::pair<int64_t, int32_t>;
-        std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
-        for (int32_t c = 0; c < ctas; ++c) least.push({0, c});
-        std::vector<std::vector<int32_t>> lists(ctas);
-        size_t longest = 0;
-        for (int32_t i : order) {
-            const Load l = least.top();
-            least.pop();
-            lists[l.second].push_back(i);
-            longest = std::max(longest, lists[l.second].size());
-            least.push({l.first + work[i] + 1, l.second});
-        }
-        std::vector<WorkItem> dealt;
-        for (size_t r = 0; r < longest; ++r)
-            for (int32_t c = 0; c < ctas; ++c)
-                dealt.push_back(r < lists[c].size() ? (*items)[lists[c][r]] : WorkItem{0, 0, 0, 0});
-        items->swap(dealt);
+    auto steps_of = [&](const std::vector<WorkItem>& items, bool few) {
+        std::vector<int64_t> steps;
+        for (const WorkItem& w : items) steps.push_back(item_steps(*s, w, few, true));
+        return steps;
     };
+    s->fwd_masked_few = s->max_item_rows <= kTileQ;
     s->fwd_items_masked = s->fwd_items;
-    std::vector<int64_t> work;
-    for (const WorkItem& w : s->fwd_items_masked) {
-        const Task& t = s->tasks[w.unit];
-        int64_t tiles = 0;
-        for (int32_t r = 0; r < w.rows; r += kTileQ)
-            tiles += (visible_keys(s->task_pos[w.unit], t.kv_len, w.row0 + std::min(w.rows, r + kTileQ) - 1) + kTileKV - 1) / kTileKV;
-        work.push_back(tiles);
+    const int64_t two = deal(&s->fwd_items_masked, steps_of(s->fwd_items, s->fwd_masked_few), n_sms);
+    if (!s->fwd_masked_few) {
+        std::vector<WorkItem> blocks = forward_blocks(*s, kTileQ);
+        const std::vector<int64_t> steps = steps_of(blocks, true);
+        if (few_rows_pay(deal(&blocks, steps, n_sms), two)) {
+            s->fwd_items_masked.swap(blocks);
+            s->fwd_masked_few = true;
+        }
     }
-    by_work(&s->fwd_items_masked, work);
     s->bwd_items_masked = s->bwd_items;
-    work.clear();
+    std::vector<int64_t> work;
     for (const WorkItem& w : s->bwd_items_masked) {
         const KvGroup& g = s->kv_groups[w.unit];
-        int64_t tiles = 0;
+        int64_t tiles = kItemSteps;
         for (int32_t j = 0; j < g.n_tasks; ++j) {
             const int32_t ti = s->kv_group_tasks[g.task_begin + j];
             const int32_t n = (s->tasks[ti].q_len + kTileQ - 1) / kTileQ;
@@ -523,7 +575,7 @@ zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard
         }
         work.push_back(tiles);
     }
-    by_work(&s->bwd_items_masked, work);
+    deal(&s->bwd_items_masked, work, n_sms);
     return ZL_OK;
 }
 
