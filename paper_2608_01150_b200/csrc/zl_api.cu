@@ -34,6 +34,7 @@ struct zl_tasks {
     KvGroup* d_kv_groups = nullptr;
     int32_t* d_kv_group_tasks = nullptr;
     int32_t* d_status = nullptr;
+    int32_t* d_part_count = nullptr;
     uint8_t* d_positions = nullptr;  // zl_set_positions: one allocation for the three tables below
     size_t positions_bytes = 0;
     TaskPos* d_task_pos = nullptr;
@@ -195,6 +196,7 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     const size_t o_kg = place<KvGroup>(off, s.kv_groups.size());
     const size_t o_kt = place<int32_t>(off, s.kv_group_tasks.size());
     const size_t o_st = place<int32_t>(off, 2);
+    const size_t o_pc = place<int32_t>(off, s.max_item_rows <= kTileQ && s.partial_rows > 0 ? s.tasks.size() * s.n_heads : 0);
     const size_t total = align_up(off, 256);
 
     std::vector<uint8_t> host(total, 0);
@@ -230,6 +232,7 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     h->d_kv_groups = reinterpret_cast<KvGroup*>(h->d_tables + o_kg);
     h->d_kv_group_tasks = reinterpret_cast<int32_t*>(h->d_tables + o_kt);
     h->d_status = reinterpret_cast<int32_t*>(h->d_tables + o_st);
+    h->d_part_count = reinterpret_cast<int32_t*>(h->d_tables + o_pc);
     *out = h;
     return ZL_OK;
 }
@@ -465,6 +468,7 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     p.o_partial = o_partial;
     p.lse_partial = lse_partial;
     p.status = t->d_status;
+    p.part_count = t->d_part_count;
     ScoreParams sp{};
     if (score) {
         sp = score->params;

@@ -24,6 +24,7 @@ struct FwdParams {
     float* o_partial;
     float* lse_partial;
     int32_t* status;  // [0] = code, [1] = where
+    int32_t* part_count;  // [tasks, H] finished pieces of an item cut along the keys; zero between launches
 };
 
 struct MergeParams {

@@ -42,9 +42,24 @@ struct FewSmem {
     uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
     uint64_t bias_full[2], bias_empty[2];
     uint64_t s_full[2], p_half[2][2], o_full[2];
-    uint64_t stat_full, join_done;  // between the warpgroups at the end of an item
+    uint64_t stat_full, join_done, part_bar;  // between the warpgroups at the end of an item
+    int32_t ticket;
     uint32_t tmem_base;
     volatile int32_t abort_flag;
+};
+
+// An item as the roles walk it: `rows` query rows from row0 of the task over key tiles [tile0, tile0 + n_kv), piece `part` of `parts`.
+struct FewItem {
+    int row0, rows, part, parts, tile0, n_kv;
+    __device__ __forceinline__ FewItem(const WorkItem& wi, const ScoreParams& sp, const Task& t) {
+        parts = wi.rows >> kPartsShift;
+        rows = wi.rows & ((1 << kPartsShift) - 1);
+        part = parts > 1 ? wi.row0 : 0;
+        row0 = parts > 1 ? 0 : wi.row0;
+        const int tiles = key_tiles(sp, t, wi.unit, row0, rows);
+        tile0 = parts > 1 ? tiles * part / parts : 0;
+        n_kv = (parts > 1 ? tiles * (part + 1) / parts : tiles) - tile0;
+    }
 };
 
 #define ZL_WAIT(bar, parity, site)                                        \
@@ -106,6 +121,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         for (int s = 0; s < kStagesV; ++s) { mbar_init(&sm.v_full[s], 1); mbar_init(&sm.v_empty[s], 1); }
         mbar_init(&sm.stat_full, 256);
         mbar_init(&sm.join_done, 256);
+        mbar_init(&sm.part_bar, 256);
         sm.abort_flag = 0;
         fence_mbar_init();
         prefetch_tmap(&tm_q);
@@ -132,28 +148,29 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 const WorkItem wi = p.items[it];
                 if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
-                const int n_kv = key_tiles(sp, t, wi.unit, wi.row0, wi.rows);
+                const FewItem fi(wi, sp, t);
+                const int n_kv = fi.n_kv;
                 if (n_kv == 0) continue;
                 const int qb = item_cnt & 1;
                 ZL_WAIT(&sm.q_empty[qb], ((item_cnt >> 1) & 1) ^ 1, 1);
                 ++item_cnt;
                 mbar_arrive_expect_tx(&sm.q_full[qb], q_box_rows * D * 2);
                 for (int b = 0; b < kBoxes; ++b)
-                    tma_load_3d(sm.q[qb] + b * Smem::kQBoxBytes, &tm_q, &sm.q_full[qb], b * 64, wi.head, t.q_off + wi.row0);
+                    tma_load_3d(sm.q[qb] + b * Smem::kQBoxBytes, &tm_q, &sm.q_full[qb], b * 64, wi.head, t.q_off + fi.row0);
                 for (int j = 0; j <= n_kv; ++j) {  // K runs one tile ahead of V: its slots free up first
                     if (j < n_kv) {
                         const uint32_t c = kv_cnt + j, ks = c % kStagesK;
                         ZL_WAIT(&sm.k_empty[ks], ((c / kStagesK) & 1) ^ 1, 2);
                         mbar_arrive_expect_tx(&sm.k_full[ks], Smem::kTileBytes);
                         for (int b = 0; b < kBoxes; ++b)
-                            tma_load_3d(sm.k[ks] + b * Smem::kBoxBytes, &tm_k, &sm.k_full[ks], b * 64, wi.head, t.kv_off + j * kTileKV);
+                            tma_load_3d(sm.k[ks] + b * Smem::kBoxBytes, &tm_k, &sm.k_full[ks], b * 64, wi.head, t.kv_off + (fi.tile0 + j) * kTileKV);
                     }
                     if (j > 0) {
                         const uint32_t c = kv_cnt + j - 1, vs = c % kStagesV;
                         ZL_WAIT(&sm.v_empty[vs], ((c / kStagesV) & 1) ^ 1, 3);
                         mbar_arrive_expect_tx(&sm.v_full[vs], Smem::kTileBytes);
                         for (int b = 0; b < kBoxes; ++b)
-                            tma_load_3d(sm.v[vs] + b * Smem::kBoxBytes, &tm_v, &sm.v_full[vs], b * 64, wi.head, t.kv_off + (j - 1) * kTileKV);
+                            tma_load_3d(sm.v[vs] + b * Smem::kBoxBytes, &tm_v, &sm.v_full[vs], b * 64, wi.head, t.kv_off + (fi.tile0 + j - 1) * kTileKV);
                     }
                 }
                 kv_cnt += n_kv;
@@ -172,7 +189,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 const WorkItem wi = p.items[it];
                 if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
-                const int n_kv = key_tiles(sp, t, wi.unit, wi.row0, wi.rows);
+                const int n_kv = FewItem(wi, sp, t).n_kv;
                 if (n_kv == 0) continue;
                 const uint32_t qb = item_cnt & 1;
                 ZL_WAIT_WARP(&sm.q_full[qb], (item_cnt >> 1) & 1, 11);
@@ -225,11 +242,11 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const TaskPos tp = task_pos(sp, wi.unit);
-                const int n_kv = key_tiles(sp, t, wi.unit, wi.row0, wi.rows);
+                const FewItem fi(wi, sp, t);
                 HeadBias hb;
                 hb.load(sp, wi.head);
-                for (int j = x; j < n_kv; j += 2) {
-                    const int lo = tp.kv_pos + j * kTileKV - (tp.q_pos + wi.row0 + kTileQ - 1);
+                for (int j = x; j < fi.n_kv; j += 2) {
+                    const int lo = tp.kv_pos + (fi.tile0 + j) * kTileKV - (tp.q_pos + fi.row0 + kTileQ - 1);
                     if (patch_side(sp, lo, lo + kTileQ + kTileKV - 2) != kNear) continue;
                     if (!feed.put(sp, hb, wi.head, lo, lane, &sm.abort_flag)) {
                         report(p.status, &sm.abort_flag, 5000 + 31);
@@ -253,15 +270,16 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (wi.rows == 0) break;  // end of this CTA's list
             const Task t = p.tasks[wi.unit];
             const TaskPos tp = task_pos(sp, wi.unit);
-            const int n_kv = key_tiles(sp, t, wi.unit, wi.row0, wi.rows);
-            const int keys = sp.masked ? visible_keys(tp, t.kv_len, wi.row0 + row) : t.kv_len;  // this row's
-            const bool busy = quarter * 32 < wi.rows;  // warp-uniform: the warp has a valid row
-            const bool row_ok = row < wi.rows;
+            const FewItem fi(wi, sp, t);
+            const int n_kv = fi.n_kv;
+            const int keys = (sp.masked ? visible_keys(tp, t.kv_len, fi.row0 + row) : t.kv_len) - fi.tile0 * kTileKV;  // this row's, from the piece on
+            const bool busy = quarter * 32 < fi.rows;  // warp-uniform: the warp has a valid row
+            const bool row_ok = row < fi.rows;
             HeadBias hb;
             if constexpr (kBias) hb.load(sp, wi.head);
             float m_ref = -INFINITY, l = 0.f;
             for (int j = x; j < n_kv; j += 2) {
-                const int dist_lo = tp.kv_pos + j * kTileKV - (tp.q_pos + wi.row0 + kTileQ - 1);  // last row, first column
+                const int dist_lo = tp.kv_pos + (fi.tile0 + j) * kTileKV - (tp.q_pos + fi.row0 + kTileQ - 1);  // last row, first column
                 const PatchSide side = kBias ? patch_side(sp, dist_lo, dist_lo + kTileQ + kTileKV - 2) : kNear;
                 const bool ragged = __any_sync(0xffffffffu, keys - j * kTileKV < kTileKV);
                 ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
@@ -317,7 +335,7 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 }
             }
             if (busy) {
-                const int64_t grow = (int64_t)(t.partial_slot >= 0 ? t.partial_slot : t.q_off) + wi.row0 + row;
+                const int64_t grow = (int64_t)(t.partial_slot >= 0 ? t.partial_slot + fi.part * fi.rows : t.q_off) + fi.row0 + row;
                 const int c0 = x * (D / 2);
 #pragma unroll 1
                 for (int c = 0; c < D / 64; ++c) {
@@ -362,6 +380,63 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 mbar_arrive(&sm.join_done);
                 ZL_WAIT_REGS(&sm.join_done, join_cnt & 1, 28);
                 ++join_cnt;
+            }
+            // (the item is read again rather than kept: registers are short in the loop over tiles)
+            const int4 again = __ldcg(reinterpret_cast<const int4*>(p.items + it));
+            const int parts = again.w >> kPartsShift;
+            if (parts > 1) {
+                const int unit = again.x, head = again.y, rows = again.w & ((1 << kPartsShift) - 1);
+                const int slot = __ldcg(&p.tasks[unit].partial_slot);
+                // ---- the piece that finishes last joins all of them, in order (an even number of barrier phases either way): O = sum_s 2^(LSE_s - max) O_s / sum_s 2^(LSE_s - max)
+                __threadfence();
+                mbar_arrive(&sm.part_bar);
+                ZL_WAIT_REGS(&sm.part_bar, 0, 29);  // this piece's rows are written and visible
+                int32_t* count = p.part_count + (int64_t)unit * p.n_heads + head;
+                const int tid = threadIdx.x - 128;  // 0 .. 255
+                if (tid == 0) sm.ticket = atomicAdd(count, 1);
+                mbar_arrive(&sm.part_bar);
+                ZL_WAIT_REGS(&sm.part_bar, 1, 30);
+                if (sm.ticket == parts - 1) {
+                    __threadfence();
+                    // all LSEs at once (they are contiguous in the slot), then four partial rows in flight per thread
+                    const int n_lse = parts * rows;  // at most 128
+                    float* lse_s = reinterpret_cast<float*>(&sm.stat[0][0]);
+                    float* lse_p = p.lse_partial + (int64_t)head * p.partial_rows + slot;
+                    if (tid < n_lse) lse_s[tid] = __ldcg(lse_p + tid);
+                    mbar_arrive(&sm.part_bar);
+                    ZL_WAIT_REGS(&sm.part_bar, 0, 31);
+                    float4* o_p = reinterpret_cast<float4*>(p.o_partial + ((int64_t)slot * p.n_heads + head) * D);
+                    const int64_t row4 = (int64_t)p.n_heads * D / 4;
+#pragma unroll 1
+                    for (int i = tid; i < rows * (D / 4); i += 256) {
+                        const int r = i / (D / 4), c4 = i % (D / 4);
+                        float m = -INFINITY, z = 0.f;
+#pragma unroll 4
+                        for (int s = r; s < n_lse; s += rows) m = fmaxf(m, lse_s[s]);
+                        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+                        for (int s0 = r; s0 < n_lse; s0 += 4 * rows) {
+                            float4 o_s[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (s0 + e * rows < n_lse) o_s[e] = __ldcg(o_p + (s0 + e * rows) * row4 + c4);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (s0 + e * rows < n_lse) {
+                                    const float w_s = m > -INFINITY ? ex2((lse_s[s0 + e * rows] - m) * kLog2e) : 0.f;
+                                    z += w_s;
+                                    acc.x = fmaf(w_s, o_s[e].x, acc.x); acc.y = fmaf(w_s, o_s[e].y, acc.y);
+                                    acc.z = fmaf(w_s, o_s[e].z, acc.z); acc.w = fmaf(w_s, o_s[e].w, acc.w);
+                                }
+                        }
+                        const float inv_z = z > 0.f ? 1.f / z : 0.f;
+                        o_p[r * row4 + c4] = make_float4(acc.x * inv_z, acc.y * inv_z, acc.z * inv_z, acc.w * inv_z);
+                        if (c4 == 0) lse_p[r] = m > -INFINITY ? m + logf(z) : -INFINITY;
+                    }
+                    if (tid == 0) *count = 0;  // for the next launch
+                    mbar_arrive(&sm.part_bar);
+                    ZL_WAIT_REGS(&sm.part_bar, 1, 32);  // the statistics' place is free again
+                }
             }
         }
     }

@@ -55,6 +55,11 @@ struct alignas(16) WorkItem {
     int32_t unit, head, row0, rows;
 };
 
+// Few query rows against long keys: the few-rows kernel takes an item in `parts` pieces along the keys.  Such an item has
+// row0 = the piece and rows = parts << kPartsShift | rows.  Piece s leaves its partial result in rows s * q_len .. of the
+// task's slot, which is padded to 128 rows; the piece that finishes last joins them into the first q_len.
+constexpr int kPartsShift = 16;
+
 // Shard tasks that share a query range and a head range; they are merged for heads
 // [head_begin, head_begin + head_count) only.
 struct alignas(32) MergeGroup {
@@ -114,8 +119,8 @@ struct Schedule {
     // each item (an item without rows ends a CTA's list).
     std::vector<TaskPos> task_pos;
     std::vector<WorkItem> fwd_items_masked, bwd_items_masked;
-    // Blocks of one query tile for the few-rows kernel, where they finish sooner than blocks of two (empty: they do not);
-    // fwd_masked_few says the same of fwd_items_masked.
+    // Blocks of one query tile for the few-rows kernel, where they finish sooner than blocks of two, or items of few rows in
+    // pieces along the keys (empty: neither); fwd_masked_few says that fwd_items_masked is such a list.
     std::vector<WorkItem> fwd_items_few;
     bool fwd_masked_few = false;
     std::vector<KvGroup> kv_groups;

@@ -105,13 +105,35 @@ std::vector<WorkItem> forward_blocks(const Schedule& s, int32_t block) {
 // its one query tile.  `masked`: only the visible keys.
 int64_t item_steps(const Schedule& s, const WorkItem& w, bool few, bool masked) {
     const Task& t = s.tasks[w.unit];
-    const int32_t keys = masked ? visible_keys(s.task_pos[w.unit], t.kv_len, w.row0 + w.rows - 1) : t.kv_len;
-    const int64_t tiles = (keys + kTileKV - 1) / kTileKV;
+    const int32_t parts = w.rows >> kPartsShift, rows = w.rows & ((1 << kPartsShift) - 1), row0 = parts > 1 ? 0 : w.row0;
+    const int32_t keys = masked ? visible_keys(s.task_pos[w.unit], t.kv_len, row0 + rows - 1) : t.kv_len;
+    int64_t tiles = (keys + kTileKV - 1) / kTileKV;
+    if (parts > 1) tiles = (tiles + parts - 1) / parts + 2;  // the join costs about a step
     return (few ? (tiles + 1) / 2 : tiles) + kItemSteps;
+}
+
+// `items` (of one row block each) in up to `parts` pieces along the keys, as many as their slots have room for.
+std::vector<WorkItem> in_pieces(const Schedule& s, const std::vector<WorkItem>& items, int32_t parts) {
+    std::vector<WorkItem> out;
+    for (const WorkItem& w : items) {
+        const Task& t = s.tasks[w.unit];
+        const int32_t n = t.partial_slot < 0 ? 1 : std::min(parts, kTileQ / t.q_len);
+        if (n < 2) { out.push_back(w); continue; }
+        for (int32_t i = 0; i < n; ++i) out.push_back({w.unit, w.head, i, w.rows | (n << kPartsShift)});
+    }
+    return out;
 }
 
 // Whether blocks of one query tile (`few` steps) beat blocks of two: a step of theirs loads twice the keys.
 bool few_rows_pay(int64_t few, int64_t two) { return few * 10 < two * 9; }
+
+// Numbers of pieces worth trying: a piece has two key tiles at least.
+constexpr int32_t kPieces[] = {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+bool worth_trying(const Schedule& s, int32_t parts) {
+    int32_t longest = 0;
+    for (const Task& t : s.tasks) longest = std::max(longest, t.kv_len);
+    return parts * s.max_item_rows <= kTileQ && parts * 2 * kTileKV <= longest + 2 * kTileKV;
+}
 
 // Most steps of a CTA that takes items i, i + ctas, ...
 int64_t makespan(const std::vector<int64_t>& steps, size_t ctas) {
@@ -170,15 +192,23 @@ void finish_schedule(Schedule* s) {
     std::stable_sort(s->fwd_items.begin(), s->fwd_items.end(), longest_first);
     for (int32_t c : s->task_head_count) s->all_heads = s->all_heads && c == s->n_heads;
     for (const WorkItem& w : s->fwd_items) s->max_item_rows = std::max(s->max_item_rows, w.rows);
+    auto span = [&](const std::vector<WorkItem>& items, bool few) {
+        std::vector<int64_t> steps;
+        for (const WorkItem& w : items) steps.push_back(item_steps(*s, w, few, false));
+        return makespan(steps, kSms);
+    };
     if (s->max_item_rows > kTileQ) {
         s->fwd_items_few = forward_blocks(*s, kTileQ);
         std::stable_sort(s->fwd_items_few.begin(), s->fwd_items_few.end(), longest_first);
-        auto span = [&](const std::vector<WorkItem>& items, bool few) {
-            std::vector<int64_t> steps;
-            for (const WorkItem& w : items) steps.push_back(item_steps(*s, w, few, false));
-            return makespan(steps, kSms);
-        };
         if (!few_rows_pay(span(s->fwd_items_few, true), span(s->fwd_items, false))) s->fwd_items_few.clear();
+    } else if (!s->shared_prefix) {
+        int64_t best = span(s->fwd_items, true);
+        for (int32_t parts : kPieces) {
+            if (!worth_trying(*s, parts)) break;
+            std::vector<WorkItem> items = in_pieces(*s, s->fwd_items, parts);
+            const int64_t steps = span(items, true);
+            if (steps < best) { best = steps; s->fwd_items_few.swap(items); }
+        }
     }
 
     // backward work list: (kv group, head of the group's range, key tile); cost = total query rows served
@@ -555,7 +585,16 @@ zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard
     s->fwd_masked_few = s->max_item_rows <= kTileQ;
     s->fwd_items_masked = s->fwd_items;
     const int64_t two = deal(&s->fwd_items_masked, steps_of(s->fwd_items, s->fwd_masked_few), n_sms);
-    if (!s->fwd_masked_few) {
+    if (s->fwd_masked_few && !s->shared_prefix) {
+        int64_t best = two;
+        for (int32_t parts : kPieces) {
+            if (!worth_trying(*s, parts)) break;
+            std::vector<WorkItem> items = in_pieces(*s, s->fwd_items, parts);
+            const std::vector<int64_t> steps = steps_of(items, true);
+            const int64_t most = deal(&items, steps, n_sms);
+            if (most < best) { best = most; s->fwd_items_masked.swap(items); }
+        }
+    } else if (!s->fwd_masked_few) {
         std::vector<WorkItem> blocks = forward_blocks(*s, kTileQ);
         const std::vector<int64_t> steps = steps_of(blocks, true);
         if (few_rows_pay(deal(&blocks, steps, n_sms), two)) {

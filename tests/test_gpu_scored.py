@@ -284,6 +284,68 @@ def test_single_tokens_against_chunks_at_far_positions(rows):
     check_all(Run(h, s, q, k, v, d ** -0.5), problems, s, q, k, v, d_o, d ** -0.5)
 
 
+@pytest.mark.parametrize("rows,chunk,H,masked", [(1, 5000, 2, True), (1, 5000, 2, False), (17, 2100, 3, True), (64, 1300, 1, False)])
+def test_long_chunks_cut_along_the_keys(rows, chunk, H, masked):
+    """Few rows against chunks so long that the kernel takes them in pieces: each shard's slot holds its whole partial result,
+    the merge the whole result, with the same bits launch after launch and replay after replay."""
+    import paper_2608_01150_b200 as Z
+    d = 128
+    g = torch.Generator().manual_seed(31)
+    K = 2 * chunk
+    q, k, v = rand(g, rows, H, d), rand(g, K, H, d), rand(g, K, H, d)
+    s = dict(masked=masked, slopes=torch.tensor([0.002 * (i + 1) for i in range(H)]))
+    h = Z.build_tasks([0], [(0, rows, 0, chunk, 0), (0, rows, chunk, chunk, 0)], rows, K, H, d)
+    pos = K - rows if masked else 100
+    h.set_positions(None, [(pos, 0, 0), (pos, chunk, 0)])
+    run = Run(h, s, q, k, v, d ** -0.5)
+    f = R.forward([(torch.arange(rows), torch.arange(K), pos + torch.arange(rows), torch.arange(K), 0)], q, k, v, d ** -0.5, s)
+    o, lse = run.forward()
+    R.check(o, f, "o")
+    R.check(lse, f, "lse")
+    # each slot against its own chunk
+    pr = int(h.info.partial_rows)
+    op, lp = torch.full((pr, H, d), SENTINEL, device="cuda"), torch.full((H, pr), SENTINEL, device="cuda")
+    Z.scored_attn_fwd(h, run.score, run.q, run.k, run.v, run.scale, o, lse, op, lp)
+    status_ok(h)
+    for c in range(2):
+        keys = torch.arange(c * chunk, (c + 1) * chunk)
+        part = R.forward([(torch.arange(rows), keys, pos + torch.arange(rows), keys, 0)], q, k, v, d ** -0.5, s)
+        at, _ = h.partial_slot(c)
+        R.check(op[at:at + rows], {"o": part["o"], "o_err": part["o_err"]}, "o")
+        R.check(lp[:, at:at + rows], part, "lse")
+    first = op.clone(), lp.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        Z.scored_attn_fwd(h, run.score, run.q, run.k, run.v, run.scale, o, lse, op, lp)
+    for _ in range(3):
+        op.fill_(SENTINEL)
+        lp.fill_(SENTINEL)
+        graph.replay()
+        torch.cuda.synchronize()
+        for c in range(2):
+            at, _ = h.partial_slot(c)
+            assert torch.equal(op[at:at + rows], first[0][at:at + rows]) and torch.equal(lp[:, at:at + rows], first[1][:, at:at + rows])
+    status_ok(h)
+
+
+def test_masked_calls_with_an_sm_margin():
+    """The dealt lists are for all SMs; with a margin the plain lists run, with the same results."""
+    import paper_2608_01150_b200 as Z
+    d, H, lens = 64, 2, [700, 300]
+    g = torch.Generator().manual_seed(32)
+    T = sum(lens)
+    q, k, v, d_o = (rand(g, T, H, d) for _ in range(4))
+    s = dict(masked=True)
+    h = Z.build_tasks(cu(lens), [], T, T, H, d)
+    h.set_positions([0, 50])
+    run = Run(h, s, q, k, v, d ** -0.5)
+    problems = whole_problems(lens, [0, 50])
+    check_all(run, problems, s, q, k, v, d_o, d ** -0.5)
+    for margin in (140, 146):
+        h.set_sm_margin(margin)
+        check_all(run, problems, s, q, k, v, d_o, d ** -0.5)
+
+
 def test_rows_that_see_no_chunk_at_all():
     import paper_2608_01150_b200 as Z
     d, H, rows, K = 64, 2, 140, 300
