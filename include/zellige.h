@@ -358,7 +358,7 @@ zl_status zl_coalesced_attn_bwd_noalloc(const zl_tasks* tasks, const void* q, co
  * (pairs of different sequences are never formed: the packed batch is its own document mask), then
  *     O = softmax(s) V,   LSE = log sum exp s   over the visible pairs; a row that sees no key gets O = 0, LSE = -inf.
  *
- *   cap           0 = no cap; otherwise finite and > 0.
+ *   cap           0 = no cap, otherwise 1e-4 to 1e6.
  *   slopes        device, [n_heads] fp32, finite, or NULL: a linear bias by distance.
  *   bucket_bias   device, [n_buckets, n_heads] fp32, or NULL: a learned bias by buckets of the signed distance.  An
  *                 entry of -1e30 or less (-inf, the lowest finite value of a type) removes its pairs like a mask; other entries are finite.
@@ -386,8 +386,9 @@ typedef struct {
  *   shard_pos     host, one entry per shard (may be NULL without shards): positions of the shard's first query and key row,
  *                 and the prefix of its sequence.  All >= 0, q_pos + q_len and kv_pos + kv_len at most 2^31 - 513.
  * Scores by distance need this call on handles with shards, masks on all handles.  The work lists for masked calls are
- * dealt out by what the mask leaves of each item.  Synchronises `stream`; must not run while a launch of the
- * handle is in flight; the other entry points are unaffected. */
+ * dealt out to the SMs by what the mask leaves of each item.  Synchronises `stream`; must not run while a launch of the
+ * handle is in flight.  It may be called again: a captured call uses the positions of the time of its replay.  The
+ * other entry points are unaffected. */
 zl_status zl_set_positions(zl_tasks* tasks, const int32_t* whole_prefix, const zl_shard_pos* shard_pos, void* stream);
 
 /* zl_scored_attn_fwd / _fwd_packed -- zl_coalesced_attn_fwd / _fwd_packed with scores as above; shard results are partial

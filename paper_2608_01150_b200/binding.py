@@ -455,10 +455,14 @@ class Score:
                               0 if bucket_bias is None else bucket_bias.shape[0],
                               0 if bucket_of is None else bucket_of.numel() // 2, 1 if masked else 0)
 
-    def check_heads(self, tasks: TaskHandle):
-        for name, t in (("slopes", self.slopes), ("bucket_bias", self.bucket_bias)):
-            if t is not None and t.shape[-1] != tasks.n_heads:
+    def check(self, tasks: TaskHandle):
+        for name, t in (("slopes", self.slopes), ("bucket_bias", self.bucket_bias), ("bucket_of", self.bucket_of)):
+            if t is None:
+                continue
+            if name != "bucket_of" and t.shape[-1] != tasks.n_heads:
                 raise ZlError(1, f"Score: {name} has {t.shape[-1]} heads, the handle {tasks.n_heads}")
+            if not t.is_cuda:
+                raise ZlError(1, f"Score: {name} is not on a GPU")
 
 
 def relative_position_buckets(n_buckets: int, max_distance: int, bidirectional: bool = True) -> List[int]:
@@ -496,7 +500,7 @@ def relative_position_buckets(n_buckets: int, max_distance: int, bidirectional: 
 def scored_attn_fwd(tasks: TaskHandle, score: Score, q, k, v, scale: float, o, lse, o_partial=None, lse_partial=None,
                     stream=None):
     """zl_scored_attn_fwd: coalesced_attn_fwd with capped, biased or masked scores."""
-    score.check_heads(tasks)
+    score.check(tasks)
     _check(_lib.zl_scored_attn_fwd(tasks.ptr, ctypes.byref(score.desc), _ptr(q), _ptr(k), _ptr(v), ctypes.c_float(scale),
                                    _ptr(o), _ptr(lse), _ptr(o_partial), _ptr(lse_partial), _stream_ptr(stream)),
            "zl_scored_attn_fwd")
@@ -505,7 +509,7 @@ def scored_attn_fwd(tasks: TaskHandle, score: Score, q, k, v, scale: float, o, l
 def scored_attn_fwd_packed(tasks: TaskHandle, score: Score, qkv, scale: float, o, lse, o_partial=None, lse_partial=None,
                            stream=None):
     """zl_scored_attn_fwd_packed: qkv is [T, 3, H, d] bf16."""
-    score.check_heads(tasks)
+    score.check(tasks)
     _check(_lib.zl_scored_attn_fwd_packed(tasks.ptr, ctypes.byref(score.desc), _ptr(qkv), ctypes.c_float(scale), _ptr(o),
                                           _ptr(lse), _ptr(o_partial), _ptr(lse_partial), _stream_ptr(stream)),
            "zl_scored_attn_fwd_packed")
@@ -521,7 +525,7 @@ def _check_table(score: Score, d_bucket_bias):
 def scored_attn_bwd(tasks: TaskHandle, score: Score, q, k, v, o, lse, d_o, scale: float, dq, dk, dv, d_bucket_bias,
                     workspace, workspace_bytes: Optional[int] = None, stream=None):
     """zl_scored_attn_bwd.  d_bucket_bias: fp32 [n_buckets, n_heads] or None."""
-    score.check_heads(tasks)
+    score.check(tasks)
     _check_table(score, d_bucket_bias)
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
@@ -534,7 +538,7 @@ def scored_attn_bwd(tasks: TaskHandle, score: Score, q, k, v, o, lse, d_o, scale
 def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, scale: float, dqkv, d_bucket_bias,
                            workspace, workspace_bytes: Optional[int] = None, stream=None):
     """zl_scored_attn_bwd_packed: reads qkv [T, 3, H, d], writes dqkv [T, 3, H, d]."""
-    score.check_heads(tasks)
+    score.check(tasks)
     _check_table(score, d_bucket_bias)
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()

@@ -35,11 +35,13 @@ struct zl_tasks {
     int32_t* d_kv_group_tasks = nullptr;
     int32_t* d_status = nullptr;
     int32_t* d_part_count = nullptr;
-    uint8_t* d_positions = nullptr;  // zl_set_positions: one allocation for the three tables below
-    size_t positions_bytes = 0;
+    size_t n_part_count = 0;
+    uint8_t* d_positions = nullptr;  // zl_set_positions: one allocation for the tables below, whose sizes never change
     TaskPos* d_task_pos = nullptr;
     WorkItem* d_fwd_items_masked = nullptr;
     WorkItem* d_bwd_items_masked = nullptr;
+    int32_t* d_fwd_lists = nullptr;
+    int32_t* d_bwd_lists = nullptr;
     // optional per-kernel event timing (measurement only)
     mutable bool timing = false;
     mutable std::vector<cudaEvent_t> ev_start[ZL_K_COUNT], ev_stop[ZL_K_COUNT];
@@ -196,7 +198,8 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     const size_t o_kg = place<KvGroup>(off, s.kv_groups.size());
     const size_t o_kt = place<int32_t>(off, s.kv_group_tasks.size());
     const size_t o_st = place<int32_t>(off, 2);
-    const size_t o_pc = place<int32_t>(off, s.max_item_rows <= kTileQ && s.partial_rows > 0 ? s.tasks.size() * s.n_heads : 0);
+    h->n_part_count = s.max_item_rows <= kTileQ && s.partial_rows > 0 ? s.tasks.size() * s.n_heads : 0;
+    const size_t o_pc = place<int32_t>(off, h->n_part_count);
     const size_t total = align_up(off, 256);
 
     std::vector<uint8_t> host(total, 0);
@@ -289,23 +292,28 @@ zl_status zl_build_tasks_heads(const zl_whole_desc* whole, int32_t n_whole, cons
     *out = nullptr;
     if (flags & ~ZL_BUILD_FUSE_LOCAL_CHUNKS) return ZL_ERR_INVALID_ARG;
     if (n_whole < 0 || n_shards < 0 || (n_whole > 0 && !whole) || (n_shards > 0 && !shards)) return ZL_ERR_INVALID_ARG;
-    std::vector<InputTask> in;
-    in.reserve((size_t)n_whole + n_shards);
-    for (int i = 0; i < n_whole; ++i) {
-        const zl_whole_desc& w = whole[i];
-        if (w.off < 0 || w.len < 0 || (int64_t)w.off + w.len > std::min(total_q, total_kv)) return ZL_ERR_INVALID_ARG;
-        in.push_back({w.off, w.len, w.off, w.len, 0, w.head_begin, w.head_count, -1});
-    }
-    for (int i = 0; i < n_shards; ++i) {
-        const zl_shard_desc& d = shards[i];
-        const zl_head_range hr = shard_heads ? shard_heads[i] : zl_head_range{0, n_heads};
-        in.push_back({d.q_off, d.q_len, d.kv_off, d.kv_len, d.seq_id, hr.head_begin, hr.head_count, i});
-    }
     zl_tasks* h = new (std::nothrow) zl_tasks();
     if (!h) return ZL_ERR_INVALID_ARG;
-    const zl_status st = build_schedule(in, n_shards, total_q, total_kv, n_heads, head_dim, flags, &h->sched);
-    if (st != ZL_OK) { delete h; return st; }
-    return upload_handle(h, stream, out);
+    try {
+        std::vector<InputTask> in;
+        in.reserve((size_t)n_whole + n_shards);
+        for (int i = 0; i < n_whole; ++i) {
+            const zl_whole_desc& w = whole[i];
+            if (w.off < 0 || w.len < 0 || (int64_t)w.off + w.len > std::min(total_q, total_kv)) { delete h; return ZL_ERR_INVALID_ARG; }
+            in.push_back({w.off, w.len, w.off, w.len, 0, w.head_begin, w.head_count, -1});
+        }
+        for (int i = 0; i < n_shards; ++i) {
+            const zl_shard_desc& d = shards[i];
+            const zl_head_range hr = shard_heads ? shard_heads[i] : zl_head_range{0, n_heads};
+            in.push_back({d.q_off, d.q_len, d.kv_off, d.kv_len, d.seq_id, hr.head_begin, hr.head_count, i});
+        }
+        const zl_status st = build_schedule(in, n_shards, total_q, total_kv, n_heads, head_dim, flags, &h->sched);
+        if (st != ZL_OK) { delete h; return st; }
+        return upload_handle(h, stream, out);
+    } catch (const std::bad_alloc&) {
+        delete h;
+        return ZL_ERR_INVALID_ARG;
+    }
 }
 
 zl_status zl_build_tasks_prefix(const int32_t* cu_q, const int32_t* cu_kv, int32_t n_seqs, int32_t prefix_len,
@@ -393,7 +401,7 @@ zl_status check_score(const zl_tasks* t, const zl_score* score, CheckedScore* ou
     if (!score) return ZL_ERR_INVALID_ARG;
     const Schedule& s = t->sched;
     auto aligned4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; };
-    if (!(score->cap >= 0.f) || !std::isfinite(score->cap)) return ZL_ERR_INVALID_ARG;
+    if (!(score->cap == 0.f || (score->cap >= 1e-4f && score->cap <= 1e6f))) return ZL_ERR_INVALID_ARG;
     if (score->masked != 0 && score->masked != 1) return ZL_ERR_INVALID_ARG;
     if (score->max_distance < 0 || score->max_distance > (1 << 24)) return ZL_ERR_INVALID_ARG;
     if (score->bucket_bias) {
@@ -473,6 +481,7 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     if (score) {
         sp = score->params;
         sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
+        if (!std::isfinite(sp.scale_over_cap)) return ZL_ERR_INVALID_ARG;
     }
     // Items of at most one query tile are bound by their keys' bytes and have a kernel of their own, which also takes the
     // blocks of longer query ranges where these are too few for the SMs; plain calls on handles without a shared
@@ -481,13 +490,14 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     if (sp.masked && t->sm_margin == 0) {  // dealt out to as many CTAs as there are SMs; another grid takes the plain lists
         p.items = t->d_fwd_items_masked;
         p.n_items = (int32_t)s.fwd_items_masked.size();
+        p.lists = t->d_fwd_lists;
         few = s.fwd_masked_few;
     } else if ((score || s.shared_prefix) && phase < 0 && !s.fwd_items_few.empty()) {
         p.items = t->d_fwd_items_few;
         p.n_items = (int32_t)s.fwd_items_few.size();
         few = true;
     }
-    const int grid = std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
+    const int grid = p.lists ? t->n_sms : std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
     const ScoreKind kind = score && score->biased ? kScoreBias : kScorePlain;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     CUtensorMap tq, tk, tv, to, top;
@@ -659,6 +669,7 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         const ScoredWorkspace at(s, *score);
         sp = score->params;
         sp.scale_over_cap = score->capped ? scale * 1.4426950408889634f / sp.cap_log2 : 0.f;
+        if (!std::isfinite(sp.scale_over_cap)) return ZL_ERR_INVALID_ARG;
         if (score->capped) p.lse_tiles = reinterpret_cast<float*>(ws + at.lse);
         if (d_bucket_bias) {
             sp.bucket_part = reinterpret_cast<float*>(ws + at.part);
@@ -671,6 +682,7 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         if (sp.masked && t->sm_margin == 0) {
             p.items = t->d_bwd_items_masked;
             p.n_items = (int32_t)s.bwd_items_masked.size();
+            p.lists = t->d_bwd_lists;
         }
     }
 
@@ -703,7 +715,7 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         if (launch_bwd_pair(tq, tq64, tk, tv, tdo, tdo64, tdq16, taug, tdk32, tdv32, pp, n_clusters, cs) != cudaSuccess) return ZL_ERR_CUDA;
         g_launches.fetch_add(1);
     } else if (p.n_items > 0) {
-        const int grid = std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
+        const int grid = p.lists ? t->n_sms : std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
         LaunchTimer lt(t, ZL_K_BWD_MAIN, cs);
         if (scored) {
             const ScoreKind kind = !score || !score->biased ? kScorePlain : (d_bucket_bias ? kScoreBiasGrad : kScoreBias);
@@ -834,24 +846,29 @@ zl_status zl_set_positions(zl_tasks* t, const int32_t* whole_prefix, const zl_sh
         const size_t o_pos = place<TaskPos>(off, s.task_pos.size());
         const size_t o_fwd = place<WorkItem>(off, s.fwd_items_masked.size());
         const size_t o_bwd = place<WorkItem>(off, s.bwd_items_masked.size());
-        if (off > t->positions_bytes) {  // the lists' lengths depend on the positions
-            if (t->d_positions) cudaFree(t->d_positions);
+        const size_t o_fl = place<int32_t>(off, s.fwd_lists.size());
+        const size_t o_bl = place<int32_t>(off, s.bwd_lists.size());
+        const size_t total = align_up(off, 256);
+        std::vector<uint8_t> host(total, 0);
+        auto put = [&](size_t at, const void* src, size_t bytes) { if (bytes) std::memcpy(host.data() + at, src, bytes); };
+        put(o_pos, s.task_pos.data(), s.task_pos.size() * sizeof(TaskPos));
+        put(o_fwd, s.fwd_items_masked.data(), s.fwd_items_masked.size() * sizeof(WorkItem));
+        put(o_bwd, s.bwd_items_masked.data(), s.bwd_items_masked.size() * sizeof(WorkItem));
+        put(o_fl, s.fwd_lists.data(), s.fwd_lists.size() * sizeof(int32_t));
+        put(o_bl, s.bwd_lists.data(), s.bwd_lists.size() * sizeof(int32_t));
+        if (!t->d_positions && cudaMalloc(&t->d_positions, total) != cudaSuccess) {
             t->d_positions = nullptr;
-            t->positions_bytes = 0;
-            if (cudaMalloc(&t->d_positions, align_up(off, 256)) != cudaSuccess) {
-                t->d_positions = nullptr;
-                s.task_pos.clear();
-                return ZL_ERR_CUDA;
-            }
-            t->positions_bytes = off;
+            s.task_pos.clear();
+            return ZL_ERR_CUDA;
         }
         t->d_task_pos = reinterpret_cast<TaskPos*>(t->d_positions + o_pos);
         t->d_fwd_items_masked = reinterpret_cast<WorkItem*>(t->d_positions + o_fwd);
         t->d_bwd_items_masked = reinterpret_cast<WorkItem*>(t->d_positions + o_bwd);
+        t->d_fwd_lists = reinterpret_cast<int32_t*>(t->d_positions + o_fl);
+        t->d_bwd_lists = reinterpret_cast<int32_t*>(t->d_positions + o_bl);
         cudaStream_t cs = static_cast<cudaStream_t>(stream);
-        if (cudaMemcpyAsync(t->d_task_pos, s.task_pos.data(), s.task_pos.size() * sizeof(TaskPos), cudaMemcpyHostToDevice, cs) != cudaSuccess ||
-            upload_items(t, t->d_fwd_items_masked, s.fwd_items_masked, cs) != ZL_OK ||
-            upload_items(t, t->d_bwd_items_masked, s.bwd_items_masked, cs) != ZL_OK || cudaStreamSynchronize(cs) != cudaSuccess) {
+        if (cudaMemcpyAsync(t->d_positions, host.data(), total, cudaMemcpyHostToDevice, cs) != cudaSuccess ||
+            cudaStreamSynchronize(cs) != cudaSuccess) {
             s.task_pos.clear();
             return ZL_ERR_CUDA;
         }
@@ -1056,7 +1073,10 @@ zl_status zl_last_device_status(const zl_tasks* t, int32_t* code, int32_t* where
     if (cudaDeviceSynchronize() != cudaSuccess) return ZL_ERR_CUDA;
     if (cudaMemcpy(host, t->d_status, sizeof(host), cudaMemcpyDeviceToHost) != cudaSuccess) return ZL_ERR_CUDA;
     *code = host[0]; *where = host[1];
-    if (host[0] != 0 && cudaMemset(t->d_status, 0, sizeof(host)) != cudaSuccess) return ZL_ERR_CUDA;
+    if (host[0] != 0) {  // a launch that gave up may also have left pieces counted
+        if (cudaMemset(t->d_status, 0, sizeof(host)) != cudaSuccess) return ZL_ERR_CUDA;
+        if (t->n_part_count && cudaMemset(t->d_part_count, 0, t->n_part_count * sizeof(int32_t)) != cudaSuccess) return ZL_ERR_CUDA;
+    }
     return ZL_OK;
 }
 

@@ -24,6 +24,7 @@ struct FwdParams {
     float* o_partial;
     float* lse_partial;
     int32_t* status;  // [0] = code, [1] = where
+    const int32_t* lists;  // CTA c walks items [lists[c], lists[c + 1]); NULL: items c, c + grid, ... (scored kernels only)
     int32_t* part_count;  // [tasks, H] finished pieces of an item cut along the keys; zero between launches
 };
 
@@ -66,6 +67,7 @@ struct BwdParams {
     uint8_t* aug;   // [H, q_pad_total / 128] tiles of 4 KB: bf16 splits of -lse/scale and -rowsum(dO o O)
     int32_t* status;
     float* lse_tiles;  // [H, q_pad_total] LSE * log2(e), 1e30 for rows without a key; NULL unless scores are capped
+    const int32_t* lists;  // as in FwdParams
     bool zero_dq;      // the preprocess kernel clears dq_acc (its rows are the padded query rows)
     float* d_bucket_bias;      // [n_buckets, H] gradient of the bucket table, summed beside the dQ conversion; NULL: not wanted
     const float* bucket_part;  // [H, n_kv_tiles, kMaxBuckets] key tiles' shares of it

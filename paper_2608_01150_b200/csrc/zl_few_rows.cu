@@ -138,15 +138,15 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const uint32_t tmem = sm.tmem_base;
     grid_release();
     grid_wait();
+    const Walk walk(p);
 
     if (warp < 4) {
         reg_dec<72>();
         if (warp == 0 && lane == 0) {
             // -------------------------------------------------------------- TMA producer
             uint32_t item_cnt = 0, kv_cnt = 0;
-            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+            for (int it = walk.first; it < walk.end; it += walk.step) {
                 const WorkItem wi = p.items[it];
-                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const FewItem fi(wi, sp, t);
                 const int n_kv = fi.n_kv;
@@ -185,9 +185,8 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             const uint64_t dv0 = make_desc_sw128(smem_u32(sm.v[0]), Smem::kBoxBytes, 1024);  // V is the MN-major B operand
             constexpr uint32_t kTileStep = Smem::kTileBytes >> 4, kQStep = (uint32_t)sizeof(sm.q[0]) >> 4;
             uint32_t item_cnt = 0, kv_cnt = 0, pa_cnt = 0, pb_cnt = 0;
-            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+            for (int it = walk.first; it < walk.end; it += walk.step) {
                 const WorkItem wi = p.items[it];
-                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const int n_kv = FewItem(wi, sp, t).n_kv;
                 if (n_kv == 0) continue;
@@ -237,9 +236,8 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             // -------------------------------------------------------------- biases of near tiles, one warp per warpgroup
             const int x = warp - 2;
             WindowFeed feed{&sm.bias_full[x], &sm.bias_empty[x], sm.window[x]};
-            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+            for (int it = walk.first; it < walk.end; it += walk.step) {
                 const WorkItem wi = p.items[it];
-                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const TaskPos tp = task_pos(sp, wi.unit);
                 const FewItem fi(wi, sp, t);
@@ -265,9 +263,8 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const uint32_t col_s = kColS + x * 128, col_o = kColO + x * 128;
         uint32_t bias_cnt = 0;
         uint32_t s_cnt = 0, o_cnt[2] = {0, 0}, join_cnt = 0;
-        for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+        for (int it = walk.first; it < walk.end; it += walk.step) {
             const WorkItem wi = p.items[it];
-            if (wi.rows == 0) break;  // end of this CTA's list
             const Task t = p.tasks[wi.unit];
             const TaskPos tp = task_pos(sp, wi.unit);
             const FewItem fi(wi, sp, t);

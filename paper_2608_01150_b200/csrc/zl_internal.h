@@ -116,9 +116,11 @@ struct Schedule {
     bool all_heads = true;                  // every task covers all heads
     bool shared_prefix = false;             // built by build_prefix_schedule: query ranges nest
     // Positions (zl_set_positions): one entry per task, and the work lists dealt out to the CTAs by what the mask leaves of
-    // each item (an item without rows ends a CTA's list).
+    // each item: CTA c walks items [lists[c], lists[c + 1]).
     std::vector<TaskPos> task_pos;
     std::vector<WorkItem> fwd_items_masked, bwd_items_masked;
+    std::vector<int32_t> fwd_lists, bwd_lists;
+    int32_t masked_parts = 0;  // pieces along the keys in fwd_items_masked; 0: not chosen yet
     // Blocks of one query tile for the few-rows kernel, where they finish sooner than blocks of two, or items of few rows in
     // pieces along the keys (empty: neither); fwd_masked_few says that fwd_items_masked is such a list.
     std::vector<WorkItem> fwd_items_few;

@@ -94,6 +94,17 @@ __device__ __forceinline__ PatchSide patch_side(const ScoreParams& sp, int lo, i
     return lo >= sp.reach ? kFarPos : (hi <= -sp.reach ? kFarNeg : kNear);
 }
 
+// The items of a CTA: for (int it = w.first; it < w.end; it += w.step).
+struct Walk {
+    int first, end, step;
+    template <class Params>
+    __device__ __forceinline__ explicit Walk(const Params& p) {
+        first = p.lists ? __ldg(p.lists + blockIdx.x) : (int)blockIdx.x;
+        end = p.lists ? __ldg(p.lists + blockIdx.x + 1) : p.n_items;
+        step = p.lists ? 1 : (int)gridDim.x;
+    }
+};
+
 __device__ __forceinline__ TaskPos task_pos(const ScoreParams& sp, int task) {
     return sp.pos ? sp.pos[task] : TaskPos{0, 0, 0, 0};
 }

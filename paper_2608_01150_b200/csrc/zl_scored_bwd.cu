@@ -218,15 +218,15 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = sm.tmem_base;
     grid_wait();
+    const Walk walk(p);
 
     if (warp < 4) {
         reg_dec<72>();
         if (warp == 0 && lane == 0) {
             // -------------------------------------------------------------- TMA producer
             uint32_t item_cnt = 0, it_cnt = 0;
-            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+            for (int it = walk.first; it < walk.end; it += walk.step) {
                 const WorkItem wi = p.items[it];
-                if (wi.rows == 0) break;  // end of this CTA's list
                 const KvGroup g = p.kv_groups[wi.unit];
                 if (count_q_tiles(p, sp, g, wi.row0) == 0) continue;  // no query sees these keys
                 ZL_WAIT(&sm.kv_empty, (item_cnt & 1) ^ 1, 1);
@@ -312,9 +312,8 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 if (mma_lane) mma_commit(&sm.do_empty);
             };
             uint32_t item_cnt = 0, it_cnt = 0;
-            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+            for (int it = walk.first; it < walk.end; it += walk.step) {
                 const WorkItem wi = p.items[it];
-                if (wi.rows == 0) break;  // end of this CTA's list
                 const KvGroup g = p.kv_groups[wi.unit];
                 const int n_it = count_q_tiles(p, sp, g, wi.row0);
                 if (n_it == 0) continue;
@@ -388,9 +387,8 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         const bool store_leader = (warp & 3) == 0 && lane == 0;  // one thread per warpgroup issues its TMA stores
         bool store_pending = false;
         float* const window = sm.window[warp - 4];
-        for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+        for (int it = walk.first; it < walk.end; it += walk.step) {
             const WorkItem wi = p.items[it];
-            if (wi.rows == 0) break;  // end of this CTA's list
             const KvGroup g = p.kv_groups[wi.unit];
             const bool row_ok = row < wi.rows;
             HeadBias hb;
@@ -711,9 +709,8 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
         const bool leader = (lane == 0);  // per warp
         uint32_t it_cnt = 0, chunk_cnt = 0;
-        for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+        for (int it = walk.first; it < walk.end; it += walk.step) {
             const WorkItem wi = p.items[it];
-            if (wi.rows == 0) break;  // end of this CTA's list
             const KvGroup g = p.kv_groups[wi.unit];
             for (int ti = 0; ti < g.n_tasks; ++ti) {
                 const int task = p.kv_group_tasks[g.task_begin + ti];

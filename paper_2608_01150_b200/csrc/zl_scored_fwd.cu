@@ -132,15 +132,15 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     const uint32_t tmem = sm.tmem_base;
     grid_release();
     grid_wait();
+    const Walk walk(p);
 
     if (warp < 4) {
         reg_dec<72>();
         if (warp == 0 && lane == 0) {
             // -------------------------------------------------------------- TMA producer
             uint32_t q_cnt = 0, qb_cnt = 0, kv_cnt = 0;
-            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+            for (int it = walk.first; it < walk.end; it += walk.step) {
                 const WorkItem wi = p.items[it];
-                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const bool has_b = wi.rows > kTileQ;
                 const int n_a = key_tiles(sp, t, wi.unit, wi.row0, min(wi.rows, kTileQ));
@@ -204,9 +204,8 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     if (mma_lane) mma_ts(tmem + kColO + x * 128, tp + ks * 8, dv + ks * (2048 >> 4), idesc_o, acc || ks > 0);
             };
             uint32_t q_cnt = 0, qb_cnt = 0, kv_cnt = 0, p_cnt[2] = {0, 0};
-            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+            for (int it = walk.first; it < walk.end; it += walk.step) {
                 const WorkItem wi = p.items[it];
-                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const bool has_b = wi.rows > kTileQ;
                 const int n_a = key_tiles(sp, t, wi.unit, wi.row0, min(wi.rows, kTileQ));
@@ -256,9 +255,8 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             // -------------------------------------------------------------- biases of near tiles: warp 2 tile A, warp 3 tile B
             const int x = warp - 2;
             WindowFeed feed{&sm.bias_full[x], &sm.bias_empty[x], sm.window[x]};
-            for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+            for (int it = walk.first; it < walk.end; it += walk.step) {
                 const WorkItem wi = p.items[it];
-                if (wi.rows == 0) break;  // end of this CTA's list
                 const Task t = p.tasks[wi.unit];
                 const TaskPos tp = task_pos(sp, wi.unit);
                 const int row0 = wi.row0 + x * kTileQ;
@@ -287,9 +285,8 @@ zl_scored_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         const bool store_leader = quarter == 0 && lane == 0;  // one thread per warpgroup issues its TMA stores
         bool store_pending = false;                            // this warpgroup's box may still be read by a store
         uint32_t bias_cnt = 0;
-        for (int it = blockIdx.x; it < p.n_items; it += gridDim.x) {
+        for (int it = walk.first; it < walk.end; it += walk.step) {
             const WorkItem wi = p.items[it];
-            if (wi.rows == 0) break;  // end of this CTA's list
             const int tile_rows = min(kTileQ, wi.rows - x * kTileQ);  // rows of this warpgroup's tile
             if (tile_rows <= 0) continue;
             const Task t = p.tasks[wi.unit];

@@ -127,12 +127,15 @@ std::vector<WorkItem> in_pieces(const Schedule& s, const std::vector<WorkItem>& 
 // Whether blocks of one query tile (`few` steps) beat blocks of two: a step of theirs loads twice the keys.
 bool few_rows_pay(int64_t few, int64_t two) { return few * 10 < two * 9; }
 
+// Beyond this many items per SM the rounds are even enough, whatever their blocks.
+constexpr size_t kEvenItems = 16 * kSms;
+
 // Numbers of pieces worth trying: a piece has two key tiles at least.
 constexpr int32_t kPieces[] = {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
-bool worth_trying(const Schedule& s, int32_t parts) {
+bool worth_trying(const Schedule& s, int32_t parts, size_t n_items) {
     int32_t longest = 0;
     for (const Task& t : s.tasks) longest = std::max(longest, t.kv_len);
-    return parts * s.max_item_rows <= kTileQ && parts * 2 * kTileKV <= longest + 2 * kTileKV;
+    return parts * s.max_item_rows <= kTileQ && parts * 2 * kTileKV <= longest + 2 * kTileKV && parts * n_items <= kEvenItems;
 }
 
 // Most steps of a CTA that takes items i, i + ctas, ...
@@ -142,34 +145,33 @@ int64_t makespan(const std::vector<int64_t>& steps, size_t ctas) {
     return *std::max_element(load.begin(), load.end());
 }
 
-// Deals items out to CTAs.  A CTA of the persistent kernels walks items i, i + grid, i + 2 grid, ...; under a mask their work
-// differs from a tile to the whole row, and round robin would give the first CTA the longest item of every round.  So the
-// items, longest first, go to the CTA with the least work so far, and an item without rows ends a list before the
-// longest one.  Returns the most steps of a CTA.
-int64_t deal(std::vector<WorkItem>* items, const std::vector<int64_t>& steps, int32_t n_sms) {
+// Deals items out to CTAs: under a mask their work differs from a tile to the whole row, and walking items i, i + grid, ... would
+// give the first CTA the longest item of every round.  So the items, longest first, go to the CTA with the least work so
+// far.  `items` becomes the CTAs' lists one after the other, `begin` where each starts (n_sms + 1 entries).  Returns the
+// most steps of a CTA.
+int64_t deal(std::vector<WorkItem>* items, const std::vector<int64_t>& steps, int32_t n_sms, std::vector<int32_t>* begin) {
     std::vector<int32_t> order(items->size());
     for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
     std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return steps[a] > steps[b]; });
-    const int32_t ctas = (int32_t)std::min<size_t>(n_sms, items->size());
     using Load = std::pair<int64_t, int32_t>;
     std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
-    for (int32_t c = 0; c < ctas; ++c) least.push({0, c});
-    std::vector<std::vector<int32_t>> lists(ctas);
-    size_t longest = 0;
+    for (int32_t c = 0; c < n_sms; ++c) least.push({0, c});
+    std::vector<std::vector<int32_t>> lists(n_sms);
     int64_t most = 0;
     for (int32_t i : order) {
         const Load l = least.top();
         least.pop();
         lists[l.second].push_back(i);
-        longest = std::max(longest, lists[l.second].size());
         most = std::max(most, l.first + steps[i]);
         least.push({l.first + steps[i], l.second});
     }
     std::vector<WorkItem> dealt;
-    dealt.reserve(longest * ctas);
-    for (size_t r = 0; r < longest; ++r)
-        for (int32_t c = 0; c < ctas; ++c)
-            dealt.push_back(r < lists[c].size() ? (*items)[lists[c][r]] : WorkItem{0, 0, 0, 0});
+    dealt.reserve(items->size());
+    begin->assign(1, 0);
+    for (const std::vector<int32_t>& list : lists) {
+        for (int32_t i : list) dealt.push_back((*items)[i]);
+        begin->push_back((int32_t)dealt.size());
+    }
     items->swap(dealt);
     return most;
 }
@@ -197,14 +199,14 @@ void finish_schedule(Schedule* s) {
         for (const WorkItem& w : items) steps.push_back(item_steps(*s, w, few, false));
         return makespan(steps, kSms);
     };
-    if (s->max_item_rows > kTileQ) {
+    if (s->max_item_rows > kTileQ && s->fwd_items.size() <= kEvenItems) {
         s->fwd_items_few = forward_blocks(*s, kTileQ);
         std::stable_sort(s->fwd_items_few.begin(), s->fwd_items_few.end(), longest_first);
         if (!few_rows_pay(span(s->fwd_items_few, true), span(s->fwd_items, false))) s->fwd_items_few.clear();
-    } else if (!s->shared_prefix) {
+    } else if (s->max_item_rows <= kTileQ && !s->shared_prefix) {
         int64_t best = span(s->fwd_items, true);
         for (int32_t parts : kPieces) {
-            if (!worth_trying(*s, parts)) break;
+            if (!worth_trying(*s, parts, s->fwd_items.size())) break;
             std::vector<WorkItem> items = in_pieces(*s, s->fwd_items, parts);
             const int64_t steps = span(items, true);
             if (steps < best) { best = steps; s->fwd_items_few.swap(items); }
@@ -582,26 +584,34 @@ zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard
         for (const WorkItem& w : items) steps.push_back(item_steps(*s, w, few, true));
         return steps;
     };
-    s->fwd_masked_few = s->max_item_rows <= kTileQ;
-    s->fwd_items_masked = s->fwd_items;
-    const int64_t two = deal(&s->fwd_items_masked, steps_of(s->fwd_items, s->fwd_masked_few), n_sms);
-    if (s->fwd_masked_few && !s->shared_prefix) {
-        int64_t best = two;
-        for (int32_t parts : kPieces) {
-            if (!worth_trying(*s, parts)) break;
-            std::vector<WorkItem> items = in_pieces(*s, s->fwd_items, parts);
-            const std::vector<int64_t> steps = steps_of(items, true);
-            const int64_t most = deal(&items, steps, n_sms);
-            if (most < best) { best = most; s->fwd_items_masked.swap(items); }
-        }
-    } else if (!s->fwd_masked_few) {
-        std::vector<WorkItem> blocks = forward_blocks(*s, kTileQ);
-        const std::vector<int64_t> steps = steps_of(blocks, true);
-        if (few_rows_pay(deal(&blocks, steps, n_sms), two)) {
-            s->fwd_items_masked.swap(blocks);
-            s->fwd_masked_few = true;
+    // Blocks and pieces are chosen once: later positions may suit others better, but launches captured before this call must
+    // find lists of their kind and length.
+    auto blocks = [&](int32_t parts, bool few) {
+        if (parts > 1) return in_pieces(*s, s->fwd_items, parts);
+        return few && s->max_item_rows > kTileQ ? forward_blocks(*s, kTileQ) : s->fwd_items;
+    };
+    auto deal_fwd = [&](int32_t parts, bool few, std::vector<WorkItem>* items, std::vector<int32_t>* begin) {
+        *items = blocks(parts, few);
+        return deal(items, steps_of(*items, few), n_sms, begin);
+    };
+    if (s->masked_parts == 0) {
+        const bool all_few = s->max_item_rows <= kTileQ;
+        std::vector<WorkItem> items;
+        std::vector<int32_t> begin;
+        int64_t best = deal_fwd(1, all_few, &items, &begin);
+        s->masked_parts = 1;
+        s->fwd_masked_few = all_few;
+        if (all_few && !s->shared_prefix) {
+            for (int32_t parts : kPieces) {
+                if (!worth_trying(*s, parts, s->fwd_items.size())) break;
+                const int64_t most = deal_fwd(parts, true, &items, &begin);
+                if (most < best) { best = most; s->masked_parts = parts; }
+            }
+        } else if (!all_few && s->fwd_items.size() <= kEvenItems) {
+            s->fwd_masked_few = few_rows_pay(deal_fwd(1, true, &items, &begin), best);
         }
     }
+    deal_fwd(s->masked_parts, s->fwd_masked_few, &s->fwd_items_masked, &s->fwd_lists);
     s->bwd_items_masked = s->bwd_items;
     std::vector<int64_t> work;
     for (const WorkItem& w : s->bwd_items_masked) {
@@ -614,7 +624,7 @@ zl_status set_positions(Schedule* s, const int32_t* whole_prefix, const zl_shard
         }
         work.push_back(tiles);
     }
-    deal(&s->bwd_items_masked, work, n_sms);
+    deal(&s->bwd_items_masked, work, n_sms, &s->bwd_lists);
     return ZL_OK;
 }
 

@@ -550,6 +550,42 @@ def test_positions_can_change_and_leave_plain_calls_alone():
     assert torch.equal(o0, o1) and torch.equal(l0, l1)
 
 
+@pytest.mark.parametrize("lens", [[400, 900], [130, 70]])
+def test_captured_masked_calls_follow_new_positions(lens):
+    """Forward and backward captured under one mask, replayed under others: the results of eager calls with those."""
+    import paper_2608_01150_b200 as Z
+    d, H, T = 64, 2, sum(lens)
+    g = torch.Generator().manual_seed(33)
+    q, k, v, d_o = (rand(g, T, H, d).cuda() for _ in range(4))
+    h = Z.build_tasks(cu(lens), [], T, T, H, d)
+    h.set_positions([0, 0])
+    sc = Z.Score(masked=True)
+    o, dq, dk, dv = (torch.empty_like(q) for _ in range(4))
+    lse = torch.empty(H, T, device="cuda")
+    ws = torch.empty(h.scored_workspace_bytes(sc), dtype=torch.uint8, device="cuda")
+
+    def step():
+        Z.scored_attn_fwd(h, sc, q, k, v, 0.125, o, lse)
+        Z.scored_attn_bwd(h, sc, q, k, v, o, lse, d_o, 0.125, dq, dk, dv, None, ws)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for prefix in ([0, 0], [lens[0], 0], [7, lens[1]], [lens[0], lens[1]], [0, 0]):
+        h.set_positions(prefix)
+        step()
+        torch.cuda.synchronize()
+        want = [x.clone() for x in (o, lse, dk, dv)]
+        for x in (o, lse, dk, dv):
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, (o, lse, dk, dv)):
+            assert torch.equal(a, b), prefix
+    status_ok(h)
+
+
 def test_refusals_on_the_device():
     import paper_2608_01150_b200 as Z
     h = Z.build_tasks([0, 10], [], 10, 10, 2, 64)
@@ -567,6 +603,8 @@ def test_refusals_on_the_device():
     assert status(Z.scored_attn_fwd, h, s, x, x, x, 0.0, x, lse) == 1
     assert status(Z.scored_attn_fwd, h, s, x.data_ptr() + 2, x, x, 1.0, x, lse) == 1
     assert status(Z.scored_attn_fwd, h, Z.Score(masked=True), x, x, x, 1.0, x, lse) == 1
+    assert status(Z.scored_attn_fwd, h, Z.Score(slopes=torch.zeros(2)), x, x, x, 1.0, x, lse) == 1             # slopes on the host
+    assert status(Z.scored_attn_fwd, h, Z.Score(cap=1e-4), x, x, x, 3e38, x, lse) == 1                          # scale / cap overflows
     assert status(Z.scored_attn_bwd, h, s, x, x, x, x, lse, x, 1.0, x, x, x, f, ws) == 1            # a table's gradient without a table
     assert status(Z.scored_attn_bwd, h, s, x, x, x, x, lse, x, 1.0, x, x, x, None, ws[:-4]) == 4
     assert status(Z.scored_attn_bwd, h, s, x, x, x, x, lse, x, 1.0, x, x, x, None, ws[16:], ws.numel()) == 1

@@ -59,7 +59,7 @@ no_device = pytest.mark.skipif(torch.cuda.is_available(), reason="made-up pointe
 
 @no_device
 @pytest.mark.parametrize("score,status", [
-    (dict(cap=-1.0), 1), (dict(cap=math.inf), 1), (dict(cap=math.nan), 1), (dict(masked=2), 1),
+    (dict(cap=-1.0), 1), (dict(cap=math.inf), 1), (dict(cap=1e-5), 1), (dict(cap=2e6), 1), (dict(cap=math.nan), 1), (dict(masked=2), 1),
     (dict(bias=16, of=16, n=0), 1), (dict(bias=16, n=4), 1), (dict(of=16), 1), (dict(n=4), 1),
     (dict(bias=16, of=16, n=65), 3), (dict(bias=16, of=16, n=4, dist=-1), 1), (dict(bias=16, of=16, n=4, dist=(1 << 24) + 1), 1),
     (dict(slopes=2), 1), (dict(masked=1), 1),                            # misaligned; mask without positions
