@@ -117,34 +117,30 @@ __device__ __forceinline__ int count_q_tiles(const BwdParams& p, const ScorePara
 
 // Adds the sums v[i] of distances 32 i + lane (bucket b[i], -1 for none) to a table of kMaxBuckets sums in shared memory that
 // only this warp uses.  Among 32 consecutive distances runs of equal buckets are summed by shuffles; where a bucket has
-// several runs their sums are added one after the other, in lane order.
-__device__ __forceinline__ void add_by_bucket(float* sums, float (&v)[kPatch / 32], const int (&b)[kPatch / 32], int lane) {
-    bool head[kPatch / 32];
-    int run_end[kPatch / 32];
-#pragma unroll
+// several runs their sums are added one after the other, in lane order.  (One copy of the code: the instruction cache counts
+// for more here than three chains side by side.)
+__device__ __forceinline__ void add_by_bucket(float* sums, const float (&v)[kPatch / 32], const int (&b)[kPatch / 32], int lane) {
+    static_assert(kPatch / 32 == 3, "");
+#pragma unroll 1
     for (int i = 0; i < kPatch / 32; ++i) {
-        const int before = __shfl_up_sync(0xffffffffu, b[i], 1);
-        const uint32_t heads = __ballot_sync(0xffffffffu, lane == 0 || b[i] != before);
+        float x = i == 0 ? v[0] : (i == 1 ? v[1] : v[2]);
+        const int bucket = i == 0 ? b[0] : (i == 1 ? b[1] : b[2]);
+        const int before = __shfl_up_sync(0xffffffffu, bucket, 1);
+        const uint32_t heads = __ballot_sync(0xffffffffu, lane == 0 || bucket != before);
         const uint32_t later = heads & (0xfffffffeu << lane);  // run starts after this lane
-        run_end[i] = later ? __ffs(later) - 1 : 32;
-        head[i] = ((heads >> lane) & 1u) && b[i] >= 0;
-    }
+        const int run = (later ? __ffs(later) - 1 : 32) - lane;
 #pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        float o[kPatch / 32];
-#pragma unroll
-        for (int i = 0; i < kPatch / 32; ++i) o[i] = __shfl_down_sync(0xffffffffu, v[i], off);
-#pragma unroll
-        for (int i = 0; i < kPatch / 32; ++i)
-            if (lane + off < run_end[i]) v[i] += o[i];
-    }
-#pragma unroll
-    for (int i = 0; i < kPatch / 32; ++i) {
-        const uint32_t same = __match_any_sync(0xffffffffu, head[i] ? b[i] : -1 - lane);
+        for (int off = 1; off < 32; off <<= 1) {
+            const float o = __shfl_down_sync(0xffffffffu, x, off);
+            if (off < run) x += o;
+        }
+        const bool head = ((heads >> lane) & 1u) && bucket >= 0;
+        const uint32_t same = __match_any_sync(0xffffffffu, head ? bucket : -1 - lane);
         const int rank = __popc(same & ((1u << lane) - 1u));
-        const int rounds = __reduce_max_sync(0xffffffffu, head[i] ? rank : 0);
+        const int rounds = __reduce_max_sync(0xffffffffu, head ? rank : 0);
+#pragma unroll 1
         for (int r = 0; r <= rounds; ++r) {
-            if (head[i] && rank == r) sums[b[i]] += v[i];
+            if (head && rank == r) sums[bucket] += x;
             __syncwarp();
         }
     }
