@@ -173,7 +173,8 @@ zl_status zl_build_tasks_heads(const zl_whole_desc* whole, int32_t n_whole,
  * summed over all sequences; own key rows of a sequence without queries are covered by no task and left untouched.
  * The prefix is cut into chunks along the keys so that few query rows (one token per sequence) still occupy the GPU.
  * Shard numbers (zl_tasks_get_partial_slot, zl_set_*_phases, zl_set_positions) are sequence numbers and mean the
- * part over the sequence's own keys; the chunks of the prefix run in launch phase 0.
+ * part over the sequence's own keys; the chunks of the prefix run in launch phase 0 (results of phased launches agree with the
+ * single launch's within rounding: the two may use different kernels).
  * Scores: caps and, after zl_set_positions, the prefix mask work (the mask applies among a sequence's own rows, the
  * shared prefix is seen whole); scores that depend on the distance are refused (ZL_ERR_UNSUPPORTED), because the
  * distance of a prefix key differs from sequence to sequence. */

@@ -132,7 +132,8 @@ struct WindowFeed {
         float v[kWindow / 32];
 #pragma unroll
         for (int i = 0; i < kWindow / 32; ++i) v[i] = hb.at(sp, head, lo + i * 32 + lane);
-        const bool ok = wait(empty, (count & 1) ^ 1, abort_flag);
+        // up to a whole item of far tiles may lie between two near ones: a limit for the longest keys that fit the memory
+        const bool ok = mbar_try_wait(empty, (count & 1) ^ 1) || mbar_wait_slow(empty, (count & 1) ^ 1, 16 * kWaitLimitNs, abort_flag);
         if (!__all_sync(0xffffffffu, ok)) return false;
         ++count;
 #pragma unroll

@@ -700,3 +700,52 @@ def test_shared_prefix_both_backward_kernels_and_a_captured_step():
         torch.cuda.synchronize()
         assert torch.equal(o, run.o) and torch.equal(lse, run.lse) and torch.equal(dk, want["dk"]) and torch.equal(dv, want["dv"])
     status_ok(h)
+
+
+def test_shared_prefix_in_phases_and_without_a_workspace():
+    """Own parts in a later launch phase than the prefix; the backward in phases and with the library's own scratch."""
+    import paper_2608_01150_b200 as Z
+    d, H, P, lens = 64, 2, 900, [40, 1, 200]
+    g = torch.Generator().manual_seed(25)
+    nq, nk = sum(lens), P + sum(lens)
+    q, d_o, k, v = rand(g, nq, H, d), rand(g, nq, H, d), rand(g, nk, H, d), rand(g, nk, H, d)
+    problems = prefix_problems(lens, lens, P)
+    f = R.forward(problems, q, k, v, d ** -0.5, {})
+    h = Z.build_tasks_prefix(cu(lens), cu(lens), P, nq, nk, H, d)
+    h.set_fwd_phases(None, [1, 1, 1], 2)
+    h.set_bwd_phases(None, [1, 1, 1], 2)
+    run = Run(h, {}, q, k, v, d ** -0.5, plain=True)
+    pr = int(h.info.partial_rows)
+    op, lp = torch.full((pr, H, d), SENTINEL, device="cuda"), torch.full((H, pr), SENTINEL, device="cuda")
+    o, lse = torch.empty_like(run.q), torch.empty(H, nq, device="cuda")
+    for phase in (1, 0):
+        Z.coalesced_attn_fwd_phase(h, phase, run.q, run.k, run.v, d ** -0.5, o, lse, op, lp)
+    Z.lse_merge(h, op, lp, o, lse)
+    status_ok(h)
+    R.check(o, f, "o")
+    R.check(lse, f, "lse")
+    b = R.backward(problems, q, k, v, o.cpu(), lse.cpu(), d_o, d ** -0.5, {}, ds_roundings=1)
+    ws = torch.full((int(h.info.bwd_workspace_bytes),), 255, dtype=torch.uint8, device="cuda")
+    dd = d_o.cuda()
+    for noalloc in (False, True):
+        dq, dk, dv = (torch.full_like(x, SENTINEL) for x in (run.q, run.k, run.v))
+        if noalloc:
+            Z.coalesced_attn_bwd_noalloc(h, run.q, run.k, run.v, o, lse, dd, d ** -0.5, dq, dk, dv)
+        else:
+            for phase in (0, 1):
+                Z.coalesced_attn_bwd_phase(h, phase, run.q, run.k, run.v, o, lse, dd, d ** -0.5, dq, dk, dv, ws)
+        status_ok(h)
+        for name, x in (("dq", dq), ("dk", dk), ("dv", dv)):
+            R.check(x, b, name)
+
+
+def test_many_rows_over_a_short_prefix_and_one_row_over_a_long_one():
+    """Row blocks of two query tiles, of one, and a handle whose prefix is cut into many chunks."""
+    import paper_2608_01150_b200 as Z
+    d, H = 128, 2
+    g = torch.Generator().manual_seed(26)
+    for qlens, klens, P in (([500, 600], [3, 0], 130), ([1], [0], 9000), ([1, 1, 1], [128, 129, 1], 5000)):
+        nq, nk = sum(qlens), P + sum(klens)
+        q, d_o, k, v = rand(g, nq, H, d), rand(g, nq, H, d), rand(g, nk, H, d), rand(g, nk, H, d)
+        h = Z.build_tasks_prefix(cu(qlens), cu(klens), P, nq, nk, H, d)
+        check_all(Run(h, {}, q, k, v, d ** -0.5, plain=True), prefix_problems(qlens, klens, P), {}, q, k, v, d_o, d ** -0.5)
