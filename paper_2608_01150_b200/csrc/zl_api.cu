@@ -30,6 +30,7 @@ struct zl_tasks {
     MergeGroup* d_merge_groups = nullptr;
     int32_t* d_merge_parts = nullptr;
     int32_t* d_merge_prefix = nullptr;
+    int32_t* d_merge_row_group = nullptr;
     QGroup* d_q_groups = nullptr;
     KvGroup* d_kv_groups = nullptr;
     int32_t* d_kv_group_tasks = nullptr;
@@ -194,6 +195,7 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     const size_t o_mg = place<MergeGroup>(off, s.merge_groups.size());
     const size_t o_mp = place<int32_t>(off, s.merge_parts.size());
     const size_t o_mr = place<int32_t>(off, s.merge_row_prefix.size());
+    const size_t o_rg = place<int32_t>(off, s.merge_row_group.size());
     const size_t o_qg = place<QGroup>(off, s.q_groups.size());
     const size_t o_kg = place<KvGroup>(off, s.kv_groups.size());
     const size_t o_kt = place<int32_t>(off, s.kv_group_tasks.size());
@@ -212,6 +214,7 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     put(o_mg, s.merge_groups.data(), s.merge_groups.size() * sizeof(MergeGroup));
     put(o_mp, s.merge_parts.data(), s.merge_parts.size() * sizeof(int32_t));
     put(o_mr, s.merge_row_prefix.data(), s.merge_row_prefix.size() * sizeof(int32_t));
+    put(o_rg, s.merge_row_group.data(), s.merge_row_group.size() * sizeof(int32_t));
     put(o_qg, s.q_groups.data(), s.q_groups.size() * sizeof(QGroup));
     put(o_kg, s.kv_groups.data(), s.kv_groups.size() * sizeof(KvGroup));
     put(o_kt, s.kv_group_tasks.data(), s.kv_group_tasks.size() * sizeof(int32_t));
@@ -231,6 +234,7 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     h->d_merge_groups = reinterpret_cast<MergeGroup*>(h->d_tables + o_mg);
     h->d_merge_parts = reinterpret_cast<int32_t*>(h->d_tables + o_mp);
     h->d_merge_prefix = reinterpret_cast<int32_t*>(h->d_tables + o_mr);
+    h->d_merge_row_group = reinterpret_cast<int32_t*>(h->d_tables + o_rg);
     h->d_q_groups = reinterpret_cast<QGroup*>(h->d_tables + o_qg);
     h->d_kv_groups = reinterpret_cast<KvGroup*>(h->d_tables + o_kg);
     h->d_kv_group_tasks = reinterpret_cast<int32_t*>(h->d_tables + o_kt);
@@ -574,6 +578,7 @@ zl_status zl_lse_merge(const zl_tasks* t, const float* o_partial, const float* l
     p.groups = t->d_merge_groups;
     p.parts = t->d_merge_parts;
     p.row_prefix = t->d_merge_prefix;
+    p.row_group = t->d_merge_row_group;
     p.n_groups = (int32_t)s.merge_groups.size();
     p.n_heads = s.n_heads;
     p.total_q = s.total_q;

@@ -32,6 +32,7 @@ struct MergeParams {
     const MergeGroup* groups;
     const int32_t* parts;       // partial slot row offsets
     const int32_t* row_prefix;  // n_groups + 1
+    const int32_t* row_group;   // [row_prefix[n_groups]] group of every row; handles over a shared prefix only
     int32_t n_groups;
     int32_t n_heads;
     int32_t total_q;

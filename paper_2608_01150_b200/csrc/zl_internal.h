@@ -106,6 +106,7 @@ struct Schedule {
     std::vector<int32_t> shard_slot_rows;   // per input shard: padded slot rows (0 if skipped)
     std::vector<MergeGroup> merge_groups;
     std::vector<int32_t> merge_parts;       // slot row offsets, ascending shard order per group
+    std::vector<int32_t> merge_row_group;   // group of every row (shared prefixes only)
     std::vector<int32_t> merge_row_prefix;  // n_merge_groups+1 prefix sums of q_len
     std::vector<QGroup> q_groups;
     int64_t q_pad_total = 0;                // rows of the padded backward scratch arrays

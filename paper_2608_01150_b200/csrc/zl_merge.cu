@@ -168,13 +168,9 @@ __global__ void __launch_bounds__(128) zl_merge_rows_kernel(const MergeParams p,
     if (u >= n_rows * p.n_heads) return;
     const int64_t r = u / p.n_heads;
     const int h = (int)(u - r * p.n_heads);
-    int lo = 0, hi = p.n_groups;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.row_prefix[mid] <= r) lo = mid; else hi = mid;
-    }
-    const MergeGroup g = p.groups[lo];
-    const int row = (int)(r - p.row_prefix[lo]);
+    const int group = p.row_group[r];  // (a search would be a chain of dependent loads as long as the rest)
+    const MergeGroup g = p.groups[group];
+    const int row = (int)(r - p.row_prefix[group]);
     const int32_t* part = p.parts + g.part_begin;
     const float* lse_h = p.lse_partial + (int64_t)h * p.partial_rows + row;
     float M = -INFINITY;

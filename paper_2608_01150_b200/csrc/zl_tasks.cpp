@@ -541,6 +541,7 @@ zl_status build_prefix_schedule(const int32_t* cu_q, const int32_t* cu_kv, int32
             if (st != ZL_OK) return st;
         }
         mg.n_parts = (int32_t)s->merge_parts.size() - mg.part_begin;
+        s->merge_row_group.insert(s->merge_row_group.end(), ql, (int32_t)s->merge_groups.size());
         s->merge_groups.push_back(mg);
         s->merge_row_prefix.push_back(s->merge_row_prefix.back() + ql);
     }
