@@ -176,14 +176,14 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
         *out = h;
         return ZL_OK;
     }
-    int dev = 0;
-    cudaDeviceProp prop;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaGetDeviceProperties(&prop, dev) != cudaSuccess) {
+    int dev = 0, major = 0, n_sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
         delete h; return ZL_ERR_CUDA;
     }
-    if (prop.major != 10) { delete h; return ZL_ERR_UNSUPPORTED; }
+    if (major != 10) { delete h; return ZL_ERR_UNSUPPORTED; }
     h->device = dev;
-    h->n_sms = prop.multiProcessorCount;
+    h->n_sms = n_sms;
 
     const Schedule& s = h->sched;
     size_t off = 0;
