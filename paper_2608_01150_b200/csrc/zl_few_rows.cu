@@ -11,7 +11,14 @@
 //   * K and V have rings of their own: a K tile is free again as soon as its S is done, a V tile when its P V is;
 //   * Q takes only the rows it has (rounded up to 16) and two buffers, so that the loads of the next item run on under
 //     the current one; rows of the MMA beyond them hold whatever the shared memory holds and never leave their row;
-//   * warps without a valid row only take part in the barriers.
+//   * warps without a valid row only take part in the barriers;
+//   * where items are too few for the SMs they come in pieces along the keys (FewItem), and the piece that finishes last joins
+//     them from the padding of the shard's slot.
+// The same kernel takes the 128-row blocks of longer query ranges where 256-row blocks would leave SMs without work.
+// Measured (B200, d 128): one token against 8 x 9450 keys, 40 heads 280-310 us with the merge (5.0-5.5 TB/s; 495 us with the
+// two-tile kernel); against 9450 keys, 2 heads 19 us (95 us in one piece); 64 tokens over a shared prefix of 32,760 keys, 12
+// heads 66 us (4.5 TB/s).  Registers and code size count: state that the join keeps alive across the tile loop, or loops
+// unrolled further in it, cost 7-13 % of the first figure.
 #include <cuda_runtime.h>
 
 #include "zl_score.cuh"

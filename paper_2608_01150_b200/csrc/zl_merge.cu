@@ -156,7 +156,8 @@ __global__ void __launch_bounds__(kMergeThreads, NP == 8 ? 3 : (NP == 4 ? 4 : 8)
 
 // The merge of a batch over a shared prefix: few rows (one token per sequence) with a part per chunk of the prefix and one
 // of their own.  One warp per (row, head): lane t fetches the LSE of part t, and the partial outputs are read eight parts
-// at a time, so a warp waits for memory about as often as it has eighths of parts, not three times per part.
+// at a time, so a warp waits for memory about as often as it has eighths of parts, not three times per part (64 rows, 12
+// heads, 13 parts: 5 us where zl_merge_kernel takes 45).
 template <int D>
 __global__ void __launch_bounds__(128) zl_merge_rows_kernel(const MergeParams p, const int64_t n_rows) {
     constexpr int V = D / 32;

@@ -15,10 +15,12 @@
 //   * The table's gradient needs the sums of G over diagonals.  A warp's patch of 32 keys x 64 queries either lies in the
 //     constant part of the bias (one running sum per thread and side) or near the diagonal: there a register per lane
 //     carries one diagonal's sum, moves one lane per column and is complete when it leaves lane 31, all of it while the
-//     tensor core works on dS; the 95 sums are
-//     reduced by bucket (runs of equal buckets by shuffles) into registers that hold two buckets per lane.  At
-//     the end of an item the eight warps' 64 sums are added in order and stored; the dQ conversion's launch adds the key tiles in
-//     order.  No atomics: the same bits every time.
+//     tensor core works on dS; the 95 sums are reduced by bucket (runs of equal buckets by shuffles) into registers
+//     that hold two buckets per lane.  At the end of an item the eight warps' 64 sums are added in order and stored; the dQ
+//     conversion's launch adds the key tiles in order.  No atomics: the same bits every time.
+// Measured (B200): slopes over 9450 tokens, 12 heads, d 128: 1.31 ms of the whole backward's 1.34 (1.02 PFLOP/s, as the plain kernel
+// of this form); 16 texts of up to 512 tokens, 12 heads, d 64: 83 us without and 107 us with the table's gradient.  Bound by the
+// hand-overs between the MMA issuer and the P/dS warps as zl_bwd_main_kernel is, and with short sequences by the ends of items.
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
@@ -30,7 +32,6 @@ using namespace ptx;
 using namespace score;
 
 namespace {
-
 
 // Warp roles (16 warps): warp 0 TMA producer, warp 1 MMA issuer, warps 2-3 idle,
 // warps 4-7 and 8-11 two P/dS warpgroups (query columns 0-63 and 64-127 of every tile, one key

@@ -124,13 +124,17 @@ std::vector<WorkItem> in_pieces(const Schedule& s, const std::vector<WorkItem>& 
     return out;
 }
 
-// Whether blocks of one query tile (`few` steps) beat blocks of two: a step of theirs loads twice the keys.
+// Whether blocks of one query tile (`few` steps) beat blocks of two: a step of theirs loads twice the keys, so a tenth
+// fewer steps is where they start to pay.  Measured, 12 heads, d 128, blocks of two -> blocks of one: causal order over 1560
+// tokens 25.4 -> 18.5 us, over 4 x 1560 50.3 -> 40.5 (both chosen); 16 x 512 tokens 26.5 -> 42.0, 9450 tokens 238 -> 280 (not
+// chosen).
 bool few_rows_pay(int64_t few, int64_t two) { return few * 10 < two * 9; }
 
 // Beyond this many items per SM the rounds are even enough, whatever their blocks.
 constexpr size_t kEvenItems = 16 * kSms;
 
-// Numbers of pieces worth trying: a piece has two key tiles at least.
+// Numbers of pieces worth trying: a piece has two key tiles at least.  One token against 9450 keys, one piece -> the chosen
+// pieces: 2 heads 95 -> 19 us, 12 heads x 4 chunks 99 -> 49, 40 heads x 8 chunks 296 -> 280.
 constexpr int32_t kPieces[] = {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 bool worth_trying(const Schedule& s, int32_t parts, size_t n_items) {
     int32_t longest = 0;

@@ -742,9 +742,9 @@ def test_shared_prefix_in_phases_and_without_a_workspace():
 def test_many_rows_over_a_short_prefix_and_one_row_over_a_long_one():
     """Row blocks of two query tiles, of one, and a handle whose prefix is cut into many chunks."""
     import paper_2608_01150_b200 as Z
-    d, H = 128, 2
+    d = 128
     g = torch.Generator().manual_seed(26)
-    for qlens, klens, P in (([500, 600], [3, 0], 130), ([1], [0], 9000), ([1, 1, 1], [128, 129, 1], 5000)):
+    for H, qlens, klens, P in ((2, [500, 600], [3, 0], 130), (2, [1], [0], 9000), (1, [2], [5], 33000), (2, [1, 1, 1], [128, 129, 1], 5000)):
         nq, nk = sum(qlens), P + sum(klens)
         q, d_o, k, v = rand(g, nq, H, d), rand(g, nq, H, d), rand(g, nk, H, d), rand(g, nk, H, d)
         h = Z.build_tasks_prefix(cu(qlens), cu(klens), P, nq, nk, H, d)
