@@ -391,7 +391,8 @@ zl_few_rows_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (parts > 1) {
                 const int unit = again.x, head = again.y, rows = again.w & ((1 << kPartsShift) - 1);
                 const int slot = __ldcg(&p.tasks[unit].partial_slot);
-                // ---- the piece that finishes last joins all of them, in order (an even number of barrier phases either way): O = sum_s 2^(LSE_s - max) O_s / sum_s 2^(LSE_s - max)
+                // ---- the piece that finishes last joins all of them, in order (an even number of barrier phases either way):
+                //      O = sum_s 2^(LSE_s - max) O_s / sum_s 2^(LSE_s - max)
                 __threadfence();
                 mbar_arrive(&sm.part_bar);
                 ZL_WAIT_REGS(&sm.part_bar, 0, 29);  // this piece's rows are written and visible
