@@ -186,8 +186,9 @@ __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScorePa
                                              float& m_ref, float& l) {
     float mul = scale_log2, base = 0.f, step = 0.f;  // score(c) = sv[c] * mul + base + step * c, in powers of two
     float2 sum2 = make_float2(0.f, 0.f);
-    auto hand_over = [&](int h, const uint32_t (&pk)[kTileKV / 4]) {
-        tmem_st_x32(s_addr + h * 32, pk);
+    // Half h of P is on its way to TMEM; the first half is handed over some way into the second, when its store has landed.
+    constexpr int kLater = 16;  // columns of the second half
+    auto hand_over = [&](int h) {
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&p_half[h]);
@@ -213,6 +214,7 @@ __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScorePa
                     uint32_t pk[kTileKV / 4];
 #pragma unroll
                     for (int g = 0; g < kTileKV / 4; g += kGroup) {
+                        if (h == 1 && 2 * g == kLater) hand_over(0);
                         float2 y[kGroup], r[kGroup];
 #pragma unroll
                         for (int i = 0; i < kGroup; ++i) {
@@ -236,8 +238,9 @@ __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScorePa
                             pk[g + i] = pack_bf16(p0, p1);
                         }
                     }
-                    hand_over(h, pk);
+                    tmem_st_x32(s_addr + h * 32, pk);
                 }
+                hand_over(1);
                 l += sum2.x + sum2.y;
                 return;
             }
@@ -310,13 +313,15 @@ __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScorePa
 #pragma unroll
         for (int c = 0; c < kTileKV / 2; c += 2) {
             const int cc = h * (kTileKV / 2) + c;
+            if (h == 1 && c == kLater) hand_over(0);
             const float2 b = decltype(linear)::value ? make_float2(fmaf(step, (float)cc, add), fmaf(step, (float)(cc + 1), add)) : splat(add);
             const float2 e = fma2(make_float2(sv[cc], sv[cc + 1]), splat(mul), b);
             const float p0 = ex2(e.x), p1 = ex2(e.y);
             sum2 = add2(sum2, make_float2(p0, p1));
             pk[c / 2] = pack_bf16(p0, p1);
         }
-        hand_over(h, pk);
+        tmem_st_x32(s_addr + h * 32, pk);
+        if (h == 1) hand_over(1);
     };
     if (kBias && step != 0.f) {  // warp-uniform
         half_of_p(0, std::true_type());
