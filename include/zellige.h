@@ -169,8 +169,9 @@ zl_status zl_build_tasks_heads(const zl_whole_desc* whole, int32_t n_whole,
  *                [prefix_len + cu_kv[i], prefix_len + cu_kv[i+1]); its queries see the prefix rows [0, prefix_len)
  *                and its own keys.  Any of these lengths may be zero: a row without any key gets O = 0, LSE = -inf.
  * The handle is used like one of shards: zl_coalesced_attn_fwd, then zl_lse_merge (every row is a partial result
- * until the merge; o_partial / lse_partial as zl_tasks_info says), then any zl_coalesced_attn_bwd form.  dK and dV of the prefix are
- * summed over all sequences; own key rows of a sequence without queries are covered by no task and left untouched.
+ * until the merge; o_partial / lse_partial as zl_tasks_info says), then any zl_coalesced_attn_bwd form.  dK and dV of the
+ * prefix are summed over all sequences; own key rows of a sequence without queries are covered by no task and left
+ * untouched.
  * The prefix is cut into chunks along the keys so that few query rows (one token per sequence) still occupy the GPU.
  * Shard numbers (zl_tasks_get_partial_slot, zl_set_*_phases, zl_set_positions) are sequence numbers and mean the
  * part over the sequence's own keys; the chunks of the prefix run in launch phase 0 (results of phased launches agree with the
@@ -394,7 +395,8 @@ zl_status zl_set_positions(zl_tasks* tasks, const int32_t* whole_prefix, const z
 
 /* zl_scored_attn_fwd / _fwd_packed -- zl_coalesced_attn_fwd / _fwd_packed with scores as above; shard results are partial
  * and are joined by zl_lse_merge.  `score` is read during the call.  A query chunk whose keys all come later
- * gets an empty partial (O = 0, LSE = -inf). */
+ * gets an empty partial (O = 0, LSE = -inf).  Long key chunks under few query rows run in pieces that use the padding
+ * rows of the shard's slot (row_off + q_len .. row_off + rows_padded) as scratch. */
 zl_status zl_scored_attn_fwd(const zl_tasks* tasks, const zl_score* score, const void* q, const void* k, const void* v,
                              float scale, void* o, float* lse, float* o_partial, float* lse_partial, void* stream);
 zl_status zl_scored_attn_fwd_packed(const zl_tasks* tasks, const zl_score* score, const void* qkv, float scale,

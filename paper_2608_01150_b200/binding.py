@@ -169,6 +169,11 @@ def _stream_ptr(stream=None) -> int:
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _current_device() -> int:
+    import torch
+    return torch._C._cuda_getDevice()
+
+
 def _ptr(t) -> Optional[int]:
     if t is None:
         return None
@@ -461,8 +466,8 @@ class Score:
                 continue
             if name != "bucket_of" and t.shape[-1] != tasks.n_heads:
                 raise ZlError(1, f"Score: {name} has {t.shape[-1]} heads, the handle {tasks.n_heads}")
-            if not t.is_cuda:
-                raise ZlError(1, f"Score: {name} is not on a GPU")
+            if not t.is_cuda or t.get_device() != _current_device():
+                raise ZlError(1, f"Score: {name} is not on the current GPU")
 
 
 def relative_position_buckets(n_buckets: int, max_distance: int, bidirectional: bool = True) -> List[int]:
