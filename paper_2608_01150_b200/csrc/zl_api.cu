@@ -22,7 +22,8 @@ struct zl_tasks {
     uint8_t* d_tables = nullptr;  // one allocation holding every device table
     Task* d_tasks = nullptr;
     WorkItem* d_fwd_items = nullptr;
-    WorkItem* d_fwd_items_few = nullptr;
+    struct DeviceList { WorkItem* items = nullptr; int32_t* begin = nullptr; };
+    DeviceList d_fwd_all, d_bwd_all;  // schedule lists of the same names
     WorkItem* d_bwd_items = nullptr;
     WorkItem* d_bwd_pair_items = nullptr;
     int bwd_kernel = 0;           // 0: library default, 1: one CTA per key tile, 2: CTA pairs (head_dim 128)
@@ -39,10 +40,7 @@ struct zl_tasks {
     size_t n_part_count = 0;
     uint8_t* d_positions = nullptr;  // zl_set_positions: one allocation for the tables below, whose sizes never change
     TaskPos* d_task_pos = nullptr;
-    WorkItem* d_fwd_items_masked = nullptr;
-    WorkItem* d_bwd_items_masked = nullptr;
-    int32_t* d_fwd_lists = nullptr;
-    int32_t* d_bwd_lists = nullptr;
+    DeviceList d_fwd_masked, d_bwd_masked;
     // optional per-kernel event timing (measurement only)
     mutable bool timing = false;
     mutable std::vector<cudaEvent_t> ev_start[ZL_K_COUNT], ev_stop[ZL_K_COUNT];
@@ -189,7 +187,10 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     size_t off = 0;
     const size_t o_tasks = place<Task>(off, s.tasks.size());
     const size_t o_fwd = place<WorkItem>(off, s.fwd_items.size());
-    const size_t o_few = place<WorkItem>(off, s.fwd_items_few.size());
+    const size_t o_fa = place<WorkItem>(off, s.fwd_all.items.size());
+    const size_t o_fab = place<int32_t>(off, s.fwd_all.begin.size());
+    const size_t o_ba = place<WorkItem>(off, s.bwd_all.items.size());
+    const size_t o_bab = place<int32_t>(off, s.bwd_all.begin.size());
     const size_t o_bwd = place<WorkItem>(off, s.bwd_items.size());
     const size_t o_bwd2 = place<WorkItem>(off, s.bwd_pair_items.size());
     const size_t o_mg = place<MergeGroup>(off, s.merge_groups.size());
@@ -208,7 +209,10 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     auto put = [&](size_t at, const void* src, size_t bytes) { if (bytes) std::memcpy(host.data() + at, src, bytes); };
     put(o_tasks, s.tasks.data(), s.tasks.size() * sizeof(Task));
     put(o_fwd, s.fwd_items.data(), s.fwd_items.size() * sizeof(WorkItem));
-    put(o_few, s.fwd_items_few.data(), s.fwd_items_few.size() * sizeof(WorkItem));
+    put(o_fa, s.fwd_all.items.data(), s.fwd_all.items.size() * sizeof(WorkItem));
+    put(o_fab, s.fwd_all.begin.data(), s.fwd_all.begin.size() * sizeof(int32_t));
+    put(o_ba, s.bwd_all.items.data(), s.bwd_all.items.size() * sizeof(WorkItem));
+    put(o_bab, s.bwd_all.begin.data(), s.bwd_all.begin.size() * sizeof(int32_t));
     put(o_bwd, s.bwd_items.data(), s.bwd_items.size() * sizeof(WorkItem));
     put(o_bwd2, s.bwd_pair_items.data(), s.bwd_pair_items.size() * sizeof(WorkItem));
     put(o_mg, s.merge_groups.data(), s.merge_groups.size() * sizeof(MergeGroup));
@@ -228,7 +232,8 @@ zl_status upload_handle(zl_tasks* h, void* stream, zl_tasks** out) {
     }
     h->d_tasks = reinterpret_cast<Task*>(h->d_tables + o_tasks);
     h->d_fwd_items = reinterpret_cast<WorkItem*>(h->d_tables + o_fwd);
-    h->d_fwd_items_few = reinterpret_cast<WorkItem*>(h->d_tables + o_few);
+    h->d_fwd_all = {reinterpret_cast<WorkItem*>(h->d_tables + o_fa), reinterpret_cast<int32_t*>(h->d_tables + o_fab)};
+    h->d_bwd_all = {reinterpret_cast<WorkItem*>(h->d_tables + o_ba), reinterpret_cast<int32_t*>(h->d_tables + o_bab)};
     h->d_bwd_items = reinterpret_cast<WorkItem*>(h->d_tables + o_bwd);
     h->d_bwd_pair_items = reinterpret_cast<WorkItem*>(h->d_tables + o_bwd2);
     h->d_merge_groups = reinterpret_cast<MergeGroup*>(h->d_tables + o_mg);
@@ -491,17 +496,15 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     // blocks of longer query ranges where these are too few for the SMs; plain calls on handles without a shared
     // prefix keep the kernel (and the bits) they always had, and launch phases their lists.
     bool few = (score || s.shared_prefix) && s.max_item_rows <= kTileQ;
-    if (sp.masked && t->sm_margin == 0) {  // dealt out to as many CTAs as there are SMs; another grid takes the plain lists
-        p.items = t->d_fwd_items_masked;
-        p.n_items = (int32_t)s.fwd_items_masked.size();
-        p.lists = t->d_fwd_lists;
-        few = s.fwd_masked_few;
-    } else if ((score || s.shared_prefix) && phase < 0 && !s.fwd_items_few.empty()) {
-        p.items = t->d_fwd_items_few;
-        p.n_items = (int32_t)s.fwd_items_few.size();
-        few = true;
+    const DealtList& dealt = sp.masked ? s.fwd_masked : s.fwd_all;
+    if ((score || (s.shared_prefix && dealt.few)) && phase < 0 && !dealt.items.empty()) {
+        p.items = sp.masked ? t->d_fwd_masked.items : t->d_fwd_all.items;
+        // dealt out to every SM; with a margin, or at one item per CTA, the CTAs take the items in turn
+        p.lists = t->sm_margin > 0 || dealt.ctas() == (int32_t)dealt.items.size() ? nullptr : sp.masked ? t->d_fwd_masked.begin : t->d_fwd_all.begin;
+        p.n_items = (int32_t)dealt.items.size();
+        few = dealt.few;
     }
-    const int grid = p.lists ? t->n_sms : std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
+    const int grid = p.lists ? dealt.ctas() : std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
     const ScoreKind kind = score && score->biased ? kScoreBias : kScorePlain;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     CUtensorMap tq, tk, tv, to, top;
@@ -684,11 +687,6 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
             p.n_kv_tiles = s.n_kv_tiles;
         }
         p.zero_dq = !s.shared_prefix;
-        if (sp.masked && t->sm_margin == 0) {
-            p.items = t->d_bwd_items_masked;
-            p.n_items = (int32_t)s.bwd_items_masked.size();
-            p.lists = t->d_bwd_lists;
-        }
     }
 
     if (first) {
@@ -721,7 +719,12 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
         if (launch_bwd_pair(tq, tq64, tk, tv, tdo, tdo64, tdq16, taug, tdk32, tdv32, pp, n_clusters, cs) != cudaSuccess) return ZL_ERR_CUDA;
         g_launches.fetch_add(1);
     } else if (p.n_items > 0) {
-        const int grid = p.lists ? t->n_sms : std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
+        const DealtList& dealt = sp.masked ? s.bwd_masked : s.bwd_all;
+        if (scored && phase < 0 && t->sm_margin == 0 && !dealt.items.empty()) {
+            p.items = sp.masked ? t->d_bwd_masked.items : t->d_bwd_all.items;
+            p.lists = sp.masked ? t->d_bwd_masked.begin : t->d_bwd_all.begin;
+        }
+        const int grid = p.lists ? dealt.ctas() : std::min<int>(std::max(2, t->n_sms - t->sm_margin), p.n_items);
         LaunchTimer lt(t, ZL_K_BWD_MAIN, cs);
         if (scored) {
             const ScoreKind kind = !score || !score->biased ? kScorePlain : (d_bucket_bias ? kScoreBiasGrad : kScoreBias);
@@ -850,28 +853,26 @@ zl_status zl_set_positions(zl_tasks* t, const int32_t* whole_prefix, const zl_sh
         // no entry is left that the device does not have: a failure below takes the positions back
         size_t off = 0;
         const size_t o_pos = place<TaskPos>(off, s.task_pos.size());
-        const size_t o_fwd = place<WorkItem>(off, s.fwd_items_masked.size());
-        const size_t o_bwd = place<WorkItem>(off, s.bwd_items_masked.size());
-        const size_t o_fl = place<int32_t>(off, s.fwd_lists.size());
-        const size_t o_bl = place<int32_t>(off, s.bwd_lists.size());
+        const size_t o_fwd = place<WorkItem>(off, s.fwd_masked.items.size());
+        const size_t o_bwd = place<WorkItem>(off, s.bwd_masked.items.size());
+        const size_t o_fl = place<int32_t>(off, s.fwd_masked.begin.size());
+        const size_t o_bl = place<int32_t>(off, s.bwd_masked.begin.size());
         const size_t total = align_up(off, 256);
         std::vector<uint8_t> host(total, 0);
         auto put = [&](size_t at, const void* src, size_t bytes) { if (bytes) std::memcpy(host.data() + at, src, bytes); };
         put(o_pos, s.task_pos.data(), s.task_pos.size() * sizeof(TaskPos));
-        put(o_fwd, s.fwd_items_masked.data(), s.fwd_items_masked.size() * sizeof(WorkItem));
-        put(o_bwd, s.bwd_items_masked.data(), s.bwd_items_masked.size() * sizeof(WorkItem));
-        put(o_fl, s.fwd_lists.data(), s.fwd_lists.size() * sizeof(int32_t));
-        put(o_bl, s.bwd_lists.data(), s.bwd_lists.size() * sizeof(int32_t));
+        put(o_fwd, s.fwd_masked.items.data(), s.fwd_masked.items.size() * sizeof(WorkItem));
+        put(o_bwd, s.bwd_masked.items.data(), s.bwd_masked.items.size() * sizeof(WorkItem));
+        put(o_fl, s.fwd_masked.begin.data(), s.fwd_masked.begin.size() * sizeof(int32_t));
+        put(o_bl, s.bwd_masked.begin.data(), s.bwd_masked.begin.size() * sizeof(int32_t));
         if (!t->d_positions && cudaMalloc(&t->d_positions, total) != cudaSuccess) {
             t->d_positions = nullptr;
             s.task_pos.clear();
             return ZL_ERR_CUDA;
         }
         t->d_task_pos = reinterpret_cast<TaskPos*>(t->d_positions + o_pos);
-        t->d_fwd_items_masked = reinterpret_cast<WorkItem*>(t->d_positions + o_fwd);
-        t->d_bwd_items_masked = reinterpret_cast<WorkItem*>(t->d_positions + o_bwd);
-        t->d_fwd_lists = reinterpret_cast<int32_t*>(t->d_positions + o_fl);
-        t->d_bwd_lists = reinterpret_cast<int32_t*>(t->d_positions + o_bl);
+        t->d_fwd_masked = {reinterpret_cast<WorkItem*>(t->d_positions + o_fwd), reinterpret_cast<int32_t*>(t->d_positions + o_fl)};
+        t->d_bwd_masked = {reinterpret_cast<WorkItem*>(t->d_positions + o_bwd), reinterpret_cast<int32_t*>(t->d_positions + o_bl)};
         cudaStream_t cs = static_cast<cudaStream_t>(stream);
         if (cudaMemcpyAsync(t->d_positions, host.data(), total, cudaMemcpyHostToDevice, cs) != cudaSuccess ||
             cudaStreamSynchronize(cs) != cudaSuccess) {

@@ -94,6 +94,15 @@ struct InputTask {
     int32_t shard_idx;  // index into the caller's shard array, -1 for a whole sequence
 };
 
+// Work items dealt out to CTAs: CTA c walks items [begin[c], begin[c + 1]).
+struct DealtList {
+    std::vector<WorkItem> items;
+    std::vector<int32_t> begin;
+    bool few = false;   // forward: for the few-rows kernel (blocks of one query tile, or pieces along the keys)
+    int32_t parts = 0;  // forward: pieces along the keys; 0: blocks and pieces not chosen yet
+    int32_t ctas() const { return begin.empty() ? 0 : (int32_t)begin.size() - 1; }
+};
+
 // Everything zl_build_tasks derives from a placement, on the host.
 struct Schedule {
     int32_t n_heads = 0, head_dim = 0, total_q = 0, total_kv = 0;
@@ -116,16 +125,10 @@ struct Schedule {
     int32_t max_item_rows = 0;              // most query rows of a forward item
     bool all_heads = true;                  // every task covers all heads
     bool shared_prefix = false;             // built by build_prefix_schedule: query ranges nest
-    // Positions (zl_set_positions): one entry per task, and the work lists dealt out to the CTAs by what the mask leaves of
-    // each item: CTA c walks items [lists[c], lists[c + 1]).
+    // Lists of the scored kernels, dealt out to the CTAs: for calls without a mask (built with the handle, empty where
+    // the plain lists are as even) and, with the positions (one entry per task, zl_set_positions), for masked ones.
+    DealtList fwd_all, bwd_all, fwd_masked, bwd_masked;
     std::vector<TaskPos> task_pos;
-    std::vector<WorkItem> fwd_items_masked, bwd_items_masked;
-    std::vector<int32_t> fwd_lists, bwd_lists;
-    int32_t masked_parts = 0;  // pieces along the keys in fwd_items_masked; 0: not chosen yet
-    // Blocks of one query tile for the few-rows kernel, where they finish sooner than blocks of two, or items of few rows in
-    // pieces along the keys (empty: neither); fwd_masked_few says that fwd_items_masked is such a list.
-    std::vector<WorkItem> fwd_items_few;
-    bool fwd_masked_few = false;
     std::vector<KvGroup> kv_groups;
     std::vector<int32_t> kv_group_tasks;
     std::vector<WorkItem> fwd_items;

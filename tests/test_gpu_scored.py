@@ -346,6 +346,33 @@ def test_masked_calls_with_an_sm_margin():
         check_all(run, problems, s, q, k, v, d_o, d ** -0.5)
 
 
+@pytest.mark.parametrize("lens,chunks,H", [([700, 1, 300, 130], [], 3), ([60, 128, 5], [], 2), ([], [3000, 2000], 2)])
+def test_unmasked_calls_with_an_sm_margin(lens, chunks, H):
+    """Which CTA takes an item changes no bit of the forward: all SMs by dealt lists, few SMs in turn."""
+    import paper_2608_01150_b200 as Z
+    d, scale = 64, 0.125
+    g = torch.Generator().manual_seed(33)
+    rows, keys = (sum(lens), sum(lens)) if lens else (7, sum(chunks))
+    q, d_o = rand(g, rows, H, d), rand(g, rows, H, d)
+    k, v = rand(g, keys, H, d), rand(g, keys, H, d)
+    s = make_score(g, H, cap=20.0, buckets=8, reach=40)
+    if lens:
+        h = Z.build_tasks(cu(lens), [], rows, keys, H, d)
+        h.set_positions([0] * len(lens))
+        problems = whole_problems(lens, [0] * len(lens))
+    else:
+        h = Z.build_tasks([0], [(0, rows, sum(chunks[:i]), n, 0) for i, n in enumerate(chunks)], rows, keys, H, d)
+        h.set_positions(None, [(2900, sum(chunks[:i]), 0) for i in range(len(chunks))])
+        problems = [(torch.arange(rows), torch.arange(keys), 2900 + torch.arange(rows), torch.arange(keys), 0)]
+    run = Run(h, s, q, k, v, scale)
+    check_all(run, problems, s, q, k, v, d_o, scale)
+    o, lse = run.o.clone(), run.lse.clone()
+    for margin in (8, 145):
+        h.set_sm_margin(margin)
+        check_all(run, problems, s, q, k, v, d_o, scale)
+        assert torch.equal(run.o, o) and torch.equal(run.lse, lse)
+
+
 def test_rows_that_see_no_chunk_at_all():
     import paper_2608_01150_b200 as Z
     d, H, rows, K = 64, 2, 140, 300
