@@ -361,9 +361,11 @@ zl_status zl_coalesced_attn_bwd_noalloc(const zl_tasks* tasks, const void* q, co
  *     O = softmax(s) V,   LSE = log sum exp s   over the visible pairs; a row that sees no key gets O = 0, LSE = -inf.
  *
  *   cap           0 = no cap, otherwise 1e-4 to 1e6.
- *   slopes        device, [n_heads] fp32, finite, or NULL: a linear bias by distance.
+ *   slopes        device, [n_heads] fp32, of magnitude at most 1e18, or NULL: a linear bias by distance.
  *   bucket_bias   device, [n_buckets, n_heads] fp32, or NULL: a learned bias by buckets of the signed distance.  An
- *                 entry of -1e30 or less (-inf, the lowest finite value of a type) removes its pairs like a mask; other entries are finite.
+ *                 entry of -1e30 or less (-inf, the lowest finite value of a type) removes its pairs like a mask; other
+ *                 entries are of magnitude below 1e30.
+ * Scores and LSE are fp32: where a row's largest score is M, P carries M * 2^-23 as a relative error.
  *   bucket_of     device, [2 * max_distance + 1] int32: the bucket of every distance from -max_distance to
  *                 max_distance; farther pairs use the bucket of the clamped distance.  A number outside
  *                 [0, n_buckets) means no bias.

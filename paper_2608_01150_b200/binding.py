@@ -436,7 +436,7 @@ class Score:
     """zl_score: scores beyond ``scale * q.k``.
 
     cap          0 = none, else scores become ``cap * tanh(scale * q.k / cap)``
-    slopes       fp32 [n_heads]: ``- slope * |distance|``
+    slopes       fp32 [n_heads]: ``- slope * |distance|``, of magnitude at most 1e18
     bucket_bias  fp32 [n_buckets, n_heads]: learned bias, with
     bucket_of    int32 [2 * max_distance + 1]: the bucket of every distance key - query from -max_distance on
                  (see :func:`relative_position_buckets`)

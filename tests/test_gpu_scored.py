@@ -210,6 +210,40 @@ def test_bucket_entries_that_remove_pairs(value):
     assert (got["dtable"][:4, 0] == 0).all()
 
 
+@pytest.mark.parametrize("lens", [[300, 5], [1, 60, 128]])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("by", ["slopes", "table"])
+def test_largest_biases_leave_every_row_its_own_key(by, cap, lens):
+    """Biases at the documented limits outweigh every product: P is the identity, so O = V and dV = dO to the bit, and what is
+    left of dQ and dK is the rounding of dO.V - D (products of bf16 are exact, d additions each, D once more)."""
+    import paper_2608_01150_b200 as Z
+    d, H, scale, reach = 64, 2, 0.125, 3
+    g = torch.Generator().manual_seed(34)
+    T = sum(lens)
+    q, k, v, d_o = (rand(g, T, H, d) for _ in range(4))
+    s = dict(cap=cap, masked=False)
+    if by == "slopes":
+        s["slopes"] = torch.tensor([1e18, 1e6])
+    else:
+        s["table"] = torch.tensor([[-9e29, -1e6], [0.0, 0.0]])
+        s["bucket_of"] = (torch.arange(-reach, reach + 1) == 0).to(torch.int32)
+    h = Z.build_tasks(cu(lens), [], T, T, H, d)
+    run = Run(h, s, q, k, v, scale)
+    o, lse = run.forward()
+    assert torch.equal(o.cpu(), v)
+    x = (q.double() * k.double()).sum(-1) * scale
+    x = cap * torch.tanh(x / cap) if cap else x
+    assert (lse.cpu().double().T - x).abs().max() <= 1e-4  # |x| < 16: 2^-20 for each of a few roundings and the exponent's base
+    got = run.backward(d_o)
+    assert torch.equal(got["dv"].cpu(), d_o)
+    noise = (2 * d + 4) * 2.0 ** -23 * (d_o.double() * v.double()).abs().sum(-1, keepdim=True) * scale
+    for name, other in (("dq", k), ("dk", q)):
+        assert (got[name].cpu().double().abs() <= noise * other.double().abs() * 1.01 + 1e-30).all()
+    if by == "table":  # all of it in the diagonal's bucket
+        assert got["dtable"][0].abs().max() == 0
+        assert (got["dtable"][1].cpu().double().abs() <= noise.sum(0)[:, 0] / scale).all()
+
+
 def test_every_pair_removed_leaves_empty_rows():
     import paper_2608_01150_b200 as Z
     d, H, T = 128, 2, 140
