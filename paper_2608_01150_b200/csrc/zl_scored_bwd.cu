@@ -444,6 +444,13 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     float mul = p.scale_log2;
                     if constexpr (kCap) {
                         mul = 1.f;
+                        if (!tile_full) {
+                            // products with rows of other tasks, or of none: C' must not come from them (here finite rows give
+                            // +-inf at most, hence a C' of 0, but nothing promises that an overflowing sum is never NaN)
+#pragma unroll
+                            for (int c = 0; c < 64; ++c)
+                                if (c < col_lo || c >= col_hi) pr[c] = 0.f;
+                        }
                         float big = 0.f;
 #pragma unroll
                         for (int c = 0; c < 64; c += 2) big = max3_abs(big, pr[c], pr[c + 1]);

@@ -1,0 +1,66 @@
+"""Scored attention on the GPU where memory next to a task, numbers at their limits or several calls could reach results:
+against the definition in 64 bits, with the bounds of scored_ref."""
+import pytest
+import torch
+
+from test_gpu_scored import KINDS, Run, check_all, cu, make_score, rand, whole_problems
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------- neighbours
+def poison(x, rows, every):
+    """Huge finite values of both signs: products of two such rows overflow, their sums are NaN."""
+    big = torch.full(x.shape[1:], 3e38)
+    big.view(-1)[::every] *= -1
+    x[rows] = big.to(x.dtype)
+
+
+@pytest.mark.parametrize("kind", ["cap", "cap_mask", "slopes_mask", "all"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_finite_neighbours_of_whole_sequences_and_shards_cannot_leak(kind, d):
+    """Rows that no task owns, behind ragged sequences, shards and key chunks: tiles read them, results do not."""
+    import paper_2608_01150_b200 as Z
+    H, T = 2, 330
+    g = torch.Generator().manual_seed(41)
+    s = make_score(g, H, **KINDS[kind])
+    q, k, v, d_o = (rand(g, T, H, d) for _ in range(4))
+    owned_q = list(range(0, 230)) + list(range(240, 290))
+    owned_k = list(range(0, 230)) + list(range(240, 310))
+    for x in (q, d_o):
+        poison(x, [i for i in range(T) if i not in owned_q], 3)
+    for x in (k, v):
+        poison(x, [i for i in range(T) if i not in owned_k], 2)
+    h = Z.build_tasks([0, 100, 230], [(240, 50, 240, 70, 0)], T, T, H, d)
+    h.set_positions([3, 0], [(30, 0, 5)])
+    problems = whole_problems([100, 130], [3, 0])
+    problems.append((torch.arange(240, 290), torch.arange(240, 310), 30 + torch.arange(50), torch.arange(70), 5))
+    check_all(Run(h, s, q, k, v, d ** -0.5), problems, s, q, k, v, d_o, d ** -0.5)
+
+
+@pytest.mark.parametrize("s", [dict(cap=6.0), dict(cap=20.0, masked=True), dict(masked=True)])
+def test_finite_neighbours_of_a_shared_prefix_cannot_leak(s):
+    """Keys of a sequence without queries lie behind a ragged key tile whose ragged query tile reaches into the next
+    sequence: nothing of them arrives in any gradient."""
+    import paper_2608_01150_b200 as Z
+    d, H, P, qlens, klens = 128, 2, 520, [30, 0, 140], [50, 40, 140]
+    g = torch.Generator().manual_seed(42)
+    nq, nk = sum(qlens) + 20, P + sum(klens) + 20
+    q, d_o, k, v = rand(g, nq, H, d), rand(g, nq, H, d), rand(g, nk, H, d), rand(g, nk, H, d)
+    for x in (k, v):
+        poison(x, slice(P + 50, P + 90), 2)
+        poison(x, slice(P + sum(klens), nk), 2)
+    for x in (q, d_o):
+        poison(x, slice(sum(qlens), nq), 3)
+    h = Z.build_tasks_prefix(cu(qlens), cu(klens), P, nq, nk, H, d)
+    own = [(20, 0, 0), (0, 0, 0), (0, 0, 33)]
+    if s.get("masked"):
+        h.set_positions(shard_pos=own)
+    problems, qa, ka = [], 0, P
+    for ql, kl, (qp, kp, pre) in zip(qlens, klens, own):
+        if ql:
+            keys = torch.cat([torch.arange(P), torch.arange(ka, ka + kl)])
+            problems.append((torch.arange(qa, qa + ql), keys, P + qp + torch.arange(ql),
+                             torch.cat([torch.arange(P), P + kp + torch.arange(kl)]), P + pre))
+        qa, ka = qa + ql, ka + kl
+    check_all(Run(h, s, q, k, v, d ** -0.5), problems, s, q, k, v, d_o, d ** -0.5)
