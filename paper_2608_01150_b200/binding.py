@@ -442,25 +442,42 @@ class Score:
                  (see :func:`relative_position_buckets`)
     masked       prefix mask of ``TaskHandle.set_positions``
 
-    Holds references to its tensors; their values are read when a kernel runs.
+    The attributes can be changed, and their storage swapped (``module.to``): every call takes what they hold then.  Their
+    values are read when a kernel runs, so a captured call keeps the storage of its capture.
     """
 
     def __init__(self, cap: float = 0.0, slopes=None, bucket_bias=None, bucket_of=None, masked: bool = False):
-        import torch
-        for name, t, dtype, dims in (("slopes", slopes, torch.float32, 1), ("bucket_bias", bucket_bias, torch.float32, 2),
-                                     ("bucket_of", bucket_of, torch.int32, 1)):
-            if t is not None and (t.dtype != dtype or t.dim() != dims or not t.is_contiguous()):
-                raise ZlError(1, f"Score: {name} must be a contiguous {dtype} tensor of {dims} dimension(s)")
-        if (bucket_bias is None) != (bucket_of is None):
-            raise ZlError(1, "Score: bucket_bias and bucket_of come together")
-        if bucket_of is not None and bucket_of.numel() % 2 == 0:
-            raise ZlError(1, "Score: bucket_of has an entry for every distance from -max_distance to max_distance")
         self.cap, self.slopes, self.bucket_bias, self.bucket_of, self.masked = cap, slopes, bucket_bias, bucket_of, masked
-        self.desc = ScoreDesc(cap, _ptr(slopes), _ptr(bucket_bias), _ptr(bucket_of),
-                              0 if bucket_bias is None else bucket_bias.shape[0],
-                              0 if bucket_of is None else bucket_of.numel() // 2, 1 if masked else 0)
+        self.desc
 
-    def check(self, tasks: TaskHandle):
+    @property
+    def desc(self) -> ScoreDesc:
+        """The C struct of what the attributes hold now; raises where they do not fit."""
+        import torch
+        slopes, bias, of = self.slopes, self.bucket_bias, self.bucket_of
+        desc = ScoreDesc(self.cap, None, None, None, 0, 0, 1 if self.masked else 0)
+        if slopes is not None:
+            desc.slopes = self._address("slopes", slopes, torch.float32, 1)
+        if bias is not None or of is not None:
+            if bias is None or of is None:
+                raise ZlError(1, "Score: bucket_bias and bucket_of come together")
+            desc.bucket_bias = self._address("bucket_bias", bias, torch.float32, 2)
+            desc.bucket_of = self._address("bucket_of", of, torch.int32, 1)
+            desc.n_buckets, entries = bias.shape[0], of.shape[0]
+            if entries % 2 == 0:
+                raise ZlError(1, "Score: bucket_of has an entry for every distance from -max_distance to max_distance")
+            desc.max_distance = entries // 2
+        return desc
+
+    @staticmethod
+    def _address(name: str, t, dtype, dims: int) -> int:
+        if t.dtype != dtype or t.dim() != dims or not t.is_contiguous():
+            raise ZlError(1, f"Score: {name} must be a contiguous {dtype} tensor of {dims} dimension(s)")
+        return t.data_ptr()
+
+    def check(self, tasks: TaskHandle) -> ScoreDesc:
+        """The descriptor for a call on `tasks`."""
+        desc = self.desc
         for name, t in (("slopes", self.slopes), ("bucket_bias", self.bucket_bias), ("bucket_of", self.bucket_of)):
             if t is None:
                 continue
@@ -468,6 +485,7 @@ class Score:
                 raise ZlError(1, f"Score: {name} has {t.shape[-1]} heads, the handle {tasks.n_heads}")
             if not t.is_cuda or t.get_device() != _current_device():
                 raise ZlError(1, f"Score: {name} is not on the current GPU")
+        return desc
 
 
 def relative_position_buckets(n_buckets: int, max_distance: int, bidirectional: bool = True) -> List[int]:
@@ -505,8 +523,8 @@ def relative_position_buckets(n_buckets: int, max_distance: int, bidirectional: 
 def scored_attn_fwd(tasks: TaskHandle, score: Score, q, k, v, scale: float, o, lse, o_partial=None, lse_partial=None,
                     stream=None):
     """zl_scored_attn_fwd: coalesced_attn_fwd with capped, biased or masked scores."""
-    score.check(tasks)
-    _check(_lib.zl_scored_attn_fwd(tasks.ptr, ctypes.byref(score.desc), _ptr(q), _ptr(k), _ptr(v), ctypes.c_float(scale),
+    desc = score.check(tasks)
+    _check(_lib.zl_scored_attn_fwd(tasks.ptr, ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), ctypes.c_float(scale),
                                    _ptr(o), _ptr(lse), _ptr(o_partial), _ptr(lse_partial), _stream_ptr(stream)),
            "zl_scored_attn_fwd")
 
@@ -514,8 +532,8 @@ def scored_attn_fwd(tasks: TaskHandle, score: Score, q, k, v, scale: float, o, l
 def scored_attn_fwd_packed(tasks: TaskHandle, score: Score, qkv, scale: float, o, lse, o_partial=None, lse_partial=None,
                            stream=None):
     """zl_scored_attn_fwd_packed: qkv is [T, 3, H, d] bf16."""
-    score.check(tasks)
-    _check(_lib.zl_scored_attn_fwd_packed(tasks.ptr, ctypes.byref(score.desc), _ptr(qkv), ctypes.c_float(scale), _ptr(o),
+    desc = score.check(tasks)
+    _check(_lib.zl_scored_attn_fwd_packed(tasks.ptr, ctypes.byref(desc), _ptr(qkv), ctypes.c_float(scale), _ptr(o),
                                           _ptr(lse), _ptr(o_partial), _ptr(lse_partial), _stream_ptr(stream)),
            "zl_scored_attn_fwd_packed")
 
@@ -530,11 +548,11 @@ def _check_table(score: Score, d_bucket_bias):
 def scored_attn_bwd(tasks: TaskHandle, score: Score, q, k, v, o, lse, d_o, scale: float, dq, dk, dv, d_bucket_bias,
                     workspace, workspace_bytes: Optional[int] = None, stream=None):
     """zl_scored_attn_bwd.  d_bucket_bias: fp32 [n_buckets, n_heads] or None."""
-    score.check(tasks)
+    desc = score.check(tasks)
     _check_table(score, d_bucket_bias)
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
-    _check(_lib.zl_scored_attn_bwd(tasks.ptr, ctypes.byref(score.desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
+    _check(_lib.zl_scored_attn_bwd(tasks.ptr, ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
                                    _ptr(d_o), ctypes.c_float(scale), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_bucket_bias),
                                    _ptr(workspace), ctypes.c_size_t(workspace_bytes), _stream_ptr(stream)),
            "zl_scored_attn_bwd")
@@ -543,11 +561,11 @@ def scored_attn_bwd(tasks: TaskHandle, score: Score, q, k, v, o, lse, d_o, scale
 def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, scale: float, dqkv, d_bucket_bias,
                            workspace, workspace_bytes: Optional[int] = None, stream=None):
     """zl_scored_attn_bwd_packed: reads qkv [T, 3, H, d], writes dqkv [T, 3, H, d]."""
-    score.check(tasks)
+    desc = score.check(tasks)
     _check_table(score, d_bucket_bias)
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
-    _check(_lib.zl_scored_attn_bwd_packed(tasks.ptr, ctypes.byref(score.desc), _ptr(qkv), _ptr(o), _ptr(lse), _ptr(d_o),
+    _check(_lib.zl_scored_attn_bwd_packed(tasks.ptr, ctypes.byref(desc), _ptr(qkv), _ptr(o), _ptr(lse), _ptr(d_o),
                                           ctypes.c_float(scale), _ptr(dqkv), _ptr(d_bucket_bias), _ptr(workspace),
                                           ctypes.c_size_t(workspace_bytes), _stream_ptr(stream)),
            "zl_scored_attn_bwd_packed")

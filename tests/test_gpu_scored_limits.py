@@ -64,3 +64,25 @@ def test_finite_neighbours_of_a_shared_prefix_cannot_leak(s):
                              torch.cat([torch.arange(P), P + kp + torch.arange(kl)]), P + pre))
         qa, ka = qa + ql, ka + kl
     check_all(Run(h, s, q, k, v, d ** -0.5), problems, s, q, k, v, d_o, d ** -0.5)
+
+
+# ------------------------------------------------------------------------------------------------- calls
+def test_a_score_made_before_its_module_moves():
+    """Made on the CPU, moved, given another table, a cap and a mask later: each call takes what is there."""
+    import paper_2608_01150_b200 as Z
+    d, H, T = 64, 2, 150
+    g = torch.Generator().manual_seed(43)
+    s = make_score(g, H, **KINDS["all"])
+    q, k, v, d_o = (rand(g, T, H, d) for _ in range(4))
+    h = Z.build_tasks([0, T], [], T, T, H, d)
+    h.set_positions([4])
+    run = Run(h, s, q, k, v, d ** -0.5)
+    module = torch.nn.Module()
+    module.slopes, module.table = torch.nn.Parameter(s["slopes"].clone()), torch.nn.Parameter(s["table"].clone())
+    run.score = Z.Score(slopes=module.slopes, bucket_bias=module.table, bucket_of=s["bucket_of"].cuda())
+    module.cuda()
+    run.score.cap, run.score.masked = s["cap"], True
+    check_all(run, whole_problems([T], [4]), s, q, k, v, d_o, d ** -0.5)
+    s["table"] = torch.randn(40, H, generator=g)
+    module.table.data = s["table"].cuda()
+    check_all(run, whole_problems([T], [4]), s, q, k, v, d_o, d ** -0.5)
