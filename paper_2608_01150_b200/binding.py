@@ -543,6 +543,8 @@ def _check_table(score: Score, d_bucket_bias):
     if d_bucket_bias is not None and t is not None and not isinstance(d_bucket_bias, int):
         if d_bucket_bias.shape != t.shape or d_bucket_bias.dtype != t.dtype or not d_bucket_bias.is_contiguous():
             raise ZlError(1, "d_bucket_bias must be contiguous and of bucket_bias' shape and type")
+        if not d_bucket_bias.is_cuda or d_bucket_bias.get_device() != _current_device():
+            raise ZlError(1, "d_bucket_bias is not on the current GPU")
 
 
 def scored_attn_bwd(tasks: TaskHandle, score: Score, q, k, v, o, lse, d_o, scale: float, dq, dk, dv, d_bucket_bias,

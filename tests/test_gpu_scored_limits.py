@@ -86,3 +86,17 @@ def test_a_score_made_before_its_module_moves():
     s["table"] = torch.randn(40, H, generator=g)
     module.table.data = s["table"].cuda()
     check_all(run, whole_problems([T], [4]), s, q, k, v, d_o, d ** -0.5)
+
+
+def test_a_table_gradient_on_the_host_is_refused():
+    import paper_2608_01150_b200 as Z
+    h = Z.build_tasks([0, 10], [], 10, 10, 2, 64)
+    x, lse = torch.zeros(10, 2, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 10, device="cuda")
+    s = Z.Score(bucket_bias=torch.zeros(3, 2, device="cuda"), bucket_of=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    ws = torch.zeros(h.scored_workspace_bytes(s), dtype=torch.uint8, device="cuda")
+    for packed in (False, True):
+        args = (torch.zeros(10, 3, 2, 64, dtype=torch.bfloat16, device="cuda"),) if packed else (x, x, x)
+        fn = Z.scored_attn_bwd_packed if packed else Z.scored_attn_bwd
+        with pytest.raises(Z.ZlError) as e:
+            fn(h, s, *args, x, lse, x, 1.0, *(torch.zeros_like(a) for a in args), torch.zeros(3, 2), ws)
+        assert e.value.status == 1

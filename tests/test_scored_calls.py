@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2608_01150_b200 as Z
+from paper_2608_01150_b200 import binding as B
 
 
 # ---------------------------------------------------------------------------------------------- a Score follows its attributes
@@ -51,3 +52,13 @@ def test_a_score_with_unfit_attributes_is_refused_at_the_call(name, value):
     with pytest.raises(Z.ZlError) as e:
         Z.scored_attn_fwd(h, s, 0, 0, 0, 1.0, 0, 0)
     assert e.value.status == 1
+
+
+def test_a_table_gradient_that_is_not_on_the_gpu_is_refused():
+    """It is written by a kernel; shape, type and layout alone do not make its address one that a kernel can use."""
+    s = Z.Score(**buckets(4, 3, 2))
+    with pytest.raises(Z.ZlError) as e:
+        B._check_table(s, torch.zeros(4, 3))
+    assert e.value.status == 1 and "GPU" in str(e.value)
+    B._check_table(s, None)
+    B._check_table(s, 4096)      # raw addresses are the caller's word, as everywhere in the binding
