@@ -424,7 +424,7 @@ zl_status check_score(const zl_tasks* t, const zl_score* score, CheckedScore* ou
     out->biased = score->slopes || score->bucket_bias;
     out->any = out->capped || out->biased || score->masked;
     if (out->biased && s.shared_prefix) return ZL_ERR_UNSUPPORTED;  // a prefix key's distance differs by sequence
-    if (out->biased && !s.shard_to_task.empty() && s.task_pos.empty()) return ZL_ERR_INVALID_ARG;
+    if (out->biased && !s.shard_to_task.empty() && s.task_pos.empty() && !s.tasks.empty()) return ZL_ERR_INVALID_ARG;
     if (score->masked && s.task_pos.empty() && !s.tasks.empty()) return ZL_ERR_INVALID_ARG;
     ScoreParams& p = out->params;
     p.pos = s.task_pos.empty() ? nullptr : t->d_task_pos;

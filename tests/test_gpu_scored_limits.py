@@ -3,7 +3,7 @@ against the definition in 64 bits, with the bounds of scored_ref."""
 import pytest
 import torch
 
-from test_gpu_scored import KINDS, Run, check_all, cu, make_score, rand, whole_problems
+from test_gpu_scored import KINDS, Run, check_all, cu, make_score, rand, status_ok, whole_problems
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +100,19 @@ def test_a_table_gradient_on_the_host_is_refused():
         with pytest.raises(Z.ZlError) as e:
             fn(h, s, *args, x, lse, x, 1.0, *(torch.zeros_like(a) for a in args), torch.zeros(3, 2), ws)
         assert e.value.status == 1
+
+
+@pytest.mark.parametrize("cu_seqlens,shards", [([0], [(0, 0, 0, 10, 0)]), ([0, 0], [])])
+def test_the_table_gradient_of_a_handle_without_queries_is_zero(cu_seqlens, shards):
+    """A rank without query rows adds nothing to the sum over ranks."""
+    import paper_2608_01150_b200 as Z
+    h = Z.build_tasks(cu_seqlens, shards, 0, 10, 2, 64)
+    x = torch.zeros(10, 2, 64, dtype=torch.bfloat16, device="cuda")
+    none, lse = x[:0], torch.zeros(2, 0, device="cuda")
+    s = Z.Score(bucket_bias=torch.ones(3, 2, device="cuda"), bucket_of=torch.zeros(3, dtype=torch.int32, device="cuda"))
+    ws = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    dt = torch.full((3, 2), 7.0, device="cuda")
+    Z.scored_attn_fwd(h, s, none, x, x, 1.0, none, lse)
+    Z.scored_attn_bwd(h, s, none, x, x, none, lse, none, 1.0, none, torch.zeros_like(x), torch.zeros_like(x), dt, ws)
+    status_ok(h)
+    assert (dt == 0).all()

@@ -1,4 +1,6 @@
 """What the binding and the library make of a scored call's arguments, without a GPU."""
+import ctypes
+
 import pytest
 import torch
 
@@ -62,3 +64,22 @@ def test_a_table_gradient_that_is_not_on_the_gpu_is_refused():
     assert e.value.status == 1 and "GPU" in str(e.value)
     B._check_table(s, None)
     B._check_table(s, 4096)      # raw addresses are the caller's word, as everywhere in the binding
+
+
+# ---------------------------------------------------------------------------------------------- handles without work
+@pytest.mark.parametrize("cu,shards", [([0], [(0, 0, 0, 10, 0)]), ([0], [(0, 0, 0, 10, 0), (0, 0, 0, 0, 1)]), ([0, 0], [(0, 0, 0, 4, 0)])])
+@pytest.mark.parametrize("placed", [False, True])
+def test_every_score_is_accepted_where_no_shard_has_queries(cu, shards, placed):
+    """A rank without query rows makes the same calls as the others."""
+    h = Z.build_tasks(cu, shards, 0, 10, 2, 64)
+    assert h.info.n_tasks == 0
+    if placed:
+        h.set_positions([0] * (len(cu) - 1), [(0, 0, 0)] * len(shards))
+    for kw in (dict(masked=1), dict(cap=3.0), dict(slopes=16), dict(bucket_bias=16, bucket_of=16, n_buckets=4, max_distance=2),
+               dict(cap=3.0, slopes=16, masked=1)):
+        desc = ctypes.byref(B.ScoreDesc(**kw))
+        assert B.lib().zl_scored_attn_fwd(h.ptr, desc, None, 16, 16, ctypes.c_float(1.0), None, None, None, None, None) == 0, kw
+        n = ctypes.c_size_t(1)
+        assert B.lib().zl_scored_workspace_bytes(h.ptr, desc, ctypes.byref(n)) == 0 and n.value == 0, kw
+        assert B.lib().zl_scored_attn_bwd(h.ptr, desc, None, 16, 16, None, None, None, ctypes.c_float(1.0), None, 16, 16, None,
+                                          None, 0, None) == 0, kw
