@@ -365,7 +365,9 @@ zl_status zl_coalesced_attn_bwd_noalloc(const zl_tasks* tasks, const void* q, co
  *   bucket_bias   device, [n_buckets, n_heads] fp32, or NULL: a learned bias by buckets of the signed distance.  An
  *                 entry of -1e30 or less (-inf, the lowest finite value of a type) removes its pairs like a mask; other
  *                 entries are of magnitude below 1e30.
- * Scores and LSE are fp32: where a row's largest score is M, P carries M * 2^-23 as a relative error.
+ * Scores and LSE are fp32: a pair's P carries a few 2^-24 of |scale * q.k|, of its bias and of its row's LSE as a relative
+ * error.  A capped score is off by at most 2^-20 of its own magnitude, whatever other rows hold; C' in the backward is off
+ * by at most 2^-10 of its value or 2^-19, whichever is more.
  *   bucket_of     device, [2 * max_distance + 1] int32: the bucket of every distance from -max_distance to
  *                 max_distance; farther pairs use the bucket of the clamped distance.  A number outside
  *                 [0, n_buckets) means no bias.

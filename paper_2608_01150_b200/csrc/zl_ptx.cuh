@@ -310,6 +310,12 @@ __device__ __forceinline__ float max3_abs(float a, float b, float c) {
     asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
+// a clamped to [-end, end], end > 0; NaN stays NaN.
+__device__ __forceinline__ float clamp_abs(float a, float end) {
+    float d;
+    asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(end));
+    return d;
+}
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     uint64_t ra, rb, rc, rd;
     asm("mov.b64 %0, {%1, %2};" : "=l"(ra) : "f"(a.x), "f"(a.y));

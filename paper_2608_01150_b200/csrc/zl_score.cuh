@@ -35,10 +35,12 @@ __device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_
 }
 
 // ------------------------------------------------------------------------------------------------ cap
-// tanh(y) / y as a polynomial in y^2 for |y| <= kTanhRange: fitted by iterated reweighted least squares on 4,000
-// Chebyshev nodes, largest relative error 7e-8.  Five multiply-adds in packed fp32 instead of two special-function
-// operations (exponential and reciprocal) per score: the special-function unit gives 16 results a clock and SM and
-// already computes the softmax's exponentials (forward over 9450 tokens, 12 heads, d 128: 600 us against 1,000).
+// A capped score is off by at most 2^-20 of its own magnitude: 4e-7 of the tanh itself (below), and the roundings of the factors
+// around it.  Two forms of the tanh:
+// Near zero: tanh(y) / y as a polynomial in y^2 for |y| <= kTanhRange, fitted by iterated reweighted least squares on 4,000
+// Chebyshev nodes, largest relative error 7e-8.  Five multiply-adds in packed fp32 and no special-function operation: that
+// unit gives 16 results a clock and SM and already computes the softmax's exponentials (forward over 9450 tokens, 12
+// heads, d 128: 600 us against 1,000 with exponential and reciprocal for every tanh).
 constexpr float kTanhRange = 0.6f;
 constexpr float kTanhC0 = 0.9999999307553031f, kTanhC1 = -0.3333234430833674f, kTanhC2 = 0.13310648814868545f,
                 kTanhC3 = -0.052122548544318484f, kTanhC4 = 0.015504640407993653f;
@@ -54,9 +56,29 @@ __device__ __forceinline__ float2 tanh_near(float2 y) {
     r = fma2(z, r, splat(kTanhC0));
     return mul2(y, r);
 }
-// tanh of any y, as 1 - 2 / (exp(2y) + 1): absolute error about 1e-7, exact limits at +-inf.
-__device__ __forceinline__ float tanh_any(float y) {
+// |y| > kTanhRange, for the backward, whose C' = 1 - tanh^2 wants small absolute errors near 1: 1 - 2 / (exp(2y) + 1), with
+// exact limits at +-inf.
+__device__ __forceinline__ float tanh_far(float y) {
     return 1.f - 2.f * rcp(ex2(y * (2.f * kLog2e)) + 1.f);
+}
+// Any y: tanh(y) / y = P(y^2) / Q(y^2) for |y| <= kTanhEnd, fitted the same way (largest relative error 1.5e-7, 4.3e-7 as
+// evaluated); beyond, tanh is 1 to 2.3e-7.  1 - 2 / (exp(2y) + 1) would be right for large y only: near 0 its difference
+// cancels, and a tile that saturates in one row may be small in the next.  One special-function operation per score instead
+// of two: saturating scores of 1560 + 1560 + 3600 tokens 274 -> 261 us (12 heads, d 128).
+constexpr float kTanhEnd = 8.f;
+constexpr float kTanhP0 = 0.999999854f, kTanhP1 = 0.12925662f, kTanhP2 = 0.00295102275f, kTanhP3 = 1.14284123e-05f;
+constexpr float kTanhQ1 = 0.462588777f, kTanhQ2 = 0.02381555f, kTanhQ3 = 0.000238669022f, kTanhQ4 = 2.45920737e-07f;
+__device__ __forceinline__ float2 tanh_all(float2 y, float times) {  // times * tanh
+    y = make_float2(clamp_abs(y.x, kTanhEnd), clamp_abs(y.y, kTanhEnd));
+    const float2 z = mul2(y, y);
+    float2 n = fma2(z, splat(kTanhP3), splat(kTanhP2));
+    n = fma2(z, n, splat(kTanhP1));
+    n = fma2(z, n, splat(kTanhP0));
+    float2 q = fma2(z, splat(kTanhQ4), splat(kTanhQ3));
+    q = fma2(z, q, splat(kTanhQ2));
+    q = fma2(z, q, splat(kTanhQ1));
+    q = fma2(z, q, splat(1.f));
+    return mul2(mul2(y, n), mul2(make_float2(rcp(q.x), rcp(q.y)), splat(times)));  // (products with `times` ahead would stay in registers)
 }
 
 // ------------------------------------------------------------------------------------------------ bias by distance
@@ -256,7 +278,11 @@ __device__ __forceinline__ void softmax_tile(float (&sv)[kTileKV], const ScorePa
             }
         } else {
 #pragma unroll
-            for (int c = 0; c < kTileKV; ++c) sv[c] = tanh_any(sv[c] * sp.scale_over_cap) * sp.cap_log2;
+            for (int c = 0; c < kTileKV; c += 2) {
+                const float2 v = tanh_all(mul2(make_float2(sv[c], sv[c + 1]), k1), sp.cap_log2);
+                sv[c] = v.x;
+                sv[c + 1] = v.y;
+            }
         }
     }
     if constexpr (kBias) {

@@ -424,7 +424,9 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     if constexpr (kCap) ZL_WAIT_REGS(&sm.q_full[stage], (it_cnt >> 1) & 1, 26);  // the LSE came with Q: already complete
                     tc_fence_after();
                     float pr[64];        // P of this thread's key row, fp32
-                    uint32_t slope[32];  // C' of the capped scores, pairs of fp16 (off by at most 2^-11 of the value)
+                    // C' of the capped scores, pairs of fp16: off by at most 2^-11 of the value down to 2^-14, by 2^-25 below.  There 1 - tanh^2 in
+                    // fp32 holds no more: it carries twice the error of the tanh, some 2^-21 near 1
+                    uint32_t slope[32];
                     {
                         uint32_t sr[2][32];
                         tmem_ld_x32(lane_addr + kColS + col0, sr[0]);
@@ -456,15 +458,28 @@ zl_scored_bwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         for (int c = 0; c < 64; c += 2) big = max3_abs(big, pr[c], pr[c + 1]);
                         const float2 k1 = splat(sp.scale_over_cap), cl = splat(sp.cap_log2);
                         const float4* lse4 = reinterpret_cast<const float4*>(sm.lse[stage] + col0);
-                        const bool near_zero = __all_sync(0xffffffffu, big * sp.scale_over_cap <= kTanhRange);
+                        if (__all_sync(0xffffffffu, big * sp.scale_over_cap <= kTanhRange)) {
+#pragma unroll
+                            for (int c = 0; c < 64; c += 2) {
+                                const float2 th = tanh_near(mul2(make_float2(pr[c], pr[c + 1]), k1));
+                                pr[c] = th.x;
+                                pr[c + 1] = th.y;
+                            }
+                        } else {  // each product in the form that fits it: a warp's may be small in one row and saturate in another
+#pragma unroll
+                            for (int c = 0; c < 64; c += 2) {
+                                const float2 y = mul2(make_float2(pr[c], pr[c + 1]), k1);
+                                const float2 th = tanh_near(y);
+                                pr[c] = fabsf(y.x) <= kTanhRange ? th.x : tanh_far(y.x);
+                                pr[c + 1] = fabsf(y.y) <= kTanhRange ? th.y : tanh_far(y.y);
+                            }
+                        }
 #pragma unroll
                         for (int c = 0; c < 64; c += 4) {
                             const float4 ls = lse4[c / 4];
 #pragma unroll
                             for (int e = 0; e < 4; e += 2) {
-                                float2 th = mul2(make_float2(pr[c + e], pr[c + e + 1]), k1);
-                                if (near_zero) th = tanh_near(th);
-                                else th = make_float2(tanh_any(th.x), tanh_any(th.y));
+                                float2 th = make_float2(pr[c + e], pr[c + e + 1]);
                                 const float2 cp = fma2(make_float2(-th.x, -th.y), th, splat(1.f));
                                 const __half2 h2 = __floats2half2_rn(cp.x, cp.y);
                                 slope[(c + e) / 2] = *reinterpret_cast<const uint32_t*>(&h2);

@@ -3,6 +3,7 @@ against the definition in 64 bits, with the bounds of scored_ref."""
 import pytest
 import torch
 
+import scored_ref as R
 from test_gpu_scored import KINDS, Run, check_all, cu, make_score, rand, status_ok, whole_problems
 
 pytestmark = pytest.mark.gpu
@@ -116,3 +117,53 @@ def test_the_table_gradient_of_a_handle_without_queries_is_zero(cu_seqlens, shar
     Z.scored_attn_bwd(h, s, none, x, x, none, lse, none, 1.0, none, torch.zeros_like(x), torch.zeros_like(x), dt, ws)
     status_ok(h)
     assert (dt == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------- the cap's accuracy
+def tight_scores(qh, kh, qpos, kpos, prefix, scale, cap=0.0, **kw):
+    """scored_ref.scores with the header's bound on a capped score: 2^-20 of its own magnitude, whatever the cap and
+    whatever other rows hold (scored_ref allows 2^-20 of the cap)."""
+    s, slope, bucket, es = loose_scores(qh, kh, qpos, kpos, prefix, scale, cap=cap, **kw)
+    capped = cap * torch.tanh(scale * (qh @ kh.T) / cap)
+    return s, slope, bucket, es + 2.0 ** -20 * (capped.abs() - cap)
+
+
+loose_scores = R.scores
+
+
+@pytest.mark.parametrize("cap", [50.0, 1e3, 1e6])
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("L,d", [(160, 64), (100, 128)])
+def test_small_scores_beside_saturating_ones(L, d, slopes, cap, monkeypatch):
+    """Every third query saturates the cap, in the same warps (and, backward, in the same registers) as queries whose scores are
+    near zero: those keep their accuracy.  The saturating queries get no gradient of their own, so that dK and dV are the
+    others'."""
+    import paper_2608_01150_b200 as Z
+    monkeypatch.setattr(R, "scores", tight_scores)
+    H = 2
+    g = torch.Generator().manual_seed(44)
+    q, k, v, d_o = (rand(g, L, H, d) for _ in range(4))
+    q[::3] = (q[::3].float() * cap).to(q.dtype)
+    d_o[::3] = 0
+    s = make_score(g, H, cap=cap, slopes=slopes)
+    h = Z.build_tasks([0, L], [], L, L, H, d)
+    check_all(Run(h, s, q, k, v, d ** -0.5), whole_problems([L], [0]), s, q, k, v, d_o, d ** -0.5)
+
+
+@pytest.mark.parametrize("cap,slopes", [(0.5, False), (50.0, False), (0.5, True)])
+def test_a_query_of_nan_stays_its_own_and_stays_nan(cap, slopes):
+    """No clamp or maximum turns it into a number, and no other row of its warp notices."""
+    import paper_2608_01150_b200 as Z
+    d, H, L = 64, 2, 200
+    g = torch.Generator().manual_seed(45)
+    q, k, v = rand(g, L, H, d, times=2.0), rand(g, L, H, d), rand(g, L, H, d)
+    s = make_score(g, H, cap=cap, slopes=slopes)
+    h = Z.build_tasks([0, L], [], L, L, H, d)
+    q[70, 1] = float("nan")
+    o, lse = Run(h, s, q, k, v, d ** -0.5).forward()
+    assert o[70, 1].isnan().all()
+    f = R.forward(whole_problems([L], [0]), torch.nan_to_num(q), k, v, d ** -0.5, s)
+    rows = [i for i in range(L) if i != 70]
+    R.check(o.cpu()[rows], {"o": f["o"][rows], "o_err": f["o_err"][rows]}, "o")
+    R.check(lse.cpu()[:, rows], {"lse": f["lse"][:, rows], "lse_err": f["lse_err"][:, rows]}, "lse")
+    assert not o[70, 0].isnan().any()
