@@ -111,12 +111,14 @@ int64_t item_steps(const Schedule& s, const WorkItem& w, bool few, bool masked) 
     return (few ? (tiles + 1) / 2 : tiles) + kItemSteps;
 }
 
-// `items` (of one row block each) in up to `parts` pieces along the keys, as many as their slots have room for.
+// Of up to `parts` pieces along the keys, as many as the task's slot has room for.
+int32_t pieces(const Task& t, int32_t parts) { return parts < 2 || t.partial_slot < 0 ? 1 : std::min(parts, kTileQ / t.q_len); }
+
+// `items` (of one row block each) in up to `parts` pieces along the keys.
 std::vector<WorkItem> in_pieces(const Schedule& s, const std::vector<WorkItem>& items, int32_t parts) {
     std::vector<WorkItem> out;
     for (const WorkItem& w : items) {
-        const Task& t = s.tasks[w.unit];
-        const int32_t n = t.partial_slot < 0 ? 1 : std::min(parts, kTileQ / t.q_len);
+        const int32_t n = pieces(s.tasks[w.unit], parts);
         if (n < 2) { out.push_back(w); continue; }
         for (int32_t i = 0; i < n; ++i) out.push_back({w.unit, w.head, i, w.rows | (n << kPartsShift)});
     }
@@ -146,36 +148,77 @@ bool worth_trying(const Schedule& s, int32_t parts, size_t n_items) {
 // with the least work so far; one CTA per SM, or per item where there are fewer.  Returns the most steps of a CTA.
 // Walking in turn -> dealt: causal order over 9450 tokens 286 -> 247 us; without a mask, 16 texts of up to 512 tokens, 12
 // heads, 31.9 -> 30.5 us, gradients of 8 continuations of a shared prefix 167 -> 159 us.
+// Every handle pays for this, so it takes constant time per item: items are sorted by counting, and as the least load never
+// falls, the CTAs wait in queues by their load, of which the first that is not empty only moves up.
 int64_t deal(const std::vector<WorkItem>& items, const std::vector<int64_t>& steps, int32_t n_sms, DealtList* out) {
-    const int32_t ctas = (int32_t)std::min<size_t>(n_sms, items.size());
-    std::vector<int32_t> order(items.size()), owner(items.size());
-    for (size_t i = 0; i < order.size(); ++i) order[i] = (int32_t)i;
-    if (!std::is_sorted(steps.rbegin(), steps.rend()))
-        std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return steps[a] > steps[b]; });
-    // a heap of the CTAs by (steps, number), the least on top: the first items go to CTAs 0, 1, ...
-    std::vector<std::pair<int64_t, int32_t>> heap(ctas);
-    for (int32_t c = 0; c < ctas; ++c) heap[c] = {0, c};
-    int64_t most = 0;
+    const size_t n = items.size();
+    const int32_t ctas = (int32_t)std::min<size_t>(n_sms, n);
     out->begin.assign(ctas + 1, 0);
+    out->items.resize(n);
+    if (n == 0) return 0;
+    int64_t total = 0, longest = 0;
+    for (int64_t st : steps) { total += st; longest = std::max(longest, st); }
+    // steps in units of 2^shift: very long items need no finer queues
+    constexpr int64_t kMaxUnits = 1 << 14;
+    int shift = 0;
+    while ((total / ctas + longest) >> shift > kMaxUnits) ++shift;
+    auto units = [&](size_t i) { return (int32_t)((steps[i] + ((int64_t)1 << shift) - 1) >> shift); };
+    int32_t most_units = 0;
+    int64_t total_units = 0;
+    for (size_t i = 0; i < n; ++i) { most_units = std::max(most_units, units(i)); total_units += units(i); }
+    std::vector<int32_t> place(most_units + 2, 0), order(n), owner(n);
+    for (size_t i = 0; i < n; ++i) ++place[most_units - units(i) + 1];
+    for (int32_t u = 0; u <= most_units; ++u) place[u + 1] += place[u];
+    for (size_t i = 0; i < n; ++i) order[place[most_units - units(i)]++] = (int32_t)i;
+    // queues of CTAs by load; no load exceeds the mean and one item more
+    std::vector<int32_t> first((size_t)(total_units / ctas) + most_units + 2, -1), last(first.size(), -1), next(ctas);
+    std::vector<int64_t> load(ctas, 0);
+    for (int32_t c = 0; c < ctas; ++c) next[c] = c + 1 < ctas ? c + 1 : -1;
+    first[0] = 0;
+    last[0] = ctas - 1;
+    size_t least = 0;
     for (int32_t i : order) {
-        auto load = heap[0];
-        owner[i] = load.second;
-        ++out->begin[load.second + 1];
-        load.first += steps[i];
-        most = std::max(most, load.first);
-        size_t at = 0;
-        for (size_t child; (child = 2 * at + 1) < heap.size(); at = child) {
-            if (child + 1 < heap.size() && heap[child + 1] < heap[child]) ++child;
-            if (load < heap[child]) break;
-            heap[at] = heap[child];
-        }
-        heap[at] = load;
+        while (first[least] < 0) ++least;
+        const int32_t c = first[least];
+        first[least] = next[c];
+        const size_t to = least + units(i);
+        next[c] = -1;
+        if (first[to] < 0) first[to] = c; else next[last[to]] = c;
+        last[to] = c;
+        load[c] += steps[i];
+        owner[i] = c;
+        ++out->begin[c + 1];
     }
     for (int32_t c = 0; c < ctas; ++c) out->begin[c + 1] += out->begin[c];
-    out->items.resize(items.size());
     std::vector<int32_t> at(out->begin.begin(), out->begin.end() - 1);
     for (int32_t i : order) out->items[at[owner[i]]++] = items[i];
-    return most;
+    return *std::max_element(load.begin(), load.end());
+}
+
+// No deal of items with these steps takes fewer: the mean, or the longest item.
+struct LeastSteps {
+    int64_t total = 0, longest = 0, items = 0;
+    void add(int64_t steps, int64_t times) { total += steps * times; longest = std::max(longest, steps); items += times; }
+    int64_t of(int32_t n_sms) const {
+        const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(n_sms, items));
+        return std::max((total + ctas - 1) / ctas, longest);
+    }
+};
+
+// The same for deal_forward(): its items without a list of them.
+int64_t least_forward(const Schedule& s, bool few, int32_t parts, bool masked, int32_t n_sms) {
+    LeastSteps least;
+    const int32_t block = few ? kTileQ : kFwdBlockQ;
+    for (size_t ti = 0; ti < s.tasks.size(); ++ti) {
+        const Task& t = s.tasks[ti];
+        for (int32_t r = 0; r < t.q_len; r += block) {
+            const int32_t rows = std::min(block, t.q_len - r), n = pieces(t, parts);
+            for (int32_t i = 0; i < n; ++i)
+                least.add(item_steps(s, n < 2 ? WorkItem{(int32_t)ti, 0, r, rows} : WorkItem{(int32_t)ti, 0, i, rows | (n << kPartsShift)}, few, masked),
+                          s.task_head_count[ti]);
+        }
+    }
+    return least.of(n_sms);
 }
 
 // Forward list in `parts` pieces, or in blocks of one query tile (`few`) or two.
@@ -202,13 +245,20 @@ void choose_forward(const Schedule& s, bool masked, int32_t n_sms, DealtList* ou
     const bool all_few = s.max_item_rows <= kTileQ;
     int64_t best = deal_forward(s, all_few, 1, masked, n_sms, out);
     if (all_few && !s.shared_prefix) {
+        // numbers of pieces by the least they could take, and of equal ones the smaller first
+        std::vector<std::pair<int64_t, int32_t>> tries;
         for (int32_t parts : kPieces) {
             if (!worth_trying(s, parts, s.fwd_items.size())) break;
+            tries.push_back({least_forward(s, true, parts, masked, n_sms), parts});
+        }
+        std::sort(tries.begin(), tries.end());
+        for (const auto& [least, parts] : tries) {
+            if (least > best || (least == best && parts > out->parts)) continue;
             DealtList other;
             const int64_t most = deal_forward(s, true, parts, masked, n_sms, &other);
-            if (most < best) { best = most; *out = std::move(other); }
+            if (most < best || (most == best && parts < out->parts)) { best = most; *out = std::move(other); }
         }
-    } else if (!all_few && s.fwd_items.size() <= kEvenItems) {
+    } else if (!all_few && s.fwd_items.size() <= kEvenItems && few_rows_pay(least_forward(s, true, 1, masked, n_sms), best)) {
         DealtList other;
         if (few_rows_pay(deal_forward(s, true, 1, masked, n_sms, &other), best)) *out = std::move(other);
     }
@@ -216,24 +266,29 @@ void choose_forward(const Schedule& s, bool masked, int32_t n_sms, DealtList* ou
 
 // Backward list: an item's work is the query tiles that see its keys.  Without a mask it is left empty where items c,
 // c + grid, ... of the longest-first list are within 3 % of it: neighbours then read the same queries at the same time.
+// With one, where no item has more than one query tile (a token against a long past): there is nothing to even out, and
+// the keys of such a handle are many (23,680 items of 40 heads x 75,600 keys took 1.5 ms to deal).
 void deal_backward(const Schedule& s, bool masked, int32_t n_sms, DealtList* out) {
+    if (masked && std::all_of(s.kv_groups.begin(), s.kv_groups.end(), [](const KvGroup& g) { return g.n_q_tiles <= 1; })) return;
     std::vector<int64_t> steps;
     steps.reserve(s.bwd_items.size());
     for (const WorkItem& w : s.bwd_items) {
         const KvGroup& g = s.kv_groups[w.unit];
-        int64_t tiles = kItemSteps;
-        for (int32_t j = 0; j < g.n_tasks; ++j) {
+        int64_t tiles = kItemSteps + g.n_q_tiles;
+        for (int32_t j = 0; masked && j < g.n_tasks; ++j) {
             const int32_t ti = s.kv_group_tasks[g.task_begin + j];
-            const int32_t n = (s.tasks[ti].q_len + kTileQ - 1) / kTileQ;
-            tiles += n - (masked ? std::min(n, first_query(s.task_pos[ti], w.row0) / kTileQ) : 0);
+            tiles -= std::min((s.tasks[ti].q_len + kTileQ - 1) / kTileQ, first_query(s.task_pos[ti], w.row0) / kTileQ);
         }
         steps.push_back(tiles);
     }
-    const int64_t most = deal(s.bwd_items, steps, n_sms, out);
-    if (masked || steps.empty()) return;
-    std::vector<int64_t> load(out->ctas(), 0);
-    for (size_t i = 0; i < steps.size(); ++i) load[i % load.size()] += steps[i];
-    if (most * 100 > *std::max_element(load.begin(), load.end()) * 97) *out = DealtList();
+    if (masked) { deal(s.bwd_items, steps, n_sms, out); return; }
+    if (steps.empty()) return;
+    std::vector<int64_t> load(std::min<size_t>(n_sms, steps.size()), 0);
+    LeastSteps least;
+    for (size_t i = 0; i < steps.size(); ++i) { load[i % load.size()] += steps[i]; least.add(steps[i], 1); }
+    const int64_t in_turn = *std::max_element(load.begin(), load.end());
+    if (least.of(n_sms) * 100 > in_turn * 97) return;
+    if (deal(s.bwd_items, steps, n_sms, out) * 100 > in_turn * 97) *out = DealtList();
 }
 
 // Work lists, launch phases and workspace layout from the tasks, query groups and kv groups.

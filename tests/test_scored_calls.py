@@ -1,5 +1,6 @@
 """What the binding and the library make of a scored call's arguments, without a GPU."""
 import ctypes
+import time
 
 import pytest
 import torch
@@ -83,3 +84,26 @@ def test_every_score_is_accepted_where_no_shard_has_queries(cu, shards, placed):
         assert B.lib().zl_scored_workspace_bytes(h.ptr, desc, ctypes.byref(n)) == 0 and n.value == 0, kw
         assert B.lib().zl_scored_attn_bwd(h.ptr, desc, None, 16, 16, None, None, None, ctypes.c_float(1.0), None, 16, 16, None,
                                           None, 0, None) == 0, kw
+
+
+# ---------------------------------------------------------------------------------------------- preparation
+def test_new_positions_cost_less_than_a_handle():
+    """One token against a long past in chunks: a decoding loop sets positions at every token (the masked lists of 40 heads x
+    75,600 keys used to take twice the time of building the whole handle)."""
+    def best(f):
+        def once():
+            a = time.perf_counter()
+            f()
+            return time.perf_counter() - a
+        return min(once() for _ in range(7))
+
+    shards = [(0, 1, i * 9450, 9450, 0) for i in range(8)]
+    build = lambda: Z.build_tasks([0], shards, 1, 8 * 9450, 40, 128)  # noqa: E731
+    h = build()
+    at = iter(range(75000, 76000))
+
+    def place():
+        p = next(at)
+        h.set_positions(None, [(p, i * 9450, 0) for i in range(8)])
+
+    assert best(place) < best(build) / 2
