@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import scored_ref as R
-from test_gpu_scored import KINDS, Run, check_all, cu, make_score, rand, status_ok, whole_problems
+from test_gpu_scored import KINDS, Run, check_all, cu, make_score, prefix_problems, rand, status_ok, whole_problems
 
 pytestmark = pytest.mark.gpu
 
@@ -167,3 +167,17 @@ def test_a_query_of_nan_stays_its_own_and_stays_nan(cap, slopes):
     R.check(o.cpu()[rows], {"o": f["o"][rows], "o_err": f["o_err"][rows]}, "o")
     R.check(lse.cpu()[:, rows], {"lse": f["lse"][:, rows], "lse_err": f["lse_err"][:, rows]}, "lse")
     assert not o[70, 0].isnan().any()
+
+
+# ------------------------------------------------------------------------------------------------- shared prefixes
+@pytest.mark.parametrize("qlens,klens,P,H,d", [
+    ([1] * 37, [1 + 5 * i for i in range(37)], 700, 2, 128), ([1] * 130, [0] * 130, 1025, 1, 64), ([100, 1, 0, 257, 64, 130], [100, 1, 9, 257, 0, 300], 640, 2, 128),
+    ([3, 129, 128], [3, 129, 128], 1, 3, 64), ([5, 40], [70, 0], 0, 2, 128), ([300], [200], 300, 1, 64), ([2, 200, 1], [2, 200, 1], 4000, 1, 128)])
+def test_shared_prefixes_round_ds_once(qlens, klens, P, H, d):
+    """The default backward of these handles, against the bounds of a single rounding between P, dP and the products."""
+    import paper_2608_01150_b200 as Z
+    g = torch.Generator().manual_seed(46)
+    nq, nk = sum(qlens), P + sum(klens)
+    q, d_o, k, v = rand(g, nq, H, d), rand(g, nq, H, d), rand(g, nk, H, d), rand(g, nk, H, d)
+    h = Z.build_tasks_prefix(cu(qlens), cu(klens), P, nq, nk, H, d)
+    check_all(Run(h, {}, q, k, v, d ** -0.5, plain=True), prefix_problems(qlens, klens, P), {}, q, k, v, d_o, d ** -0.5, ds_roundings=1)
