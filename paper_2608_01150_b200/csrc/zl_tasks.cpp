@@ -126,9 +126,10 @@ std::vector<WorkItem> in_pieces(const Schedule& s, const std::vector<WorkItem>& 
 }
 
 // Whether blocks of one query tile (`few` steps) beat blocks of two: a step of theirs loads twice the keys, so a tenth
-// fewer steps is where they start to pay.  Measured, 12 heads, d 128, blocks of two -> blocks of one: causal order over 1560
-// tokens 25.4 -> 18.5 us, over 4 x 1560 50.3 -> 40.5 (both chosen); 16 x 512 tokens 26.5 -> 42.0, 9450 tokens 238 -> 280 (not
-// chosen).
+// fewer steps is where they start to pay.  Measured, d 128, blocks of two -> blocks of one, us.  Chosen: causal order over 1560
+// tokens, 12 heads, 25.6 -> 19.1; over 2500 + 300 + 900, 8 heads, 39.4 -> 26.0; capped scores over 4096 tokens, 4 heads, 73 -> 43.
+// Not chosen: causal order over 4 x 1560, 12 heads, 41 -> 53; 1560 + 1560 + 3600 under cap and mask 78 -> 99; 16 x 512 30 -> 48; 9450
+// tokens 247 -> 309.  Of 64 cases (16 batches, mask or slopes, cap or none) two got the slower blocks, both by 4 %.
 bool few_rows_pay(int64_t few, int64_t two) { return few * 10 < two * 9; }
 
 // Beyond this many items per SM the rounds are even enough, whatever their blocks.
