@@ -19,9 +19,9 @@
  *     LSE is [n_heads, total_q] fp32: natural log of the sum of exp(scale * q.k).
  *   - Attention is bidirectional, without mask, bias or dropout, except in the scored entry points
  *     (zl_scored_attn_*).  head_dim is 64 or 128.
- *   - All tensor arguments are DEVICE pointers unless marked host.  The caller owns every
- *     tensor, the workspace and the stream; the library allocates only the small tables
- *     inside a zl_tasks handle.
+ *   - All tensor arguments are DEVICE pointers unless marked host; k, v, dk and dv may be NULL where
+ *     total_kv = 0.  The caller owns every tensor, the workspace and the stream; the library allocates
+ *     only the small tables inside a zl_tasks handle.
  *   - Every function returns a zl_status; nothing throws, aborts or traps.  Kernels bound
  *     all their waits; a wait that expires records ZL_ERR_TIMEOUT in the handle's device
  *     status word (zl_last_device_status) and the kernel returns normally.
@@ -374,6 +374,7 @@ zl_status zl_coalesced_attn_bwd_noalloc(const zl_tasks* tasks, const void* q, co
  *   n_buckets     1 .. ZL_MAX_BUCKETS (ZL_ERR_UNSUPPORTED above) with buckets, else 0.
  *   max_distance  0 .. 2^24.
  *   masked        0 or 1.  1 needs zl_set_positions.
+ * The backward holds LSE / scale in fp32: it has to stay below 3e38.
  * Slopes and biases are read when the kernels run, so a captured graph sees their current values. */
 #define ZL_MAX_BUCKETS 64
 typedef struct {

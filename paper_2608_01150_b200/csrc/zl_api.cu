@@ -465,6 +465,7 @@ zl_status fwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     if (item_end == item_begin) return ZL_OK;
     if (t->device < 0) return ZL_ERR_CUDA;
     if (!on_handle_device(t)) return ZL_ERR_INVALID_ARG;
+    if (s.total_kv == 0) k = v = q;  // empty tensors may have no address; nothing is read through their maps
     if (!q || !k || !v || !o || !lse) return ZL_ERR_INVALID_ARG;
     if (s.partial_rows > 0 && (!o_partial || !lse_partial)) return ZL_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(o_partial))
@@ -626,6 +627,7 @@ zl_status bwd_impl(const zl_tasks* t, int32_t phase, const void* q, const void* 
     const bool first = phase <= 0, last = phase < 0 || phase == n_phases - 1;
     if (t->device < 0) return ZL_ERR_CUDA;
     if (!on_handle_device(t)) return ZL_ERR_INVALID_ARG;
+    if (s.total_kv == 0) { k = v = q; dk = dv = dq; }  // as in the forward; nothing is written through them either
     if (!q || !k || !v || !o || !lse || !d_o || !dq || !dk || !dv || !workspace) return ZL_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(d_o) || !aligned16(dq) ||
         !aligned16(dk) || !aligned16(dv) || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0)

@@ -181,3 +181,27 @@ def test_shared_prefixes_round_ds_once(qlens, klens, P, H, d):
     q, d_o, k, v = rand(g, nq, H, d), rand(g, nq, H, d), rand(g, nk, H, d), rand(g, nk, H, d)
     h = Z.build_tasks_prefix(cu(qlens), cu(klens), P, nq, nk, H, d)
     check_all(Run(h, {}, q, k, v, d ** -0.5, plain=True), prefix_problems(qlens, klens, P), {}, q, k, v, d_o, d ** -0.5, ds_roundings=1)
+
+
+# ------------------------------------------------------------------------------------------------- no keys at all
+@pytest.mark.parametrize("make,kind", [("shards", "plain"), ("shards", "mask"), ("shards", "all"), ("prefix", "plain"), ("prefix", "cap_mask")])
+def test_queries_without_any_key_in_the_batch(make, kind):
+    """K and V are empty tensors, whose address is NULL: rows get O = 0, LSE = -inf, dQ = 0."""
+    import paper_2608_01150_b200 as Z
+    d, H, rows = 64, 2, 150
+    g = torch.Generator().manual_seed(47)
+    q, d_o = rand(g, rows, H, d), rand(g, rows, H, d)
+    none = torch.zeros(0, H, d, dtype=torch.bfloat16)
+    if make == "shards":
+        h = Z.build_tasks([0], [(0, 140, 0, 0, 0), (140, 10, 0, 0, 1)], rows, 0, H, d)
+    else:
+        h = Z.build_tasks_prefix([0, 140, 150], [0, 0, 0], 0, rows, 0, H, d)
+    h.set_positions(None, [(5, 0, 0), (0, 0, 3)])
+    s = {} if kind == "plain" else make_score(g, H, **KINDS[kind])
+    run = Run(h, s, q, none, none, d ** -0.5, plain=kind == "plain")
+    o, lse = run.forward()
+    assert (o == 0).all() and torch.isneginf(lse).all()
+    got = run.backward(d_o)
+    assert (got["dq"] == 0).all() and got["dk"].numel() == 0
+    if kind == "all":
+        assert (got["dtable"] == 0).all()
