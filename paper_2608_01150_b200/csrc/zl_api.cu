@@ -8,6 +8,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <new>
 #include <tuple>
 
@@ -101,6 +102,14 @@ struct LaunchTimer {
         if ((int)t->ev_start[id].size() <= i) {
             cudaEvent_t a, b;
             if (cudaEventCreate(&a) != cudaSuccess || cudaEventCreate(&b) != cudaSuccess) return;
+            try {
+                t->ev_start[id].reserve(kMaxTimedLaunches);
+                t->ev_stop[id].reserve(kMaxTimedLaunches);
+            } catch (const std::exception&) {  // not timed
+                cudaEventDestroy(a);
+                cudaEventDestroy(b);
+                return;
+            }
             t->ev_start[id].push_back(a);
             t->ev_stop[id].push_back(b);
         }
@@ -140,6 +149,16 @@ bool make_tmap_aug_rows(CUtensorMap* m, const void* base, int64_t n_tiles) {
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
+}
+
+// Runs a call's host work; what it throws (its vectors may find no memory) becomes a status at the C interface.
+template <class F>
+zl_status guarded(F&& work) {
+    try {
+        return work();
+    } catch (const std::exception&) {
+        return ZL_ERR_INVALID_ARG;
+    }
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -281,16 +300,18 @@ zl_status zl_build_tasks_ex(const int32_t* cu_seqlens, int32_t n_whole, const zl
     if (!out) return ZL_ERR_INVALID_ARG;
     *out = nullptr;
     if (n_whole < 0 || (n_whole > 0 && !cu_seqlens)) return ZL_ERR_INVALID_ARG;
-    std::vector<zl_whole_desc> whole;
-    if (n_whole > 0) {
-        if (cu_seqlens[0] != 0) return ZL_ERR_INVALID_ARG;
-        for (int i = 0; i < n_whole; ++i) {
-            if (cu_seqlens[i + 1] < cu_seqlens[i]) return ZL_ERR_INVALID_ARG;
-            whole.push_back({cu_seqlens[i], cu_seqlens[i + 1] - cu_seqlens[i], 0, n_heads});
+    return guarded([&]() -> zl_status {
+        std::vector<zl_whole_desc> whole;
+        if (n_whole > 0) {
+            if (cu_seqlens[0] != 0) return ZL_ERR_INVALID_ARG;
+            for (int i = 0; i < n_whole; ++i) {
+                if (cu_seqlens[i + 1] < cu_seqlens[i]) return ZL_ERR_INVALID_ARG;
+                whole.push_back({cu_seqlens[i], cu_seqlens[i + 1] - cu_seqlens[i], 0, n_heads});
+            }
         }
-    }
-    return zl_build_tasks_heads(whole.data(), n_whole, shards, nullptr, n_shards, total_q, total_kv, n_heads,
-                                head_dim, flags, stream, out);
+        return zl_build_tasks_heads(whole.data(), n_whole, shards, nullptr, n_shards, total_q, total_kv, n_heads,
+                                    head_dim, flags, stream, out);
+    });
 }
 
 zl_status zl_build_tasks_heads(const zl_whole_desc* whole, int32_t n_whole, const zl_shard_desc* shards,
@@ -319,7 +340,7 @@ zl_status zl_build_tasks_heads(const zl_whole_desc* whole, int32_t n_whole, cons
         const zl_status st = build_schedule(in, n_shards, total_q, total_kv, n_heads, head_dim, flags, &h->sched);
         if (st != ZL_OK) { delete h; return st; }
         return upload_handle(h, stream, out);
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {
         delete h;
         return ZL_ERR_INVALID_ARG;
     }
@@ -336,7 +357,7 @@ zl_status zl_build_tasks_prefix(const int32_t* cu_q, const int32_t* cu_kv, int32
         const zl_status st = build_prefix_schedule(cu_q, cu_kv, n_seqs, prefix_len, total_q, total_kv, n_heads, head_dim, &h->sched);
         if (st != ZL_OK) { delete h; return st; }
         return upload_handle(h, stream, out);
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {
         delete h;
         return ZL_ERR_INVALID_ARG;
     }
@@ -882,7 +903,7 @@ zl_status zl_set_positions(zl_tasks* t, const int32_t* whole_prefix, const zl_sh
             return ZL_ERR_CUDA;
         }
         return ZL_OK;
-    } catch (const std::bad_alloc&) {
+    } catch (const std::exception&) {
         s.task_pos.clear();
         return ZL_ERR_INVALID_ARG;
     }
@@ -963,34 +984,48 @@ zl_status zl_set_fwd_phases(zl_tasks* t, const int32_t* whole_phase, const int32
                             void* stream) {
     if (!t) return ZL_ERR_INVALID_ARG;
     if (t->device >= 0 && !on_handle_device(t)) return ZL_ERR_INVALID_ARG;
-    Schedule& s = t->sched;
-    std::vector<int32_t> ph;
-    const zl_status st = task_phases(s, whole_phase, shard_phase, n_phases, &ph);
-    if (st != ZL_OK) return st;
-    s.fwd_task_phase = ph;
-    regroup_by_phase(&s.fwd_items, s.fwd_task_phase, n_phases, &s.fwd_phase_begin);
-    return upload_items(t, t->d_fwd_items, s.fwd_items, static_cast<cudaStream_t>(stream));
+    return guarded([&]() -> zl_status {
+        Schedule& s = t->sched;
+        std::vector<int32_t> ph;
+        const zl_status st = task_phases(s, whole_phase, shard_phase, n_phases, &ph);
+        if (st != ZL_OK) return st;
+        std::vector<WorkItem> items = s.fwd_items;  // taken over as a whole, or not at all
+        std::vector<int32_t> begin;
+        regroup_by_phase(&items, ph, n_phases, &begin);
+        s.fwd_items.swap(items);
+        s.fwd_phase_begin.swap(begin);
+        s.fwd_task_phase.swap(ph);
+        return upload_items(t, t->d_fwd_items, s.fwd_items, static_cast<cudaStream_t>(stream));
+    });
 }
 
 zl_status zl_set_bwd_phases(zl_tasks* t, const int32_t* whole_phase, const int32_t* shard_phase, int32_t n_phases,
                             void* stream) {
     if (!t) return ZL_ERR_INVALID_ARG;
     if (t->device >= 0 && !on_handle_device(t)) return ZL_ERR_INVALID_ARG;
-    Schedule& s = t->sched;
-    std::vector<int32_t> ph;
-    const zl_status st = task_phases(s, whole_phase, shard_phase, n_phases, &ph);
-    if (st != ZL_OK) return st;
-    // a kv group is finished by one work item, so it runs in the latest phase any of its tasks asks for
-    s.bwd_group_phase.assign(s.kv_groups.size(), 0);
-    for (size_t g = 0; g < s.kv_groups.size(); ++g)
-        for (int32_t j = 0; j < s.kv_groups[g].n_tasks; ++j)
-            s.bwd_group_phase[g] = std::max(s.bwd_group_phase[g], ph[s.kv_group_tasks[s.kv_groups[g].task_begin + j]]);
-    regroup_by_phase(&s.bwd_items, s.bwd_group_phase, n_phases, &s.bwd_phase_begin);
-    regroup_by_phase(&s.bwd_pair_items, s.bwd_group_phase, n_phases, &s.bwd_pair_phase_begin);
-    cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    const zl_status st1 = upload_items(t, t->d_bwd_items, s.bwd_items, cs);
-    if (st1 != ZL_OK) return st1;
-    return upload_items(t, t->d_bwd_pair_items, s.bwd_pair_items, cs);
+    return guarded([&]() -> zl_status {
+        Schedule& s = t->sched;
+        std::vector<int32_t> ph;
+        const zl_status st = task_phases(s, whole_phase, shard_phase, n_phases, &ph);
+        if (st != ZL_OK) return st;
+        // a kv group is finished by one work item, so it runs in the latest phase any of its tasks asks for
+        std::vector<int32_t> group_phase(s.kv_groups.size(), 0), begin, pair_begin;
+        for (size_t g = 0; g < s.kv_groups.size(); ++g)
+            for (int32_t j = 0; j < s.kv_groups[g].n_tasks; ++j)
+                group_phase[g] = std::max(group_phase[g], ph[s.kv_group_tasks[s.kv_groups[g].task_begin + j]]);
+        std::vector<WorkItem> items = s.bwd_items, pair_items = s.bwd_pair_items;  // taken over as a whole, or not at all
+        regroup_by_phase(&items, group_phase, n_phases, &begin);
+        regroup_by_phase(&pair_items, group_phase, n_phases, &pair_begin);
+        s.bwd_items.swap(items);
+        s.bwd_pair_items.swap(pair_items);
+        s.bwd_phase_begin.swap(begin);
+        s.bwd_pair_phase_begin.swap(pair_begin);
+        s.bwd_group_phase.swap(group_phase);
+        cudaStream_t cs = static_cast<cudaStream_t>(stream);
+        const zl_status st1 = upload_items(t, t->d_bwd_items, s.bwd_items, cs);
+        if (st1 != ZL_OK) return st1;
+        return upload_items(t, t->d_bwd_pair_items, s.bwd_pair_items, cs);
+    });
 }
 
 zl_status zl_phase_info(const zl_tasks* t, int32_t* n_fwd_phases, int32_t* n_bwd_phases, int32_t* fwd_items_per_phase,
@@ -1009,22 +1044,28 @@ zl_status zl_phase_info(const zl_tasks* t, int32_t* n_fwd_phases, int32_t* n_bwd
 
 zl_status zl_debug_set_fwd_order(zl_tasks* t, int32_t mode, void* stream) {
     if (!t || mode < 0 || mode > 2) return ZL_ERR_INVALID_ARG;
-    Schedule& s = t->sched;
-    auto placement_order = [](const WorkItem& a, const WorkItem& b) {
-        return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
-    };
-    std::stable_sort(s.fwd_items.begin(), s.fwd_items.end(), placement_order);
-    if (mode != 1) {
-        std::stable_sort(s.fwd_items.begin(), s.fwd_items.end(), [&](const WorkItem& a, const WorkItem& b) {
-            const int32_t ka = s.tasks[a.unit].kv_len, kb = s.tasks[b.unit].kv_len;
-            if (ka != kb) return mode == 0 ? ka > kb : ka < kb;
-            if (a.rows != b.rows) return mode == 0 ? a.rows > b.rows : a.rows < b.rows;
-            return false;
-        });
-    }
-    // the list stays grouped by launch phase
-    regroup_by_phase(&s.fwd_items, s.fwd_task_phase, (int32_t)s.fwd_phase_begin.size() - 1, &s.fwd_phase_begin);
-    return upload_items(t, t->d_fwd_items, s.fwd_items, static_cast<cudaStream_t>(stream));
+    return guarded([&]() -> zl_status {
+        Schedule& s = t->sched;
+        auto placement_order = [](const WorkItem& a, const WorkItem& b) {
+            return std::tie(a.unit, a.head, a.row0) < std::tie(b.unit, b.head, b.row0);
+        };
+        std::vector<WorkItem> items = s.fwd_items;  // taken over as a whole, or not at all
+        std::stable_sort(items.begin(), items.end(), placement_order);
+        if (mode != 1) {
+            std::stable_sort(items.begin(), items.end(), [&](const WorkItem& a, const WorkItem& b) {
+                const int32_t ka = s.tasks[a.unit].kv_len, kb = s.tasks[b.unit].kv_len;
+                if (ka != kb) return mode == 0 ? ka > kb : ka < kb;
+                if (a.rows != b.rows) return mode == 0 ? a.rows > b.rows : a.rows < b.rows;
+                return false;
+            });
+        }
+        // the list stays grouped by launch phase
+        std::vector<int32_t> begin;
+        regroup_by_phase(&items, s.fwd_task_phase, (int32_t)s.fwd_phase_begin.size() - 1, &begin);
+        s.fwd_items.swap(items);
+        s.fwd_phase_begin.swap(begin);
+        return upload_items(t, t->d_fwd_items, s.fwd_items, static_cast<cudaStream_t>(stream));
+    });
 }
 
 zl_status zl_set_sm_margin(zl_tasks* t, int32_t n_sms) {

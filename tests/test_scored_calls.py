@@ -1,5 +1,8 @@
 """What the binding and the library make of a scored call's arguments, without a GPU."""
 import ctypes
+import os
+import subprocess
+import sys
 import time
 
 import pytest
@@ -7,6 +10,8 @@ import torch
 
 import paper_2608_01150_b200 as Z
 from paper_2608_01150_b200 import binding as B
+
+no_device = pytest.mark.skipif(torch.cuda.is_available(), reason="host-only handles: no table is uploaded")
 
 
 # ---------------------------------------------------------------------------------------------- a Score follows its attributes
@@ -107,3 +112,36 @@ def test_new_positions_cost_less_than_a_handle():
         h.set_positions(None, [(p, i * 9450, 0) for i in range(8)])
 
     assert best(place) < best(build) / 2
+
+
+# ---------------------------------------------------------------------------------------------- memory
+STARVED = """
+import ctypes, resource, sys
+sys.path.insert(0, {root!r})
+from paper_2608_01150_b200 import binding as B
+import paper_2608_01150_b200 as Z
+n = 20_000_000
+zeros = (ctypes.c_int32 * (n + 1))()
+h = Z.build_tasks([i for i in range(200_001)], [], 200_000, 200_000, 4, 64)
+used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (used + (8 << 20), resource.RLIM_INFINITY))
+out = ctypes.c_void_p()
+print(B.lib().zl_build_tasks(zeros, n, None, 0, 0, 0, 1, 64, None, ctypes.byref(out)))
+print(B.lib().zl_build_tasks_prefix(zeros, zeros, n, 0, 0, 0, 1, 64, None, ctypes.byref(out)))
+print(B.lib().zl_set_positions(h.ptr, None, None, None))
+print(B.lib().zl_set_fwd_phases(h.ptr, None, None, 2, None))
+print(B.lib().zl_set_bwd_phases(h.ptr, None, None, 2, None))
+print(B.lib().zl_debug_set_fwd_order(h.ptr, 2, None))
+print("alive")
+"""
+
+
+@no_device
+def test_calls_without_memory_return_an_error():
+    """Nothing throws through the C interface: a process whose memory is used up gets a status and lives on."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", STARVED.format(root=root)], capture_output=True, text=True, timeout=300)
+    lines = run.stdout.split()
+    assert run.returncode == 0 and lines[-1] == "alive", (lines, run.stderr[-400:])
+    # 20 million sequences fit nowhere; what the handle's own calls need may be left over from building it
+    assert lines[:2] == ["1", "1"] and len(lines) == 7 and set(lines[2:-1]) <= {"0", "1"}
