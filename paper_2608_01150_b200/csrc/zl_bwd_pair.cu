@@ -136,6 +136,13 @@ __device__ __forceinline__ bool pair_wait_cluster(uint64_t* bar, uint32_t parity
         }                                                                                     \
     } while (0)
 
+// Clears the bf16 pairs of query columns from `valid` on.
+__device__ __forceinline__ void keep_columns(uint32_t (&pairs)[32], int valid) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if (2 * i + 1 >= valid) pairs[i] &= 2 * i < valid ? 0xffffu : 0u;
+}
+
 __device__ __forceinline__ int count_q_tiles(const BwdParams&, const KvGroup& g) { return g.n_q_tiles; }
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
@@ -483,11 +490,17 @@ zl_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (has_next) wi_cur = p.items[it + n_clusters];
             const int rows_here = min(kTileKV, wi.rows - kTileKV * (int)rank);  // key rows of this CTA's tile (may be <= 0)
             const bool row_ok = row < rows_here;
-            const float row_bias = row_ok ? 0.f : -INFINITY;
             const int n_it = count_q_tiles(p, g);
+            int task = 0, rows_left = g.first_q_len;  // query rows of the current task from this tile on
             {
                 #pragma unroll 1
-                for (int i = 0; i < n_it; ++i, ++it_cnt) {
+                for (int i = 0; i < n_it; ++i, ++it_cnt, rows_left -= kTileQ) {
+                    if (rows_left <= 0) rows_left = p.tasks[p.kv_group_tasks[g.task_begin + ++task]].q_len;
+                    // Key rows behind the item and query columns behind the task are rows of others, or of none, whose products may
+                    // be anything up to an infinity.  P is cleared there, and dP^T - D is packed as a finite number, so that dS is
+                    // zero too: sums of finite products that overflow are infinities on these tensor cores, never NaN.
+                    // (Clearing dS as well, in registers or behind its hand-over, cost 1.5 to 3 %; this 0 to 0.8 %.)
+                    const bool whole = rows_left - col0 >= 64 && quarter * 32 + 32 <= rows_here;  // warp-uniform
                     ZL_WAIT_WARP(&sm.s_full, it_cnt & 1, 31);
                     tc_fence_after();
                     uint32_t pk[32];  // P^T of this thread's row, bf16 pairs
@@ -504,15 +517,13 @@ zl_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             mbar_arrive_cluster(s_read_l);
                             if (wg == 0) mbar_arrive(&sm.sp_read[quarter]);
                         }
-                        // S^T already has -LSE/scale folded in; query columns past the end of the task carry -1e30
-                        // there (preprocess kernel) and key rows past the end of the item get -inf here, so their
-                        // P is exactly zero without a second code path
+                        // S^T already has -LSE/scale folded in
 #pragma unroll
                         for (int c = 0; c < 2; ++c)
 #pragma unroll
                             for (int i = 0; i < 32; i += 2)
-                                pk[c * 16 + i / 2] = pack_bf16(ex2(fmaf(__uint_as_float(sr[c][i]), sl2, row_bias)),
-                                                               ex2(fmaf(__uint_as_float(sr[c][i + 1]), sl2, row_bias)));
+                                pk[c * 16 + i / 2] = pack_bf16(ex2(__uint_as_float(sr[c][i]) * sl2), ex2(__uint_as_float(sr[c][i + 1]) * sl2));
+                        if (!whole) keep_columns(pk, row_ok ? rows_left - col0 : 0);
                         if (wg == 1) {
                             ZL_WAIT_WARP(&sm.sp_read[quarter], it_cnt & 1, 36);
                             tc_fence_after();
@@ -539,14 +550,13 @@ zl_bwd_pair_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             if (lane == 0) mbar_arrive(&sm.dp_read[quarter]);
                         }
                         uint32_t dd[32];
-                        // dS^T = P^T o (dP^T - D) in packed bf16 arithmetic; where P is zero by masking, dP^T - D is
-                        // finite (rows of other sequences or the zero fill of the loads), so the product is zero
+                        // dS^T = P^T o (dP^T - D) in packed bf16 arithmetic
 #pragma unroll
                         for (int c = 0; c < 2; ++c)
 #pragma unroll
                             for (int i = 0; i < 32; i += 2)
                                 dd[c * 16 + i / 2] = mul_bf16x2(pk[c * 16 + i / 2],
-                                                                pack_bf16(__uint_as_float(dr[c][i]), __uint_as_float(dr[c][i + 1])));
+                                                                pack_bf16_finite(__uint_as_float(dr[c][i]), __uint_as_float(dr[c][i + 1])));
                         // A operand of dK first (dS^T as bf16 pairs in TMEM): the dK MMAs start while the rows for
                         // the dQ operand are still being stored and sent
                         if (wg == 1) {

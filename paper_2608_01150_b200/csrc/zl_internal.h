@@ -82,7 +82,8 @@ struct alignas(16) KvGroup {
     int32_t task_begin, n_tasks;  // range in the kv-group task list
     int32_t n_q_tiles;            // 128-row query tiles of all its tasks together
     int32_t tile_begin;           // number of 128-row key tiles of the groups before it
-    int32_t pad_[2];
+    int32_t first_q_len;          // query rows of its first task
+    int32_t pad_;
 };
 
 // One attention problem of a placement as the builder receives it: a whole sequence (q range ==

@@ -296,6 +296,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// The same with infinities as the largest finite numbers.
+__device__ __forceinline__ uint32_t pack_bf16_finite(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 
 // Three-input maximum and packed fp32x2 arithmetic (sm_100): halve the instruction count of
 // the row-maximum and of the scale/subtract/accumulate steps of the softmax.

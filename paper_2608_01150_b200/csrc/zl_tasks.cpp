@@ -544,7 +544,7 @@ zl_status build_schedule(const std::vector<InputTask>& in, int32_t n_shards, int
         }
         for (size_t g = 0; g < kmembers.size(); ++g) {
             const Task& t0 = s->tasks[kmembers[g][0]];
-            KvGroup kgp{t0.kv_off, t0.kv_len, (int32_t)s->kv_group_tasks.size(), (int32_t)kmembers[g].size(), 0, 0, {0, 0}};
+            KvGroup kgp{t0.kv_off, t0.kv_len, (int32_t)s->kv_group_tasks.size(), (int32_t)kmembers[g].size(), 0, 0, t0.q_len, 0};
             for (int32_t ti : kmembers[g]) {
                 s->kv_group_tasks.push_back(ti);
                 kgp.n_q_tiles += (s->tasks[ti].q_len + kTileQ - 1) / kTileQ;
@@ -594,7 +594,7 @@ zl_status build_prefix_schedule(const int32_t* cu_q, const int32_t* cu_kv, int32
         if (s->partial_rows > INT32_MAX) return ZL_ERR_INVALID_ARG;
         if (kv_len > 0) {
             t.kv_group = (int32_t)s->kv_groups.size();
-            s->kv_groups.push_back(KvGroup{kv_off, kv_len, (int32_t)s->kv_group_tasks.size(), 1, (q_len + kTileQ - 1) / kTileQ, 0, {0, 0}});
+            s->kv_groups.push_back(KvGroup{kv_off, kv_len, (int32_t)s->kv_group_tasks.size(), 1, (q_len + kTileQ - 1) / kTileQ, 0, q_len, 0});
             s->kv_group_tasks.push_back((int32_t)s->tasks.size());
         }
         s->tasks.push_back(t);
