@@ -182,6 +182,14 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+def _int32s(values) -> List[int]:
+    """The values as ints that fit the ABI's int32; ctypes would keep the low 32 bits of others without a word."""
+    out = [int(v) for v in values]
+    if out and (min(out) < -2 ** 31 or max(out) >= 2 ** 31):
+        raise ZlError(1, f"{max(out, key=abs)} does not fit 32 bits")
+    return out
+
+
 class TaskHandle:
     """Owns a ``zl_tasks*``.  Built once per placement, reused for every layer and step."""
 
@@ -240,7 +248,7 @@ class TaskHandle:
     def _phase_array(values):
         if values is None:
             return None, None
-        arr = (ctypes.c_int32 * max(1, len(values)))(*[int(v) for v in values])
+        arr = (ctypes.c_int32 * max(1, len(values)))(*_int32s(values))
         return arr, ctypes.cast(arr, ctypes.c_void_p)
 
     def set_fwd_phases(self, whole_phase, shard_phase, n_phases: int, stream=None):
@@ -262,7 +270,7 @@ class TaskHandle:
         if shard_pos is not None and len(shard_pos) != self.n_shards:
             raise ZlError(1, f"set_positions: {self.n_shards} shards, {len(shard_pos)} positions")
         a, ap = self._phase_array(whole_prefix)
-        b = (ShardPos * max(1, self.n_shards))(*[ShardPos(*[int(v) for v in s]) for s in shard_pos or ()])
+        b = (ShardPos * max(1, self.n_shards))(*[ShardPos(*_int32s(s)) for s in shard_pos or ()])
         bp = ctypes.cast(b, ctypes.c_void_p) if shard_pos is not None else None
         _check(_lib.zl_set_positions(self._ptr, ap, bp, _stream_ptr(stream)), "zl_set_positions")
 
@@ -313,8 +321,9 @@ def build_tasks(cu_seqlens: Sequence[int], shards: Sequence[Sequence[int]], tota
     """zl_build_tasks / zl_build_tasks_ex: placement (cu_seqlens + shard descriptors) -> task handle.
     flags: 0 or BUILD_FUSE_LOCAL_CHUNKS."""
     n_whole = max(0, len(cu_seqlens) - 1)
-    cu = (ctypes.c_int32 * max(1, len(cu_seqlens)))(*[int(c) for c in cu_seqlens])
-    sh = (ShardDesc * max(1, len(shards)))(*[ShardDesc(*[int(v) for v in s]) for s in shards])
+    total_q, total_kv, n_heads, head_dim = _int32s((total_q, total_kv, n_heads, head_dim))
+    cu = (ctypes.c_int32 * max(1, len(cu_seqlens)))(*_int32s(cu_seqlens))
+    sh = (ShardDesc * max(1, len(shards)))(*[ShardDesc(*_int32s(s)) for s in shards])
     out = ctypes.c_void_p()
     cu_p = ctypes.cast(cu, ctypes.c_void_p) if len(cu_seqlens) else None
     sh_p = ctypes.cast(sh, ctypes.c_void_p) if len(shards) else None
@@ -334,12 +343,13 @@ def build_tasks_heads(whole: Sequence[Sequence[int]], shards: Sequence[Sequence[
     """zl_build_tasks_heads: whole = (off, len, head_begin, head_count) per whole sequence, shards =
     (q_off, q_len, kv_off, kv_len, seq_id) per shard, shard_heads = (head_begin, head_count) per shard or
     None for all heads."""
-    wd = (WholeDesc * max(1, len(whole)))(*[WholeDesc(*[int(v) for v in w]) for w in whole])
-    sh = (ShardDesc * max(1, len(shards)))(*[ShardDesc(*[int(v) for v in s[:5]]) for s in shards])
+    total_q, total_kv, n_heads, head_dim = _int32s((total_q, total_kv, n_heads, head_dim))
+    wd = (WholeDesc * max(1, len(whole)))(*[WholeDesc(*_int32s(w)) for w in whole])
+    sh = (ShardDesc * max(1, len(shards)))(*[ShardDesc(*_int32s(s[:5])) for s in shards])
     hr = None
     if shard_heads is not None:
         assert len(shard_heads) == len(shards)
-        hr = (HeadRange * max(1, len(shards)))(*[HeadRange(int(a), int(b)) for a, b in shard_heads])
+        hr = (HeadRange * max(1, len(shards)))(*[HeadRange(*_int32s((a, b))) for a, b in shard_heads])
     out = ctypes.c_void_p()
     st = _lib.zl_build_tasks_heads(ctypes.cast(wd, ctypes.c_void_p) if len(whole) else None, len(whole),
                                    ctypes.cast(sh, ctypes.c_void_p) if len(shards) else None,
@@ -357,8 +367,9 @@ def build_tasks_prefix(cu_q: Sequence[int], cu_kv: Sequence[int], prefix_len: in
     n = max(0, len(cu_q) - 1)
     if max(0, len(cu_kv) - 1) != n:
         raise ZlError(1, f"build_tasks_prefix: {n} query ranges, {max(0, len(cu_kv) - 1)} key ranges")
-    a = (ctypes.c_int32 * max(1, len(cu_q)))(*[int(c) for c in cu_q])
-    b = (ctypes.c_int32 * max(1, len(cu_kv)))(*[int(c) for c in cu_kv])
+    prefix_len, total_q, total_kv, n_heads, head_dim = _int32s((prefix_len, total_q, total_kv, n_heads, head_dim))
+    a = (ctypes.c_int32 * max(1, len(cu_q)))(*_int32s(cu_q))
+    b = (ctypes.c_int32 * max(1, len(cu_kv)))(*_int32s(cu_kv))
     out = ctypes.c_void_p()
     _check(_lib.zl_build_tasks_prefix(ctypes.cast(a, ctypes.c_void_p), ctypes.cast(b, ctypes.c_void_p), n, prefix_len,
                                       total_q, total_kv, n_heads, head_dim, _stream_ptr(stream), ctypes.byref(out)),

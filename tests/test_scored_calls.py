@@ -145,3 +145,21 @@ def test_calls_without_memory_return_an_error():
     assert run.returncode == 0 and lines[-1] == "alive", (lines, run.stderr[-400:])
     # 20 million sequences fit nowhere; what the handle's own calls need may be left over from building it
     assert lines[:2] == ["1", "1"] and len(lines) == 7 and set(lines[2:-1]) <= {"0", "1"}
+
+
+# ---------------------------------------------------------------------------------------------- numbers beyond 32 bits
+def test_numbers_beyond_32_bits_are_refused():
+    """ctypes would keep the low 32 bits: a position of 2^32 would be position 0."""
+    big = 2 ** 32
+    h = Z.build_tasks([0, 10], [(10, 5, 10, 7, 0)], 20, 20, 1, 64)
+    calls = [lambda: h.set_positions([big], [(0, 0, 0)]), lambda: h.set_positions([0], [(big, 0, 0)]), lambda: h.set_positions([0], [(0, big + 3, 0)]),
+             lambda: h.set_positions([0], [(0, 0, -big)]), lambda: Z.build_tasks_prefix([0, 5], [0, 5], big, 5, 5, 1, 64),
+             lambda: Z.build_tasks_prefix([0, big + 5], [0, 5], 0, 5, 5, 1, 64), lambda: Z.build_tasks_prefix([0, 5], [0, big + 5], 0, 5, 5, 1, 64),
+             lambda: Z.build_tasks_prefix([0, 5], [0, 5], 0, big + 5, 5, 1, 64), lambda: Z.build_tasks([0, big + 10], [], 10, 10, 1, 64),
+             lambda: Z.build_tasks([0], [(0, 5, big, 5, 0)], 5, 5, 1, 64), lambda: Z.build_tasks([0, 10], [], 10, 10, big + 1, 64),
+             lambda: Z.build_tasks_heads([(big, 10, 0, 1)], [], None, 10, 10, 1, 64), lambda: Z.build_tasks_heads([(0, 10, 0, 1)], [], None, 10, big + 10, 1, 64),
+             lambda: Z.build_tasks_heads([], [(0, 5, 0, 5, 0)], [(0, big + 1)], 5, 5, 1, 64), lambda: h.set_fwd_phases([big], [0], 1)]
+    for i, call in enumerate(calls):
+        with pytest.raises(Z.ZlError) as e:
+            call()
+        assert e.value.status == 1, i
