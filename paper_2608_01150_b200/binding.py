@@ -175,9 +175,7 @@ def _current_device() -> int:
 
 
 def _ptr(t) -> Optional[int]:
-    if t is None:
-        return None
-    if isinstance(t, int):
+    if t is None or isinstance(t, int):
         return t
     return t.data_ptr()
 
@@ -459,44 +457,60 @@ class Score:
 
     def __init__(self, cap: float = 0.0, slopes=None, bucket_bias=None, bucket_of=None, masked: bool = False):
         self.cap, self.slopes, self.bucket_bias, self.bucket_of, self.masked = cap, slopes, bucket_bias, bucket_of, masked
+        self._fields = self._desc = None
         self.desc
 
     @property
     def desc(self) -> ScoreDesc:
-        """The C struct of what the attributes hold now; raises where they do not fit."""
+        """The C struct of what the attributes hold now (not to be written to); raises where they do not fit."""
+        return self._read(None)
+
+    def check(self, tasks: TaskHandle) -> ScoreDesc:
+        """The same for a call on `tasks`: the tensors are of its heads and on the current GPU."""
+        return self._read(tasks.n_heads)
+
+    def _read(self, heads: Optional[int]) -> ScoreDesc:
         import torch
         slopes, bias, of = self.slopes, self.bucket_bias, self.bucket_of
-        desc = ScoreDesc(self.cap, None, None, None, 0, 0, 1 if self.masked else 0)
+        p_slopes = p_bias = p_of = None
+        buckets = reach = 0
         if slopes is not None:
-            desc.slopes = self._address("slopes", slopes, torch.float32, 1)
+            shape = slopes.shape
+            if slopes.dtype is not torch.float32 or len(shape) != 1 or not slopes.is_contiguous():
+                raise ZlError(1, "Score: slopes must be a contiguous torch.float32 tensor of 1 dimension")
+            if heads is not None:
+                device = _current_device() if slopes.is_cuda else None
+                self._fits("slopes", slopes, shape[0], heads, device)
+            p_slopes = slopes.data_ptr()
         if bias is not None or of is not None:
             if bias is None or of is None:
                 raise ZlError(1, "Score: bucket_bias and bucket_of come together")
-            desc.bucket_bias = self._address("bucket_bias", bias, torch.float32, 2)
-            desc.bucket_of = self._address("bucket_of", of, torch.int32, 1)
-            desc.n_buckets, entries = bias.shape[0], of.shape[0]
-            if entries % 2 == 0:
+            shape, entries = bias.shape, of.shape
+            if bias.dtype is not torch.float32 or len(shape) != 2 or not bias.is_contiguous():
+                raise ZlError(1, "Score: bucket_bias must be a contiguous torch.float32 tensor of 2 dimensions")
+            if of.dtype is not torch.int32 or len(entries) != 1 or not of.is_contiguous():
+                raise ZlError(1, "Score: bucket_of must be a contiguous torch.int32 tensor of 1 dimension")
+            if entries[0] % 2 == 0:
                 raise ZlError(1, "Score: bucket_of has an entry for every distance from -max_distance to max_distance")
-            desc.max_distance = entries // 2
+            if heads is not None:
+                device = _current_device() if bias.is_cuda else None
+                self._fits("bucket_bias", bias, shape[1], heads, device)
+                self._fits("bucket_of", of, heads, heads, device)
+            p_bias, p_of, buckets, reach = bias.data_ptr(), of.data_ptr(), shape[0], entries[0] // 2
+        fields = (self.cap, p_slopes, p_bias, p_of, buckets, reach, 1 if self.masked else 0)
+        desc = self._desc
+        if fields != self._fields:
+            # a struct of its own per state: a call of another thread may be reading the one before
+            self._desc = desc = ScoreDesc(*fields)
+            self._fields = fields
         return desc
 
     @staticmethod
-    def _address(name: str, t, dtype, dims: int) -> int:
-        if t.dtype != dtype or t.dim() != dims or not t.is_contiguous():
-            raise ZlError(1, f"Score: {name} must be a contiguous {dtype} tensor of {dims} dimension(s)")
-        return t.data_ptr()
-
-    def check(self, tasks: TaskHandle) -> ScoreDesc:
-        """The descriptor for a call on `tasks`."""
-        desc = self.desc
-        for name, t in (("slopes", self.slopes), ("bucket_bias", self.bucket_bias), ("bucket_of", self.bucket_of)):
-            if t is None:
-                continue
-            if name != "bucket_of" and t.shape[-1] != tasks.n_heads:
-                raise ZlError(1, f"Score: {name} has {t.shape[-1]} heads, the handle {tasks.n_heads}")
-            if not t.is_cuda or t.get_device() != _current_device():
-                raise ZlError(1, f"Score: {name} is not on the current GPU")
-        return desc
+    def _fits(name: str, t, n: int, heads: int, device: Optional[int]):
+        if n != heads:
+            raise ZlError(1, f"Score: {name} has {n} heads, the handle {heads}")
+        if not t.is_cuda or t.get_device() != device:
+            raise ZlError(1, f"Score: {name} is not on the current GPU")
 
 
 def relative_position_buckets(n_buckets: int, max_distance: int, bidirectional: bool = True) -> List[int]:
@@ -535,7 +549,7 @@ def scored_attn_fwd(tasks: TaskHandle, score: Score, q, k, v, scale: float, o, l
                     stream=None):
     """zl_scored_attn_fwd: coalesced_attn_fwd with capped, biased or masked scores."""
     desc = score.check(tasks)
-    _check(_lib.zl_scored_attn_fwd(tasks.ptr, ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), ctypes.c_float(scale),
+    _check(_lib.zl_scored_attn_fwd(tasks.ptr, ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), scale,
                                    _ptr(o), _ptr(lse), _ptr(o_partial), _ptr(lse_partial), _stream_ptr(stream)),
            "zl_scored_attn_fwd")
 
@@ -544,7 +558,7 @@ def scored_attn_fwd_packed(tasks: TaskHandle, score: Score, qkv, scale: float, o
                            stream=None):
     """zl_scored_attn_fwd_packed: qkv is [T, 3, H, d] bf16."""
     desc = score.check(tasks)
-    _check(_lib.zl_scored_attn_fwd_packed(tasks.ptr, ctypes.byref(desc), _ptr(qkv), ctypes.c_float(scale), _ptr(o),
+    _check(_lib.zl_scored_attn_fwd_packed(tasks.ptr, ctypes.byref(desc), _ptr(qkv), scale, _ptr(o),
                                           _ptr(lse), _ptr(o_partial), _ptr(lse_partial), _stream_ptr(stream)),
            "zl_scored_attn_fwd_packed")
 
@@ -566,7 +580,7 @@ def scored_attn_bwd(tasks: TaskHandle, score: Score, q, k, v, o, lse, d_o, scale
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
     _check(_lib.zl_scored_attn_bwd(tasks.ptr, ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
-                                   _ptr(d_o), ctypes.c_float(scale), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_bucket_bias),
+                                   _ptr(d_o), scale, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_bucket_bias),
                                    _ptr(workspace), ctypes.c_size_t(workspace_bytes), _stream_ptr(stream)),
            "zl_scored_attn_bwd")
 
@@ -579,7 +593,7 @@ def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, sc
     if workspace_bytes is None:
         workspace_bytes = workspace.numel() * workspace.element_size()
     _check(_lib.zl_scored_attn_bwd_packed(tasks.ptr, ctypes.byref(desc), _ptr(qkv), _ptr(o), _ptr(lse), _ptr(d_o),
-                                          ctypes.c_float(scale), _ptr(dqkv), _ptr(d_bucket_bias), _ptr(workspace),
+                                          scale, _ptr(dqkv), _ptr(d_bucket_bias), _ptr(workspace),
                                           ctypes.c_size_t(workspace_bytes), _stream_ptr(stream)),
            "zl_scored_attn_bwd_packed")
 
@@ -593,7 +607,7 @@ def coalesced_attn_bwd_noalloc(tasks: TaskHandle, q, k, v, o, lse, d_o, scale: f
     ZL_ERR_WORKSPACE for placements that need more scratch than that.  Calls must not overlap on
     the GPU, and the first call on a device should be made outside stream capture."""
     _check(_lib.zl_coalesced_attn_bwd_noalloc(tasks.ptr, _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o),
-                                              ctypes.c_float(scale), _ptr(dq), _ptr(dk), _ptr(dv),
+                                              scale, _ptr(dq), _ptr(dk), _ptr(dv),
                                               _stream_ptr(stream)), "zl_coalesced_attn_bwd_noalloc")
 
 
