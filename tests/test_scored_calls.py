@@ -124,7 +124,7 @@ n = 20_000_000
 zeros = (ctypes.c_int32 * (n + 1))()
 h = Z.build_tasks([i for i in range(200_001)], [], 200_000, 200_000, 4, 64)
 used = int(open("/proc/self/statm").read().split()[0]) * resource.getpagesize()
-resource.setrlimit(resource.RLIMIT_AS, (used + (8 << 20), resource.RLIM_INFINITY))
+resource.setrlimit(resource.RLIMIT_AS, (used + (64 << 20), resource.RLIM_INFINITY))
 out = ctypes.c_void_p()
 print(B.lib().zl_build_tasks(zeros, n, None, 0, 0, 0, 1, 64, None, ctypes.byref(out)))
 print(B.lib().zl_build_tasks_prefix(zeros, zeros, n, 0, 0, 0, 1, 64, None, ctypes.byref(out)))
