@@ -18,7 +18,7 @@
  *   - Tensors are [tokens, n_heads, head_dim], contiguous, bf16, base 16-byte aligned.
  *     LSE is [n_heads, total_q] fp32: natural log of the sum of exp(scale * q.k).
  *   - Attention is bidirectional, without mask, bias or dropout, except in the scored entry points
- *     (zl_scored_attn_*).  head_dim is 64 or 128.
+ *     (zl_scored_attn_*) and over the paged cache (zl_cached_attn_fwd).  head_dim is 64 or 128.
  *   - All tensor arguments are DEVICE pointers unless marked host; k, v, dk and dv may be NULL where
  *     total_kv = 0.  The caller owns every tensor, the workspace and the stream; the library allocates
  *     only the small tables inside a zl_tasks handle.
@@ -423,6 +423,94 @@ zl_status zl_scored_attn_bwd_packed(const zl_tasks* tasks, const zl_score* score
                                     void* workspace, size_t workspace_bytes, void* stream);
 /* Workspace of zl_scored_attn_bwd for this handle and score (its cap and its buckets count, not its pointers' contents). */
 zl_status zl_scored_workspace_bytes(const zl_tasks* tasks, const zl_score* score, size_t* bytes);
+
+/* Paged key/value cache -- keys and values of sequences that grow by new tokens (images and videos generated token by token,
+ * or chunk by chunk), kept in pages; attention of the new tokens over all of a sequence.  Inference only.
+ *
+ * zl_kv_cache: one layer's cache.
+ *   k, v          device: n_pages pages of page_size tokens of n_kv_heads x head_dim elements, the elements of a row contiguous;
+ *                 strides in elements, the same for k and v, multiples of 16 bytes.  [n_pages, page_size, H, d] and
+ *                 [n_pages, H, page_size, d] are both such layouts.  Bases 16-byte aligned.
+ *   format        ZL_CACHE_BF16; ZL_CACHE_INT8 (whole numbers from -127 to 127) or ZL_CACHE_E4M3, each with one scale per
+ *                 token and head: the value held is code * scale.
+ *   k_scale, v_scale  device, [n_pages, page_size, n_kv_heads] fp32, contiguous; NULL with ZL_CACHE_BF16.
+ *   page_size     a power of two, at least 8.   head_dim  64 or 128.
+ *
+ * zl_cache_batch: sequences over it.  All arrays are DEVICE memory and read when the kernels run, so that a captured call
+ * follows the values of the time of its replay.
+ *   cu_q     [n_seqs + 1], non-decreasing: rows [cu_q[s], cu_q[s+1]) of the token tensors are the new tokens of sequence s.
+ *            Rows before the first and behind the last sequence are left as they are.
+ *   kv_len   [n_seqs] tokens of the sequence, the new ones included: new token i has position kv_len - q_len + i.
+ *   pages    [n_seqs, max_pages]: page number of positions [j * page_size, (j + 1) * page_size).  A number outside
+ *            [0, n_pages) is a page without keys (dropped, or not there yet): nothing is written to it, nobody sees it.
+ *            The same page may stand in several tables (a shared beginning), as long as no two new tokens of a write fall on
+ *            one place.  Positions from max_pages * page_size on hold no keys.
+ *   prefix   [n_seqs] or NULL (all 0): keys that every new token of the sequence sees (a condition, or an image seen whole);
+ *            INT32_MAX is no mask at all.
+ *   max_q    at least the largest number of new tokens of a sequence, 0 if not known.  It only chooses kernels.
+ * A token at a negative position (kv_len < q_len) is not written, and sees no key but those of the prefix. */
+typedef enum { ZL_CACHE_BF16 = 0, ZL_CACHE_INT8 = 1, ZL_CACHE_E4M3 = 2 } zl_cache_format;
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    int64_t page_stride, token_stride, head_stride;
+    int32_t n_pages, page_size, n_kv_heads, head_dim, format;
+} zl_kv_cache;
+typedef struct {
+    const int32_t* cu_q;
+    const int32_t* kv_len;
+    const int32_t* pages;
+    const int32_t* prefix;
+    int32_t n_seqs, max_pages, total_q, max_q;
+} zl_cache_batch;
+
+/* zl_cache_write -- put the new tokens' keys and values into their places.
+ *   k, v        [total_q, n_kv_heads, head_dim] bf16, rows `row_stride` elements apart (slices of packed QKV), a multiple of
+ *               8; 16-byte aligned.  Rows that are written have to be finite.
+ * In 8 bits: scale = max |x| / T over the row, code = x / scale rounded to the nearest of the type (ties to even), T = 127 or
+ * 448 (e4m3), both quotients rounded to fp32; a row whose scale is 0 has the codes of 0.  A value is off by at most
+ * scale / 2 (int8), or by 2^-4 of itself and scale / 1024 (e4m3).  (The codes that e4m3 has for NaN are never written; in a
+ * cache filled by other means they stand for +-480.) */
+zl_status zl_cache_write(const zl_kv_cache* cache, const zl_cache_batch* batch, const void* k, const void* v,
+                         int64_t row_stride, void* stream);
+
+/* zl_cache_read -- rows of the cache as packed bf16, e.g. as KV-space of the other entry points.
+ *   cu_kv    device, [n_seqs + 1], non-decreasing: rows [cu_kv[s], cu_kv[s+1]) of k and v receive the tokens of sequence s
+ *            from position first[s] on (first: device, [n_seqs]; NULL = 0 for all).  Rows without a key (positions outside
+ *            [0, kv_len), pages without keys) are set to 0; rows of no sequence are left as they are.
+ *   k, v     [total_kv, n_kv_heads, head_dim] bf16, contiguous, 16-byte aligned.
+ * cu_q, prefix, total_q and max_q of the batch are not used.  8-bit values are rounded to bf16 once. */
+zl_status zl_cache_read(const zl_kv_cache* cache, const zl_cache_batch* batch, const int32_t* first, const int32_t* cu_kv,
+                        int32_t total_kv, void* k, void* v, void* stream);
+
+/* zl_build_cached_attn -- handle of zl_cached_attn_fwd for a number of heads: it owns the counters by which parts of a long
+ * sequence are joined and the device status word, and belongs to the device that is current (without one it is host-only).
+ * n_heads is a multiple of n_kv_heads, at most 128 times as many; query head h reads key head h / (n_heads / n_kv_heads).
+ * One handle serves every layer and any cache and batch of its heads.  A handle and a workspace may be in flight on one
+ * stream at a time; captured graphs may share them as far as their replays do not overlap. */
+typedef struct zl_cached_attn zl_cached_attn;
+zl_status zl_build_cached_attn(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void* stream, zl_cached_attn** out);
+void zl_free_cached_attn(zl_cached_attn* attn);
+/* Device scratch of zl_cached_attn_fwd, whatever the batch; contents need not be initialised and are clobbered. */
+zl_status zl_cached_attn_workspace_bytes(const zl_cached_attn* attn, size_t* bytes);
+/* As zl_last_device_status; also makes the handle usable again after a wait has expired. */
+zl_status zl_cached_attn_device_status(const zl_cached_attn* attn, int32_t* code, int32_t* where);
+
+/* zl_cached_attn_fwd -- attention of the new tokens over the cache (which holds their own keys already, zl_cache_write):
+ *     new token i at position p sees keys j <= p and j < prefix;  s_j = scale * q_i.k_j,  O = softmax(s) V,  LSE = log sum exp s
+ * A token that sees no key gets O = 0, LSE = -inf.  Chunks of a prompt, single tokens and sequences without new tokens may
+ * stand in one batch; results do not depend on what else the batch holds beyond rounding, and are the same from run to run.
+ *   q          [total_q, n_heads, head_dim] bf16, rows `q_stride` elements apart, a multiple of 8; 16-byte aligned
+ *   o          [total_q, n_heads, head_dim] bf16, contiguous
+ *   lse        [n_heads, total_q] fp32, or NULL
+ *   workspace  at least zl_cached_attn_workspace_bytes, 256-byte aligned
+ * Q, and the keys and values inside the sequences' lengths, have to be finite; other places of the cache may hold anything.
+ * Asynchronous on `stream`; captured like the other entry points. */
+zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cache, const zl_cache_batch* batch, const void* q,
+                             int64_t q_stride, float scale, void* o, float* lse, void* workspace, size_t workspace_bytes,
+                             void* stream);
 
 /* Synchronises the handle's device and reads the device status word written by the
  * kernels: code is ZL_OK or ZL_ERR_TIMEOUT, `where` identifies the wait that expired

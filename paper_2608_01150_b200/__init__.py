@@ -14,6 +14,7 @@ _BINDING_NAMES = ("ZlError", "TaskHandle", "ShardDesc", "WholeDesc", "HeadRange"
                   "coalesced_attn_fwd_phase", "coalesced_attn_bwd_phase", "MAX_PHASES",
                   "build_tasks_prefix", "Score", "scored_attn_fwd", "scored_attn_fwd_packed", "scored_attn_bwd",
                   "scored_attn_bwd_packed", "relative_position_buckets", "MAX_BUCKETS",
+                  "KvCache", "CacheBatch", "CachedAttnHandle", "build_cached_attn", "cache_write", "cache_read", "cached_attn_fwd",
                   "NOALLOC_SCRATCH_BYTES", "BUILD_FUSE_LOCAL_CHUNKS", "launch_count", "library_path", "STATUS_NAMES")
 
 

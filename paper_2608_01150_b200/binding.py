@@ -51,6 +51,18 @@ class ScoreDesc(ctypes.Structure):
                 ("masked", ctypes.c_int32)]
 
 
+class KvCacheDesc(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class CacheBatchDesc(ctypes.Structure):
+    _fields_ = [("cu_q", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("prefix", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("total_q", ctypes.c_int32), ("max_q", ctypes.c_int32)]
+
+
 class TasksInfo(ctypes.Structure):
     _fields_ = [("n_tasks", ctypes.c_int32), ("n_merge_groups", ctypes.c_int32),
                 ("n_kv_groups", ctypes.c_int32), ("n_fwd_items", ctypes.c_int32),
@@ -126,6 +138,21 @@ def _load():
     lib.zl_scored_attn_bwd_packed.argtypes = [vp, sd, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
     lib.zl_scored_workspace_bytes.restype = ctypes.c_int
     lib.zl_scored_workspace_bytes.argtypes = [vp, sd, ctypes.POINTER(ctypes.c_size_t)]
+    cd, bd = ctypes.POINTER(KvCacheDesc), ctypes.POINTER(CacheBatchDesc)
+    lib.zl_cache_write.restype = ctypes.c_int
+    lib.zl_cache_write.argtypes = [cd, bd, vp, vp, ctypes.c_int64, vp]
+    lib.zl_cache_read.restype = ctypes.c_int
+    lib.zl_cache_read.argtypes = [cd, bd, vp, vp, i32, vp, vp, vp]
+    lib.zl_build_cached_attn.restype = ctypes.c_int
+    lib.zl_build_cached_attn.argtypes = [i32, i32, i32, vp, ctypes.POINTER(vp)]
+    lib.zl_free_cached_attn.restype = None
+    lib.zl_free_cached_attn.argtypes = [vp]
+    lib.zl_cached_attn_workspace_bytes.restype = ctypes.c_int
+    lib.zl_cached_attn_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
+    lib.zl_cached_attn_device_status.restype = ctypes.c_int
+    lib.zl_cached_attn_device_status.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32)]
+    lib.zl_cached_attn_fwd.restype = ctypes.c_int
+    lib.zl_cached_attn_fwd.argtypes = [vp, cd, bd, vp, ctypes.c_int64, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
     lib.zl_last_device_status.restype = ctypes.c_int
     lib.zl_last_device_status.argtypes = [vp, ctypes.POINTER(i32), ctypes.POINTER(i32)]
     lib.zl_set_kernel_timing.restype = ctypes.c_int
@@ -596,6 +623,218 @@ def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, sc
                                           scale, _ptr(dqkv), _ptr(d_bucket_bias), _ptr(workspace),
                                           ctypes.c_size_t(workspace_bytes), _stream_ptr(stream)),
            "zl_scored_attn_bwd_packed")
+
+
+def _on_gpu(what: str, t):
+    """The tensor is on the current GPU, where the call's kernels run."""
+    if not t.is_cuda or t.get_device() != _current_device():
+        raise ZlError(1, f"{what} is not on the current GPU")
+
+
+def _ints(what: str, t, shape=None):
+    import torch
+    if t.dtype is not torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+        raise ZlError(1, f"{what} must be a contiguous torch.int32 tensor" + (f" of shape {shape}" if shape is not None else ""))
+
+
+class KvCache:
+    """zl_kv_cache: the keys and values of one layer in pages.
+
+    k, v              [n_pages, page_size, n_kv_heads, head_dim] of torch.bfloat16, torch.int8 or torch.float8_e4m3fn; any
+                      strides (the same for both) with contiguous rows, e.g. ``pool[:, 0]``, ``pool[:, 1]`` or a transposed
+                      [n_pages, n_kv_heads, page_size, head_dim]
+    k_scale, v_scale  fp32 [n_pages, page_size, n_kv_heads] of an 8-bit cache, written by cache_write; else None
+
+    The attributes can be changed, and their storage swapped: every call takes what they hold then.
+    """
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._fields = self._desc = None
+        self.desc
+
+    @property
+    def desc(self) -> KvCacheDesc:
+        """The C struct of what the attributes hold now (not to be written to); raises where they do not fit."""
+        return self._read(False)
+
+    def check(self) -> KvCacheDesc:
+        """The same for a call: the tensors are on the current GPU."""
+        return self._read(True)
+
+    def _read(self, on_gpu: bool) -> KvCacheDesc:
+        import torch
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        fmt = {torch.bfloat16: 0, torch.int8: 1, torch.float8_e4m3fn: 2}.get(k.dtype)
+        if fmt is None or v.dtype is not k.dtype:
+            raise ZlError(1, "KvCache: k and v must both be torch.bfloat16, torch.int8 or torch.float8_e4m3fn")
+        shape, strides = k.shape, k.stride()
+        if len(shape) != 4 or v.shape != shape or v.stride() != strides or strides[3] != 1:
+            raise ZlError(1, "KvCache: k and v must be [n_pages, page_size, n_kv_heads, head_dim] with the same strides and contiguous rows")
+        if (ks is None) != (fmt == 0) or (vs is None) != (fmt == 0):
+            raise ZlError(1, "KvCache: an 8-bit cache has k_scale and v_scale, one in bf16 neither")
+        for name, t in (("k_scale", ks), ("v_scale", vs)):
+            if t is not None and (t.dtype is not torch.float32 or t.shape != shape[:3] or not t.is_contiguous()):
+                raise ZlError(1, f"KvCache: {name} must be a contiguous torch.float32 tensor [n_pages, page_size, n_kv_heads]")
+        if on_gpu:
+            for name, t in (("k", k), ("v", v), ("k_scale", ks), ("v_scale", vs)):
+                if t is not None:
+                    _on_gpu(f"KvCache: {name}", t)
+        # (a stride of a dimension of one entry may be any number)
+        page, token, head = (strides[i] if shape[i] > 1 else shape[3] for i in range(3))
+        fields = (k.data_ptr(), v.data_ptr(), _ptr(ks), _ptr(vs), page, token, head, shape[0], shape[1], shape[2], shape[3], fmt)
+        desc = self._desc
+        if fields != self._fields:
+            # a struct of its own per state: a call of another thread may be reading the one before
+            self._desc = desc = KvCacheDesc(*fields)
+            self._fields = fields
+        return desc
+
+
+class CacheBatch:
+    """zl_cache_batch: sequences over a cache.  int32 tensors on the GPU, read when a kernel runs:
+
+    cu_q    [n_seqs + 1]: rows [cu_q[s], cu_q[s+1]) are the new tokens of sequence s
+    kv_len  [n_seqs]: tokens of the sequence, the new ones included
+    pages   [n_seqs, max_pages]: the sequence's pages; a number outside the cache is a page without keys
+    prefix  [n_seqs]: keys that every new token sees, or None for causal order
+    max_q   the largest number of new tokens of a sequence, where it is known (it only chooses kernels)
+    """
+
+    def __init__(self, cu_q, kv_len, pages, prefix=None, max_q: int = 0):
+        self.cu_q, self.kv_len, self.pages, self.prefix, self.max_q = cu_q, kv_len, pages, prefix, max_q
+        self.check(0, False)
+
+    def check(self, total_q: int, on_gpu: bool = True) -> CacheBatchDesc:
+        """The C struct of what the attributes hold now, for token tensors of total_q rows; raises where they do not fit."""
+        cu, lens, pages, prefix = self.cu_q, self.kv_len, self.pages, self.prefix
+        n = lens.shape[0] if lens.dim() == 1 else -1
+        _ints("CacheBatch: kv_len", lens, (max(0, n),))
+        _ints("CacheBatch: cu_q", cu, (n + 1,))
+        if pages.dim() != 2 or pages.shape[0] != n:
+            raise ZlError(1, f"CacheBatch: pages must be [{n}, max_pages]")
+        _ints("CacheBatch: pages", pages)
+        if prefix is not None:
+            _ints("CacheBatch: prefix", prefix, (n,))
+        if on_gpu:
+            for name in ("cu_q", "kv_len", "pages", "prefix"):
+                t = getattr(self, name)
+                if t is not None:
+                    _on_gpu(f"CacheBatch: {name}", t)
+        max_q, = _int32s((self.max_q,))
+        return CacheBatchDesc(cu.data_ptr(), lens.data_ptr(), pages.data_ptr(), _ptr(prefix), n, pages.shape[1], total_q, max_q)
+
+
+def _token_rows(what: str, t, heads: int, dim: int) -> int:
+    """Stride of the rows of a bf16 tensor [tokens, heads, dim] whose rows are contiguous."""
+    import torch
+    shape, strides = t.shape, t.stride()
+    if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[1] != heads or shape[2] != dim:
+        raise ZlError(1, f"{what} must be a torch.bfloat16 tensor [tokens, {heads}, {dim}]")
+    if strides[2] != 1 or (heads > 1 and strides[1] != dim):
+        raise ZlError(1, f"{what}: heads and elements of a token must be contiguous")
+    _on_gpu(what, t)
+    return strides[0] if shape[0] > 1 else heads * dim
+
+
+def _packed_rows(what: str, t, heads: int, dim: int):
+    _token_rows(what, t, heads, dim)
+    if not t.is_contiguous():
+        raise ZlError(1, f"{what} must be contiguous")
+
+
+def cache_write(cache: KvCache, batch: CacheBatch, k, v, stream=None):
+    """zl_cache_write: the new tokens' k, v [total_q, n_kv_heads, head_dim] bf16 (slices of a packed tensor will do) go into
+    their places of the cache, quantised where it holds 8 bits."""
+    c = cache.check()
+    stride = _token_rows("k", k, c.n_kv_heads, c.head_dim)
+    if k.shape != v.shape or _token_rows("v", v, c.n_kv_heads, c.head_dim) != stride:
+        raise ZlError(1, "k and v must be of the same shape and strides")
+    b = batch.check(k.shape[0])
+    _check(_lib.zl_cache_write(ctypes.byref(c), ctypes.byref(b), k.data_ptr(), v.data_ptr(), stride, _stream_ptr(stream)), "zl_cache_write")
+
+
+def cache_read(cache: KvCache, batch: CacheBatch, cu_kv, k, v, first=None, stream=None):
+    """zl_cache_read: the tokens of sequence s from position first[s] on (None: 0) into rows [cu_kv[s], cu_kv[s+1]) of the
+    packed bf16 tensors k, v [total_kv, n_kv_heads, head_dim]; rows without a key become 0."""
+    c = cache.check()
+    _packed_rows("k", k, c.n_kv_heads, c.head_dim)
+    _packed_rows("v", v, c.n_kv_heads, c.head_dim)
+    if k.shape != v.shape:
+        raise ZlError(1, "k and v must be of the same shape")
+    b = batch.check(0)
+    _ints("cu_kv", cu_kv, (b.n_seqs + 1,))
+    _on_gpu("cu_kv", cu_kv)
+    if first is not None:
+        _ints("first", first, (b.n_seqs,))
+        _on_gpu("first", first)
+    _check(_lib.zl_cache_read(ctypes.byref(c), ctypes.byref(b), _ptr(first), cu_kv.data_ptr(), k.shape[0], k.data_ptr(), v.data_ptr(),
+                              _stream_ptr(stream)), "zl_cache_read")
+
+
+class CachedAttnHandle:
+    """Owns a ``zl_cached_attn*``: attention over caches of a number of heads, for every layer and batch."""
+
+    def __init__(self, ptr: int, n_heads: int, n_kv_heads: int, head_dim: int):
+        self._ptr = ctypes.c_void_p(ptr)
+        self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim
+
+    @property
+    def ptr(self):
+        return self._ptr
+
+    @property
+    def workspace_bytes(self) -> int:
+        """zl_cached_attn_workspace_bytes: workspace of cached_attn_fwd, whatever the batch."""
+        n = ctypes.c_size_t()
+        _check(_lib.zl_cached_attn_workspace_bytes(self._ptr, ctypes.byref(n)), "zl_cached_attn_workspace_bytes")
+        return int(n.value)
+
+    def last_device_status(self) -> Tuple[int, int]:
+        c, w = ctypes.c_int32(), ctypes.c_int32()
+        _check(_lib.zl_cached_attn_device_status(self._ptr, ctypes.byref(c), ctypes.byref(w)), "zl_cached_attn_device_status")
+        return c.value, w.value
+
+    def close(self):
+        if self._ptr:
+            _lib.zl_free_cached_attn(self._ptr)
+            self._ptr = ctypes.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def build_cached_attn(n_heads: int, n_kv_heads: int, head_dim: int, stream=None) -> CachedAttnHandle:
+    """zl_build_cached_attn: n_heads query heads, a multiple of n_kv_heads."""
+    n_heads, n_kv_heads, head_dim = _int32s((n_heads, n_kv_heads, head_dim))
+    out = ctypes.c_void_p()
+    _check(_lib.zl_build_cached_attn(n_heads, n_kv_heads, head_dim, _stream_ptr(stream), ctypes.byref(out)), "zl_build_cached_attn")
+    return CachedAttnHandle(out.value, n_heads, n_kv_heads, head_dim)
+
+
+def cached_attn_fwd(attn: CachedAttnHandle, cache: KvCache, batch: CacheBatch, q, scale: float, o, lse, workspace, stream=None):
+    """zl_cached_attn_fwd: attention of the new tokens q [total_q, n_heads, head_dim] over the cache, which holds their own keys
+    already; o like q (contiguous), lse fp32 [n_heads, total_q] or None, workspace of attn.workspace_bytes."""
+    import torch
+    c = cache.check()
+    stride = _token_rows("q", q, attn.n_heads, attn.head_dim)
+    _packed_rows("o", o, attn.n_heads, attn.head_dim)
+    if o.shape != q.shape:
+        raise ZlError(1, "o must be of q's shape")
+    if lse is not None:
+        if lse.dtype is not torch.float32 or tuple(lse.shape) != (attn.n_heads, q.shape[0]) or not lse.is_contiguous():
+            raise ZlError(1, f"lse must be a contiguous torch.float32 tensor [{attn.n_heads}, {q.shape[0]}]")
+        _on_gpu("lse", lse)
+    _on_gpu("workspace", workspace)
+    if not workspace.is_contiguous():
+        raise ZlError(1, "workspace must be contiguous")
+    b = batch.check(q.shape[0])
+    _check(_lib.zl_cached_attn_fwd(attn.ptr, ctypes.byref(c), ctypes.byref(b), q.data_ptr(), stride, scale, o.data_ptr(), _ptr(lse),
+                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "zl_cached_attn_fwd")
 
 
 NOALLOC_SCRATCH_BYTES = 64 * 1024 * 1024

@@ -52,11 +52,11 @@ namespace {
 
 std::atomic<int64_t> g_launches{0};
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+}  // namespace
 
-EncodeTiledFn get_encode_fn() {
+void zl::count_launch() { g_launches.fetch_add(1); }
+
+EncodeTiledFn zl::get_encode_fn() {
     static EncodeTiledFn fn = nullptr;
     static bool tried = false;
     if (!tried) {
@@ -69,6 +69,8 @@ EncodeTiledFn get_encode_fn() {
     }
     return fn;
 }
+
+namespace {
 
 // Tensor map over a packed [rows, H, d] bf16 tensor: box = 64 columns x 1 head x box_rows rows,
 // 128-byte swizzle, zero fill outside the tensor.

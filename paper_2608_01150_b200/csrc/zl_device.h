@@ -141,4 +141,57 @@ cudaError_t launch_merge(int head_dim, const MergeParams& p, int max_parts, int 
 cudaError_t launch_merge_rows(int head_dim, const MergeParams& p, int64_t n_rows, cudaStream_t stream);
 cudaError_t launch_wait_selftest(int32_t* status, uint64_t limit_ns, cudaStream_t stream);
 
+// ------------------------------------------------------------------------------------------------ paged cache
+// Keys and values in pages (zl_kv_cache); strides in bytes, a page has 1 << page_shift tokens.
+struct CacheView {
+    uint8_t* k;
+    uint8_t* v;
+    float* k_scale;  // [n_pages, page, n_kv_heads]; NULL where the cache holds bf16
+    float* v_scale;
+    int64_t page_stride, token_stride, head_stride;
+    int32_t n_pages, page_shift, n_kv_heads;
+};
+// A batch of sequences over it (zl_cache_batch).
+struct CacheBatch {
+    const int32_t* cu_q;
+    const int32_t* kv_len;
+    const int32_t* pages;
+    const int32_t* prefix;
+    int32_t n_seqs, max_pages, total_q;
+};
+struct CacheReadParams {
+    const int32_t* first;
+    const int32_t* cu_kv;
+    int32_t total_kv;
+    __nv_bfloat16* k;
+    __nv_bfloat16* v;
+};
+// Attention of a batch's new tokens over the cache.
+struct CachedParams {
+    CacheView c;
+    CacheBatch b;
+    const __nv_bfloat16* q;
+    int64_t q_stride;    // elements between token rows
+    int32_t n_heads, group;  // query heads, query heads per key head
+    float scale_log2;
+    __nv_bfloat16* o;
+    float* lse;          // may be NULL
+    float* part;         // two partial results per CTA
+    int32_t* part_count; // per CTA: finished parts of the item that is cut first in it; zero between launches
+    int32_t* status;
+};
+cudaError_t launch_cache_write(int head_dim, int format, const CacheView& c, const CacheBatch& b, const __nv_bfloat16* k,
+                               const __nv_bfloat16* v, int64_t row_stride, cudaStream_t stream);
+cudaError_t launch_cache_read(int head_dim, int format, const CacheView& c, const CacheBatch& b, const CacheReadParams& p,
+                              cudaStream_t stream);
+cudaError_t launch_cached_tokens(int head_dim, int format, const CachedParams& p, int grid, cudaStream_t stream);
+size_t cached_tokens_part_bytes(int head_dim);  // of a CTA's two partial results
+
+// Of the C-ABI layer.
+void count_launch();
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn get_encode_fn();
+
 }  // namespace zl
