@@ -625,6 +625,18 @@ def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, sc
            "zl_scored_attn_bwd_packed")
 
 
+def _look(t):
+    """What the checks of a call look at: a tensor with the same answers has passed them before."""
+    return None if t is None else (t.data_ptr(), t.dtype, t.shape, t.stride(), t.get_device())
+
+
+def _all_on_gpu(what: str, looks):
+    device = _current_device() if looks[0][4] >= 0 else -2
+    for x in looks:
+        if x is not None and x[4] != device:
+            raise ZlError(1, f"{what}: not all tensors are on the current GPU")
+
+
 def _on_gpu(what: str, t):
     """The tensor is on the current GPU, where the call's kernels run."""
     if not t.is_cuda or t.get_device() != _current_device():
@@ -650,19 +662,27 @@ class KvCache:
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self._fields = self._desc = None
+        self._seen = (None, None)
         self.desc
 
     @property
     def desc(self) -> KvCacheDesc:
         """The C struct of what the attributes hold now (not to be written to); raises where they do not fit."""
-        return self._read(False)
+        key = (_look(self.k), _look(self.v), _look(self.k_scale), _look(self.v_scale))
+        seen, desc = self._seen
+        if key != seen:
+            # a struct of its own per state: a call of another thread may be reading the one before
+            desc = self._read()
+            self._seen = (key, desc)
+        return desc
 
     def check(self) -> KvCacheDesc:
         """The same for a call: the tensors are on the current GPU."""
-        return self._read(True)
+        desc = self.desc
+        _all_on_gpu("KvCache", self._seen[0])
+        return desc
 
-    def _read(self, on_gpu: bool) -> KvCacheDesc:
+    def _read(self) -> KvCacheDesc:
         import torch
         k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
         fmt = {torch.bfloat16: 0, torch.int8: 1, torch.float8_e4m3fn: 2}.get(k.dtype)
@@ -676,19 +696,9 @@ class KvCache:
         for name, t in (("k_scale", ks), ("v_scale", vs)):
             if t is not None and (t.dtype is not torch.float32 or t.shape != shape[:3] or not t.is_contiguous()):
                 raise ZlError(1, f"KvCache: {name} must be a contiguous torch.float32 tensor [n_pages, page_size, n_kv_heads]")
-        if on_gpu:
-            for name, t in (("k", k), ("v", v), ("k_scale", ks), ("v_scale", vs)):
-                if t is not None:
-                    _on_gpu(f"KvCache: {name}", t)
         # (a stride of a dimension of one entry may be any number)
         page, token, head = (strides[i] if shape[i] > 1 else shape[3] for i in range(3))
-        fields = (k.data_ptr(), v.data_ptr(), _ptr(ks), _ptr(vs), page, token, head, shape[0], shape[1], shape[2], shape[3], fmt)
-        desc = self._desc
-        if fields != self._fields:
-            # a struct of its own per state: a call of another thread may be reading the one before
-            self._desc = desc = KvCacheDesc(*fields)
-            self._fields = fields
-        return desc
+        return KvCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(ks), _ptr(vs), page, token, head, *_int32s(shape), fmt)
 
 
 class CacheBatch:
@@ -699,14 +709,31 @@ class CacheBatch:
     pages   [n_seqs, max_pages]: the sequence's pages; a number outside the cache is a page without keys
     prefix  [n_seqs]: keys that every new token sees, or None for causal order
     max_q   the largest number of new tokens of a sequence, where it is known (it only chooses kernels)
+
+    The attributes can be changed: every call takes what they hold then.
     """
 
     def __init__(self, cu_q, kv_len, pages, prefix=None, max_q: int = 0):
         self.cu_q, self.kv_len, self.pages, self.prefix, self.max_q = cu_q, kv_len, pages, prefix, max_q
-        self.check(0, False)
+        self._seen = (None, None)
+        self._desc(0)
 
-    def check(self, total_q: int, on_gpu: bool = True) -> CacheBatchDesc:
-        """The C struct of what the attributes hold now, for token tensors of total_q rows; raises where they do not fit."""
+    def _desc(self, total_q: int) -> CacheBatchDesc:
+        key = (_look(self.cu_q), _look(self.kv_len), _look(self.pages), _look(self.prefix), self.max_q, total_q)
+        seen, desc = self._seen
+        if key != seen:
+            desc = self._read(total_q)
+            self._seen = (key, desc)
+        return desc
+
+    def check(self, total_q: int) -> CacheBatchDesc:
+        """The C struct of what the attributes hold now, for a call with token tensors of total_q rows; raises where they do
+        not fit or are not on the current GPU."""
+        desc = self._desc(total_q)
+        _all_on_gpu("CacheBatch", self._seen[0][:4])
+        return desc
+
+    def _read(self, total_q: int) -> CacheBatchDesc:
         cu, lens, pages, prefix = self.cu_q, self.kv_len, self.pages, self.prefix
         n = lens.shape[0] if lens.dim() == 1 else -1
         _ints("CacheBatch: kv_len", lens, (max(0, n),))
@@ -716,13 +743,8 @@ class CacheBatch:
         _ints("CacheBatch: pages", pages)
         if prefix is not None:
             _ints("CacheBatch: prefix", prefix, (n,))
-        if on_gpu:
-            for name in ("cu_q", "kv_len", "pages", "prefix"):
-                t = getattr(self, name)
-                if t is not None:
-                    _on_gpu(f"CacheBatch: {name}", t)
-        max_q, = _int32s((self.max_q,))
-        return CacheBatchDesc(cu.data_ptr(), lens.data_ptr(), pages.data_ptr(), _ptr(prefix), n, pages.shape[1], total_q, max_q)
+        n, width, total_q, max_q = _int32s((n, pages.shape[1], total_q, self.max_q))
+        return CacheBatchDesc(cu.data_ptr(), lens.data_ptr(), pages.data_ptr(), _ptr(prefix), n, width, total_q, max_q)
 
 
 def _token_rows(what: str, t, heads: int, dim: int) -> int:

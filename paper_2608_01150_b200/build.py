@@ -10,7 +10,8 @@ _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB = os.path.join(_PKG, "libzellige.so")
 SOURCES = ["zl_api.cu", "zl_fwd.cu", "zl_merge.cu", "zl_bwd.cu", "zl_bwd_pair.cu", "zl_scored_fwd.cu",
-           "zl_scored_bwd.cu", "zl_few_rows.cu", "zl_cache_rows.cu", "zl_cached_tokens.cu", "zl_cache_api.cu",
+           "zl_scored_bwd.cu", "zl_few_rows.cu", "zl_cache_rows.cu", "zl_cached_tokens.cu", "zl_cached_chunk.cu",
+           "zl_cache_api.cu",
            "zl_tasks.cpp"]
 
 

@@ -1,6 +1,7 @@
 // C-ABI layer of the paged cache: argument checks and launches.
 #include <cmath>
 #include <new>
+#include <utility>
 
 #include "zl_device.h"
 
@@ -10,12 +11,14 @@ struct zl_cached_attn {
     int32_t n_heads = 0, n_kv_heads = 0, head_dim = 0;
     int device = -1;  // -1: host-only handle (no CUDA device present)
     int n_sms = 0;
-    int32_t* d_words = nullptr;  // [0, 2): status; from kCounters on one counter per CTA
+    int32_t* d_words = nullptr;  // [0, 2): status; from kCounters on two counters per SM
 };
 
 namespace {
 
 constexpr int kCounters = 64;  // a line of its own for the status word
+
+size_t tokens_bytes(const zl_cached_attn& a) { return align_up((size_t)a.n_sms * cached_tokens_part_bytes(a.head_dim), 256); }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -50,6 +53,40 @@ zl_status view(const zl_kv_cache* cache, const zl_cache_batch* batch, bool token
 }
 
 bool rows_fit(int64_t rows, int32_t heads) { return rows * heads < (int64_t)1 << 32; }
+
+// Maps of the kernel for chunks.
+bool make_maps(const zl_kv_cache& x, const CachedParams& p, CUtensorMap* tq, CUtensorMap* tk, CUtensorMap* tv) {
+    EncodeTiledFn fn = get_encode_fn();
+    if (!fn) return false;
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    const cuuint64_t d = (cuuint64_t)x.head_dim;
+    {
+        const cuuint64_t dims[4] = {d, (cuuint64_t)p.group, (cuuint64_t)x.n_kv_heads, (cuuint64_t)p.b.total_q};
+        const cuuint64_t strides[3] = {d * 2, d * 2 * p.group, (cuuint64_t)p.q_stride * 2};
+        const cuuint32_t box[4] = {64, (cuuint32_t)p.group, 1, (cuuint32_t)(kTileQ / p.group)};
+        if (fn(tq, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<__nv_bfloat16*>(p.q), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return false;
+    }
+    const bool codes = x.format != ZL_CACHE_BF16;
+    const cuuint32_t rows = (cuuint32_t)(x.page_size < (codes ? 64 : 128) ? x.page_size : (codes ? 64 : 128));
+    const cuuint64_t heads = (cuuint64_t)x.n_kv_heads, tokens = (cuuint64_t)x.page_size, pages = (cuuint64_t)x.n_pages;
+    cuuint64_t dims[4] = {d, tokens, heads, pages}, strides[3] = {(cuuint64_t)p.c.token_stride, (cuuint64_t)p.c.head_stride, (cuuint64_t)p.c.page_stride};
+    const cuuint64_t row = d * (codes ? 1 : 2);
+    for (cuuint64_t& stride : strides) stride = stride ? stride : row;  // (of a dimension with one entry)
+    cuuint32_t box[4] = {codes ? (cuuint32_t)d : 64u, rows, 1, 1};
+    if (p.head_first) {
+        std::swap(dims[1], dims[2]);
+        std::swap(strides[0], strides[1]);
+        std::swap(box[1], box[2]);
+    }
+    const CUtensorMapSwizzle swizzle = codes && x.head_dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B;
+    for (int i = 0; i < 2; ++i)
+        if (fn(i == 0 ? tk : tv, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, i == 0 ? p.c.k : p.c.v, dims, strides, box, ones,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return false;
+    return true;
+}
 
 // No device, or one that the kernels are not built for.
 zl_status usable_device() {
@@ -124,7 +161,7 @@ zl_status zl_build_cached_attn(int32_t n_heads, int32_t n_kv_heads, int32_t head
         return ZL_ERR_CUDA;
     }
     if (major != 10) { delete h; return ZL_ERR_UNSUPPORTED; }
-    const size_t bytes = (size_t)(kCounters + n_sms) * sizeof(int32_t);
+    const size_t bytes = (size_t)(kCounters + 2 * n_sms) * sizeof(int32_t);
     if (cudaMalloc(&h->d_words, bytes) != cudaSuccess) { delete h; return ZL_ERR_CUDA; }
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (cudaMemsetAsync(h->d_words, 0, bytes, cs) != cudaSuccess || cudaStreamSynchronize(cs) != cudaSuccess) {
@@ -146,7 +183,7 @@ void zl_free_cached_attn(zl_cached_attn* attn) {
 
 zl_status zl_cached_attn_workspace_bytes(const zl_cached_attn* attn, size_t* bytes) {
     if (!attn || !bytes) return ZL_ERR_INVALID_ARG;
-    *bytes = align_up((size_t)attn->n_sms * cached_tokens_part_bytes(attn->head_dim), 256);
+    *bytes = tokens_bytes(*attn) + align_up((size_t)attn->n_sms * cached_chunk_part_bytes(attn->head_dim), 256);
     return ZL_OK;
 }
 
@@ -160,7 +197,7 @@ zl_status zl_cached_attn_device_status(const zl_cached_attn* attn, int32_t* code
     zl_status st = ZL_OK;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(words, attn->d_words, sizeof(words), cudaMemcpyDeviceToHost) != cudaSuccess)
         st = ZL_ERR_CUDA;
-    if (st == ZL_OK && words[0] != 0 && cudaMemset(attn->d_words, 0, (size_t)(kCounters + attn->n_sms) * sizeof(int32_t)) != cudaSuccess)
+    if (st == ZL_OK && words[0] != 0 && cudaMemset(attn->d_words, 0, (size_t)(kCounters + 2 * attn->n_sms) * sizeof(int32_t)) != cudaSuccess)
         st = ZL_ERR_CUDA;
     cudaSetDevice(prev);
     *code = words[0];
@@ -197,10 +234,30 @@ zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cach
     p.lse = lse;
     p.part = static_cast<float*>(workspace);
     p.part_count = attn->d_words + kCounters;
+    p.chunk_part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + tokens_bytes(*attn));
+    p.chunk_count = p.part_count + attn->n_sms;
     p.status = attn->d_words;
-    if (launch_cached_tokens(attn->head_dim, cache->format, p, attn->n_sms, static_cast<cudaStream_t>(stream)) != cudaSuccess)
-        return ZL_ERR_CUDA;
-    count_launch();
+    // Sequences of more than 16 rows per key head are the chunk kernel's.  Where max_q says that there are none, or that all
+    // are of that kind (as many rows as the longest times their number), the other kernel is not launched.
+    const int32_t max_q = batch->max_q;
+    const bool few = max_q > 0 && (int64_t)max_q * p.group <= kTokenRows;
+    const bool all_long = !few && max_q > 0 && (int64_t)max_q * p.b.n_seqs == p.b.total_q;
+    // a cache without a page has no key, and nothing to describe to the copy engine
+    const bool chunk = !few && p.c.n_pages > 0 && p.b.max_pages > 0;
+    p.split = chunk && !all_long;
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    if (chunk) {
+        // dimensions in the order of their strides
+        p.head_first = p.c.head_stride < p.c.token_stride;
+        CUtensorMap tq, tk, tv;
+        if (!make_maps(*cache, p, &tq, &tk, &tv)) return ZL_ERR_CUDA;
+        if (launch_cached_chunk(attn->head_dim, cache->format, tq, tk, tv, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
+        count_launch();
+    }
+    if (!chunk || p.split) {
+        if (launch_cached_tokens(attn->head_dim, cache->format, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
+        count_launch();
+    }
     return ZL_OK;
 }
 

@@ -1,0 +1,863 @@
+// Attention of chunks of new tokens over the paged cache (sm_100a): the products of many rows with every key, on the tensor cores.
+//
+// The rows of a key head are its sequence's new tokens times the query heads of its group; a tile takes as many whole tokens as
+// fit 128 rows, so that one box of Q holds a tile.  An item is two such tiles (or the one that is left) of a sequence and key
+// head.  All CTAs (one per SM) walk one line of work, measured in keys times tiles, and each takes an equal stretch of it,
+// wherever that cuts an item; the lengths are read when the kernel runs.  Stretches are found from sums in closed form: block b
+// of a sequence sees min(keys, max(prefix, pos0 + (b + 1) tokens)) keys.
+//   warp 0       TMA producer: Q once per item, K and V page by page through shared-memory rings
+//   warp 2       walks the line and hands the items' descriptions to the others
+//   warp 1       MMA issuer: S_x = Q K^T, O_x += P_x V (P read from TMEM), one step two ahead of the other
+//   warps 4-11   softmax, a thread per row; with two query tiles warpgroup x takes tile x, with one tile it takes key tiles x,
+//                x + 2, ... and both accumulators are joined at the end
+//   warps 12-15  (8-bit caches) codes become bf16, exactly, on their way from the ring of codes to the rings of K and V; the scale of
+//                a key multiplies its column of S, the scale of a value its column of P, in fp32
+// An item that lies in several CTAs leaves its parts in the workspace, and the one that finishes last joins them in the order
+// of the CTAs.
+#include "zl_cache.cuh"
+
+namespace zl {
+
+using namespace cache;
+
+namespace {
+
+constexpr uint64_t kWaitLimitNs = 4000000000ull;
+constexpr float kRescaleThresholdLog2 = 8.f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kMaskRing = 8;   // key tiles whose masks are kept: more than can be under way
+constexpr int32_t kItemCost = 512;   // start and end of an item, in keys times tiles
+constexpr int64_t kLeastUnits = 1024;  // least stretch of a CTA
+
+// A CTA's part of an item, as warp 2 hands it to the other warps.
+struct alignas(16) Item {
+    int32_t s, head, tile0, tile1;       // sequence, key head, key tiles of this part (tile1 < 0: no more items)
+    int32_t tok0, tokens, keys, two;     // new tokens, keys that they see, two query tiles
+    int32_t q0, pos0, seq_keys, prefix;  // SeqView
+    int32_t c_first, c_last;             // the CTAs that have parts of it
+    int32_t place_first, pad_;           // the first of them keeps its part in place 1 (its stretch begins before) or 0
+    __device__ __forceinline__ SeqView seq() const { return {q0, 0, pos0, seq_keys, prefix}; }
+    __device__ __forceinline__ int32_t place(int32_t cta) const { return cta == c_first ? place_first : 0; }
+};
+constexpr int kItems = 4;  // descriptions under way
+
+template <int D, int kFormat>
+struct ChunkSmem {
+    static constexpr bool kCodes = kFormat != ZL_CACHE_BF16;
+    static constexpr int kTileBytes = kTileKV * D * 2;  // one 128-row tile of Q, K or V
+    static constexpr int kBoxBytes = kTileKV * 128;     // 128 rows x 64 bf16
+    static constexpr int kBoxes = D / 64;
+    static constexpr int kStages = D == 128 ? 2 : (kCodes ? 4 : 5);
+    // A tile's K is prepared once V of the tile two before it has its place, which P V of kStages tiles earlier gave up: until
+    // then masks and scales of a tile may be read.
+    static constexpr int kScaleRing = D == 128 ? 4 : 8;
+    static_assert(kScaleRing >= kStages + 2 || !kCodes, "scales of a tile are kept until its softmax is done");
+    static_assert(kMaskRing >= kStages + 2, "masks of a tile are kept until its P V is done");
+    static constexpr int kRawRows = 64;                 // codes travel in halves of a tile
+    static constexpr int kRawBytes = kRawRows * D;
+    static constexpr int kRaw = !kCodes ? 1 : (D == 128 ? 3 : 6);
+    alignas(1024) uint8_t q[2][kTileBytes];
+    alignas(1024) uint8_t k[kStages][kTileBytes];
+    alignas(1024) uint8_t v[kStages][kTileBytes];
+    alignas(1024) uint8_t raw[kRaw][kCodes ? kRawBytes : 16];
+    alignas(16) float scale_k[kCodes ? kScaleRing : 1][kTileKV], scale_v[kCodes ? kScaleRing : 1][kTileKV];
+    alignas(16) uint32_t mask[kMaskRing][4];            // keys of a tile that exist
+    Item items[kItems];
+    float2 stat[2][kTileQ];                             // per warpgroup and row: reference maximum (raw scores), sum
+    alignas(8) uint64_t q_full, q_empty;
+    uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], raw_full[kRaw], raw_empty[kRaw];
+    uint64_t s_full[2], p_half[2][2], o_full[2], tile_full[kMaskRing];
+    uint64_t stat_full, join_done, part_bar, item_full[kItems], item_empty[kItems];
+    int64_t scan[16], start_base, total;
+    int32_t start_seq, ticket;
+    uint32_t tmem_base;
+    volatile int32_t abort_flag;
+};
+
+template <int D>
+constexpr int kPartTileFloats = kTileQ * (D + 2);  // maxima, sums, then the unnormalised output as [D / 4][row] of four
+
+// ------------------------------------------------------------------------------------------------ the line of work
+struct Geometry {
+    int32_t tokens;  // whole tokens of a tile
+    int32_t heads;
+    bool rest_only;  // sequences of at most 16 rows are another kernel's
+    __device__ __forceinline__ explicit Geometry(const CachedParams& p)
+        : tokens(kTileQ / p.group), heads(p.c.n_kv_heads), rest_only(p.split != 0) {}
+};
+
+struct SeqLine {
+    SeqView v;
+    int32_t blocks;
+    __device__ __forceinline__ SeqLine(const CachedParams& p, const Geometry& g, int s) : v(load_seq(p.b, p.c.page_shift, s)) {
+        blocks = (v.q_len + 2 * g.tokens - 1) / (2 * g.tokens);
+        if (g.rest_only && (int64_t)v.q_len * p.group <= kTokenRows) blocks = 0;
+    }
+    __device__ __forceinline__ int32_t block_tokens(const Geometry& g, int b) const { return min(2 * g.tokens, v.q_len - b * 2 * g.tokens); }
+    __device__ __forceinline__ int32_t block_keys(const Geometry& g, int b) const {
+        return keys_seen(v, b * 2 * g.tokens + block_tokens(g, b) - 1);
+    }
+    __device__ __forceinline__ int64_t block_cost(const Geometry& g, int b) const {
+        return kItemCost + (int64_t)block_keys(g, b) * (block_tokens(g, b) > g.tokens ? 2 : 1);
+    }
+    // Cost of blocks 0 .. b - 1 for one head, all of them full: sum of 2 * min(keys, max(prefix, pos0 + (i + 1) T)).
+    __device__ __forceinline__ int64_t cost_before(const Geometry& g, int b) const {
+        const int32_t T = 2 * g.tokens;
+        const int64_t by_prefix = min(v.keys, max(v.prefix, 0));
+        int64_t i0 = b, i1 = b;  // blocks bound by the prefix, by the order or the prefix
+        if (by_prefix < v.keys) {
+            i0 = by_prefix < v.pos0 ? 0 : min((int64_t)b, (by_prefix - v.pos0) / T);
+            i1 = v.keys < v.pos0 ? i0 : max(i0, min((int64_t)b, ((int64_t)v.keys - v.pos0) / T));
+        }
+        const int64_t keys = i0 * by_prefix + (i1 - i0) * v.pos0 + (i1 * (i1 + 1) - i0 * (i0 + 1)) / 2 * T + (b - i1) * (int64_t)v.keys;
+        return (int64_t)b * kItemCost + 2 * keys;
+    }
+    __device__ __forceinline__ int64_t units(const Geometry& g) const {
+        return blocks == 0 ? 0 : g.heads * (cost_before(g, blocks - 1) + block_cost(g, blocks - 1));
+    }
+};
+
+// The items of a CTA's stretch [begin, end), in order.
+struct ItemWalk {
+    const CachedParams& p;
+    const Geometry g;
+    SeqLine line;
+    int64_t base, at, end, per;
+    int32_t s;
+
+    __device__ __forceinline__ ItemWalk(const CachedParams& p_, int32_t s_, int64_t base_, int64_t per_, int64_t total)
+        : p(p_), g(p_), line(p_, g, s_), base(base_), at(per_ * blockIdx.x), per(per_), s(s_) {
+        end = min(at + per, total);
+    }
+    __device__ __forceinline__ bool next(Item& w) {
+        while (at < end) {
+            int64_t units = line.units(g);
+            while (at >= base + units) {
+                base += units;
+                line = SeqLine(p, g, ++s);
+                units = line.units(g);
+            }
+            int lo = 0, hi = line.blocks - 1;  // the last block that begins at or before `at`
+            const int64_t in = at - base;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (g.heads * line.cost_before(g, mid) <= in) lo = mid; else hi = mid - 1;
+            }
+            const int64_t cost = line.block_cost(g, lo);
+            const int64_t block0 = g.heads * line.cost_before(g, lo);
+            const int32_t head = (int32_t)((in - block0) / cost);
+            const int64_t item0 = base + block0 + head * cost;
+            const int64_t stop = min(end, item0 + cost);
+            const int32_t keys = line.block_keys(g, lo), tokens = line.block_tokens(g, lo);
+            const bool two = tokens > g.tokens;
+            const int32_t tiles = (keys + kTileKV - 1) / kTileKV;
+            const int64_t step = kTileKV * (two ? 2 : 1), first = item0 + kItemCost;  // tile t lies where its first key does
+            auto tiles_before = [&](int64_t u) { return u <= first ? 0 : (int32_t)min((int64_t)tiles, (u - first + step - 1) / step); };
+            const int32_t tile0 = tiles_before(at), tile1 = tiles_before(stop);
+            const bool starts_here = at == item0;
+            at = stop;
+            if (tile1 <= tile0 && !(tiles == 0 && starts_here)) continue;  // only the start of an item whose tiles lie in later CTAs
+            const int32_t c_first = tiles > 0 ? (int32_t)(first / per) : 0;
+            w = Item{s, head, tile0, tile1, lo * 2 * g.tokens, tokens, keys, two ? 1 : 0, line.v.q0, line.v.pos0, line.v.keys, line.v.prefix,
+                     c_first, tiles > 0 ? (int32_t)((first + (tiles - 1) * step) / per) : 0, first > c_first * per ? 1 : 0, 0};
+            return true;
+        }
+        return false;
+    }
+};
+
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u); }
+
+__device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_flag, int where) {
+    *abort_flag = 1;
+    if (atomicCAS(status, 0, (int)ZL_ERR_TIMEOUT) == 0) status[1] = where;
+}
+static __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, const volatile int32_t* abort_flag) {
+    return mbar_wait_slow(bar, parity, kWaitLimitNs, abort_flag);
+}
+
+// All lanes of a warp wait; the outcome is warp-uniform and the warp reconverges.
+#define ZL_WAIT_WARP(bar, parity, site)                                                                       \
+    do {                                                                                                      \
+        const bool ok_ = mbar_try_wait((bar), (parity)) || wait_slow((bar), (parity), &sm.abort_flag);      \
+        if (!__all_sync(0xffffffffu, ok_)) {                                                                  \
+            report(p.status, &sm.abort_flag, 7000 + (site));                                                 \
+            goto teardown;                                                                                    \
+        }                                                                                                     \
+    } while (0)
+// The same from the warps that hold tiles in registers.
+#define ZL_WAIT_REGS(bar, parity, site)                                            \
+    do {                                                                           \
+        const bool ok_ = mbar_wait((bar), (parity), kWaitLimitNs, &sm.abort_flag); \
+        if (!__all_sync(0xffffffffu, ok_)) {                                       \
+            report(p.status, &sm.abort_flag, 7000 + (site));                      \
+            goto teardown;                                                         \
+        }                                                                          \
+    } while (0)
+
+// for (every item `w` of the CTA) { ... ZL_ITEM_DONE }
+#define ZL_FOR_ITEMS(wait_, site)                                          \
+    for (uint32_t it_ = 0;; ++it_) {                                       \
+        const uint32_t slot_ = it_ % kItems;                               \
+        wait_(&sm.item_full[slot_], (it_ / kItems) & 1, site);             \
+        const Item& w = sm.items[slot_];                                   \
+        if (w.tile1 < 0) break;                                            \
+        const int n = w.tile1 - w.tile0;
+#define ZL_ITEM_DONE                                                       \
+        __syncwarp();                                                      \
+        if (lane == 0) mbar_arrive(&sm.item_empty[slot_]);                 \
+    }
+
+template <int D, int kFormat>
+__global__ void __launch_bounds__(kFormat == ZL_CACHE_BF16 ? 384 : 512, 1)
+zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                       const __grid_constant__ CUtensorMap tm_v, const CachedParams p) {
+    using Smem = ChunkSmem<D, kFormat>;
+    constexpr bool kCodes = Smem::kCodes;
+    constexpr int kBoxes = Smem::kBoxes, kStages = Smem::kStages, kRaw = Smem::kRaw;
+    constexpr int kThreads = kCodes ? 512 : 384;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+
+    // TMEM columns: S_0 [0,128), S_1 [128,256), O_0 [256,256+D), O_1 [384,384+D); P_x over the first half of S_x
+    constexpr uint32_t kColS = 0, kColO = 256, kTmemCols = 512;
+
+    if ((smem_u32(smem_raw) & 1023u) != 0) {  // swizzled tiles need a 1024-byte aligned base
+        if (threadIdx.x == 0 && atomicCAS(p.status, 0, (int)ZL_ERR_CUDA) == 0) p.status[1] = 7999;
+        return;
+    }
+    if (threadIdx.x == 0) {
+        mbar_init(&sm.q_full, 1);
+        mbar_init(&sm.q_empty, 1);
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&sm.s_full[x], 1);
+            mbar_init(&sm.p_half[x][0], 128);
+            mbar_init(&sm.p_half[x][1], 128);
+            mbar_init(&sm.o_full[x], 1);
+        }
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&sm.k_full[s], kCodes ? 128 : 1);
+            mbar_init(&sm.k_empty[s], 1);
+            mbar_init(&sm.v_full[s], kCodes ? 128 : 1);
+            mbar_init(&sm.v_empty[s], 1);
+        }
+        for (int s = 0; s < kRaw; ++s) {
+            mbar_init(&sm.raw_full[s], 1);
+            mbar_init(&sm.raw_empty[s], 128);
+        }
+        for (int s = 0; s < kMaskRing; ++s) mbar_init(&sm.tile_full[s], kCodes ? 128 : 1);
+        mbar_init(&sm.stat_full, 256);
+        mbar_init(&sm.join_done, 256);
+        mbar_init(&sm.part_bar, 256);
+        for (int i = 0; i < kItems; ++i) {
+            mbar_init(&sm.item_full[i], 1);
+            mbar_init(&sm.item_empty[i], kCodes ? 14 : 10);  // warps that read it
+        }
+        sm.abort_flag = 0;
+        fence_mbar_init();
+        prefetch_tmap(&tm_q);
+        prefetch_tmap(&tm_k);
+        prefetch_tmap(&tm_v);
+    }
+    if (warp == 1) {
+        tmem_alloc(&sm.tmem_base, kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem_base;
+    grid_release();
+    grid_wait();
+
+    // ---- where this CTA's stretch begins
+    {
+        const Geometry g(p);
+        const int tid = threadIdx.x, chunk = (p.b.n_seqs + kThreads - 1) / kThreads;
+        const int s_end = min((tid + 1) * chunk, p.b.n_seqs);
+        int64_t mine = 0;
+        for (int s = tid * chunk; s < s_end; ++s) mine += SeqLine(p, g, s).units(g);
+        int64_t upto = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += x;
+        }
+        if (lane == 31) sm.scan[warp] = upto;
+        __syncthreads();
+        int64_t before = 0, total = 0;
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) {
+            if (w < warp) before += sm.scan[w];
+            total += sm.scan[w];
+        }
+        const int64_t per = max((total + gridDim.x - 1) / gridDim.x, kLeastUnits);
+        const int64_t begin = per * blockIdx.x;
+        int64_t at = before + upto - mine;
+        if (tid == 0) sm.total = total;
+        if (at <= begin && begin < at + mine) {  // one thread
+            int s = tid * chunk;
+            while (true) {
+                const int64_t n = SeqLine(p, g, s).units(g);
+                if (begin < at + n) break;
+                at += n;
+                ++s;
+            }
+            sm.start_seq = s;
+            sm.start_base = at;
+        }
+        __syncthreads();
+    }
+    const int64_t total = sm.total;
+    const int64_t per = max((total + gridDim.x - 1) / gridDim.x, kLeastUnits);
+    const bool idle = per * blockIdx.x >= total;
+
+    if (idle) {
+        // nothing to do
+    } else if (warp < 4) {
+        if constexpr (kCodes) reg_dec<64>(); else reg_dec<72>();
+        if (warp == 2) {
+            // -------------------------------------------------------------- the line of work
+            ItemWalk walk(p, sm.start_seq, sm.start_base, per, total);
+            bool more = true;
+            for (uint32_t it = 0; more; ++it) {
+                Item w;
+                more = walk.next(w);
+                if (!more) w.tile1 = -1;
+                ZL_WAIT_WARP(&sm.item_empty[it % kItems], ((it / kItems) & 1) ^ 1, 9);
+                if (lane == 0) {
+                    sm.items[it % kItems] = w;
+                    mbar_arrive(&sm.item_full[it % kItems]);
+                }
+            }
+        } else if (warp == 0) {
+            // -------------------------------------------------------------- TMA producer (a lane per page)
+            const int32_t tile_tokens = kTileQ / p.group;
+            constexpr int kSpan = kCodes ? Smem::kRawRows : kTileKV;  // rows of a load
+            const int page = 1 << p.c.page_shift;
+            const int box = min(page, kSpan);
+            const int row = lane * box;          // this lane's rows of a load: [row, row + box)
+            const bool has_rows = row < kSpan;
+            uint32_t item_cnt = 0, kv_cnt = 0, raw_cnt = 0;
+            auto page_of = [&](const Item& w, int32_t pos) { return has_rows && pos < w.keys ? page_at(p.b, p.c, w.s, pos) : -1; };
+            auto load = [&](const Item& w, uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, int32_t pg, int32_t pos) {
+                const uint32_t n = __popc(__ballot_sync(0xffffffffu, pg >= 0));
+                if (lane == 0) mbar_arrive_expect_tx(bar, n * box * (kCodes ? D : D * 2));
+                __syncwarp();
+                if (pg >= 0) {
+                    const int32_t in = pos & (page - 1);
+                    const int32_t c1 = p.head_first ? w.head : in, c2 = p.head_first ? in : w.head;
+                    if constexpr (kCodes) {
+                        tma_load_4d(dst + row * D, tm, bar, 0, c1, c2, pg);
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < kBoxes; ++b) tma_load_4d(dst + b * Smem::kBoxBytes + row * 128, tm, bar, b * 64, c1, c2, pg);
+                    }
+                }
+            };
+            ZL_FOR_ITEMS(ZL_WAIT_WARP, 6)
+                if (n > 0) {
+                ZL_WAIT_WARP(&sm.q_empty, (item_cnt & 1) ^ 1, 1);
+                ++item_cnt;
+                if (lane == 0) {
+                    const int q_tiles = w.two ? 2 : 1;
+                    mbar_arrive_expect_tx(&sm.q_full, q_tiles * tile_tokens * p.group * D * 2);
+                    for (int x = 0; x < q_tiles; ++x)
+                        for (int b = 0; b < kBoxes; ++b)
+                            tma_load_4d(sm.q[x] + b * Smem::kBoxBytes, &tm_q, &sm.q_full, b * 64, 0, w.head, w.q0 + w.tok0 + x * tile_tokens);
+                }
+                if constexpr (kCodes) {
+                    // K runs one tile ahead of V
+                    int32_t pg_k[2], pg_v[2] = {-1, -1};
+                    for (int h = 0; h < 2; ++h) pg_k[h] = page_of(w, w.tile0 * kTileKV + h * kSpan + row);
+                    for (int j = 0; j <= n; ++j) {
+                        int32_t pg_next[2];
+                        for (int h = 0; h < 2; ++h) pg_next[h] = j + 1 < n ? page_of(w, (w.tile0 + j + 1) * kTileKV + h * kSpan + row) : -1;
+                        for (int m = 0; m < 2; ++m) {
+                            if (m == 0 ? j == n : j == 0) continue;
+                            for (int h = 0; h < 2; ++h, ++raw_cnt) {
+                                const uint32_t slot = raw_cnt % kRaw;
+                                ZL_WAIT_WARP(&sm.raw_empty[slot], ((raw_cnt / kRaw) & 1) ^ 1, 2);
+                                load(w, sm.raw[slot], m == 0 ? &tm_k : &tm_v, &sm.raw_full[slot], m == 0 ? pg_k[h] : pg_v[h],
+                                     (w.tile0 + j - m) * kTileKV + h * kSpan + row);
+                            }
+                        }
+                        for (int h = 0; h < 2; ++h) {
+                            pg_v[h] = pg_k[h];
+                            pg_k[h] = pg_next[h];
+                        }
+                    }
+                } else {
+                    int32_t pg_k = page_of(w, w.tile0 * kTileKV + row), pg_v = -1;
+                    for (int j = 0; j <= n; ++j) {
+                        const int32_t key0 = (w.tile0 + j) * kTileKV;
+                        const int32_t pg_next = j + 1 < n ? page_of(w, key0 + kTileKV + row) : -1;
+                        if (j < n) {
+                            const uint32_t c = kv_cnt + j, st = c % kStages;
+                            ZL_WAIT_WARP(&sm.k_empty[st], ((c / kStages) & 1) ^ 1, 2);
+                            const int32_t end_row = pg_k >= 0 ? row + min(box, w.keys - (key0 + row)) : 0;  // first row without a key
+                            uint32_t word = 0;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t all = __reduce_or_sync(0xffffffffu, pg_k >= 0 ? low_bits(end_row - 32 * i) & ~low_bits(row - 32 * i) : 0u);
+                                if (lane == i) word = all;
+                            }
+                            if (lane < 4) sm.mask[c % kMaskRing][lane] = word;
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&sm.tile_full[c % kMaskRing]);
+                            load(w, sm.k[st], &tm_k, &sm.k_full[st], pg_k, key0 + row);
+                        }
+                        if (j > 0) {
+                            const uint32_t c = kv_cnt + j - 1, st = c % kStages;
+                            ZL_WAIT_WARP(&sm.v_empty[st], ((c / kStages) & 1) ^ 1, 3);
+                            load(w, sm.v[st], &tm_v, &sm.v_full[st], pg_v, key0 - kTileKV + row);
+                        }
+                        pg_v = pg_k;
+                        pg_k = pg_next;
+                    }
+                    kv_cnt += n;
+                }
+                }
+            ZL_ITEM_DONE
+        } else if (warp == 1) {
+            // -------------------------------------------------------------- MMA issuer (whole warp, one elected lane issues)
+            const bool mma_lane = elect_one();
+            constexpr uint32_t idesc_s = make_idesc_bf16(kTileQ, kTileKV, 0, 0);
+            constexpr uint32_t idesc_o = make_idesc_bf16(kTileQ, D, 0, 1);
+            const uint64_t dq0 = make_desc_sw128(smem_u32(sm.q[0]), 16, 1024);
+            const uint64_t dk0 = make_desc_sw128(smem_u32(sm.k[0]), 16, 1024);
+            const uint64_t dv0 = make_desc_sw128(smem_u32(sm.v[0]), Smem::kBoxBytes, 1024);  // V is the MN-major B operand
+            constexpr uint32_t kTileStep = Smem::kTileBytes >> 4;
+            uint32_t item_cnt = 0, kv_cnt = 0, pa_cnt = 0, pb_cnt = 0;
+            ZL_FOR_ITEMS(ZL_WAIT_WARP, 7)
+                const bool two = w.two != 0;
+                const int steps = two ? 2 * n : n;
+                if (steps > 0) {
+                ZL_WAIT_WARP(&sm.q_full, item_cnt & 1, 11);
+                ++item_cnt;
+                // step u: S of step u, then (before it) P V of step u - 2; x is the accumulator, j the key tile
+                for (int u = 0; u < steps + 2; ++u) {
+                    const int x = u & 1;
+                    if (u >= 2) {
+                        const int j = two ? (u - 2) >> 1 : u - 2;
+                        const uint32_t c = kv_cnt + j, st = c % kStages;
+                        if (!two || x == 0) {
+                            ZL_WAIT_WARP(&sm.v_full[st], (c / kStages) & 1, 12);
+                            if constexpr (!kCodes) {
+                                // rows without a key may hold anything, NaN too: zeros, before they meet their weight of 0
+                                const uint4 m4 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                                if ((m4.x & m4.y & m4.z & m4.w) != 0xffffffffu) {
+                                    const uint32_t words[4] = {m4.x, m4.y, m4.z, m4.w};
+                                    for (int i = 0; i < 4; ++i) {
+                                        if ((words[i] >> lane) & 1) continue;
+                                        const uint32_t at = smem_u32(sm.v[st]) + (i * 32 + lane) * 128;
+#pragma unroll 1
+                                        for (int e = 0; e < 8 * kBoxes; ++e)
+                                            st_shared_v4(at + (e >> 3) * Smem::kBoxBytes + (((e + lane) & 7) << 4), 0, 0, 0, 0);
+                                    }
+                                    fence_proxy_async_smem();
+                                    __syncwarp();
+                                }
+                            }
+                        }
+                        const uint64_t dv = dv0 + st * kTileStep;
+#pragma unroll 1
+                        for (int half = 0; half < 2; ++half) {
+                            ZL_WAIT_WARP(&sm.p_half[x][half], (x == 0 ? pa_cnt : pb_cnt) & 1, 13);
+                            tc_fence_after();
+#pragma unroll
+                            for (int ks = 0; ks < kTileKV / 32; ++ks) {
+                                const int at = half * (kTileKV / 32) + ks;
+                                if (mma_lane) mma_ts(tmem + kColO + x * 128, tmem + kColS + x * 128 + at * 8, dv + at * (2048 >> 4),
+                                                     idesc_o, u > 3 || half > 0 || ks > 0);
+                            }
+                        }
+                        if (x == 0) ++pa_cnt; else ++pb_cnt;
+                        if (!two || x == 1) if (mma_lane) mma_commit(&sm.v_empty[st]);
+                        if (u >= steps) if (mma_lane) mma_commit(&sm.o_full[x]);  // the accumulator's last step
+                    }
+                    if (u < steps) {
+                        const int j = two ? u >> 1 : u;
+                        const uint32_t c = kv_cnt + j, st = c % kStages;
+                        if (!two || x == 0) ZL_WAIT_WARP(&sm.k_full[st], (c / kStages) & 1, 15);
+                        tc_fence_after();
+                        const uint64_t dq = dq0 + (two ? x : 0) * kTileStep, dk = dk0 + st * kTileStep;
+#pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks) {  // over P_x of step u - 2: ordered after P_x V on the tensor pipe
+                            const uint32_t off = ((ks / 4) * Smem::kBoxBytes + (ks % 4) * 32) >> 4;
+                            if (mma_lane) mma_ss(tmem + kColS + x * 128, dq + off, dk + off, idesc_s, ks > 0);
+                        }
+                        if (mma_lane) mma_commit(&sm.s_full[x]);
+                        if (!two || x == 1) if (mma_lane) mma_commit(&sm.k_empty[st]);
+                        if (u + 1 == steps) if (mma_lane) mma_commit(&sm.q_empty);
+                    }
+                }
+                kv_cnt += n;
+                }
+            ZL_ITEM_DONE
+        }
+    } else if (kCodes && warp >= 12) {
+        // ------------------------------------------------------------------ codes to bf16
+        reg_dec<64>();
+        if constexpr (kCodes) {
+            const int t = threadIdx.x - 384;
+            uint32_t kv_cnt = 0, raw_cnt = 0;
+            // scales of this thread's key (key t of the tile), zeros without one
+            auto scales_of = [&](const Item& w, int32_t key, bool& there) {
+                const int32_t pg = key < w.keys ? page_at(p.b, p.c, w.s, key) : -1;
+                there = pg >= 0;
+                float2 r = make_float2(0.f, 0.f);
+                if (there) {
+                    const int64_t at = (((int64_t)pg << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1))) * p.c.n_kv_heads + w.head;
+                    r = make_float2(__ldg(p.c.k_scale + at), __ldg(p.c.v_scale + at));
+                }
+                return r;
+            };
+            ZL_FOR_ITEMS(ZL_WAIT_WARP, 8)
+                if (n > 0) {
+                bool there;
+                float2 sc = scales_of(w, w.tile0 * kTileKV + t, there);
+                for (int j = 0; j <= n; ++j) {
+                    for (int m = 0; m < 2; ++m) {
+                        if (m == 0 ? j == n : j == 0) continue;
+                        const uint32_t c = kv_cnt + j - m, st = c % kStages;
+                        uint64_t* const empty = m == 0 ? &sm.k_empty[st] : &sm.v_empty[st];
+                        ZL_WAIT_WARP(empty, ((c / kStages) & 1) ^ 1, 4);
+                        if (m == 0) {
+                            const uint32_t word = __ballot_sync(0xffffffffu, there);
+                            sm.scale_k[c % Smem::kScaleRing][t] = sc.x * p.scale_log2;
+                            sm.scale_v[c % Smem::kScaleRing][t] = sc.y;
+                            if (lane == 0) sm.mask[c % kMaskRing][t >> 5] = word;
+                            __syncwarp();
+                            mbar_arrive(&sm.tile_full[c % kMaskRing]);
+                            if (j + 1 < n) sc = scales_of(w, (w.tile0 + j + 1) * kTileKV + t, there);
+                        }
+                        const uint32_t dst = smem_u32(m == 0 ? sm.k[st] : sm.v[st]);
+                        for (int h = 0; h < 2; ++h, ++raw_cnt) {
+                            const uint32_t slot = raw_cnt % kRaw;
+                            ZL_WAIT_WARP(&sm.raw_full[slot], (raw_cnt / kRaw) & 1, 5);
+                            constexpr int kChunks = D / 16;  // 16-byte pieces of a row of codes
+#pragma unroll
+                            for (int i = 0; i < Smem::kRawRows * kChunks / 128; ++i) {
+                                const int e = i * 128 + t, r = e / kChunks, ch = e % kChunks;
+                                const int line = D == 128 ? r & 7 : (r >> 1) & 3;
+                                const uint4 x = *reinterpret_cast<const uint4*>(sm.raw[slot] + r * D + ((ch ^ line) << 4));
+                                const uint32_t lo[4] = {code_pair<kFormat, 0, 1>(x.x), code_pair<kFormat, 2, 3>(x.x), code_pair<kFormat, 0, 1>(x.y),
+                                                        code_pair<kFormat, 2, 3>(x.y)};
+                                const uint32_t hi[4] = {code_pair<kFormat, 0, 1>(x.z), code_pair<kFormat, 2, 3>(x.z), code_pair<kFormat, 0, 1>(x.w),
+                                                        code_pair<kFormat, 2, 3>(x.w)};
+                                const int row = h * Smem::kRawRows + r, c0 = 2 * (ch & 3);
+                                const uint32_t to = dst + (ch >> 2) * Smem::kBoxBytes + row * 128;
+                                // the pieces of the second box go odd one first, so that eight lanes meet all banks
+                                const bool swap = ch >= 4;
+                                const uint32_t a0 = to + (((c0 + (swap ? 1 : 0)) ^ (row & 7)) << 4), a1 = to + (((c0 + (swap ? 0 : 1)) ^ (row & 7)) << 4);
+                                st_shared_v4(a0, swap ? hi[0] : lo[0], swap ? hi[1] : lo[1], swap ? hi[2] : lo[2], swap ? hi[3] : lo[3]);
+                                st_shared_v4(a1, swap ? lo[0] : hi[0], swap ? lo[1] : hi[1], swap ? lo[2] : hi[2], swap ? lo[3] : hi[3]);
+                            }
+                            mbar_arrive(&sm.raw_empty[slot]);
+                        }
+                        fence_proxy_async_smem();
+                        mbar_arrive(m == 0 ? &sm.k_full[st] : &sm.v_full[st]);
+                    }
+                }
+                kv_cnt += n;
+                }
+            ZL_ITEM_DONE
+        }
+    } else {
+        // ------------------------------------------------------------------ softmax, join and output
+        if constexpr (kCodes) reg_inc<192>(); else reg_inc<216>();
+        const int x = (warp - 4) >> 2;
+        const int quarter = warp & 3;              // TMEM lane quarter this warp may access
+        const int row = quarter * 32 + lane;
+        const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t col_s = kColS + x * 128, col_o = kColO + x * 128;
+        const float mul = kCodes ? 1.f : p.scale_log2;  // scores of 8-bit keys have theirs in the key's scale
+        const int32_t tile_tokens = kTileQ / p.group;
+        const int32_t row_tok = row / p.group, row_head = row - row_tok * p.group;
+        uint32_t kv_cnt = 0, s_cnt = 0, o_cnt[2] = {0, 0}, join_cnt = 0;
+        ZL_FOR_ITEMS(ZL_WAIT_REGS, 28)
+            const bool two = w.two != 0;
+            const int32_t tok = w.tok0 + (two ? x * tile_tokens : 0) + row_tok;  // of the sequence
+            const bool row_ok = row_tok < tile_tokens && tok < w.tok0 + w.tokens;
+            // (rows that do not exist hold anything, and take no part in what a warp decides together)
+            const int32_t seen = row_ok ? keys_seen(w.seq(), tok) - w.tile0 * kTileKV : INT32_MAX;
+            float m_ref = -INFINITY, l = 0.f;
+            for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
+                const uint32_t c = kv_cnt + j;
+                const bool first = j == (two ? 0 : x);
+                ZL_WAIT_REGS(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 20);
+                ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
+                ++s_cnt;
+                tc_fence_after();
+                float sv[kTileKV];
+#pragma unroll
+                for (int q = 0; q < kTileKV / 32; ++q) {
+                    uint32_t r[32];
+                    tmem_ld_x32(lane_addr + col_s + q * 32, r);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sv[q * 32 + i] = __uint_as_float(r[i]);
+                }
+                tmem_wait_ld();
+                if constexpr (kCodes) {
+                    const float4* ks = reinterpret_cast<const float4*>(sm.scale_k[c % Smem::kScaleRing]);
+#pragma unroll
+                    for (int i = 0; i < kTileKV / 4; ++i) {
+                        const float4 f = ks[i];
+                        const float2 a = mul2(make_float2(sv[4 * i], sv[4 * i + 1]), make_float2(f.x, f.y));
+                        const float2 b = mul2(make_float2(sv[4 * i + 2], sv[4 * i + 3]), make_float2(f.z, f.w));
+                        sv[4 * i] = a.x; sv[4 * i + 1] = a.y; sv[4 * i + 2] = b.x; sv[4 * i + 3] = b.y;
+                    }
+                }
+                const uint4 m4 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                const int valid = row_ok ? seen - j * kTileKV : kTileKV;
+                if (__any_sync(0xffffffffu, valid < kTileKV) || (m4.x & m4.y & m4.z & m4.w) != 0xffffffffu) {
+                    const uint32_t words[4] = {m4.x & low_bits(valid), m4.y & low_bits(valid - 32), m4.z & low_bits(valid - 64), m4.w & low_bits(valid - 96)};
+#pragma unroll
+                    for (int i = 0; i < kTileKV; ++i)
+                        if (!((words[i >> 5] >> (i & 31)) & 1)) sv[i] = -INFINITY;  // select, never multiply
+                }
+                // four independent chains: a single running maximum is a 64-deep dependent chain
+                float mx0 = max3(sv[0], sv[1], sv[2]), mx1 = max3(sv[3], sv[4], sv[5]);
+                float mx2 = max3(sv[6], sv[7], sv[8]), mx3 = max3(sv[9], sv[10], sv[11]);
+#pragma unroll
+                for (int i = 12; i + 7 < kTileKV; i += 8) {
+                    mx0 = max3(mx0, sv[i], sv[i + 1]);
+                    mx1 = max3(mx1, sv[i + 2], sv[i + 3]);
+                    mx2 = max3(mx2, sv[i + 4], sv[i + 5]);
+                    mx3 = max3(mx3, sv[i + 6], sv[i + 7]);
+                }
+                mx0 = max3(mx0, sv[kTileKV - 4], sv[kTileKV - 3]);
+                mx1 = max3(mx1, sv[kTileKV - 2], sv[kTileKV - 1]);
+                const float mx = fmaxf(max3(mx0, mx1, mx2), mx3);
+                const bool raise = row_ok && (mx - m_ref) * mul > kRescaleThresholdLog2;
+                if (__any_sync(0xffffffffu, raise && !first)) {
+                    // rescale O (the step before this one is complete: S of this one was issued after it)
+                    const float alpha = raise ? ex2((m_ref - mx) * mul) : 1.f;
+#pragma unroll
+                    for (int q = 0; q < D / 32; ++q) {
+                        uint32_t r[32];
+                        tmem_ld_x32(lane_addr + col_o + q * 32, r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+                        tmem_st_x32(lane_addr + col_o + q * 32, r);
+                    }
+                    l *= alpha;
+                }
+                if (raise) m_ref = mx;
+                const float nmb = m_ref == -INFINITY ? 0.f : -m_ref * mul;  // (a row that has seen no key yet)
+                float2 sum2 = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {  // P goes to the MMA warp in two halves of 64 key columns, rounded to bf16 once
+                    uint32_t pk[kTileKV / 4];
+                    const float4* vs = reinterpret_cast<const float4*>(sm.scale_v[kCodes ? c % Smem::kScaleRing : 0] + h * (kTileKV / 2));
+#pragma unroll
+                    for (int i = 0; i < kTileKV / 2; i += 4) {
+                        const int cc = h * (kTileKV / 2) + i;
+                        float2 e0 = fma2(make_float2(sv[cc], sv[cc + 1]), make_float2(mul, mul), make_float2(nmb, nmb));
+                        float2 e1 = fma2(make_float2(sv[cc + 2], sv[cc + 3]), make_float2(mul, mul), make_float2(nmb, nmb));
+                        e0 = make_float2(ex2(e0.x), ex2(e0.y));
+                        e1 = make_float2(ex2(e1.x), ex2(e1.y));
+                        sum2 = add2(sum2, e0);
+                        sum2 = add2(sum2, e1);
+                        if constexpr (kCodes) {
+                            const float4 f = vs[i / 4];
+                            e0 = mul2(e0, make_float2(f.x, f.y));
+                            e1 = mul2(e1, make_float2(f.z, f.w));
+                        }
+                        pk[i / 2] = pack_bf16(e0.x, e0.y);
+                        pk[i / 2 + 1] = pack_bf16(e1.x, e1.y);
+                    }
+                    tmem_st_x32(lane_addr + col_s + h * 32, pk);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(&sm.p_half[x][h]);
+                }
+                l += sum2.x + sum2.y;
+            }
+            // ---- the item's end: weights of the accumulators for this row, and the columns this warpgroup writes
+            float wt[2] = {two && x == 1 ? 0.f : 1.f, two && x == 1 ? 1.f : 0.f};
+            if (n > 0) {
+                if (two) {
+                    ZL_WAIT_REGS(&sm.o_full[x], o_cnt[x] & 1, 22);
+                } else {
+                    for (int y = 0; y < 2; ++y)
+                        if (n > y) ZL_WAIT_REGS(&sm.o_full[y], o_cnt[y] & 1, 23);
+                }
+                for (int y = 0; y < 2; ++y)
+                    if (two || n > y) ++o_cnt[y];
+                tc_fence_after();
+                if (!two) {
+                    sm.stat[x][row] = make_float2(m_ref, l);
+                    mbar_arrive(&sm.stat_full);
+                    ZL_WAIT_REGS(&sm.stat_full, join_cnt & 1, 24);
+                    const float2 a = sm.stat[0][row], b = sm.stat[1][row];
+                    m_ref = fmaxf(a.x, b.x);
+                    wt[0] = m_ref == -INFINITY ? 0.f : ex2((a.x - m_ref) * mul);
+                    wt[1] = m_ref == -INFINITY ? 0.f : ex2((b.x - m_ref) * mul);
+                    l = wt[0] * a.y + wt[1] * b.y;
+                }
+            }
+            const int c0 = two ? 0 : x * (D / 2), n_cols = two ? D : D / 2;
+            const int32_t c_first = w.c_first, c_last = w.c_last;
+            const bool whole = c_first == c_last;
+            const int64_t grow = (int64_t)w.q0 + tok;
+            const int32_t q_head = w.head * p.group + row_head;
+            const bool has_lse = row_ok && (two || x == 0);  // one thread per row
+            const int64_t o_at = (grow * p.n_heads + q_head) * D + c0;
+            const int tile = two ? x : 0;
+            auto part_of = [&](int32_t cta) { return p.chunk_part + (((int64_t)cta * 2 + w.place(cta)) * 2 + tile) * kPartTileFloats<D>; };
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll 1
+            for (int q = 0; q < n_cols / 32; ++q) {
+                float o[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0.f;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    if (two ? y == x && n > 0 : n > y) {
+                        uint32_t r[32];
+                        tmem_ld_x32(lane_addr + kColO + y * 128 + c0 + q * 32, r);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = fmaf(wt[y], __uint_as_float(r[i]), o[i]);
+                    }
+                }
+                if (!row_ok) continue;
+                if (whole) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        uint4 o4;
+                        o4.x = pack_bf16(o[i] * inv, o[i + 1] * inv);
+                        o4.y = pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
+                        o4.z = pack_bf16(o[i + 4] * inv, o[i + 5] * inv);
+                        o4.w = pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
+                        *reinterpret_cast<uint4*>(p.o + o_at + q * 32 + i) = o4;
+                    }
+                } else {
+                    float4* to = reinterpret_cast<float4*>(part_of(blockIdx.x) + 2 * kTileQ) + (c0 / 4 + q * 8) * kTileQ + row;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) to[i * kTileQ] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                }
+            }
+            if (has_lse) {
+                if (whole) {
+                    if (p.lse) p.lse[(int64_t)q_head * p.b.total_q + grow] = l > 0.f ? (m_ref * mul + log2f(l)) * kLn2 : -INFINITY;
+                } else {
+                    float* to = part_of(blockIdx.x);
+                    to[row] = m_ref * mul;
+                    to[kTileQ + row] = l;
+                }
+            }
+            tc_fence_before();
+            if (!two && n > 0) {  // both accumulators and the statistics have been read
+                mbar_arrive(&sm.join_done);
+                ZL_WAIT_REGS(&sm.join_done, join_cnt & 1, 25);
+                ++join_cnt;
+            }
+            if (!whole) {
+                // ---- the part that finishes last joins all of them, in order (an even number of barrier phases)
+                __threadfence();
+                mbar_arrive(&sm.part_bar);
+                ZL_WAIT_REGS(&sm.part_bar, 0, 26);
+                if (threadIdx.x == 128) sm.ticket = atomicAdd(p.chunk_count + c_first, 1);
+                mbar_arrive(&sm.part_bar);
+                ZL_WAIT_REGS(&sm.part_bar, 1, 27);
+                if (sm.ticket == c_last - c_first) {
+                    __threadfence();
+                    if (row_ok) {
+                        float mm = -INFINITY, ll = 0.f;
+                        for (int32_t cta = c_first; cta <= c_last; ++cta) mm = fmaxf(mm, __ldcg(part_of(cta) + row));
+                        if (mm > -INFINITY)
+                            for (int32_t cta = c_first; cta <= c_last; ++cta)
+                                ll = fmaf(ex2(__ldcg(part_of(cta) + row) - mm), __ldcg(part_of(cta) + kTileQ + row), ll);
+                        const float scale = ll > 0.f ? 1.f / ll : 0.f;
+#pragma unroll 1
+                        for (int q = 0; q < n_cols / 32; ++q) {
+                            float o[32];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = 0.f;
+                            if (mm > -INFINITY)
+#pragma unroll 1
+                                for (int32_t cta = c_first; cta <= c_last; ++cta) {
+                                    const float* part = part_of(cta);
+                                    const float f = ex2(__ldcg(part + row) - mm);
+                                    const float4* from = reinterpret_cast<const float4*>(part + 2 * kTileQ) + (c0 / 4 + q * 8) * kTileQ + row;
+                                    float4 y[8];
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) y[i] = __ldcg(from + i * kTileQ);
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) {
+                                        o[4 * i] = fmaf(f, y[i].x, o[4 * i]);
+                                        o[4 * i + 1] = fmaf(f, y[i].y, o[4 * i + 1]);
+                                        o[4 * i + 2] = fmaf(f, y[i].z, o[4 * i + 2]);
+                                        o[4 * i + 3] = fmaf(f, y[i].w, o[4 * i + 3]);
+                                    }
+                                }
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8) {
+                                uint4 o4;
+                                o4.x = pack_bf16(o[i] * scale, o[i + 1] * scale);
+                                o4.y = pack_bf16(o[i + 2] * scale, o[i + 3] * scale);
+                                o4.z = pack_bf16(o[i + 4] * scale, o[i + 5] * scale);
+                                o4.w = pack_bf16(o[i + 6] * scale, o[i + 7] * scale);
+                                *reinterpret_cast<uint4*>(p.o + o_at + q * 32 + i) = o4;
+                            }
+                        }
+                        if (has_lse && p.lse) p.lse[(int64_t)q_head * p.b.total_q + grow] = ll > 0.f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
+                    }
+                    if (threadIdx.x == 128) p.chunk_count[c_first] = 0;  // for the next launch
+                }
+            }
+            kv_cnt += n;
+        ZL_ITEM_DONE
+    }
+
+teardown:
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+template <int D, int kFormat>
+cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CachedParams& p, int grid, cudaStream_t stream) {
+    constexpr int smem = sizeof(ChunkSmem<D, kFormat>);
+    static_assert(smem <= 232448, "shared memory of a CTA");
+    constexpr int kMaxDevices = 64;
+    static bool configured[kMaxDevices] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices || !configured[dev]) {
+        e = cudaFuncSetAttribute(zl_cached_chunk_kernel<D, kFormat>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < kMaxDevices) configured[dev] = true;
+    }
+    return launch_dependent(zl_cached_chunk_kernel<D, kFormat>, grid, kFormat == ZL_CACHE_BF16 ? 384 : 512, smem, stream, true, tq, tk, tv, p);
+}
+
+}  // namespace
+
+size_t cached_chunk_part_bytes(int head_dim) {
+    return 4 * sizeof(float) * (head_dim == 128 ? kPartTileFloats<128> : kPartTileFloats<64>);
+}
+
+cudaError_t launch_cached_chunk(int head_dim, int format, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
+                                const CachedParams& p, int grid, cudaStream_t stream) {
+    if (head_dim == 128) {
+        if (format == ZL_CACHE_BF16) return launch_t<128, ZL_CACHE_BF16>(tq, tk, tv, p, grid, stream);
+        return format == ZL_CACHE_INT8 ? launch_t<128, ZL_CACHE_INT8>(tq, tk, tv, p, grid, stream) : launch_t<128, ZL_CACHE_E4M3>(tq, tk, tv, p, grid, stream);
+    }
+    if (format == ZL_CACHE_BF16) return launch_t<64, ZL_CACHE_BF16>(tq, tk, tv, p, grid, stream);
+    return format == ZL_CACHE_INT8 ? launch_t<64, ZL_CACHE_INT8>(tq, tk, tv, p, grid, stream) : launch_t<64, ZL_CACHE_E4M3>(tq, tk, tv, p, grid, stream);
+}
+
+}  // namespace zl

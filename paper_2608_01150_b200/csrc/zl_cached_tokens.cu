@@ -24,7 +24,7 @@ using namespace cache;
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kRows = 16;    // query rows of an item
+constexpr int kRows = kTokenRows;  // query rows of an item
 constexpr int kKeys = 16;    // keys of a warp's step
 constexpr int kTile = kKeys * kWarps;
 constexpr float kRescale = 8.f;  // powers of two by which a score may exceed the reference before sums are rescaled
@@ -95,6 +95,7 @@ struct SeqWork {
 __device__ __forceinline__ SeqWork seq_work(const CachedParams& p, const SeqView& v) {
     SeqWork w;
     w.blocks = (int32_t)(((int64_t)v.q_len * p.group + kRows - 1) / kRows);
+    if (p.split && w.blocks > 1) w.blocks = 0;  // the other kernel's
     w.items = w.blocks * p.c.n_kv_heads;
     w.tiles = v.q_len > 0 ? (keys_seen(v, v.q_len - 1) + kTile - 1) / kTile : 0;
     return w;

@@ -166,6 +166,7 @@ struct CacheReadParams {
     __nv_bfloat16* k;
     __nv_bfloat16* v;
 };
+constexpr int kTokenRows = 16;  // rows (new tokens times query heads of a key head) of a sequence for which mma.sync tiles do
 // Attention of a batch's new tokens over the cache.
 struct CachedParams {
     CacheView c;
@@ -178,6 +179,10 @@ struct CachedParams {
     float* lse;          // may be NULL
     float* part;         // two partial results per CTA
     int32_t* part_count; // per CTA: finished parts of the item that is cut first in it; zero between launches
+    float* chunk_part;   // the same of the kernel for chunks
+    int32_t* chunk_count;
+    int32_t split;       // both kernels run: sequences of at most kTokenRows rows per key head are the tokens kernel's
+    int32_t head_first;  // coordinates of the K and V maps are (column, head, token, page), else (column, token, head, page)
     int32_t* status;
 };
 cudaError_t launch_cache_write(int head_dim, int format, const CacheView& c, const CacheBatch& b, const __nv_bfloat16* k,
@@ -186,6 +191,11 @@ cudaError_t launch_cache_read(int head_dim, int format, const CacheView& c, cons
                               cudaStream_t stream);
 cudaError_t launch_cached_tokens(int head_dim, int format, const CachedParams& p, int grid, cudaStream_t stream);
 size_t cached_tokens_part_bytes(int head_dim);  // of a CTA's two partial results
+// Maps: tq of [total_q, n_kv_heads, group, d], box 64 columns x group x 1 x whole tokens of 128 rows; tk and tv over the pages, box 64
+// columns of bf16 or a row of codes, rows of one page, at most 128 (bf16) or 64.
+cudaError_t launch_cached_chunk(int head_dim, int format, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
+                                const CachedParams& p, int grid, cudaStream_t stream);
+size_t cached_chunk_part_bytes(int head_dim);
 
 // Of the C-ABI layer.
 void count_launch();
