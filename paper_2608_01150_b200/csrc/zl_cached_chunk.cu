@@ -504,13 +504,21 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         reg_dec<64>();
         if constexpr (kCodes) {
             const int t = threadIdx.x - 384;
+            // This thread's 16-byte pieces of half a tile: piece `ch` of rows r, r + kRowStep, ... (a multiple of 8: the exchange
+            // of pieces within a line is the same for all of them).  A piece of 16 codes becomes two of eight numbers; in the
+            // second box the odd one goes first, so that eight lanes meet all banks.
+            constexpr int kChunks = D / 16, kRowStep = 128 / kChunks, kPieces = Smem::kRawRows / kRowStep;
+            const int r = t / kChunks, ch = t % kChunks;
+            const bool swap = ch >= 4;
+            const uint32_t from = r * D + ((ch ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4);
+            const uint32_t to = (ch >> 2) * Smem::kBoxBytes + r * 128;
+            const uint32_t to0 = to + (((2 * (ch & 3) + (swap ? 1 : 0)) ^ (r & 7)) << 4), to1 = to0 ^ 16;
             uint32_t kv_cnt = 0, raw_cnt = 0;
+            auto page_of = [&](const Item& w, int32_t key) { return key < w.keys ? page_at(p.b, p.c, w.s, key) : -1; };
             // scales of this thread's key (key t of the tile), zeros without one
-            auto scales_of = [&](const Item& w, int32_t key, bool& there) {
-                const int32_t pg = key < w.keys ? page_at(p.b, p.c, w.s, key) : -1;
-                there = pg >= 0;
+            auto scales_of = [&](const Item& w, int32_t key, int32_t pg) {
                 float2 r = make_float2(0.f, 0.f);
-                if (there) {
+                if (pg >= 0) {
                     const int64_t at = (((int64_t)pg << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1))) * p.c.n_kv_heads + w.head;
                     r = make_float2(__ldg(p.c.k_scale + at), __ldg(p.c.v_scale + at));
                 }
@@ -518,8 +526,10 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             };
             ZL_FOR_ITEMS(ZL_WAIT_WARP, 8)
                 if (n > 0) {
-                bool there;
-                float2 sc = scales_of(w, w.tile0 * kTileKV + t, there);
+                // pages are looked up two tiles ahead, scales one: neither is waited for
+                const int32_t key0 = w.tile0 * kTileKV + t;
+                int32_t pg = page_of(w, key0), pg_next = page_of(w, key0 + kTileKV);
+                float2 sc = scales_of(w, key0, pg);
                 for (int j = 0; j <= n; ++j) {
                     for (int m = 0; m < 2; ++m) {
                         if (m == 0 ? j == n : j == 0) continue;
@@ -527,35 +537,29 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         uint64_t* const empty = m == 0 ? &sm.k_empty[st] : &sm.v_empty[st];
                         ZL_WAIT_WARP(empty, ((c / kStages) & 1) ^ 1, 4);
                         if (m == 0) {
-                            const uint32_t word = __ballot_sync(0xffffffffu, there);
+                            const uint32_t word = __ballot_sync(0xffffffffu, pg >= 0);
                             sm.scale_k[c % Smem::kScaleRing][t] = sc.x * p.scale_log2;
                             sm.scale_v[c % Smem::kScaleRing][t] = sc.y;
                             if (lane == 0) sm.mask[c % kMaskRing][t >> 5] = word;
                             __syncwarp();
                             mbar_arrive(&sm.tile_full[c % kMaskRing]);
-                            if (j + 1 < n) sc = scales_of(w, (w.tile0 + j + 1) * kTileKV + t, there);
+                            pg = pg_next;
+                            sc = scales_of(w, key0 + (j + 1) * kTileKV, pg);
+                            pg_next = page_of(w, key0 + (j + 2) * kTileKV);
                         }
                         const uint32_t dst = smem_u32(m == 0 ? sm.k[st] : sm.v[st]);
                         for (int h = 0; h < 2; ++h, ++raw_cnt) {
                             const uint32_t slot = raw_cnt % kRaw;
                             ZL_WAIT_WARP(&sm.raw_full[slot], (raw_cnt / kRaw) & 1, 5);
-                            constexpr int kChunks = D / 16;  // 16-byte pieces of a row of codes
+                            uint4 x[kPieces];
 #pragma unroll
-                            for (int i = 0; i < Smem::kRawRows * kChunks / 128; ++i) {
-                                const int e = i * 128 + t, r = e / kChunks, ch = e % kChunks;
-                                const int line = D == 128 ? r & 7 : (r >> 1) & 3;
-                                const uint4 x = *reinterpret_cast<const uint4*>(sm.raw[slot] + r * D + ((ch ^ line) << 4));
-                                const uint32_t lo[4] = {code_pair<kFormat, 0, 1>(x.x), code_pair<kFormat, 2, 3>(x.x), code_pair<kFormat, 0, 1>(x.y),
-                                                        code_pair<kFormat, 2, 3>(x.y)};
-                                const uint32_t hi[4] = {code_pair<kFormat, 0, 1>(x.z), code_pair<kFormat, 2, 3>(x.z), code_pair<kFormat, 0, 1>(x.w),
-                                                        code_pair<kFormat, 2, 3>(x.w)};
-                                const int row = h * Smem::kRawRows + r, c0 = 2 * (ch & 3);
-                                const uint32_t to = dst + (ch >> 2) * Smem::kBoxBytes + row * 128;
-                                // the pieces of the second box go odd one first, so that eight lanes meet all banks
-                                const bool swap = ch >= 4;
-                                const uint32_t a0 = to + (((c0 + (swap ? 1 : 0)) ^ (row & 7)) << 4), a1 = to + (((c0 + (swap ? 0 : 1)) ^ (row & 7)) << 4);
-                                st_shared_v4(a0, swap ? hi[0] : lo[0], swap ? hi[1] : lo[1], swap ? hi[2] : lo[2], swap ? hi[3] : lo[3]);
-                                st_shared_v4(a1, swap ? lo[0] : hi[0], swap ? lo[1] : hi[1], swap ? lo[2] : hi[2], swap ? lo[3] : hi[3]);
+                            for (int i = 0; i < kPieces; ++i) x[i] = *reinterpret_cast<const uint4*>(sm.raw[slot] + from + i * kRowStep * D);
+#pragma unroll
+                            for (int i = 0; i < kPieces; ++i) {
+                                const uint32_t a = swap ? x[i].z : x[i].x, b = swap ? x[i].w : x[i].y, c = swap ? x[i].x : x[i].z, d = swap ? x[i].y : x[i].w;
+                                const uint32_t at = dst + (h * Smem::kRawRows + i * kRowStep) * 128;
+                                st_shared_v4(at + to0, code_pair<kFormat, 0, 1>(a), code_pair<kFormat, 2, 3>(a), code_pair<kFormat, 0, 1>(b), code_pair<kFormat, 2, 3>(b));
+                                st_shared_v4(at + to1, code_pair<kFormat, 0, 1>(c), code_pair<kFormat, 2, 3>(c), code_pair<kFormat, 0, 1>(d), code_pair<kFormat, 2, 3>(d));
                             }
                             mbar_arrive(&sm.raw_empty[slot]);
                         }
