@@ -81,9 +81,9 @@ constexpr int kPartTileFloats = kTileQ * (D + 2);  // maxima, sums, then the unn
 struct Geometry {
     int32_t tokens;  // whole tokens of a tile
     int32_t heads;
-    bool rest_only;  // sequences of at most 16 rows are another kernel's
+    int32_t rest_rows;  // sequences of at most as many rows are another kernel's
     __device__ __forceinline__ explicit Geometry(const CachedParams& p)
-        : tokens(kTileQ / p.group), heads(p.c.n_kv_heads), rest_only(p.split != 0) {}
+        : tokens(kTileQ / p.group), heads(p.c.n_kv_heads), rest_rows(p.split ? p.token_rows : 0) {}
 };
 
 struct SeqLine {
@@ -91,7 +91,7 @@ struct SeqLine {
     int32_t blocks;
     __device__ __forceinline__ SeqLine(const CachedParams& p, const Geometry& g, int s) : v(load_seq(p.b, p.c.page_shift, s)) {
         blocks = (v.q_len + 2 * g.tokens - 1) / (2 * g.tokens);
-        if (g.rest_only && (int64_t)v.q_len * p.group <= kTokenRows) blocks = 0;
+        if ((int64_t)v.q_len * p.group <= g.rest_rows) blocks = 0;
     }
     __device__ __forceinline__ int32_t block_tokens(const Geometry& g, int b) const { return min(2 * g.tokens, v.q_len - b * 2 * g.tokens); }
     __device__ __forceinline__ int32_t block_keys(const Geometry& g, int b) const {
