@@ -471,8 +471,7 @@ typedef struct {
  *               8; 16-byte aligned.  Rows that are written have to be finite.
  * In 8 bits: scale = max |x| / T over the row, code = x / scale rounded to the nearest of the type (ties to even), T = 127 or
  * 448 (e4m3), both quotients rounded to fp32; a row whose scale is 0 has the codes of 0.  A value is off by at most
- * scale / 2 (int8), or by 2^-4 of itself and scale / 1024 (e4m3).  (The codes that e4m3 has for NaN are never written; in a
- * cache filled by other means they stand for +-480.) */
+ * scale / 2 (int8), or by 2^-4 of itself and scale / 1024 (e4m3). */
 zl_status zl_cache_write(const zl_kv_cache* cache, const zl_cache_batch* batch, const void* k, const void* v,
                          int64_t row_stride, void* stream);
 
@@ -507,6 +506,8 @@ zl_status zl_cached_attn_device_status(const zl_cached_attn* attn, int32_t* code
  *   lse        [n_heads, total_q] fp32, or NULL
  *   workspace  at least zl_cached_attn_workspace_bytes, 256-byte aligned
  * Q, and the keys and values inside the sequences' lengths, have to be finite; other places of the cache may hold anything.
+ * P is rounded to bf16 (8-bit caches: times the value's scale, to fp16) for its product with V; everything else is fp32.
+ * Scales of values below 2^-90 count as 2^-90.
  * Asynchronous on `stream`; captured like the other entry points. */
 zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cache, const zl_cache_batch* batch, const void* q,
                              int64_t q_stride, float scale, void* o, float* lse, void* workspace, size_t workspace_bytes,

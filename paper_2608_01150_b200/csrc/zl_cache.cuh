@@ -76,5 +76,61 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
     return kFormat == ZL_CACHE_INT8 ? int8_pair<I, J>(w) : e4m3_pair<I, J>(w);
 }
 
+// Attention over 8-bit caches multiplies in fp16, which holds every code exactly and is reached in a third of the
+// instructions: a whole number c goes through 0x64 in front of c + 128 (1152 + c, in steps of one), e4m3 through a conversion
+// of its own (whose NaN codes stay NaN).  Four codes of a word, in pairs (0, 1), (2, 3) or (0, 2), (1, 3).
+__device__ __forceinline__ uint32_t int8_half(uint32_t shifted, uint32_t sel) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(__byte_perm(shifted, 0x64646464u, sel)), "r"(0x64806480u));
+    return r;
+}
+__device__ __forceinline__ void e4m3_half(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 a, b;\n\t"
+        "mov.b32 {a, b}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=r"(lo), "=r"(hi) : "r"(w));
+}
+template <int kFormat>
+__device__ __forceinline__ void halves(uint32_t w, uint32_t& p01, uint32_t& p23) {
+    if constexpr (kFormat == ZL_CACHE_INT8) {
+        w ^= 0x80808080u;
+        p01 = int8_half(w, 0x4140);
+        p23 = int8_half(w, 0x4342);
+    } else {
+        e4m3_half(w, p01, p23);
+    }
+}
+template <int kFormat>
+__device__ __forceinline__ void halves_apart(uint32_t w, uint32_t& p02, uint32_t& p13) {
+    if constexpr (kFormat == ZL_CACHE_INT8) {
+        w ^= 0x80808080u;
+        p02 = int8_half(w, 0x4240);
+        p13 = int8_half(w, 0x4341);
+    } else {
+        e4m3_half(__byte_perm(w, 0u, 0x3120), p02, p13);
+    }
+}
+// Queries, bf16, as fp16: times the power of two that brings the largest magnitude `big` to 2^14 .. 2^15.  What is
+// 2^-29 of it or more keeps all its bits; the rest is off by 2^-40 of it.  `back`: the factor that undoes it.
+__device__ __forceinline__ float half_factor(float big, float& back) {
+    const int e = big > 0.f ? min(max((int)(__float_as_uint(big) >> 23) - 127 - 14, -112), 113) : 0;
+    back = __uint_as_float((uint32_t)(127 + e) << 23);
+    return __uint_as_float((uint32_t)(127 - e) << 23);
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16_pair_to_half(uint32_t w, float factor) {
+    return pack_half(__uint_as_float(w << 16) * factor, __uint_as_float(w & 0xffff0000u) * factor);
+}
+// The weight of a value is its p times its scale.  Weights are held relative to a reference that follows the largest of
+// THEM (not of the scores), so that fp16 gives a weight 11 bits down to 2^-14 of that reference and 2^-25 of it below,
+// whatever the scales of other values are; the row's sum of p is kept relative to the same reference in fp32.  Scales below 2^-90
+// count as 2^-90, which keeps the sum in range.
+constexpr float kLeastScale = 0x1p-90f;
+
 }  // namespace cache
 }  // namespace zl

@@ -10,8 +10,10 @@
 //   warp 1       MMA issuer: S_x = Q K^T, O_x += P_x V (P read from TMEM), one step two ahead of the other
 //   warps 4-11   softmax, a thread per row; with two query tiles warpgroup x takes tile x, with one tile it takes key tiles x,
 //                x + 2, ... and both accumulators are joined at the end
-//   warps 12-15  (8-bit caches) codes become bf16, exactly, on their way from the ring of codes to the rings of K and V; the scale of
-//                a key multiplies its column of S, the scale of a value its column of P, in fp32
+//   warps 12-15  (8-bit caches) codes become fp16, exactly, on their way from the ring of codes to the rings of K and V, and the queries
+//                of an item in their place; the scale of a key multiplies its column of S, the scale of a value its column of P, in
+//                fp32: the softmax takes s_j = S_j k_j + log2 v_j, so that its exponentials are the weights of the values, and sums
+//                weight / v_j beside them
 // An item that lies in several CTAs leaves its parts in the workspace, and the one that finishes last joins them in the order
 // of the CTAs.
 #include "zl_cache.cuh"
@@ -60,11 +62,13 @@ struct ChunkSmem {
     alignas(1024) uint8_t k[kStages][kTileBytes];
     alignas(1024) uint8_t v[kStages][kTileBytes];
     alignas(1024) uint8_t raw[kRaw][kCodes ? kRawBytes : 16];
-    alignas(16) float scale_k[kCodes ? kScaleRing : 1][kTileKV], scale_v[kCodes ? kScaleRing : 1][kTileKV];
+    alignas(16) float key_scale[kCodes ? kScaleRing : 1][kTileKV];  // of the scores, in powers of two
+    alignas(16) float value_log2[kCodes ? kScaleRing : 1][kTileKV], value_inv[kCodes ? kScaleRing : 1][kTileKV];  // log2 and inverse of its scale
     alignas(16) uint32_t mask[kMaskRing][4];            // keys of a tile that exist
     Item items[kItems];
     float2 stat[2][kTileQ];                             // per warpgroup and row: reference maximum (raw scores), sum
-    alignas(8) uint64_t q_full, q_empty;
+    float q_big[4];  // per converting warp: largest magnitude of its queries
+    alignas(8) uint64_t q_full, q_empty, q_max, q_ready;
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], raw_full[kRaw], raw_empty[kRaw];
     uint64_t s_full[2], p_half[2][2], o_full[2], tile_full[kMaskRing];
     uint64_t stat_full, join_done, part_bar, item_full[kItems], item_empty[kItems];
@@ -232,6 +236,8 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     if (threadIdx.x == 0) {
         mbar_init(&sm.q_full, 1);
         mbar_init(&sm.q_empty, 1);
+        mbar_init(&sm.q_max, 128);
+        mbar_init(&sm.q_ready, 128);
         for (int x = 0; x < 2; ++x) {
             mbar_init(&sm.s_full[x], 1);
             mbar_init(&sm.p_half[x][0], 128);
@@ -425,8 +431,8 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         } else if (warp == 1) {
             // -------------------------------------------------------------- MMA issuer (whole warp, one elected lane issues)
             const bool mma_lane = elect_one();
-            constexpr uint32_t idesc_s = make_idesc_bf16(kTileQ, kTileKV, 0, 0);
-            constexpr uint32_t idesc_o = make_idesc_bf16(kTileQ, D, 0, 1);
+            constexpr uint32_t idesc_s = make_idesc_f16(kCodes, kTileQ, kTileKV, 0, 0);
+            constexpr uint32_t idesc_o = make_idesc_f16(kCodes, kTileQ, D, 0, 1);
             const uint64_t dq0 = make_desc_sw128(smem_u32(sm.q[0]), 16, 1024);
             const uint64_t dk0 = make_desc_sw128(smem_u32(sm.k[0]), 16, 1024);
             const uint64_t dv0 = make_desc_sw128(smem_u32(sm.v[0]), Smem::kBoxBytes, 1024);  // V is the MN-major B operand
@@ -436,7 +442,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 const bool two = w.two != 0;
                 const int steps = two ? 2 * n : n;
                 if (steps > 0) {
-                ZL_WAIT_WARP(&sm.q_full, item_cnt & 1, 11);
+                ZL_WAIT_WARP(kCodes ? &sm.q_ready : &sm.q_full, item_cnt & 1, 11);
                 ++item_cnt;
                 // step u: S of step u, then (before it) P V of step u - 2; x is the accumulator, j the key tile
                 for (int u = 0; u < steps + 2; ++u) {
@@ -513,7 +519,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const uint32_t from = r * D + ((ch ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4);
             const uint32_t to = (ch >> 2) * Smem::kBoxBytes + r * 128;
             const uint32_t to0 = to + (((2 * (ch & 3) + (swap ? 1 : 0)) ^ (r & 7)) << 4), to1 = to0 ^ 16;
-            uint32_t kv_cnt = 0, raw_cnt = 0;
+            uint32_t kv_cnt = 0, raw_cnt = 0, item_cnt = 0;
             auto page_of = [&](const Item& w, int32_t key) { return key < w.keys ? page_at(p.b, p.c, w.s, key) : -1; };
             // scales of this thread's key (key t of the tile), zeros without one
             auto scales_of = [&](const Item& w, int32_t key, int32_t pg) {
@@ -526,6 +532,41 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             };
             ZL_FOR_ITEMS(ZL_WAIT_WARP, 8)
                 if (n > 0) {
+                // ---- queries: a thread has row t of both tiles.  One factor for the item: the keys' scales take it back
+                ZL_WAIT_WARP(&sm.q_full, item_cnt & 1, 30);
+                float scores_by;
+                {
+                    const int q_tiles = w.two ? 2 : 1;
+                    float big = 0.f;
+                    const int32_t row_tok = t / p.group, tile_tokens = kTileQ / p.group;
+                    for (int x = 0; x < q_tiles; ++x)
+                        if (row_tok < tile_tokens && x * tile_tokens + row_tok < w.tokens)  // (other rows may hold anything)
+#pragma unroll 1
+                            for (int e = 0; e < 8 * kBoxes; ++e) {
+                                const uint4 u = *reinterpret_cast<const uint4*>(sm.q[x] + (e >> 3) * Smem::kBoxBytes + t * 128 + (((e + t) & 7) << 4));
+                                for (uint32_t v : {u.x, u.y, u.z, u.w}) big = max3_abs(big, __uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+                            }
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, d));
+                    if (lane == 0) sm.q_big[t >> 5] = big;
+                    __syncwarp();
+                    mbar_arrive(&sm.q_max);
+                    ZL_WAIT_WARP(&sm.q_max, item_cnt & 1, 31);
+                    float back;
+                    const float factor = half_factor(fmaxf(fmaxf(sm.q_big[0], sm.q_big[1]), fmaxf(sm.q_big[2], sm.q_big[3])), back);
+                    scores_by = back * p.scale_log2;
+                    for (int x = 0; x < q_tiles; ++x)
+#pragma unroll 1
+                        for (int e = 0; e < 8 * kBoxes; ++e) {
+                            uint4* const at = reinterpret_cast<uint4*>(sm.q[x] + (e >> 3) * Smem::kBoxBytes + t * 128 + (((e + t) & 7) << 4));
+                            const uint4 u = *at;
+                            *at = make_uint4(bf16_pair_to_half(u.x, factor), bf16_pair_to_half(u.y, factor), bf16_pair_to_half(u.z, factor),
+                                             bf16_pair_to_half(u.w, factor));
+                        }
+                    fence_proxy_async_smem();
+                    mbar_arrive(&sm.q_ready);
+                    ++item_cnt;
+                }
                 // pages are looked up two tiles ahead, scales one: neither is waited for
                 const int32_t key0 = w.tile0 * kTileKV + t;
                 int32_t pg = page_of(w, key0), pg_next = page_of(w, key0 + kTileKV);
@@ -538,8 +579,10 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         ZL_WAIT_WARP(empty, ((c / kStages) & 1) ^ 1, 4);
                         if (m == 0) {
                             const uint32_t word = __ballot_sync(0xffffffffu, pg >= 0);
-                            sm.scale_k[c % Smem::kScaleRing][t] = sc.x * p.scale_log2;
-                            sm.scale_v[c % Smem::kScaleRing][t] = sc.y;
+                            const float v_scale = fmaxf(sc.y, kLeastScale);
+                            sm.key_scale[c % Smem::kScaleRing][t] = sc.x * scores_by;
+                            sm.value_log2[c % Smem::kScaleRing][t] = log2f(v_scale);
+                            sm.value_inv[c % Smem::kScaleRing][t] = 1.f / v_scale;
                             if (lane == 0) sm.mask[c % kMaskRing][t >> 5] = word;
                             __syncwarp();
                             mbar_arrive(&sm.tile_full[c % kMaskRing]);
@@ -548,6 +591,13 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             pg_next = page_of(w, key0 + (j + 2) * kTileKV);
                         }
                         const uint32_t dst = smem_u32(m == 0 ? sm.k[st] : sm.v[st]);
+                        // rows without a key may hold codes of NaN: zeros, before they meet their weight of 0
+                        uint4 there = make_uint4(~0u, ~0u, ~0u, ~0u);
+                        if (kFormat == ZL_CACHE_E4M3 && m == 1) {
+                            ZL_WAIT_WARP(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 32);
+                            there = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                        }
+                        const bool holes = (there.x & there.y & there.z & there.w) != ~0u;
                         for (int h = 0; h < 2; ++h, ++raw_cnt) {
                             const uint32_t slot = raw_cnt % kRaw;
                             ZL_WAIT_WARP(&sm.raw_full[slot], (raw_cnt / kRaw) & 1, 5);
@@ -556,10 +606,20 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             for (int i = 0; i < kPieces; ++i) x[i] = *reinterpret_cast<const uint4*>(sm.raw[slot] + from + i * kRowStep * D);
 #pragma unroll
                             for (int i = 0; i < kPieces; ++i) {
-                                const uint32_t a = swap ? x[i].z : x[i].x, b = swap ? x[i].w : x[i].y, c = swap ? x[i].x : x[i].z, d = swap ? x[i].y : x[i].w;
+                                uint32_t a = swap ? x[i].z : x[i].x, b = swap ? x[i].w : x[i].y, c = swap ? x[i].x : x[i].z, d = swap ? x[i].y : x[i].w;
+                                if (holes) {
+                                    const int row = h * Smem::kRawRows + r + i * kRowStep;
+                                    const uint32_t word = row < 64 ? (row < 32 ? there.x : there.y) : (row < 96 ? there.z : there.w);
+                                    if (!((word >> (row & 31)) & 1)) a = b = c = d = 0;
+                                }
                                 const uint32_t at = dst + (h * Smem::kRawRows + i * kRowStep) * 128;
-                                st_shared_v4(at + to0, code_pair<kFormat, 0, 1>(a), code_pair<kFormat, 2, 3>(a), code_pair<kFormat, 0, 1>(b), code_pair<kFormat, 2, 3>(b));
-                                st_shared_v4(at + to1, code_pair<kFormat, 0, 1>(c), code_pair<kFormat, 2, 3>(c), code_pair<kFormat, 0, 1>(d), code_pair<kFormat, 2, 3>(d));
+                                uint32_t y[8];
+                                halves<kFormat>(a, y[0], y[1]);
+                                halves<kFormat>(b, y[2], y[3]);
+                                halves<kFormat>(c, y[4], y[5]);
+                                halves<kFormat>(d, y[6], y[7]);
+                                st_shared_v4(at + to0, y[0], y[1], y[2], y[3]);
+                                st_shared_v4(at + to1, y[4], y[5], y[6], y[7]);
                             }
                             mbar_arrive(&sm.raw_empty[slot]);
                         }
@@ -579,7 +639,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         const int row = quarter * 32 + lane;
         const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
         const uint32_t col_s = kColS + x * 128, col_o = kColO + x * 128;
-        const float mul = kCodes ? 1.f : p.scale_log2;  // scores of 8-bit keys have theirs in the key's scale
+        const float mul = kCodes ? 1.f : p.scale_log2;  // of 8-bit caches the keys' scales have it
         const int32_t tile_tokens = kTileQ / p.group;
         const int32_t row_tok = row / p.group, row_head = row - row_tok * p.group;
         uint32_t kv_cnt = 0, s_cnt = 0, o_cnt[2] = {0, 0}, join_cnt = 0;
@@ -607,12 +667,13 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 tmem_wait_ld();
                 if constexpr (kCodes) {
-                    const float4* ks = reinterpret_cast<const float4*>(sm.scale_k[c % Smem::kScaleRing]);
+                    const float4* ks = reinterpret_cast<const float4*>(sm.key_scale[c % Smem::kScaleRing]);
+                    const float4* vl = reinterpret_cast<const float4*>(sm.value_log2[c % Smem::kScaleRing]);
 #pragma unroll
                     for (int i = 0; i < kTileKV / 4; ++i) {
-                        const float4 f = ks[i];
-                        const float2 a = mul2(make_float2(sv[4 * i], sv[4 * i + 1]), make_float2(f.x, f.y));
-                        const float2 b = mul2(make_float2(sv[4 * i + 2], sv[4 * i + 3]), make_float2(f.z, f.w));
+                        const float4 f = ks[i], g = vl[i];
+                        const float2 a = fma2(make_float2(sv[4 * i], sv[4 * i + 1]), make_float2(f.x, f.y), make_float2(g.x, g.y));
+                        const float2 b = fma2(make_float2(sv[4 * i + 2], sv[4 * i + 3]), make_float2(f.z, f.w), make_float2(g.z, g.w));
                         sv[4 * i] = a.x; sv[4 * i + 1] = a.y; sv[4 * i + 2] = b.x; sv[4 * i + 3] = b.y;
                     }
                 }
@@ -656,25 +717,35 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 const float nmb = m_ref == -INFINITY ? 0.f : -m_ref * mul;  // (a row that has seen no key yet)
                 float2 sum2 = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {  // P goes to the MMA warp in two halves of 64 key columns, rounded to bf16 once
+                for (int h = 0; h < 2; ++h) {  // P goes to the MMA warp in two halves of 64 key columns, rounded once
                     uint32_t pk[kTileKV / 4];
-                    const float4* vs = reinterpret_cast<const float4*>(sm.scale_v[kCodes ? c % Smem::kScaleRing : 0] + h * (kTileKV / 2));
+                    const float4* vi = reinterpret_cast<const float4*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0] + (kCodes ? h * (kTileKV / 2) : 0));
 #pragma unroll
                     for (int i = 0; i < kTileKV / 2; i += 4) {
                         const int cc = h * (kTileKV / 2) + i;
-                        float2 e0 = fma2(make_float2(sv[cc], sv[cc + 1]), make_float2(mul, mul), make_float2(nmb, nmb));
-                        float2 e1 = fma2(make_float2(sv[cc + 2], sv[cc + 3]), make_float2(mul, mul), make_float2(nmb, nmb));
+                        float2 e0 = make_float2(sv[cc], sv[cc + 1]), e1 = make_float2(sv[cc + 2], sv[cc + 3]);
+                        const float2 nm = make_float2(nmb, nmb);
+                        if constexpr (kCodes) {
+                            e0 = add2(e0, nm);
+                            e1 = add2(e1, nm);
+                        } else {
+                            e0 = fma2(e0, make_float2(mul, mul), nm);
+                            e1 = fma2(e1, make_float2(mul, mul), nm);
+                        }
                         e0 = make_float2(ex2(e0.x), ex2(e0.y));
                         e1 = make_float2(ex2(e1.x), ex2(e1.y));
-                        sum2 = add2(sum2, e0);
-                        sum2 = add2(sum2, e1);
                         if constexpr (kCodes) {
-                            const float4 f = vs[i / 4];
-                            e0 = mul2(e0, make_float2(f.x, f.y));
-                            e1 = mul2(e1, make_float2(f.z, f.w));
+                            const float4 f = vi[i / 4];
+                            sum2 = fma2(e0, make_float2(f.x, f.y), sum2);
+                            sum2 = fma2(e1, make_float2(f.z, f.w), sum2);
+                            pk[i / 2] = pack_half(e0.x, e0.y);
+                            pk[i / 2 + 1] = pack_half(e1.x, e1.y);
+                        } else {
+                            sum2 = add2(sum2, e0);
+                            sum2 = add2(sum2, e1);
+                            pk[i / 2] = pack_bf16(e0.x, e0.y);
+                            pk[i / 2 + 1] = pack_bf16(e1.x, e1.y);
                         }
-                        pk[i / 2] = pack_bf16(e0.x, e0.y);
-                        pk[i / 2 + 1] = pack_bf16(e1.x, e1.y);
                     }
                     tmem_st_x32(lane_addr + col_s + h * 32, pk);
                     tmem_wait_st();

@@ -13,9 +13,9 @@
 //     as the 8: half the instructions, registers and exponentials of the other way round where a sequence has at most eight
 //     rows; up to 16 rows take two such columns of tiles.  Products of so few rows are far from the tensor cores' rate with either kind
 //     of instruction, and registers spare the way of S and P through tensor memory (about 2,000 clocks a tile for one row);
-//   * codes of 8 bits become bf16 exactly, in registers; the scale of a key multiplies its score and the scale of a value its
-//     weight, both in fp32.  Columns are summed, and come out, in the order in which ldmatrix gives 8-bit codes.  Twice the warps
-//     share that work;
+//   * codes of 8 bits become fp16 exactly, in registers (the integer pipe's half rate bounds that; bf16 took three times the
+//     instructions); the scale of a key multiplies its score and the scale of a value its weight, both in fp32.  Columns are
+//     summed, and come out, in the order in which ldmatrix gives 8-bit codes.  Twice the warps share that work;
 //   * the warps of a CTA join at the end of a stretch of an item; an item that lies in several CTAs is joined by the one that
 //     finishes last, in the order of the CTAs, so that results do not depend on which that is.
 #include "zl_cache.cuh"
@@ -84,6 +84,12 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
 // c += a b: 16 rows x 8 columns, 16 deep
 __device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void mma16h(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -253,6 +259,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
         const SeqView sv = w.sv;
         // ---- queries of the item as B operands (row gid of every column), and the keys that rows 2 quad, 2 quad + 1 see
         uint32_t q[kCols][D / 16][2];
+        float by_row[kCols][2];  // 8-bit caches: what multiplies a score beside the key's scale
         int32_t seen[kCols][2], all_see = INT32_MAX;
 #pragma unroll
         for (int n = 0; n < kCols; ++n) {
@@ -272,6 +279,21 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 }
                 q[n][ks][0] = x.x;
                 q[n][ks][1] = x.y;
+            }
+            if constexpr (kCodes) {  // to fp16, and the factor that undoes its scale, for the lane's columns of S^T
+                float big = 0.f, back;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint32_t x = q[n][i >> 1][i & 1];
+                    big = max3_abs(big, __uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+                }
+                big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+                big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+                const float factor = half_factor(big, back);
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) q[n][i >> 1][i & 1] = bf16_pair_to_half(q[n][i >> 1][i & 1], factor);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) by_row[n][e] = __shfl_sync(0xffffffffu, back, (2 * quad + e) * 4) * p.scale_log2;
             }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -308,10 +330,11 @@ zl_cached_tokens_kernel(const CachedParams p) {
                     ldm4(r, ks_addr + swizzled<kRowBytes>(lane & 15, ks + (lane >> 4)));
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const uint32_t a0 = code_pair<kFormat, 0, 1>(r[2 * e]), a1 = code_pair<kFormat, 0, 1>(r[2 * e + 1]);
-                        const uint32_t a2 = code_pair<kFormat, 2, 3>(r[2 * e]), a3 = code_pair<kFormat, 2, 3>(r[2 * e + 1]);
+                        uint32_t a0, a1, a2, a3;
+                        halves<kFormat>(r[2 * e], a0, a2);
+                        halves<kFormat>(r[2 * e + 1], a1, a3);
 #pragma unroll
-                        for (int n = 0; n < kCols; ++n) mma16(c[n], a0, a1, a2, a3, q[n][ks + e][0], q[n][ks + e][1]);
+                        for (int n = 0; n < kCols; ++n) mma16h(c[n], a0, a1, a2, a3, q[n][ks + e][0], q[n][ks + e][1]);
                     }
                 }
             } else {
@@ -325,13 +348,14 @@ zl_cached_tokens_kernel(const CachedParams p) {
             }
             const int32_t key0 = tile * kTile + warp * kKeys;
             const uint32_t exists = sm.mask[warp][st];
-            float by_key[2] = {p.scale_log2, p.scale_log2}, value_scale[2] = {1.f, 1.f};
+            float key_scale[2], value_scale[2], value_log2[2];
             if constexpr (kCodes) {
                 const float* sc = reinterpret_cast<const float*>(sm.ring[warp][st] + 2 * kMatrixBytes);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    by_key[h] *= sc[8 * h + gid];
-                    value_scale[h] = sc[kKeys + 8 * h + gid];
+                    key_scale[h] = sc[8 * h + gid];
+                    value_scale[h] = fmaxf(sc[kKeys + 8 * h + gid], kLeastScale);
+                    value_log2[h] = __log2f(value_scale[h]);
                 }
             }
             const bool cut = key0 + kKeys > all_see || exists != 0xffffu;
@@ -339,7 +363,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
 #pragma unroll
             for (int n = 0; n < kCols; ++n) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) c[n][i] *= by_key[i >> 1];
+                for (int i = 0; i < 4; ++i) c[n][i] *= kCodes ? by_row[n][i & 1] * key_scale[i >> 1] : p.scale_log2;
                 if (cut) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -347,9 +371,10 @@ zl_cached_tokens_kernel(const CachedParams p) {
                         if (key0 + col >= seen[n][i & 1] || !((exists >> col) & 1)) c[n][i] = -INFINITY;
                     }
                 }
-                float mx[2];
+                float mx[2];  // what the reference has to follow: scores, or weights of 8-bit values
 #pragma unroll
-                for (int e = 0; e < 2; ++e) mx[e] = fmaxf(c[n][e], c[n][2 + e]);
+                for (int e = 0; e < 2; ++e)
+                    mx[e] = kCodes ? fmaxf(c[n][e] + value_log2[0], c[n][2 + e] + value_log2[1]) : fmaxf(c[n][e], c[n][2 + e]);
                 if (__any_sync(0xffffffffu, mx[0] > m[n][0] + kRescale || mx[1] > m[n][1] + kRescale)) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
@@ -366,14 +391,14 @@ zl_cached_tokens_kernel(const CachedParams p) {
                         }
                     }
                 }
-                // ---- P, rounded to bf16 (8-bit values: with their scale) for its product with V; the sums take it unrounded
+                // ---- P, rounded once for its product with V (bf16, or with the value's scale to fp16); the sums take it unrounded
                 const float ref[2] = {m[n][0] == -INFINITY ? 0.f : m[n][0], m[n][1] == -INFINITY ? 0.f : m[n][1]};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float x = ex2(c[n][2 * h] - ref[0]), y = ex2(c[n][2 * h + 1] - ref[1]);
                     l[n][0] += x;
                     l[n][1] += y;
-                    b[n][h] = transposed(kCodes ? pack_bf16(x * value_scale[h], y * value_scale[h]) : pack_bf16(x, y));
+                    b[n][h] = transposed(kCodes ? pack_half(x * value_scale[h], y * value_scale[h]) : pack_bf16(x, y));
                 }
             }
             // ---- O^T += V^T P^T
@@ -384,10 +409,11 @@ zl_cached_tokens_kernel(const CachedParams p) {
                     ldm4t(r, vs_addr + swizzled<kRowBytes>(lane & 15, ch + (lane >> 4)));
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {  // even columns of the chunk as rows 0-7, odd ones as rows 8-15
-                        const uint32_t a0 = code_pair<kFormat, 0, 2>(r[2 * e]), a1 = code_pair<kFormat, 1, 3>(r[2 * e]);
-                        const uint32_t a2 = code_pair<kFormat, 0, 2>(r[2 * e + 1]), a3 = code_pair<kFormat, 1, 3>(r[2 * e + 1]);
+                        uint32_t a0, a1, a2, a3;
+                        halves_apart<kFormat>(r[2 * e], a0, a1);
+                        halves_apart<kFormat>(r[2 * e + 1], a2, a3);
 #pragma unroll
-                        for (int n = 0; n < kCols; ++n) mma16(o[n][ch + e], a0, a1, a2, a3, b[n][0], b[n][1]);
+                        for (int n = 0; n < kCols; ++n) mma16h(o[n][ch + e], a0, a1, a2, a3, b[n][0], b[n][1]);
                     }
                 }
             } else {

@@ -228,6 +228,11 @@ __host__ __device__ constexpr uint32_t make_idesc_bf16(int M, int N, int a_mn_ma
            ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+// The same, or (half) with fp16 inputs.
+__host__ __device__ constexpr uint32_t make_idesc_f16(bool half, int M, int N, int a_mn_major, int b_mn_major) {
+    return make_idesc_bf16(M, N, a_mn_major, b_mn_major) & (half ? ~((1u << 7) | (1u << 10)) : ~0u);
+}
+
 // D[tmem] (+)= A[smem] * B[smem]
 __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                        bool accumulate) {

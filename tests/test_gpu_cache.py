@@ -263,6 +263,44 @@ def test_growing_scores_move_the_reference(dtype):
     check(s, qlens, q, o, lse)
 
 
+@pytest.mark.parametrize("dtype", [BF16, INT8, E4M3])
+def test_rows_of_no_sequence_and_of_others_do_not_matter(dtype):
+    """Queries behind the last sequence hold NaN and infinities, those of another sequence 2^60 times the rest; tiles read both."""
+    lens, qlens = [200, 30, 150], [40, 3, 21]
+    s = Setup(dtype, 64, 16, 2, lens)
+    s.fill()
+    q = rand(s.g, 70, 4, 64, times=1.5)
+    q[64:67], q[67:] = math.nan, math.inf
+    small = q[:64].clone()
+    small[40:43] *= 2.0 ** -60
+    q[40:43] *= 2.0 ** 60
+    o, lse = attend(s, qlens, q)
+    check(s, [40], q[:40], o[:40], lse[:, :40], lens=lens[:1])
+    s.tables, tables = s.tables[2:], s.tables
+    check(s, [21], q[43:64], o[43:64], lse[:, 43:64], lens=lens[2:])
+    s.tables = tables
+    o, lse = attend(s, qlens, small)
+    check(s, qlens, small, o, lse)
+
+
+@pytest.mark.parametrize("dtype", [INT8, E4M3])
+@pytest.mark.parametrize("rows", [1, 12, 60])
+def test_values_of_very_different_scales(dtype, rows):
+    """One token's values are 2^20 times the others', and next to nobody looks at it; one head's are 2^-60 times."""
+    import paper_2608_01150_b200 as Z
+    n, dim = 300, 64
+    s = Setup(dtype, dim, 16, 2, [n])
+    k, v = rand(s.g, n, 2, dim), rand(s.g, n, 2, dim)
+    q = rand(s.g, rows, 4, dim).abs()
+    k[17] = -2.0                     # scores some 2^5 below the rest
+    v[17] *= 2.0 ** 20
+    v[:, 1] *= 2.0 ** -60
+    Z.cache_write(s.cache, s.batch([n]), k.cuda(), v.cuda())
+    s.ref.write([0, n], [n], s.tables, k, v)
+    o, lse = attend(s, [rows], q)
+    check(s, [rows], q, o, lse)
+
+
 @pytest.mark.parametrize("n_seqs", [255, 257, 700])
 def test_many_sequences(n_seqs):
     """More sequences than a CTA has threads."""
