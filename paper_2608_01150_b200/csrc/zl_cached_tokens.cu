@@ -210,6 +210,15 @@ zl_cached_tokens_kernel(const CachedParams p) {
     W ahead(p, sm.start_seq, sm.start_base, begin, end);
     int32_t f_tile = 0, f_keys = 0;  // the next step's tile; keys that the item's last row sees
     uint32_t f_stage = 0;
+    // Offsets within a matrix: of this lane's piece of the rows it copies (rows 8 apart are alike), and of its row of ldmatrix,
+    // whose chunks c, c + 2, ... are an exclusive or away.
+    constexpr int kChunks = kRowBytes / 16, kRowsAtOnce = 32 / kChunks;
+    uint32_t f_to[kRowsAtOnce < 8 ? 8 / kRowsAtOnce : 1];
+#pragma unroll
+    for (int i = 0; i < (kRowsAtOnce < 8 ? 8 / kRowsAtOnce : 1); ++i)
+        f_to[i] = swizzled<kRowBytes>(i * kRowsAtOnce + lane / kChunks, lane % kChunks) - i * kRowsAtOnce * kRowBytes;
+    const uint32_t k_at = swizzled<kRowBytes>(lane & 15, lane >> 4);
+    const uint32_t v_at = kCodes ? k_at : swizzled<kRowBytes>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1);
     auto fetch = [&]() {
         while (f_tile >= ahead.tile1) {
             if (!ahead.next(p)) {
@@ -226,22 +235,21 @@ zl_cached_tokens_kernel(const CachedParams p) {
             const int32_t pg = key < f_keys ? page_at(p.b, p.c, ahead.s, key) : -1;
             const uint32_t exists = __ballot_sync(0xffffffffu, pg >= 0);
             if (lane == 0) sm.mask[warp][f_stage] = exists & 0xffffu;
-            const int32_t in_mask = (1 << p.c.page_shift) - 1;
-            constexpr int kChunks = kRowBytes / 16, kRowsAtOnce = 32 / kChunks;
-            const int64_t in_row = ahead.head * p.c.head_stride + (lane % kChunks) * 16;
+            // every lane works out its key's place; the copies of a row take it from there
+            const int32_t in = key & ((1 << p.c.page_shift) - 1);
+            const int64_t place = pg >= 0 ? pg * p.c.page_stride + in * p.c.token_stride + ahead.head * p.c.head_stride : -1;
 #pragma unroll
             for (int i = 0; i < kKeys / kRowsAtOnce; ++i) {
-                const int r = i * kRowsAtOnce + lane / kChunks;
-                const int32_t page = __shfl_sync(0xffffffffu, pg, r);
-                const bool live = page >= 0;
-                const int64_t off = live ? page * p.c.page_stride + ((key0 + r) & in_mask) * p.c.token_stride + in_row : 0;
-                const uint32_t to = dst + swizzled<kRowBytes>(r, lane % kChunks);
+                const int64_t from = __shfl_sync(0xffffffffu, place, i * kRowsAtOnce + lane / kChunks);
+                const bool live = from >= 0;
+                const uint32_t to = dst + f_to[(i * kRowsAtOnce % 8) / kRowsAtOnce] + i * kRowsAtOnce * kRowBytes;
+                const int64_t off = live ? from + lane % kChunks * 16 : 0;
                 cp16(to, p.c.k + off, live);
                 cp16(to + kMatrixBytes, p.c.v + off, live);
             }
             if constexpr (kCodes) {
                 const bool live = pg >= 0;
-                const int64_t off = live ? (((int64_t)pg << p.c.page_shift) + (key & in_mask)) * p.c.n_kv_heads + ahead.head : 0;
+                const int64_t off = live ? (((int64_t)pg << p.c.page_shift) + in) * p.c.n_kv_heads + ahead.head : 0;
                 cp4(dst + 2 * kMatrixBytes + lane * 4, (lane < 16 ? p.c.k_scale : p.c.v_scale) + off, live);
             }
             ++f_tile;
@@ -318,7 +326,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
             cp_wait<kStages - 2>();
             __syncwarp();
             fetch();  // into the stage of the step before this one
-            const uint32_t ks_addr = ring + st * Smem::kStageBytes, vs_addr = ks_addr + kMatrixBytes;
+            const uint32_t k_addr = ring + st * Smem::kStageBytes + k_at, v_addr = ring + st * Smem::kStageBytes + kMatrixBytes + v_at;
             // ---- S^T: keys gid and gid + 8, rows 2 quad and 2 quad + 1
             float c[kCols][4];
 #pragma unroll
@@ -327,7 +335,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ks += 2) {
                     uint32_t r[4];  // keys 0-7 and 8-15 of chunk ks, the same of chunk ks + 1
-                    ldm4(r, ks_addr + swizzled<kRowBytes>(lane & 15, ks + (lane >> 4)));
+                    ldm4(r, k_addr ^ (ks << 4));
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         uint32_t a0, a1, a2, a3;
@@ -341,7 +349,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks) {
                     uint32_t r[4];  // keys 0-7 and 8-15 of chunk 2 ks, the same of chunk 2 ks + 1
-                    ldm4(r, ks_addr + swizzled<kRowBytes>(lane & 15, 2 * ks + (lane >> 4)));
+                    ldm4(r, k_addr ^ (ks << 5));
 #pragma unroll
                     for (int n = 0; n < kCols; ++n) mma16(c[n], r[0], r[1], r[2], r[3], q[n][ks][0], q[n][ks][1]);
                 }
@@ -406,7 +414,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
 #pragma unroll
                 for (int ch = 0; ch < D / 16; ch += 2) {
                     uint32_t r[4];  // keys 0-7 and 8-15 of chunk ch, the same of chunk ch + 1
-                    ldm4t(r, vs_addr + swizzled<kRowBytes>(lane & 15, ch + (lane >> 4)));
+                    ldm4t(r, v_addr ^ (ch << 4));
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {  // even columns of the chunk as rows 0-7, odd ones as rows 8-15
                         uint32_t a0, a1, a2, a3;
@@ -420,7 +428,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
                     uint32_t r[4];  // keys 0-7 of chunks 2 i and 2 i + 1, keys 8-15 of the same
-                    ldm4t(r, vs_addr + swizzled<kRowBytes>((lane & 7) + ((lane >> 4) << 3), 2 * i + ((lane >> 3) & 1)));
+                    ldm4t(r, v_addr ^ (i << 5));
 #pragma unroll
                     for (int n = 0; n < kCols; ++n) mma16(o[n][i], r[0], r[1], r[2], r[3], b[n][0], b[n][1]);
                 }
