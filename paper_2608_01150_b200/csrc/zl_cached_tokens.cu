@@ -29,7 +29,11 @@ using namespace cache;
 namespace {
 
 constexpr int kKeys = 16;        // keys of a warp's step
+constexpr int kJoin = 32;        // parts that are joined at a time
 constexpr int kHelpers = 4;      // warps that do not stream
+// Least units of a CTA's stretch, where items are that long: cutting an item costs its parts' way through memory, some
+// 6,000 clocks, as much as six of its steps.
+constexpr int64_t kLeastUnits = 6;
 constexpr uint64_t kWaitLimitNs = 4000000000ull;
 constexpr float kRescale = 8.f;  // powers of two by which a score may exceed the reference before sums are rescaled
 constexpr float kLn2 = 0.6931471805599453f;
@@ -46,7 +50,7 @@ template <int D, int kFormat, int kCols>
 struct TokenSmem {
     static constexpr bool kCodes = kFormat != ZL_CACHE_BF16;
     static constexpr int kRows = 8 * kCols;
-    static constexpr int kWarps = kCodes || D == 64 ? (kCols == 1 ? 12 : 8) : (kCols == 1 ? 7 : 6);  // that stream
+    static constexpr int kWarps = kCodes ? (kCols == 1 ? 12 : 8) : (D == 64 ? (kCols == 1 ? 11 : 8) : (kCols == 1 ? 7 : 6));  // that stream
     static constexpr int kRowBytes = D * (kCodes ? 1 : 2);
     static constexpr int kMatrixBytes = kKeys * kRowBytes;  // 16 keys or 16 values
     static constexpr int kStageBytes = 2 * kMatrixBytes + (kCodes ? 2 * kKeys * 4 : 0);
@@ -66,6 +70,10 @@ struct TokenSmem {
     int32_t seen[kItems][kRows];     // keys that a row sees
     alignas(8) uint64_t item_full[kItems], q_full[kItems], item_done[kItems], o_free, helpers;
     int64_t scan[kWarps + kHelpers];
+    int32_t longest[kWarps + kHelpers];
+    float join_w[kJoin][kRows];      // weights and sums of parts that are joined
+    float4 join_o[kHelpers * 32];
+    float join_l[kHelpers * 32];
     int64_t start_base;
     int32_t start_seq, ticket;
     volatile int32_t abort_flag;
@@ -187,22 +195,32 @@ zl_cached_tokens_kernel(const CachedParams p) {
         const int chunk = (p.b.n_seqs + kThreads - 1) / kThreads;
         const int s_end = min((tid + 1) * chunk, p.b.n_seqs);
         int64_t mine = 0;
-        for (int s = tid * chunk; s < s_end; ++s) mine += Work(p, load_seq(p.b, p.c.page_shift, s)).units();
+        int32_t longest = 0;
+        for (int s = tid * chunk; s < s_end; ++s) {
+            const Work x(p, load_seq(p.b, p.c.page_shift, s));
+            mine += x.units();
+            if (x.items > 0) longest = max(longest, x.tiles + 1);
+        }
+        longest = __reduce_max_sync(0xffffffffu, longest);
         int64_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
             if (lane >= d) upto += x;
         }
-        if (lane == 31) sm.scan[warp] = upto;
+        if (lane == 31) {
+            sm.scan[warp] = upto;
+            sm.longest[warp] = longest;
+        }
         __syncthreads();
         int64_t before = 0, total = 0;
 #pragma unroll
         for (int w = 0; w < kWarps + kHelpers; ++w) {
             if (w < warp) before += sm.scan[w];
             total += sm.scan[w];
+            longest = max(longest, sm.longest[w]);
         }
-        per = quotient(total + gridDim.x - 1, gridDim.x);
+        per = max(quotient(total + gridDim.x - 1, gridDim.x), min((int64_t)longest, kLeastUnits));
         begin = per * blockIdx.x;
         end = min(begin + per, total);
         if (begin >= end) return;
@@ -362,23 +380,55 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 ZL_WAIT_WARP(&sm.helpers, 1, 3);
                 if (sm.ticket == w.c_last - w.c_first) {
                     __threadfence();
-                    for (int j = t; j < rows * (D / 4); j += kHelpers * 32) {
-                        const int r = j / (D / 4), c4 = j % (D / 4);
+                    // Threads beyond a quadruple of columns each take every `groups`th part; weights are worked out once per part and
+                    // row, kJoin parts at a time.  (An even number of barrier phases each time.)
+                    const int quads = rows * (D / 4), parts = w.c_last - w.c_first + 1;
+                    const int groups = quads >= kHelpers * 32 ? 1 : kHelpers * 32 / quads;
+                    for (int j0 = 0; j0 < quads; j0 += kHelpers * 32) {
+                        const int j = j0 + (groups > 1 ? t % quads : t), group = groups > 1 ? t / quads : 0;
+                        const bool mine = j < quads && group < groups;
+                        const int r = mine ? j / (D / 4) : 0, c4 = j % (D / 4);
                         float mm = -INFINITY, ll = 0.f;
-#pragma unroll 4
-                        for (int v = w.c_first; v <= w.c_last; ++v) mm = fmaxf(mm, __ldcg(part_of(v) + r));
                         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (mm > -INFINITY) {
-#pragma unroll 4
-                            for (int v = w.c_first; v <= w.c_last; ++v) {
-                                const float* from = part_of(v);
-                                const float f = ex2(__ldcg(from + r) - mm);
-                                const float4 x = __ldcg(reinterpret_cast<const float4*>(from + 2 * kTokenRows + r * D + c4 * 4));
-                                ll = fmaf(f, __ldcg(from + kTokenRows + r), ll);
-                                acc.x = fmaf(f, x.x, acc.x); acc.y = fmaf(f, x.y, acc.y); acc.z = fmaf(f, x.z, acc.z); acc.w = fmaf(f, x.w, acc.w);
+                        for (int p0 = 0; p0 < parts; p0 += kJoin) {
+                            const int n = min(kJoin, parts - p0);
+                            for (int i = t; i < n * rows; i += kHelpers * 32) sm.join_w[i / rows][i % rows] = __ldcg(part_of(w.c_first + p0 + i / rows) + i % rows);
+                            mbar_arrive(&sm.helpers);
+                            ZL_WAIT_WARP(&sm.helpers, 0, 4);
+                            float up = mm;
+                            for (int v = 0; v < n; ++v) up = fmaxf(up, sm.join_w[v][r]);
+                            if (mine && up > -INFINITY) {
+                                const float alpha = ex2(mm - up);
+                                mm = up;
+                                ll *= alpha;
+                                acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+#pragma unroll 8
+                                for (int v = group; v < n; v += groups) {
+                                    const float* from = part_of(w.c_first + p0 + v);
+                                    const float4 x = __ldcg(reinterpret_cast<const float4*>(from + 2 * kTokenRows + r * D + c4 * 4));
+                                    const float lv = __ldcg(from + kTokenRows + r), f = ex2(sm.join_w[v][r] - mm);
+                                    ll = fmaf(f, lv, ll);
+                                    acc.x = fmaf(f, x.x, acc.x); acc.y = fmaf(f, x.y, acc.y); acc.z = fmaf(f, x.z, acc.z); acc.w = fmaf(f, x.w, acc.w);
+                                }
                             }
+                            mbar_arrive(&sm.helpers);
+                            ZL_WAIT_WARP(&sm.helpers, 1, 5);
                         }
-                        finish(w, r, c4, mm, ll, acc);
+                        if (groups > 1) {  // (all groups have the same maximum)
+                            sm.join_o[t] = acc;
+                            sm.join_l[t] = ll;
+                            mbar_arrive(&sm.helpers);
+                            ZL_WAIT_WARP(&sm.helpers, 0, 6);
+                            if (mine && group == 0)
+                                for (int g = 1; g < groups; ++g) {
+                                    const float4 x = sm.join_o[g * quads + j];
+                                    ll += sm.join_l[g * quads + j];
+                                    acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+                                }
+                            mbar_arrive(&sm.helpers);
+                            ZL_WAIT_WARP(&sm.helpers, 1, 7);
+                        }
+                        if (mine && group == 0) finish(w, r, c4, mm, ll, acc);
                     }
                     if (t == 0) p.part_count[w.c_first] = 0;  // for the next launch
                 }
@@ -404,6 +454,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
         // ---- copies: this warp's 16 keys of every tile of every item, kStages - 1 steps ahead of their use
         uint32_t f_item = 0, f_stage = 0;
         int32_t f_tile = 0, f_end = 0;  // the next step's tile, the item's last; f_end < 0: no more items
+        int32_t f_page = -1;            // page of this lane's key (key lane % 16) of the next step, looked up a step ahead
         bool waited = true;
         auto fetch = [&]() {
             if (f_tile >= f_end && f_end >= 0) {
@@ -414,14 +465,19 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 f_tile = sm.items[place].tile0;
                 f_end = waited ? sm.items[place].tile1 : -1;
                 ++f_item;
+                if (f_end >= 0) {
+                    const int32_t key = f_tile * kTile + warp * kKeys + (lane & 15);
+                    f_page = key < sm.items[place].keys ? page_at(p.b, p.c, sm.items[place].s, key) : -1;
+                }
             }
             if (f_end >= 0) {
                 const Item& w = sm.items[(f_item - 1) % kItems];
                 const int32_t key0 = f_tile * kTile + warp * kKeys;
                 const uint32_t dst = ring + f_stage * Smem::kStageBytes;
                 const int32_t key = key0 + (lane & 15);
-                const int32_t pg = key < w.keys ? page_at(p.b, p.c, w.s, key) : -1;
+                const int32_t pg = f_page;
                 const uint32_t exists = __ballot_sync(0xffffffffu, pg >= 0);
+                if (++f_tile < f_end) f_page = key + kTile < w.keys ? page_at(p.b, p.c, w.s, key + kTile) : -1;
                 if (lane == 0) sm.mask[warp][f_stage] = exists & 0xffffu;
                 // every lane works out its key's place; the copies of a row take it from there
                 const int32_t in = key & ((1 << p.c.page_shift) - 1);
@@ -440,7 +496,6 @@ zl_cached_tokens_kernel(const CachedParams p) {
                     const int64_t off = live ? (((int64_t)pg << p.c.page_shift) + in) * p.c.n_kv_heads + w.head : 0;
                     cp4(dst + 2 * kMatrixBytes + lane * 4, (lane < 16 ? p.c.k_scale : p.c.v_scale) + off, live);
                 }
-                ++f_tile;
             }
             cp_commit();
             f_stage = f_stage + 1 == kStages ? 0 : f_stage + 1;
