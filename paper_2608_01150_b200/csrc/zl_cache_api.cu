@@ -69,7 +69,7 @@ bool make_maps(const zl_kv_cache& x, const CachedParams& p, CUtensorMap* tq, CUt
             return false;
     }
     const bool codes = x.format != ZL_CACHE_BF16;
-    const cuuint32_t rows = (cuuint32_t)(x.page_size < (codes ? 64 : 128) ? x.page_size : (codes ? 64 : 128));
+    const cuuint32_t rows = (cuuint32_t)(x.page_size < kTileKV ? x.page_size : kTileKV);
     const cuuint64_t heads = (cuuint64_t)x.n_kv_heads, tokens = (cuuint64_t)x.page_size, pages = (cuuint64_t)x.n_pages;
     cuuint64_t dims[4] = {d, tokens, heads, pages}, strides[3] = {(cuuint64_t)p.c.token_stride, (cuuint64_t)p.c.head_stride, (cuuint64_t)p.c.page_stride};
     const cuuint64_t row = d * (codes ? 1 : 2);

@@ -10,8 +10,8 @@
 //   warp 1       MMA issuer: S_x = Q K^T, O_x += P_x V (P read from TMEM), one step two ahead of the other
 //   warps 4-11   softmax, a thread per row; with two query tiles warpgroup x takes tile x, with one tile it takes key tiles x,
 //                x + 2, ... and both accumulators are joined at the end
-//   warps 12-15  (8-bit caches) codes become fp16, exactly, on their way from the ring of codes to the rings of K and V, and the queries
-//                of an item in their place; the scale of a key multiplies its column of S, the scale of a value its column of P, in
+//   warps 12-15  (8-bit caches) codes become fp16, exactly, in their place (a tile of codes arrives in the second half of the tile it
+//                becomes), and so do the queries of an item; the scale of a key multiplies its column of S, the scale of a value its column of P, in
 //                fp32: the softmax takes s_j = S_j k_j + log2 v_j, so that its exponentials are the weights of the values, and sums
 //                weight / v_j beside them
 // An item that lies in several CTAs leaves its parts in the workspace, and the one that finishes last joins them in the order
@@ -49,19 +49,15 @@ struct ChunkSmem {
     static constexpr int kTileBytes = kTileKV * D * 2;  // one 128-row tile of Q, K or V
     static constexpr int kBoxBytes = kTileKV * 128;     // 128 rows x 64 bf16
     static constexpr int kBoxes = D / 64;
-    static constexpr int kStages = D == 128 ? 2 : (kCodes ? 4 : 5);
+    static constexpr int kStages = D == 128 ? 2 : 5;
     // A tile's K is prepared once V of the tile two before it has its place, which P V of kStages tiles earlier gave up: until
     // then masks and scales of a tile may be read.
     static constexpr int kScaleRing = D == 128 ? 4 : 8;
     static_assert(kScaleRing >= kStages + 2 || !kCodes, "scales of a tile are kept until its softmax is done");
     static_assert(kMaskRing >= kStages + 2, "masks of a tile are kept until its P V is done");
-    static constexpr int kRawRows = 64;                 // codes travel in halves of a tile
-    static constexpr int kRawBytes = kRawRows * D;
-    static constexpr int kRaw = !kCodes ? 1 : (D == 128 ? 3 : 6);
     alignas(1024) uint8_t q[2][kTileBytes];
     alignas(1024) uint8_t k[kStages][kTileBytes];
     alignas(1024) uint8_t v[kStages][kTileBytes];
-    alignas(1024) uint8_t raw[kRaw][kCodes ? kRawBytes : 16];
     alignas(16) float key_scale[kCodes ? kScaleRing : 1][kTileKV];  // of the scores, in powers of two
     alignas(16) float value_log2[kCodes ? kScaleRing : 1][kTileKV], value_inv[kCodes ? kScaleRing : 1][kTileKV];  // log2 and inverse of its scale
     alignas(16) uint32_t mask[kMaskRing][4];            // keys of a tile that exist
@@ -69,7 +65,8 @@ struct ChunkSmem {
     float2 stat[2][kTileQ];                             // per warpgroup and row: reference maximum (raw scores), sum
     float q_big[4];  // per converting warp: largest magnitude of its queries
     alignas(8) uint64_t q_full, q_empty, q_max, q_ready;
-    uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], raw_full[kRaw], raw_empty[kRaw];
+    uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+    uint64_t k_codes[kCodes ? kStages : 1], v_codes[kCodes ? kStages : 1], codes_read;
     uint64_t s_full[2], p_half[2][2], o_full[2], tile_full[kMaskRing];
     uint64_t stat_full, join_done, part_bar, item_full[kItems], item_empty[kItems];
     int64_t scan[16], start_base, total;
@@ -218,7 +215,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                        const __grid_constant__ CUtensorMap tm_v, const CachedParams p) {
     using Smem = ChunkSmem<D, kFormat>;
     constexpr bool kCodes = Smem::kCodes;
-    constexpr int kBoxes = Smem::kBoxes, kStages = Smem::kStages, kRaw = Smem::kRaw;
+    constexpr int kBoxes = Smem::kBoxes, kStages = Smem::kStages;
     constexpr int kThreads = kCodes ? 512 : 384;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
@@ -250,9 +247,12 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             mbar_init(&sm.v_full[s], kCodes ? 128 : 1);
             mbar_init(&sm.v_empty[s], 1);
         }
-        for (int s = 0; s < kRaw; ++s) {
-            mbar_init(&sm.raw_full[s], 1);
-            mbar_init(&sm.raw_empty[s], 128);
+        if constexpr (kCodes) {
+            for (int s = 0; s < kStages; ++s) {
+                mbar_init(&sm.k_codes[s], 1);
+                mbar_init(&sm.v_codes[s], 1);
+            }
+            mbar_init(&sm.codes_read, 128);
         }
         for (int s = 0; s < kMaskRing; ++s) mbar_init(&sm.tile_full[s], kCodes ? 128 : 1);
         mbar_init(&sm.stat_full, 256);
@@ -324,7 +324,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     if (idle) {
         // nothing to do
     } else if (warp < 4) {
-        if constexpr (kCodes) reg_dec<64>(); else reg_dec<72>();
+        if constexpr (kCodes) reg_dec<88>(); else reg_dec<136>();
         if (warp == 2) {
             // -------------------------------------------------------------- the line of work
             ItemWalk walk(p, sm.start_seq, sm.start_base, per, total);
@@ -342,12 +342,11 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         } else if (warp == 0) {
             // -------------------------------------------------------------- TMA producer (a lane per page)
             const int32_t tile_tokens = kTileQ / p.group;
-            constexpr int kSpan = kCodes ? Smem::kRawRows : kTileKV;  // rows of a load
             const int page = 1 << p.c.page_shift;
-            const int box = min(page, kSpan);
-            const int row = lane * box;          // this lane's rows of a load: [row, row + box)
-            const bool has_rows = row < kSpan;
-            uint32_t item_cnt = 0, kv_cnt = 0, raw_cnt = 0;
+            const int box = min(page, kTileKV);
+            const int row = lane * box;          // this lane's rows of a tile: [row, row + box)
+            const bool has_rows = row < kTileKV;
+            uint32_t item_cnt = 0, kv_cnt = 0;
             auto page_of = [&](const Item& w, int32_t pos) { return has_rows && pos < w.keys ? page_at(p.b, p.c, w.s, pos) : -1; };
             auto load = [&](const Item& w, uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, int32_t pg, int32_t pos) {
                 const uint32_t n = __popc(__ballot_sync(0xffffffffu, pg >= 0));
@@ -357,7 +356,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     const int32_t in = pos & (page - 1);
                     const int32_t c1 = p.head_first ? w.head : in, c2 = p.head_first ? in : w.head;
                     if constexpr (kCodes) {
-                        tma_load_4d(dst + row * D, tm, bar, 0, c1, c2, pg);
+                        tma_load_4d(dst + Smem::kTileBytes / 2 + row * D, tm, bar, 0, c1, c2, pg);
                     } else {
 #pragma unroll
                         for (int b = 0; b < kBoxes; ++b) tma_load_4d(dst + b * Smem::kBoxBytes + row * 128, tm, bar, b * 64, c1, c2, pg);
@@ -375,28 +374,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         for (int b = 0; b < kBoxes; ++b)
                             tma_load_4d(sm.q[x] + b * Smem::kBoxBytes, &tm_q, &sm.q_full, b * 64, 0, w.head, w.q0 + w.tok0 + x * tile_tokens);
                 }
-                if constexpr (kCodes) {
-                    // K runs one tile ahead of V
-                    int32_t pg_k[2], pg_v[2] = {-1, -1};
-                    for (int h = 0; h < 2; ++h) pg_k[h] = page_of(w, w.tile0 * kTileKV + h * kSpan + row);
-                    for (int j = 0; j <= n; ++j) {
-                        int32_t pg_next[2];
-                        for (int h = 0; h < 2; ++h) pg_next[h] = j + 1 < n ? page_of(w, (w.tile0 + j + 1) * kTileKV + h * kSpan + row) : -1;
-                        for (int m = 0; m < 2; ++m) {
-                            if (m == 0 ? j == n : j == 0) continue;
-                            for (int h = 0; h < 2; ++h, ++raw_cnt) {
-                                const uint32_t slot = raw_cnt % kRaw;
-                                ZL_WAIT_WARP(&sm.raw_empty[slot], ((raw_cnt / kRaw) & 1) ^ 1, 2);
-                                load(w, sm.raw[slot], m == 0 ? &tm_k : &tm_v, &sm.raw_full[slot], m == 0 ? pg_k[h] : pg_v[h],
-                                     (w.tile0 + j - m) * kTileKV + h * kSpan + row);
-                            }
-                        }
-                        for (int h = 0; h < 2; ++h) {
-                            pg_v[h] = pg_k[h];
-                            pg_k[h] = pg_next[h];
-                        }
-                    }
-                } else {
+                {  // K runs one tile ahead of V
                     int32_t pg_k = page_of(w, w.tile0 * kTileKV + row), pg_v = -1;
                     for (int j = 0; j <= n; ++j) {
                         const int32_t key0 = (w.tile0 + j) * kTileKV;
@@ -404,22 +382,24 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         if (j < n) {
                             const uint32_t c = kv_cnt + j, st = c % kStages;
                             ZL_WAIT_WARP(&sm.k_empty[st], ((c / kStages) & 1) ^ 1, 2);
-                            const int32_t end_row = pg_k >= 0 ? row + min(box, w.keys - (key0 + row)) : 0;  // first row without a key
-                            uint32_t word = 0;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t all = __reduce_or_sync(0xffffffffu, pg_k >= 0 ? low_bits(end_row - 32 * i) & ~low_bits(row - 32 * i) : 0u);
-                                if (lane == i) word = all;
+                            if constexpr (!kCodes) {
+                                const int32_t end_row = pg_k >= 0 ? row + min(box, w.keys - (key0 + row)) : 0;  // first row without a key
+                                uint32_t word = 0;
+    #pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint32_t all = __reduce_or_sync(0xffffffffu, pg_k >= 0 ? low_bits(end_row - 32 * i) & ~low_bits(row - 32 * i) : 0u);
+                                    if (lane == i) word = all;
+                                }
+                                if (lane < 4) sm.mask[c % kMaskRing][lane] = word;
+                                __syncwarp();
+                                if (lane == 0) mbar_arrive(&sm.tile_full[c % kMaskRing]);
                             }
-                            if (lane < 4) sm.mask[c % kMaskRing][lane] = word;
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(&sm.tile_full[c % kMaskRing]);
-                            load(w, sm.k[st], &tm_k, &sm.k_full[st], pg_k, key0 + row);
+                            load(w, sm.k[st], &tm_k, kCodes ? &sm.k_codes[st] : &sm.k_full[st], pg_k, key0 + row);
                         }
                         if (j > 0) {
                             const uint32_t c = kv_cnt + j - 1, st = c % kStages;
                             ZL_WAIT_WARP(&sm.v_empty[st], ((c / kStages) & 1) ^ 1, 3);
-                            load(w, sm.v[st], &tm_v, &sm.v_full[st], pg_v, key0 - kTileKV + row);
+                            load(w, sm.v[st], &tm_v, kCodes ? &sm.v_codes[st] : &sm.v_full[st], pg_v, key0 - kTileKV + row);
                         }
                         pg_v = pg_k;
                         pg_k = pg_next;
@@ -507,19 +487,19 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
     } else if (kCodes && warp >= 12) {
         // ------------------------------------------------------------------ codes to bf16
-        reg_dec<64>();
+        reg_dec<88>();
         if constexpr (kCodes) {
             const int t = threadIdx.x - 384;
-            // This thread's 16-byte pieces of half a tile: piece `ch` of rows r, r + kRowStep, ... (a multiple of 8: the exchange
+            // This thread's 16-byte pieces of a tile of codes: piece `ch` of rows r, r + kRowStep, ... (a multiple of 8: the exchange
             // of pieces within a line is the same for all of them).  A piece of 16 codes becomes two of eight numbers; in the
             // second box the odd one goes first, so that eight lanes meet all banks.
-            constexpr int kChunks = D / 16, kRowStep = 128 / kChunks, kPieces = Smem::kRawRows / kRowStep;
+            constexpr int kChunks = D / 16, kRowStep = 128 / kChunks, kPieces = kTileKV / kRowStep;
             const int r = t / kChunks, ch = t % kChunks;
             const bool swap = ch >= 4;
-            const uint32_t from = r * D + ((ch ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4);
+            const uint32_t from = Smem::kTileBytes / 2 + r * D + ((ch ^ (D == 128 ? r & 7 : (r >> 1) & 3)) << 4);
             const uint32_t to = (ch >> 2) * Smem::kBoxBytes + r * 128;
             const uint32_t to0 = to + (((2 * (ch & 3) + (swap ? 1 : 0)) ^ (r & 7)) << 4), to1 = to0 ^ 16;
-            uint32_t kv_cnt = 0, raw_cnt = 0, item_cnt = 0;
+            uint32_t kv_cnt = 0, read_cnt = 0, item_cnt = 0;
             auto page_of = [&](const Item& w, int32_t key) { return key < w.keys ? page_at(p.b, p.c, w.s, key) : -1; };
             // scales of this thread's key (key t of the tile), zeros without one
             auto scales_of = [&](const Item& w, int32_t key, int32_t pg) {
@@ -575,8 +555,6 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     for (int m = 0; m < 2; ++m) {
                         if (m == 0 ? j == n : j == 0) continue;
                         const uint32_t c = kv_cnt + j - m, st = c % kStages;
-                        uint64_t* const empty = m == 0 ? &sm.k_empty[st] : &sm.v_empty[st];
-                        ZL_WAIT_WARP(empty, ((c / kStages) & 1) ^ 1, 4);
                         if (m == 0) {
                             const uint32_t word = __ballot_sync(0xffffffffu, pg >= 0);
                             const float v_scale = fmaxf(sc.y, kLeastScale);
@@ -590,38 +568,41 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             sc = scales_of(w, key0 + (j + 1) * kTileKV, pg);
                             pg_next = page_of(w, key0 + (j + 2) * kTileKV);
                         }
-                        const uint32_t dst = smem_u32(m == 0 ? sm.k[st] : sm.v[st]);
+                        uint8_t* const tile = m == 0 ? sm.k[st] : sm.v[st];
+                        ZL_WAIT_WARP(m == 0 ? &sm.k_codes[st] : &sm.v_codes[st], (c / kStages) & 1, 5);
+                        uint4 code[kPieces];
+#pragma unroll
+                        for (int i = 0; i < kPieces; ++i) code[i] = *reinterpret_cast<const uint4*>(tile + from + i * kRowStep * D);
+                        // all codes have been read when the first of them is written over
+                        mbar_arrive(&sm.codes_read);
                         // rows without a key may hold codes of NaN: zeros, before they meet their weight of 0
-                        uint4 there = make_uint4(~0u, ~0u, ~0u, ~0u);
                         if (kFormat == ZL_CACHE_E4M3 && m == 1) {
                             ZL_WAIT_WARP(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 32);
-                            there = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
-                        }
-                        const bool holes = (there.x & there.y & there.z & there.w) != ~0u;
-                        for (int h = 0; h < 2; ++h, ++raw_cnt) {
-                            const uint32_t slot = raw_cnt % kRaw;
-                            ZL_WAIT_WARP(&sm.raw_full[slot], (raw_cnt / kRaw) & 1, 5);
-                            uint4 x[kPieces];
+                            const uint4 there = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                            if ((there.x & there.y & there.z & there.w) != ~0u) {
 #pragma unroll
-                            for (int i = 0; i < kPieces; ++i) x[i] = *reinterpret_cast<const uint4*>(sm.raw[slot] + from + i * kRowStep * D);
-#pragma unroll
-                            for (int i = 0; i < kPieces; ++i) {
-                                uint32_t a = swap ? x[i].z : x[i].x, b = swap ? x[i].w : x[i].y, c = swap ? x[i].x : x[i].z, d = swap ? x[i].y : x[i].w;
-                                if (holes) {
-                                    const int row = h * Smem::kRawRows + r + i * kRowStep;
+                                for (int i = 0; i < kPieces; ++i) {
+                                    const int row = r + i * kRowStep;
                                     const uint32_t word = row < 64 ? (row < 32 ? there.x : there.y) : (row < 96 ? there.z : there.w);
-                                    if (!((word >> (row & 31)) & 1)) a = b = c = d = 0;
+                                    if (!((word >> (row & 31)) & 1)) code[i] = make_uint4(0, 0, 0, 0);
                                 }
-                                const uint32_t at = dst + (h * Smem::kRawRows + i * kRowStep) * 128;
-                                uint32_t y[8];
-                                halves<kFormat>(a, y[0], y[1]);
-                                halves<kFormat>(b, y[2], y[3]);
-                                halves<kFormat>(c, y[4], y[5]);
-                                halves<kFormat>(d, y[6], y[7]);
-                                st_shared_v4(at + to0, y[0], y[1], y[2], y[3]);
-                                st_shared_v4(at + to1, y[4], y[5], y[6], y[7]);
                             }
-                            mbar_arrive(&sm.raw_empty[slot]);
+                        }
+                        ZL_WAIT_WARP(&sm.codes_read, read_cnt & 1, 4);
+                        ++read_cnt;
+                        const uint32_t dst = smem_u32(tile);
+#pragma unroll
+                        for (int i = 0; i < kPieces; ++i) {
+                            const uint32_t a = swap ? code[i].z : code[i].x, b = swap ? code[i].w : code[i].y;
+                            const uint32_t c_ = swap ? code[i].x : code[i].z, d = swap ? code[i].y : code[i].w;
+                            const uint32_t at = dst + i * kRowStep * 128;
+                            uint32_t y[8];
+                            halves<kFormat>(a, y[0], y[1]);
+                            halves<kFormat>(b, y[2], y[3]);
+                            halves<kFormat>(c_, y[4], y[5]);
+                            halves<kFormat>(d, y[6], y[7]);
+                            st_shared_v4(at + to0, y[0], y[1], y[2], y[3]);
+                            st_shared_v4(at + to1, y[4], y[5], y[6], y[7]);
                         }
                         fence_proxy_async_smem();
                         mbar_arrive(m == 0 ? &sm.k_full[st] : &sm.v_full[st]);
@@ -633,11 +614,16 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
     } else {
         // ------------------------------------------------------------------ softmax, join and output
-        if constexpr (kCodes) reg_inc<192>(); else reg_inc<216>();
+        if constexpr (kCodes) reg_inc<168>(); else reg_inc<184>();
+        // Scores are read in the layout of an mma accumulator: a thread has 32 columns (8 k + 2 (lane % 4) + {0, 1}) of four rows (lane / 4
+        // + 8 i of the warp's 32).  A scale of a column is so fetched by eight lanes for four rows each; with a row per thread every
+        // thread fetches all of them, and those broadcasts alone kept shared memory busy for 3,000 clocks a tile.
         const int x = (warp - 4) >> 2;
         const int quarter = warp & 3;              // TMEM lane quarter this warp may access
-        const int row = quarter * 32 + lane;
+        const int row = quarter * 32 + lane;       // of the output
+        const int quad = lane & 3;
         const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
+        constexpr uint32_t kSlab = 16u << 16;      // 16 lanes further on
         const uint32_t col_s = kColS + x * 128, col_o = kColO + x * 128;
         const float mul = kCodes ? 1.f : p.scale_log2;  // of 8-bit caches the keys' scales have it
         const int32_t tile_tokens = kTileQ / p.group;
@@ -647,9 +633,23 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const bool two = w.two != 0;
             const int32_t tok = w.tok0 + (two ? x * tile_tokens : 0) + row_tok;  // of the sequence
             const bool row_ok = row_tok < tile_tokens && tok < w.tok0 + w.tokens;
-            // (rows that do not exist hold anything, and take no part in what a warp decides together)
-            const int32_t seen = row_ok ? keys_seen(w.seq(), tok) - w.tile0 * kTileKV : INT32_MAX;
             float m_ref = -INFINITY, l = 0.f;
+            {
+            // (rows that do not exist hold anything, and take no part in what a warp decides together)
+            int32_t seen[4], seen_least = INT32_MAX;
+            uint32_t ok = 0;
+            float m4[4], l4[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t rt = (quarter * 32 + 8 * i + (lane >> 2)) / p.group, tk = w.tok0 + (two ? x * tile_tokens : 0) + rt;
+                const bool there = rt < tile_tokens && tk < w.tok0 + w.tokens;
+                ok |= there ? 1u << i : 0u;
+                seen[i] = there ? keys_seen(w.seq(), tk) - w.tile0 * kTileKV : INT32_MAX;
+                seen_least = min(seen_least, seen[i]);
+                m4[i] = -INFINITY;
+                l4[i] = 0.f;
+            }
+            seen_least = __reduce_min_sync(0xffffffffu, seen_least);
             for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
                 const uint32_t c = kv_cnt + j;
                 const bool first = j == (two ? 0 : x);
@@ -657,102 +657,138 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
                 ++s_cnt;
                 tc_fence_after();
-                float sv[kTileKV];
+                const uint4 m128 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                const bool cut = seen_least - j * kTileKV < kTileKV || (m128.x & m128.y & m128.z & m128.w) != 0xffffffffu;
+                const float2* ks = reinterpret_cast<const float2*>(sm.key_scale[kCodes ? c % Smem::kScaleRing : 0]) + quad;
+                const float2* vl = reinterpret_cast<const float2*>(sm.value_log2[kCodes ? c % Smem::kScaleRing : 0]) + quad;
+                const float2* vi = reinterpret_cast<const float2*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0]) + quad;
+                // Sixteen rows of the warp at a time: two rows per thread, 64 scores.  (All four at once took more registers than there
+                // are, and a spill is an L2 access beside so much shared memory: 525 -> SLAB_US us, 1560 tokens over 9,750 int8 keys.)
 #pragma unroll
-                for (int q = 0; q < kTileKV / 32; ++q) {
-                    uint32_t r[32];
-                    tmem_ld_x32(lane_addr + col_s + q * 32, r);
+                for (int slab = 0; slab < 2; ++slab) {
+                    float2 sv[2][16];  // row, pair of columns
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) sv[q * 32 + i] = __uint_as_float(r[i]);
-                }
-                tmem_wait_ld();
-                if constexpr (kCodes) {
-                    const float4* ks = reinterpret_cast<const float4*>(sm.key_scale[c % Smem::kScaleRing]);
-                    const float4* vl = reinterpret_cast<const float4*>(sm.value_log2[c % Smem::kScaleRing]);
-#pragma unroll
-                    for (int i = 0; i < kTileKV / 4; ++i) {
-                        const float4 f = ks[i], g = vl[i];
-                        const float2 a = fma2(make_float2(sv[4 * i], sv[4 * i + 1]), make_float2(f.x, f.y), make_float2(g.x, g.y));
-                        const float2 b = fma2(make_float2(sv[4 * i + 2], sv[4 * i + 3]), make_float2(f.z, f.w), make_float2(g.z, g.w));
-                        sv[4 * i] = a.x; sv[4 * i + 1] = a.y; sv[4 * i + 2] = b.x; sv[4 * i + 3] = b.y;
-                    }
-                }
-                const uint4 m4 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
-                const int valid = row_ok ? seen - j * kTileKV : kTileKV;
-                if (__any_sync(0xffffffffu, valid < kTileKV) || (m4.x & m4.y & m4.z & m4.w) != 0xffffffffu) {
-                    const uint32_t words[4] = {m4.x & low_bits(valid), m4.y & low_bits(valid - 32), m4.z & low_bits(valid - 64), m4.w & low_bits(valid - 96)};
-#pragma unroll
-                    for (int i = 0; i < kTileKV; ++i)
-                        if (!((words[i >> 5] >> (i & 31)) & 1)) sv[i] = -INFINITY;  // select, never multiply
-                }
-                // four independent chains: a single running maximum is a 64-deep dependent chain
-                float mx0 = max3(sv[0], sv[1], sv[2]), mx1 = max3(sv[3], sv[4], sv[5]);
-                float mx2 = max3(sv[6], sv[7], sv[8]), mx3 = max3(sv[9], sv[10], sv[11]);
-#pragma unroll
-                for (int i = 12; i + 7 < kTileKV; i += 8) {
-                    mx0 = max3(mx0, sv[i], sv[i + 1]);
-                    mx1 = max3(mx1, sv[i + 2], sv[i + 3]);
-                    mx2 = max3(mx2, sv[i + 4], sv[i + 5]);
-                    mx3 = max3(mx3, sv[i + 6], sv[i + 7]);
-                }
-                mx0 = max3(mx0, sv[kTileKV - 4], sv[kTileKV - 3]);
-                mx1 = max3(mx1, sv[kTileKV - 2], sv[kTileKV - 1]);
-                const float mx = fmaxf(max3(mx0, mx1, mx2), mx3);
-                const bool raise = row_ok && (mx - m_ref) * mul > kRescaleThresholdLog2;
-                if (__any_sync(0xffffffffu, raise && !first)) {
-                    // rescale O (the step before this one is complete: S of this one was issued after it)
-                    const float alpha = raise ? ex2((m_ref - mx) * mul) : 1.f;
-#pragma unroll
-                    for (int q = 0; q < D / 32; ++q) {
+                    for (int h = 0; h < 2; ++h) {
                         uint32_t r[32];
-                        tmem_ld_x32(lane_addr + col_o + q * 32, r);
-                        tmem_wait_ld();
+                        tmem_ld_16x64(lane_addr + slab * kSlab + col_s + h * 64, r);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-                        tmem_st_x32(lane_addr + col_o + q * 32, r);
-                    }
-                    l *= alpha;
-                }
-                if (raise) m_ref = mx;
-                const float nmb = m_ref == -INFINITY ? 0.f : -m_ref * mul;  // (a row that has seen no key yet)
-                float2 sum2 = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {  // P goes to the MMA warp in two halves of 64 key columns, rounded once
-                    uint32_t pk[kTileKV / 4];
-                    const float4* vi = reinterpret_cast<const float4*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0] + (kCodes ? h * (kTileKV / 2) : 0));
-#pragma unroll
-                    for (int i = 0; i < kTileKV / 2; i += 4) {
-                        const int cc = h * (kTileKV / 2) + i;
-                        float2 e0 = make_float2(sv[cc], sv[cc + 1]), e1 = make_float2(sv[cc + 2], sv[cc + 3]);
-                        const float2 nm = make_float2(nmb, nmb);
-                        if constexpr (kCodes) {
-                            e0 = add2(e0, nm);
-                            e1 = add2(e1, nm);
-                        } else {
-                            e0 = fma2(e0, make_float2(mul, mul), nm);
-                            e1 = fma2(e1, make_float2(mul, mul), nm);
-                        }
-                        e0 = make_float2(ex2(e0.x), ex2(e0.y));
-                        e1 = make_float2(ex2(e1.x), ex2(e1.y));
-                        if constexpr (kCodes) {
-                            const float4 f = vi[i / 4];
-                            sum2 = fma2(e0, make_float2(f.x, f.y), sum2);
-                            sum2 = fma2(e1, make_float2(f.z, f.w), sum2);
-                            pk[i / 2] = pack_half(e0.x, e0.y);
-                            pk[i / 2 + 1] = pack_half(e1.x, e1.y);
-                        } else {
-                            sum2 = add2(sum2, e0);
-                            sum2 = add2(sum2, e1);
-                            pk[i / 2] = pack_bf16(e0.x, e0.y);
-                            pk[i / 2 + 1] = pack_bf16(e1.x, e1.y);
+                        for (int k = 0; k < 8; ++k) {
+                            sv[0][h * 8 + k] = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
+                            sv[1][h * 8 + k] = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
                         }
                     }
-                    tmem_st_x32(lane_addr + col_s + h * 32, pk);
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(&sm.p_half[x][h]);
+                    tmem_wait_ld();
+                    if constexpr (kCodes) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const float2 f = ks[4 * k], g = vl[4 * k];
+                            sv[0][k] = fma2(sv[0][k], f, g);
+                            sv[1][k] = fma2(sv[1][k], f, g);
+                        }
+                    }
+                    if (cut) {
+                        const uint32_t words[4] = {m128.x, m128.y, m128.z, m128.w};
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const int valid = (ok >> (2 * slab + b)) & 1 ? seen[2 * slab + b] - j * kTileKV : kTileKV;
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {  // select, never multiply
+                                const uint32_t keep = (words[k >> 2] & low_bits(valid - 32 * (k >> 2))) >> (8 * (k & 3) + 2 * quad);
+                                if (!(keep & 1)) sv[b][k].x = -INFINITY;
+                                if (!(keep & 2)) sv[b][k].y = -INFINITY;
+                            }
+                        }
+                    }
+                    float mx[2];
+                    bool raise = false;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        float u = max3(sv[b][0].x, sv[b][0].y, sv[b][1].x), v = max3(sv[b][1].y, sv[b][2].x, sv[b][2].y);
+#pragma unroll
+                        for (int k = 3; k < 15; k += 2) {
+                            u = max3(u, sv[b][k].x, sv[b][k].y);
+                            v = max3(v, sv[b][k + 1].x, sv[b][k + 1].y);
+                        }
+                        mx[b] = fmaxf(max3(u, sv[b][15].x, sv[b][15].y), v);
+                        raise |= ((ok >> (2 * slab + b)) & 1) && (mx[b] - m4[2 * slab + b]) * mul > kRescaleThresholdLog2;
+                    }
+                    if (__any_sync(0xffffffffu, raise)) {
+                        // all lanes of a row take its maximum as the new reference; O is rescaled (the step before this one is complete:
+                        // S of this one was issued after it)
+                        float alpha[2];
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const int i = 2 * slab + b;
+                            mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
+                            mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
+                            alpha[b] = 1.f;
+                            if (((ok >> i) & 1) && mx[b] > m4[i]) {
+                                alpha[b] = ex2((m4[i] - mx[b]) * mul);
+                                m4[i] = mx[b];
+                                l4[i] *= alpha[b];
+                            }
+                        }
+                        if (!first) {
+#pragma unroll 1
+                            for (int h = 0; h < D / 64; ++h) {
+                                const uint32_t at = lane_addr + slab * kSlab + col_o + h * 64;
+                                uint32_t r[32];
+                                tmem_ld_16x64(at, r);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha[(k >> 1) & 1]);
+                                tmem_st_16x64(at, r);
+                            }
+                        }
+                    }
+                    float2 nm[2], sum[2];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const float ref = m4[2 * slab + b], nmb = ref == -INFINITY ? 0.f : -ref * mul;  // (a row that has seen no key yet)
+                        nm[b] = make_float2(nmb, nmb);
+                        sum[b] = make_float2(0.f, 0.f);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {  // P, rounded once
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float2 f = kCodes ? vi[4 * (8 * h + k)] : make_float2(1.f, 1.f);
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                float2 e = sv[b][8 * h + k];
+                                if constexpr (kCodes) e = add2(e, nm[b]); else e = fma2(e, make_float2(mul, mul), nm[b]);
+                                e = make_float2(ex2(e.x), ex2(e.y));
+                                if constexpr (kCodes) {
+                                    sum[b] = fma2(e, f, sum[b]);
+                                    pk[2 * k + b] = pack_half(e.x, e.y);
+                                } else {
+                                    sum[b] = add2(sum[b], e);
+                                    pk[2 * k + b] = pack_bf16(e.x, e.y);
+                                }
+                            }
+                        }
+                        tmem_st_16x32(lane_addr + slab * kSlab + col_s + h * 32, pk);
+                        if (slab == 1) {  // to the MMA warp in two halves of 64 key columns
+                            tmem_wait_st();
+                            tc_fence_before();
+                            mbar_arrive(&sm.p_half[x][h]);
+                        }
+                    }
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) l4[2 * slab + b] += sum[b].x + sum[b].y;
                 }
-                l += sum2.x + sum2.y;
+            }
+            // a row per thread from here on
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 1);
+                l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 2);
+                if (quad == 0) sm.stat[x][quarter * 32 + 8 * i + (lane >> 2)] = make_float2(m4[i], l4[i]);
+            }
+            __syncwarp();
+            m_ref = sm.stat[x][row].x;
+            l = sm.stat[x][row].y;
             }
             // ---- the item's end: weights of the accumulators for this row, and the columns this warpgroup writes
             float wt[2] = {two && x == 1 ? 0.f : 1.f, two && x == 1 ? 1.f : 0.f};
@@ -767,7 +803,6 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     if (two || n > y) ++o_cnt[y];
                 tc_fence_after();
                 if (!two) {
-                    sm.stat[x][row] = make_float2(m_ref, l);
                     mbar_arrive(&sm.stat_full);
                     ZL_WAIT_REGS(&sm.stat_full, join_cnt & 1, 24);
                     const float2 a = sm.stat[0][row], b = sm.stat[1][row];

@@ -193,7 +193,7 @@ cudaError_t launch_cache_read(int head_dim, int format, const CacheView& c, cons
 cudaError_t launch_cached_tokens(int head_dim, int format, const CachedParams& p, int grid, cudaStream_t stream);
 size_t cached_tokens_part_bytes(int head_dim);  // of a CTA's two partial results
 // Maps: tq of [total_q, n_kv_heads, group, d], box 64 columns x group x 1 x whole tokens of 128 rows; tk and tv over the pages, box 64
-// columns of bf16 or a row of codes, rows of one page, at most 128 (bf16) or 64.
+// columns of bf16 or a row of codes, rows of one page, at most 128.
 cudaError_t launch_cached_chunk(int head_dim, int format, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
                                 const CachedParams& p, int grid, cudaStream_t stream);
 size_t cached_chunk_part_bytes(int head_dim);
