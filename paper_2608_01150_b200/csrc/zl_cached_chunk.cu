@@ -2,7 +2,7 @@
 //
 // The rows of a key head are its sequence's new tokens times the query heads of its group; a tile takes as many whole tokens as
 // fit 128 rows, so that one box of Q holds a tile.  An item is two such tiles (or the one that is left) of a sequence and key
-// head.  All CTAs (one per SM) walk one line of work, measured in keys times tiles, and each takes an equal stretch of it,
+// head.  All CTAs (one per SM) walk one line of work and each takes an equal stretch of it,
 // wherever that cuts an item; the lengths are read when the kernel runs.  Stretches are found from sums in closed form: block b
 // of a sequence sees min(keys, max(prefix, pos0 + (b + 1) tokens)) keys.
 //   warp 0       TMA producer: Q once per item, K and V page by page through shared-memory rings
@@ -28,8 +28,11 @@ constexpr uint64_t kWaitLimitNs = 4000000000ull;
 constexpr float kRescaleThresholdLog2 = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaskRing = 8;   // key tiles whose masks are kept: more than can be under way
-constexpr int32_t kItemCost = 512;   // start and end of an item, in keys times tiles
-constexpr int64_t kLeastUnits = 1024;  // least stretch of a CTA
+// Units of work: a key tile under two query tiles takes 4,700 clocks (bf16, 8-bit codes 5,500), under one 2,800 (3,600).  Counted as
+// half, the CTAs with single tiles finished a fifth later than the others.
+constexpr int32_t kTwoCost = 8, kOneCost = 5;  // a key under two query tiles, under one
+constexpr int32_t kItemCost = 1536;            // start and end of an item
+constexpr int64_t kLeastUnits = 4 * kTileKV * kTwoCost;  // least stretch of a CTA
 
 // A CTA's part of an item, as warp 2 hands it to the other warps.
 struct alignas(16) Item {
@@ -99,9 +102,9 @@ struct SeqLine {
         return keys_seen(v, b * 2 * g.tokens + block_tokens(g, b) - 1);
     }
     __device__ __forceinline__ int64_t block_cost(const Geometry& g, int b) const {
-        return kItemCost + (int64_t)block_keys(g, b) * (block_tokens(g, b) > g.tokens ? 2 : 1);
+        return kItemCost + (int64_t)block_keys(g, b) * (block_tokens(g, b) > g.tokens ? kTwoCost : kOneCost);
     }
-    // Cost of blocks 0 .. b - 1 for one head, all of them full: sum of 2 * min(keys, max(prefix, pos0 + (i + 1) T)).
+    // Cost of blocks 0 .. b - 1 for one head, all of them full: kTwoCost times the sum of min(keys, max(prefix, pos0 + (i + 1) T)).
     __device__ __forceinline__ int64_t cost_before(const Geometry& g, int b) const {
         const int32_t T = 2 * g.tokens;
         const int64_t by_prefix = min(v.keys, max(v.prefix, 0));
@@ -111,7 +114,7 @@ struct SeqLine {
             i1 = v.keys < v.pos0 ? i0 : max(i0, min((int64_t)b, ((int64_t)v.keys - v.pos0) / T));
         }
         const int64_t keys = i0 * by_prefix + (i1 - i0) * v.pos0 + (i1 * (i1 + 1) - i0 * (i0 + 1)) / 2 * T + (b - i1) * (int64_t)v.keys;
-        return (int64_t)b * kItemCost + 2 * keys;
+        return (int64_t)b * kItemCost + kTwoCost * keys;
     }
     __device__ __forceinline__ int64_t units(const Geometry& g) const {
         return blocks == 0 ? 0 : g.heads * (cost_before(g, blocks - 1) + block_cost(g, blocks - 1));
@@ -152,7 +155,7 @@ struct ItemWalk {
             const int32_t keys = line.block_keys(g, lo), tokens = line.block_tokens(g, lo);
             const bool two = tokens > g.tokens;
             const int32_t tiles = (keys + kTileKV - 1) / kTileKV;
-            const int64_t step = kTileKV * (two ? 2 : 1), first = item0 + kItemCost;  // tile t lies where its first key does
+            const int64_t step = kTileKV * (two ? kTwoCost : kOneCost), first = item0 + kItemCost;  // tile t lies where its first key does
             auto tiles_before = [&](int64_t u) { return u <= first ? 0 : (int32_t)min((int64_t)tiles, (u - first + step - 1) / step); };
             const int32_t tile0 = tiles_before(at), tile1 = tiles_before(stop);
             const bool starts_here = at == item0;
