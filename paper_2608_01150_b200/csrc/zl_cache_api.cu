@@ -11,7 +11,7 @@ struct zl_cached_attn {
     int32_t n_heads = 0, n_kv_heads = 0, head_dim = 0;
     int device = -1;  // -1: host-only handle (no CUDA device present)
     int n_sms = 0;
-    int32_t* d_words = nullptr;  // [0, 2): status; from kCounters on two counters per SM
+    int32_t* d_words = nullptr;  // [0, 2): status; from kCounters on one counter per SM
 };
 
 namespace {
@@ -19,6 +19,8 @@ namespace {
 constexpr int kCounters = 64;  // a line of its own for the status word
 
 size_t tokens_bytes(const zl_cached_attn& a) { return align_up((size_t)a.n_sms * cached_tokens_part_bytes(a.head_dim), 256); }
+
+size_t chunk_bytes(const zl_cached_attn& a) { return align_up((size_t)a.n_sms * cached_chunk_part_bytes(a.head_dim), 256); }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -161,7 +163,7 @@ zl_status zl_build_cached_attn(int32_t n_heads, int32_t n_kv_heads, int32_t head
         return ZL_ERR_CUDA;
     }
     if (major != 10) { delete h; return ZL_ERR_UNSUPPORTED; }
-    const size_t bytes = (size_t)(kCounters + 2 * n_sms) * sizeof(int32_t);
+    const size_t bytes = (size_t)(kCounters + n_sms) * sizeof(int32_t);
     if (cudaMalloc(&h->d_words, bytes) != cudaSuccess) { delete h; return ZL_ERR_CUDA; }
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (cudaMemsetAsync(h->d_words, 0, bytes, cs) != cudaSuccess || cudaStreamSynchronize(cs) != cudaSuccess) {
@@ -183,7 +185,7 @@ void zl_free_cached_attn(zl_cached_attn* attn) {
 
 zl_status zl_cached_attn_workspace_bytes(const zl_cached_attn* attn, size_t* bytes) {
     if (!attn || !bytes) return ZL_ERR_INVALID_ARG;
-    *bytes = tokens_bytes(*attn) + align_up((size_t)attn->n_sms * cached_chunk_part_bytes(attn->head_dim), 256);
+    *bytes = tokens_bytes(*attn) + chunk_bytes(*attn) + align_up((size_t)attn->n_sms * cached_chunk_cut_bytes(), 256);
     return ZL_OK;
 }
 
@@ -197,7 +199,7 @@ zl_status zl_cached_attn_device_status(const zl_cached_attn* attn, int32_t* code
     zl_status st = ZL_OK;
     if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(words, attn->d_words, sizeof(words), cudaMemcpyDeviceToHost) != cudaSuccess)
         st = ZL_ERR_CUDA;
-    if (st == ZL_OK && words[0] != 0 && cudaMemset(attn->d_words, 0, (size_t)(kCounters + 2 * attn->n_sms) * sizeof(int32_t)) != cudaSuccess)
+    if (st == ZL_OK && words[0] != 0 && cudaMemset(attn->d_words, 0, (size_t)(kCounters + attn->n_sms) * sizeof(int32_t)) != cudaSuccess)
         st = ZL_ERR_CUDA;
     cudaSetDevice(prev);
     *code = words[0];
@@ -235,7 +237,7 @@ zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cach
     p.part = static_cast<float*>(workspace);
     p.part_count = attn->d_words + kCounters;
     p.chunk_part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + tokens_bytes(*attn));
-    p.chunk_count = p.part_count + attn->n_sms;
+    p.chunk_cut = static_cast<uint8_t*>(workspace) + tokens_bytes(*attn) + chunk_bytes(*attn);
     p.status = attn->d_words;
     // Sequences of more rows per key head than an item of the tokens kernel has are the chunk kernel's.  Where max_q says that
     // there are none, or that all are of that kind (as many rows as the longest times their number), the other kernel is not
@@ -254,6 +256,8 @@ zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cach
         CUtensorMap tq, tk, tv;
         if (!make_maps(*cache, p, &tq, &tk, &tv)) return ZL_ERR_CUDA;
         if (launch_cached_chunk(attn->head_dim, cache->format, tq, tk, tv, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
+        count_launch();
+        if (launch_cached_join(attn->head_dim, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
         count_launch();
     }
     if (!chunk || p.split) {

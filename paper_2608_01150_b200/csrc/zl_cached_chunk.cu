@@ -14,8 +14,8 @@
 //                becomes), and so do the queries of an item; the scale of a key multiplies its column of S, the scale of a value its column of P, in
 //                fp32: the softmax takes s_j = S_j k_j + log2 v_j, so that its exponentials are the weights of the values, and sums
 //                weight / v_j beside them
-// An item that lies in several CTAs leaves its parts in the workspace, and the one that finishes last joins them in the order
-// of the CTAs.
+// An item that lies in several CTAs leaves its parts in the workspace, and a second launch joins them, in the order of the CTAs: a
+// part is 133 KB, and one CTA alone took 20 us to join the six parts of 256 rows over 8,700 keys.
 #include "zl_cache.cuh"
 
 namespace zl {
@@ -71,9 +71,9 @@ struct ChunkSmem {
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
     uint64_t k_codes[kCodes ? kStages : 1], v_codes[kCodes ? kStages : 1], codes_read;
     uint64_t s_full[2], p_half[2][2], o_full[2], tile_full[kMaskRing];
-    uint64_t stat_full, join_done, part_bar, item_full[kItems], item_empty[kItems];
+    uint64_t stat_full, join_done, item_full[kItems], item_empty[kItems];
     int64_t scan[16], start_base, total;
-    int32_t start_seq, ticket;
+    int32_t start_seq;
     uint32_t tmem_base;
     volatile int32_t abort_flag;
 };
@@ -260,7 +260,6 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         for (int s = 0; s < kMaskRing; ++s) mbar_init(&sm.tile_full[s], kCodes ? 128 : 1);
         mbar_init(&sm.stat_full, 256);
         mbar_init(&sm.join_done, 256);
-        mbar_init(&sm.part_bar, 256);
         for (int i = 0; i < kItems; ++i) {
             mbar_init(&sm.item_full[i], 1);
             mbar_init(&sm.item_empty[i], kCodes ? 14 : 10);  // warps that read it
@@ -325,23 +324,29 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     const bool idle = per * blockIdx.x >= total;
 
     if (idle) {
-        // nothing to do
+        if (threadIdx.x == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;
     } else if (warp < 4) {
         if constexpr (kCodes) reg_dec<88>(); else reg_dec<136>();
         if (warp == 2) {
             // -------------------------------------------------------------- the line of work
             ItemWalk walk(p, sm.start_seq, sm.start_base, per, total);
             bool more = true;
+            bool cut = false;  // an item's first part is the last of this CTA's stretch
             for (uint32_t it = 0; more; ++it) {
                 Item w;
                 more = walk.next(w);
                 if (!more) w.tile1 = -1;
+                if (more && w.c_first == (int32_t)blockIdx.x && w.c_last > w.c_first) {
+                    cut = true;
+                    if (lane == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x] = w;
+                }
                 ZL_WAIT_WARP(&sm.item_empty[it % kItems], ((it / kItems) & 1) ^ 1, 9);
                 if (lane == 0) {
                     sm.items[it % kItems] = w;
                     mbar_arrive(&sm.item_full[it % kItems]);
                 }
             }
+            if (lane == 0 && !cut) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;
         } else if (warp == 0) {
             // -------------------------------------------------------------- TMA producer (a lane per page)
             const int32_t tile_tokens = kTileQ / p.group;
@@ -872,60 +877,6 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 ZL_WAIT_REGS(&sm.join_done, join_cnt & 1, 25);
                 ++join_cnt;
             }
-            if (!whole) {
-                // ---- the part that finishes last joins all of them, in order (an even number of barrier phases)
-                __threadfence();
-                mbar_arrive(&sm.part_bar);
-                ZL_WAIT_REGS(&sm.part_bar, 0, 26);
-                if (threadIdx.x == 128) sm.ticket = atomicAdd(p.chunk_count + c_first, 1);
-                mbar_arrive(&sm.part_bar);
-                ZL_WAIT_REGS(&sm.part_bar, 1, 27);
-                if (sm.ticket == c_last - c_first) {
-                    __threadfence();
-                    if (row_ok) {
-                        float mm = -INFINITY, ll = 0.f;
-                        for (int32_t cta = c_first; cta <= c_last; ++cta) mm = fmaxf(mm, __ldcg(part_of(cta) + row));
-                        if (mm > -INFINITY)
-                            for (int32_t cta = c_first; cta <= c_last; ++cta)
-                                ll = fmaf(ex2(__ldcg(part_of(cta) + row) - mm), __ldcg(part_of(cta) + kTileQ + row), ll);
-                        const float scale = ll > 0.f ? 1.f / ll : 0.f;
-#pragma unroll 1
-                        for (int q = 0; q < n_cols / 32; ++q) {
-                            float o[32];
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = 0.f;
-                            if (mm > -INFINITY)
-#pragma unroll 1
-                                for (int32_t cta = c_first; cta <= c_last; ++cta) {
-                                    const float* part = part_of(cta);
-                                    const float f = ex2(__ldcg(part + row) - mm);
-                                    const float4* from = reinterpret_cast<const float4*>(part + 2 * kTileQ) + (c0 / 4 + q * 8) * kTileQ + row;
-                                    float4 y[8];
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i) y[i] = __ldcg(from + i * kTileQ);
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i) {
-                                        o[4 * i] = fmaf(f, y[i].x, o[4 * i]);
-                                        o[4 * i + 1] = fmaf(f, y[i].y, o[4 * i + 1]);
-                                        o[4 * i + 2] = fmaf(f, y[i].z, o[4 * i + 2]);
-                                        o[4 * i + 3] = fmaf(f, y[i].w, o[4 * i + 3]);
-                                    }
-                                }
-#pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                uint4 o4;
-                                o4.x = pack_bf16(o[i] * scale, o[i + 1] * scale);
-                                o4.y = pack_bf16(o[i + 2] * scale, o[i + 3] * scale);
-                                o4.z = pack_bf16(o[i + 4] * scale, o[i + 5] * scale);
-                                o4.w = pack_bf16(o[i + 6] * scale, o[i + 7] * scale);
-                                *reinterpret_cast<uint4*>(p.o + o_at + q * 32 + i) = o4;
-                            }
-                        }
-                        if (has_lse && p.lse) p.lse[(int64_t)q_head * p.b.total_q + grow] = ll > 0.f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
-                    }
-                    if (threadIdx.x == 128) p.chunk_count[c_first] = 0;  // for the next launch
-                }
-            }
             kv_cnt += n;
         ZL_ITEM_DONE
     }
@@ -937,6 +888,67 @@ teardown:
         __syncwarp();
         tc_fence_after();
         tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ parts of cut items
+// Block (c, i): rows 32 i .. of the item that is cut first in CTA c, a row per lane.
+// O = sum_c 2^(m_c - max) O_c / sum_c 2^(m_c - max) l_c over its parts.
+constexpr int kJoinThreads = 128, kJoinRows = 32;
+
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads)
+zl_cached_join_kernel(const CachedParams p) {
+    __shared__ __align__(16) __nv_bfloat16 out[kJoinRows][D + 8];
+    grid_release();
+    grid_wait();
+    const Item w = reinterpret_cast<const Item*>(p.chunk_cut)[blockIdx.x];
+    if (w.tile1 < 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tile = blockIdx.y * kJoinRows / kTileQ, row0 = blockIdx.y * kJoinRows % kTileQ, row = row0 + lane;
+    const int32_t tile_tokens = kTileQ / p.group, tok0 = w.tok0 + tile * tile_tokens;
+    if ((tile == 1 && !w.two) || row0 / p.group >= min(tile_tokens, w.tok0 + w.tokens - tok0)) return;
+    const int32_t parts = w.c_last - w.c_first + 1;
+    auto part_of = [&](int32_t i) {
+        return p.chunk_part + (((int64_t)(w.c_first + i) * 2 + (i == 0 ? w.place_first : 0)) * 2 + tile) * kPartTileFloats<D>;
+    };
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < parts; ++i) m = fmaxf(m, __ldcg(part_of(i) + row));
+    constexpr int kEach = D / 4 / (kJoinThreads / 32);  // quadruples of columns of a warp
+    float4 acc[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) acc[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (m > -INFINITY) {
+#pragma unroll 2
+        for (int i = 0; i < parts; ++i) {
+            const float* part = part_of(i);
+            const float f = ex2(__ldcg(part + row) - m);
+            l = fmaf(f, __ldcg(part + kTileQ + row), l);
+            const float4* from = reinterpret_cast<const float4*>(part + 2 * kTileQ) + (warp * kEach) * kTileQ + row;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const float4 x = __ldcg(from + e * kTileQ);
+                acc[e].x = fmaf(f, x.x, acc[e].x); acc[e].y = fmaf(f, x.y, acc[e].y); acc[e].z = fmaf(f, x.z, acc[e].z); acc[e].w = fmaf(f, x.w, acc[e].w);
+            }
+        }
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e)
+        *reinterpret_cast<uint2*>(&out[lane][(warp * kEach + e) * 4]) = make_uint2(pack_bf16(acc[e].x * inv, acc[e].y * inv), pack_bf16(acc[e].z * inv, acc[e].w * inv));
+    __syncthreads();
+    constexpr int kChunks = D / 8;
+    for (int j = threadIdx.x; j < kJoinRows * kChunks; j += kJoinThreads) {
+        const int r = j / kChunks, tok = (row0 + r) / p.group, head = w.head * p.group + (row0 + r) - tok * p.group;
+        if (tok >= tile_tokens || tok0 + tok >= w.tok0 + w.tokens) continue;
+        const int64_t grow = (int64_t)w.q0 + tok0 + tok;
+        *reinterpret_cast<uint4*>(p.o + (grow * p.n_heads + head) * D + j % kChunks * 8) = *reinterpret_cast<const uint4*>(&out[r][j % kChunks * 8]);
+    }
+    if (warp == 0 && p.lse) {
+        const int tok = row / p.group, head = w.head * p.group + row - tok * p.group;
+        if (tok < tile_tokens && tok0 + tok < w.tok0 + w.tokens)
+            p.lse[(int64_t)head * p.b.total_q + w.q0 + tok0 + tok] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
     }
 }
 
@@ -961,6 +973,20 @@ cudaError_t launch_t(const CUtensorMap& tq, const CUtensorMap& tk, const CUtenso
 
 size_t cached_chunk_part_bytes(int head_dim) {
     return 4 * sizeof(float) * (head_dim == 128 ? kPartTileFloats<128> : kPartTileFloats<64>);
+}
+size_t cached_chunk_cut_bytes() { return sizeof(Item); }
+
+cudaError_t launch_cached_join(int head_dim, const CachedParams& p, int ctas, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ctas, 2 * kTileQ / kJoinRows);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, head_dim == 128 ? zl_cached_join_kernel<128> : zl_cached_join_kernel<64>, p);
 }
 
 cudaError_t launch_cached_chunk(int head_dim, int format, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,

@@ -180,7 +180,7 @@ struct CachedParams {
     float* part;         // two partial results per CTA
     int32_t* part_count; // per CTA: finished parts of the item that is cut first in it; zero between launches
     float* chunk_part;   // the same of the kernel for chunks
-    int32_t* chunk_count;
+    void* chunk_cut;     // per CTA of it: the item that is cut first in it
     int32_t split;       // both kernels run: sequences of at most token_rows rows per key head are the tokens kernel's
     int32_t token_rows;  // rows of an item of the tokens kernel: 8 or kTokenRows
     int32_t head_first;  // coordinates of the K and V maps are (column, head, token, page), else (column, token, head, page)
@@ -196,7 +196,10 @@ size_t cached_tokens_part_bytes(int head_dim);  // of a CTA's two partial result
 // columns of bf16 or a row of codes, rows of one page, at most 128.
 cudaError_t launch_cached_chunk(int head_dim, int format, const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv,
                                 const CachedParams& p, int grid, cudaStream_t stream);
-size_t cached_chunk_part_bytes(int head_dim);
+size_t cached_chunk_part_bytes(int head_dim);  // of a CTA's two partial results
+size_t cached_chunk_cut_bytes();
+// Joins the parts of items that the chunk kernel's CTAs share.
+cudaError_t launch_cached_join(int head_dim, const CachedParams& p, int ctas, cudaStream_t stream);
 
 // Of the C-ABI layer.
 void count_launch();
