@@ -326,7 +326,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     if (idle) {
         if (threadIdx.x == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;
     } else if (warp < 4) {
-        if constexpr (kCodes) reg_dec<88>(); else reg_dec<136>();
+        if constexpr (kCodes) reg_dec<88>(); else reg_dec<72>();
         if (warp == 2) {
             // -------------------------------------------------------------- the line of work
             ItemWalk walk(p, sm.start_seq, sm.start_base, per, total);
@@ -425,71 +425,133 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const uint64_t dk0 = make_desc_sw128(smem_u32(sm.k[0]), 16, 1024);
             const uint64_t dv0 = make_desc_sw128(smem_u32(sm.v[0]), Smem::kBoxBytes, 1024);  // V is the MN-major B operand
             constexpr uint32_t kTileStep = Smem::kTileBytes >> 4;
-            uint32_t item_cnt = 0, kv_cnt = 0, pa_cnt = 0, pb_cnt = 0;
-            ZL_FOR_ITEMS(ZL_WAIT_WARP, 7)
-                const bool two = w.two != 0;
-                const int steps = two ? 2 * n : n;
-                if (steps > 0) {
-                ZL_WAIT_WARP(kCodes ? &sm.q_ready : &sm.q_full, item_cnt & 1, 11);
-                ++item_cnt;
-                // step u: S of step u, then (before it) P V of step u - 2; x is the accumulator, j the key tile
-                for (int u = 0; u < steps + 2; ++u) {
-                    const int x = u & 1;
-                    if (u >= 2) {
-                        const int j = two ? (u - 2) >> 1 : u - 2;
-                        const uint32_t c = kv_cnt + j, st = c % kStages;
-                        if (!two || x == 0) {
-                            ZL_WAIT_WARP(&sm.v_full[st], (c / kStages) & 1, 12);
-                            if constexpr (!kCodes) {
-                                // rows without a key may hold anything, NaN too: zeros, before they meet their weight of 0
-                                const uint4 m4 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
-                                if ((m4.x & m4.y & m4.z & m4.w) != 0xffffffffu) {
-                                    const uint32_t words[4] = {m4.x, m4.y, m4.z, m4.w};
-                                    for (int i = 0; i < 4; ++i) {
-                                        if ((words[i] >> lane) & 1) continue;
-                                        const uint32_t at = smem_u32(sm.v[st]) + (i * 32 + lane) * 128;
-#pragma unroll 1
-                                        for (int e = 0; e < 8 * kBoxes; ++e)
-                                            st_shared_v4(at + (e >> 3) * Smem::kBoxBytes + (((e + lane) & 7) << 4), 0, 0, 0, 0);
-                                    }
-                                    fence_proxy_async_smem();
-                                    __syncwarp();
-                                }
-                            }
-                        }
-                        const uint64_t dv = dv0 + st * kTileStep;
-#pragma unroll 1
-                        for (int half = 0; half < 2; ++half) {
-                            ZL_WAIT_WARP(&sm.p_half[x][half], (x == 0 ? pa_cnt : pb_cnt) & 1, 13);
-                            tc_fence_after();
+            // Stages and phases are counted, not computed: this warp's own instructions lie on the way from P to the next scores.
+            uint32_t item_cnt = 0, tile_cnt = 0, k_st = 0, k_ph = 0, v_st = 0, v_ph = 0, p_ph[2] = {0, 0};
+            auto issue_s = [&](int x, int q) {  // S_x = Q_q K^T, over P_x of the step before: ordered after its P V on the tensor pipe
+                const uint64_t dq = dq0 + q * kTileStep, dk = dk0 + k_st * kTileStep;
 #pragma unroll
-                            for (int ks = 0; ks < kTileKV / 32; ++ks) {
-                                const int at = half * (kTileKV / 32) + ks;
-                                if (mma_lane) mma_ts(tmem + kColO + x * 128, tmem + kColS + x * 128 + at * 8, dv + at * (2048 >> 4),
-                                                     idesc_o, u > 3 || half > 0 || ks > 0);
-                            }
-                        }
-                        if (x == 0) ++pa_cnt; else ++pb_cnt;
-                        if (!two || x == 1) if (mma_lane) mma_commit(&sm.v_empty[st]);
-                        if (u >= steps) if (mma_lane) mma_commit(&sm.o_full[x]);  // the accumulator's last step
-                    }
-                    if (u < steps) {
-                        const int j = two ? u >> 1 : u;
-                        const uint32_t c = kv_cnt + j, st = c % kStages;
-                        if (!two || x == 0) ZL_WAIT_WARP(&sm.k_full[st], (c / kStages) & 1, 15);
-                        tc_fence_after();
-                        const uint64_t dq = dq0 + (two ? x : 0) * kTileStep, dk = dk0 + st * kTileStep;
+                for (int ks = 0; ks < D / 16; ++ks) {
+                    const uint32_t off = ((ks / 4) * Smem::kBoxBytes + (ks % 4) * 32) >> 4;
+                    if (mma_lane) mma_ss(tmem + kColS + x * 128, dq + off, dk + off, idesc_s, ks > 0);
+                }
+                if (mma_lane) mma_commit(&sm.s_full[x]);
+            };
+            auto issue_pv = [&](int x, int half, bool acc) {  // O_x (+)= P_x V over one half of the key columns
+                const uint64_t dv = dv0 + v_st * kTileStep + half * (kTileKV / 32) * (2048 >> 4);
 #pragma unroll
-                        for (int ks = 0; ks < D / 16; ++ks) {  // over P_x of step u - 2: ordered after P_x V on the tensor pipe
-                            const uint32_t off = ((ks / 4) * Smem::kBoxBytes + (ks % 4) * 32) >> 4;
-                            if (mma_lane) mma_ss(tmem + kColS + x * 128, dq + off, dk + off, idesc_s, ks > 0);
+                for (int ks = 0; ks < kTileKV / 32; ++ks)
+                    if (mma_lane)
+                        mma_ts(tmem + kColO + x * 128, tmem + kColS + x * 128 + (half * (kTileKV / 32) + ks) * 8, dv + ks * (2048 >> 4), idesc_o, acc || ks > 0);
+            };
+            auto done_with_k = [&]() {
+                if (mma_lane) mma_commit(&sm.k_empty[k_st]);
+                if (++k_st == kStages) { k_st = 0; k_ph ^= 1; }
+            };
+            auto done_with_v = [&]() {
+                if (mma_lane) mma_commit(&sm.v_empty[v_st]);
+                if (++v_st == kStages) { v_st = 0; v_ph ^= 1; }
+                ++tile_cnt;
+            };
+            // bf16: rows without a key may hold anything, NaN too: zeros, before they meet their weight of 0
+            auto clean_v = [&]() {
+                if constexpr (!kCodes) {
+                    const uint4 m4 = *reinterpret_cast<const uint4*>(sm.mask[tile_cnt % kMaskRing]);
+                    if ((m4.x & m4.y & m4.z & m4.w) != 0xffffffffu) {
+                        const uint32_t words[4] = {m4.x, m4.y, m4.z, m4.w};
+                        for (int i = 0; i < 4; ++i) {
+                            if ((words[i] >> lane) & 1) continue;
+                            const uint32_t at = smem_u32(sm.v[v_st]) + (i * 32 + lane) * 128;
+#pragma unroll 1
+                            for (int e = 0; e < 8 * kBoxes; ++e) st_shared_v4(at + (e >> 3) * Smem::kBoxBytes + (((e + lane) & 7) << 4), 0, 0, 0, 0);
                         }
-                        if (mma_lane) mma_commit(&sm.s_full[x]);
-                        if (!two || x == 1) if (mma_lane) mma_commit(&sm.k_empty[st]);
-                        if (u + 1 == steps) if (mma_lane) mma_commit(&sm.q_empty);
+                        fence_proxy_async_smem();
+                        __syncwarp();
                     }
                 }
-                kv_cnt += n;
+            };
+#define ZL_PV(x_, acc_)                                                \
+            do {                                                       \
+                ZL_WAIT_WARP(&sm.p_half[x_][0], p_ph[x_], 13);         \
+                tc_fence_after();                                      \
+                issue_pv(x_, 0, acc_);                                 \
+                ZL_WAIT_WARP(&sm.p_half[x_][1], p_ph[x_], 14);         \
+                tc_fence_after();                                      \
+                issue_pv(x_, 1, true);                                 \
+                p_ph[x_] ^= 1;                                         \
+            } while (0)
+            ZL_FOR_ITEMS(ZL_WAIT_WARP, 7)
+                if (n > 0) {
+                    ZL_WAIT_WARP(kCodes ? &sm.q_ready : &sm.q_full, item_cnt & 1, 11);
+                    ++item_cnt;
+                    ZL_WAIT_WARP(&sm.k_full[k_st], k_ph, 15);
+                    tc_fence_after();
+                    issue_s(0, 0);
+                    if (w.two) {
+                        issue_s(1, 1);
+                        done_with_k();
+                        if (n == 1) if (mma_lane) mma_commit(&sm.q_empty);
+                        for (int j = 0; j < n; ++j) {
+                            const bool next = j + 1 < n;
+                            ZL_WAIT_WARP(&sm.v_full[v_st], v_ph, 12);
+                            clean_v();
+                            ZL_PV(0, j > 0);
+                            if (next) {
+                                ZL_WAIT_WARP(&sm.k_full[k_st], k_ph, 16);
+                                tc_fence_after();
+                                issue_s(0, 0);
+                            } else if (mma_lane) {
+                                mma_commit(&sm.o_full[0]);
+                            }
+                            ZL_PV(1, j > 0);
+                            done_with_v();
+                            if (next) {
+                                issue_s(1, 1);
+                                done_with_k();
+                                if (j + 2 == n) if (mma_lane) mma_commit(&sm.q_empty);  // the item's last S
+                            } else if (mma_lane) {
+                                mma_commit(&sm.o_full[1]);
+                            }
+                        }
+                    } else {
+                        // key tiles in turn to the two accumulators: S two tiles ahead of P V
+                        done_with_k();
+                        if (n > 1) {
+                            ZL_WAIT_WARP(&sm.k_full[k_st], k_ph, 17);
+                            tc_fence_after();
+                            issue_s(1, 0);
+                            done_with_k();
+                        }
+                        if (n <= 2) if (mma_lane) mma_commit(&sm.q_empty);
+                        for (int j = 0; j < n; j += 2) {
+                            ZL_WAIT_WARP(&sm.v_full[v_st], v_ph, 18);
+                            clean_v();
+                            ZL_PV(0, j > 0);
+                            done_with_v();
+                            if (j + 2 < n) {
+                                ZL_WAIT_WARP(&sm.k_full[k_st], k_ph, 19);
+                                tc_fence_after();
+                                issue_s(0, 0);
+                                done_with_k();
+                                if (j + 3 == n) if (mma_lane) mma_commit(&sm.q_empty);
+                            } else if (mma_lane) {
+                                mma_commit(&sm.o_full[0]);
+                            }
+                            if (j + 1 == n) break;
+                            ZL_WAIT_WARP(&sm.v_full[v_st], v_ph, 40);
+                            clean_v();
+                            ZL_PV(1, j > 0);
+                            done_with_v();
+                            if (j + 3 < n) {
+                                ZL_WAIT_WARP(&sm.k_full[k_st], k_ph, 41);
+                                tc_fence_after();
+                                issue_s(1, 0);
+                                done_with_k();
+                                if (j + 4 == n) if (mma_lane) mma_commit(&sm.q_empty);
+                            } else if (mma_lane) {
+                                mma_commit(&sm.o_full[1]);
+                            }
+                        }
+                    }
                 }
             ZL_ITEM_DONE
         }
@@ -622,10 +684,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
     } else {
         // ------------------------------------------------------------------ softmax, join and output
-        if constexpr (kCodes) reg_inc<168>(); else reg_inc<184>();
-        // Scores are read in the layout of an mma accumulator: a thread has 32 columns (8 k + 2 (lane % 4) + {0, 1}) of four rows (lane / 4
-        // + 8 i of the warp's 32).  A scale of a column is so fetched by eight lanes for four rows each; with a row per thread every
-        // thread fetches all of them, and those broadcasts alone kept shared memory busy for 3,000 clocks a tile.
+        if constexpr (kCodes) reg_inc<168>(); else reg_inc<216>();
         const int x = (warp - 4) >> 2;
         const int quarter = warp & 3;              // TMEM lane quarter this warp may access
         const int row = quarter * 32 + lane;       // of the output
@@ -641,162 +700,247 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const bool two = w.two != 0;
             const int32_t tok = w.tok0 + (two ? x * tile_tokens : 0) + row_tok;  // of the sequence
             const bool row_ok = row_tok < tile_tokens && tok < w.tok0 + w.tokens;
-            float m_ref = -INFINITY, l = 0.f;
-            {
             // (rows that do not exist hold anything, and take no part in what a warp decides together)
-            int32_t seen[4], seen_least = INT32_MAX;
-            uint32_t ok = 0;
-            float m4[4], l4[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t rt = (quarter * 32 + 8 * i + (lane >> 2)) / p.group, tk = w.tok0 + (two ? x * tile_tokens : 0) + rt;
-                const bool there = rt < tile_tokens && tk < w.tok0 + w.tokens;
-                ok |= there ? 1u << i : 0u;
-                seen[i] = there ? keys_seen(w.seq(), tk) - w.tile0 * kTileKV : INT32_MAX;
-                seen_least = min(seen_least, seen[i]);
-                m4[i] = -INFINITY;
-                l4[i] = 0.f;
-            }
-            seen_least = __reduce_min_sync(0xffffffffu, seen_least);
-            for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
-                const uint32_t c = kv_cnt + j;
-                const bool first = j == (two ? 0 : x);
-                ZL_WAIT_REGS(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 20);
-                ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
-                ++s_cnt;
-                tc_fence_after();
-                const uint4 m128 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
-                const bool cut = seen_least - j * kTileKV < kTileKV || (m128.x & m128.y & m128.z & m128.w) != 0xffffffffu;
-                const float2* ks = reinterpret_cast<const float2*>(sm.key_scale[kCodes ? c % Smem::kScaleRing : 0]) + quad;
-                const float2* vl = reinterpret_cast<const float2*>(sm.value_log2[kCodes ? c % Smem::kScaleRing : 0]) + quad;
-                const float2* vi = reinterpret_cast<const float2*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0]) + quad;
-                // Sixteen rows of the warp at a time: two rows per thread, 64 scores.  (All four at once took more registers than there
-                // are, and a spill is an L2 access beside so much shared memory: 525 -> SLAB_US us, 1560 tokens over 9,750 int8 keys.)
-#pragma unroll
-                for (int slab = 0; slab < 2; ++slab) {
-                    float2 sv[2][16];  // row, pair of columns
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+            float m_ref = -INFINITY, l = 0.f;
+            if constexpr (!kCodes) {
+                const int32_t seen = row_ok ? keys_seen(w.seq(), tok) - w.tile0 * kTileKV : INT32_MAX;
+                for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
+                    const uint32_t c = kv_cnt + j;
+                    const bool first = j == (two ? 0 : x);
+                    ZL_WAIT_REGS(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 20);
+                    ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
+                    ++s_cnt;
+                    tc_fence_after();
+                    float sv[kTileKV];
+    #pragma unroll
+                    for (int q = 0; q < kTileKV / 32; ++q) {
                         uint32_t r[32];
-                        tmem_ld_16x64(lane_addr + slab * kSlab + col_s + h * 64, r);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            sv[0][h * 8 + k] = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
-                            sv[1][h * 8 + k] = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
-                        }
+                        tmem_ld_x32(lane_addr + col_s + q * 32, r);
+    #pragma unroll
+                        for (int i = 0; i < 32; ++i) sv[q * 32 + i] = __uint_as_float(r[i]);
                     }
                     tmem_wait_ld();
-                    if constexpr (kCodes) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const float2 f = ks[4 * k], g = vl[4 * k];
-                            sv[0][k] = fma2(sv[0][k], f, g);
-                            sv[1][k] = fma2(sv[1][k], f, g);
-                        }
+                    const uint4 m4 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                    const int valid = row_ok ? seen - j * kTileKV : kTileKV;
+                    if (__any_sync(0xffffffffu, valid < kTileKV) || (m4.x & m4.y & m4.z & m4.w) != 0xffffffffu) {
+                        const uint32_t words[4] = {m4.x & low_bits(valid), m4.y & low_bits(valid - 32), m4.z & low_bits(valid - 64), m4.w & low_bits(valid - 96)};
+    #pragma unroll
+                        for (int i = 0; i < kTileKV; ++i)
+                            if (!((words[i >> 5] >> (i & 31)) & 1)) sv[i] = -INFINITY;  // select, never multiply
                     }
-                    if (cut) {
-                        const uint32_t words[4] = {m128.x, m128.y, m128.z, m128.w};
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            const int valid = (ok >> (2 * slab + b)) & 1 ? seen[2 * slab + b] - j * kTileKV : kTileKV;
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) {  // select, never multiply
-                                const uint32_t keep = (words[k >> 2] & low_bits(valid - 32 * (k >> 2))) >> (8 * (k & 3) + 2 * quad);
-                                if (!(keep & 1)) sv[b][k].x = -INFINITY;
-                                if (!(keep & 2)) sv[b][k].y = -INFINITY;
+                    // four independent chains: a single running maximum is a 64-deep dependent chain
+                    float mx0 = max3(sv[0], sv[1], sv[2]), mx1 = max3(sv[3], sv[4], sv[5]);
+                    float mx2 = max3(sv[6], sv[7], sv[8]), mx3 = max3(sv[9], sv[10], sv[11]);
+    #pragma unroll
+                    for (int i = 12; i + 7 < kTileKV; i += 8) {
+                        mx0 = max3(mx0, sv[i], sv[i + 1]);
+                        mx1 = max3(mx1, sv[i + 2], sv[i + 3]);
+                        mx2 = max3(mx2, sv[i + 4], sv[i + 5]);
+                        mx3 = max3(mx3, sv[i + 6], sv[i + 7]);
+                    }
+                    mx0 = max3(mx0, sv[kTileKV - 4], sv[kTileKV - 3]);
+                    mx1 = max3(mx1, sv[kTileKV - 2], sv[kTileKV - 1]);
+                    const float mx = fmaxf(max3(mx0, mx1, mx2), mx3);
+                    const bool raise = row_ok && (mx - m_ref) * mul > kRescaleThresholdLog2;
+                    if (__any_sync(0xffffffffu, raise && !first)) {
+                        // rescale O (the step before this one is complete: S of this one was issued after it)
+                        const float alpha = raise ? ex2((m_ref - mx) * mul) : 1.f;
+    #pragma unroll
+                        for (int q = 0; q < D / 32; ++q) {
+                            uint32_t r[32];
+                            tmem_ld_x32(lane_addr + col_o + q * 32, r);
+                            tmem_wait_ld();
+    #pragma unroll
+                            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+                            tmem_st_x32(lane_addr + col_o + q * 32, r);
+                        }
+                        l *= alpha;
+                    }
+                    if (raise) m_ref = mx;
+                    const float nmb = m_ref == -INFINITY ? 0.f : -m_ref * mul;  // (a row that has seen no key yet)
+                    float2 sum2 = make_float2(0.f, 0.f);
+    #pragma unroll
+                    for (int h = 0; h < 2; ++h) {  // P goes to the MMA warp in two halves of 64 key columns, rounded once
+                        uint32_t pk[kTileKV / 4];
+    #pragma unroll
+                        for (int i = 0; i < kTileKV / 2; i += 4) {
+                            const int cc = h * (kTileKV / 2) + i;
+                            float2 e0 = make_float2(sv[cc], sv[cc + 1]), e1 = make_float2(sv[cc + 2], sv[cc + 3]);
+                            const float2 nm = make_float2(nmb, nmb);
+                            e0 = fma2(e0, make_float2(mul, mul), nm);
+                            e1 = fma2(e1, make_float2(mul, mul), nm);
+                            e0 = make_float2(ex2(e0.x), ex2(e0.y));
+                            e1 = make_float2(ex2(e1.x), ex2(e1.y));
+                            sum2 = add2(sum2, e0);
+                            sum2 = add2(sum2, e1);
+                            pk[i / 2] = pack_bf16(e0.x, e0.y);
+                            pk[i / 2 + 1] = pack_bf16(e1.x, e1.y);
+                        }
+                        tmem_st_x32(lane_addr + col_s + h * 32, pk);
+                        tmem_wait_st();
+                        tc_fence_before();
+                        mbar_arrive(&sm.p_half[x][h]);
+                    }
+                    l += sum2.x + sum2.y;
+                }
+                sm.stat[x][row] = make_float2(m_ref, l);
+            } else {
+                // Scores are read in the layout of an mma accumulator: a thread has 32 columns (8 k + 2 (lane % 4) + {0, 1}) of four rows
+                // (lane / 4 + 8 i of the warp's 32), and a column's scales are fetched by eight lanes for four rows each, not by every
+                // thread.
+                int32_t seen[4], seen_least = INT32_MAX;
+                uint32_t ok = 0;
+                float m4[4], l4[4];
+    #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t rt = (quarter * 32 + 8 * i + (lane >> 2)) / p.group, tk = w.tok0 + (two ? x * tile_tokens : 0) + rt;
+                    const bool there = rt < tile_tokens && tk < w.tok0 + w.tokens;
+                    ok |= there ? 1u << i : 0u;
+                    seen[i] = there ? keys_seen(w.seq(), tk) - w.tile0 * kTileKV : INT32_MAX;
+                    seen_least = min(seen_least, seen[i]);
+                    m4[i] = -INFINITY;
+                    l4[i] = 0.f;
+                }
+                seen_least = __reduce_min_sync(0xffffffffu, seen_least);
+                for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
+                    const uint32_t c = kv_cnt + j;
+                    const bool first = j == (two ? 0 : x);
+                    ZL_WAIT_REGS(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 20);
+                    ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
+                    ++s_cnt;
+                    tc_fence_after();
+                    const uint4 m128 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                    const bool cut = seen_least - j * kTileKV < kTileKV || (m128.x & m128.y & m128.z & m128.w) != 0xffffffffu;
+                    const float2* ks = reinterpret_cast<const float2*>(sm.key_scale[kCodes ? c % Smem::kScaleRing : 0]) + quad;
+                    const float2* vl = reinterpret_cast<const float2*>(sm.value_log2[kCodes ? c % Smem::kScaleRing : 0]) + quad;
+                    const float2* vi = reinterpret_cast<const float2*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0]) + quad;
+                    // Sixteen rows of the warp at a time: two rows per thread, 64 scores.  (All four at once took more registers than there
+                    // are, and a spill is an L2 access beside so much shared memory: 525 -> SLAB_US us, 1560 tokens over 9,750 int8 keys.)
+    #pragma unroll
+                    for (int slab = 0; slab < 2; ++slab) {
+                        float2 sv[2][16];  // row, pair of columns
+    #pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t r[32];
+                            tmem_ld_16x64(lane_addr + slab * kSlab + col_s + h * 64, r);
+    #pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                sv[0][h * 8 + k] = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
+                                sv[1][h * 8 + k] = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
                             }
                         }
-                    }
-                    float mx[2];
-                    bool raise = false;
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        float u = max3(sv[b][0].x, sv[b][0].y, sv[b][1].x), v = max3(sv[b][1].y, sv[b][2].x, sv[b][2].y);
-#pragma unroll
-                        for (int k = 3; k < 15; k += 2) {
-                            u = max3(u, sv[b][k].x, sv[b][k].y);
-                            v = max3(v, sv[b][k + 1].x, sv[b][k + 1].y);
-                        }
-                        mx[b] = fmaxf(max3(u, sv[b][15].x, sv[b][15].y), v);
-                        raise |= ((ok >> (2 * slab + b)) & 1) && (mx[b] - m4[2 * slab + b]) * mul > kRescaleThresholdLog2;
-                    }
-                    if (__any_sync(0xffffffffu, raise)) {
-                        // all lanes of a row take its maximum as the new reference; O is rescaled (the step before this one is complete:
-                        // S of this one was issued after it)
-                        float alpha[2];
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            const int i = 2 * slab + b;
-                            mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
-                            mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
-                            alpha[b] = 1.f;
-                            if (((ok >> i) & 1) && mx[b] > m4[i]) {
-                                alpha[b] = ex2((m4[i] - mx[b]) * mul);
-                                m4[i] = mx[b];
-                                l4[i] *= alpha[b];
+                        tmem_wait_ld();
+                        if constexpr (kCodes) {
+    #pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                const float2 f = ks[4 * k], g = vl[4 * k];
+                                sv[0][k] = fma2(sv[0][k], f, g);
+                                sv[1][k] = fma2(sv[1][k], f, g);
                             }
                         }
-                        if (!first) {
-#pragma unroll 1
-                            for (int h = 0; h < D / 64; ++h) {
-                                const uint32_t at = lane_addr + slab * kSlab + col_o + h * 64;
-                                uint32_t r[32];
-                                tmem_ld_16x64(at, r);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha[(k >> 1) & 1]);
-                                tmem_st_16x64(at, r);
-                            }
-                        }
-                    }
-                    float2 nm[2], sum[2];
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const float ref = m4[2 * slab + b], nmb = ref == -INFINITY ? 0.f : -ref * mul;  // (a row that has seen no key yet)
-                        nm[b] = make_float2(nmb, nmb);
-                        sum[b] = make_float2(0.f, 0.f);
-                    }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {  // P, rounded once
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float2 f = kCodes ? vi[4 * (8 * h + k)] : make_float2(1.f, 1.f);
-#pragma unroll
+                        if (cut) {
+                            const uint32_t words[4] = {m128.x, m128.y, m128.z, m128.w};
+    #pragma unroll
                             for (int b = 0; b < 2; ++b) {
-                                float2 e = sv[b][8 * h + k];
-                                if constexpr (kCodes) e = add2(e, nm[b]); else e = fma2(e, make_float2(mul, mul), nm[b]);
-                                e = make_float2(ex2(e.x), ex2(e.y));
-                                if constexpr (kCodes) {
-                                    sum[b] = fma2(e, f, sum[b]);
-                                    pk[2 * k + b] = pack_half(e.x, e.y);
-                                } else {
-                                    sum[b] = add2(sum[b], e);
-                                    pk[2 * k + b] = pack_bf16(e.x, e.y);
+                                const int valid = (ok >> (2 * slab + b)) & 1 ? seen[2 * slab + b] - j * kTileKV : kTileKV;
+    #pragma unroll
+                                for (int k = 0; k < 16; ++k) {  // select, never multiply
+                                    const uint32_t keep = (words[k >> 2] & low_bits(valid - 32 * (k >> 2))) >> (8 * (k & 3) + 2 * quad);
+                                    if (!(keep & 1)) sv[b][k].x = -INFINITY;
+                                    if (!(keep & 2)) sv[b][k].y = -INFINITY;
                                 }
                             }
                         }
-                        tmem_st_16x32(lane_addr + slab * kSlab + col_s + h * 32, pk);
-                        if (slab == 1) {  // to the MMA warp in two halves of 64 key columns
-                            tmem_wait_st();
-                            tc_fence_before();
-                            mbar_arrive(&sm.p_half[x][h]);
+                        float mx[2];
+                        bool raise = false;
+    #pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            float u = max3(sv[b][0].x, sv[b][0].y, sv[b][1].x), v = max3(sv[b][1].y, sv[b][2].x, sv[b][2].y);
+    #pragma unroll
+                            for (int k = 3; k < 15; k += 2) {
+                                u = max3(u, sv[b][k].x, sv[b][k].y);
+                                v = max3(v, sv[b][k + 1].x, sv[b][k + 1].y);
+                            }
+                            mx[b] = fmaxf(max3(u, sv[b][15].x, sv[b][15].y), v);
+                            raise |= ((ok >> (2 * slab + b)) & 1) && (mx[b] - m4[2 * slab + b]) * mul > kRescaleThresholdLog2;
                         }
+                        if (__any_sync(0xffffffffu, raise)) {
+                            // all lanes of a row take its maximum as the new reference; O is rescaled (the step before this one is complete:
+                            // S of this one was issued after it)
+                            float alpha[2];
+    #pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                const int i = 2 * slab + b;
+                                mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
+                                mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
+                                alpha[b] = 1.f;
+                                if (((ok >> i) & 1) && mx[b] > m4[i]) {
+                                    alpha[b] = ex2((m4[i] - mx[b]) * mul);
+                                    m4[i] = mx[b];
+                                    l4[i] *= alpha[b];
+                                }
+                            }
+                            if (!first) {
+    #pragma unroll 1
+                                for (int h = 0; h < D / 64; ++h) {
+                                    const uint32_t at = lane_addr + slab * kSlab + col_o + h * 64;
+                                    uint32_t r[32];
+                                    tmem_ld_16x64(at, r);
+                                    tmem_wait_ld();
+    #pragma unroll
+                                    for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha[(k >> 1) & 1]);
+                                    tmem_st_16x64(at, r);
+                                }
+                            }
+                        }
+                        float2 nm[2], sum[2];
+    #pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const float ref = m4[2 * slab + b], nmb = ref == -INFINITY ? 0.f : -ref * mul;  // (a row that has seen no key yet)
+                            nm[b] = make_float2(nmb, nmb);
+                            sum[b] = make_float2(0.f, 0.f);
+                        }
+    #pragma unroll
+                        for (int h = 0; h < 2; ++h) {  // P, rounded once
+                            uint32_t pk[16];
+    #pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const float2 f = kCodes ? vi[4 * (8 * h + k)] : make_float2(1.f, 1.f);
+    #pragma unroll
+                                for (int b = 0; b < 2; ++b) {
+                                    float2 e = sv[b][8 * h + k];
+                                    if constexpr (kCodes) e = add2(e, nm[b]); else e = fma2(e, make_float2(mul, mul), nm[b]);
+                                    e = make_float2(ex2(e.x), ex2(e.y));
+                                    if constexpr (kCodes) {
+                                        sum[b] = fma2(e, f, sum[b]);
+                                        pk[2 * k + b] = pack_half(e.x, e.y);
+                                    } else {
+                                        sum[b] = add2(sum[b], e);
+                                        pk[2 * k + b] = pack_bf16(e.x, e.y);
+                                    }
+                                }
+                            }
+                            tmem_st_16x32(lane_addr + slab * kSlab + col_s + h * 32, pk);
+                            if (slab == 1) {  // to the MMA warp in two halves of 64 key columns
+                                tmem_wait_st();
+                                tc_fence_before();
+                                mbar_arrive(&sm.p_half[x][h]);
+                            }
+                        }
+    #pragma unroll
+                        for (int b = 0; b < 2; ++b) l4[2 * slab + b] += sum[b].x + sum[b].y;
                     }
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) l4[2 * slab + b] += sum[b].x + sum[b].y;
                 }
-            }
-            // a row per thread from here on
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 1);
-                l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 2);
-                if (quad == 0) sm.stat[x][quarter * 32 + 8 * i + (lane >> 2)] = make_float2(m4[i], l4[i]);
-            }
-            __syncwarp();
-            m_ref = sm.stat[x][row].x;
-            l = sm.stat[x][row].y;
+                // a row per thread from here on
+    #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 1);
+                    l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 2);
+                    if (quad == 0) sm.stat[x][quarter * 32 + 8 * i + (lane >> 2)] = make_float2(m4[i], l4[i]);
+                }
+                __syncwarp();
+                m_ref = sm.stat[x][row].x;
+                l = sm.stat[x][row].y;
             }
             // ---- the item's end: weights of the accumulators for this row, and the columns this warpgroup writes
             float wt[2] = {two && x == 1 ? 0.f : 1.f, two && x == 1 ? 1.f : 0.f};
