@@ -11,9 +11,11 @@
 //   warps 4-11   softmax, a thread per row; with two query tiles warpgroup x takes tile x, with one tile it takes key tiles x,
 //                x + 2, ... and both accumulators are joined at the end
 //   warps 12-15  (8-bit caches) codes become fp16, exactly, in their place (a tile of codes arrives in the second half of the tile it
-//                becomes), and so do the queries of an item; the scale of a key multiplies its column of S, the scale of a value its column of P, in
-//                fp32: the softmax takes s_j = S_j k_j + log2 v_j, so that its exponentials are the weights of the values, and sums
-//                weight / v_j beside them
+//                becomes), and so do the queries of an item; the scale of a key multiplies its column of S, the scale of a value its
+//                column of P, in fp32: the softmax takes s_j = S_j k_j + log2 v_j, so that its exponentials are the weights of the
+//                values, and sums weight / v_j beside them.  (Values times their scale in fp16 would spare two of the three scales,
+//                but lose the small ones beside a large one, and the two multiplications more kept these warps busy: 420 -> 572
+//                us, 1560 tokens over 9,750 int8 keys.)
 // An item that lies in several CTAs leaves its parts in the workspace, and a second launch joins them, in the order of the CTAs: a
 // part is 133 KB, and one CTA alone took 20 us to join the six parts of 256 rows over 8,700 keys.
 #include "zl_cache.cuh"
@@ -65,7 +67,7 @@ struct ChunkSmem {
     alignas(16) float value_log2[kCodes ? kScaleRing : 1][kTileKV], value_inv[kCodes ? kScaleRing : 1][kTileKV];  // log2 and inverse of its scale
     alignas(16) uint32_t mask[kMaskRing][4];            // keys of a tile that exist
     Item items[kItems];
-    float2 stat[2][kTileQ];                             // per warpgroup and row: reference maximum (raw scores), sum
+    float2 stat[2][kTileQ];                             // per warpgroup and row: reference maximum (powers of two), sum
     float q_big[4];  // per converting warp: largest magnitude of its queries
     alignas(8) uint64_t q_full, q_empty, q_max, q_ready;
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
@@ -326,7 +328,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     if (idle) {
         if (threadIdx.x == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;
     } else if (warp < 4) {
-        if constexpr (kCodes) reg_dec<88>(); else reg_dec<72>();
+        if constexpr (kCodes) reg_dec<88>(); else reg_dec<136>();
         if (warp == 2) {
             // -------------------------------------------------------------- the line of work
             ItemWalk walk(p, sm.start_seq, sm.start_base, per, total);
@@ -684,7 +686,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
     } else {
         // ------------------------------------------------------------------ softmax, join and output
-        if constexpr (kCodes) reg_inc<168>(); else reg_inc<216>();
+        if constexpr (kCodes) reg_inc<168>(); else reg_inc<184>();
         const int x = (warp - 4) >> 2;
         const int quarter = warp & 3;              // TMEM lane quarter this warp may access
         const int row = quarter * 32 + lane;       // of the output
@@ -692,7 +694,6 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
         constexpr uint32_t kSlab = 16u << 16;      // 16 lanes further on
         const uint32_t col_s = kColS + x * 128, col_o = kColO + x * 128;
-        const float mul = kCodes ? 1.f : p.scale_log2;  // of 8-bit caches the keys' scales have it
         const int32_t tile_tokens = kTileQ / p.group;
         const int32_t row_tok = row / p.group, row_head = row - row_tok * p.group;
         uint32_t kv_cnt = 0, s_cnt = 0, o_cnt[2] = {0, 0}, join_cnt = 0;
@@ -701,247 +702,161 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int32_t tok = w.tok0 + (two ? x * tile_tokens : 0) + row_tok;  // of the sequence
             const bool row_ok = row_tok < tile_tokens && tok < w.tok0 + w.tokens;
             // (rows that do not exist hold anything, and take no part in what a warp decides together)
-            float m_ref = -INFINITY, l = 0.f;
-            if constexpr (!kCodes) {
-                const int32_t seen = row_ok ? keys_seen(w.seq(), tok) - w.tile0 * kTileKV : INT32_MAX;
-                for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
-                    const uint32_t c = kv_cnt + j;
-                    const bool first = j == (two ? 0 : x);
-                    ZL_WAIT_REGS(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 20);
-                    ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
-                    ++s_cnt;
-                    tc_fence_after();
-                    float sv[kTileKV];
-    #pragma unroll
-                    for (int q = 0; q < kTileKV / 32; ++q) {
+            int32_t seen[4], seen_least = INT32_MAX;
+            uint32_t ok = 0;
+            float m4[4], l4[4];  // reference maximum in powers of two, sum
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t rt = (quarter * 32 + 8 * i + (lane >> 2)) / p.group, tk = w.tok0 + (two ? x * tile_tokens : 0) + rt;
+                const bool there = rt < tile_tokens && tk < w.tok0 + w.tokens;
+                ok |= there ? 1u << i : 0u;
+                seen[i] = there ? keys_seen(w.seq(), tk) - w.tile0 * kTileKV : INT32_MAX;
+                seen_least = min(seen_least, seen[i]);
+                m4[i] = -INFINITY;
+                l4[i] = 0.f;
+            }
+            seen_least = __reduce_min_sync(0xffffffffu, seen_least);
+            const float mul = kCodes ? 1.f : p.scale_log2;  // (of 8-bit caches the keys' scales have it)
+            for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
+                const uint32_t c = kv_cnt + j;
+                const bool first = j == (two ? 0 : x);
+                ZL_WAIT_REGS(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 20);
+                ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
+                ++s_cnt;
+                tc_fence_after();
+                const uint4 m128 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                const bool cut = seen_least - j * kTileKV < kTileKV || (m128.x & m128.y & m128.z & m128.w) != 0xffffffffu;
+                const float2* vi = reinterpret_cast<const float2*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0]) + quad;
+                // Sixteen rows of the warp at a time, in the layout of an mma accumulator: a thread has 32 columns of two rows.  (With all 128
+                // columns of its row a thread needs more registers than there are beside the converting warps; a spill is an L2 access
+                // here.  For bf16, where they nearly fit, both ways take the same time.)
+#pragma unroll
+                for (int slab = 0; slab < 2; ++slab) {
+                    float2 sv[2][16];  // row, pair of columns
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
                         uint32_t r[32];
-                        tmem_ld_x32(lane_addr + col_s + q * 32, r);
-    #pragma unroll
-                        for (int i = 0; i < 32; ++i) sv[q * 32 + i] = __uint_as_float(r[i]);
+                        tmem_ld_16x64(lane_addr + slab * kSlab + col_s + h * 64, r);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            sv[0][h * 8 + k] = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
+                            sv[1][h * 8 + k] = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
+                        }
+                    }
+                    float2 by_key[kCodes ? 16 : 1], by_value[kCodes ? 16 : 1];
+                    if constexpr (kCodes) {  // (fetched under the load of S; eight lanes share a column's)
+                        const float2* ks = reinterpret_cast<const float2*>(sm.key_scale[c % Smem::kScaleRing]) + quad;
+                        const float2* vl = reinterpret_cast<const float2*>(sm.value_log2[c % Smem::kScaleRing]) + quad;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            by_key[k] = ks[4 * k];
+                            by_value[k] = vl[4 * k];
+                        }
                     }
                     tmem_wait_ld();
-                    const uint4 m4 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
-                    const int valid = row_ok ? seen - j * kTileKV : kTileKV;
-                    if (__any_sync(0xffffffffu, valid < kTileKV) || (m4.x & m4.y & m4.z & m4.w) != 0xffffffffu) {
-                        const uint32_t words[4] = {m4.x & low_bits(valid), m4.y & low_bits(valid - 32), m4.z & low_bits(valid - 64), m4.w & low_bits(valid - 96)};
-    #pragma unroll
-                        for (int i = 0; i < kTileKV; ++i)
-                            if (!((words[i >> 5] >> (i & 31)) & 1)) sv[i] = -INFINITY;  // select, never multiply
+                    if constexpr (kCodes) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            sv[0][k] = fma2(sv[0][k], by_key[k], by_value[k]);
+                            sv[1][k] = fma2(sv[1][k], by_key[k], by_value[k]);
+                        }
                     }
-                    // four independent chains: a single running maximum is a 64-deep dependent chain
-                    float mx0 = max3(sv[0], sv[1], sv[2]), mx1 = max3(sv[3], sv[4], sv[5]);
-                    float mx2 = max3(sv[6], sv[7], sv[8]), mx3 = max3(sv[9], sv[10], sv[11]);
-    #pragma unroll
-                    for (int i = 12; i + 7 < kTileKV; i += 8) {
-                        mx0 = max3(mx0, sv[i], sv[i + 1]);
-                        mx1 = max3(mx1, sv[i + 2], sv[i + 3]);
-                        mx2 = max3(mx2, sv[i + 4], sv[i + 5]);
-                        mx3 = max3(mx3, sv[i + 6], sv[i + 7]);
-                    }
-                    mx0 = max3(mx0, sv[kTileKV - 4], sv[kTileKV - 3]);
-                    mx1 = max3(mx1, sv[kTileKV - 2], sv[kTileKV - 1]);
-                    const float mx = fmaxf(max3(mx0, mx1, mx2), mx3);
-                    const bool raise = row_ok && (mx - m_ref) * mul > kRescaleThresholdLog2;
-                    if (__any_sync(0xffffffffu, raise && !first)) {
-                        // rescale O (the step before this one is complete: S of this one was issued after it)
-                        const float alpha = raise ? ex2((m_ref - mx) * mul) : 1.f;
-    #pragma unroll
-                        for (int q = 0; q < D / 32; ++q) {
-                            uint32_t r[32];
-                            tmem_ld_x32(lane_addr + col_o + q * 32, r);
-                            tmem_wait_ld();
-    #pragma unroll
-                            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-                            tmem_st_x32(lane_addr + col_o + q * 32, r);
-                        }
-                        l *= alpha;
-                    }
-                    if (raise) m_ref = mx;
-                    const float nmb = m_ref == -INFINITY ? 0.f : -m_ref * mul;  // (a row that has seen no key yet)
-                    float2 sum2 = make_float2(0.f, 0.f);
-    #pragma unroll
-                    for (int h = 0; h < 2; ++h) {  // P goes to the MMA warp in two halves of 64 key columns, rounded once
-                        uint32_t pk[kTileKV / 4];
-    #pragma unroll
-                        for (int i = 0; i < kTileKV / 2; i += 4) {
-                            const int cc = h * (kTileKV / 2) + i;
-                            float2 e0 = make_float2(sv[cc], sv[cc + 1]), e1 = make_float2(sv[cc + 2], sv[cc + 3]);
-                            const float2 nm = make_float2(nmb, nmb);
-                            e0 = fma2(e0, make_float2(mul, mul), nm);
-                            e1 = fma2(e1, make_float2(mul, mul), nm);
-                            e0 = make_float2(ex2(e0.x), ex2(e0.y));
-                            e1 = make_float2(ex2(e1.x), ex2(e1.y));
-                            sum2 = add2(sum2, e0);
-                            sum2 = add2(sum2, e1);
-                            pk[i / 2] = pack_bf16(e0.x, e0.y);
-                            pk[i / 2 + 1] = pack_bf16(e1.x, e1.y);
-                        }
-                        tmem_st_x32(lane_addr + col_s + h * 32, pk);
-                        tmem_wait_st();
-                        tc_fence_before();
-                        mbar_arrive(&sm.p_half[x][h]);
-                    }
-                    l += sum2.x + sum2.y;
-                }
-                sm.stat[x][row] = make_float2(m_ref, l);
-            } else {
-                // Scores are read in the layout of an mma accumulator: a thread has 32 columns (8 k + 2 (lane % 4) + {0, 1}) of four rows
-                // (lane / 4 + 8 i of the warp's 32), and a column's scales are fetched by eight lanes for four rows each, not by every
-                // thread.
-                int32_t seen[4], seen_least = INT32_MAX;
-                uint32_t ok = 0;
-                float m4[4], l4[4];
-    #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int32_t rt = (quarter * 32 + 8 * i + (lane >> 2)) / p.group, tk = w.tok0 + (two ? x * tile_tokens : 0) + rt;
-                    const bool there = rt < tile_tokens && tk < w.tok0 + w.tokens;
-                    ok |= there ? 1u << i : 0u;
-                    seen[i] = there ? keys_seen(w.seq(), tk) - w.tile0 * kTileKV : INT32_MAX;
-                    seen_least = min(seen_least, seen[i]);
-                    m4[i] = -INFINITY;
-                    l4[i] = 0.f;
-                }
-                seen_least = __reduce_min_sync(0xffffffffu, seen_least);
-                for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
-                    const uint32_t c = kv_cnt + j;
-                    const bool first = j == (two ? 0 : x);
-                    ZL_WAIT_REGS(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 20);
-                    ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
-                    ++s_cnt;
-                    tc_fence_after();
-                    const uint4 m128 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
-                    const bool cut = seen_least - j * kTileKV < kTileKV || (m128.x & m128.y & m128.z & m128.w) != 0xffffffffu;
-                    const float2* ks = reinterpret_cast<const float2*>(sm.key_scale[kCodes ? c % Smem::kScaleRing : 0]) + quad;
-                    const float2* vl = reinterpret_cast<const float2*>(sm.value_log2[kCodes ? c % Smem::kScaleRing : 0]) + quad;
-                    const float2* vi = reinterpret_cast<const float2*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0]) + quad;
-                    // Sixteen rows of the warp at a time: two rows per thread, 64 scores.  (All four at once took more registers than there
-                    // are, and a spill is an L2 access beside so much shared memory: 525 -> SLAB_US us, 1560 tokens over 9,750 int8 keys.)
-    #pragma unroll
-                    for (int slab = 0; slab < 2; ++slab) {
-                        float2 sv[2][16];  // row, pair of columns
-    #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t r[32];
-                            tmem_ld_16x64(lane_addr + slab * kSlab + col_s + h * 64, r);
-    #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                sv[0][h * 8 + k] = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
-                                sv[1][h * 8 + k] = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
-                            }
-                        }
-                        tmem_wait_ld();
-                        if constexpr (kCodes) {
-    #pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                const float2 f = ks[4 * k], g = vl[4 * k];
-                                sv[0][k] = fma2(sv[0][k], f, g);
-                                sv[1][k] = fma2(sv[1][k], f, g);
-                            }
-                        }
-                        if (cut) {
-                            const uint32_t words[4] = {m128.x, m128.y, m128.z, m128.w};
-    #pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                const int valid = (ok >> (2 * slab + b)) & 1 ? seen[2 * slab + b] - j * kTileKV : kTileKV;
-    #pragma unroll
-                                for (int k = 0; k < 16; ++k) {  // select, never multiply
-                                    const uint32_t keep = (words[k >> 2] & low_bits(valid - 32 * (k >> 2))) >> (8 * (k & 3) + 2 * quad);
-                                    if (!(keep & 1)) sv[b][k].x = -INFINITY;
-                                    if (!(keep & 2)) sv[b][k].y = -INFINITY;
-                                }
-                            }
-                        }
-                        float mx[2];
-                        bool raise = false;
-    #pragma unroll
+                    if (cut) {
+                        const uint32_t words[4] = {m128.x, m128.y, m128.z, m128.w};
+#pragma unroll
                         for (int b = 0; b < 2; ++b) {
-                            float u = max3(sv[b][0].x, sv[b][0].y, sv[b][1].x), v = max3(sv[b][1].y, sv[b][2].x, sv[b][2].y);
-    #pragma unroll
-                            for (int k = 3; k < 15; k += 2) {
-                                u = max3(u, sv[b][k].x, sv[b][k].y);
-                                v = max3(v, sv[b][k + 1].x, sv[b][k + 1].y);
-                            }
-                            mx[b] = fmaxf(max3(u, sv[b][15].x, sv[b][15].y), v);
-                            raise |= ((ok >> (2 * slab + b)) & 1) && (mx[b] - m4[2 * slab + b]) * mul > kRescaleThresholdLog2;
-                        }
-                        if (__any_sync(0xffffffffu, raise)) {
-                            // all lanes of a row take its maximum as the new reference; O is rescaled (the step before this one is complete:
-                            // S of this one was issued after it)
-                            float alpha[2];
-    #pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                const int i = 2 * slab + b;
-                                mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
-                                mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
-                                alpha[b] = 1.f;
-                                if (((ok >> i) & 1) && mx[b] > m4[i]) {
-                                    alpha[b] = ex2((m4[i] - mx[b]) * mul);
-                                    m4[i] = mx[b];
-                                    l4[i] *= alpha[b];
-                                }
-                            }
-                            if (!first) {
-    #pragma unroll 1
-                                for (int h = 0; h < D / 64; ++h) {
-                                    const uint32_t at = lane_addr + slab * kSlab + col_o + h * 64;
-                                    uint32_t r[32];
-                                    tmem_ld_16x64(at, r);
-                                    tmem_wait_ld();
-    #pragma unroll
-                                    for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha[(k >> 1) & 1]);
-                                    tmem_st_16x64(at, r);
-                                }
+                            const int valid = (ok >> (2 * slab + b)) & 1 ? seen[2 * slab + b] - j * kTileKV : kTileKV;
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {  // select, never multiply
+                                const uint32_t keep = (words[k >> 2] & low_bits(valid - 32 * (k >> 2))) >> (8 * (k & 3) + 2 * quad);
+                                if (!(keep & 1)) sv[b][k].x = -INFINITY;
+                                if (!(keep & 2)) sv[b][k].y = -INFINITY;
                             }
                         }
-                        float2 nm[2], sum[2];
-    #pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            const float ref = m4[2 * slab + b], nmb = ref == -INFINITY ? 0.f : -ref * mul;  // (a row that has seen no key yet)
-                            nm[b] = make_float2(nmb, nmb);
-                            sum[b] = make_float2(0.f, 0.f);
-                        }
-    #pragma unroll
-                        for (int h = 0; h < 2; ++h) {  // P, rounded once
-                            uint32_t pk[16];
-    #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                const float2 f = kCodes ? vi[4 * (8 * h + k)] : make_float2(1.f, 1.f);
-    #pragma unroll
-                                for (int b = 0; b < 2; ++b) {
-                                    float2 e = sv[b][8 * h + k];
-                                    if constexpr (kCodes) e = add2(e, nm[b]); else e = fma2(e, make_float2(mul, mul), nm[b]);
-                                    e = make_float2(ex2(e.x), ex2(e.y));
-                                    if constexpr (kCodes) {
-                                        sum[b] = fma2(e, f, sum[b]);
-                                        pk[2 * k + b] = pack_half(e.x, e.y);
-                                    } else {
-                                        sum[b] = add2(sum[b], e);
-                                        pk[2 * k + b] = pack_bf16(e.x, e.y);
-                                    }
-                                }
-                            }
-                            tmem_st_16x32(lane_addr + slab * kSlab + col_s + h * 32, pk);
-                            if (slab == 1) {  // to the MMA warp in two halves of 64 key columns
-                                tmem_wait_st();
-                                tc_fence_before();
-                                mbar_arrive(&sm.p_half[x][h]);
-                            }
-                        }
-    #pragma unroll
-                        for (int b = 0; b < 2; ++b) l4[2 * slab + b] += sum[b].x + sum[b].y;
                     }
+                    float mx[2];
+                    bool raise = false;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        float u = max3(sv[b][0].x, sv[b][0].y, sv[b][1].x), v = max3(sv[b][1].y, sv[b][2].x, sv[b][2].y);
+#pragma unroll
+                        for (int k = 3; k < 15; k += 2) {
+                            u = max3(u, sv[b][k].x, sv[b][k].y);
+                            v = max3(v, sv[b][k + 1].x, sv[b][k + 1].y);
+                        }
+                        mx[b] = fmaxf(max3(u, sv[b][15].x, sv[b][15].y), v) * mul;
+                        raise |= ((ok >> (2 * slab + b)) & 1) && mx[b] - m4[2 * slab + b] > kRescaleThresholdLog2;
+                    }
+                    if (__any_sync(0xffffffffu, raise)) {
+                        // all lanes of a row take its maximum as the new reference; O is rescaled (the step before this one is complete:
+                        // S of this one was issued after it)
+                        float alpha[2];
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            const int i = 2 * slab + b;
+                            mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
+                            mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
+                            alpha[b] = 1.f;
+                            if (((ok >> i) & 1) && mx[b] > m4[i]) {
+                                alpha[b] = ex2(m4[i] - mx[b]);
+                                l4[i] *= alpha[b];
+                                m4[i] = mx[b];
+                            }
+                        }
+                        if (!first) {
+#pragma unroll 1
+                            for (int h = 0; h < D / 64; ++h) {
+                                const uint32_t at = lane_addr + slab * kSlab + col_o + h * 64;
+                                uint32_t r[32];
+                                tmem_ld_16x64(at, r);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha[(k >> 1) & 1]);
+                                tmem_st_16x64(at, r);
+                            }
+                        }
+                    }
+                    float2 nm[2], sum[2];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const float ref = m4[2 * slab + b], nmb = ref == -INFINITY ? 0.f : -ref;  // (a row may have seen no key yet)
+                        nm[b] = make_float2(nmb, nmb);
+                        sum[b] = make_float2(0.f, 0.f);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {  // P, rounded once
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float2 f = kCodes ? vi[4 * (8 * h + k)] : make_float2(1.f, 1.f);
+#pragma unroll
+                            for (int b = 0; b < 2; ++b) {
+                                float2 e = kCodes ? add2(sv[b][8 * h + k], nm[b]) : fma2(sv[b][8 * h + k], make_float2(mul, mul), nm[b]);
+                                e = make_float2(ex2(e.x), ex2(e.y));
+                                sum[b] = kCodes ? fma2(e, f, sum[b]) : add2(sum[b], e);
+                                pk[2 * k + b] = kCodes ? pack_half(e.x, e.y) : pack_bf16(e.x, e.y);
+                            }
+                        }
+                        tmem_st_16x32(lane_addr + slab * kSlab + col_s + h * 32, pk);
+                        if (slab == 1) {  // to the MMA warp in two halves of 64 key columns
+                            tmem_wait_st();
+                            tc_fence_before();
+                            mbar_arrive(&sm.p_half[x][h]);
+                        }
+                    }
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) l4[2 * slab + b] += sum[b].x + sum[b].y;
                 }
-                // a row per thread from here on
-    #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 1);
-                    l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 2);
-                    if (quad == 0) sm.stat[x][quarter * 32 + 8 * i + (lane >> 2)] = make_float2(m4[i], l4[i]);
-                }
-                __syncwarp();
-                m_ref = sm.stat[x][row].x;
-                l = sm.stat[x][row].y;
             }
+            // a row per thread from here on
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 1);
+                l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 2);
+                if (quad == 0) sm.stat[x][quarter * 32 + 8 * i + (lane >> 2)] = make_float2(m4[i], l4[i]);
+            }
+            __syncwarp();
+            float m_ref = sm.stat[x][row].x, l = sm.stat[x][row].y;
             // ---- the item's end: weights of the accumulators for this row, and the columns this warpgroup writes
             float wt[2] = {two && x == 1 ? 0.f : 1.f, two && x == 1 ? 1.f : 0.f};
             if (n > 0) {
@@ -959,8 +874,8 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     ZL_WAIT_REGS(&sm.stat_full, join_cnt & 1, 24);
                     const float2 a = sm.stat[0][row], b = sm.stat[1][row];
                     m_ref = fmaxf(a.x, b.x);
-                    wt[0] = m_ref == -INFINITY ? 0.f : ex2((a.x - m_ref) * mul);
-                    wt[1] = m_ref == -INFINITY ? 0.f : ex2((b.x - m_ref) * mul);
+                    wt[0] = m_ref == -INFINITY ? 0.f : ex2(a.x - m_ref);
+                    wt[1] = m_ref == -INFINITY ? 0.f : ex2(b.x - m_ref);
                     l = wt[0] * a.y + wt[1] * b.y;
                 }
             }
@@ -1008,10 +923,10 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             }
             if (has_lse) {
                 if (whole) {
-                    if (p.lse) p.lse[(int64_t)q_head * p.b.total_q + grow] = l > 0.f ? (m_ref * mul + log2f(l)) * kLn2 : -INFINITY;
+                    if (p.lse) p.lse[(int64_t)q_head * p.b.total_q + grow] = l > 0.f ? (m_ref + log2f(l)) * kLn2 : -INFINITY;
                 } else {
                     float* to = part_of(blockIdx.x);
-                    to[row] = m_ref * mul;
+                    to[row] = m_ref;
                     to[kTileQ + row] = l;
                 }
             }
