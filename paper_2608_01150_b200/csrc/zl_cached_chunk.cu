@@ -8,8 +8,10 @@
 //   warp 0       TMA producer: Q once per item, K and V page by page through shared-memory rings
 //   warp 2       walks the line and hands the items' descriptions to the others
 //   warp 1       MMA issuer: S_x = Q K^T, O_x += P_x V (P read from TMEM), one step two ahead of the other
-//   warps 4-11   softmax, a thread per row; with two query tiles warpgroup x takes tile x, with one tile it takes key tiles x,
-//                x + 2, ... and both accumulators are joined at the end
+//   warps 4-11   softmax.  All of them work on the same scores, sixteen rows a warp, in turn on S_0 and S_1: those are two query tiles
+//                against a key tile, or one query tile against two key tiles, whose accumulators are joined at the end.  While the
+//                warps are at one, the tensor core has the other's P V and next S before it: a warpgroup with a tile of its own
+//                stood still for those (1560 tokens over 9,750 keys: bf16 306 -> SHARE_B us, int8 421 -> SHARE_I us)
 //   warps 12-15  (8-bit caches) codes become fp16, exactly, in their place (a tile of codes arrives in the second half of the tile it
 //                becomes), and so do the queries of an item; the scale of a key multiplies its column of S, the scale of a value its
 //                column of P, in fp32: the softmax takes s_j = S_j k_j + log2 v_j, so that its exponentials are the weights of the
@@ -18,6 +20,8 @@
 //                us, 1560 tokens over 9,750 int8 keys.)
 // An item that lies in several CTAs leaves its parts in the workspace, and a second launch joins them, in the order of the CTAs: a
 // part is 133 KB, and one CTA alone took 20 us to join the six parts of 256 rows over 8,700 keys.
+#include <type_traits>
+
 #include "zl_cache.cuh"
 
 namespace zl {
@@ -73,7 +77,7 @@ struct ChunkSmem {
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
     uint64_t k_codes[kCodes ? kStages : 1], v_codes[kCodes ? kStages : 1], codes_read;
     uint64_t s_full[2], p_half[2][2], o_full[2], tile_full[kMaskRing];
-    uint64_t stat_full, join_done, item_full[kItems], item_empty[kItems];
+    uint64_t stat_full, item_full[kItems], item_empty[kItems];
     int64_t scan[16], start_base, total;
     int32_t start_seq;
     uint32_t tmem_base;
@@ -242,8 +246,8 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         mbar_init(&sm.q_ready, 128);
         for (int x = 0; x < 2; ++x) {
             mbar_init(&sm.s_full[x], 1);
-            mbar_init(&sm.p_half[x][0], 128);
-            mbar_init(&sm.p_half[x][1], 128);
+            mbar_init(&sm.p_half[x][0], 256);
+            mbar_init(&sm.p_half[x][1], 256);
             mbar_init(&sm.o_full[x], 1);
         }
         for (int s = 0; s < kStages; ++s) {
@@ -261,7 +265,6 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
         for (int s = 0; s < kMaskRing; ++s) mbar_init(&sm.tile_full[s], kCodes ? 128 : 1);
         mbar_init(&sm.stat_full, 256);
-        mbar_init(&sm.join_done, 256);
         for (int i = 0; i < kItems; ++i) {
             mbar_init(&sm.item_full[i], 1);
             mbar_init(&sm.item_empty[i], kCodes ? 14 : 10);  // warps that read it
@@ -687,196 +690,208 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     } else {
         // ------------------------------------------------------------------ softmax, join and output
         if constexpr (kCodes) reg_inc<168>(); else reg_inc<184>();
-        const int x = (warp - 4) >> 2;
+        const int x = (warp - 4) >> 2;             // half of the rows of a warp's TMEM quarter; tile or columns of the output
         const int quarter = warp & 3;              // TMEM lane quarter this warp may access
         const int row = quarter * 32 + lane;       // of the output
         const int quad = lane & 3;
-        const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
-        constexpr uint32_t kSlab = 16u << 16;      // 16 lanes further on
-        const uint32_t col_s = kColS + x * 128, col_o = kColO + x * 128;
+        const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16), slab_addr = lane_addr + ((uint32_t)(x * 16) << 16);
+        const float mul = kCodes ? 1.f : p.scale_log2;  // (of 8-bit caches the keys' scales have it)
         const int32_t tile_tokens = kTileQ / p.group;
         const int32_t row_tok = row / p.group, row_head = row - row_tok * p.group;
-        uint32_t kv_cnt = 0, s_cnt = 0, o_cnt[2] = {0, 0}, join_cnt = 0;
+        const int32_t slab_row = quarter * 32 + x * 16 + (lane >> 2);  // this thread's rows of S: slab_row, slab_row + 8
+        const int32_t slab_tok[2] = {slab_row / p.group, (slab_row + 8) / p.group};
+        uint32_t kv_cnt = 0, s_ph[2] = {0, 0}, o_cnt[2] = {0, 0}, join_cnt = 0;
         ZL_FOR_ITEMS(ZL_WAIT_REGS, 28)
             const bool two = w.two != 0;
+            // (rows that do not exist hold anything, and take no part in what a warp decides together)
+            int32_t seen[2][2], seen_least[2];
+            bool ok[2][2];
+            float m2[2][2], l2[2][2];  // of S_0 and S_1: reference maximum in powers of two, sum
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int32_t tk = w.tok0 + (two ? y * tile_tokens : 0) + slab_tok[b];
+                    ok[y][b] = slab_tok[b] < tile_tokens && tk < w.tok0 + w.tokens;
+                    seen[y][b] = ok[y][b] ? keys_seen(w.seq(), tk) - w.tile0 * kTileKV : INT32_MAX;
+                    m2[y][b] = -INFINITY;
+                    l2[y][b] = 0.f;
+                }
+                seen_least[y] = __reduce_min_sync(0xffffffffu, min(seen[y][0], seen[y][1]));
+            }
+            // One step: P of accumulator Y against key tile j of this part.
+            auto step = [&](auto which, int j, bool first) -> bool {
+                constexpr int Y = decltype(which)::value;
+                const uint32_t c = kv_cnt + j;
+                const bool okay = mbar_wait(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, kWaitLimitNs, &sm.abort_flag) &&
+                                  mbar_wait(&sm.s_full[Y], s_ph[Y], kWaitLimitNs, &sm.abort_flag);
+                if (!__all_sync(0xffffffffu, okay)) return false;
+                s_ph[Y] ^= 1;
+                tc_fence_after();
+                // in the layout of an mma accumulator: 32 columns (8 k + 2 (lane % 4) + {0, 1}) of two rows
+                float2 sv[2][16];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t r[32];
+                    tmem_ld_16x64(slab_addr + kColS + Y * 128 + h * 64, r);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        sv[0][h * 8 + k] = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
+                        sv[1][h * 8 + k] = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
+                    }
+                }
+                float2 by_key[kCodes ? 16 : 1], by_value[kCodes ? 16 : 1];
+                if constexpr (kCodes) {  // (fetched under the load of S; eight lanes share a column's)
+                    const float2* ks = reinterpret_cast<const float2*>(sm.key_scale[c % Smem::kScaleRing]) + quad;
+                    const float2* vl = reinterpret_cast<const float2*>(sm.value_log2[c % Smem::kScaleRing]) + quad;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        by_key[k] = ks[4 * k];
+                        by_value[k] = vl[4 * k];
+                    }
+                }
+                const uint4 m128 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
+                tmem_wait_ld();
+                if constexpr (kCodes) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        sv[0][k] = fma2(sv[0][k], by_key[k], by_value[k]);
+                        sv[1][k] = fma2(sv[1][k], by_key[k], by_value[k]);
+                    }
+                }
+                if (seen_least[Y] - j * kTileKV < kTileKV || (m128.x & m128.y & m128.z & m128.w) != 0xffffffffu) {
+                    const uint32_t words[4] = {m128.x, m128.y, m128.z, m128.w};
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int valid = ok[Y][b] ? seen[Y][b] - j * kTileKV : kTileKV;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {  // select, never multiply
+                            const uint32_t keep = (words[k >> 2] & low_bits(valid - 32 * (k >> 2))) >> (8 * (k & 3) + 2 * quad);
+                            if (!(keep & 1)) sv[b][k].x = -INFINITY;
+                            if (!(keep & 2)) sv[b][k].y = -INFINITY;
+                        }
+                    }
+                }
+                float mx[2];
+                bool raise = false;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    float u = max3(sv[b][0].x, sv[b][0].y, sv[b][1].x), v = max3(sv[b][1].y, sv[b][2].x, sv[b][2].y);
+#pragma unroll
+                    for (int k = 3; k < 15; k += 2) {
+                        u = max3(u, sv[b][k].x, sv[b][k].y);
+                        v = max3(v, sv[b][k + 1].x, sv[b][k + 1].y);
+                    }
+                    mx[b] = fmaxf(max3(u, sv[b][15].x, sv[b][15].y), v) * mul;
+                    raise |= ok[Y][b] && mx[b] - m2[Y][b] > kRescaleThresholdLog2;
+                }
+                if (__any_sync(0xffffffffu, raise)) {
+                    // all lanes of a row take its maximum as the new reference; O is rescaled (the step before this one is complete: S of
+                    // this one was issued after it)
+                    float alpha[2];
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
+                        mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
+                        alpha[b] = 1.f;
+                        if (ok[Y][b] && mx[b] > m2[Y][b]) {
+                            alpha[b] = ex2(m2[Y][b] - mx[b]);
+                            l2[Y][b] *= alpha[b];
+                            m2[Y][b] = mx[b];
+                        }
+                    }
+                    if (!first) {
+#pragma unroll 1
+                        for (int h = 0; h < D / 64; ++h) {
+                            const uint32_t at = slab_addr + kColO + Y * 128 + h * 64;
+                            uint32_t r[32];
+                            tmem_ld_16x64(at, r);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha[(k >> 1) & 1]);
+                            tmem_st_16x64(at, r);
+                        }
+                    }
+                }
+                const float2* vi = reinterpret_cast<const float2*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0]) + quad;
+                float2 nm[2], sum[2];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const float ref = m2[Y][b], nmb = ref == -INFINITY ? 0.f : -ref;  // (a row may have seen no key yet)
+                    nm[b] = make_float2(nmb, nmb);
+                    sum[b] = make_float2(0.f, 0.f);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {  // P, rounded once, goes to the MMA warp in two halves of 64 key columns
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float2 f = kCodes ? vi[4 * (8 * h + k)] : make_float2(1.f, 1.f);
+#pragma unroll
+                        for (int b = 0; b < 2; ++b) {
+                            float2 e = kCodes ? add2(sv[b][8 * h + k], nm[b]) : fma2(sv[b][8 * h + k], make_float2(mul, mul), nm[b]);
+                            e = make_float2(ex2(e.x), ex2(e.y));
+                            sum[b] = kCodes ? fma2(e, f, sum[b]) : add2(sum[b], e);
+                            pk[2 * k + b] = kCodes ? pack_half(e.x, e.y) : pack_bf16(e.x, e.y);
+                        }
+                    }
+                    tmem_st_16x32(slab_addr + kColS + Y * 128 + h * 32, pk);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(&sm.p_half[Y][h]);
+                }
+#pragma unroll
+                for (int b = 0; b < 2; ++b) l2[Y][b] += sum[b].x + sum[b].y;
+                return true;
+            };
+            bool okay = true;
+            if (two) {
+                for (int j = 0; j < n && okay; ++j)
+                    okay = step(std::integral_constant<int, 0>(), j, j == 0) && step(std::integral_constant<int, 1>(), j, j == 0);
+            } else {
+                for (int j = 0; j < n && okay; j += 2) {
+                    okay = step(std::integral_constant<int, 0>(), j, j == 0);
+                    if (j + 1 < n && okay) okay = step(std::integral_constant<int, 1>(), j + 1, j == 0);
+                }
+            }
+            if (!okay) {
+                report(p.status, &sm.abort_flag, 7021);
+                goto teardown;
+            }
+            // ---- the item's end.  P V of the last steps has seen every warp, so all are through with the item before: the statistics'
+            // place is free.  From here on a row per thread; with two query tiles warpgroup x writes tile x, with one half of its columns
+            if (n > 0) {
+                for (int y = 0; y < 2; ++y)
+                    if (two || n > y) {
+                        ZL_WAIT_REGS(&sm.o_full[y], o_cnt[y] & 1, 22 + y);
+                        ++o_cnt[y];
+                    }
+                tc_fence_after();
+            }
             const int32_t tok = w.tok0 + (two ? x * tile_tokens : 0) + row_tok;  // of the sequence
             const bool row_ok = row_tok < tile_tokens && tok < w.tok0 + w.tokens;
-            // (rows that do not exist hold anything, and take no part in what a warp decides together)
-            int32_t seen[4], seen_least = INT32_MAX;
-            uint32_t ok = 0;
-            float m4[4], l4[4];  // reference maximum in powers of two, sum
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t rt = (quarter * 32 + 8 * i + (lane >> 2)) / p.group, tk = w.tok0 + (two ? x * tile_tokens : 0) + rt;
-                const bool there = rt < tile_tokens && tk < w.tok0 + w.tokens;
-                ok |= there ? 1u << i : 0u;
-                seen[i] = there ? keys_seen(w.seq(), tk) - w.tile0 * kTileKV : INT32_MAX;
-                seen_least = min(seen_least, seen[i]);
-                m4[i] = -INFINITY;
-                l4[i] = 0.f;
-            }
-            seen_least = __reduce_min_sync(0xffffffffu, seen_least);
-            const float mul = kCodes ? 1.f : p.scale_log2;  // (of 8-bit caches the keys' scales have it)
-            for (int j = two ? 0 : x; j < n; j += two ? 1 : 2) {
-                const uint32_t c = kv_cnt + j;
-                const bool first = j == (two ? 0 : x);
-                ZL_WAIT_REGS(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, 20);
-                ZL_WAIT_REGS(&sm.s_full[x], s_cnt & 1, 21);
-                ++s_cnt;
-                tc_fence_after();
-                const uint4 m128 = *reinterpret_cast<const uint4*>(sm.mask[c % kMaskRing]);
-                const bool cut = seen_least - j * kTileKV < kTileKV || (m128.x & m128.y & m128.z & m128.w) != 0xffffffffu;
-                const float2* vi = reinterpret_cast<const float2*>(sm.value_inv[kCodes ? c % Smem::kScaleRing : 0]) + quad;
-                // Sixteen rows of the warp at a time, in the layout of an mma accumulator: a thread has 32 columns of two rows.  (With all 128
-                // columns of its row a thread needs more registers than there are beside the converting warps; a spill is an L2 access
-                // here.  For bf16, where they nearly fit, both ways take the same time.)
-#pragma unroll
-                for (int slab = 0; slab < 2; ++slab) {
-                    float2 sv[2][16];  // row, pair of columns
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t r[32];
-                        tmem_ld_16x64(lane_addr + slab * kSlab + col_s + h * 64, r);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            sv[0][h * 8 + k] = make_float2(__uint_as_float(r[4 * k]), __uint_as_float(r[4 * k + 1]));
-                            sv[1][h * 8 + k] = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
-                        }
-                    }
-                    float2 by_key[kCodes ? 16 : 1], by_value[kCodes ? 16 : 1];
-                    if constexpr (kCodes) {  // (fetched under the load of S; eight lanes share a column's)
-                        const float2* ks = reinterpret_cast<const float2*>(sm.key_scale[c % Smem::kScaleRing]) + quad;
-                        const float2* vl = reinterpret_cast<const float2*>(sm.value_log2[c % Smem::kScaleRing]) + quad;
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            by_key[k] = ks[4 * k];
-                            by_value[k] = vl[4 * k];
-                        }
-                    }
-                    tmem_wait_ld();
-                    if constexpr (kCodes) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            sv[0][k] = fma2(sv[0][k], by_key[k], by_value[k]);
-                            sv[1][k] = fma2(sv[1][k], by_key[k], by_value[k]);
-                        }
-                    }
-                    if (cut) {
-                        const uint32_t words[4] = {m128.x, m128.y, m128.z, m128.w};
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            const int valid = (ok >> (2 * slab + b)) & 1 ? seen[2 * slab + b] - j * kTileKV : kTileKV;
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) {  // select, never multiply
-                                const uint32_t keep = (words[k >> 2] & low_bits(valid - 32 * (k >> 2))) >> (8 * (k & 3) + 2 * quad);
-                                if (!(keep & 1)) sv[b][k].x = -INFINITY;
-                                if (!(keep & 2)) sv[b][k].y = -INFINITY;
-                            }
-                        }
-                    }
-                    float mx[2];
-                    bool raise = false;
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        float u = max3(sv[b][0].x, sv[b][0].y, sv[b][1].x), v = max3(sv[b][1].y, sv[b][2].x, sv[b][2].y);
-#pragma unroll
-                        for (int k = 3; k < 15; k += 2) {
-                            u = max3(u, sv[b][k].x, sv[b][k].y);
-                            v = max3(v, sv[b][k + 1].x, sv[b][k + 1].y);
-                        }
-                        mx[b] = fmaxf(max3(u, sv[b][15].x, sv[b][15].y), v) * mul;
-                        raise |= ((ok >> (2 * slab + b)) & 1) && mx[b] - m4[2 * slab + b] > kRescaleThresholdLog2;
-                    }
-                    if (__any_sync(0xffffffffu, raise)) {
-                        // all lanes of a row take its maximum as the new reference; O is rescaled (the step before this one is complete:
-                        // S of this one was issued after it)
-                        float alpha[2];
-#pragma unroll
-                        for (int b = 0; b < 2; ++b) {
-                            const int i = 2 * slab + b;
-                            mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 1));
-                            mx[b] = fmaxf(mx[b], __shfl_xor_sync(0xffffffffu, mx[b], 2));
-                            alpha[b] = 1.f;
-                            if (((ok >> i) & 1) && mx[b] > m4[i]) {
-                                alpha[b] = ex2(m4[i] - mx[b]);
-                                l4[i] *= alpha[b];
-                                m4[i] = mx[b];
-                            }
-                        }
-                        if (!first) {
-#pragma unroll 1
-                            for (int h = 0; h < D / 64; ++h) {
-                                const uint32_t at = lane_addr + slab * kSlab + col_o + h * 64;
-                                uint32_t r[32];
-                                tmem_ld_16x64(at, r);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(r[k]) * alpha[(k >> 1) & 1]);
-                                tmem_st_16x64(at, r);
-                            }
-                        }
-                    }
-                    float2 nm[2], sum[2];
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const float ref = m4[2 * slab + b], nmb = ref == -INFINITY ? 0.f : -ref;  // (a row may have seen no key yet)
-                        nm[b] = make_float2(nmb, nmb);
-                        sum[b] = make_float2(0.f, 0.f);
-                    }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {  // P, rounded once
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float2 f = kCodes ? vi[4 * (8 * h + k)] : make_float2(1.f, 1.f);
-#pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                float2 e = kCodes ? add2(sv[b][8 * h + k], nm[b]) : fma2(sv[b][8 * h + k], make_float2(mul, mul), nm[b]);
-                                e = make_float2(ex2(e.x), ex2(e.y));
-                                sum[b] = kCodes ? fma2(e, f, sum[b]) : add2(sum[b], e);
-                                pk[2 * k + b] = kCodes ? pack_half(e.x, e.y) : pack_bf16(e.x, e.y);
-                            }
-                        }
-                        tmem_st_16x32(lane_addr + slab * kSlab + col_s + h * 32, pk);
-                        if (slab == 1) {  // to the MMA warp in two halves of 64 key columns
-                            tmem_wait_st();
-                            tc_fence_before();
-                            mbar_arrive(&sm.p_half[x][h]);
-                        }
-                    }
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) l4[2 * slab + b] += sum[b].x + sum[b].y;
-                }
-            }
-            // a row per thread from here on
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 1);
-                l4[i] += __shfl_xor_sync(0xffffffffu, l4[i], 2);
-                if (quad == 0) sm.stat[x][quarter * 32 + 8 * i + (lane >> 2)] = make_float2(m4[i], l4[i]);
-            }
-            __syncwarp();
-            float m_ref = sm.stat[x][row].x, l = sm.stat[x][row].y;
-            // ---- the item's end: weights of the accumulators for this row, and the columns this warpgroup writes
-            float wt[2] = {two && x == 1 ? 0.f : 1.f, two && x == 1 ? 1.f : 0.f};
+            float m_ref = -INFINITY, l = 0.f, wt[2] = {two && x == 1 ? 0.f : 1.f, two && x == 1 ? 1.f : 0.f};  // weights of the accumulators
             if (n > 0) {
-                if (two) {
-                    ZL_WAIT_REGS(&sm.o_full[x], o_cnt[x] & 1, 22);
-                } else {
-                    for (int y = 0; y < 2; ++y)
-                        if (n > y) ZL_WAIT_REGS(&sm.o_full[y], o_cnt[y] & 1, 23);
-                }
+#pragma unroll
                 for (int y = 0; y < 2; ++y)
-                    if (two || n > y) ++o_cnt[y];
-                tc_fence_after();
-                if (!two) {
-                    mbar_arrive(&sm.stat_full);
-                    ZL_WAIT_REGS(&sm.stat_full, join_cnt & 1, 24);
-                    const float2 a = sm.stat[0][row], b = sm.stat[1][row];
-                    m_ref = fmaxf(a.x, b.x);
-                    wt[0] = m_ref == -INFINITY ? 0.f : ex2(a.x - m_ref);
-                    wt[1] = m_ref == -INFINITY ? 0.f : ex2(b.x - m_ref);
-                    l = wt[0] * a.y + wt[1] * b.y;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        l2[y][b] += __shfl_xor_sync(0xffffffffu, l2[y][b], 1);
+                        l2[y][b] += __shfl_xor_sync(0xffffffffu, l2[y][b], 2);
+                        if (quad == 0) sm.stat[y][slab_row + 8 * b] = make_float2(m2[y][b], l2[y][b]);
+                    }
+                mbar_arrive(&sm.stat_full);
+                ZL_WAIT_REGS(&sm.stat_full, join_cnt & 1, 24);
+                ++join_cnt;
+                const float2 s0 = sm.stat[0][row], s1 = sm.stat[1][row];
+                if (two) {
+                    m_ref = x == 0 ? s0.x : s1.x;
+                    l = x == 0 ? s0.y : s1.y;
+                } else {
+                    m_ref = fmaxf(s0.x, s1.x);
+                    wt[0] = m_ref == -INFINITY ? 0.f : ex2(s0.x - m_ref);
+                    wt[1] = m_ref == -INFINITY ? 0.f : ex2(s1.x - m_ref);
+                    l = wt[0] * s0.y + wt[1] * s1.y;
                 }
             }
             const int c0 = two ? 0 : x * (D / 2), n_cols = two ? D : D / 2;
@@ -931,11 +946,6 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
             }
             tc_fence_before();
-            if (!two && n > 0) {  // both accumulators and the statistics have been read
-                mbar_arrive(&sm.join_done);
-                ZL_WAIT_REGS(&sm.join_done, join_cnt & 1, 25);
-                ++join_cnt;
-            }
             kv_cnt += n;
         ZL_ITEM_DONE
     }
