@@ -34,9 +34,9 @@ constexpr uint64_t kWaitLimitNs = 4000000000ull;
 constexpr float kRescaleThresholdLog2 = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaskRing = 8;   // key tiles whose masks are kept: more than can be under way
-// Units of work: a key tile under two query tiles takes 4,700 clocks (bf16, 8-bit codes 5,500), under one 2,800 (3,600).  Counted as
-// half, the CTAs with single tiles finished a fifth later than the others.
-constexpr int32_t kTwoCost = 8, kOneCost = 5;  // a key under two query tiles, under one
+// Units of work: a key tile under two query tiles takes 4,100 clocks (bf16; 8-bit codes 5,800), under one 2,900 (4,500).  With
+// the second counted as half of the first, CTAs with single tiles finished a third later than the others.
+constexpr int32_t kTwoCost = 8, kOneCost = 6;  // a key under two query tiles, under one
 constexpr int32_t kItemCost = 1536;            // start and end of an item
 constexpr int64_t kLeastUnits = 4 * kTileKV * kTwoCost;  // least stretch of a CTA
 
