@@ -331,7 +331,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     if (idle) {
         if (threadIdx.x == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;
     } else if (warp < 4) {
-        if constexpr (kCodes) reg_dec<88>(); else reg_dec<136>();
+        if constexpr (kCodes) reg_dec<80>(); else reg_dec<136>();
         if (warp == 2) {
             // -------------------------------------------------------------- the line of work
             ItemWalk walk(p, sm.start_seq, sm.start_base, per, total);
@@ -562,7 +562,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
     } else if (kCodes && warp >= 12) {
         // ------------------------------------------------------------------ codes to bf16
-        reg_dec<88>();
+        reg_dec<80>();
         if constexpr (kCodes) {
             const int t = threadIdx.x - 384;
             // This thread's 16-byte pieces of a tile of codes: piece `ch` of rows r, r + kRowStep, ... (a multiple of 8: the exchange
@@ -689,7 +689,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
     } else {
         // ------------------------------------------------------------------ softmax, join and output
-        if constexpr (kCodes) reg_inc<168>(); else reg_inc<184>();
+        if constexpr (kCodes) reg_inc<176>(); else reg_inc<184>();
         const int x = (warp - 4) >> 2;             // half of the rows of a warp's TMEM quarter; tile or columns of the output
         const int quarter = warp & 3;              // TMEM lane quarter this warp may access
         const int row = quarter * 32 + lane;       // of the output
@@ -720,7 +720,8 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 seen_least[y] = __reduce_min_sync(0xffffffffu, min(seen[y][0], seen[y][1]));
             }
             // One step: P of accumulator Y against key tile j of this part.
-            auto step = [&](auto which, int j, bool first) -> bool {
+            float2 by_key[kCodes ? 16 : 1], by_value[kCodes ? 16 : 1];  // 8-bit caches: of this thread's columns of key tile j
+            auto step = [&](auto which, auto fetch, int j, bool first) -> bool {
                 constexpr int Y = decltype(which)::value;
                 const uint32_t c = kv_cnt + j;
                 const bool okay = mbar_wait(&sm.tile_full[c % kMaskRing], (c / kMaskRing) & 1, kWaitLimitNs, &sm.abort_flag) &&
@@ -740,8 +741,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         sv[1][h * 8 + k] = make_float2(__uint_as_float(r[4 * k + 2]), __uint_as_float(r[4 * k + 3]));
                     }
                 }
-                float2 by_key[kCodes ? 16 : 1], by_value[kCodes ? 16 : 1];
-                if constexpr (kCodes) {  // (fetched under the load of S; eight lanes share a column's)
+                if constexpr (kCodes && decltype(fetch)::value) {  // (fetched under the load of S; eight lanes share a column's)
                     const float2* ks = reinterpret_cast<const float2*>(sm.key_scale[c % Smem::kScaleRing]) + quad;
                     const float2* vl = reinterpret_cast<const float2*>(sm.value_log2[c % Smem::kScaleRing]) + quad;
 #pragma unroll
@@ -847,11 +847,12 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             bool okay = true;
             if (two) {
                 for (int j = 0; j < n && okay; ++j)
-                    okay = step(std::integral_constant<int, 0>(), j, j == 0) && step(std::integral_constant<int, 1>(), j, j == 0);
+                    okay = step(std::integral_constant<int, 0>(), std::true_type(), j, j == 0) &&
+                           step(std::integral_constant<int, 1>(), std::false_type(), j, j == 0);
             } else {
                 for (int j = 0; j < n && okay; j += 2) {
-                    okay = step(std::integral_constant<int, 0>(), j, j == 0);
-                    if (j + 1 < n && okay) okay = step(std::integral_constant<int, 1>(), j + 1, j == 0);
+                    okay = step(std::integral_constant<int, 0>(), std::true_type(), j, j == 0);
+                    if (j + 1 < n && okay) okay = step(std::integral_constant<int, 1>(), std::true_type(), j + 1, j == 0);
                 }
             }
             if (!okay) {
