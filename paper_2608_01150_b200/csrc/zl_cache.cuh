@@ -54,6 +54,11 @@ __device__ __forceinline__ int find_seq(const int32_t* cu, int n, int32_t row) {
     return lo < n && __ldg(cu + lo) <= row ? lo : -1;
 }
 
+// a / b for numbers, not negative, that nearly always fit 32 bits.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // ------------------------------------------------------------------------------------------------ 8-bit codes
 // Two whole numbers in bytes I and J of `w` as a bf16 pair, exactly: 0x43 in front of the low seven bits is 128 + low bits
 // (one unit in the last place is 1 there), and 128, or 256 for a negative number, is taken off again.

@@ -239,13 +239,13 @@ zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cach
     p.chunk_part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + tokens_bytes(*attn));
     p.chunk_cut = static_cast<uint8_t*>(workspace) + tokens_bytes(*attn) + chunk_bytes(*attn);
     p.status = attn->d_words;
-    // Sequences of more rows per key head than an item of the tokens kernel has are the chunk kernel's.  Where max_q says that
-    // there are none, or that all are of that kind (as many rows as the longest times their number), the other kernel is not
-    // launched.  An item has eight rows, or 16 where a single token, or the longest sequence, has more than eight.
+    // Sequences of more than kTokenRows rows per key head are the chunk kernel's.  Where max_q says that there are none, or that
+    // all are of that kind (as many rows as the longest times their number), the other kernel is not launched.  An item of the
+    // tokens kernel has eight rows, or 16 where a single token, or the longest sequence, has more than eight.
     const int32_t max_q = batch->max_q;
     const bool few = max_q > 0 && (int64_t)max_q * p.group <= kTokenRows;
     p.token_rows = few ? (max_q * p.group <= 8 ? 8 : kTokenRows) : (p.group <= 8 ? 8 : kTokenRows);
-    const bool all_long = !few && max_q > 0 && (int64_t)max_q * p.b.n_seqs == p.b.total_q;
+    const bool all_long = !few && max_q > 0 && (int64_t)max_q * p.b.n_seqs == p.b.total_q;  // (if not so after all, it takes the rest too)
     // a cache without a page has no key, and nothing to describe to the copy engine
     const bool chunk = !few && p.c.n_pages > 0 && p.b.max_pages > 0;
     p.split = chunk && !all_long;

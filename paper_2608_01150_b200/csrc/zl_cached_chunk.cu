@@ -93,7 +93,7 @@ struct Geometry {
     int32_t heads;
     int32_t rest_rows;  // sequences of at most as many rows are another kernel's
     __device__ __forceinline__ explicit Geometry(const CachedParams& p)
-        : tokens(kTileQ / p.group), heads(p.c.n_kv_heads), rest_rows(p.split ? p.token_rows : 0) {}
+        : tokens(kTileQ / p.group), heads(p.c.n_kv_heads), rest_rows(p.split ? kTokenRows : 0) {}
 };
 
 struct SeqLine {
@@ -116,8 +116,8 @@ struct SeqLine {
         const int64_t by_prefix = min(v.keys, max(v.prefix, 0));
         int64_t i0 = b, i1 = b;  // blocks bound by the prefix, by the order or the prefix
         if (by_prefix < v.keys) {
-            i0 = by_prefix < v.pos0 ? 0 : min((int64_t)b, (by_prefix - v.pos0) / T);
-            i1 = v.keys < v.pos0 ? i0 : max(i0, min((int64_t)b, ((int64_t)v.keys - v.pos0) / T));
+            i0 = by_prefix < v.pos0 ? 0 : min((int64_t)b, quotient(by_prefix - v.pos0, T));
+            i1 = v.keys < v.pos0 ? i0 : max(i0, min((int64_t)b, quotient((int64_t)v.keys - v.pos0, T)));
         }
         const int64_t keys = i0 * by_prefix + (i1 - i0) * v.pos0 + (i1 * (i1 + 1) - i0 * (i0 + 1)) / 2 * T + (b - i1) * (int64_t)v.keys;
         return (int64_t)b * kItemCost + kTwoCost * keys;
@@ -155,21 +155,21 @@ struct ItemWalk {
             }
             const int64_t cost = line.block_cost(g, lo);
             const int64_t block0 = g.heads * line.cost_before(g, lo);
-            const int32_t head = (int32_t)((in - block0) / cost);
+            const int32_t head = (int32_t)quotient(in - block0, cost);
             const int64_t item0 = base + block0 + head * cost;
             const int64_t stop = min(end, item0 + cost);
             const int32_t keys = line.block_keys(g, lo), tokens = line.block_tokens(g, lo);
             const bool two = tokens > g.tokens;
             const int32_t tiles = (keys + kTileKV - 1) / kTileKV;
             const int64_t step = kTileKV * (two ? kTwoCost : kOneCost), first = item0 + kItemCost;  // tile t lies where its first key does
-            auto tiles_before = [&](int64_t u) { return u <= first ? 0 : (int32_t)min((int64_t)tiles, (u - first + step - 1) / step); };
+            auto tiles_before = [&](int64_t u) { return u <= first ? 0 : (int32_t)min((int64_t)tiles, quotient(u - first + step - 1, step)); };
             const int32_t tile0 = tiles_before(at), tile1 = tiles_before(stop);
             const bool starts_here = at == item0;
             at = stop;
             if (tile1 <= tile0 && !(tiles == 0 && starts_here)) continue;  // only the start of an item whose tiles lie in later CTAs
-            const int32_t c_first = tiles > 0 ? (int32_t)(first / per) : 0;
+            const int32_t c_first = tiles > 0 ? (int32_t)quotient(first, per) : 0;
             w = Item{s, head, tile0, tile1, lo * 2 * g.tokens, tokens, keys, two ? 1 : 0, line.v.q0, line.v.pos0, line.v.keys, line.v.prefix,
-                     c_first, tiles > 0 ? (int32_t)((first + (tiles - 1) * step) / per) : 0, first > c_first * per ? 1 : 0, 0};
+                     c_first, tiles > 0 ? (int32_t)quotient(first + (tiles - 1) * step, per) : 0, first > c_first * per ? 1 : 0, 0};
             return true;
         }
         return false;
@@ -307,7 +307,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             if (w < warp) before += sm.scan[w];
             total += sm.scan[w];
         }
-        const int64_t per = max((total + gridDim.x - 1) / gridDim.x, kLeastUnits);
+        const int64_t per = max(quotient(total + gridDim.x - 1, gridDim.x), kLeastUnits);
         const int64_t begin = per * blockIdx.x;
         int64_t at = before + upto - mine;
         if (tid == 0) sm.total = total;
@@ -325,7 +325,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         __syncthreads();
     }
     const int64_t total = sm.total;
-    const int64_t per = max((total + gridDim.x - 1) / gridDim.x, kLeastUnits);
+    const int64_t per = max(quotient(total + gridDim.x - 1, gridDim.x), kLeastUnits);
     const bool idle = per * blockIdx.x >= total;
 
     if (idle) {
@@ -596,7 +596,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     const int32_t row_tok = t / p.group, tile_tokens = kTileQ / p.group;
                     for (int x = 0; x < q_tiles; ++x)
                         if (row_tok < tile_tokens && x * tile_tokens + row_tok < w.tokens)  // (other rows may hold anything)
-#pragma unroll 1
+#pragma unroll 4
                             for (int e = 0; e < 8 * kBoxes; ++e) {
                                 const uint4 u = *reinterpret_cast<const uint4*>(sm.q[x] + (e >> 3) * Smem::kBoxBytes + t * 128 + (((e + t) & 7) << 4));
                                 for (uint32_t v : {u.x, u.y, u.z, u.w}) big = max3_abs(big, __uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
@@ -611,7 +611,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                     const float factor = half_factor(fmaxf(fmaxf(sm.q_big[0], sm.q_big[1]), fmaxf(sm.q_big[2], sm.q_big[3])), back);
                     scores_by = back * p.scale_log2;
                     for (int x = 0; x < q_tiles; ++x)
-#pragma unroll 1
+#pragma unroll 4
                         for (int e = 0; e < 8 * kBoxes; ++e) {
                             uint4* const at = reinterpret_cast<uint4*>(sm.q[x] + (e >> 3) * Smem::kBoxBytes + t * 128 + (((e + t) & 7) << 4));
                             const uint4 u = *at;

@@ -135,17 +135,12 @@ struct SeqWork {
     int32_t items, tiles;
     __device__ __forceinline__ SeqWork(const CachedParams& p, const SeqView& v) {
         int32_t blocks = (int32_t)(((int64_t)v.q_len * p.group + kRows - 1) / kRows);
-        if (p.split && blocks > 1) blocks = 0;  // the other kernel's
+        if (p.split && (int64_t)v.q_len * p.group > kTokenRows) blocks = 0;  // the other kernel's
         items = blocks * p.c.n_kv_heads;
         tiles = v.q_len > 0 ? (keys_seen(v, v.q_len - 1) + kTile - 1) / kTile : 0;
     }
     __device__ __forceinline__ int64_t units() const { return (int64_t)items * (tiles + 1); }
 };
-
-// a / b for numbers that nearly always fit 32 bits.
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
 
 __device__ __forceinline__ void report(int32_t* status, volatile int32_t* abort_flag, int where) {
     *abort_flag = 1;

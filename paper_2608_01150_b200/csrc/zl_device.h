@@ -166,7 +166,7 @@ struct CacheReadParams {
     __nv_bfloat16* k;
     __nv_bfloat16* v;
 };
-constexpr int kTokenRows = 16;  // most rows (new tokens times query heads of a key head) of an item of the tokens kernel
+constexpr int kTokenRows = 16;  // most rows (new tokens times query heads of a key head) for which mma.sync tiles do
 // Attention of a batch's new tokens over the cache.
 struct CachedParams {
     CacheView c;
@@ -181,7 +181,7 @@ struct CachedParams {
     int32_t* part_count; // per CTA: finished parts of the item that is cut first in it; zero between launches
     float* chunk_part;   // the same of the kernel for chunks
     void* chunk_cut;     // per CTA of it: the item that is cut first in it
-    int32_t split;       // both kernels run: sequences of at most token_rows rows per key head are the tokens kernel's
+    int32_t split;       // both kernels run: sequences of at most kTokenRows rows per key head are the tokens kernel's
     int32_t token_rows;  // rows of an item of the tokens kernel: 8 or kTokenRows
     int32_t head_first;  // coordinates of the K and V maps are (column, head, token, page), else (column, token, head, page)
     int32_t* status;
