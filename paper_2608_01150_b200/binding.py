@@ -625,18 +625,6 @@ def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, sc
            "zl_scored_attn_bwd_packed")
 
 
-def _look(t):
-    """What the checks of a call look at: a tensor with the same answers has passed them before."""
-    return None if t is None else (t.data_ptr(), t.dtype, t.shape, t.stride(), t.get_device())
-
-
-def _all_on_gpu(what: str, looks):
-    device = _current_device() if looks[0][4] >= 0 else -2
-    for x in looks:
-        if x is not None and x[4] != device:
-            raise ZlError(1, f"{what}: not all tensors are on the current GPU")
-
-
 def _on_gpu(what: str, t):
     """The tensor is on the current GPU, where the call's kernels run."""
     if not t.is_cuda or t.get_device() != _current_device():
@@ -662,25 +650,31 @@ class KvCache:
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self._seen = (None, None)
+        self._seen = (None,) * 6
         self.desc
 
     @property
     def desc(self) -> KvCacheDesc:
         """The C struct of what the attributes hold now (not to be written to); raises where they do not fit."""
-        key = (_look(self.k), _look(self.v), _look(self.k_scale), _look(self.v_scale))
-        seen, desc = self._seen
-        if key != seen:
-            # a struct of its own per state: a call of another thread may be reading the one before
-            desc = self._read()
-            self._seen = (key, desc)
-        return desc
+        return self._look()[5]
 
     def check(self) -> KvCacheDesc:
         """The same for a call: the tensors are on the current GPU."""
-        desc = self.desc
-        _all_on_gpu("KvCache", self._seen[0])
-        return desc
+        seen = self._look()
+        if not seen[0].is_cuda or seen[0].get_device() != _current_device():
+            raise ZlError(1, "KvCache: the tensors are not on the current GPU")
+        return seen[5]
+
+    def _look(self):
+        # the same tensors with the same storage and strides have passed the checks before; a state of its own per change: a
+        # call of another thread may be reading the one before
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        key = (k.data_ptr(), v.data_ptr(), k.shape, k.stride(), v.stride(), k.dtype, None if ks is None else ks.data_ptr(),
+               None if vs is None else vs.data_ptr())
+        seen = self._seen
+        if seen[0] is not k or seen[1] is not v or seen[2] is not ks or seen[3] is not vs or seen[4] != key:
+            self._seen = seen = (k, v, ks, vs, key, self._read())
+        return seen
 
     def _read(self) -> KvCacheDesc:
         import torch
@@ -696,6 +690,9 @@ class KvCache:
         for name, t in (("k_scale", ks), ("v_scale", vs)):
             if t is not None and (t.dtype is not torch.float32 or t.shape != shape[:3] or not t.is_contiguous()):
                 raise ZlError(1, f"KvCache: {name} must be a contiguous torch.float32 tensor [n_pages, page_size, n_kv_heads]")
+        for t in (v, ks, vs):
+            if t is not None and t.get_device() != k.get_device():
+                raise ZlError(1, "KvCache: the tensors are on different devices")
         # (a stride of a dimension of one entry may be any number)
         page, token, head = (strides[i] if shape[i] > 1 else shape[3] for i in range(3))
         return KvCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(ks), _ptr(vs), page, token, head, *_int32s(shape), fmt)
@@ -715,23 +712,28 @@ class CacheBatch:
 
     def __init__(self, cu_q, kv_len, pages, prefix=None, max_q: int = 0):
         self.cu_q, self.kv_len, self.pages, self.prefix, self.max_q = cu_q, kv_len, pages, prefix, max_q
-        self._seen = (None, None)
-        self._desc(0)
+        self._seen = (None,) * 6
+        self._look(0)
 
-    def _desc(self, total_q: int) -> CacheBatchDesc:
-        key = (_look(self.cu_q), _look(self.kv_len), _look(self.pages), _look(self.prefix), self.max_q, total_q)
-        seen, desc = self._seen
-        if key != seen:
-            desc = self._read(total_q)
-            self._seen = (key, desc)
-        return desc
-
-    def check(self, total_q: int) -> CacheBatchDesc:
+    def check(self, total_q: Optional[int]) -> CacheBatchDesc:
         """The C struct of what the attributes hold now, for a call with token tensors of total_q rows; raises where they do
         not fit or are not on the current GPU."""
-        desc = self._desc(total_q)
-        _all_on_gpu("CacheBatch", self._seen[0][:4])
-        return desc
+        seen = self._look(total_q)
+        if not seen[0].is_cuda or seen[0].get_device() != _current_device():
+            raise ZlError(1, "CacheBatch: the tensors are not on the current GPU")
+        return seen[5]
+
+    def _look(self, total_q: Optional[int]):
+        # as KvCache._look; None: the call has no token tensors, whatever was there last will do
+        cu, lens, pages, prefix = self.cu_q, self.kv_len, self.pages, self.prefix
+        seen = self._seen
+        if total_q is None:
+            total_q = 0 if seen[5] is None else seen[5].total_q
+        key = (cu.data_ptr(), lens.data_ptr(), pages.data_ptr(), pages.shape, None if prefix is None else prefix.data_ptr(),
+               self.max_q, total_q)
+        if seen[0] is not cu or seen[1] is not lens or seen[2] is not pages or seen[3] is not prefix or seen[4] != key:
+            self._seen = seen = (cu, lens, pages, prefix, key, self._read(total_q))
+        return seen
 
     def _read(self, total_q: int) -> CacheBatchDesc:
         cu, lens, pages, prefix = self.cu_q, self.kv_len, self.pages, self.prefix
@@ -743,6 +745,9 @@ class CacheBatch:
         _ints("CacheBatch: pages", pages)
         if prefix is not None:
             _ints("CacheBatch: prefix", prefix, (n,))
+        for t in (lens, pages, prefix):
+            if t is not None and t.get_device() != cu.get_device():
+                raise ZlError(1, "CacheBatch: the tensors are on different devices")
         n, width, total_q, max_q = _int32s((n, pages.shape[1], total_q, self.max_q))
         return CacheBatchDesc(cu.data_ptr(), lens.data_ptr(), pages.data_ptr(), _ptr(prefix), n, width, total_q, max_q)
 
@@ -770,8 +775,8 @@ def cache_write(cache: KvCache, batch: CacheBatch, k, v, stream=None):
     their places of the cache, quantised where it holds 8 bits."""
     c = cache.check()
     stride = _token_rows("k", k, c.n_kv_heads, c.head_dim)
-    if k.shape != v.shape or _token_rows("v", v, c.n_kv_heads, c.head_dim) != stride:
-        raise ZlError(1, "k and v must be of the same shape and strides")
+    if v.shape != k.shape or v.stride() != k.stride() or v.dtype is not k.dtype or v.get_device() != k.get_device():
+        raise ZlError(1, "k and v must be of the same shape, strides, type and device")
     b = batch.check(k.shape[0])
     _check(_lib.zl_cache_write(ctypes.byref(c), ctypes.byref(b), k.data_ptr(), v.data_ptr(), stride, _stream_ptr(stream)), "zl_cache_write")
 
@@ -781,10 +786,9 @@ def cache_read(cache: KvCache, batch: CacheBatch, cu_kv, k, v, first=None, strea
     packed bf16 tensors k, v [total_kv, n_kv_heads, head_dim]; rows without a key become 0."""
     c = cache.check()
     _packed_rows("k", k, c.n_kv_heads, c.head_dim)
-    _packed_rows("v", v, c.n_kv_heads, c.head_dim)
-    if k.shape != v.shape:
-        raise ZlError(1, "k and v must be of the same shape")
-    b = batch.check(0)
+    if v.shape != k.shape or v.dtype is not k.dtype or not v.is_contiguous() or v.get_device() != k.get_device():
+        raise ZlError(1, "v must be contiguous, of k's shape and type, on its device")
+    b = batch.check(None)
     _ints("cu_kv", cu_kv, (b.n_seqs + 1,))
     _on_gpu("cu_kv", cu_kv)
     if first is not None:
@@ -843,9 +847,8 @@ def cached_attn_fwd(attn: CachedAttnHandle, cache: KvCache, batch: CacheBatch, q
     import torch
     c = cache.check()
     stride = _token_rows("q", q, attn.n_heads, attn.head_dim)
-    _packed_rows("o", o, attn.n_heads, attn.head_dim)
-    if o.shape != q.shape:
-        raise ZlError(1, "o must be of q's shape")
+    if o.shape != q.shape or o.dtype is not q.dtype or not o.is_contiguous() or o.get_device() != q.get_device():
+        raise ZlError(1, "o must be contiguous, of q's shape and type, on its device")
     if lse is not None:
         if lse.dtype is not torch.float32 or tuple(lse.shape) != (attn.n_heads, q.shape[0]) or not lse.is_contiguous():
             raise ZlError(1, f"lse must be a contiguous torch.float32 tensor [{attn.n_heads}, {q.shape[0]}]")
