@@ -433,7 +433,9 @@ zl_status zl_scored_workspace_bytes(const zl_tasks* tasks, const zl_score* score
  *                 [n_pages, H, page_size, d] are both such layouts.  Bases 16-byte aligned.
  *   format        ZL_CACHE_BF16; ZL_CACHE_INT8 (whole numbers from -127 to 127) or ZL_CACHE_E4M3, each with one scale per
  *                 token and head: the value held is code * scale.
- *   k_scale, v_scale  device, [n_pages, page_size, n_kv_heads] fp32, contiguous; NULL with ZL_CACHE_BF16.
+ *   k_scale, v_scale  device, fp32, a number for every page, token and key head, strides in elements, the same for both; NULL
+ *                 with ZL_CACHE_BF16.  [n_pages, page_size, n_kv_heads] will do; [n_pages, n_kv_heads, page_size] is read faster
+ *                 (a head's scales lie together: single tokens over 300,000 8-bit keys gain a sixth).
  *   page_size     a power of two, at least 8.   head_dim  64 or 128.
  *
  * zl_cache_batch: sequences over it.  All arrays are DEVICE memory and read when the kernels run, so that a captured call
@@ -456,6 +458,7 @@ typedef struct {
     float* k_scale;
     float* v_scale;
     int64_t page_stride, token_stride, head_stride;
+    int64_t scale_page_stride, scale_token_stride, scale_head_stride;
     int32_t n_pages, page_size, n_kv_heads, head_dim, format;
 } zl_kv_cache;
 typedef struct {

@@ -54,6 +54,7 @@ class ScoreDesc(ctypes.Structure):
 class KvCacheDesc(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("scale_page_stride", ctypes.c_int64), ("scale_token_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64),
                 ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32)]
 
@@ -643,7 +644,8 @@ class KvCache:
     k, v              [n_pages, page_size, n_kv_heads, head_dim] of torch.bfloat16, torch.int8 or torch.float8_e4m3fn; any
                       strides (the same for both) with contiguous rows, e.g. ``pool[:, 0]``, ``pool[:, 1]`` or a transposed
                       [n_pages, n_kv_heads, page_size, head_dim]
-    k_scale, v_scale  fp32 [n_pages, page_size, n_kv_heads] of an 8-bit cache, written by cache_write; else None
+    k_scale, v_scale  fp32 [n_pages, page_size, n_kv_heads] of an 8-bit cache, written by cache_write; else None.  Any strides
+                      (the same for both); a transposed [n_pages, n_kv_heads, page_size] is read faster
 
     The attributes can be changed, and their storage swapped: every call takes what they hold then.
     """
@@ -669,8 +671,8 @@ class KvCache:
         # the same tensors with the same storage and strides have passed the checks before; a state of its own per change: a
         # call of another thread may be reading the one before
         k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
-        key = (k.data_ptr(), v.data_ptr(), k.shape, k.stride(), v.stride(), k.dtype, None if ks is None else ks.data_ptr(),
-               None if vs is None else vs.data_ptr())
+        key = (k.data_ptr(), v.data_ptr(), k.shape, k.stride(), v.stride(), k.dtype, ks is None or (ks.data_ptr(), ks.stride()),
+               vs is None or (vs.data_ptr(), vs.stride()))
         seen = self._seen
         if seen[0] is not k or seen[1] is not v or seen[2] is not ks or seen[3] is not vs or seen[4] != key:
             self._seen = seen = (k, v, ks, vs, key, self._read())
@@ -688,14 +690,15 @@ class KvCache:
         if (ks is None) != (fmt == 0) or (vs is None) != (fmt == 0):
             raise ZlError(1, "KvCache: an 8-bit cache has k_scale and v_scale, one in bf16 neither")
         for name, t in (("k_scale", ks), ("v_scale", vs)):
-            if t is not None and (t.dtype is not torch.float32 or t.shape != shape[:3] or not t.is_contiguous()):
-                raise ZlError(1, f"KvCache: {name} must be a contiguous torch.float32 tensor [n_pages, page_size, n_kv_heads]")
+            if t is not None and (t.dtype is not torch.float32 or t.shape != shape[:3] or t.stride() != ks.stride()):
+                raise ZlError(1, f"KvCache: {name} must be torch.float32 [n_pages, page_size, n_kv_heads], the strides of k_scale and v_scale the same")
         for t in (v, ks, vs):
             if t is not None and t.get_device() != k.get_device():
                 raise ZlError(1, "KvCache: the tensors are on different devices")
         # (a stride of a dimension of one entry may be any number)
         page, token, head = (strides[i] if shape[i] > 1 else shape[3] for i in range(3))
-        return KvCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(ks), _ptr(vs), page, token, head, *_int32s(shape), fmt)
+        by = (0, 0, 0) if ks is None else tuple(ks.stride()[i] if shape[i] > 1 else 1 for i in range(3))
+        return KvCacheDesc(k.data_ptr(), v.data_ptr(), _ptr(ks), _ptr(vs), page, token, head, *by, *_int32s(shape), fmt)
 
 
 class CacheBatch:

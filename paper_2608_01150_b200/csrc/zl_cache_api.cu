@@ -35,9 +35,15 @@ zl_status view(const zl_kv_cache* cache, const zl_cache_batch* batch, bool token
     const int bytes = x.format == ZL_CACHE_BF16 ? 2 : 1;
     for (int64_t s : {x.page_stride, x.token_stride, x.head_stride})
         if (s < 0 || s > (int64_t)1 << 38 || (s * bytes) % 16 != 0) return ZL_ERR_INVALID_ARG;
+    for (int64_t s : {x.scale_page_stride, x.scale_token_stride, x.scale_head_stride})
+        if (s < 0 || s > (int64_t)1 << 38) return ZL_ERR_INVALID_ARG;
     if (x.n_pages > 0) {
         if (!x.k || !x.v || !aligned16(x.k) || !aligned16(x.v)) return ZL_ERR_INVALID_ARG;
-        if (x.format != ZL_CACHE_BF16 && (!x.k_scale || !x.v_scale)) return ZL_ERR_INVALID_ARG;
+        if (x.format != ZL_CACHE_BF16) {
+            if (!x.k_scale || !x.v_scale) return ZL_ERR_INVALID_ARG;
+            if (x.scale_token_stride < 1 || (x.n_kv_heads > 1 && x.scale_head_stride < 1) || (x.n_pages > 1 && x.scale_page_stride < 1))
+                return ZL_ERR_INVALID_ARG;
+        }
         // rows of the cache may not lie over one another
         if (x.token_stride < x.head_dim || (x.n_kv_heads > 1 && x.head_stride < x.head_dim) || (x.n_pages > 1 && x.page_stride < x.head_dim))
             return ZL_ERR_INVALID_ARG;
@@ -49,7 +55,7 @@ zl_status view(const zl_kv_cache* cache, const zl_cache_batch* batch, bool token
     int shift = 0;
     while ((1 << shift) < x.page_size) ++shift;
     *c = CacheView{static_cast<uint8_t*>(x.k), static_cast<uint8_t*>(x.v), x.k_scale, x.v_scale,
-                   x.page_stride * bytes, x.token_stride * bytes, x.head_stride * bytes, x.n_pages, shift, x.n_kv_heads};
+                   x.page_stride * bytes, x.token_stride * bytes, x.head_stride * bytes, x.scale_page_stride, x.scale_token_stride, x.scale_head_stride, x.n_pages, shift, x.n_kv_heads};
     *b = CacheBatch{batch->cu_q, batch->kv_len, batch->pages, batch->prefix, batch->n_seqs, batch->max_pages, batch->total_q};
     return ZL_OK;
 }

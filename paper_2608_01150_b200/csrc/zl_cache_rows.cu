@@ -111,7 +111,7 @@ zl_cache_write_kernel(const CacheView c, const CacheBatch b, const __nv_bfloat16
                 const int32_t pg = page_at(b, c, s, pos), in = pos & ((1 << c.page_shift) - 1);
                 if (pg >= 0) {
                     slot = pg * c.page_stride + in * c.token_stride + head * c.head_stride;
-                    at_scale = (((int64_t)pg << c.page_shift) + in) * c.n_kv_heads + head;
+                    at_scale = pg * c.scale_page + in * c.scale_token + head * c.scale_head;
                 }
             }
         }
@@ -175,7 +175,7 @@ zl_cache_read_kernel(const CacheView c, const CacheBatch b, const CacheReadParam
                     xv[i] = *(reinterpret_cast<const uint4*>(c.v + slot + lane * 32) + i);
                 }
             } else {
-                const int64_t at = (((int64_t)pg << c.page_shift) + in) * c.n_kv_heads + head;
+                const int64_t at = pg * c.scale_page + in * c.scale_token + head * c.scale_head;
                 const uint4 ck = *reinterpret_cast<const uint4*>(c.k + slot + lane * 16);
                 const uint4 cv = *reinterpret_cast<const uint4*>(c.v + slot + lane * 16);
                 const float sk = c.k_scale[at], sv = c.v_scale[at];

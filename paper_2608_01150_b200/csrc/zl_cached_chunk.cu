@@ -580,7 +580,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             auto scales_of = [&](const Item& w, int32_t key, int32_t pg) {
                 float2 r = make_float2(0.f, 0.f);
                 if (pg >= 0) {
-                    const int64_t at = (((int64_t)pg << p.c.page_shift) + (key & ((1 << p.c.page_shift) - 1))) * p.c.n_kv_heads + w.head;
+                    const int64_t at = pg * p.c.scale_page + (key & ((1 << p.c.page_shift) - 1)) * p.c.scale_token + w.head * p.c.scale_head;
                     r = make_float2(__ldg(p.c.k_scale + at), __ldg(p.c.v_scale + at));
                 }
                 return r;

@@ -106,18 +106,18 @@ __device__ __forceinline__ void ldm4t(uint32_t (&r)[4], uint32_t addr) {
 // An 8x8 matrix of 16-bit numbers, one row pair per lane, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
 // c += a b: 16 rows x 8 columns, 16 deep
 __device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 __device__ __forceinline__ void mma16h(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -488,7 +488,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 }
                 if constexpr (kCodes) {
                     const bool live = pg >= 0;
-                    const int64_t off = live ? (((int64_t)pg << p.c.page_shift) + in) * p.c.n_kv_heads + w.head : 0;
+                    const int64_t off = live ? pg * p.c.scale_page + in * p.c.scale_token + w.head * p.c.scale_head : 0;
                     cp4(dst + 2 * kMatrixBytes + lane * 4, (lane < 16 ? p.c.k_scale : p.c.v_scale) + off, live);
                 }
             }
@@ -546,14 +546,20 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 fetch();  // into the stage of the step before this one
                 const uint32_t k_addr = ring + st * Smem::kStageBytes + k_at, v_addr = ring + st * Smem::kStageBytes + kMatrixBytes + v_at;
                 // ---- S^T: keys gid and gid + 8, rows 2 quad and 2 quad + 1
-                float c[kCols][4];
+                float c[kCols][4], d[kCols][4];  // even and odd chunks: two chains of sums
 #pragma unroll
-                for (int n = 0; n < kCols; ++n) c[n][0] = c[n][1] = c[n][2] = c[n][3] = 0.f;
+                for (int n = 0; n < kCols; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) c[n][i] = d[n][i] = 0.f;
+                // (all of a step's keys are fetched ahead of the products, its values ahead of the exponentials: their order is the
+                // program's)
+                uint32_t kv[Smem::kRowBytes / 32][4];
+#pragma unroll
+                for (int i = 0; i < kRowBytes / 32; ++i) ldm4(kv[i], k_addr ^ (i << 5));
                 if constexpr (kCodes) {
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ks += 2) {
-                        uint32_t r[4];  // keys 0-7 and 8-15 of chunk ks, the same of chunk ks + 1
-                        ldm4(r, k_addr ^ (ks << 4));
+                        const uint32_t(&r)[4] = kv[ks / 2];  // keys 0-7 and 8-15 of chunk ks, the same of chunk ks + 1
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             uint32_t a0, a1, a2, a3;
@@ -563,23 +569,24 @@ zl_cached_tokens_kernel(const CachedParams p) {
                             for (int n = 0; n < kCols; ++n) {
                                 uint32_t q0, q1;
                                 if constexpr (kCols == 1) { q0 = q[ks + e][0]; q1 = q[ks + e][1]; } else load_q(n, ks + e, q0, q1);
-                                mma16h(c[n], a0, a1, a2, a3, q0, q1);
+                                mma16h(e == 0 ? c[n] : d[n], a0, a1, a2, a3, q0, q1);
                             }
                         }
                     }
                 } else {
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks) {
-                        uint32_t r[4];  // keys 0-7 and 8-15 of chunk 2 ks, the same of chunk 2 ks + 1
-                        ldm4(r, k_addr ^ (ks << 5));
+                        const uint32_t(&r)[4] = kv[ks];  // keys 0-7 and 8-15 of chunk 2 ks, the same of chunk 2 ks + 1
 #pragma unroll
                         for (int n = 0; n < kCols; ++n) {
                             uint32_t q0, q1;
                             if constexpr (kCols == 1) { q0 = q[ks][0]; q1 = q[ks][1]; } else load_q(n, ks, q0, q1);
-                            mma16(c[n], r[0], r[1], r[2], r[3], q0, q1);
+                            mma16(ks % 2 == 0 ? c[n] : d[n], r[0], r[1], r[2], r[3], q0, q1);
                         }
                     }
                 }
+#pragma unroll
+                for (int i = 0; i < kRowBytes / 32; ++i) ldm4t(kv[i], v_addr ^ (i << 5));
                 const int32_t key0 = tile * kTile + warp * kKeys;
                 const uint32_t exists = sm.mask[warp][st];
                 float key_scale[2], value_scale[2], value_log2[2];
@@ -597,7 +604,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
 #pragma unroll
                 for (int n = 0; n < kCols; ++n) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) c[n][i] *= kCodes ? by_row[n][i & 1] * key_scale[i >> 1] : p.scale_log2;
+                    for (int i = 0; i < 4; ++i) c[n][i] = (c[n][i] + d[n][i]) * (kCodes ? by_row[n][i & 1] * key_scale[i >> 1] : p.scale_log2);
                     if (cut) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -613,7 +620,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                            for (int d = 4; d < 32; d <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], d));
+                            for (int u = 4; u < 32; u <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], u));
                             const float up = fmaxf(m[n][e], mx[e]);
                             const float alpha = up == -INFINITY ? 1.f : ex2(m[n][e] - up);
                             m[n][e] = up;
@@ -639,8 +646,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 if constexpr (kCodes) {
 #pragma unroll
                     for (int ch = 0; ch < D / 16; ch += 2) {
-                        uint32_t r[4];  // keys 0-7 and 8-15 of chunk ch, the same of chunk ch + 1
-                        ldm4t(r, v_addr ^ (ch << 4));
+                        const uint32_t(&r)[4] = kv[ch / 2];  // keys 0-7 and 8-15 of chunk ch, the same of chunk ch + 1
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {  // even columns of the chunk as rows 0-7, odd ones as rows 8-15
                             uint32_t a0, a1, a2, a3;
@@ -653,8 +659,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 } else {
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i) {
-                        uint32_t r[4];  // keys 0-7 of chunks 2 i and 2 i + 1, keys 8-15 of the same
-                        ldm4t(r, v_addr ^ (i << 5));
+                        const uint32_t(&r)[4] = kv[i];  // keys 0-7 of chunks 2 i and 2 i + 1, keys 8-15 of the same
 #pragma unroll
                         for (int n = 0; n < kCols; ++n) mma16(o[n][i], r[0], r[1], r[2], r[3], b[n][0], b[n][1]);
                     }

@@ -146,9 +146,10 @@ cudaError_t launch_wait_selftest(int32_t* status, uint64_t limit_ns, cudaStream_
 struct CacheView {
     uint8_t* k;
     uint8_t* v;
-    float* k_scale;  // [n_pages, page, n_kv_heads]; NULL where the cache holds bf16
+    float* k_scale;  // one number a token and head; NULL where the cache holds bf16
     float* v_scale;
     int64_t page_stride, token_stride, head_stride;
+    int64_t scale_page, scale_token, scale_head;  // strides of the scales, elements
     int32_t n_pages, page_shift, n_kv_heads;
 };
 // A batch of sequences over it (zl_cache_batch).

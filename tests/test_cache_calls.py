@@ -29,7 +29,8 @@ def refused(call, status=INVALID):
 
 
 def cache_desc(**kw):
-    f = dict(k=4096, v=8192, k_scale=None, v_scale=None, page_stride=16 * 2 * 64, token_stride=2 * 64, head_stride=64, n_pages=4,
+    f = dict(k=4096, v=8192, k_scale=None, v_scale=None, page_stride=16 * 2 * 64, token_stride=2 * 64, head_stride=64,
+             scale_page_stride=32, scale_token_stride=2, scale_head_stride=1, n_pages=4,
              page_size=16, n_kv_heads=2, head_dim=64, format=0)
     f.update(kw)
     return B.KvCacheDesc(**f)
@@ -68,7 +69,7 @@ def test_a_cache_follows_its_attributes():
     refused(lambda: c.desc)
 
 
-@pytest.mark.parametrize("bad", ["type", "types", "shape", "strides", "rows", "no_scale", "one_scale", "scale_type", "scale_shape", "scale_rows", "bf16_scale"])
+@pytest.mark.parametrize("bad", ["type", "types", "shape", "strides", "rows", "no_scale", "one_scale", "scale_type", "scale_shape", "scale_strides", "bf16_scale"])
 def test_unfit_caches_are_refused(bad):
     k, v, ks, vs = pool(torch.int8)
     if bad == "type":
@@ -89,7 +90,7 @@ def test_unfit_caches_are_refused(bad):
         ks = ks.double()
     elif bad == "scale_shape":
         ks = ks[:, :, :1].contiguous()
-    elif bad == "scale_rows":
+    elif bad == "scale_strides":
         ks = torch.zeros(4, 2, 16).transpose(1, 2)
     elif bad == "bf16_scale":
         k, v = k.to(torch.bfloat16), v.to(torch.bfloat16)
@@ -138,7 +139,9 @@ def test_tensors_that_are_not_on_the_gpu_are_refused():
     (dict(n_kv_heads=0), INVALID), (dict(k=None), INVALID), (dict(v=8200), INVALID), (dict(page_stride=2052), INVALID),
     (dict(token_stride=-128), INVALID), (dict(token_stride=32), INVALID), (dict(head_stride=0), INVALID), (dict(page_stride=0), INVALID),
     (dict(format=1), INVALID), (dict(format=2, k_scale=4096), INVALID), (dict(format=1, k_scale=4098, v_scale=4096), INVALID),
-    (dict(k_scale=4096), INVALID), (dict(format=1, k_scale=4096, v_scale=4096, token_stride=136), INVALID)])
+    (dict(k_scale=4096), INVALID), (dict(scale_page_stride=-1), INVALID), (dict(format=1, k_scale=4096, v_scale=4096, scale_token_stride=0), INVALID),
+    (dict(format=2, k_scale=4096, v_scale=4096, scale_head_stride=0), INVALID), (dict(format=2, k_scale=4096, v_scale=4096, scale_page_stride=0), INVALID),
+    (dict(format=1, k_scale=4096, v_scale=4096, token_stride=136), INVALID)])
 def test_caches_the_library_refuses(kw, status):
     lib, c, b = B.lib(), cache_desc(**kw), batch_desc()
     assert lib.zl_cache_write(ctypes.byref(c), ctypes.byref(b), 4096, 4096, 128, 0) == status

@@ -57,6 +57,8 @@ class Setup:
                 p.view(torch.int8).fill_(NAN_CODE[dtype])
         if dtype is not BF16:
             self.scales = [torch.full(shape[:3], math.nan, device="cuda") for _ in "kv"]
+            if layout == "heads":  # and the scales by heads too
+                self.scales = [torch.full((n_pages, heads, page), math.nan, device="cuda").transpose(1, 2) for _ in "kv"]
         self.pools = pools
         import paper_2608_01150_b200 as Z
         self.cache = Z.KvCache(pools[0], pools[1], *self.scales)
