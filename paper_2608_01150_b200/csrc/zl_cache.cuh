@@ -44,6 +44,14 @@ __device__ __forceinline__ int32_t page_at(const CacheBatch& b, const CacheView&
     return (uint32_t)pg < (uint32_t)c.n_pages ? pg : -1;
 }
 
+// The same in two halves, for code that looks ahead: the entry of the table, whose use would wait for it, and what it means.
+__device__ __forceinline__ int32_t page_entry(const CacheBatch& b, const CacheView& c, int s, int32_t pos) {
+    return __ldg(b.pages + (int64_t)s * b.max_pages + (pos >> c.page_shift));
+}
+__device__ __forceinline__ int32_t valid_page(const CacheView& c, int32_t entry) {
+    return (uint32_t)entry < (uint32_t)c.n_pages ? entry : -1;
+}
+
 // The sequence whose range [cu[s], cu[s + 1]) holds a row, -1 for none.
 __device__ __forceinline__ int find_seq(const int32_t* cu, int n, int32_t row) {
     int lo = 0, hi = n;  // the last s with cu[s] <= row

@@ -34,9 +34,9 @@ zl_status view(const zl_kv_cache* cache, const zl_cache_batch* batch, bool token
     if (x.page_size < 8 || (x.page_size & (x.page_size - 1)) != 0 || x.page_size > (1 << 24)) return ZL_ERR_UNSUPPORTED;
     const int bytes = x.format == ZL_CACHE_BF16 ? 2 : 1;
     for (int64_t s : {x.page_stride, x.token_stride, x.head_stride})
-        if (s < 0 || s > (int64_t)1 << 38 || (s * bytes) % 16 != 0) return ZL_ERR_INVALID_ARG;
+        if (s < 0 || s > (int64_t)1 << 35 || (s * bytes) % 16 != 0) return ZL_ERR_INVALID_ARG;  // (in units of 16 bytes they fit 32 bits)
     for (int64_t s : {x.scale_page_stride, x.scale_token_stride, x.scale_head_stride})
-        if (s < 0 || s > (int64_t)1 << 38) return ZL_ERR_INVALID_ARG;
+        if (s < 0 || s >= (int64_t)1 << 32) return ZL_ERR_INVALID_ARG;
     if (x.n_pages > 0) {
         if (!x.k || !x.v || !aligned16(x.k) || !aligned16(x.v)) return ZL_ERR_INVALID_ARG;
         if (x.format != ZL_CACHE_BF16) {
@@ -55,7 +55,8 @@ zl_status view(const zl_kv_cache* cache, const zl_cache_batch* batch, bool token
     int shift = 0;
     while ((1 << shift) < x.page_size) ++shift;
     *c = CacheView{static_cast<uint8_t*>(x.k), static_cast<uint8_t*>(x.v), x.k_scale, x.v_scale,
-                   x.page_stride * bytes, x.token_stride * bytes, x.head_stride * bytes, x.scale_page_stride, x.scale_token_stride, x.scale_head_stride, x.n_pages, shift, x.n_kv_heads};
+                   x.page_stride * bytes, x.token_stride * bytes, x.head_stride * bytes, x.scale_page_stride, x.scale_token_stride, x.scale_head_stride,
+                   (uint32_t)(x.page_stride * bytes / 16), (uint32_t)(x.token_stride * bytes / 16), (uint32_t)(x.head_stride * bytes / 16), x.n_pages, shift, x.n_kv_heads};
     *b = CacheBatch{batch->cu_q, batch->kv_len, batch->pages, batch->prefix, batch->n_seqs, batch->max_pages, batch->total_q};
     return ZL_OK;
 }

@@ -449,7 +449,12 @@ zl_cached_tokens_kernel(const CachedParams p) {
         // ---- copies: this warp's 16 keys of every tile of every item, kStages - 1 steps ahead of their use
         uint32_t f_item = 0, f_stage = 0;
         int32_t f_tile = 0, f_end = 0;  // the next step's tile, the item's last; f_end < 0: no more items
-        int32_t f_page = -1;            // page of this lane's key (key lane % 16) of the next step, looked up a step ahead
+        int32_t f_page = -1;            // table entry of this lane's key (key lane % 16) of the next step, looked up a step ahead
+        // the item's: keys, row of the page table, where its head lies in a token (16 bytes; elements of the scales)
+        int32_t f_keys = 0;
+        const int32_t* f_pages = nullptr;
+        uint64_t f_head = 0, f_scale = 0;
+        const int32_t in_page = (1 << p.c.page_shift) - 1;
         bool waited = true;
         auto fetch = [&]() {
             if (f_tile >= f_end && f_end >= 0) {
@@ -461,22 +466,27 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 f_end = waited ? sm.items[place].tile1 : -1;
                 ++f_item;
                 if (f_end >= 0) {
+                    const Item& w = sm.items[place];
+                    f_keys = w.keys;
+                    f_pages = p.b.pages + (int64_t)w.s * p.b.max_pages;
+                    f_head = (uint64_t)(uint32_t)w.head * p.c.head16;
+                    f_scale = (uint64_t)(uint32_t)w.head * (uint32_t)p.c.scale_head;
                     const int32_t key = f_tile * kTile + warp * kKeys + (lane & 15);
-                    f_page = key < sm.items[place].keys ? page_at(p.b, p.c, sm.items[place].s, key) : -1;
+                    f_page = key < f_keys ? __ldg(f_pages + (key >> p.c.page_shift)) : -1;
                 }
             }
             if (f_end >= 0) {
-                const Item& w = sm.items[(f_item - 1) % kItems];
                 const int32_t key0 = f_tile * kTile + warp * kKeys;
                 const uint32_t dst = ring + f_stage * Smem::kStageBytes;
                 const int32_t key = key0 + (lane & 15);
-                const int32_t pg = f_page;
+                const int32_t pg = valid_page(p.c, f_page);
                 const uint32_t exists = __ballot_sync(0xffffffffu, pg >= 0);
-                if (++f_tile < f_end) f_page = key + kTile < w.keys ? page_at(p.b, p.c, w.s, key + kTile) : -1;
+                if (++f_tile < f_end) f_page = key + kTile < f_keys ? __ldg(f_pages + ((key + kTile) >> p.c.page_shift)) : -1;
                 if (lane == 0) sm.mask[warp][f_stage] = exists & 0xffffu;
                 // every lane works out its key's place; the copies of a row take it from there
-                const int32_t in = key & ((1 << p.c.page_shift) - 1);
-                const int64_t place = pg >= 0 ? pg * p.c.page_stride + in * p.c.token_stride + w.head * p.c.head_stride : -1;
+                const uint32_t in = key & in_page;
+                const uint64_t at16 = (uint64_t)(uint32_t)pg * p.c.page16 + ((uint64_t)in * p.c.token16 + f_head);
+                const int64_t place = pg >= 0 ? (int64_t)(at16 << 4) : -1;
 #pragma unroll
                 for (int i = 0; i < kKeys / kRowsAtOnce; ++i) {
                     const int64_t from = __shfl_sync(0xffffffffu, place, i * kRowsAtOnce + lane / kChunks);
@@ -488,7 +498,8 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 }
                 if constexpr (kCodes) {
                     const bool live = pg >= 0;
-                    const int64_t off = live ? pg * p.c.scale_page + in * p.c.scale_token + w.head * p.c.scale_head : 0;
+                    const uint64_t at = (uint64_t)(uint32_t)pg * (uint32_t)p.c.scale_page + ((uint64_t)in * (uint32_t)p.c.scale_token + f_scale);
+                    const uint64_t off = live ? at : 0;
                     cp4(dst + 2 * kMatrixBytes + lane * 4, (lane < 16 ? p.c.k_scale : p.c.v_scale) + off, live);
                 }
             }

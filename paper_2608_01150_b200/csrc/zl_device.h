@@ -150,6 +150,7 @@ struct CacheView {
     float* v_scale;
     int64_t page_stride, token_stride, head_stride;
     int64_t scale_page, scale_token, scale_head;  // strides of the scales, elements
+    uint32_t page16, token16, head16;             // strides of the keys in 16 bytes
     int32_t n_pages, page_shift, n_kv_heads;
 };
 // A batch of sequences over it (zl_cache_batch).
