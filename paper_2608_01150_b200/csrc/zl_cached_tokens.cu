@@ -6,7 +6,7 @@
 //   * one CTA per SM; all CTAs together walk one line of work, item after item (sequence, block of rows, key head), in tiles
 //     of some hundred keys, and each takes an equal stretch of it, wherever that cuts an item.  The lengths are read from
 //     device memory when the kernel runs: a captured call follows them, and nothing is planned on the host;
-//   * a streaming warp fetches 16 keys and values at a time into its private ring (16-byte asynchronous copies, page by page)
+//   * a streaming warp fetches 16 keys and values (32 of 8 bits) at a time into its private ring (16-byte asynchronous copies, page by page)
 //     and keeps its own running maximum, sum and accumulator: no barrier in the loop, and no pause between items;
 //   * four helper warps do what items need beside that: they walk the line ahead of the stream, prepare an item's queries, and
 //     join the streaming warps' results from shared memory while those are in the next item already.  (Done by all warps
@@ -28,7 +28,6 @@ using namespace cache;
 
 namespace {
 
-constexpr int kKeys = 16;        // keys of a warp's step
 constexpr int kJoin = 32;        // parts that are joined at a time
 constexpr int kHelpers = 4;      // warps that do not stream
 // Least units of a CTA's stretch, where items are that long: cutting an item costs its parts' way through memory, some
@@ -50,11 +49,12 @@ template <int D, int kFormat, int kCols>
 struct TokenSmem {
     static constexpr bool kCodes = kFormat != ZL_CACHE_BF16;
     static constexpr int kRows = 8 * kCols;
-    static constexpr int kWarps = kCodes ? (kCols == 1 ? 12 : 8) : (D == 64 ? (kCols == 1 ? 11 : 8) : (kCols == 1 ? 7 : 6));  // that stream
+    static constexpr int kWarps = kCodes ? (kCols == 1 ? (D == 128 ? 10 : 12) : 8) : (D == 64 ? (kCols == 1 ? 11 : 8) : (kCols == 1 ? 7 : 6));  // that stream
+    static constexpr int kKeys = kCodes && kCols == 1 ? 32 : 16;  // of a warp's step: as many as amortise what a step costs beside them
     static constexpr int kRowBytes = D * (kCodes ? 1 : 2);
-    static constexpr int kMatrixBytes = kKeys * kRowBytes;  // 16 keys or 16 values
+    static constexpr int kMatrixBytes = kKeys * kRowBytes;  // the keys or the values of a step
     static constexpr int kStageBytes = 2 * kMatrixBytes + (kCodes ? 2 * kKeys * 4 : 0);
-    static constexpr int kStages = D == 128 ? 3 : (kCodes ? 6 : 4);
+    static constexpr int kStages = D == 128 ? (kKeys == 32 ? 2 : 3) : (kKeys == 32 ? 3 : (kCodes ? 6 : 4));
     // An item has a step at least, and a warp's copies are at most kStages - 1 steps ahead: with an item more than that
     // prepared, no warp waits for one that the helpers can only prepare after it has moved on.
     static constexpr int kItems = kStages + 1;
@@ -165,7 +165,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
     using Smem = TokenSmem<D, kFormat, kCols>;
     constexpr bool kCodes = Smem::kCodes;
     constexpr int kRowBytes = Smem::kRowBytes, kMatrixBytes = Smem::kMatrixBytes, kStages = Smem::kStages, kWarps = Smem::kWarps;
-    constexpr int kThreads = (kWarps + kHelpers) * 32, kTile = kKeys * kWarps, kRows = Smem::kRows, kItems = Smem::kItems;
+    constexpr int kThreads = (kWarps + kHelpers) * 32, kKeys = Smem::kKeys, kTile = kKeys * kWarps, kRows = Smem::kRows, kItems = Smem::kItems;
     using Work = SeqWork<kTile, kRows>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     Smem& sm = *reinterpret_cast<Smem*>(smem_raw);
@@ -471,18 +471,18 @@ zl_cached_tokens_kernel(const CachedParams p) {
                     f_pages = p.b.pages + (int64_t)w.s * p.b.max_pages;
                     f_head = (uint64_t)(uint32_t)w.head * p.c.head16;
                     f_scale = (uint64_t)(uint32_t)w.head * (uint32_t)p.c.scale_head;
-                    const int32_t key = f_tile * kTile + warp * kKeys + (lane & 15);
+                    const int32_t key = f_tile * kTile + warp * kKeys + (lane & (kKeys - 1));
                     f_page = key < f_keys ? __ldg(f_pages + (key >> p.c.page_shift)) : -1;
                 }
             }
             if (f_end >= 0) {
                 const int32_t key0 = f_tile * kTile + warp * kKeys;
                 const uint32_t dst = ring + f_stage * Smem::kStageBytes;
-                const int32_t key = key0 + (lane & 15);
+                const int32_t key = key0 + (lane & (kKeys - 1));
                 const int32_t pg = valid_page(p.c, f_page);
                 const uint32_t exists = __ballot_sync(0xffffffffu, pg >= 0);
                 if (++f_tile < f_end) f_page = key + kTile < f_keys ? __ldg(f_pages + ((key + kTile) >> p.c.page_shift)) : -1;
-                if (lane == 0) sm.mask[warp][f_stage] = exists & 0xffffu;
+                if (lane == 0) sm.mask[warp][f_stage] = kKeys == 32 ? exists : exists & 0xffffu;
                 // every lane works out its key's place; the copies of a row take it from there
                 const uint32_t in = key & in_page;
                 const uint64_t at16 = (uint64_t)(uint32_t)pg * p.c.page16 + ((uint64_t)in * p.c.token16 + f_head);
@@ -500,7 +500,12 @@ zl_cached_tokens_kernel(const CachedParams p) {
                     const bool live = pg >= 0;
                     const uint64_t at = (uint64_t)(uint32_t)pg * (uint32_t)p.c.scale_page + ((uint64_t)in * (uint32_t)p.c.scale_token + f_scale);
                     const uint64_t off = live ? at : 0;
-                    cp4(dst + 2 * kMatrixBytes + lane * 4, (lane < 16 ? p.c.k_scale : p.c.v_scale) + off, live);
+                    if constexpr (kKeys == 32) {
+                        cp4(dst + 2 * kMatrixBytes + lane * 4, p.c.k_scale + off, live);
+                        cp4(dst + 2 * kMatrixBytes + 128 + lane * 4, p.c.v_scale + off, live);
+                    } else {
+                        cp4(dst + 2 * kMatrixBytes + lane * 4, (lane < 16 ? p.c.k_scale : p.c.v_scale) + off, live);
+                    }
                 }
             }
             cp_commit();
@@ -556,77 +561,81 @@ zl_cached_tokens_kernel(const CachedParams p) {
                 __syncwarp();
                 fetch();  // into the stage of the step before this one
                 const uint32_t k_addr = ring + st * Smem::kStageBytes + k_at, v_addr = ring + st * Smem::kStageBytes + kMatrixBytes + v_at;
-                // ---- S^T: keys gid and gid + 8, rows 2 quad and 2 quad + 1
-                float c[kCols][4], d[kCols][4];  // even and odd chunks: two chains of sums
+                // ---- S^T: keys gid and gid + 8 of every sixteen, rows 2 quad and 2 quad + 1
+                constexpr int kParts = kKeys / 16;
+                float c[kParts][kCols][4];
 #pragma unroll
-                for (int n = 0; n < kCols; ++n)
+                for (int g = 0; g < kParts; ++g) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) c[n][i] = d[n][i] = 0.f;
-                // (all of a step's keys are fetched ahead of the products, its values ahead of the exponentials: their order is the
-                // program's)
-                uint32_t kv[Smem::kRowBytes / 32][4];
+                    for (int n = 0; n < kCols; ++n) c[g][n][0] = c[g][n][1] = c[g][n][2] = c[g][n][3] = 0.f;
+                    const uint32_t at = k_addr + g * 16 * kRowBytes;
+                    if constexpr (kCodes) {
 #pragma unroll
-                for (int i = 0; i < kRowBytes / 32; ++i) ldm4(kv[i], k_addr ^ (i << 5));
-                if constexpr (kCodes) {
+                        for (int ks = 0; ks < D / 16; ks += 2) {
+                            uint32_t r[4];  // keys 0-7 and 8-15 of chunk ks, the same of chunk ks + 1
+                            ldm4(r, at ^ (ks << 4));
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ks += 2) {
-                        const uint32_t(&r)[4] = kv[ks / 2];  // keys 0-7 and 8-15 of chunk ks, the same of chunk ks + 1
+                            for (int e = 0; e < 2; ++e) {
+                                uint32_t a0, a1, a2, a3;
+                                halves<kFormat>(r[2 * e], a0, a2);
+                                halves<kFormat>(r[2 * e + 1], a1, a3);
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            uint32_t a0, a1, a2, a3;
-                            halves<kFormat>(r[2 * e], a0, a2);
-                            halves<kFormat>(r[2 * e + 1], a1, a3);
+                                for (int n = 0; n < kCols; ++n) {
+                                    uint32_t q0, q1;
+                                    if constexpr (kCols == 1) { q0 = q[ks + e][0]; q1 = q[ks + e][1]; } else load_q(n, ks + e, q0, q1);
+                                    mma16h(c[g][n], a0, a1, a2, a3, q0, q1);
+                                }
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int ks = 0; ks < D / 16; ++ks) {
+                            uint32_t r[4];  // keys 0-7 and 8-15 of chunk 2 ks, the same of chunk 2 ks + 1
+                            ldm4(r, at ^ (ks << 5));
 #pragma unroll
                             for (int n = 0; n < kCols; ++n) {
                                 uint32_t q0, q1;
-                                if constexpr (kCols == 1) { q0 = q[ks + e][0]; q1 = q[ks + e][1]; } else load_q(n, ks + e, q0, q1);
-                                mma16h(e == 0 ? c[n] : d[n], a0, a1, a2, a3, q0, q1);
+                                if constexpr (kCols == 1) { q0 = q[ks][0]; q1 = q[ks][1]; } else load_q(n, ks, q0, q1);
+                                mma16(c[g][n], r[0], r[1], r[2], r[3], q0, q1);
                             }
                         }
                     }
-                } else {
-#pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks) {
-                        const uint32_t(&r)[4] = kv[ks];  // keys 0-7 and 8-15 of chunk 2 ks, the same of chunk 2 ks + 1
-#pragma unroll
-                        for (int n = 0; n < kCols; ++n) {
-                            uint32_t q0, q1;
-                            if constexpr (kCols == 1) { q0 = q[ks][0]; q1 = q[ks][1]; } else load_q(n, ks, q0, q1);
-                            mma16(ks % 2 == 0 ? c[n] : d[n], r[0], r[1], r[2], r[3], q0, q1);
-                        }
-                    }
                 }
-#pragma unroll
-                for (int i = 0; i < kRowBytes / 32; ++i) ldm4t(kv[i], v_addr ^ (i << 5));
                 const int32_t key0 = tile * kTile + warp * kKeys;
                 const uint32_t exists = sm.mask[warp][st];
-                float key_scale[2], value_scale[2], value_log2[2];
+                float key_scale[kParts][2], value_scale[kParts][2], value_log2[kParts][2];
                 if constexpr (kCodes) {
                     const float* sc = reinterpret_cast<const float*>(sm.ring[warp][st] + 2 * kMatrixBytes);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        key_scale[h] = sc[8 * h + gid];
-                        value_scale[h] = fmaxf(sc[kKeys + 8 * h + gid], kLeastScale);
-                        value_log2[h] = __log2f(value_scale[h]);
-                    }
+                    for (int g = 0; g < kParts; ++g)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            key_scale[g][h] = sc[16 * g + 8 * h + gid];
+                            value_scale[g][h] = fmaxf(sc[kKeys + 16 * g + 8 * h + gid], kLeastScale);
+                            value_log2[g][h] = __log2f(value_scale[g][h]);
+                        }
                 }
-                const bool cut = key0 + kKeys > all_see || exists != 0xffffu;
-                uint32_t b[kCols][2];
+                const bool cut = key0 + kKeys > all_see || exists != (kKeys == 32 ? 0xffffffffu : 0xffffu);
+                uint32_t b[kParts][kCols][2];
 #pragma unroll
                 for (int n = 0; n < kCols; ++n) {
+                    float mx[2] = {-INFINITY, -INFINITY};  // what the reference has to follow: scores, or weights of 8-bit values
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) c[n][i] = (c[n][i] + d[n][i]) * (kCodes ? by_row[n][i & 1] * key_scale[i >> 1] : p.scale_log2);
-                    if (cut) {
+                    for (int g = 0; g < kParts; ++g) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int col = gid + 8 * (i >> 1);
-                            if (key0 + col >= sm.seen[place][8 * n + 2 * quad + (i & 1)] || !((exists >> col) & 1)) c[n][i] = -INFINITY;
+                        for (int i = 0; i < 4; ++i) c[g][n][i] *= kCodes ? by_row[n][i & 1] * key_scale[g][i >> 1] : p.scale_log2;
+                        if (cut) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int col = 16 * g + gid + 8 * (i >> 1);
+                                if (key0 + col >= sm.seen[place][8 * n + 2 * quad + (i & 1)] || !((exists >> col) & 1)) c[g][n][i] = -INFINITY;
+                            }
                         }
-                    }
-                    float mx[2];  // what the reference has to follow: scores, or weights of 8-bit values
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        mx[e] = kCodes ? fmaxf(c[n][e] + value_log2[0], c[n][2 + e] + value_log2[1]) : fmaxf(c[n][e], c[n][2 + e]);
+                        for (int e = 0; e < 2; ++e)
+                            mx[e] = kCodes ? max3(mx[e], c[g][n][e] + value_log2[g][0], c[g][n][2 + e] + value_log2[g][1])
+                                           : max3(mx[e], c[g][n][e], c[g][n][2 + e]);
+                    }
                     if (__any_sync(0xffffffffu, mx[0] > m[n][0] + kRescale || mx[1] > m[n][1] + kRescale)) {
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
@@ -646,33 +655,41 @@ zl_cached_tokens_kernel(const CachedParams p) {
                     // ---- P, rounded once for its product with V (bf16, or with the value's scale to fp16); the sums take it unrounded
                     const float ref[2] = {m[n][0] == -INFINITY ? 0.f : m[n][0], m[n][1] == -INFINITY ? 0.f : m[n][1]};
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float x = ex2(c[n][2 * h] - ref[0]), y = ex2(c[n][2 * h + 1] - ref[1]);
-                        l[n][0] += x;
-                        l[n][1] += y;
-                        b[n][h] = transposed(kCodes ? pack_half(x * value_scale[h], y * value_scale[h]) : pack_bf16(x, y));
-                    }
+                    for (int g = 0; g < kParts; ++g)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float x = ex2(c[g][n][2 * h] - ref[0]), y = ex2(c[g][n][2 * h + 1] - ref[1]);
+                            l[n][0] += x;
+                            l[n][1] += y;
+                            b[g][n][h] = transposed(kCodes ? pack_half(x * value_scale[g][h], y * value_scale[g][h]) : pack_bf16(x, y));
+                        }
                 }
                 // ---- O^T += V^T P^T
-                if constexpr (kCodes) {
 #pragma unroll
-                    for (int ch = 0; ch < D / 16; ch += 2) {
-                        const uint32_t(&r)[4] = kv[ch / 2];  // keys 0-7 and 8-15 of chunk ch, the same of chunk ch + 1
+                for (int g = 0; g < kParts; ++g) {
+                    const uint32_t at = v_addr + g * 16 * kRowBytes;
+                    if constexpr (kCodes) {
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {  // even columns of the chunk as rows 0-7, odd ones as rows 8-15
-                            uint32_t a0, a1, a2, a3;
-                            halves_apart<kFormat>(r[2 * e], a0, a1);
-                            halves_apart<kFormat>(r[2 * e + 1], a2, a3);
+                        for (int ch = 0; ch < D / 16; ch += 2) {
+                            uint32_t r[4];  // keys 0-7 and 8-15 of chunk ch, the same of chunk ch + 1
+                            ldm4t(r, at ^ (ch << 4));
 #pragma unroll
-                            for (int n = 0; n < kCols; ++n) mma16h(o[n][ch + e], a0, a1, a2, a3, b[n][0], b[n][1]);
+                            for (int e = 0; e < 2; ++e) {  // even columns of the chunk as rows 0-7, odd ones as rows 8-15
+                                uint32_t a0, a1, a2, a3;
+                                halves_apart<kFormat>(r[2 * e], a0, a1);
+                                halves_apart<kFormat>(r[2 * e + 1], a2, a3);
+#pragma unroll
+                                for (int n = 0; n < kCols; ++n) mma16h(o[n][ch + e], a0, a1, a2, a3, b[g][n][0], b[g][n][1]);
+                            }
                         }
-                    }
-                } else {
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t(&r)[4] = kv[i];  // keys 0-7 of chunks 2 i and 2 i + 1, keys 8-15 of the same
+                        for (int i = 0; i < D / 16; ++i) {
+                            uint32_t r[4];  // keys 0-7 of chunks 2 i and 2 i + 1, keys 8-15 of the same
+                            ldm4t(r, at ^ (i << 5));
 #pragma unroll
-                        for (int n = 0; n < kCols; ++n) mma16(o[n][i], r[0], r[1], r[2], r[3], b[n][0], b[n][1]);
+                            for (int n = 0; n < kCols; ++n) mma16(o[n][i], r[0], r[1], r[2], r[3], b[g][n][0], b[g][n][1]);
+                        }
                     }
                 }
                 st = st + 1 == kStages ? 0 : st + 1;
