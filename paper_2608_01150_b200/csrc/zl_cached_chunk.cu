@@ -360,7 +360,8 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const int row = lane * box;          // this lane's rows of a tile: [row, row + box)
             const bool has_rows = row < kTileKV;
             uint32_t item_cnt = 0, kv_cnt = 0;
-            auto page_of = [&](const Item& w, int32_t pos) { return has_rows && pos < w.keys ? page_at(p.b, p.c, w.s, pos) : -1; };
+            // (entries of the table: what they mean is asked a tile later, when they are there)
+            auto page_of = [&](const Item& w, int32_t pos) { return has_rows && pos < w.keys ? page_entry(p.b, p.c, w.s, pos) : -1; };
             auto load = [&](const Item& w, uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, int32_t pg, int32_t pos) {
                 const uint32_t n = __popc(__ballot_sync(0xffffffffu, pg >= 0));
                 if (lane == 0) mbar_arrive_expect_tx(bar, n * box * (kCodes ? D : D * 2));
@@ -388,7 +389,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             tma_load_4d(sm.q[x] + b * Smem::kBoxBytes, &tm_q, &sm.q_full, b * 64, 0, w.head, w.q0 + w.tok0 + x * tile_tokens);
                 }
                 {  // K runs one tile ahead of V
-                    int32_t pg_k = page_of(w, w.tile0 * kTileKV + row), pg_v = -1;
+                    int32_t pg_k = valid_page(p.c, page_of(w, w.tile0 * kTileKV + row)), pg_v = -1;
                     for (int j = 0; j <= n; ++j) {
                         const int32_t key0 = (w.tile0 + j) * kTileKV;
                         const int32_t pg_next = j + 1 < n ? page_of(w, key0 + kTileKV + row) : -1;
@@ -415,7 +416,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             load(w, sm.v[st], &tm_v, kCodes ? &sm.v_codes[st] : &sm.v_full[st], pg_v, key0 - kTileKV + row);
                         }
                         pg_v = pg_k;
-                        pg_k = pg_next;
+                        pg_k = valid_page(p.c, pg_next);
                     }
                     kv_cnt += n;
                 }
@@ -575,7 +576,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             const uint32_t to = (ch >> 2) * Smem::kBoxBytes + r * 128;
             const uint32_t to0 = to + (((2 * (ch & 3) + (swap ? 1 : 0)) ^ (r & 7)) << 4), to1 = to0 ^ 16;
             uint32_t kv_cnt = 0, read_cnt = 0, item_cnt = 0;
-            auto page_of = [&](const Item& w, int32_t key) { return key < w.keys ? page_at(p.b, p.c, w.s, key) : -1; };
+            auto page_of = [&](const Item& w, int32_t key) { return key < w.keys ? page_entry(p.b, p.c, w.s, key) : -1; };
             // scales of this thread's key (key t of the tile), zeros without one
             auto scales_of = [&](const Item& w, int32_t key, int32_t pg) {
                 float2 r = make_float2(0.f, 0.f);
@@ -624,7 +625,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 }
                 // pages are looked up two tiles ahead, scales one: neither is waited for
                 const int32_t key0 = w.tile0 * kTileKV + t;
-                int32_t pg = page_of(w, key0), pg_next = page_of(w, key0 + kTileKV);
+                int32_t pg = valid_page(p.c, page_of(w, key0)), pg_next = page_of(w, key0 + kTileKV);
                 float2 sc = scales_of(w, key0, pg);
                 for (int j = 0; j <= n; ++j) {
                     for (int m = 0; m < 2; ++m) {
@@ -639,7 +640,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             if (lane == 0) sm.mask[c % kMaskRing][t >> 5] = word;
                             __syncwarp();
                             mbar_arrive(&sm.tile_full[c % kMaskRing]);
-                            pg = pg_next;
+                            pg = valid_page(p.c, pg_next);
                             sc = scales_of(w, key0 + (j + 1) * kTileKV, pg);
                             pg_next = page_of(w, key0 + (j + 2) * kTileKV);
                         }
