@@ -99,9 +99,18 @@ struct Geometry {
 struct SeqLine {
     SeqView v;
     int32_t blocks;
+    int32_t by_prefix, by_prefix_until, by_order_until;  // keys that blocks before by_prefix_until see; blocks after by_order_until see all
     __device__ __forceinline__ SeqLine(const CachedParams& p, const Geometry& g, int s) : v(load_seq(p.b, p.c.page_shift, s)) {
-        blocks = (v.q_len + 2 * g.tokens - 1) / (2 * g.tokens);
+        const uint32_t T = 2 * g.tokens;
+        blocks = (int32_t)((uint32_t)v.q_len / T + ((uint32_t)v.q_len % T != 0));
         if ((int64_t)v.q_len * p.group <= g.rest_rows) blocks = 0;
+        by_prefix = min(v.keys, max(v.prefix, 0));
+        by_prefix_until = by_order_until = blocks;
+        if (by_prefix < v.keys) {  // (differences of numbers of 31 bits and a sign: they fit 32 bits without one)
+            by_prefix_until = by_prefix < v.pos0 ? 0 : (int32_t)min((uint32_t)blocks, ((uint32_t)by_prefix - (uint32_t)v.pos0) / T);
+            by_order_until = v.keys < v.pos0 ? by_prefix_until
+                                             : max(by_prefix_until, (int32_t)min((uint32_t)blocks, ((uint32_t)v.keys - (uint32_t)v.pos0) / T));
+        }
     }
     __device__ __forceinline__ int32_t block_tokens(const Geometry& g, int b) const { return min(2 * g.tokens, v.q_len - b * 2 * g.tokens); }
     __device__ __forceinline__ int32_t block_keys(const Geometry& g, int b) const {
@@ -112,13 +121,7 @@ struct SeqLine {
     }
     // Cost of blocks 0 .. b - 1 for one head, all of them full: kTwoCost times the sum of min(keys, max(prefix, pos0 + (i + 1) T)).
     __device__ __forceinline__ int64_t cost_before(const Geometry& g, int b) const {
-        const int32_t T = 2 * g.tokens;
-        const int64_t by_prefix = min(v.keys, max(v.prefix, 0));
-        int64_t i0 = b, i1 = b;  // blocks bound by the prefix, by the order or the prefix
-        if (by_prefix < v.keys) {
-            i0 = by_prefix < v.pos0 ? 0 : min((int64_t)b, quotient(by_prefix - v.pos0, T));
-            i1 = v.keys < v.pos0 ? i0 : max(i0, min((int64_t)b, quotient((int64_t)v.keys - v.pos0, T)));
-        }
+        const int64_t T = 2 * g.tokens, i0 = min(b, by_prefix_until), i1 = min(b, by_order_until);
         const int64_t keys = i0 * by_prefix + (i1 - i0) * v.pos0 + (i1 * (i1 + 1) - i0 * (i0 + 1)) / 2 * T + (b - i1) * (int64_t)v.keys;
         return (int64_t)b * kItemCost + kTwoCost * keys;
     }
