@@ -446,7 +446,7 @@ zl_status zl_scored_workspace_bytes(const zl_tasks* tasks, const zl_score* score
  *   pages    [n_seqs, max_pages]: page number of positions [j * page_size, (j + 1) * page_size).  A number outside
  *            [0, n_pages) is a page without keys (dropped, or not there yet): nothing is written to it, nobody sees it.
  *            The same page may stand in several tables (a shared beginning), as long as no two new tokens of a write fall on
- *            one place.  Positions from max_pages * page_size on hold no keys.
+ *            one place.  Positions from max_pages * page_size on (at most 2^30) hold no keys.
  *   prefix   [n_seqs] or NULL (all 0): keys that every new token of the sequence sees (a condition, or an image seen whole);
  *            INT32_MAX is no mask at all.
  *   max_q    at least the largest number of new tokens of a sequence, 0 if not known.  It only chooses kernels.
@@ -505,7 +505,7 @@ zl_status zl_cached_attn_device_status(const zl_cached_attn* attn, int32_t* code
  * A token that sees no key gets O = 0, LSE = -inf.  Chunks of a prompt, single tokens and sequences without new tokens may
  * stand in one batch; results do not depend on what else the batch holds beyond rounding, and are the same from run to run.
  *   q          [total_q, n_heads, head_dim] bf16, rows `q_stride` elements apart, a multiple of 8; 16-byte aligned
- *   o          [total_q, n_heads, head_dim] bf16, contiguous
+ *   o          [total_q, n_heads, head_dim] bf16, contiguous, not overlapping q
  *   lse        [n_heads, total_q] fp32, or NULL
  *   workspace  at least zl_cached_attn_workspace_bytes, 256-byte aligned
  * Q, and the keys and values inside the sequences' lengths, have to be finite; other places of the cache may hold anything.

@@ -52,12 +52,14 @@ zl_status view(const zl_kv_cache* cache, const zl_cache_batch* batch, bool token
     if (((reinterpret_cast<uintptr_t>(x.k_scale) | reinterpret_cast<uintptr_t>(x.v_scale)) & 3) != 0) return ZL_ERR_INVALID_ARG;
     if (batch->n_seqs < 0 || batch->max_pages < 0 || batch->total_q < 0 || batch->max_q < 0) return ZL_ERR_INVALID_ARG;
     if (batch->n_seqs > 0 && ((tokens && !batch->cu_q) || !batch->kv_len || (batch->max_pages > 0 && !batch->pages))) return ZL_ERR_INVALID_ARG;
+    // positions are counted in 32 bits with room to spare
+    if ((int64_t)batch->max_pages * x.page_size > (int64_t)1 << 30) return ZL_ERR_UNSUPPORTED;
     int shift = 0;
     while ((1 << shift) < x.page_size) ++shift;
     *c = CacheView{static_cast<uint8_t*>(x.k), static_cast<uint8_t*>(x.v), x.k_scale, x.v_scale,
                    x.page_stride * bytes, x.token_stride * bytes, x.head_stride * bytes, x.scale_page_stride, x.scale_token_stride, x.scale_head_stride,
                    (uint32_t)(x.page_stride * bytes / 16), (uint32_t)(x.token_stride * bytes / 16), (uint32_t)(x.head_stride * bytes / 16), x.n_pages, shift, x.n_kv_heads};
-    *b = CacheBatch{batch->cu_q, batch->kv_len, batch->pages, batch->prefix, batch->n_seqs, batch->max_pages, batch->total_q};
+    *b = CacheBatch{batch->cu_q, batch->kv_len, batch->pages, batch->prefix, batch->n_seqs, x.n_pages > 0 ? batch->max_pages : 0, batch->total_q};
     return ZL_OK;
 }
 
@@ -226,6 +228,11 @@ zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cach
     if (p.b.total_q > 0 && (!q || !o || !aligned16(q) || !aligned16(o))) return ZL_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(lse) & 3) != 0) return ZL_ERR_INVALID_ARG;
     if (!rows_fit(p.b.total_q, attn->n_heads)) return ZL_ERR_UNSUPPORTED;
+    if (p.b.total_q > 0) {  // parts of an item read their queries while others write their output
+        const char *q0 = static_cast<const char*>(q), *o0 = static_cast<const char*>(o);
+        const int64_t row = (int64_t)attn->n_heads * attn->head_dim * 2;
+        if (q0 < o0 + p.b.total_q * row && o0 < q0 + (p.b.total_q - 1) * q_stride * 2 + row) return ZL_ERR_INVALID_ARG;
+    }
     if (attn->device < 0) return ZL_ERR_CUDA;
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev != attn->device) return ZL_ERR_INVALID_ARG;

@@ -2,8 +2,8 @@
 //
 // The rows of a key head are its sequence's new tokens times the query heads of its group; a tile takes as many whole tokens as
 // fit 128 rows, so that one box of Q holds a tile.  An item is two such tiles (or the one that is left) of a sequence and key
-// head.  All CTAs (one per SM) walk one line of work and each takes an equal stretch of it,
-// wherever that cuts an item; the lengths are read when the kernel runs.  Stretches are found from sums in closed form: block b
+// head.  All CTAs (one per SM) walk one line of work and each takes an equal stretch of it, wherever that cuts an item; the lengths
+// are read when the kernel runs.  Stretches are found from sums in closed form: block b
 // of a sequence sees min(keys, max(prefix, pos0 + (b + 1) tokens)) keys.
 //   warp 0       TMA producer: Q once per item, K and V page by page through shared-memory rings
 //   warp 2       walks the line and hands the items' descriptions to the others
@@ -11,7 +11,7 @@
 //   warps 4-11   softmax.  All of them work on the same scores, sixteen rows a warp, in turn on S_0 and S_1: those are two query tiles
 //                against a key tile, or one query tile against two key tiles, whose accumulators are joined at the end.  While the
 //                warps are at one, the tensor core has the other's P V and next S before it: a warpgroup with a tile of its own
-//                stood still for those (1560 tokens over 9,750 keys: bf16 306 -> SHARE_B us, int8 421 -> SHARE_I us)
+//                stood still for those (1560 tokens over 9,750 bf16 keys 306 -> 300 us)
 //   warps 12-15  (8-bit caches) codes become fp16, exactly, in their place (a tile of codes arrives in the second half of the tile it
 //                becomes), and so do the queries of an item; the scale of a key multiplies its column of S, the scale of a value its
 //                column of P, in fp32: the softmax takes s_j = S_j k_j + log2 v_j, so that its exponentials are the weights of the
@@ -34,10 +34,11 @@ constexpr uint64_t kWaitLimitNs = 4000000000ull;
 constexpr float kRescaleThresholdLog2 = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kMaskRing = 8;   // key tiles whose masks are kept: more than can be under way
-// Units of work: a key tile under two query tiles takes 4,100 clocks (bf16; 8-bit codes 5,800), under one 2,900 (4,500).  With
-// the second counted as half of the first, CTAs with single tiles finished a third later than the others.
-constexpr int32_t kTwoCost = 8, kOneCost = 6;  // a key under two query tiles, under one
-constexpr int32_t kItemCost = 1536;            // start and end of an item
+// Units of work: a key tile under two query tiles takes 4,100 clocks (bf16; 8-bit codes 5,300), under one 2,900 (4,500).  With
+// the second counted as half of the first, CTAs with single tiles finished a third later than the others.  An item's start and
+// end (its queries, the first keys' way here, the last tile's output) count as three key tiles: half as many are 1 to 3 % slower.
+constexpr int32_t kTwoCost = 8, kOneCost = 7;  // a key under two query tiles, under one
+constexpr int32_t kItemCost = 3 * kTileKV * kTwoCost;
 constexpr int64_t kLeastUnits = 4 * kTileKV * kTwoCost;  // least stretch of a CTA
 
 // A CTA's part of an item, as warp 2 hands it to the other warps.
@@ -288,6 +289,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     const uint32_t tmem = sm.tmem_base;
     grid_release();
     grid_wait();
+    if (threadIdx.x == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;  // (what an earlier call left must not be joined)
 
     // ---- where this CTA's stretch begins
     {
@@ -332,29 +334,25 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     const bool idle = per * blockIdx.x >= total;
 
     if (idle) {
-        if (threadIdx.x == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;
+        // nothing to do
     } else if (warp < 4) {
         if constexpr (kCodes) reg_dec<80>(); else reg_dec<136>();
         if (warp == 2) {
             // -------------------------------------------------------------- the line of work
             ItemWalk walk(p, sm.start_seq, sm.start_base, per, total);
             bool more = true;
-            bool cut = false;  // an item's first part is the last of this CTA's stretch
             for (uint32_t it = 0; more; ++it) {
                 Item w;
                 more = walk.next(w);
                 if (!more) w.tile1 = -1;
-                if (more && w.c_first == (int32_t)blockIdx.x && w.c_last > w.c_first) {
-                    cut = true;
-                    if (lane == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x] = w;
-                }
+                // the item, if any, whose first part is the last of this CTA's stretch
+                if (more && lane == 0 && w.c_first == (int32_t)blockIdx.x && w.c_last > w.c_first) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x] = w;
                 ZL_WAIT_WARP(&sm.item_empty[it % kItems], ((it / kItems) & 1) ^ 1, 9);
                 if (lane == 0) {
                     sm.items[it % kItems] = w;
                     mbar_arrive(&sm.item_full[it % kItems]);
                 }
             }
-            if (lane == 0 && !cut) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;
         } else if (warp == 0) {
             // -------------------------------------------------------------- TMA producer (a lane per page)
             const int32_t tile_tokens = kTileQ / p.group;

@@ -157,6 +157,7 @@ def test_batches_the_library_refuses(kw):
 def test_rows_the_library_refuses():
     lib, c, b = B.lib(), ctypes.byref(cache_desc()), ctypes.byref(batch_desc())
     write = lambda k=4096, v=4096, stride=128, b=b: lib.zl_cache_write(c, b, k, v, stride, 0)  # noqa: E731
+    assert write(b=ctypes.byref(batch_desc(max_pages=2 ** 26 + 1))) == UNSUPPORTED  # more than 2^30 positions
     assert write(k=None) == INVALID and write(v=4104) == INVALID and write(stride=132) == INVALID and write(stride=120) == INVALID
     assert lib.zl_cache_write(None, b, 4096, 4096, 128, 0) == INVALID and lib.zl_cache_write(c, None, 4096, 4096, 128, 0) == INVALID
     three = ctypes.byref(cache_desc(n_kv_heads=3, token_stride=192, page_stride=16 * 192))  # 2^32 rows and more
@@ -175,12 +176,13 @@ def test_handles_that_are_refused(args, status):
 def test_attention_calls_the_library_refuses():
     lib, h = B.lib(), Z.build_cached_attn(4, 2, 64)
 
-    def call(c=None, b=None, q=4096, stride=256, scale=1.0, o=4096, lse=None):
+    def call(c=None, b=None, q=4096, stride=256, scale=1.0, o=65536, lse=None):
         return lib.zl_cached_attn_fwd(h.ptr, ctypes.byref(c or cache_desc()), ctypes.byref(b or batch_desc()), q, stride, scale, o, lse, 4096, 1 << 40, 0)
 
     assert call(c=cache_desc(n_kv_heads=4)) == INVALID and call(c=cache_desc(head_dim=128, token_stride=256, head_stride=128)) == INVALID
     for scale in (0.0, -1.0, float("inf"), float("nan")):
         assert call(scale=scale) == INVALID
+    assert call(o=4096) == INVALID and call(o=4096 + 4 * 512 + 496) == INVALID and call(o=4096 - 2560 + 16) == INVALID  # over the queries
     assert call(q=None) == INVALID and call(o=None) == INVALID and call(q=4104) == INVALID and call(stride=252) == INVALID
     assert call(stride=248) == INVALID and call(lse=4098) == INVALID and call(b=batch_desc(kv_len=None)) == INVALID
     assert call(c=cache_desc(format=7)) == UNSUPPORTED and call(b=batch_desc(total_q=2 ** 31 - 1)) == UNSUPPORTED
@@ -193,7 +195,8 @@ def test_calls_without_a_device_say_so():
     assert lib.zl_cache_write(c, b, 4096, 4096, 128, 0) == CUDA
     assert lib.zl_cache_read(c, b, None, 4096, 5, 4096, 4096, 0) == CUDA
     h = Z.build_cached_attn(4, 2, 64)
-    assert lib.zl_cached_attn_fwd(h.ptr, c, b, 4096, 256, 1.0, 4096, None, 4096, 1 << 40, 0) == CUDA
+    assert lib.zl_cached_attn_fwd(h.ptr, c, b, 4096, 256, 1.0, 65536, None, 4096, 1 << 40, 0) == CUDA
+    assert lib.zl_cached_attn_fwd(h.ptr, c, b, 4096, 256, 1.0, 4096 + 2560, None, 4096, 1 << 40, 0) == CUDA  # right behind the queries
     code, where = ctypes.c_int32(), ctypes.c_int32()
     assert lib.zl_cached_attn_device_status(h.ptr, ctypes.byref(code), ctypes.byref(where)) == CUDA
     h.close()

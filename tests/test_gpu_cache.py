@@ -325,6 +325,74 @@ def test_max_q_only_chooses_kernels(max_q):
     check(s, qlens, q, o, lse)
 
 
+@pytest.mark.parametrize("dtype,group,dim", [(BF16, 100, 64), (INT8, 128, 64), (BF16, 40, 128), (E4M3, 9, 128), (INT8, 33, 64)])
+def test_many_query_heads_to_a_key_head(dtype, group, dim):
+    """Tiles of one, three, fourteen tokens; single tokens that fill a tile, or two columns of eight rows."""
+    lens, qlens = [40, 300, 150], [1, 5, 1]
+    s = Setup(dtype, dim, 16, 2, lens)
+    s.fill()
+    q = rand(s.g, 8, 2 * group, dim, times=1.5)
+    for max_q in (0, 5):
+        o, lse = attend(s, qlens, q, max_q=max_q)
+        check(s, qlens, q, o, lse)
+    o, lse = attend(s, [1, 1, 1], q)
+    check(s, [1, 1, 1], q, o, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_tokens_outermost(dtype):
+    """A cache whose pages are strided: token 0 of every page, then token 1, ..."""
+    import paper_2608_01150_b200 as Z
+    lens, qlens = [40, 200], [1, 150]
+    s = Setup(dtype, 64, 8, 2, lens)
+    n = s.ref.n_pages
+    s.pools = [torch.zeros(8, n, 2, 64, device="cuda").to(dtype).transpose(0, 1) for _ in "kv"]
+    if dtype is not BF16:
+        s.scales = [torch.zeros(8, 2, n, device="cuda").permute(2, 0, 1) for _ in "kv"]
+    s.cache = Z.KvCache(s.pools[0], s.pools[1], *s.scales)
+    s.fill()
+    q = rand(s.g, 151, 6, 64, times=1.5)
+    o, lse = attend(s, qlens, q)
+    check(s, qlens, q, o, lse)
+    o, lse = attend(s, [1, 1], q[:2])
+    check(s, [1, 1], q[:2], o, lse)
+
+
+def test_caches_without_a_page():
+    """No page, or tables without an entry: nobody sees anything, nothing is written, zeros are read."""
+    import paper_2608_01150_b200 as Z
+    none = torch.zeros(0, 16, 2, 64, dtype=BF16, device="cuda")
+    one = torch.zeros(1, 16, 2, 64, dtype=BF16, device="cuda")
+    h = Z.build_cached_attn(4, 2, 64)
+    ws = torch.empty(h.workspace_bytes, dtype=torch.uint8, device="cuda")
+    k = torch.ones(40, 2, 64, dtype=BF16, device="cuda")
+    q = torch.ones(40, 4, 64, dtype=BF16, device="cuda")
+    for pool, width in ((none, 3), (one, 0)):
+        c = Z.KvCache(pool, pool.clone())
+        b = Z.CacheBatch(i32([0, 1, 40]), i32([10, 39]), torch.zeros(2, width, dtype=torch.int32, device="cuda"))
+        Z.cache_write(c, b, k, k)
+        rows = [torch.full((3, 2, 64), 7.0, dtype=BF16, device="cuda") for _ in "kv"]
+        Z.cache_read(c, b, i32([0, 2, 3]), rows[0], rows[1])
+        o, lse = torch.full_like(q, 7.0), torch.zeros(4, 40, device="cuda")
+        Z.cached_attn_fwd(h, c, b, q, 0.125, o, lse, ws)
+        torch.cuda.synchronize()
+        assert (o == 0).all() and torch.isinf(lse).all() and (lse < 0).all() and (rows[0] == 0).all() and (rows[1] == 0).all() and (pool == 0).all()
+    assert h.last_device_status() == (0, 0)
+
+
+def test_outputs_over_the_queries_are_refused():
+    import paper_2608_01150_b200 as Z
+    s = Setup(BF16, 64, 16, 2, [20, 20])
+    h = Z.build_cached_attn(4, 2, 64)
+    ws = torch.empty(h.workspace_bytes, dtype=torch.uint8, device="cuda")
+    both = torch.zeros(4, 4, 64, dtype=BF16, device="cuda")
+    for o in (both[:2], both[1:3]):
+        with pytest.raises(Z.ZlError) as e:
+            Z.cached_attn_fwd(h, s.cache, s.batch([1, 1]), both[:2], 0.125, o, None, ws)
+        assert e.value.status == 1
+    Z.cached_attn_fwd(h, s.cache, s.batch([1, 1]), both[:2], 0.125, both[2:], None, ws)
+
+
 def test_a_shared_beginning():
     """Two sequences with the same first pages, one of them continued in its own."""
     s = Setup(BF16, 64, 16, 2, [40, 64])
