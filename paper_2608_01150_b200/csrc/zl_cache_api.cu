@@ -271,11 +271,13 @@ zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cach
         if (!make_maps(*cache, p, &tq, &tk, &tv)) return ZL_ERR_CUDA;
         if (launch_cached_chunk(attn->head_dim, cache->format, tq, tk, tv, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
         count_launch();
-        if (launch_cached_join(attn->head_dim, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
+    }
+    if (!chunk || p.split) {  // (next behind the other: it starts before that has ended)
+        if (launch_cached_tokens(attn->head_dim, cache->format, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
         count_launch();
     }
-    if (!chunk || p.split) {
-        if (launch_cached_tokens(attn->head_dim, cache->format, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
+    if (chunk) {
+        if (launch_cached_join(attn->head_dim, p, attn->n_sms, cs) != cudaSuccess) return ZL_ERR_CUDA;
         count_launch();
     }
     return ZL_OK;

@@ -287,8 +287,9 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem_base;
-    grid_release();
+    // (in this order: the tokens kernel behind it starts on the strength of what this grid has waited for)
     grid_wait();
+    grid_release();
     if (threadIdx.x == 0) reinterpret_cast<Item*>(p.chunk_cut)[blockIdx.x].tile1 = -1;  // (what an earlier call left must not be joined)
 
     // ---- where this CTA's stretch begins

@@ -182,7 +182,10 @@ zl_cached_tokens_kernel(const CachedParams p) {
         fence_mbar_init();
     }
     grid_release();
-    grid_wait();
+    // Behind the chunk kernel, whose CTAs release this grid when all that came before them has completed, it begins on SMs that have
+    // no more chunks: neither reads what the other writes.  It waits at its end instead, so that its own end means that of both.
+    const bool behind = p.split != 0;
+    if (!behind) grid_wait();
 
     // ---- this CTA's stretch [begin, end) of the line, and the sequence that `begin` lies in
     int64_t begin, end, per;
@@ -218,7 +221,10 @@ zl_cached_tokens_kernel(const CachedParams p) {
         per = max(quotient(total + gridDim.x - 1, gridDim.x), min((int64_t)longest, kLeastUnits));
         begin = per * blockIdx.x;
         end = min(begin + per, total);
-        if (begin >= end) return;
+        if (begin >= end) {
+            if (behind) grid_wait();
+            return;
+        }
         int64_t at = before + upto - mine;
         if (at <= begin && begin < at + mine) {  // one thread
             int s = tid * chunk;
@@ -725,6 +731,7 @@ zl_cached_tokens_kernel(const CachedParams p) {
 
 teardown:
     cp_wait<0>();
+    if (behind) grid_wait();
 }
 
 template <int D, int kFormat, int kCols>

@@ -393,6 +393,35 @@ def test_outputs_over_the_queries_are_refused():
     Z.cached_attn_fwd(h, s.cache, s.batch([1, 1]), both[:2], 0.125, both[2:], None, ws)
 
 
+@pytest.mark.parametrize("dtype", [BF16, INT8])
+def test_calls_one_behind_the_other(dtype):
+    """Writes and attention of chunks beside single tokens, each call needing the one before it and writing over what that has read:
+    the same without a pause as with one behind every call."""
+    import paper_2608_01150_b200 as Z
+    qlens = [300, 1, 1, 40, 1, 1, 1, 1]
+    s = Setup(dtype, 128, 16, 4, [1200, 3000, 40, 900, 2000, 17, 2500, 600])
+    s.fill()
+    n, heads, steps = sum(qlens), 8, 12
+    k, v, q = (rand(s.g, steps, n, h, 128, times=1.5).cuda() for h in (4, 4, heads))
+    h = Z.build_cached_attn(heads, 4, 128)
+    ws = torch.empty(h.workspace_bytes, dtype=torch.uint8, device="cuda")
+    b = s.batch(qlens)
+    outs = []
+    for pause in (True, False):
+        o = torch.zeros(steps, n, heads, 128, dtype=BF16, device="cuda")
+        torch.cuda.synchronize()
+        for i in range(steps):
+            Z.cache_write(s.cache, b, k[i], v[i])
+            if pause:
+                torch.cuda.synchronize()
+            Z.cached_attn_fwd(h, s.cache, b, q[0] if i == 0 else o[i - 1], 128 ** -0.5, o[i], None, ws)  # (reads what the last call wrote)
+            if pause:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        outs.append(o)
+    assert h.last_device_status() == (0, 0) and torch.equal(outs[0], outs[1])
+
+
 def test_a_shared_beginning():
     """Two sequences with the same first pages, one of them continued in its own."""
     s = Setup(BF16, 64, 16, 2, [40, 64])
