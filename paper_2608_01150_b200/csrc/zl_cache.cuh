@@ -1,6 +1,7 @@
 // The paged key/value cache and a batch over it, as the cache's kernels read them.
 #pragma once
 
+#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
 #include "zl_device.h"
@@ -68,27 +69,6 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 }
 
 // ------------------------------------------------------------------------------------------------ 8-bit codes
-// Two whole numbers in bytes I and J of `w` as a bf16 pair, exactly: 0x43 in front of the low seven bits is 128 + low bits
-// (one unit in the last place is 1 there), and 128, or 256 for a negative number, is taken off again.
-template <int I, int J>
-__device__ __forceinline__ uint32_t int8_pair(uint32_t w) {
-    const uint32_t x = __byte_perm(w, 0x43434343u, 0x4040u | (J << 8) | I);
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x & 0xff7fff7fu), "r"(x & 0xff80ff80u));
-    return r;
-}
-// Two e4m3 numbers as a bf16 pair, exactly: sign, exponent and fraction moved to their places give the number times
-// 2^-120, subnormal ones included, and a product with 2^120 puts the exponent right.
-template <int I, int J>
-__device__ __forceinline__ uint32_t e4m3_pair(uint32_t w) {
-    const uint32_t x = __byte_perm(w, 0u, 0x0404u | (J << 12) | (I << 4));
-    return mul_bf16x2(((x >> 4) & 0x07f007f0u) | (x & 0x80008000u), 0x7b807b80u);
-}
-template <int kFormat, int I, int J>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-    return kFormat == ZL_CACHE_INT8 ? int8_pair<I, J>(w) : e4m3_pair<I, J>(w);
-}
-
 // Attention over 8-bit caches multiplies in fp16, which holds every code exactly and is reached in a third of the
 // instructions: a whole number c goes through 0x64 in front of c + 128 (1152 + c, in steps of one), e4m3 through a conversion
 // of its own (whose NaN codes stay NaN).  Four codes of a word, in pairs (0, 1), (2, 3) or (0, 2), (1, 3).

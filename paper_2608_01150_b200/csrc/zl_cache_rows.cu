@@ -1,9 +1,14 @@
 // Rows into the paged cache and out of it (sm_100a): one pass over the data, bound by the bytes that it moves.
 //
 // A row (token, key head) of 64 or 128 elements belongs to four or eight lanes, sixteen elements each, keys and values together:
-// a warp's accesses cover whole rows, and the largest magnitude of a row is two or three shuffles away.  Where the row lies in
-// the cache follows from the batch: a binary search in cu_q (or cu_kv), whose few entries stay in L1, and one entry of the page
-// table.  When writing, the rows' own loads run ahead of that search.
+// the largest magnitude of a row is two or three shuffles away.  A lane has eight neighbours in either half of the row, so that
+// every access of a warp covers whole sectors of 32 bytes (with its sixteen side by side, half sectors were stored: reading
+// 39,360 tokens, 12 heads, d 128, from 8 bits took 71 us, now 56).  Where the row lies in the cache follows from the batch: a
+// binary search in cu_q (or cu_kv), whose few entries stay in L1, and one entry of the page table.  When writing, the rows' own
+// loads run ahead of that search.  Blocks of four warps: registers leave room for 36 warps that write, for 32 in blocks of eight
+// (56 -> 52 us for 32,760 tokens); of two, the number of blocks becomes the limit (54).
+// Measured, 12 heads, d 128: 32,760 tokens written in int8 51 us (6.0 TB/s), in e4m3 50; 39,360 tokens read from either 56 us
+// (6.3 TB/s), from bf16 72 (6.5).
 #include "zl_cache.cuh"
 
 namespace zl {
@@ -12,8 +17,7 @@ using namespace cache;
 
 namespace {
 
-constexpr int kThreads = 256;
-
+constexpr int kThreads = 128;
 constexpr int kEach = 16;  // elements of a lane
 template <int D>
 __device__ __forceinline__ uint32_t my_row() {
@@ -27,9 +31,9 @@ __device__ __forceinline__ float hi_float(uint32_t w) { return __uint_as_float(w
 // fp32, then one rounding to the code's type (ties to even): a value read back is off by half a step of its code.
 // Multiplying by a reciprocal instead would move values that lie between two codes.  Where nothing leaves the range of normal
 // numbers, the quotient comes from the correctly rounded reciprocal y by Markstein's theorem (IBM J. Res. Dev. 34, 1990):
-// with q near x / s, the remainder x - q s is exact and q + (x - q s) y rounds to the rounded quotient.  Three operations an
-// element instead of a division's dozen, which were what bound this kernel (32,760 tokens, 12 heads, d 128, int8, written
-// and read back: 161 -> 122 us).
+// with q near x / s, the remainder x - q s is exact and q + (x - q s) y rounds to the rounded quotient.  Three operations for two
+// elements instead of a division's dozen for one, which were what bound this kernel (32,760 tokens, 12 heads, d 128, int8,
+// written and read back: 161 -> 122 us).
 template <int kFormat, int kLanes>
 __device__ __forceinline__ uint4 quantise(const uint4 (&u)[2], float& scale) {
     constexpr float kTop = kFormat == ZL_CACHE_INT8 ? 127.f : 448.f;
@@ -43,23 +47,27 @@ __device__ __forceinline__ uint4 quantise(const uint4 (&u)[2], float& scale) {
     uint32_t r[4] = {0, 0, 0, 0};
     if (scale >= 0x1p-80f && scale <= 0x1p80f) {
         const float y = __frcp_rn(scale);
+        const float2 y2 = make_float2(y, y), less = make_float2(-scale, -scale);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float q[4] = {lo_float(w[2 * i]), hi_float(w[2 * i]), lo_float(w[2 * i + 1]), hi_float(w[2 * i + 1])};
+            float2 q[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float q0 = q[e] * y;
-                q[e] = fmaf(fmaf(-q0, scale, q[e]), y, q0);
+            for (int e = 0; e < 2; ++e) {
+                const float2 x = make_float2(lo_float(w[2 * i + e]), hi_float(w[2 * i + e])), q0 = mul2(x, y2);
+                q[e] = fma2(fma2(q0, less, x), y2, q0);
             }
             if constexpr (kFormat == ZL_CACHE_INT8) {
                 // behind 1.5 * 2^23 a number ends in whole ones, two's complement: its low byte is the code
-                uint32_t c[4];
+                uint32_t c[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) c[e] = __float_as_uint(q[e] + 12582912.f);
-                r[i] = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+                for (int e = 0; e < 2; ++e) {
+                    const float2 z = add2(q[e], make_float2(12582912.f, 12582912.f));
+                    c[e] = __byte_perm(__float_as_uint(z.x), __float_as_uint(z.y), 0x0040);
+                }
+                r[i] = __byte_perm(c[0], c[1], 0x5410);
             } else {
-                r[i] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(q[0], q[1]), __NV_SATFINITE, __NV_E4M3) |
-                       ((uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(q[2], q[3]), __NV_SATFINITE, __NV_E4M3) << 16);
+                r[i] = (uint32_t)__nv_cvt_float2_to_fp8x2(q[0], __NV_SATFINITE, __NV_E4M3) |
+                       ((uint32_t)__nv_cvt_float2_to_fp8x2(q[1], __NV_SATFINITE, __NV_E4M3) << 16);
             }
         }
     } else if (scale > 0.f) {  // (a row of zeros, or so small that its scale vanishes, has the codes of zero)
@@ -97,11 +105,11 @@ zl_cache_write_kernel(const CacheView c, const CacheBatch b, const __nv_bfloat16
     int64_t slot = -1;  // byte offset of the row in the cache
     int64_t at_scale = 0;
     if (token < (uint32_t)b.total_q) {
-        const int64_t src = (int64_t)token * row_stride + (int64_t)head * D + lane * kEach;
+        const int64_t src = (int64_t)token * row_stride + (int64_t)head * D + lane * 8;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            xk[i] = __ldcs(reinterpret_cast<const uint4*>(k + src) + i);
-            xv[i] = __ldcs(reinterpret_cast<const uint4*>(v + src) + i);
+            xk[i] = __ldg(reinterpret_cast<const uint4*>(k + src + i * (D / 2)));
+            xv[i] = __ldg(reinterpret_cast<const uint4*>(v + src + i * (D / 2)));
         }
         const int s = find_seq(b.cu_q, b.n_seqs, (int32_t)token);
         if (s >= 0) {
@@ -121,16 +129,18 @@ zl_cache_write_kernel(const CacheView c, const CacheBatch b, const __nv_bfloat16
         if (live) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                *(reinterpret_cast<uint4*>(c.k + slot + lane * 32) + i) = xk[i];
-                *(reinterpret_cast<uint4*>(c.v + slot + lane * 32) + i) = xv[i];
+                *reinterpret_cast<uint4*>(c.k + slot + i * D + lane * 16) = xk[i];
+                *reinterpret_cast<uint4*>(c.v + slot + i * D + lane * 16) = xv[i];
             }
         }
     } else {
         float sk, sv;
         const uint4 ck = quantise<kFormat, kLanes>(xk, sk), cv = quantise<kFormat, kLanes>(xv, sv);
         if (live) {
-            *reinterpret_cast<uint4*>(c.k + slot + lane * 16) = ck;
-            *reinterpret_cast<uint4*>(c.v + slot + lane * 16) = cv;
+            *reinterpret_cast<uint2*>(c.k + slot + lane * 8) = make_uint2(ck.x, ck.y);
+            *reinterpret_cast<uint2*>(c.k + slot + D / 2 + lane * 8) = make_uint2(ck.z, ck.w);
+            *reinterpret_cast<uint2*>(c.v + slot + lane * 8) = make_uint2(cv.x, cv.y);
+            *reinterpret_cast<uint2*>(c.v + slot + D / 2 + lane * 8) = make_uint2(cv.z, cv.w);
             if (lane == 0) c.k_scale[at_scale] = sk;
             if (lane == 1) c.v_scale[at_scale] = sv;
         }
@@ -139,15 +149,26 @@ zl_cache_write_kernel(const CacheView c, const CacheBatch b, const __nv_bfloat16
 
 template <int kFormat>
 __device__ __forceinline__ uint4 dequantise(uint32_t a, uint32_t b, float scale) {
-    const uint32_t w[4] = {code_pair<kFormat, 0, 1>(a), code_pair<kFormat, 2, 3>(a), code_pair<kFormat, 0, 1>(b), code_pair<kFormat, 2, 3>(b)};
     uint32_t r[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = pack_bf16(lo_float(w[i]) * scale, hi_float(w[i]) * scale);  // one rounding, of the product
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = i < 2 ? a : b;
+        float2 x;
+        if constexpr (kFormat == ZL_CACHE_INT8) {
+            // 0x4b0000 in front of c + 128 is 2^23 + 128 + c
+            const uint32_t up = w ^ 0x80808080u;
+            const uint32_t lo = __byte_perm(up, 0x4b000000u, 0x7650 + 2 * (i & 1)), hi = __byte_perm(up, 0x4b000000u, 0x7651 + 2 * (i & 1));
+            x = add2(make_float2(__uint_as_float(lo), __uint_as_float(hi)), make_float2(-8388736.f, -8388736.f));
+        } else {
+            uint32_t p[2];
+            e4m3_half(w, p[0], p[1]);
+            x = __half22float2(*reinterpret_cast<const __half2*>(&p[i & 1]));
+        }
+        x = mul2(x, make_float2(scale, scale));
+        r[i] = pack_bf16(x.x, x.y);  // one rounding, of the product
+    }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
-
-// Of 8-bit caches two bytes are written for one that is read: 5.0 TB/s, where as many of both run at 6.2 (39,360 tokens, 12
-// heads, d 128).  Two rows a lane, for more bytes in flight, lost 4 to 10 % (short calls 2.9 -> 4.2 us).
 
 template <int D, int kFormat>
 __global__ void __launch_bounds__(kThreads)
@@ -171,26 +192,31 @@ zl_cache_read_kernel(const CacheView c, const CacheBatch b, const CacheReadParam
             if constexpr (kFormat == ZL_CACHE_BF16) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    xk[i] = *(reinterpret_cast<const uint4*>(c.k + slot + lane * 32) + i);
-                    xv[i] = *(reinterpret_cast<const uint4*>(c.v + slot + lane * 32) + i);
+                    xk[i] = *reinterpret_cast<const uint4*>(c.k + slot + i * D + lane * 16);
+                    xv[i] = *reinterpret_cast<const uint4*>(c.v + slot + i * D + lane * 16);
                 }
             } else {
                 const int64_t at = pg * c.scale_page + in * c.scale_token + head * c.scale_head;
-                const uint4 ck = *reinterpret_cast<const uint4*>(c.k + slot + lane * 16);
-                const uint4 cv = *reinterpret_cast<const uint4*>(c.v + slot + lane * 16);
+                uint2 ck[2], cv[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    ck[i] = *reinterpret_cast<const uint2*>(c.k + slot + i * (D / 2) + lane * 8);
+                    cv[i] = *reinterpret_cast<const uint2*>(c.v + slot + i * (D / 2) + lane * 8);
+                }
                 const float sk = c.k_scale[at], sv = c.v_scale[at];
-                xk[0] = dequantise<kFormat>(ck.x, ck.y, sk);
-                xk[1] = dequantise<kFormat>(ck.z, ck.w, sk);
-                xv[0] = dequantise<kFormat>(cv.x, cv.y, sv);
-                xv[1] = dequantise<kFormat>(cv.z, cv.w, sv);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    xk[i] = dequantise<kFormat>(ck[i].x, ck[i].y, sk);
+                    xv[i] = dequantise<kFormat>(cv[i].x, cv[i].y, sv);
+                }
             }
         }
     }
-    const int64_t dst = ((int64_t)row * c.n_kv_heads + head) * D + lane * kEach;
+    const int64_t dst = ((int64_t)row * c.n_kv_heads + head) * D + lane * 8;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        *(reinterpret_cast<uint4*>(p.k + dst) + i) = xk[i];
-        *(reinterpret_cast<uint4*>(p.v + dst) + i) = xv[i];
+        *reinterpret_cast<uint4*>(p.k + dst + i * (D / 2)) = xk[i];
+        *reinterpret_cast<uint4*>(p.v + dst + i * (D / 2)) = xv[i];
     }
 }
 
