@@ -223,7 +223,7 @@ zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cach
     CachedParams p{};
     if (const zl_status st = view(cache, batch, true, &p.c, &p.b)) return st;
     if (cache->n_kv_heads != attn->n_kv_heads || cache->head_dim != attn->head_dim) return ZL_ERR_INVALID_ARG;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return ZL_ERR_INVALID_ARG;
+    if (!(scale > 0.f) || !std::isfinite(scale * 1.4426950408889634f)) return ZL_ERR_INVALID_ARG;
     if (q_stride % 8 != 0 || q_stride < (int64_t)attn->n_heads * attn->head_dim) return ZL_ERR_INVALID_ARG;
     if (p.b.total_q > 0 && (!q || !o || !aligned16(q) || !aligned16(o))) return ZL_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(lse) & 3) != 0) return ZL_ERR_INVALID_ARG;

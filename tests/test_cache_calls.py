@@ -180,7 +180,7 @@ def test_attention_calls_the_library_refuses():
         return lib.zl_cached_attn_fwd(h.ptr, ctypes.byref(c or cache_desc()), ctypes.byref(b or batch_desc()), q, stride, scale, o, lse, 4096, 1 << 40, 0)
 
     assert call(c=cache_desc(n_kv_heads=4)) == INVALID and call(c=cache_desc(head_dim=128, token_stride=256, head_stride=128)) == INVALID
-    for scale in (0.0, -1.0, float("inf"), float("nan")):
+    for scale in (0.0, -1.0, float("inf"), float("nan"), 3e38):
         assert call(scale=scale) == INVALID
     assert call(o=4096) == INVALID and call(o=4096 + 4 * 512 + 496) == INVALID and call(o=4096 - 2560 + 16) == INVALID  # over the queries
     assert call(q=None) == INVALID and call(o=None) == INVALID and call(q=4104) == INVALID and call(stride=252) == INVALID
