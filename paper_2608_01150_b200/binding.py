@@ -626,15 +626,15 @@ def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, sc
            "zl_scored_attn_bwd_packed")
 
 
-def _on_gpu(what: str, t):
-    """The tensor is on the current GPU, where the call's kernels run."""
-    if not t.is_cuda or t.get_device() != _current_device():
+def _on_gpu(what: str, t, device: int):
+    """The tensor is on the current GPU (`device`), where the call's kernels run."""
+    if not t.is_cuda or t.get_device() != device:
         raise ZlError(1, f"{what} is not on the current GPU")
 
 
 def _ints(what: str, t, shape=None):
     import torch
-    if t.dtype is not torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+    if t.dtype is not torch.int32 or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ZlError(1, f"{what} must be a contiguous torch.int32 tensor" + (f" of shape {shape}" if shape is not None else ""))
 
 
@@ -660,12 +660,13 @@ class KvCache:
         """The C struct of what the attributes hold now (not to be written to); raises where they do not fit."""
         return self._look()[5]
 
-    def check(self) -> KvCacheDesc:
-        """The same for a call: the tensors are on the current GPU."""
+    def check(self) -> Tuple[KvCacheDesc, int]:
+        """The same for a call: the tensors are on the current GPU, whose number comes with it."""
         seen = self._look()
-        if not seen[0].is_cuda or seen[0].get_device() != _current_device():
+        device = seen[0].get_device()
+        if not seen[0].is_cuda or device != _current_device():
             raise ZlError(1, "KvCache: the tensors are not on the current GPU")
-        return seen[5]
+        return seen[5], device
 
     def _look(self):
         # the same tensors with the same storage and strides have passed the checks before; a state of its own per change: a
@@ -718,11 +719,11 @@ class CacheBatch:
         self._seen = (None,) * 6
         self._look(0)
 
-    def check(self, total_q: Optional[int]) -> CacheBatchDesc:
+    def check(self, total_q: Optional[int], device: int) -> CacheBatchDesc:
         """The C struct of what the attributes hold now, for a call with token tensors of total_q rows; raises where they do
-        not fit or are not on the current GPU."""
+        not fit or are not on the current GPU (`device`)."""
         seen = self._look(total_q)
-        if not seen[0].is_cuda or seen[0].get_device() != _current_device():
+        if not seen[0].is_cuda or seen[0].get_device() != device:
             raise ZlError(1, "CacheBatch: the tensors are not on the current GPU")
         return seen[5]
 
@@ -755,49 +756,52 @@ class CacheBatch:
         return CacheBatchDesc(cu.data_ptr(), lens.data_ptr(), pages.data_ptr(), _ptr(prefix), n, width, total_q, max_q)
 
 
-def _token_rows(what: str, t, heads: int, dim: int) -> int:
-    """Stride of the rows of a bf16 tensor [tokens, heads, dim] whose rows are contiguous."""
+def _token_rows(what: str, t, heads: int, dim: int, device: int) -> Tuple[int, int]:
+    """Rows of a bf16 tensor [tokens, heads, dim] whose rows are contiguous, and their stride."""
     import torch
     shape, strides = t.shape, t.stride()
     if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[1] != heads or shape[2] != dim:
         raise ZlError(1, f"{what} must be a torch.bfloat16 tensor [tokens, {heads}, {dim}]")
     if strides[2] != 1 or (heads > 1 and strides[1] != dim):
         raise ZlError(1, f"{what}: heads and elements of a token must be contiguous")
-    _on_gpu(what, t)
-    return strides[0] if shape[0] > 1 else heads * dim
+    _on_gpu(what, t, device)
+    n = shape[0]
+    return n, strides[0] if n > 1 else heads * dim
 
 
-def _packed_rows(what: str, t, heads: int, dim: int):
-    _token_rows(what, t, heads, dim)
-    if not t.is_contiguous():
-        raise ZlError(1, f"{what} must be contiguous")
+def _like(t, other, contiguous: bool) -> bool:
+    """Of the other's shape, type and device; contiguous, or of its strides."""
+    return (t.shape == other.shape and t.dtype is other.dtype and t.get_device() == other.get_device() and
+            (t.is_contiguous() if contiguous else t.stride() == other.stride()))
 
 
 def cache_write(cache: KvCache, batch: CacheBatch, k, v, stream=None):
     """zl_cache_write: the new tokens' k, v [total_q, n_kv_heads, head_dim] bf16 (slices of a packed tensor will do) go into
     their places of the cache, quantised where it holds 8 bits."""
-    c = cache.check()
-    stride = _token_rows("k", k, c.n_kv_heads, c.head_dim)
-    if v.shape != k.shape or v.stride() != k.stride() or v.dtype is not k.dtype or v.get_device() != k.get_device():
+    c, dev = cache.check()
+    n, stride = _token_rows("k", k, c.n_kv_heads, c.head_dim, dev)
+    if not _like(v, k, False):
         raise ZlError(1, "k and v must be of the same shape, strides, type and device")
-    b = batch.check(k.shape[0])
+    b = batch.check(n, dev)
     _check(_lib.zl_cache_write(ctypes.byref(c), ctypes.byref(b), k.data_ptr(), v.data_ptr(), stride, _stream_ptr(stream)), "zl_cache_write")
 
 
 def cache_read(cache: KvCache, batch: CacheBatch, cu_kv, k, v, first=None, stream=None):
     """zl_cache_read: the tokens of sequence s from position first[s] on (None: 0) into rows [cu_kv[s], cu_kv[s+1]) of the
     packed bf16 tensors k, v [total_kv, n_kv_heads, head_dim]; rows without a key become 0."""
-    c = cache.check()
-    _packed_rows("k", k, c.n_kv_heads, c.head_dim)
-    if v.shape != k.shape or v.dtype is not k.dtype or not v.is_contiguous() or v.get_device() != k.get_device():
+    c, dev = cache.check()
+    n, _ = _token_rows("k", k, c.n_kv_heads, c.head_dim, dev)
+    if not k.is_contiguous():
+        raise ZlError(1, "k must be contiguous")
+    if not _like(v, k, True):
         raise ZlError(1, "v must be contiguous, of k's shape and type, on its device")
-    b = batch.check(None)
+    b = batch.check(None, dev)
     _ints("cu_kv", cu_kv, (b.n_seqs + 1,))
-    _on_gpu("cu_kv", cu_kv)
+    _on_gpu("cu_kv", cu_kv, dev)
     if first is not None:
         _ints("first", first, (b.n_seqs,))
-        _on_gpu("first", first)
-    _check(_lib.zl_cache_read(ctypes.byref(c), ctypes.byref(b), _ptr(first), cu_kv.data_ptr(), k.shape[0], k.data_ptr(), v.data_ptr(),
+        _on_gpu("first", first, dev)
+    _check(_lib.zl_cache_read(ctypes.byref(c), ctypes.byref(b), _ptr(first), cu_kv.data_ptr(), n, k.data_ptr(), v.data_ptr(),
                               _stream_ptr(stream)), "zl_cache_read")
 
 
@@ -848,20 +852,20 @@ def cached_attn_fwd(attn: CachedAttnHandle, cache: KvCache, batch: CacheBatch, q
     """zl_cached_attn_fwd: attention of the new tokens q [total_q, n_heads, head_dim] over the cache, which holds their own keys
     already; o like q (contiguous), lse fp32 [n_heads, total_q] or None, workspace of attn.workspace_bytes."""
     import torch
-    c = cache.check()
-    stride = _token_rows("q", q, attn.n_heads, attn.head_dim)
-    if o.shape != q.shape or o.dtype is not q.dtype or not o.is_contiguous() or o.get_device() != q.get_device():
+    c, dev = cache.check()
+    n, stride = _token_rows("q", q, attn.n_heads, attn.head_dim, dev)
+    if not _like(o, q, True):
         raise ZlError(1, "o must be contiguous, of q's shape and type, on its device")
     if lse is not None:
-        if lse.dtype is not torch.float32 or tuple(lse.shape) != (attn.n_heads, q.shape[0]) or not lse.is_contiguous():
-            raise ZlError(1, f"lse must be a contiguous torch.float32 tensor [{attn.n_heads}, {q.shape[0]}]")
-        _on_gpu("lse", lse)
-    _on_gpu("workspace", workspace)
+        if lse.dtype is not torch.float32 or lse.shape != (attn.n_heads, n) or not lse.is_contiguous():
+            raise ZlError(1, f"lse must be a contiguous torch.float32 tensor [{attn.n_heads}, {n}]")
+        _on_gpu("lse", lse, dev)
+    _on_gpu("workspace", workspace, dev)
     if not workspace.is_contiguous():
         raise ZlError(1, "workspace must be contiguous")
-    b = batch.check(q.shape[0])
+    b = batch.check(n, dev)
     _check(_lib.zl_cached_attn_fwd(attn.ptr, ctypes.byref(c), ctypes.byref(b), q.data_ptr(), stride, scale, o.data_ptr(), _ptr(lse),
-                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+                                   workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)),
            "zl_cached_attn_fwd")
 
 
