@@ -342,8 +342,10 @@ zl_cached_tokens_kernel(const CachedParams p) {
             if (more) ++n_items;
         }
         for (uint32_t it = 0; it < n_items; ++it) {
-            const Item& w = sm.items[it % kItems];
             ZL_WAIT_WARP(&sm.item_done[it % kItems], (it / kItems) & 1, 1);
+            // By value: its place is prepared anew behind the next item, whose end is ordered behind this warp's o_free and behind
+            // nothing that it does after that, while finish() needs the item to the end of its join.
+            const Item w = sm.items[it % kItems];
             // ---- O = sum_w 2^(m_w - max) O_w over the streaming warps, and the same of the sums
             const bool whole = w.c_first == w.c_last;
             auto part_of = [&](int cta) { return p.part + ((int64_t)cta * 2 + (cta == w.c_first ? w.place_first : 0)) * kPartFloats<D>; };
