@@ -195,6 +195,13 @@ static __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, co
     return mbar_wait_slow(bar, parity, kWaitLimitNs, abort_flag);
 }
 
+// A store of the lanes that have something to store, without a branch: the warp stays together for the collective instructions behind it.
+__device__ __forceinline__ void store_if(bool live, void* to, const uint4& x) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\t}" ::"l"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w),
+                 "r"((uint32_t)live)
+                 : "memory");
+}
+
 // All lanes of a warp wait; the outcome is warp-uniform and the warp reconverges.
 #define ZL_WAIT_WARP(bar, parity, site)                                                                       \
     do {                                                                                                      \
@@ -806,6 +813,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                             m2[Y][b] = mx[b];
                         }
                     }
+                    __syncwarp();  // (the choice above is a lane's own)
                     if (!first) {
 #pragma unroll 1
                         for (int h = 0; h < D / 64; ++h) {
@@ -926,7 +934,6 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         for (int i = 0; i < 32; ++i) o[i] = fmaf(wt[y], __uint_as_float(r[i]), o[i]);
                     }
                 }
-                if (!row_ok) continue;
                 if (whole) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
@@ -935,12 +942,14 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                         o4.y = pack_bf16(o[i + 2] * inv, o[i + 3] * inv);
                         o4.z = pack_bf16(o[i + 4] * inv, o[i + 5] * inv);
                         o4.w = pack_bf16(o[i + 6] * inv, o[i + 7] * inv);
-                        *reinterpret_cast<uint4*>(p.o + o_at + q * 32 + i) = o4;
+                        store_if(row_ok, p.o + o_at + q * 32 + i, o4);
                     }
                 } else {
                     float4* to = reinterpret_cast<float4*>(part_of(blockIdx.x) + 2 * kTileQ) + (c0 / 4 + q * 8) * kTileQ + row;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) to[i * kTileQ] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                    for (int i = 0; i < 8; ++i)
+                        store_if(row_ok, to + i * kTileQ,
+                                 make_uint4(__float_as_uint(o[4 * i]), __float_as_uint(o[4 * i + 1]), __float_as_uint(o[4 * i + 2]), __float_as_uint(o[4 * i + 3])));
                 }
             }
             if (has_lse) {

@@ -21,3 +21,16 @@ def test_short_items_behind_items_that_are_cut(dtype, dim, group):
     for _ in range(20):
         again = attend(s, qlens, q)
         assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, INT8, E4M3])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("group,tokens", [(1, 17), (1, 131), (3, 43), (7, 20), (11, 13), (100, 1), (48, 5)])
+def test_tiles_with_rows_that_do_not_exist(dtype, dim, group, tokens):
+    """Warps that have rows of a tile and places without one, in one query tile and in two, in items that are cut and whole ones."""
+    lens, qlens = [1500, tokens + 30, tokens], [tokens] * 3
+    s = Setup(dtype, dim, 16, 2, lens)
+    s.fill()
+    q = rand(s.g, 3 * tokens + 2, 2 * group, dim, times=1.5)
+    o, lse = attend(s, qlens, q)
+    check(s, qlens, q, o, lse)
