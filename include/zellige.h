@@ -429,8 +429,8 @@ zl_status zl_scored_workspace_bytes(const zl_tasks* tasks, const zl_score* score
  *
  * zl_kv_cache: one layer's cache.
  *   k, v          device: n_pages pages of page_size tokens of n_kv_heads x head_dim elements, the elements of a row contiguous;
- *                 strides in elements, the same for k and v, multiples of 16 bytes.  [n_pages, page_size, H, d] and
- *                 [n_pages, H, page_size, d] are both such layouts.  Bases 16-byte aligned.
+ *                 strides in elements, the same for k and v, multiples of 16 bytes, below 2^35 (those of the scales below 2^32).
+ *                 [n_pages, page_size, H, d] and [n_pages, H, page_size, d] are both such layouts.  Bases 16-byte aligned.
  *   format        ZL_CACHE_BF16; ZL_CACHE_INT8 (whole numbers from -127 to 127) or ZL_CACHE_E4M3, each with one scale per
  *                 token and head: the value held is code * scale.
  *   k_scale, v_scale  device, fp32, a number for every page, token and key head, strides in elements, the same for both; NULL

@@ -34,7 +34,7 @@ zl_status view(const zl_kv_cache* cache, const zl_cache_batch* batch, bool token
     if (x.page_size < 8 || (x.page_size & (x.page_size - 1)) != 0 || x.page_size > (1 << 24)) return ZL_ERR_UNSUPPORTED;
     const int bytes = x.format == ZL_CACHE_BF16 ? 2 : 1;
     for (int64_t s : {x.page_stride, x.token_stride, x.head_stride})
-        if (s < 0 || s > (int64_t)1 << 35 || (s * bytes) % 16 != 0) return ZL_ERR_INVALID_ARG;  // (in units of 16 bytes they fit 32 bits)
+        if (s < 0 || s >= (int64_t)1 << 35 || (s * bytes) % 16 != 0) return ZL_ERR_INVALID_ARG;  // (below 2^35, in units of 16 bytes they fit 32 bits)
     for (int64_t s : {x.scale_page_stride, x.scale_token_stride, x.scale_head_stride})
         if (s < 0 || s >= (int64_t)1 << 32) return ZL_ERR_INVALID_ARG;
     if (x.n_pages > 0) {
