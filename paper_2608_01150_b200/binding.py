@@ -628,8 +628,16 @@ def scored_attn_bwd_packed(tasks: TaskHandle, score: Score, qkv, o, lse, d_o, sc
 
 def _on_gpu(what: str, t, device: int):
     """The tensor is on the current GPU (`device`), where the call's kernels run."""
-    if not t.is_cuda or t.get_device() != device:
+    if t.get_device() != device:  # (-1 of a tensor that is on none)
         raise ZlError(1, f"{what} is not on the current GPU")
+
+
+def _call_stream(stream, device: int) -> int:
+    """_stream_ptr of a call whose tensors are on the current GPU (`device`): CUDA is up, which need not be asked."""
+    if stream is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(device)
+    return _stream_ptr(stream)
 
 
 def _ints(what: str, t, shape=None):
@@ -652,36 +660,38 @@ class KvCache:
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self._seen = (None,) * 6
+        self._seen = (None,) * 3
         self.desc
 
     @property
     def desc(self) -> KvCacheDesc:
         """The C struct of what the attributes hold now (not to be written to); raises where they do not fit."""
-        return self._look()[5]
+        return self._look()[2]
 
     def check(self) -> Tuple[KvCacheDesc, int]:
         """The same for a call: the tensors are on the current GPU, whose number comes with it."""
-        seen = self._look()
-        device = seen[0].get_device()
-        if not seen[0].is_cuda or device != _current_device():
+        key, on_gpu, desc = self._look()
+        device = key[0]
+        if not on_gpu or device != _current_device():
             raise ZlError(1, "KvCache: the tensors are not on the current GPU")
-        return seen[5], device
+        return desc, device
 
     def _look(self):
-        # the same tensors with the same storage and strides have passed the checks before; a state of its own per change: a
-        # call of another thread may be reading the one before
+        # All that _read looks at (written out: calls of a function per tensor would cost as much again): as long as that is the same, so
+        # is what it makes of it.  A state of its own per change: a call of another thread may be reading the one before
         k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
-        key = (k.data_ptr(), v.data_ptr(), k.shape, k.stride(), v.stride(), k.dtype, ks is None or (ks.data_ptr(), ks.stride()),
-               vs is None or (vs.data_ptr(), vs.stride()))
+        key = (k.get_device(), k.data_ptr(), k.dtype, k.shape, k.stride(), v.data_ptr(), v.dtype, v.shape, v.stride())
+        if ks is not None:
+            key += (ks.data_ptr(), ks.dtype, ks.shape, ks.stride())
+        if vs is not None:
+            key += (vs.data_ptr(), vs.dtype, vs.shape, vs.stride())
         seen = self._seen
-        if seen[0] is not k or seen[1] is not v or seen[2] is not ks or seen[3] is not vs or seen[4] != key:
-            self._seen = seen = (k, v, ks, vs, key, self._read())
+        if seen[0] != key:
+            self._seen = seen = (key, k.is_cuda, self._read(k, v, ks, vs))
         return seen
 
-    def _read(self) -> KvCacheDesc:
+    def _read(self, k, v, ks, vs) -> KvCacheDesc:
         import torch
-        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
         fmt = {torch.bfloat16: 0, torch.int8: 1, torch.float8_e4m3fn: 2}.get(k.dtype)
         if fmt is None or v.dtype is not k.dtype:
             raise ZlError(1, "KvCache: k and v must both be torch.bfloat16, torch.int8 or torch.float8_e4m3fn")
@@ -716,31 +726,32 @@ class CacheBatch:
 
     def __init__(self, cu_q, kv_len, pages, prefix=None, max_q: int = 0):
         self.cu_q, self.kv_len, self.pages, self.prefix, self.max_q = cu_q, kv_len, pages, prefix, max_q
-        self._seen = (None,) * 6
+        self._seen = (None,) * 3
         self._look(0)
 
     def check(self, total_q: Optional[int], device: int) -> CacheBatchDesc:
         """The C struct of what the attributes hold now, for a call with token tensors of total_q rows; raises where they do
         not fit or are not on the current GPU (`device`)."""
-        seen = self._look(total_q)
-        if not seen[0].is_cuda or seen[0].get_device() != device:
+        key, on_gpu, desc = self._look(total_q)
+        if not on_gpu or key[0] != device:
             raise ZlError(1, "CacheBatch: the tensors are not on the current GPU")
-        return seen[5]
+        return desc
 
     def _look(self, total_q: Optional[int]):
         # as KvCache._look; None: the call has no token tensors, whatever was there last will do
-        cu, lens, pages, prefix = self.cu_q, self.kv_len, self.pages, self.prefix
+        cu, lens, pages, prefix, max_q = self.cu_q, self.kv_len, self.pages, self.prefix, self.max_q
         seen = self._seen
         if total_q is None:
-            total_q = 0 if seen[5] is None else seen[5].total_q
-        key = (cu.data_ptr(), lens.data_ptr(), pages.data_ptr(), pages.shape, None if prefix is None else prefix.data_ptr(),
-               self.max_q, total_q)
-        if seen[0] is not cu or seen[1] is not lens or seen[2] is not pages or seen[3] is not prefix or seen[4] != key:
-            self._seen = seen = (cu, lens, pages, prefix, key, self._read(total_q))
+            total_q = seen[2].total_q
+        key = (cu.get_device(), total_q, max_q, cu.data_ptr(), cu.dtype, cu.shape, cu.is_contiguous(), lens.data_ptr(), lens.dtype, lens.shape,
+               lens.is_contiguous(), pages.data_ptr(), pages.dtype, pages.shape, pages.is_contiguous())
+        if prefix is not None:
+            key += (prefix.data_ptr(), prefix.dtype, prefix.shape, prefix.is_contiguous())
+        if seen[0] != key:
+            self._seen = seen = (key, cu.is_cuda, self._read(cu, lens, pages, prefix, max_q, total_q))
         return seen
 
-    def _read(self, total_q: int) -> CacheBatchDesc:
-        cu, lens, pages, prefix = self.cu_q, self.kv_len, self.pages, self.prefix
+    def _read(self, cu, lens, pages, prefix, max_q, total_q: int) -> CacheBatchDesc:
         n = lens.shape[0] if lens.dim() == 1 else -1
         _ints("CacheBatch: kv_len", lens, (max(0, n),))
         _ints("CacheBatch: cu_q", cu, (n + 1,))
@@ -752,12 +763,12 @@ class CacheBatch:
         for t in (lens, pages, prefix):
             if t is not None and t.get_device() != cu.get_device():
                 raise ZlError(1, "CacheBatch: the tensors are on different devices")
-        n, width, total_q, max_q = _int32s((n, pages.shape[1], total_q, self.max_q))
+        n, width, total_q, max_q = _int32s((n, pages.shape[1], total_q, max_q))
         return CacheBatchDesc(cu.data_ptr(), lens.data_ptr(), pages.data_ptr(), _ptr(prefix), n, width, total_q, max_q)
 
 
-def _token_rows(what: str, t, heads: int, dim: int, device: int) -> Tuple[int, int]:
-    """Rows of a bf16 tensor [tokens, heads, dim] whose rows are contiguous, and their stride."""
+def _token_rows(what: str, t, heads: int, dim: int, device: int) -> Tuple[int, int, tuple, tuple]:
+    """Rows of a bf16 tensor [tokens, heads, dim] whose rows are contiguous, and their stride; the tensor's shape and strides."""
     import torch
     shape, strides = t.shape, t.stride()
     if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[1] != heads or shape[2] != dim:
@@ -766,34 +777,34 @@ def _token_rows(what: str, t, heads: int, dim: int, device: int) -> Tuple[int, i
         raise ZlError(1, f"{what}: heads and elements of a token must be contiguous")
     _on_gpu(what, t, device)
     n = shape[0]
-    return n, strides[0] if n > 1 else heads * dim
+    return n, strides[0] if n > 1 else heads * dim, shape, strides
 
 
-def _like(t, other, contiguous: bool) -> bool:
-    """Of the other's shape, type and device; contiguous, or of its strides."""
-    return (t.shape == other.shape and t.dtype is other.dtype and t.get_device() == other.get_device() and
-            (t.is_contiguous() if contiguous else t.stride() == other.stride()))
+def _like(t, other, shape: tuple, device: int, strides: Optional[tuple] = None) -> bool:
+    """Of the other's type, of its shape, on its device; of these strides, or contiguous."""
+    return (t.shape == shape and t.dtype is other.dtype and t.get_device() == device and
+            (t.is_contiguous() if strides is None else t.stride() == strides))
 
 
 def cache_write(cache: KvCache, batch: CacheBatch, k, v, stream=None):
     """zl_cache_write: the new tokens' k, v [total_q, n_kv_heads, head_dim] bf16 (slices of a packed tensor will do) go into
     their places of the cache, quantised where it holds 8 bits."""
     c, dev = cache.check()
-    n, stride = _token_rows("k", k, c.n_kv_heads, c.head_dim, dev)
-    if not _like(v, k, False):
+    n, stride, shape, strides = _token_rows("k", k, c.n_kv_heads, c.head_dim, dev)
+    if not _like(v, k, shape, dev, strides):
         raise ZlError(1, "k and v must be of the same shape, strides, type and device")
     b = batch.check(n, dev)
-    _check(_lib.zl_cache_write(ctypes.byref(c), ctypes.byref(b), k.data_ptr(), v.data_ptr(), stride, _stream_ptr(stream)), "zl_cache_write")
+    _check(_lib.zl_cache_write(ctypes.byref(c), ctypes.byref(b), k.data_ptr(), v.data_ptr(), stride, _call_stream(stream, dev)), "zl_cache_write")
 
 
 def cache_read(cache: KvCache, batch: CacheBatch, cu_kv, k, v, first=None, stream=None):
     """zl_cache_read: the tokens of sequence s from position first[s] on (None: 0) into rows [cu_kv[s], cu_kv[s+1]) of the
     packed bf16 tensors k, v [total_kv, n_kv_heads, head_dim]; rows without a key become 0."""
     c, dev = cache.check()
-    n, _ = _token_rows("k", k, c.n_kv_heads, c.head_dim, dev)
+    n, _, shape, _ = _token_rows("k", k, c.n_kv_heads, c.head_dim, dev)
     if not k.is_contiguous():
         raise ZlError(1, "k must be contiguous")
-    if not _like(v, k, True):
+    if not _like(v, k, shape, dev):
         raise ZlError(1, "v must be contiguous, of k's shape and type, on its device")
     b = batch.check(None, dev)
     _ints("cu_kv", cu_kv, (b.n_seqs + 1,))
@@ -802,7 +813,7 @@ def cache_read(cache: KvCache, batch: CacheBatch, cu_kv, k, v, first=None, strea
         _ints("first", first, (b.n_seqs,))
         _on_gpu("first", first, dev)
     _check(_lib.zl_cache_read(ctypes.byref(c), ctypes.byref(b), _ptr(first), cu_kv.data_ptr(), n, k.data_ptr(), v.data_ptr(),
-                              _stream_ptr(stream)), "zl_cache_read")
+                              _call_stream(stream, dev)), "zl_cache_read")
 
 
 class CachedAttnHandle:
@@ -853,8 +864,8 @@ def cached_attn_fwd(attn: CachedAttnHandle, cache: KvCache, batch: CacheBatch, q
     already; o like q (contiguous), lse fp32 [n_heads, total_q] or None, workspace of attn.workspace_bytes."""
     import torch
     c, dev = cache.check()
-    n, stride = _token_rows("q", q, attn.n_heads, attn.head_dim, dev)
-    if not _like(o, q, True):
+    n, stride, shape, _ = _token_rows("q", q, attn.n_heads, attn.head_dim, dev)
+    if not _like(o, q, shape, dev):
         raise ZlError(1, "o must be contiguous, of q's shape and type, on its device")
     if lse is not None:
         if lse.dtype is not torch.float32 or lse.shape != (attn.n_heads, n) or not lse.is_contiguous():
@@ -865,7 +876,7 @@ def cached_attn_fwd(attn: CachedAttnHandle, cache: KvCache, batch: CacheBatch, q
         raise ZlError(1, "workspace must be contiguous")
     b = batch.check(n, dev)
     _check(_lib.zl_cached_attn_fwd(attn.ptr, ctypes.byref(c), ctypes.byref(b), q.data_ptr(), stride, scale, o.data_ptr(), _ptr(lse),
-                                   workspace.data_ptr(), workspace.nbytes, _stream_ptr(stream)),
+                                   workspace.data_ptr(), workspace.nbytes, _call_stream(stream, dev)),
            "zl_cached_attn_fwd")
 
 

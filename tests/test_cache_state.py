@@ -2,9 +2,11 @@
 import ctypes
 
 import pytest
+import torch
 
+import paper_2608_01150_b200 as Z
 from paper_2608_01150_b200 import binding as B
-from test_cache_calls import CUDA, INVALID, batch_desc, cache_desc, no_device
+from test_cache_calls import CUDA, INVALID, batch_desc, cache_desc, no_device, pool
 
 
 # ---------------------------------------------------------------------------------------------- limits
@@ -23,3 +25,64 @@ def test_strides_fit_32_bits_in_units_of_16_bytes(fmt, name):
 def test_the_largest_strides_are_taken(name):
     lib, c, b = B.lib(), cache_desc(**{name: (1 << 35) - 8}), batch_desc()
     assert lib.zl_cache_write(ctypes.byref(c), ctypes.byref(b), 4096, 4096, 128, 0) == CUDA
+
+
+# ---------------------------------------------------------------------------------------------- changes in place
+def refused(call):
+    with pytest.raises(Z.ZlError) as e:
+        call()
+    assert e.value.status == INVALID
+
+
+def test_a_batch_follows_changes_of_shape_in_place():
+    """The address stays, the number of sequences does not."""
+    i32 = torch.int32
+    cu, lens, pages, prefix = torch.zeros(5, dtype=i32), torch.zeros(4, dtype=i32), torch.zeros(4, 3, dtype=i32), torch.zeros(4, dtype=i32)
+    b = Z.CacheBatch(cu, lens, pages, prefix)
+    now = lambda: b._look(None)[-1]  # noqa: E731
+    assert now().n_seqs == 4
+    lens.resize_(2)
+    refused(now)
+    cu.resize_(3), prefix.resize_(2)
+    refused(now)  # (the table still has four rows)
+    pages.resize_(2, 3)
+    assert now().n_seqs == 2 and now().max_pages == 3
+
+
+@pytest.mark.parametrize("name", ["cu_q", "kv_len", "pages", "prefix"])
+@pytest.mark.parametrize("what", ["shape", "type", "strides"])
+def test_a_batch_whose_tensors_no_longer_fit_is_refused(name, what):
+    i32 = torch.int32
+    b = Z.CacheBatch(torch.zeros(5, dtype=i32), torch.zeros(4, dtype=i32), torch.zeros(4, 3, dtype=i32), torch.zeros(4, dtype=i32))
+    t = getattr(b, name)
+    if what == "shape":
+        t.data = t.data[:2]
+    elif what == "type":
+        t.data = t.data.view(torch.float32)
+    else:
+        t.as_strided_(t.shape, (0,) * t.dim())
+    refused(lambda: b._look(None))
+
+
+@pytest.mark.parametrize("name", ["k", "v", "k_scale", "v_scale"])
+@pytest.mark.parametrize("what", ["shape", "type", "strides"])
+def test_a_cache_whose_tensors_no_longer_fit_is_refused(name, what):
+    c = Z.KvCache(*pool(torch.int8))
+    t = getattr(c, name)
+    before = t.data_ptr()
+    if what == "shape":
+        t.data = t.data[:3]
+    elif what == "type":
+        t.data = t.data.view(torch.uint8 if name in "kv" else torch.int32)
+    else:
+        t.as_strided_(t.shape, (1,) * t.dim())
+    assert t.data_ptr() == before
+    refused(lambda: c.desc)
+
+
+def test_a_cache_that_changes_as_a_whole_is_followed():
+    k, v, ks, vs = pool(torch.int8)
+    c = Z.KvCache(k, v, ks, vs)
+    for t in (k, v, ks, vs):
+        t.data = t.data[:3]
+    assert c.desc.n_pages == 3
