@@ -510,9 +510,10 @@ zl_status zl_cached_attn_device_status(const zl_cached_attn* attn, int32_t* code
  *   workspace  at least zl_cached_attn_workspace_bytes, 256-byte aligned
  * Q, and the keys and values inside the sequences' lengths, have to be finite; other places of the cache may hold anything.
  * P is rounded to bf16 (8-bit caches: times the value's scale, to fp16) for its product with V; everything else is fp32.
- * 8-bit caches: scales of values below 2^-90 count as 2^-90, and values are taken to be below 2^64 (beyond, small weights vanish);
- * new tokens of a sequence are multiplied together, in fp16 of one common factor: a score is off by up to 2^-40 of the largest
- * scale * sum |q_i k_i| among them beside its own rounding.
+ * 8-bit caches: scales of values below 2^-90 count as 2^-90, and values are taken to be below 2^64 (beyond, small weights vanish).
+ * Queries are multiplied in fp16, times a power of two of the largest magnitude among those that are multiplied together (at most
+ * the rows of a sequence that share a key head): below 2^-31 of it they lose bits, and a score is off by up to
+ * 2^-39 * scale * max |q| * sum_i |k_i|, that maximum over these rows, beside its own rounding.
  * Asynchronous on `stream`; captured like the other entry points. */
 zl_status zl_cached_attn_fwd(const zl_cached_attn* attn, const zl_kv_cache* cache, const zl_cache_batch* batch, const void* q,
                              int64_t q_stride, float scale, void* o, float* lse, void* workspace, size_t workspace_bytes,

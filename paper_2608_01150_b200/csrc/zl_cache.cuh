@@ -104,8 +104,9 @@ __device__ __forceinline__ void halves_apart(uint32_t w, uint32_t& p02, uint32_t
         e4m3_half(__byte_perm(w, 0u, 0x3120), p02, p13);
     }
 }
-// Queries, bf16, as fp16: times the power of two that brings the largest magnitude `big` to 2^14 .. 2^15.  What is
-// 2^-29 of it or more keeps all its bits; the rest is off by 2^-40 of it.  `back`: the factor that undoes it.
+// Queries, bf16, as fp16: times the power of two that brings the largest magnitude `big` to 2^14 .. 2^15 (below 2^-98: times 2^112).
+// What is 2^-31 of it or more keeps its 8 bits above fp16's last step of 2^-24; the rest is off by half that step, 2^-39 of
+// `big`.  `back`: the factor that undoes it.
 __device__ __forceinline__ float half_factor(float big, float& back) {
     const int e = big > 0.f ? min(max((int)(__float_as_uint(big) >> 23) - 127 - 14, -112), 113) : 0;
     back = __uint_as_float((uint32_t)(127 + e) << 23);

@@ -4,6 +4,7 @@ import ctypes
 import pytest
 import torch
 
+import cache_bounds
 import paper_2608_01150_b200 as Z
 from paper_2608_01150_b200 import binding as B
 from test_cache_calls import CUDA, INVALID, batch_desc, cache_desc, no_device, pool
@@ -86,3 +87,20 @@ def test_a_cache_that_changes_as_a_whole_is_followed():
     for t in (k, v, ks, vs):
         t.data = t.data[:3]
     assert c.desc.n_pages == 3
+
+
+# ---------------------------------------------------------------------------------------------- bounds of 8-bit caches
+@pytest.mark.parametrize("top", [2.0 ** 120, 1.0, 1.9921875 * 2.0 ** -20, 2.0 ** -98, 2.0 ** -126])
+def test_queries_in_fp16_are_off_by_2_to_the_minus_39_of_the_largest(top):
+    """All mantissas and every exponent below the largest one's; what is 2^-31 of it or more stays as it is."""
+    m = 1 + torch.arange(128, dtype=torch.float64) / 128
+    q = torch.cat([m * top * 2.0 ** -i for i in range(1, 60)]).to(torch.bfloat16)
+    q = torch.cat([torch.tensor([top], dtype=torch.bfloat16), q, -q])
+    got, q = cache_bounds.to_half(q), q.double()
+    off = (got - q).abs()
+    assert off.max() <= 2.0 ** -39 * top
+    assert (off[q.abs() >= 2.0 ** -31 * top] == 0).all()
+    if top >= 2.0 ** -80:
+        assert off.max() > 2.0 ** -40 * top  # half of it would not do
+    if top <= 2.0 ** -98:  # (the last bit of any bf16 is 2^-133, times at least 2^112 a multiple of 2^-24)
+        assert (off == 0).all()

@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+import paper_2608_01150_b200 as Z
+from cache_bounds import check8
 from test_gpu_cache import BF16, E4M3, INT8, Setup, attend, check, rand
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +36,21 @@ def test_tiles_with_rows_that_do_not_exist(dtype, dim, group, tokens):
     q = rand(s.g, 3 * tokens + 2, 2 * group, dim, times=1.5)
     o, lse = attend(s, qlens, q)
     check(s, qlens, q, o, lse)
+
+
+@pytest.mark.parametrize("dtype,dim", [(INT8, 64), (E4M3, 128)])
+@pytest.mark.parametrize("rows", [1, 12, 150])
+@pytest.mark.parametrize("times", [2.0 ** 30, 2.0 ** 36])
+def test_a_channel_of_large_queries_without_keys(dtype, dim, rows, times):
+    """A channel whose queries are far above the others' and whose keys are 0: what is lost of the others is what the largest magnitude
+    takes, not what the products would say."""
+    n = 200 + rows
+    s = Setup(dtype, dim, 16, 2, [n])
+    k, v = rand(s.g, n, 2, dim), rand(s.g, n, 2, dim)
+    k[:, :, 3] = 0.0
+    q = rand(s.g, rows, 4, dim)
+    q[:, :, 3] = times
+    Z.cache_write(s.cache, s.batch([n]), k.cuda(), v.cuda())
+    s.ref.write([0, n], [n], s.tables, k, v)
+    o, lse = attend(s, [rows], q)
+    check8(s, [rows], q, o, lse)
