@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import cache_bounds
+import cache_ref as R
 import paper_2608_01150_b200 as Z
 from paper_2608_01150_b200 import binding as B
 from test_cache_calls import CUDA, INVALID, batch_desc, cache_desc, no_device, pool
@@ -104,3 +105,32 @@ def test_queries_in_fp16_are_off_by_2_to_the_minus_39_of_the_largest(top):
         assert off.max() > 2.0 ** -40 * top  # half of it would not do
     if top <= 2.0 ** -98:  # (the last bit of any bf16 is 2^-133, times at least 2^112 a multiple of 2^-24)
         assert (off == 0).all()
+
+
+def near_pairs(dtype):
+    """Sequences of two keys whose values cancel and whose weights are nearly the same: O is small, and what rounding the weights
+    leaves is most of its error."""
+    g = torch.Generator().manual_seed(7)
+    S, heads, dim = 60, 2, 64
+    ref = R.Ref(S, 8, heads, dim, dtype)
+    k = torch.randn(2 * S, heads, dim, generator=g).to(torch.bfloat16)
+    v = torch.randn(S, heads, dim, generator=g).to(torch.bfloat16)
+    v = torch.stack([v, -v], 1).reshape(2 * S, heads, dim)
+    q = (torch.randn(S, 2 * heads, dim, generator=g) * 0.05).to(torch.bfloat16)
+    cu, tables = list(range(0, 2 * S + 1, 2)), [[i] for i in range(S)]
+    ref.write(cu, [2] * S, tables, k, v)
+    return ref, tables, k, v, q
+
+
+@pytest.mark.parametrize("dtype", [torch.int8, torch.float8_e4m3fn])
+def test_the_bounds_tell_fp16_weights_from_bf16_ones(dtype):
+    ref, tables, _, _, q = near_pairs(dtype)
+    S = len(tables)
+
+    def worst(weights):
+        O, _, bo, _ = cache_bounds.attention8(ref, list(range(S + 1)), [2] * S, tables, None, q, 0.125)
+        o = cache_bounds.attention8(ref, list(range(S + 1)), [2] * S, tables, None, q, 0.125, weights)[0]
+        return ((o.to(torch.bfloat16).double() - O).abs() / bo).max()
+
+    assert worst(None) <= 1 and worst(lambda u: u.half().double()) <= 1
+    assert worst(lambda u: u.to(torch.bfloat16).double()) > 1.5

@@ -4,6 +4,7 @@ import torch
 
 import paper_2608_01150_b200 as Z
 from cache_bounds import check8
+from test_cache_state import near_pairs
 from test_gpu_cache import BF16, E4M3, INT8, Setup, attend, check, rand
 
 pytestmark = pytest.mark.gpu
@@ -54,3 +55,53 @@ def test_a_channel_of_large_queries_without_keys(dtype, dim, rows, times):
     s.ref.write([0, n], [n], s.tables, k, v)
     o, lse = attend(s, [rows], q)
     check8(s, [rows], q, o, lse)
+
+
+@pytest.mark.parametrize("dtype", [INT8, E4M3])
+def test_weights_of_8_bit_values_keep_eleven_bits(dtype):
+    """Single tokens over two keys each, whose values cancel: within what fp16 weights leave, an eighth of what bf16 ones would."""
+    ref, tables, k, v, q = near_pairs(dtype)
+    S = len(tables)
+    s = Setup(dtype, 64, 8, 2, [2] * S)
+    s.tables, s.ref = tables, ref
+    Z.cache_write(s.cache, s.batch([2] * S), k.cuda(), v.cuda())
+    o, lse = attend(s, [1] * S, q)
+    check8(s, [1] * S, q, o, lse)
+    # as chunks: twenty new tokens that all see their two keys and no more
+    rows = q.repeat_interleave(20, 0)
+    o, lse = attend(s, [20] * S, rows, [2] * S)
+    check8(s, [20] * S, rows, o, lse, [2] * S)
+
+
+@pytest.mark.parametrize("dtype,dim,group", [(INT8, 64, 1), (INT8, 128, 5), (E4M3, 64, 8), (E4M3, 128, 2)])
+@pytest.mark.parametrize("prefix", [None, "some"])
+def test_8_bit_caches_within_the_bounds_of_what_they_keep(dtype, dim, group, prefix):
+    """Single tokens, chunks in one and in two tiles, cut items, against the bounds of exact codes and fp16 weights."""
+    qlens = [1, 1, 3, 20, 150, 300, 1]
+    lens = [40, 900, 60, 500, 150, 2000, 3000]
+    s = Setup(dtype, dim, 32, 2, lens)
+    s.fill()
+    prefix = None if prefix is None else [0, 5, 60, 490, 2 ** 31 - 1, 7, 1]
+    q = rand(s.g, sum(qlens), 2 * group, dim, times=1.5)
+    for times in (1.0, 0.05):  # (small scores: what rounds the weights is most of the bound)
+        x = (q.float() * times).to(BF16)
+        o, lse = attend(s, qlens, x, prefix)
+        check8(s, qlens, x, o, lse, prefix)
+
+
+@pytest.mark.parametrize("dtype", [INT8, E4M3])
+@pytest.mark.parametrize("rows", [1, 12, 60, 300])
+def test_values_far_apart_within_the_bounds_of_what_they_keep(dtype, rows):
+    """One token's values are 2^20 times the others' and looked at a little, one head's are 2^-60 times, one row of values is 0."""
+    n, dim = 300, 64
+    s = Setup(dtype, dim, 16, 2, [n])
+    k, v = rand(s.g, n, 2, dim), rand(s.g, n, 2, dim)
+    q = rand(s.g, rows, 4, dim).abs()
+    k[17] = -2.0
+    v[17] *= 2.0 ** 20
+    v[:, 1] *= 2.0 ** -60
+    v[40] = 0.0
+    Z.cache_write(s.cache, s.batch([n]), k.cuda(), v.cuda())
+    s.ref.write([0, n], [n], s.tables, k, v)
+    o, lse = attend(s, [rows], q, [n])
+    check8(s, [rows], q, o, lse, [n])
