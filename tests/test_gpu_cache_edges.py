@@ -2,10 +2,11 @@
 import pytest
 import torch
 
+import cache_ref as R
 import paper_2608_01150_b200 as Z
 from cache_bounds import check8
 from test_cache_state import near_pairs
-from test_gpu_cache import BF16, E4M3, INT8, Setup, attend, check, rand
+from test_gpu_cache import BF16, E4M3, INT8, Setup, attend, check, i32, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +106,51 @@ def test_values_far_apart_within_the_bounds_of_what_they_keep(dtype, rows):
     s.ref.write([0, n], [n], s.tables, k, v)
     o, lse = attend(s, [rows], q, [n])
     check8(s, [rows], q, o, lse, [n])
+
+
+@pytest.mark.parametrize("dtype", [BF16, INT8, E4M3])
+def test_chunks_then_tokens_are_the_definitions_and_the_engines(dtype):
+    """A prompt in chunks and then token by token, each step over what the steps before it wrote, against the definition; and the engine's masked
+    attention of the whole sequence over what is read back, a rounding to bf16 away from it: 2^-8 of every key in a score
+    (M = scale * sum |q||k| of its row, weights by a factor of e^(2 * 2^-8 M)) and of every value."""
+    H, dim, total, prefix = 4, 64, 333, 50
+    s = Setup(dtype, dim, 16, H, [total])
+    q, k, v = (rand(s.g, total, H, dim) for _ in range(3))
+    qd, kd, vd = q.cuda(), k.cuda(), v.cuda()
+    h = Z.build_cached_attn(H, H, dim)
+    ws = torch.empty(h.workspace_bytes, dtype=torch.uint8, device="cuda")
+    o, lse = torch.empty_like(qd), []
+    at = 0
+    for n in [50, 130, 64, 1, 3] + [1] * 85:
+        b = s.batch([n], lens=[at + n], prefix=[prefix])
+        Z.cache_write(s.cache, b, kd[at:at + n], vd[at:at + n])
+        part = torch.empty(H, n, device="cuda")
+        Z.cached_attn_fwd(h, s.cache, b, qd[at:at + n], dim ** -0.5, o[at:at + n], part, ws)
+        lse.append(part)
+        at += n
+    assert at == total
+    held = [torch.empty_like(kd) for _ in "kv"]
+    Z.cache_read(s.cache, s.batch([0]), i32([0, total]), held[0], held[1])
+    t = Z.build_tasks([0, total], [], total, total, H, dim)
+    t.set_positions([prefix])
+    o2, lse2 = torch.empty_like(qd), torch.empty(H, total, device="cuda")
+    Z.scored_attn_fwd(t, Z.Score(masked=True), qd, held[0], held[1], dim ** -0.5, o2, lse2)
+    torch.cuda.synchronize()
+    s.ref.write([0, total], [total], s.tables, k, v)
+    lse = torch.cat(lse, 1).cpu()
+    if dtype is BF16:
+        check(s, [total], q, o.cpu(), lse, [prefix])
+    else:
+        check8(s, [total], q, o.cpu(), lse, [prefix])
+    O, L, bo, bl = R.attention(s.ref, [0, total], [total], s.tables, [prefix], q, dim ** -0.5)
+    if dtype is not BF16:
+        _, K, V = s.ref.held(0, [total], s.tables)
+        seen = torch.arange(total)[None, :] < torch.arange(1, total + 1).clamp(min=prefix)[:, None]
+        for j in range(H):
+            x = (q[:, j].double() @ K[:, j].T * dim ** -0.5).masked_fill(~seen, -torch.inf)
+            A = torch.softmax(x, 1) @ V[:, j].abs()
+            off = 2.0 ** -8 * (q[:, j].double().abs() @ K[:, j].abs().T * dim ** -0.5 * seen).amax(1)
+            bo[:, j] += torch.expm1(2 * off)[:, None] * (A + O[:, j].abs()) + 2.0 ** -8 * A
+            bl[j] += off
+    assert ((o2.cpu().double() - O).abs() <= bo).all() and ((lse2.cpu().double() - L).abs() <= bl).all()
+    assert not (O.abs() <= bo).all(-1).any()  # (no row would pass as zeros)
