@@ -154,3 +154,28 @@ def test_chunks_then_tokens_are_the_definitions_and_the_engines(dtype):
             bl[j] += off
     assert ((o2.cpu().double() - O).abs() <= bo).all() and ((lse2.cpu().double() - L).abs() <= bl).all()
     assert not (O.abs() <= bo).all(-1).any()  # (no row would pass as zeros)
+
+
+@pytest.mark.parametrize("dtype,exponents", [(INT8, 9), (E4M3, 20)])
+@pytest.mark.parametrize("times", [1.0, 2.0 ** -66, 2.0 ** 80, 2.0 ** -100])
+def test_every_quotient_of_a_number_by_a_scale(dtype, exponents, times):
+    """All mantissas of a row's largest number, and of the others with every exponent that can reach a code: codes and scales bit for bit
+    (times: powers of two within and beyond what the fast quotient takes)."""
+    m = 1 + torch.arange(128, dtype=torch.float64) / 128
+    x = torch.cat([m * 2.0 ** -e for e in range(exponents)] + [torch.zeros(64)])
+    rows = []
+    for big in m:
+        y = x[x <= big]
+        y = torch.cat([y, y.new_zeros(-len(y) % 63)]).view(-1, 63)
+        y[:, 1::2] *= -1
+        rows.append(torch.cat([big.expand(len(y), 1), y], 1))
+    rows = (torch.cat(rows) * times).to(BF16)[:, None]
+    n = len(rows)
+    s = Setup(dtype, 64, 16, 1, [n])
+    Z.cache_write(s.cache, s.batch([n]), rows.cuda(), (-rows).cuda())
+    code, scale = R.quantise(rows)(dtype)
+    table = i32(s.tables[0]).long()
+    for pool, got, sign in zip(s.pools, s.scales, (1.0, -1.0)):
+        held = pool.view(torch.uint8)[table].view(dtype).float().reshape(-1, 64)[:n].cpu().double()
+        assert torch.equal(held, sign * code[:, 0])
+        assert torch.equal(got[table].reshape(-1)[:n].cpu(), scale[:, 0])
