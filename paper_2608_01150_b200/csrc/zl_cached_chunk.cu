@@ -83,9 +83,10 @@ struct ChunkSmem {
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
     uint64_t k_codes[kCodes ? kStages : 1], v_codes[kCodes ? kStages : 1], codes_read;
     uint64_t s_full[2], p_half[2][2], o_full[2], tile_full[kMaskRing];
-    uint64_t stat_full, item_full[kItems], item_empty[kItems];
+    uint64_t stat_full, item_full[kItems], item_empty[kItems], drained;
     int64_t scan[16], start_base, total;
     int32_t start_seq;
+    uint32_t q_loads, k_loads, v_loads;  // asked for so far (the producer's count)
     uint32_t tmem_base;
     volatile int32_t abort_flag;
 };
@@ -195,6 +196,12 @@ static __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, co
     return mbar_wait_slow(bar, parity, kWaitLimitNs, abort_flag);
 }
 
+// Behind an expired wait: at most a second more for what the CTA itself has under way.
+static __device__ __noinline__ void wait_drained(uint64_t* bar, uint32_t parity) {
+    const int32_t go_on = 0;
+    mbar_wait(bar, parity, 1000000000ull, &go_on);
+}
+
 // A store of the lanes that have something to store, without a branch: the warp stays together for the collective instructions behind it.
 __device__ __forceinline__ void store_if(bool live, void* to, const uint4& x) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p st.global.v4.b32 [%0], {%1, %2, %3, %4};\n\t}" ::"l"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w),
@@ -281,10 +288,12 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
         }
         for (int s = 0; s < kMaskRing; ++s) mbar_init(&sm.tile_full[s], kCodes ? 128 : 1);
         mbar_init(&sm.stat_full, 256);
+        mbar_init(&sm.drained, 1);
         for (int i = 0; i < kItems; ++i) {
             mbar_init(&sm.item_full[i], 1);
             mbar_init(&sm.item_empty[i], kCodes ? 14 : 10);  // warps that read it
         }
+        sm.q_loads = sm.k_loads = sm.v_loads = 0;
         sm.abort_flag = 0;
         fence_mbar_init();
         prefetch_tmap(&tm_q);
@@ -374,9 +383,12 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             uint32_t item_cnt = 0, kv_cnt = 0;
             // (entries of the table: what they mean is asked a tile later, when they are there)
             auto page_of = [&](const Item& w, int32_t pos) { return has_rows && pos < w.keys ? page_entry(p.b, p.c, w.s, pos) : -1; };
-            auto load = [&](const Item& w, uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, int32_t pg, int32_t pos) {
+            auto load = [&](const Item& w, uint8_t* dst, const CUtensorMap* tm, uint64_t* bar, uint32_t* count, uint32_t c, int32_t pg, int32_t pos) {
                 const uint32_t n = __popc(__ballot_sync(0xffffffffu, pg >= 0));
-                if (lane == 0) mbar_arrive_expect_tx(bar, n * box * (kCodes ? D : D * 2));
+                if (lane == 0) {
+                    *count = c + 1;
+                    mbar_arrive_expect_tx(bar, n * box * (kCodes ? D : D * 2));
+                }
                 __syncwarp();
                 if (pg >= 0) {
                     const int32_t in = pos & (page - 1);
@@ -395,6 +407,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                 ++item_cnt;
                 if (lane == 0) {
                     const int q_tiles = w.two ? 2 : 1;
+                    sm.q_loads = item_cnt;
                     mbar_arrive_expect_tx(&sm.q_full, q_tiles * tile_tokens * p.group * D * 2);
                     for (int x = 0; x < q_tiles; ++x)
                         for (int b = 0; b < kBoxes; ++b)
@@ -420,12 +433,12 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
                                 __syncwarp();
                                 if (lane == 0) mbar_arrive(&sm.tile_full[c % kMaskRing]);
                             }
-                            load(w, sm.k[st], &tm_k, kCodes ? &sm.k_codes[st] : &sm.k_full[st], pg_k, key0 + row);
+                            load(w, sm.k[st], &tm_k, kCodes ? &sm.k_codes[st] : &sm.k_full[st], &sm.k_loads, c, pg_k, key0 + row);
                         }
                         if (j > 0) {
                             const uint32_t c = kv_cnt + j - 1, st = c % kStages;
                             ZL_WAIT_WARP(&sm.v_empty[st], ((c / kStages) & 1) ^ 1, 3);
-                            load(w, sm.v[st], &tm_v, kCodes ? &sm.v_codes[st] : &sm.v_full[st], pg_v, key0 - kTileKV + row);
+                            load(w, sm.v[st], &tm_v, kCodes ? &sm.v_codes[st] : &sm.v_full[st], &sm.v_loads, c, pg_v, key0 - kTileKV + row);
                         }
                         pg_v = pg_k;
                         pg_k = valid_page(p.c, pg_next);
@@ -969,6 +982,22 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
 teardown:
     tc_fence_before();
     __syncthreads();
+    if (sm.abort_flag) {
+        // A wait has expired: copies and products that are still under way have to end before shared memory and TMEM are given up.
+        if (warp == 0) {
+            const uint32_t q_loads = sm.q_loads, k_loads = sm.k_loads, v_loads = sm.v_loads;
+            if (q_loads > 0) wait_drained(&sm.q_full, (q_loads - 1) & 1);
+            for (uint32_t i = 0; i < kStages; ++i) {  // the last load into each stage
+                if (k_loads > i) wait_drained(kCodes ? &sm.k_codes[(k_loads - 1 - i) % kStages] : &sm.k_full[(k_loads - 1 - i) % kStages], ((k_loads - 1 - i) / kStages) & 1);
+                if (v_loads > i) wait_drained(kCodes ? &sm.v_codes[(v_loads - 1 - i) % kStages] : &sm.v_full[(v_loads - 1 - i) % kStages], ((v_loads - 1 - i) / kStages) & 1);
+            }
+        } else if (warp == 1) {
+            if (elect_one()) mma_commit(&sm.drained);
+            __syncwarp();
+            wait_drained(&sm.drained, 0);
+        }
+        __syncthreads();
+    }
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
