@@ -478,12 +478,13 @@ typedef struct {
 zl_status zl_cache_write(const zl_kv_cache* cache, const zl_cache_batch* batch, const void* k, const void* v,
                          int64_t row_stride, void* stream);
 
-/* zl_cache_read -- rows of the cache as packed bf16, e.g. as KV-space of the other entry points.
+/* zl_cache_read -- rows of the cache as packed bf16, e.g. as KV-space of the other entry points (which want as many key heads as
+ * query heads).
  *   cu_kv    device, [n_seqs + 1], non-decreasing: rows [cu_kv[s], cu_kv[s+1]) of k and v receive the tokens of sequence s
  *            from position first[s] on (first: device, [n_seqs]; NULL = 0 for all).  Rows without a key (positions outside
  *            [0, kv_len), pages without keys) are set to 0; rows of no sequence are left as they are.
  *   k, v     [total_kv, n_kv_heads, head_dim] bf16, contiguous, 16-byte aligned.
- * cu_q, prefix, total_q and max_q of the batch are not used.  8-bit values are rounded to bf16 once. */
+ * cu_q, prefix, total_q and max_q of the batch are not used.  8-bit values: code * scale is rounded to fp32, and that to bf16. */
 zl_status zl_cache_read(const zl_kv_cache* cache, const zl_cache_batch* batch, const int32_t* first, const int32_t* cu_kv,
                         int32_t total_kv, void* k, void* v, void* stream);
 

@@ -3,12 +3,12 @@
 // A row (token, key head) of 64 or 128 elements belongs to four or eight lanes, sixteen elements each, keys and values together:
 // the largest magnitude of a row is two or three shuffles away.  A lane has eight neighbours in either half of the row, so that
 // every access of a warp covers whole sectors of 32 bytes (with its sixteen side by side, half sectors were stored: reading
-// 39,360 tokens, 12 heads, d 128, from 8 bits took 71 us, now 56).  Where the row lies in the cache follows from the batch: a
+// 37,920 tokens, 12 heads, d 128, from 8 bits took 71 us, now 56).  Where the row lies in the cache follows from the batch: a
 // binary search in cu_q (or cu_kv), whose few entries stay in L1, and one entry of the page table.  When writing, the rows' own
 // loads run ahead of that search.  Blocks of four warps: registers leave room for 36 warps that write, for 32 in blocks of eight
 // (56 -> 52 us for 32,760 tokens); of two, the number of blocks becomes the limit (54).
-// Measured, 12 heads, d 128: 32,760 tokens written in int8 51 us (6.0 TB/s), in e4m3 50; 39,360 tokens read from either 56 us
-// (6.3 TB/s), from bf16 72 (6.5).
+// Measured, 12 heads, d 128: 32,760 tokens written in int8 51 us (6.0 TB/s; 56 in a run of seconds), in e4m3 50 (55), in bf16 63
+// (6.4 TB/s); 37,920 tokens read from either 56 us (6.3 TB/s), from bf16 72 (6.5).
 #include "zl_cache.cuh"
 
 namespace zl {
@@ -167,7 +167,7 @@ __device__ __forceinline__ uint4 dequantise(uint32_t a, uint32_t b, float scale)
             x = __half22float2(*reinterpret_cast<const __half2*>(&p[i & 1]));
         }
         x = mul2(x, make_float2(scale, scale));
-        r[i] = pack_bf16(x.x, x.y);  // one rounding, of the product
+        r[i] = pack_bf16(x.x, x.y);  // (the product is rounded to fp32, and that to bf16)
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }

@@ -20,10 +20,11 @@
 //                us, 1560 tokens over 9,750 int8 keys.)
 // An item that lies in several CTAs leaves its parts in the workspace, and a second launch joins them, in the order of the CTAs: a
 // part is 133 KB, and one CTA alone took 20 us to join the six parts of 256 rows over 8,700 keys.
-// Measured, d 128: 1560 tokens over 34,320 keys, 40 query heads over 8: bf16 1050 TFLOP/s (1662 is what products alone reach), e4m3
-// 880, int8 790; 512 tokens behind 8,190, 12 heads: bf16 45 us, 8 bits 57.  A step is bound by its softmax: 1,024 clocks of
-// exponentials a tile, with two warps to a scheduler, both at the same place; beside them the maximum before, the way of S and P
-// through tensor memory, and the scales.  (Part of the exponentials by multiply-adds: bf16 no faster, 8 bits 4 to 22 % slower; S of
+// Measured, d 128: 1560 tokens over 34,320 keys, 40 query heads over 8: bf16 1040 TFLOP/s (1662 is what products alone reach), e4m3
+// 870, int8 860 (in a run of seconds, whose clocks fall under the power cap: 920, 820, 800); 512 tokens behind 8,190, 12 heads: bf16
+// 45 us, 8 bits 57.  A step has 1,024 clocks of exponentials a tile and as many of products, but fills no pipe (special functions
+// and tensor cores at 30 to 42 %): there are two warps to a scheduler, both at the same place, so that the load of S, the maximum,
+// the scales, the store of P and its wait are all seen beside the exponentials.  (Part of the exponentials by multiply-adds: bf16 no faster, 8 bits 4 to 22 % slower; S of
 // the next step asked for early: bf16 no faster, 8 bits without the registers for it.)
 #include <type_traits>
 
@@ -587,7 +588,7 @@ zl_cached_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
             ZL_ITEM_DONE
         }
     } else if (kCodes && warp >= 12) {
-        // ------------------------------------------------------------------ codes to bf16
+        // ------------------------------------------------------------------ codes to fp16
         reg_dec<80>();
         if constexpr (kCodes) {
             const int t = threadIdx.x - 384;

@@ -21,8 +21,9 @@
 //   * an item that lies in several CTAs is joined by the one that finishes last, in the order of the CTAs, so that results do
 //     not depend on which that is.
 // Measured, d 128: one token each of 64 sequences of up to 8192 keys, 40 query heads over 8: bf16 160 us (6.3 TB/s of 6.4), e4m3
-// 106 (5.0); one token over 75,600 int8 keys, 12 heads: 52 us (4.6 TB/s).  With 8-bit codes the warps' own chains bound it
-// (conversion, products, softmax; 1.5 of 4 instructions a clock with 14 warps, whose registers and rings fill the SM).
+// 103 (5.1; 112 in a run of seconds, whose clocks fall); one token over 75,600 int8 keys, 12 heads: 48 to 51 us (4.7 to 5.0 TB/s).
+// With 8-bit codes the warps' own chains bound it (conversion, products, softmax; 1.5 of 4 instructions a clock with 14 warps,
+// whose registers and rings fill the SM; nothing is above 55 %).
 #include "zl_cache.cuh"
 
 namespace zl {
@@ -125,7 +126,7 @@ __device__ __forceinline__ void mma16h(float (&c)[4], uint32_t a0, uint32_t a1, 
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Byte offset of 16-byte chunk `chunk` of row `row` in a 16-row matrix: chunks are exchanged within lines of 128 bytes so that
+// Byte offset of 16-byte chunk `chunk` of row `row` in a matrix: chunks are exchanged within lines of 128 bytes so that
 // the eight rows of an 8x8 matrix lie on different banks.
 template <int kRowBytes>
 __device__ __forceinline__ uint32_t swizzled(int row, int chunk) {
@@ -457,10 +458,10 @@ zl_cached_tokens_kernel(const CachedParams p) {
         const uint32_t k_at = swizzled<kRowBytes>(lane & 15, lane >> 4);
         const uint32_t v_at = kCodes ? k_at : swizzled<kRowBytes>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1);
 
-        // ---- copies: this warp's 16 keys of every tile of every item, kStages - 1 steps ahead of their use
+        // ---- copies: this warp's kKeys keys of every tile of every item, kStages - 1 steps ahead of their use
         uint32_t f_item = 0, f_stage = 0;
         int32_t f_tile = 0, f_end = 0;  // the next step's tile, the item's last; f_end < 0: no more items
-        int32_t f_page = -1;            // table entry of this lane's key (key lane % 16) of the next step, looked up a step ahead
+        int32_t f_page = -1;            // table entry of this lane's key (key lane % kKeys) of the next step, looked up a step ahead
         // the item's: keys, row of the page table, where its head lies in a token (16 bytes; elements of the scales)
         int32_t f_keys = 0;
         const int32_t* f_pages = nullptr;
